@@ -299,6 +299,144 @@ int qsr_train_host(const qsr_config *cfg, const float *theta0_host, const float 
                    void *workspace_dev, int64_t workspace_bytes, int64_t t_end, void *cuda_stream,
                    int64_t *round_start, int64_t *round_len, int64_t cap, int64_t *n_rounds, int64_t *launches);
 
+/* ---- lists of tensors ---------------------------------------------------------------------------------- */
+
+/*
+ * The optimizer step and the round end over a model's own tensors, wherever they lie, instead of over [K, P] slabs: AdamW
+ * (OPT of Eq. 1 as at qsr_config) on bf16, fp16 or fp32 parameters and gradients with fp32 or 8-bit states, and the
+ * All-Reduce line of Algorithm 2 over K copies of the same tensors.  A list is made once from the tensors' addresses and
+ * used every step; all tensors are handled by one launch (three with clipping on).
+ *
+ * Per element, with g = grad_scale * grad (times the worker's clipping factor) and everything in fp32:
+ *   m <- m + (1-beta1)*(g - m);  v <- v + (1-beta2)*(g*g - v);
+ *   theta <- theta - (lr*weight_decay*wd_scale*theta + lr/(1-beta1^n) * m / (sqrt(v)/sqrt(1-beta2^n) + eps)).
+ * theta is rounded once to the parameter's type and once, from the same fp32 value, to the working copy's type.
+ *
+ * QSR_STATES_E4M3 holds 256 consecutive elements of a tensor (its last block may be shorter) as 8-bit floats times one
+ * fp32 scale: m as codes of m / scale, and v as codes of sqrt(v) / scale (the root needs half the range of v, so that a block
+ * can span a factor of 2^35 in v), scale = fl(amax * fl(1/448)) with amax the block's largest finite magnitude; codes are
+ * fl(x * fl(1/scale)) rounded to nearest even, saturating at 448.  A positive sqrt(v) never becomes 0 (its smallest code is
+ * 2^-9), because a vanished denominator would turn a small m into a huge step.  A block whose amax is below 2^-100 is
+ * stored as zeros.  The scale is a full fp32 number, not a power of two, so that the largest element of a block decays as it
+ * would in fp32 and takes the others along; three mantissa bits alone would hold 0.999*v at v.  The update itself uses the new
+ * m and v before they are rounded to 8 bits.  A NaN in one element stays in that element.
+ *
+ * Tensors are worker-major: entry k*(n_tensors/workers) + j is tensor j of worker k, and the same j has the same numel,
+ * param_type and copy_type for every worker.  Any element alignment works; the fast path needs each tensor of an entry
+ * aligned to eight of its elements (what allocators give), or, with fp32 states, all of them equally far from that.
+ */
+enum { QSR_F32 = 0, QSR_BF16 = 1, QSR_F16 = 2, QSR_NONE = -1 };
+enum { QSR_STATES_F32 = 0, QSR_STATES_E4M3 = 1 };
+
+typedef struct qsr_list qsr_list; /* opaque; host memory owned by the library */
+
+/* One tensor: DEVICE pointers to `numel` consecutive elements each (NULL is accepted where numel = 0). */
+typedef struct qsr_tensor {
+    void *param;          /* param_type                                                                          */
+    void *copy;           /* copy_type: written by every step and synchronization; NULL where QSR_NONE           */
+    const void *grad;     /* grad_type; may be NULL until qsr_list_set_grads                                     */
+    void *m, *v;          /* float, or E4M3 bytes (v: the codes of sqrt(v))                                      */
+    float *m_scale;       /* E4M3: ceil(numel / 256) floats, otherwise NULL                                      */
+    float *v_scale;
+    int64_t numel;
+    int32_t param_type;   /* QSR_F32, QSR_BF16 or QSR_F16                                                        */
+    int32_t grad_type;
+    int32_t copy_type;    /* the same, or QSR_NONE                                                               */
+    float wd_scale;       /* factor on the weight decay                                                          */
+} qsr_tensor;
+
+typedef struct qsr_list_config {
+    int32_t n_tensors;    /* entries, a multiple of workers                                                      */
+    int32_t workers;      /* K                                                                                   */
+    int32_t states;       /* QSR_STATES_*                                                                        */
+    int32_t reserved;     /* 0                                                                                   */
+    double beta1, beta2, eps, weight_decay;
+    double clip_norm;     /* > 0 and finite: each worker's gradients are scaled by min(1, clip_norm / (norm + 1e-6)), */
+                          /* norm over all its tensors, as at qsr_set_grad_clip; otherwise off                   */
+    float *grad_norm;     /* device [workers] or NULL: the norms before clipping, written when clipping is on    */
+} qsr_list_config;
+
+/* Bytes of device workspace for a list of tensors of these sizes (host array).  Negative qsr_status on error. */
+int64_t qsr_list_workspace_bytes(const int64_t *numel_host, int32_t n_tensors, int32_t workers);
+
+/* Makes a list over caller-owned tensors.  tensors_host is a host array of cfg->n_tensors entries, read during the call
+ * only.  workspace_dev: qsr_list_workspace_bytes bytes of device memory, 256-byte aligned, borrowed until
+ * qsr_list_destroy; it is filled by copies enqueued on cuda_stream, on which all later work of the list is enqueued too.
+ * QSR_EINVAL: NULL, unknown type, numbers that are not finite, betas outside [0, 1), sizes or types that differ between
+ * workers, or a written range that overlaps any other range of the list (tied weights: list them once); QSR_EALIGN: a pointer
+ * not aligned to its element; QSR_ERANGE: workspace too small.  No tensor is written. */
+int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor *tensors_host, void *workspace_dev,
+                    int64_t workspace_bytes, void *cuda_stream);
+
+/* Frees the list (host memory only).  NULL is accepted. */
+int qsr_list_destroy(qsr_list *list);
+
+/* New gradient addresses (host array of n_tensors device pointers, read during the call), same types: for training loops
+ * whose gradients are allocated anew every step.  One small copy on the stream; asynchronous. */
+int qsr_list_set_grads(qsr_list *list, const void *const *grads_host);
+
+/* One AdamW step of every tensor, formula above; n >= 1 counts the steps the states have seen (t + 1 - t_state_origin),
+ * lr is the learning rate of this step (qsr_config_learning_rate gives the schedules').  grad_scale multiplies every
+ * gradient first (1 / loss scale, or 1 / accumulated batches).  QSR_ESTATE: no gradients set, or another device than the
+ * list's is current.  Asynchronous. */
+int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale);
+
+/* End of a round (All-Reduce line of Algorithm 2) over the list's K workers: every parameter becomes
+ * (sum over k = 0..K-1 in fp32) / K, rounded once to its type; working copies are written from the same fp32 value.
+ * state_sync: QSR_STATE_KEEP leaves m and v alone; QSR_STATE_AVERAGE replaces them by their means (8-bit states: the means
+ * of m and of v, rounded to 8 bits once, the same codes for every worker); QSR_STATE_RESET zeroes them -- the caller's
+ * next step then has n = 1.  One launch, two in RESET mode; asynchronous. */
+int qsr_list_sync(qsr_list *list, int32_t state_sync);
+
+/* Kernel launches issued through this list so far. */
+int64_t qsr_list_launch_count(const qsr_list *list);
+
+/* ---- log probabilities of given tokens ----------------------------------------------------------------- */
+
+/*
+ * What turns a model's logits into the loss and into the gradient that a step is given (Sample() and back-propagation
+ * in Algorithm 2 start here for a model that predicts tokens or classes).  For each row x[0..vocab) of logits with its
+ * token y, tau = inv_temperature, M = max x, S = sum_j exp(tau*(x_j - M)), p_j = exp(tau*(x_j - M))/S:
+ *   logprob = tau*(x_y - M) - ln S;   entropy H = -sum_j p_j ln p_j (natural log);   row_stats = (M, ln S);
+ *   top_logprob / top_token: the n_top largest logits in descending order, ties to the lowest index, and their log
+ *   probabilities (no gradient flows through these).
+ * Gradient of  sum_r d_logprob[r]*logprob[r] + d_entropy[r]*H[r]  with respect to the logits:
+ *   d_logits[j] = tau * ( d_logprob*([j = y] - p_j) - d_entropy*p_j*(ln p_j + H) ),  rounded once to the logits' type.
+ * Logits of -inf are masked tokens: p = 0 and no gradient.  A row with nothing but -inf: logprob -inf, H = 0, top_logprob
+ * -inf (tokens 0, 1, ...), gradient 0.  A token < 0 marks a row without a score: logprob 0 and no d_logprob term.  A token
+ * >= vocab, a NaN or a +inf in the row: NaN.  Sums are kept in fp32, (x - M) is formed before it is scaled, so rows that
+ * hold the type's lowest value are treated like any other.
+ */
+typedef struct qsr_logprob_args {
+    const void *logits;      /* device, logits_type, [rows, row_stride], any element alignment                  */
+    const int64_t *tokens;   /* device [rows]                                                                    */
+    int64_t rows, vocab, row_stride;   /* 0 <= rows < 2^28, 1 <= vocab < 2^31, vocab <= row_stride (elements)    */
+    int32_t logits_type;     /* QSR_F32, QSR_BF16 or QSR_F16                                                     */
+    int32_t n_top;           /* 0..QSR_MAX_TOP, at most vocab                                                    */
+    double inv_temperature;  /* > 0, finite                                                                      */
+    float *logprob;          /* device [rows]; output                                                            */
+    float *entropy;          /* device [rows] or NULL; output (an input of the _grad call with d_entropy)        */
+    float *row_stats;        /* device [rows, 2] or NULL; output (an input of the _grad call), 8-byte aligned    */
+    float *top_logprob;      /* device [rows, n_top]; output                                                     */
+    int64_t *top_token;      /* device [rows, n_top]; output                                                     */
+    const float *d_logprob;  /* device [rows] or NULL (no such term)                                             */
+    const float *d_entropy;  /* device [rows] or NULL                                                            */
+    void *d_logits;          /* device, logits_type, [rows, d_row_stride]: output; may be the logits themselves  */
+    int64_t d_row_stride;    /* vocab <= d_row_stride; equal to row_stride if d_logits is logits                 */
+} qsr_logprob_args;
+
+#define QSR_MAX_TOP 32
+
+/* The forward quantities, and, if d_logits is not NULL, the gradient in the same pass over the logits (for losses whose
+ * d_logprob and d_entropy are known beforehand, such as cross entropy).  No context; one launch on cuda_stream (none for
+ * rows = 0); asynchronous. */
+int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream);
+
+/* The gradient by itself, for losses whose d_logprob depends on logprob: reads logits, tokens, row_stats (and entropy if
+ * d_entropy is given) of an earlier qsr_token_logprobs call, writes d_logits.  n_top, logprob and the top arrays are
+ * ignored.  One launch; asynchronous. */
+int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream);
+
 /* ---- test hook ---------------------------------------------------------------------------------------- */
 
 /* The two halves of the Box-Muller transform that turns generator words into the synthetic gradient's noise (the

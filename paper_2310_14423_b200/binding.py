@@ -24,11 +24,16 @@ STATE = {"keep": 0, "average": 1, "reset": 2}
 
 QSR_OK, QSR_EINVAL, QSR_EALIGN, QSR_ECUDA, QSR_ERANGE, QSR_ESTATE = 0, -1, -2, -3, -4, -5
 QSR_STATIC_SCRATCH_FLOATS = 1 << 20
+QSR_MAX_TOP = 32
+STATES = {"f32": 0, "e4m3": 1}
+DTYPE = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}     # QSR_F32, QSR_BF16, QSR_F16
+QSR_NONE = -1
 
 EXPORTS = ("qsr_config_check", "qsr_row_stride_hint", "qsr_config_learning_rate", "qsr_config_round_length", "qsr_config_schedule",
            "qsr_workspace_bytes", "qsr_init", "qsr_destroy", "qsr_round_length", "qsr_set_tensor_table", "qsr_clip_workspace_floats", "qsr_set_grad_clip", "qsr_set_params", "qsr_local_step",
            "qsr_local_step_sync", "qsr_parallel_step", "qsr_sync", "qsr_sync_sum_floats", "qsr_sync_partial", "qsr_local_step_partial", "qsr_sync_finish", "qsr_sync_static", "qsr_run", "qsr_launch_count",
-           "qsr_set_launch_shape", "qsr_set_graph_replay", "qsr_set_resident_steps", "qsr_train_host", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
+           "qsr_set_launch_shape", "qsr_set_graph_replay", "qsr_set_resident_steps", "qsr_train_host", "qsr_list_workspace_bytes", "qsr_list_create", "qsr_list_destroy", "qsr_list_set_grads",
+           "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
 
 
 class QsrConfig(C.Structure):
@@ -41,6 +46,29 @@ class QsrConfig(C.Structure):
                 ("T", C.c_int64), ("T_warmup", C.c_int64), ("H_base", C.c_int64), ("t_state_origin", C.c_int64),
                 ("seed", C.c_uint64), ("gamma", C.c_double), ("t_switch", C.c_int64), ("t_hold", C.c_int64),
                 ("t_period", C.c_int64)]
+
+
+class QsrTensor(C.Structure):
+    """Mirror of `qsr_tensor`."""
+    _fields_ = [("param", C.c_void_p), ("copy", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("numel", C.c_int64), ("param_type", C.c_int32),
+                ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("wd_scale", C.c_float)]
+
+
+class QsrListConfig(C.Structure):
+    """Mirror of `qsr_list_config`."""
+    _fields_ = [("n_tensors", C.c_int32), ("workers", C.c_int32), ("states", C.c_int32), ("reserved", C.c_int32),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("clip_norm", C.c_double), ("grad_norm", C.c_void_p)]
+
+
+class QsrLogprobArgs(C.Structure):
+    """Mirror of `qsr_logprob_args`."""
+    _fields_ = [("logits", C.c_void_p), ("tokens", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64),
+                ("row_stride", C.c_int64), ("logits_type", C.c_int32), ("n_top", C.c_int32), ("inv_temperature", C.c_double),
+                ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("row_stats", C.c_void_p), ("top_logprob", C.c_void_p),
+                ("top_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_entropy", C.c_void_p), ("d_logits", C.c_void_p),
+                ("d_row_stride", C.c_int64)]
 
 
 class QsrError(RuntimeError):
@@ -90,6 +118,15 @@ def lib():
             "qsr_set_graph_replay": (C.c_int, [vp, i32]),
             "qsr_set_resident_steps": (C.c_int, [vp, i32]),
             "qsr_train_host": (C.c_int, [cfg, vp, vp, vp, vp, vp, i64, i64, vp, vp, vp, i64, C.POINTER(i64), C.POINTER(i64)]),
+            "qsr_list_workspace_bytes": (i64, [vp, i32, i32]),
+            "qsr_list_create": (C.c_int, [C.POINTER(vp), C.POINTER(QsrListConfig), C.POINTER(QsrTensor), vp, i64, vp]),
+            "qsr_list_destroy": (C.c_int, [vp]),
+            "qsr_list_set_grads": (C.c_int, [vp, vp]),
+            "qsr_list_step": (C.c_int, [vp, i64, C.c_double, C.c_double]),
+            "qsr_list_sync": (C.c_int, [vp, i32]),
+            "qsr_list_launch_count": (i64, [vp]),
+            "qsr_token_logprobs": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
+            "qsr_token_logprobs_grad": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
             "qsr_debug_box_muller": (C.c_int, [vp, i64, vp, vp, vp, vp]),
             "qsr_debug_fast_math": (C.c_int, [vp, i64, vp, vp, vp]),
             "qsr_strerror": (C.c_char_p, [C.c_int]),
@@ -287,6 +324,191 @@ def qsr_train_host(cfg: QsrConfig, theta0: np.ndarray, lam: np.ndarray, theta_st
                                 _dptr(workspace), nbytes, t_end, C.c_void_p(stream),
                                 st.ctypes.data, H.ctypes.data, cap, C.byref(n), C.byref(launches)), "qsr_train_host")
     return st[:n.value].copy(), H[:n.value].copy(), int(launches.value)
+
+
+# ---- lists of tensors -----------------------------------------------------------------------------------
+
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill a stretch of memory without gaps, in whatever order of dimensions."""
+    if t.is_contiguous():
+        return True
+    expect = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != expect:
+            return False
+        expect *= size
+    return True
+
+
+def _element(t, like, what: str, dtypes=DTYPE):
+    """Device address of one operand of a list entry: a dense CUDA tensor with as many elements as the parameter, in the
+    same order in memory."""
+    name = str(t.dtype)
+    if name not in dtypes:
+        raise ValueError(f"{what}: {name} is not supported (one of {', '.join(sorted(dtypes))})")
+    if not t.is_cuda or t.device != like.device:
+        raise ValueError(f"{what}: expected a CUDA tensor on {like.device}")
+    if t.numel() != like.numel():
+        raise ValueError(f"{what}: {t.numel()} elements for a parameter of {like.numel()}")
+    if not (t.is_contiguous() and like.is_contiguous()) and not (t.shape == like.shape and t.stride() == like.stride() and _dense(t)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} does not lie in memory like its parameter")
+    return int(t.data_ptr()) if t.numel() else None
+
+
+def qsr_list_workspace_bytes(numels, workers: int = 1) -> int:
+    """Bytes of device workspace for a TensorList over tensors of these sizes (all workers' tensors)."""
+    a = np.ascontiguousarray(list(numels), np.int64)
+    n = int(lib().qsr_list_workspace_bytes(a.ctypes.data, a.size, int(workers)))
+    if n < 0:
+        raise QsrError(n, "qsr_list_workspace_bytes")
+    return n
+
+
+class TensorList:
+    """Owner of one `qsr_list`: AdamW steps and replica means over a model's own tensors.
+
+    params / grads / copies: lists of CUDA tensors in float32, bfloat16 or float16 (grads and copies may be None, or None in
+    places); with several workers, worker 0's tensors first, then worker 1's, and so on.  m, v: float32 tensors, or
+    float8_e4m3fn with m_scale / v_scale (float32, one per 256 elements, in memory order).  wd_scale: a factor on the
+    weight decay per tensor (default 1).  workspace: a CUDA tensor of qsr_list_workspace_bytes bytes.  Keeps references
+    to the tensors whose memory the library borrows."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None, wd_scale=None, workers: int = 1,
+                 beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+                 clip_norm: float = 0.0, grad_norm=None, workspace=None, stream: int = 0):
+        self._h = C.c_void_p()
+        n = len(params)
+        columns = {"grads": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies, "wd_scale": wd_scale}
+        for what, column in columns.items():
+            if column is None and what in ("m", "v"):
+                raise ValueError(f"{what} is required")
+            if column is not None and len(column) != n:
+                raise ValueError(f"{what}: {len(column)} entries for {n} parameters")
+        codes = n > 0 and str(m[0].dtype) == "torch.float8_e4m3fn"
+        if codes and (m_scale is None or v_scale is None):
+            raise ValueError("states in 8 bits need m_scale and v_scale")
+        state_types = {"torch.float8_e4m3fn": 0} if codes else {"torch.float32": 0}
+        entries = (QsrTensor * max(1, n))()
+        for i, p in enumerate(params):
+            e = entries[i]
+            e.numel, e.param_type, e.wd_scale = p.numel(), DTYPE.get(str(p.dtype), QSR_NONE), 1.0 if wd_scale is None else wd_scale[i]
+            e.param = _element(p, p, f"params[{i}]")
+            e.m, e.v = _element(m[i], p, f"m[{i}]", state_types), _element(v[i], p, f"v[{i}]", state_types)
+            e.copy_type = QSR_NONE
+            if copies is not None and copies[i] is not None:
+                e.copy, e.copy_type = _element(copies[i], p, f"copies[{i}]"), DTYPE[str(copies[i].dtype)]
+            g = None if grads is None else grads[i]
+            if g is not None:
+                e.grad, e.grad_type = _element(g, p, f"grads[{i}]"), DTYPE[str(g.dtype)]
+            else:
+                e.grad_type = e.param_type
+            if codes:
+                for name, scales in (("m_scale", m_scale), ("v_scale", v_scale)):
+                    if str(scales[i].dtype) != "torch.float32" or scales[i].numel() != (p.numel() + 255) // 256:
+                        raise ValueError(f"{name}[{i}]: one float32 per 256 elements is expected")
+                    setattr(e, name, _dptr(scales[i]) if p.numel() else None)
+        if grad_norm is not None and (str(grad_norm.dtype) != "torch.float32" or grad_norm.numel() != workers):
+            raise ValueError("grad_norm: one float32 per worker is expected")
+        cfg = QsrListConfig(n_tensors=n, workers=int(workers), states=STATES["e4m3" if codes else "f32"], beta1=beta1, beta2=beta2,
+                            eps=eps, weight_decay=weight_decay, clip_norm=clip_norm, grad_norm=_dptr(grad_norm))
+        nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
+        self._params, self._grad_types = list(params), [entries[i].grad_type for i in range(n)]
+        self._keep = (list(m), list(v), m_scale, v_scale, copies, grad_norm, workspace)
+        self._grads = grads
+        _check(lib().qsr_list_create(C.byref(self._h), C.byref(cfg), entries, _dptr(workspace), nbytes, C.c_void_p(stream)),
+               "qsr_list_create")
+
+    def close(self) -> None:
+        if self._h:
+            lib().qsr_list_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def qsr_list_set_grads(self, grads) -> None:
+        """New gradient tensors (one per parameter, of the types the list was made with)."""
+        if len(grads) != len(self._params):
+            raise ValueError(f"{len(grads)} gradients for {len(self._params)} parameters")
+        names = {v: k for k, v in DTYPE.items()}
+        table = (C.c_void_p * max(1, len(grads)))()
+        for i, (g, p) in enumerate(zip(grads, self._params)):
+            table[i] = _element(g, p, f"grads[{i}]", {names[self._grad_types[i]]: 0})
+        _check(lib().qsr_list_set_grads(self._h, table), "qsr_list_set_grads")
+        self._grads = list(grads)
+
+    def qsr_list_step(self, n: int, lr: float, grad_scale: float = 1.0) -> None:
+        _check(lib().qsr_list_step(self._h, n, lr, grad_scale), "qsr_list_step")
+
+    def qsr_list_sync(self, state_sync: str = "keep") -> None:
+        _check(lib().qsr_list_sync(self._h, STATE[state_sync]), "qsr_list_sync")
+
+    def qsr_list_launch_count(self) -> int:
+        return int(lib().qsr_list_launch_count(self._h))
+
+
+# ---- log probabilities of given tokens ------------------------------------------------------------------
+
+def _rows(t, what: str, rows: int, dtype: str, width: Optional[int] = None) -> Optional[int]:
+    """Device address of a contiguous CUDA tensor with `rows` (times `width`) elements of `dtype`; None for None."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype or t.numel() != rows * (1 if width is None else width) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {rows * (1 if width is None else width)} x {dtype} is expected")
+    return t.data_ptr()
+
+
+def _matrix(t, what: str):
+    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a CUDA matrix with adjacent columns is expected")
+    # the stride of a single row means nothing
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits) -> QsrLogprobArgs:
+    stride, kind = _matrix(logits, "logits"), str(logits.dtype)
+    if kind not in DTYPE:
+        raise ValueError(f"logits: {kind} is not supported (one of {', '.join(sorted(DTYPE))})")
+    R, V = logits.shape
+    a = QsrLogprobArgs(logits=logits.data_ptr(), tokens=_rows(tokens, "tokens", R, "torch.int64"), rows=R, vocab=V, row_stride=stride,
+                       logits_type=DTYPE[kind], inv_temperature=inv_temperature,
+                       entropy=_rows(entropy, "entropy", R, "torch.float32"),
+                       row_stats=_rows(row_stats, "row_stats", R, "torch.float32", 2),
+                       d_logprob=_rows(d_logprob, "d_logprob", R, "torch.float32"),
+                       d_entropy=_rows(d_entropy, "d_entropy", R, "torch.float32"))
+    if d_logits is not None:
+        if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
+            raise ValueError("d_logits: shape and type of the logits are expected")
+        a.d_logits, a.d_row_stride = d_logits.data_ptr(), _matrix(d_logits, "d_logits")
+    return a
+
+
+def qsr_token_logprobs(logits, tokens, logprob, entropy=None, row_stats=None, top_logprob=None, top_token=None,
+                       inv_temperature: float = 1.0, d_logprob=None, d_entropy=None, d_logits=None, stream: int = 0) -> None:
+    """Log probability of each row's token, with optional entropy, row statistics, top alternatives ([rows, n] tensors, n at
+    most QSR_MAX_TOP) and, if d_logits is given, the gradient in the same pass.  All tensors are the caller's."""
+    a = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
+    a.logprob = _rows(logprob, "logprob", a.rows, "torch.float32")
+    if (top_logprob is None) != (top_token is None):
+        raise ValueError("top_logprob and top_token come together")
+    if top_token is not None:
+        if top_token.dim() != 2:
+            raise ValueError("top_token: [rows, n] is expected")
+        a.n_top = top_token.shape[1]
+        a.top_logprob = _rows(top_logprob, "top_logprob", a.rows, "torch.float32", a.n_top)
+        a.top_token = _rows(top_token, "top_token", a.rows, "torch.int64", a.n_top)
+    _check(lib().qsr_token_logprobs(C.byref(a), stream), "qsr_token_logprobs")
+
+
+def qsr_token_logprobs_grad(logits, tokens, row_stats, d_logits, d_logprob=None, d_entropy=None, entropy=None,
+                            inv_temperature: float = 1.0, stream: int = 0) -> None:
+    """Gradient of sum(d_logprob * logprob + d_entropy * entropy) with respect to the logits, from the row_stats (and entropy)
+    that qsr_token_logprobs wrote for the same logits and temperature."""
+    a = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
+    _check(lib().qsr_token_logprobs_grad(C.byref(a), stream), "qsr_token_logprobs_grad")
 
 
 def qsr_debug_box_muller(words, radius, sine, cosine, stream: int = 0) -> None:

@@ -12,8 +12,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqsr.so")
-SOURCES = ["schedule.cpp", "kernels.cu", "api.cu"]
-HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(os.path.dirname(HERE), "include", "qsr.h")]
+SOURCES = ["schedule.cpp", "kernels.cu", "api.cu", "lists.cu", "lists_api.cu", "logprobs.cu"]
+HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "wide.cuh"), os.path.join(os.path.dirname(HERE), "include", "qsr.h")]
 
 
 def _nvcc() -> str:
@@ -35,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and up_to_date():
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off"]
+           "-shared", "--threads", "0", "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB + ".tmp", "-ldl"]

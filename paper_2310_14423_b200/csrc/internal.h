@@ -127,5 +127,65 @@ int launch_fast_math(const float *x, int64_t n, float *root, float *reciprocal, 
 // `device` (the context's) is not the current device.
 int launch_sync_static(const SyncParams &p, const LaunchShape &shape, int device, void *stream);
 
+// ---- lists of tensors (lists.cu, lists_api.cu) ----
+
+struct ListTensor {           // one tensor, in the device table
+    void *param, *copy, *m, *v;
+    float *m_scale, *v_scale;
+    int32_t param_type, grad_type, copy_type;
+    float wd_scale;
+};
+struct ListChunk {            // what one block works on: n elements of one tensor from `offset` (a multiple of 256)
+    int32_t tensor, n;
+    int64_t offset;
+};
+struct ListStepParams {
+    const ListTensor *tensors;
+    const void *const *grads;
+    const ListChunk *chunks;
+    const float *clip;        // NULL, or device [workers]
+    int32_t tensors_per_worker;
+    float omb1, omb2, eps, eta_wd, step_size, inv_sqrt_bc2, grad_scale;
+};
+struct ListNormParams {
+    const ListTensor *tensors;
+    const void *const *grads;
+    const ListChunk *chunks;
+    float *partial;           // [chunks]
+    float *clip;              // [workers]
+    unsigned *arrived;        // [workers], zero between launches
+    float *grad_norm;         // NULL, or [workers]
+    int32_t chunks_per_worker;
+    float max_norm, grad_scale;
+};
+struct ListSyncParams {
+    const ListTensor *tensors;
+    const ListChunk *chunks;
+    int32_t workers, tensors_per_worker;
+    float divisor;
+};
+int launch_list_step(const ListStepParams &p, bool states8, int64_t chunks, void *stream);
+int launch_list_norm(const ListNormParams &p, int64_t chunks, void *stream);
+int launch_list_sync(const ListSyncParams &p, bool states8, bool average, int64_t chunks_per_worker, void *stream);
+int launch_list_reset(const ListSyncParams &p, bool states8, int64_t chunks, void *stream);
+
+// ---- log probabilities of given tokens (logprobs.cu) ----
+
+struct LogprobParams {
+    const void *logits;
+    const int64_t *tokens;
+    float *logprob, *entropy;
+    float *stats;             // [rows, 2]: largest logit, ln of the sum relative to it
+    float *top_logprob;
+    int64_t *top_token;
+    const float *d_logprob, *d_entropy;
+    void *d_logits;
+    int64_t rows, vocab, stride, d_stride;
+    int32_t type, n_top;
+    float tau, tau_log2e;     // inverse temperature, and the same for powers of two
+};
+int launch_logprobs(const LogprobParams &p, void *stream);
+int launch_logprobs_grad(const LogprobParams &p, void *stream);
+
 }  // namespace qsr
 #endif

@@ -1,0 +1,648 @@
+// Log probabilities of given tokens with entropy, top alternatives and gradient (formulas in the public header).
+//
+// A row of logits is read once from global memory: a block (or, for long rows and few of them, a cluster of up to eight
+// blocks that exchange their partial results through distributed shared memory) keeps its slice of the row in shared
+// memory, so the maximum, the sums, the search for the alternatives and the gradient all work from there.  A slice is
+// split into 16-byte granules; a thread loads, reduces and writes only its own granules, so nothing but the reductions
+// needs a barrier.  Granules at a row's ends may be partial (rows of odd length start anywhere): those are loaded and
+// written element by element.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "internal.h"
+#include "wide.cuh"
+
+namespace qsr {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kMaxThreads = 512;
+constexpr int kMaxWarps = kMaxThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kCandidates = 1024;
+constexpr int kGroups = 64;                  // groups of threads whose maxima bound the n-th largest logit from below
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLowest2 = -200.0f;          // 2^-200 = 0 in fp32: log2-probabilities below are raised to it, so that 0 * (-inf) never forms
+
+template <typename T> struct Num;            // how sixteen bytes of a type are taken apart
+template <> struct Num<float> {
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ void widen(float (&x)[4], uint4 w)
+    {
+        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+    }
+    static __device__ __forceinline__ uint4 narrow(const float (&x)[4])
+    {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    static __device__ __forceinline__ float lowest() { return -infinity(); }
+    static __device__ __forceinline__ float to_float(float x) { return x; }
+    static __device__ __forceinline__ float from_float(float x) { return x; }
+    static __device__ __forceinline__ float max_of(float m, uint4 w)
+    {
+        float x[4];
+        widen(x, w);
+        return max_nan(m, max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3])));
+    }
+};
+template <> struct Num<__nv_bfloat16> {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ void widen(float (&x)[8], uint4 w)
+    {
+        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = widen2(v[i], QSR_BF16); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+    }
+    static __device__ __forceinline__ uint4 narrow(const float (&x)[8])
+    {
+        return make_uint4(narrow2(x[0], x[1], QSR_BF16), narrow2(x[2], x[3], QSR_BF16), narrow2(x[4], x[5], QSR_BF16), narrow2(x[6], x[7], QSR_BF16));
+    }
+    static __device__ __forceinline__ __nv_bfloat16 lowest() { return __ushort_as_bfloat16(0xff80); }
+    static __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+    static __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
+    static __device__ __forceinline__ float max_of(float m, uint4 w)
+    {
+        const __nv_bfloat162 *v = reinterpret_cast<const __nv_bfloat162 *>(&w);
+        const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
+        return max_nan(m, max_nan(__low2float(a), __high2float(a)));
+    }
+};
+template <> struct Num<__half> {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ void widen(float (&x)[8], uint4 w)
+    {
+        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = widen2(v[i], QSR_F16); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+    }
+    static __device__ __forceinline__ uint4 narrow(const float (&x)[8])
+    {
+        return make_uint4(narrow2(x[0], x[1], QSR_F16), narrow2(x[2], x[3], QSR_F16), narrow2(x[4], x[5], QSR_F16), narrow2(x[6], x[7], QSR_F16));
+    }
+    static __device__ __forceinline__ __half lowest() { return __ushort_as_half(0xfc00); }
+    static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+    static __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
+    static __device__ __forceinline__ float max_of(float m, uint4 w)
+    {
+        const __half2 *v = reinterpret_cast<const __half2 *>(&w);
+        const __half2 a = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
+        return max_nan(m, max_nan(__low2float(a), __high2float(a)));
+    }
+};
+
+// Orders floats as unsigned integers: -inf lowest, -0 = +0, NaN above everything.
+__device__ __forceinline__ uint32_t sort_bits(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffc00000u;
+    return b ^ (b & 0x80000000u ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float unsort_bits(uint32_t s)
+{
+    return __uint_as_float(s ^ (s & 0x80000000u ? 0x80000000u : 0xffffffffu));
+}
+// Value descending, then index ascending; 0 stands for "none" (no element maps to it: the lowest value's bits are not 0).
+__device__ __forceinline__ unsigned long long key_of(float x, uint32_t index)
+{
+    return (static_cast<unsigned long long>(sort_bits(x)) << 32) | (0xffffffffu - index);
+}
+
+__device__ __forceinline__ void cp_async16(void *smem_dst, const void *gmem_src)
+{
+    const unsigned dst = static_cast<unsigned>(__cvta_generic_to_shared(smem_dst));
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(gmem_src) : "memory");
+}
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// What a slice, and in the end the row, is reduced to: the largest logit, sum of e = 2^z and of e z with z = tau log2(e) (x - m).
+struct Sums { float m, s, t; };
+
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
+{
+    if (a.s == 0.0f) return b;
+    if (b.s == 0.0f) return a;
+    Sums r;
+    r.m = max_nan(a.m, b.m);
+    const float da = (a.m - r.m) * c, db = (b.m - r.m) * c, fa = exp2_1(da), fb = exp2_1(db);
+    r.s = fa * a.s + fb * b.s;
+    // a slice that lies 2^200 below the other adds nothing: its factor is 0, and its offset must not meet that as -inf
+    r.t = fa * fmaf(a.s, fmaxf(da, kLowest2), a.t) + fb * fmaf(b.s, fmaxf(db, kLowest2), b.t);
+    return r;
+}
+
+// One row's slice as a block sees it.
+template <typename T, bool STASH>
+struct Slice {
+    const T *row;             // the row's first element
+    const char *base;         // `row` rounded down to 16 bytes: granule 0
+    uint4 *stash;
+    int64_t vocab;
+    int head;                 // elements of granule 0 that lie before the row
+    int64_t g0, g1;           // granules of this slice
+
+    static constexpr int kPer = Num<T>::kPer;
+    __device__ __forceinline__ int64_t first(int64_t g) const { return g * kPer - head; }     // row index of the granule's element 0
+    __device__ __forceinline__ bool whole(int64_t g) const { return first(g) >= 0 && first(g) + kPer <= vocab; }
+
+    __device__ __forceinline__ uint4 from_global(int64_t g) const
+    {
+        if (whole(g)) return *reinterpret_cast<const uint4 *>(base + g * 16);
+        union { uint4 w; T e[kPer]; } u;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int64_t j = first(g) + i;
+            u.e[i] = j >= 0 && j < vocab ? row[j] : Num<T>::lowest();
+        }
+        return u.w;
+    }
+    __device__ __forceinline__ void fetch()
+    {
+        if constexpr (STASH) {
+            for (int64_t g = g0 + threadIdx.x; g < g1; g += blockDim.x) {
+                if (whole(g)) cp_async16(stash + (g - g0), base + g * 16);
+                else stash[g - g0] = from_global(g);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");      // a thread's own copies: only it reads them back
+        }
+    }
+    __device__ __forceinline__ uint4 get(int64_t g) const { return STASH ? stash[g - g0] : from_global(g); }
+};
+
+struct Shared {
+    float m[kMaxWarps], s[kMaxWarps], t[kMaxWarps];
+    Sums part;                                         // this block's, read by the whole cluster
+};
+struct TopShared {
+    float group[kGroups];
+    unsigned count;
+    float threshold;
+    unsigned long long best, warp_best[kMaxWarps];
+    unsigned long long top[QSR_MAX_TOP];
+    unsigned long long gathered[kMaxCluster * QSR_MAX_TOP];
+    unsigned long long cand[kCandidates];
+};
+
+// The k largest keys of the block's slice to sh.top (0 where the slice has fewer).  The k-th largest of the group maxima bounds
+// the k-th largest element from below, and few elements reach it unless many are equal; those that do are ranked by
+// counting.  If they do not fit (masked or constant rows), or a NaN is about, k rounds of "largest below the last one" follow.
+template <typename T, bool STASH>
+__device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &sh, int k, float thread_max, bool has_nan)
+{
+    constexpr int kPer = Num<T>::kPer;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int per_group = blockDim.x > kGroups ? blockDim.x / kGroups : 1;     // a power of two, at most 8 threads
+    const int groups = blockDim.x / per_group;
+    float gm = thread_max;
+    for (int d = 1; d < per_group; d <<= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, d));
+    if (tid % per_group == 0) sh.group[tid / per_group] = gm;
+    if (tid < k) sh.top[tid] = 0ull;
+    if (tid == 0) { sh.count = 0u; sh.threshold = -infinity(); }
+    __syncthreads();
+    if (tid < groups && !has_nan) {
+        const float mine = sh.group[tid];
+        int rank = 0;
+        for (int i = 0; i < groups; ++i) rank += sh.group[i] > mine || (sh.group[i] == mine && i < tid);
+        if (rank == k - 1) sh.threshold = mine;
+    }
+    __syncthreads();
+    const float thr = sh.threshold;
+    if (!has_nan) {
+        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+            const uint4 w = sl.get(g);
+            if (Num<T>::max_of(-infinity(), w) < thr) continue;
+            float x[kPer];
+            Num<T>::widen(x, w);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int64_t j = sl.first(g) + i;
+                if (x[i] >= thr && j >= 0 && j < sl.vocab) {
+                    const unsigned at = atomicAdd(&sh.count, 1u);
+                    if (at < kCandidates) sh.cand[at] = key_of(x[i], uint32_t(j));
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const unsigned count = sh.count;
+    if (!has_nan && count <= kCandidates) {
+        for (unsigned i = tid; i < count; i += blockDim.x) {
+            const unsigned long long mine = sh.cand[i];
+            int rank = 0;
+            for (unsigned j = 0; j < count && rank < k; ++j) rank += sh.cand[j] > mine;
+            if (rank < k) sh.top[rank] = mine;
+        }
+        __syncthreads();
+        return;
+    }
+    unsigned long long last = ~0ull;
+    for (int r = 0; r < k; ++r) {
+        unsigned long long best = 0ull;
+        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+            float x[kPer];
+            Num<T>::widen(x, sl.get(g));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int64_t j = sl.first(g) + i;
+                if (j >= 0 && j < sl.vocab) {
+                    const unsigned long long key = key_of(x[i], uint32_t(j));
+                    if (key < last && key > best) best = key;
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, d);
+            best = other > best ? other : best;
+        }
+        if (lane == 0) sh.warp_best[tid >> 5] = best;
+        __syncthreads();
+        if (tid == 0) {
+            for (int i = 1; i < int(blockDim.x >> 5); ++i) best = sh.warp_best[i] > best ? sh.warp_best[i] : best;
+            sh.best = best;
+            sh.top[r] = best;
+        }
+        __syncthreads();
+        last = sh.best;
+        if (last == 0ull) break;              // the slice has fewer than k elements
+    }
+    __syncthreads();
+}
+
+// Per-row scalars of the gradient: d = a [j = y] - p (A + B log2 p), p = 2^(z - log2 S).
+struct RowGrad {
+    float m, log2_s, c, hot, A, B;
+    int64_t y;
+    bool empty;
+};
+__device__ __forceinline__ RowGrad row_grad(const LogprobParams &p, int64_t r, int64_t y, float m, float ln_s, float H, float nan_or_0)
+{
+    RowGrad q;
+    q.empty = m == -infinity();
+    q.m = q.empty ? 0.0f : m;
+    q.log2_s = q.empty ? 0.0f : ln_s * kLog2e;
+    q.c = p.tau_log2e;
+    q.y = y;
+    const float a = p.d_logprob && y >= 0 && !q.empty ? p.tau * p.d_logprob[r] + nan_or_0 : 0.0f;
+    const float b = p.d_entropy && !q.empty ? p.tau * p.d_entropy[r] : 0.0f;
+    q.hot = a;
+    q.A = fmaf(b, H, a);
+    q.B = b * kLn2;
+    return q;
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q, int64_t first)
+{
+    constexpr int kPer = Num<T>::kPer;
+    float x[kPer];
+    Num<T>::widen(x, w);
+#pragma unroll
+    for (int i = 0; i < kPer; i += 2) {
+        const float2 d = add2(make_float2(x[i], x[i + 1]), both(-q.m));
+        const float2 l = fma2(d, both(q.c), both(-q.log2_s));
+        const float2 e = make_float2(exp2_1(l.x), exp2_1(l.y));
+        float2 f = both(q.A);
+        if (q.B != 0.0f) f = fma2(both(q.B), make_float2(fmaxf(l.x, kLowest2), fmaxf(l.y, kLowest2)), f);
+        const float2 o = mul2(make_float2(-e.x, -e.y), f);
+        x[i] = o.x; x[i + 1] = o.y;
+    }
+    const int64_t at = q.y - first;
+    if (at >= 0 && at < kPer && q.hot != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] += i == int(at) ? q.hot : 0.0f;
+    }
+    return Num<T>::narrow(x);
+}
+
+// Writes the granule whose element 0 has row index `first`; `vector`: the output row lies like the input row modulo 16 bytes.
+template <typename T>
+__device__ __forceinline__ void put_granule(T *out_row, int64_t vocab, int64_t first, bool vector, uint4 w)
+{
+    constexpr int kPer = Num<T>::kPer;
+    if (vector && first >= 0 && first + kPer <= vocab) {
+        *reinterpret_cast<uint4 *>(out_row + first) = w;
+        return;
+    }
+    union { uint4 w; T e[kPer]; } u;
+    u.w = w;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (first + i >= 0 && first + i < vocab) out_row[first + i] = u.e[i];
+}
+
+template <typename T>
+__device__ __forceinline__ bool same_phase(const T *a, const T *b)
+{
+    return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
+}
+
+// One row per cluster.  TOP: alternatives are wanted; GRAD: d_logits is.
+template <typename T, bool STASH, bool TOP, bool GRAD>
+__global__ void __launch_bounds__(kMaxThreads) logprob_kernel(const LogprobParams p, const int cluster)
+{
+    constexpr int kPer = Num<T>::kPer;
+    extern __shared__ uint4 stash[];
+    __shared__ Shared sh;
+    __shared__ typename std::conditional<TOP, TopShared, int>::type top_sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    const int64_t r = blockIdx.x / cluster;
+    const int rank = int(blockIdx.x % cluster);
+
+    Slice<T, STASH> sl;
+    sl.row = static_cast<const T *>(p.logits) + r * p.stride;
+    const uintptr_t address = reinterpret_cast<uintptr_t>(sl.row);
+    sl.base = reinterpret_cast<const char *>(address & ~uintptr_t(15));
+    sl.head = int((address & 15u) / sizeof(T));
+    sl.vocab = p.vocab;
+    sl.stash = stash;
+    const int64_t granules = (sl.head + p.vocab + kPer - 1) / kPer;
+    sl.g0 = granules * rank / cluster;
+    sl.g1 = granules * (rank + 1) / cluster;
+    const int64_t y = p.tokens[r];
+    float token_logit = 0.0f;
+    if (tid == 0 && rank == 0 && y >= 0) token_logit = y < p.vocab ? Num<T>::to_float(sl.row[y]) : quiet_nan();
+
+    // a block's shared memory may only be written by another once both run: announced here, awaited before the first write
+    if (TOP && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    sl.fetch();
+    // largest logit of the slice, NaN if there is one
+    float thread_max = -infinity();
+    for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) thread_max = Num<T>::max_of(thread_max, sl.get(g));
+    float m = warp_max_nan(thread_max);
+    if (warps > 1) {
+        if (lane == 0) sh.m[warp] = m;
+        __syncthreads();
+        m = sh.m[0];
+        for (int i = 1; i < warps; ++i) m = max_nan(m, sh.m[i]);
+    }
+    // sums relative to it
+    const float base = m == -infinity() ? 0.0f : m, c = p.tau_log2e;
+    float2 s2 = both(0.0f), t2 = both(0.0f);
+    for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+        float x[kPer];
+        Num<T>::widen(x, sl.get(g));
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2) {
+            const float2 z = mul2(add2(make_float2(x[i], x[i + 1]), both(-base)), both(c));
+            const float2 e = make_float2(exp2_1(z.x), exp2_1(z.y));
+            s2 = add2(s2, e);
+            t2 = fma2(e, make_float2(fmaxf(z.x, kLowest2), fmaxf(z.y, kLowest2)), t2);
+        }
+    }
+    float s = warp_sum(s2.x + s2.y), t = warp_sum(t2.x + t2.y);
+    if (warps > 1) {
+        if (lane == 0) { sh.s[warp] = s; sh.t[warp] = t; }
+        __syncthreads();
+        s = t = 0.0f;
+        for (int i = 0; i < warps; ++i) { s += sh.s[i]; t += sh.t[i]; }
+    }
+    Sums all{m, s, t};
+    if (!(m < infinity())) all.m = all.s = quiet_nan();       // a NaN or +inf: the row is NaN
+    if (TOP) slice_top<T, STASH>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(m));
+    if (cluster > 1) {
+        cg::cluster_group cl = cg::this_cluster();
+        if (tid == 0) sh.part = all;
+        if (TOP) {
+            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+            TopShared &mine = reinterpret_cast<TopShared &>(top_sh);
+            unsigned long long *gather = cl.map_shared_rank(mine.gathered, 0);
+            if (tid < p.n_top) gather[rank * p.n_top + tid] = mine.top[tid];
+        }
+        cl.sync();
+        all = *cl.map_shared_rank(&sh.part, 0);
+        for (int i = 1; i < cluster; ++i) all = join(all, *cl.map_shared_rank(&sh.part, i), c);
+        cl.sync();                                            // no block leaves (or reuses `part`) while another reads it
+    }
+    const bool empty = all.m == -infinity();
+    const float ln_s = empty ? 0.0f : logf(all.s);
+    const float H = empty ? 0.0f : fmaxf(ln_s - kLn2 * (all.t / all.s), 0.0f) + 0.0f * all.s;
+
+    if (rank == 0) {
+        if (tid == 0) {
+            const float lp = empty ? -infinity() : fmaf(p.tau, token_logit - all.m, -ln_s);
+            p.logprob[r] = y < 0 ? 0.0f : (y < p.vocab ? lp : quiet_nan());
+            if (p.entropy) p.entropy[r] = H;
+            if (p.stats) { p.stats[2 * r] = all.m; p.stats[2 * r + 1] = ln_s; }
+        }
+        if (TOP) {
+            TopShared &mine = reinterpret_cast<TopShared &>(top_sh);
+            if (cluster > 1) {
+                const int n = cluster * p.n_top;
+                for (int i = tid; i < n; i += blockDim.x) {
+                    const unsigned long long key = mine.gathered[i];
+                    int place = 0;
+                    for (int j = 0; j < n; ++j) place += mine.gathered[j] > key;
+                    if (key != 0ull && place < p.n_top) mine.top[place] = key;
+                }
+                __syncthreads();
+            }
+            if (tid < p.n_top) {
+                const unsigned long long key = mine.top[tid];
+                p.top_token[r * p.n_top + tid] = int64_t(0xffffffffu - uint32_t(key));
+                p.top_logprob[r * p.n_top + tid] = empty ? -infinity() : fmaf(p.tau, unsort_bits(uint32_t(key >> 32)) - all.m, -ln_s);
+            }
+        }
+    }
+    if (GRAD) {
+        __syncthreads();              // d_logits may be the logits: the token's logit has been read
+        const RowGrad q = row_grad(p, r, y, all.m, ln_s, H, y < p.vocab ? 0.0f : quiet_nan());
+        T *out = static_cast<T *>(p.d_logits) + r * p.d_stride;
+        const bool vector = same_phase<T>(sl.row, out);
+        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x)
+            put_granule<T>(out, p.vocab, sl.first(g), vector, granule_grad<T>(sl.get(g), q, sl.first(g)));
+    }
+}
+
+constexpr int kGradThreads = 256;
+constexpr int kGradPer = 4;                   // granules in flight per thread
+
+// The gradient alone, from the statistics of an earlier call.  Grid: parts of a row by rows.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const LogprobParams p, const int parts)
+{
+    constexpr int kPer = Num<T>::kPer;
+    const int64_t r = blockIdx.x / parts;
+    const int part = int(blockIdx.x % parts);
+    Slice<T, false> sl;
+    sl.row = static_cast<const T *>(p.logits) + r * p.stride;
+    const uintptr_t address = reinterpret_cast<uintptr_t>(sl.row);
+    sl.base = reinterpret_cast<const char *>(address & ~uintptr_t(15));
+    sl.head = int((address & 15u) / sizeof(T));
+    sl.vocab = p.vocab;
+    const int64_t granules = (sl.head + p.vocab + kPer - 1) / kPer;
+    const int64_t g0 = granules * part / parts + threadIdx.x, g1 = granules * (part + 1) / parts;
+    uint4 w[kGradPer];
+#pragma unroll
+    for (int i = 0; i < kGradPer; ++i)
+        if (g0 + i * int64_t(blockDim.x) < g1) w[i] = sl.from_global(g0 + i * int64_t(blockDim.x));
+    const int64_t y = p.tokens[r];
+    const RowGrad q = row_grad(p, r, y, p.stats[2 * r], p.stats[2 * r + 1], p.d_entropy ? p.entropy[r] : 0.0f,
+                               y < p.vocab ? 0.0f : quiet_nan());
+    T *out = static_cast<T *>(p.d_logits) + r * p.d_stride;
+    const bool vector = same_phase<T>(sl.row, out);
+#pragma unroll
+    for (int i = 0; i < kGradPer; ++i) {
+        const int64_t g = g0 + i * int64_t(blockDim.x);
+        if (g < g1) put_granule<T>(out, p.vocab, sl.first(g), vector, granule_grad<T>(w[i], q, sl.first(g)));
+    }
+}
+
+constexpr int64_t kSliceBytes = 64 * 1024;    // three blocks of such a slice share a multiprocessor
+constexpr int64_t kStashMax = 200 * 1024;
+constexpr int kMultiprocessors = 148;
+
+struct Shape { int cluster, threads; int64_t smem; };
+
+Shape shape_of(const LogprobParams &p, int element)
+{
+    const int64_t bytes = (p.vocab * element + 15 + 15) / 16 * 16;
+    Shape s;
+    s.cluster = 1;
+    while (s.cluster < kMaxCluster && (bytes > kSliceBytes * s.cluster ||
+                                       (p.rows * s.cluster * 2 <= kMultiprocessors && bytes >= 8192 * s.cluster)))
+        s.cluster *= 2;
+    const int64_t granules = (bytes / 16 + s.cluster - 1) / s.cluster + 1;
+    const int64_t each = p.rows * s.cluster <= kMultiprocessors ? 4 : 8;       // granules per thread
+    s.threads = 32;
+    while (s.threads < kMaxThreads && s.threads * each < granules) s.threads *= 2;
+    s.smem = granules * 16;
+    return s;
+}
+
+template <typename T, bool STASH, bool TOP, bool GRAD>
+int launch_instance(const LogprobParams &p, const Shape &s, cudaStream_t st)
+{
+    const auto kernel = logprob_kernel<T, STASH, TOP, GRAD>;
+    const size_t smem = STASH ? size_t(s.smem) : 0;
+    if (smem > 32 * 1024)
+        if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem))) return int(err);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(p.rows * s.cluster));
+    cfg.blockDim = dim3(unsigned(s.threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(s.cluster);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = s.cluster > 1 ? 1 : 0;
+    return int(cudaLaunchKernelEx(&cfg, kernel, p, s.cluster));
+}
+
+template <typename T>
+int launch_typed(const LogprobParams &p, cudaStream_t st)
+{
+    const Shape s = shape_of(p, int(sizeof(T)));
+    const bool stash = s.smem <= kStashMax, top = p.n_top > 0, grad = p.d_logits != nullptr;
+    if (stash) {
+        if (top) return grad ? launch_instance<T, true, true, true>(p, s, st) : launch_instance<T, true, true, false>(p, s, st);
+        return grad ? launch_instance<T, true, false, true>(p, s, st) : launch_instance<T, true, false, false>(p, s, st);
+    }
+    if (top) return grad ? launch_instance<T, false, true, true>(p, s, st) : launch_instance<T, false, true, false>(p, s, st);
+    return grad ? launch_instance<T, false, false, true>(p, s, st) : launch_instance<T, false, false, false>(p, s, st);
+}
+
+template <typename T>
+int launch_grad_typed(const LogprobParams &p, cudaStream_t st)
+{
+    const int64_t granules = (p.vocab * int64_t(sizeof(T)) + 15 + 15) / 16;
+    int threads = 32;
+    while (threads < kGradThreads && threads * kGradPer < granules) threads *= 2;
+    const int64_t parts = (granules + threads * kGradPer - 1) / (threads * kGradPer);
+    if (parts * p.rows > 0x7fffffff) return int(cudaErrorInvalidConfiguration);
+    logprob_grad_kernel<T><<<unsigned(parts * p.rows), threads, 0, st>>>(p, int(parts));
+    return int(cudaGetLastError());
+}
+
+}  // namespace
+
+int launch_logprobs(const LogprobParams &p, void *stream)
+{
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.type == QSR_F32) return launch_typed<float>(p, st);
+    if (p.type == QSR_BF16) return launch_typed<__nv_bfloat16>(p, st);
+    return launch_typed<__half>(p, st);
+}
+
+int launch_logprobs_grad(const LogprobParams &p, void *stream)
+{
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.type == QSR_F32) return launch_grad_typed<float>(p, st);
+    if (p.type == QSR_BF16) return launch_grad_typed<__nv_bfloat16>(p, st);
+    return launch_grad_typed<__half>(p, st);
+}
+
+}  // namespace qsr
+
+namespace {
+
+bool element_aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// Checks what both calls share and fills the kernel's arguments.
+int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &p)
+{
+    if (!a) return QSR_EINVAL;
+    if (a->logits_type != QSR_F32 && a->logits_type != QSR_BF16 && a->logits_type != QSR_F16) return QSR_EINVAL;
+    if (!std::isfinite(a->inv_temperature) || !(float(a->inv_temperature) > 0.0f) || !std::isfinite(float(a->inv_temperature)))
+        return QSR_EINVAL;
+    if (a->rows < 0 || a->rows >= (int64_t(1) << 28) || a->vocab < 1 || a->vocab > 0x7fffffff || a->row_stride < a->vocab) return QSR_ERANGE;
+    if (forward && (a->n_top < 0 || a->n_top > QSR_MAX_TOP || a->n_top > a->vocab)) return QSR_ERANGE;
+    if (a->d_logits && (a->d_row_stride < a->vocab || (a->d_logits == a->logits && a->d_row_stride != a->row_stride))) return QSR_ERANGE;
+    if (a->rows > 0) {
+        if (!a->logits || !a->tokens) return QSR_EINVAL;
+        if (forward && (!a->logprob || (a->n_top > 0 && (!a->top_logprob || !a->top_token)))) return QSR_EINVAL;
+        if (!forward && (!a->d_logits || !a->row_stats || (a->d_entropy && !a->entropy))) return QSR_EINVAL;
+    }
+    const unsigned e = a->logits_type == QSR_F32 ? 4 : 2;
+    if (!element_aligned(a->logits, e) || !element_aligned(a->d_logits, e) || !element_aligned(a->tokens, 8) ||
+        !element_aligned(a->entropy, 4) || !element_aligned(a->row_stats, 8) || !element_aligned(a->d_logprob, 4) ||
+        !element_aligned(a->d_entropy, 4))
+        return QSR_EALIGN;
+    if (forward && (!element_aligned(a->logprob, 4) || (a->n_top > 0 && (!element_aligned(a->top_logprob, 4) || !element_aligned(a->top_token, 8)))))
+        return QSR_EALIGN;
+    p.logits = a->logits; p.tokens = a->tokens;
+    p.logprob = a->logprob; p.entropy = a->entropy; p.stats = a->row_stats;
+    p.top_logprob = a->top_logprob; p.top_token = a->top_token;
+    p.d_logprob = a->d_logprob; p.d_entropy = a->d_entropy; p.d_logits = a->d_logits;
+    p.rows = a->rows; p.vocab = a->vocab; p.stride = a->row_stride; p.d_stride = a->d_row_stride;
+    p.type = a->logits_type; p.n_top = a->n_top;
+    p.tau = float(a->inv_temperature);
+    p.tau_log2e = float(a->inv_temperature * 1.4426950408889634);
+    return QSR_OK;
+}
+
+int launched(int err)
+{
+    if (err == 0) return QSR_OK;
+    cudaGetLastError();
+    return QSR_ECUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream)
+{
+    qsr::LogprobParams p;
+    if (int rc = logprob_params(args, true, p)) return rc;
+    return p.rows == 0 ? QSR_OK : launched(qsr::launch_logprobs(p, cuda_stream));
+}
+
+int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream)
+{
+    qsr::LogprobParams p;
+    if (int rc = logprob_params(args, false, p)) return rc;
+    return p.rows == 0 ? QSR_OK : launched(qsr::launch_logprobs_grad(p, cuda_stream));
+}
+
+}  // extern "C"
