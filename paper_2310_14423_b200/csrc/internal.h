@@ -146,6 +146,7 @@ struct ListStepParams {
     const float *clip;        // NULL, or device [workers]
     int32_t tensors_per_worker;
     float omb1, omb2, eps, eta_wd, step_size, inv_sqrt_bc2, grad_scale;
+    float one;                // 1, unknown to the compiler: see add2 of the kernel
 };
 struct ListNormParams {
     const ListTensor *tensors;
@@ -164,7 +165,16 @@ struct ListSyncParams {
     int32_t workers, tensors_per_worker;
     float divisor;
 };
-int launch_list_step(const ListStepParams &p, bool states8, int64_t chunks, void *stream);
+// How a list's step is launched.  8-bit states: a warp keeps `stages` blocks of 256 elements in shared memory, stage_bytes each
+// (parameter, gradient and codes of the list's widest tensor); fp32 states: both 0.
+struct ListShape {
+    int64_t chunks;
+    int stage_bytes, stages;
+    int param_type, grad_type;    // of all tensors, or both QSR_NONE where they differ
+};
+constexpr int kListWarps = 8;     // warps of a thread block
+constexpr int kListStages = 4;    // most blocks of 256 elements a warp may have
+int launch_list_step(const ListStepParams &p, const ListShape &shape, void *stream);
 int launch_list_norm(const ListNormParams &p, int64_t chunks, void *stream);
 int launch_list_sync(const ListSyncParams &p, bool states8, bool average, int64_t chunks_per_worker, void *stream);
 int launch_list_reset(const ListSyncParams &p, bool states8, int64_t chunks, void *stream);

@@ -22,6 +22,7 @@ struct qsr_list {
     unsigned *arrived;
     std::vector<qsr_tensor> host;
     bool has_grads;
+    qsr::ListShape shape;
     int64_t launches;
 };
 
@@ -40,14 +41,24 @@ int element_bytes(int type) { return type == QSR_F32 ? 4 : type == QSR_BF16 || t
 bool known(int type) { return element_bytes(type) != 0; }
 bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
-// Elements per thread block: one 256-element block per warp where the list is small (more thread blocks, less latency),
-// four where there is work for every multiprocessor many times over.
-int64_t chunk_elements(int64_t total) { return total < int64_t(148) * 8 * 8192 ? 2048 : 8192; }
+constexpr int64_t kWarpBlocks = qsr::kListWarps * kBlock;      // elements of a thread block with one block per warp
+
+// Elements per thread block where every multiprocessor has work many times over: as many blocks per warp as hide the latency of
+// their loads.  fp32 states (operands in registers): four; ViT-B/16's list takes 370 us with four, 376 with three, 391 with two.
+// 8-bit states (operands in shared memory): as many as let four thread blocks share a multiprocessor, at most four; 229 us
+// with three of fp32 parameters and bf16 gradients, 240 with four.
+int stages_of(int stage_bytes)
+{
+    const int fit = stage_bytes == 0 ? qsr::kListStages : 56 * 1024 / (qsr::kListWarps * stage_bytes);
+    return std::max(1, std::min(fit, qsr::kListStages));
+}
+// Small lists: one block per warp, so that more multiprocessors share the work.
+bool is_small(int64_t total) { return total < int64_t(148) * 8 * 8192; }
 
 struct Layout { int64_t tensors, grads, chunks, partial, clip, arrived, bytes, n_chunks, chunk; };
 
-// Where the tables lie in the workspace; n_chunks < 0 is a qsr_status.
-Layout layout_of(const int64_t *numel, int32_t n, int32_t workers)
+// Where the tables lie in the workspace; n_chunks < 0 is a qsr_status.  stages = 0: as much as any types may need.
+Layout layout_of(const int64_t *numel, int32_t n, int32_t workers, int stages)
 {
     Layout l;
     std::memset(&l, 0, sizeof l);
@@ -57,7 +68,7 @@ Layout layout_of(const int64_t *numel, int32_t n, int32_t workers)
         total += numel[i];
         if (total > (int64_t(1) << 48)) { l.n_chunks = QSR_ERANGE; return l; }
     }
-    l.chunk = chunk_elements(total);
+    l.chunk = kWarpBlocks * (is_small(total) ? 1 : stages > 0 ? stages : stages_of(int(kBlock) * 10));
     for (int32_t i = 0; i < n; ++i) l.n_chunks += (numel[i] + l.chunk - 1) / l.chunk;
     if (l.n_chunks > 0x7fffffff) { l.n_chunks = QSR_ERANGE; return l; }
     int64_t at = 0;
@@ -142,12 +153,20 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     const int32_t n = cfg.n_tensors;
     std::vector<int64_t> numel(static_cast<size_t>(n));
     for (int32_t i = 0; i < n; ++i) numel[size_t(i)] = t[i].numel;
-    const Layout l = layout_of(numel.data(), n, cfg.workers);
+    const bool codes = cfg.states == QSR_STATES_E4M3;
+    qsr::ListShape shape{0, 0, 0, t[0].param_type, t[0].grad_type};
+    for (int32_t i = 0; i < n; ++i) {
+        if (t[i].param_type != t[0].param_type || t[i].grad_type != t[0].grad_type) shape.param_type = shape.grad_type = QSR_NONE;
+        if (codes) shape.stage_bytes = std::max(shape.stage_bytes, int(kBlock) * (element_bytes(t[i].param_type) + element_bytes(t[i].grad_type) + 2));
+    }
+    shape.stages = stages_of(shape.stage_bytes);
+    const Layout l = layout_of(numel.data(), n, cfg.workers, shape.stages);
     if (l.n_chunks < 0) return int(l.n_chunks);
     if (!aligned(workspace, 256)) return QSR_EALIGN;
     if (workspace_bytes < l.bytes) return QSR_ERANGE;
 
-    const bool codes = cfg.states == QSR_STATES_E4M3;
+    shape.chunks = l.n_chunks;
+    shape.stages = int(l.chunk / kWarpBlocks);
     std::vector<Range> ranges;
     auto add = [&ranges](const void *p, int64_t bytes, bool written) {
         const uintptr_t b = reinterpret_cast<uintptr_t>(p);
@@ -201,6 +220,7 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     x->arrived = reinterpret_cast<unsigned *>(ws + l.arrived);
     x->has_grads = has_grads;
     x->launches = 0;
+    x->shape = shape;
     cudaError_t err = cudaSuccess;
     try {
         x->host.assign(t, t + n);
@@ -227,7 +247,7 @@ extern "C" {
 int64_t qsr_list_workspace_bytes(const int64_t *numel_host, int32_t n_tensors, int32_t workers)
 {
     if (!numel_host || n_tensors < 1 || workers < 1 || n_tensors % workers != 0) return QSR_EINVAL;
-    const Layout l = layout_of(numel_host, n_tensors, workers);
+    const Layout l = layout_of(numel_host, n_tensors, workers, 0);
     return l.n_chunks < 0 ? l.n_chunks : l.bytes;
 }
 
@@ -280,6 +300,7 @@ int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale)
     p.step_size = float(lr / bc1);
     p.inv_sqrt_bc2 = float(1.0 / std::sqrt(bc2));
     p.grad_scale = float(grad_scale);
+    p.one = 1.0f;
     if (c.clip_norm > 0.0 && std::isfinite(c.clip_norm)) {
         qsr::ListNormParams q;
         std::memset(&q, 0, sizeof q);
@@ -293,7 +314,7 @@ int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale)
         p.clip = list->clip;
     }
     list->launches++;
-    return cuda_rc(cudaError_t(qsr::launch_list_step(p, c.states == QSR_STATES_E4M3, list->chunks, list->stream)));
+    return cuda_rc(cudaError_t(qsr::launch_list_step(p, list->shape, list->stream)));
 }
 
 int qsr_list_sync(qsr_list *list, int32_t state_sync)

@@ -145,6 +145,36 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t w)
     return __half22float2(__half2(h));
 }
 
+// Four codes at once, low byte first.
+__device__ __forceinline__ uint32_t to_e4m3x4(float2 a, float2 b)
+{
+    uint32_t w;
+    asm("{.reg .b16 lo, hi; cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1; cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3; mov.b32 %0, {lo, hi};}"
+        : "=r"(w) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return w;
+}
+__device__ __forceinline__ void from_e4m3x4(float2 &a, float2 &b, uint32_t w)
+{
+    uint32_t x, y;
+    asm("{.reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.rn.f16x2.e4m3x2 %0, lo; cvt.rn.f16x2.e4m3x2 %1, hi;}" : "=r"(x), "=r"(y) : "r"(w));
+    a = __half22float2(*reinterpret_cast<const __half2 *>(&x));
+    b = __half22float2(*reinterpret_cast<const __half2 *>(&y));
+}
+
+// Three-operand extrema (sm_100); NaNs are passed over.
+__device__ __forceinline__ float max3_abs(float a, float b, float c)
+{
+    float y;
+    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float y;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
 // Largest value over the warp; NaNs are passed over.  One instruction on sm_100a.
 __device__ __forceinline__ float warp_max(float x)
 {
