@@ -205,6 +205,17 @@ def qsr_workspace_bytes(cfg: QsrConfig) -> int:
 
 # ---- context --------------------------------------------------------------------------------------------
 
+class _Names(dict):
+    """Name of a torch dtype; kept, because forming it anew costs more than the rest of an argument's check."""
+
+    def __missing__(self, dtype):
+        self[dtype] = name = str(dtype)
+        return name
+
+
+_NAMES = _Names()
+
+
 def _dptr(t) -> Optional[int]:
     """Device address of a torch tensor (or None)."""
     if t is None:
@@ -452,37 +463,41 @@ class TensorList:
 
 # ---- log probabilities of given tokens ------------------------------------------------------------------
 
-def _rows(t, what: str, rows: int, dtype: str, width: Optional[int] = None) -> Optional[int]:
-    """Device address of a contiguous CUDA tensor with `rows` (times `width`) elements of `dtype`; None for None."""
+def _vector(t, what: str, n: int, dtype: str) -> Optional[int]:
+    """Device address of a contiguous CUDA tensor of n elements of `dtype`; None for None."""
     if t is None:
         return None
-    if str(t.dtype) != dtype or t.numel() != rows * (1 if width is None else width) or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {rows * (1 if width is None else width)} x {dtype} is expected")
+    if _NAMES[t.dtype] != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {n} x {dtype} is expected")
     return t.data_ptr()
 
 
-def _matrix(t, what: str):
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a CUDA matrix with adjacent columns is expected")
-    # the stride of a single row means nothing
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+def _matrix(t, shape, what: str):
+    """Row stride of a CUDA matrix with adjacent columns (that of a single row means nothing)."""
+    if len(shape) != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA matrix is expected")
+    if t.is_contiguous():
+        return shape[1]
+    stride = t.stride()
+    if shape[1] > 1 and stride[1] != 1:
+        raise ValueError(f"{what}: a matrix with adjacent columns is expected")
+    return max(stride[0], shape[1]) if shape[0] <= 1 else stride[0]
 
 
 def _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits) -> QsrLogprobArgs:
-    stride, kind = _matrix(logits, "logits"), str(logits.dtype)
-    if kind not in DTYPE:
-        raise ValueError(f"logits: {kind} is not supported (one of {', '.join(sorted(DTYPE))})")
-    R, V = logits.shape
-    a = QsrLogprobArgs(logits=logits.data_ptr(), tokens=_rows(tokens, "tokens", R, "torch.int64"), rows=R, vocab=V, row_stride=stride,
-                       logits_type=DTYPE[kind], inv_temperature=inv_temperature,
-                       entropy=_rows(entropy, "entropy", R, "torch.float32"),
-                       row_stats=_rows(row_stats, "row_stats", R, "torch.float32", 2),
-                       d_logprob=_rows(d_logprob, "d_logprob", R, "torch.float32"),
-                       d_entropy=_rows(d_entropy, "d_entropy", R, "torch.float32"))
+    shape = logits.shape
+    stride, kind = _matrix(logits, shape, "logits"), DTYPE.get(_NAMES[logits.dtype])
+    if kind is None:
+        raise ValueError(f"logits: {logits.dtype} is not supported (one of {', '.join(sorted(DTYPE))})")
+    R, V = shape
+    f32 = "torch.float32"
+    a = QsrLogprobArgs(logits.data_ptr(), _vector(tokens, "tokens", R, "torch.int64"), R, V, stride, kind, 0, inv_temperature, None,
+                       _vector(entropy, "entropy", R, f32), _vector(row_stats, "row_stats", 2 * R, f32), None, None,
+                       _vector(d_logprob, "d_logprob", R, f32), _vector(d_entropy, "d_entropy", R, f32))
     if d_logits is not None:
-        if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype:
+        if d_logits.shape != shape or d_logits.dtype != logits.dtype:
             raise ValueError("d_logits: shape and type of the logits are expected")
-        a.d_logits, a.d_row_stride = d_logits.data_ptr(), _matrix(d_logits, "d_logits")
+        a.d_logits, a.d_row_stride = d_logits.data_ptr(), _matrix(d_logits, shape, "d_logits")
     return a
 
 
@@ -491,15 +506,16 @@ def qsr_token_logprobs(logits, tokens, logprob, entropy=None, row_stats=None, to
     """Log probability of each row's token, with optional entropy, row statistics, top alternatives ([rows, n] tensors, n at
     most QSR_MAX_TOP) and, if d_logits is given, the gradient in the same pass.  All tensors are the caller's."""
     a = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
-    a.logprob = _rows(logprob, "logprob", a.rows, "torch.float32")
+    R = a.rows
+    a.logprob = _vector(logprob, "logprob", R, "torch.float32")
     if (top_logprob is None) != (top_token is None):
         raise ValueError("top_logprob and top_token come together")
     if top_token is not None:
         if top_token.dim() != 2:
             raise ValueError("top_token: [rows, n] is expected")
-        a.n_top = top_token.shape[1]
-        a.top_logprob = _rows(top_logprob, "top_logprob", a.rows, "torch.float32", a.n_top)
-        a.top_token = _rows(top_token, "top_token", a.rows, "torch.int64", a.n_top)
+        a.n_top = n = top_token.shape[1]
+        a.top_logprob = _vector(top_logprob, "top_logprob", R * n, "torch.float32")
+        a.top_token = _vector(top_token, "top_token", R * n, "torch.int64")
     _check(lib().qsr_token_logprobs(C.byref(a), stream), "qsr_token_logprobs")
 
 

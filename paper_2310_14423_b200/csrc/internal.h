@@ -2,6 +2,7 @@
 #ifndef QSR_INTERNAL_H_
 #define QSR_INTERNAL_H_
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -178,6 +179,9 @@ int launch_list_step(const ListStepParams &p, const ListShape &shape, void *stre
 int launch_list_norm(const ListNormParams &p, int64_t chunks, void *stream);
 int launch_list_sync(const ListSyncParams &p, bool states8, bool average, int64_t chunks_per_worker, void *stream);
 int launch_list_reset(const ListSyncParams &p, bool states8, int64_t chunks, void *stream);
+
+// Raises a kernel's limit of dynamic shared memory, once per device (`raised`: a bit for each of the first 64 devices).
+int allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &raised);
 
 // ---- log probabilities of given tokens (logprobs.cu) ----
 

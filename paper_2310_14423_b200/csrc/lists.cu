@@ -655,7 +655,9 @@ int launch_codes(const ListStepParams &p, const ListShape &s, cudaStream_t st)
 {
     const int smem = kWarps * s.stages * s.stage_bytes;
     const auto kernel = list_step_codes_kernel<PT, GT>;
-    if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) return int(err);
+    static std::atomic<uint64_t> raised{0};
+    if (smem > 48 * 1024)
+        if (int err = allow_shared(reinterpret_cast<const void *>(kernel), 56 * 1024, raised)) return err;
     kernel<<<unsigned(s.chunks), kThreads, size_t(smem), st>>>(p, unsigned(s.stage_bytes), unsigned(s.stages));
     return int(cudaGetLastError());
 }
@@ -669,6 +671,17 @@ int launch_codes_grad(const ListStepParams &p, const ListShape &s, cudaStream_t 
 }
 
 }  // namespace
+
+int allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &raised)
+{
+    int dev = 0;
+    if (cudaError_t err = cudaGetDevice(&dev)) return int(err);
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (raised.load(std::memory_order_relaxed) & bit) return 0;
+    if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes)) return int(err);
+    raised.fetch_or(bit, std::memory_order_relaxed);
+    return 0;
+}
 
 int launch_list_step(const ListStepParams &p, const ListShape &s, void *stream)
 {

@@ -9,6 +9,7 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -20,8 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kMaxThreads = 512;
-constexpr int kMaxWarps = kMaxThreads / 32;
+constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;
 constexpr int kGroups = 64;                  // groups of threads whose maxima bound the n-th largest logit from below
@@ -31,6 +31,7 @@ constexpr float kLowest2 = -200.0f;          // 2^-200 = 0 in fp32: log2-probabi
 template <typename T> struct Num;            // how sixteen bytes of a type are taken apart
 template <> struct Num<float> {
     static constexpr int kPer = 4;
+    typedef float Max;                       // running maximum, NaN if a NaN was seen
     static __device__ __forceinline__ void widen(float (&x)[4], uint4 w)
     {
         x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
@@ -41,57 +42,44 @@ template <> struct Num<float> {
     }
     static __device__ __forceinline__ float lowest() { return -infinity(); }
     static __device__ __forceinline__ float to_float(float x) { return x; }
-    static __device__ __forceinline__ float from_float(float x) { return x; }
-    static __device__ __forceinline__ float max_of(float m, uint4 w)
+    static __device__ __forceinline__ Max nothing() { return -infinity(); }
+    static __device__ __forceinline__ Max max_of(Max m, uint4 w)
     {
         float x[4];
         widen(x, w);
         return max_nan(m, max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3])));
     }
+    static __device__ __forceinline__ float value(Max m) { return m; }
 };
-template <> struct Num<__nv_bfloat16> {
+// The two 16-bit types: elements two to a register, extrema of both at once.
+template <typename T, typename T2, int TYPE> struct Num16 {
     static constexpr int kPer = 8;
+    typedef T2 Max;
+    static __device__ __forceinline__ T2 pair(uint32_t w) { return *reinterpret_cast<const T2 *>(&w); }
     static __device__ __forceinline__ void widen(float (&x)[8], uint4 w)
     {
         const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 f = widen2(v[i], QSR_BF16); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+        for (int i = 0; i < 4; ++i) { const float2 f = widen2(v[i], TYPE); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
     }
     static __device__ __forceinline__ uint4 narrow(const float (&x)[8])
     {
-        return make_uint4(narrow2(x[0], x[1], QSR_BF16), narrow2(x[2], x[3], QSR_BF16), narrow2(x[4], x[5], QSR_BF16), narrow2(x[6], x[7], QSR_BF16));
+        return make_uint4(narrow2(x[0], x[1], TYPE), narrow2(x[2], x[3], TYPE), narrow2(x[4], x[5], TYPE), narrow2(x[6], x[7], TYPE));
     }
+    static __device__ __forceinline__ Max nothing() { return pair(TYPE == QSR_BF16 ? 0xff80ff80u : 0xfc00fc00u); }
+    static __device__ __forceinline__ Max max_of(Max m, uint4 w)
+    {
+        return __hmax2_nan(__hmax2_nan(__hmax2_nan(m, pair(w.x)), pair(w.y)), __hmax2_nan(pair(w.z), pair(w.w)));
+    }
+    static __device__ __forceinline__ float value(Max m) { return max_nan(__low2float(m), __high2float(m)); }
+};
+template <> struct Num<__nv_bfloat16> : Num16<__nv_bfloat16, __nv_bfloat162, QSR_BF16> {
     static __device__ __forceinline__ __nv_bfloat16 lowest() { return __ushort_as_bfloat16(0xff80); }
     static __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-    static __device__ __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
-    static __device__ __forceinline__ float max_of(float m, uint4 w)
-    {
-        const __nv_bfloat162 *v = reinterpret_cast<const __nv_bfloat162 *>(&w);
-        const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
-        return max_nan(m, max_nan(__low2float(a), __high2float(a)));
-    }
 };
-template <> struct Num<__half> {
-    static constexpr int kPer = 8;
-    static __device__ __forceinline__ void widen(float (&x)[8], uint4 w)
-    {
-        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 f = widen2(v[i], QSR_F16); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-    }
-    static __device__ __forceinline__ uint4 narrow(const float (&x)[8])
-    {
-        return make_uint4(narrow2(x[0], x[1], QSR_F16), narrow2(x[2], x[3], QSR_F16), narrow2(x[4], x[5], QSR_F16), narrow2(x[6], x[7], QSR_F16));
-    }
+template <> struct Num<__half> : Num16<__half, __half2, QSR_F16> {
     static __device__ __forceinline__ __half lowest() { return __ushort_as_half(0xfc00); }
     static __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-    static __device__ __forceinline__ __half from_float(float x) { return __float2half_rn(x); }
-    static __device__ __forceinline__ float max_of(float m, uint4 w)
-    {
-        const __half2 *v = reinterpret_cast<const __half2 *>(&w);
-        const __half2 a = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
-        return max_nan(m, max_nan(__low2float(a), __high2float(a)));
-    }
 };
 
 // Orders floats as unsigned integers: -inf lowest, -0 = +0, NaN above everything.
@@ -138,42 +126,59 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
     return r;
 }
 
-// One row's slice as a block sees it.
-template <typename T, bool STASH>
+// Reads a granule element by element, -inf outside the row; `first`: row index of its element 0.
+template <typename T>
+__device__ __noinline__ uint4 get_elements(const T *row, int64_t vocab, int64_t first)
+{
+    constexpr int kPer = Num<T>::kPer;
+    union { uint4 w; T e[kPer]; } u;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) u.e[i] = first + i >= 0 && first + i < vocab ? row[first + i] : Num<T>::lowest();
+    return u.w;
+}
+
+// One row's slice as a block sees it: n granules, of which those from `lo` to `hi` lie inside the row entirely.
+template <typename T, bool STASH, int NT>
 struct Slice {
     const T *row;             // the row's first element
-    const char *base;         // `row` rounded down to 16 bytes: granule 0
+    const char *src;          // the slice's granule 0
     uint4 *stash;
-    int64_t vocab;
-    int head;                 // elements of granule 0 that lie before the row
-    int64_t g0, g1;           // granules of this slice
+    int64_t vocab, first0;    // first0: row index of element 0 of granule 0 (negative where the row starts inside the granule)
+    int n, lo, hi;
 
     static constexpr int kPer = Num<T>::kPer;
-    __device__ __forceinline__ int64_t first(int64_t g) const { return g * kPer - head; }     // row index of the granule's element 0
-    __device__ __forceinline__ bool whole(int64_t g) const { return first(g) >= 0 && first(g) + kPer <= vocab; }
 
-    __device__ __forceinline__ uint4 from_global(int64_t g) const
+    __device__ __forceinline__ Slice(const T *r, int64_t v, int part, int log2_parts, uint4 *shared) : row(r), stash(shared), vocab(v)
     {
-        if (whole(g)) return *reinterpret_cast<const uint4 *>(base + g * 16);
-        union { uint4 w; T e[kPer]; } u;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int64_t j = first(g) + i;
-            u.e[i] = j >= 0 && j < vocab ? row[j] : Num<T>::lowest();
-        }
-        return u.w;
+        const uintptr_t address = reinterpret_cast<uintptr_t>(r);
+        const int head = int((address & 15u) / sizeof(T));              // elements of the row's granule 0 that lie before the row
+        const int64_t granules = (head + v + kPer - 1) / kPer;
+        const int64_t g0 = granules * part >> log2_parts, g1 = granules * (part + 1) >> log2_parts;
+        src = reinterpret_cast<const char *>(address & ~uintptr_t(15)) + g0 * 16;
+        first0 = g0 * kPer - head;
+        n = int(g1 - g0);
+        lo = first0 < 0 ? 1 : 0;
+        hi = first0 + int64_t(n) * kPer > v ? n - 1 : n;
     }
-    __device__ __forceinline__ void fetch()
+    __device__ __forceinline__ int64_t first(int i) const { return first0 + int64_t(i) * kPer; }
+    __device__ __forceinline__ bool whole(int i) const { return unsigned(i - lo) < unsigned(hi - lo); }
+    __device__ __forceinline__ uint4 partial(int i) const { return get_elements<T>(row, vocab, first(i)); }
+    __device__ __forceinline__ uint4 from_global(int i) const
+    {
+        return whole(i) ? *reinterpret_cast<const uint4 *>(src + int64_t(i) * 16) : partial(i);
+    }
+    __device__ __forceinline__ void fetch() const
     {
         if constexpr (STASH) {
-            for (int64_t g = g0 + threadIdx.x; g < g1; g += blockDim.x) {
-                if (whole(g)) cp_async16(stash + (g - g0), base + g * 16);
-                else stash[g - g0] = from_global(g);
+#pragma unroll 4
+            for (int i = threadIdx.x; i < n; i += NT) {
+                if (whole(i)) cp_async16(stash + i, src + int64_t(i) * 16);
+                else stash[i] = partial(i);
             }
             asm volatile("cp.async.wait_all;" ::: "memory");      // a thread's own copies: only it reads them back
         }
     }
-    __device__ __forceinline__ uint4 get(int64_t g) const { return STASH ? stash[g - g0] : from_global(g); }
+    __device__ __forceinline__ uint4 get(int i) const { return STASH ? stash[i] : from_global(i); }
 };
 
 struct Shared {
@@ -193,13 +198,12 @@ struct TopShared {
 // The k largest keys of the block's slice to sh.top (0 where the slice has fewer).  The k-th largest of the group maxima bounds
 // the k-th largest element from below, and few elements reach it unless many are equal; those that do are ranked by
 // counting.  If they do not fit (masked or constant rows), or a NaN is about, k rounds of "largest below the last one" follow.
-template <typename T, bool STASH>
-__device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &sh, int k, float thread_max, bool has_nan)
+template <typename T, bool STASH, int NT>
+__device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShared &sh, int k, float thread_max, bool has_nan)
 {
     constexpr int kPer = Num<T>::kPer;
     const int tid = threadIdx.x, lane = tid & 31;
-    const int per_group = blockDim.x > kGroups ? blockDim.x / kGroups : 1;     // a power of two, at most 8 threads
-    const int groups = blockDim.x / per_group;
+    constexpr int per_group = NT > kGroups ? NT / kGroups : 1, groups = NT / per_group;
     float gm = thread_max;
     for (int d = 1; d < per_group; d <<= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, d));
     if (tid % per_group == 0) sh.group[tid / per_group] = gm;
@@ -215,9 +219,9 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &
     __syncthreads();
     const float thr = sh.threshold;
     if (!has_nan) {
-        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+        for (int g = tid; g < sl.n; g += NT) {
             const uint4 w = sl.get(g);
-            if (Num<T>::max_of(-infinity(), w) < thr) continue;
+            if (Num<T>::value(Num<T>::max_of(Num<T>::nothing(), w)) < thr) continue;
             float x[kPer];
             Num<T>::widen(x, w);
 #pragma unroll
@@ -233,7 +237,7 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &
     __syncthreads();
     const unsigned count = sh.count;
     if (!has_nan && count <= kCandidates) {
-        for (unsigned i = tid; i < count; i += blockDim.x) {
+        for (unsigned i = tid; i < count; i += NT) {
             const unsigned long long mine = sh.cand[i];
             int rank = 0;
             for (unsigned j = 0; j < count && rank < k; ++j) rank += sh.cand[j] > mine;
@@ -245,7 +249,7 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &
     unsigned long long last = ~0ull;
     for (int r = 0; r < k; ++r) {
         unsigned long long best = 0ull;
-        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+        for (int g = tid; g < sl.n; g += NT) {
             float x[kPer];
             Num<T>::widen(x, sl.get(g));
 #pragma unroll
@@ -265,7 +269,7 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &
         if (lane == 0) sh.warp_best[tid >> 5] = best;
         __syncthreads();
         if (tid == 0) {
-            for (int i = 1; i < int(blockDim.x >> 5); ++i) best = sh.warp_best[i] > best ? sh.warp_best[i] : best;
+            for (int i = 1; i < NT / 32; ++i) best = sh.warp_best[i] > best ? sh.warp_best[i] : best;
             sh.best = best;
             sh.top[r] = best;
         }
@@ -280,26 +284,26 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH> &sl, TopShared &
 struct RowGrad {
     float m, log2_s, c, hot, A, B;
     int64_t y;
-    bool empty;
 };
 __device__ __forceinline__ RowGrad row_grad(const LogprobParams &p, int64_t r, int64_t y, float m, float ln_s, float H, float nan_or_0)
 {
     RowGrad q;
-    q.empty = m == -infinity();
-    q.m = q.empty ? 0.0f : m;
-    q.log2_s = q.empty ? 0.0f : ln_s * kLog2e;
+    const bool empty = m == -infinity();
+    q.m = empty ? 0.0f : m;
+    q.log2_s = empty ? 0.0f : ln_s * kLog2e;
     q.c = p.tau_log2e;
     q.y = y;
-    const float a = p.d_logprob && y >= 0 && !q.empty ? p.tau * p.d_logprob[r] + nan_or_0 : 0.0f;
-    const float b = p.d_entropy && !q.empty ? p.tau * p.d_entropy[r] : 0.0f;
+    const float a = p.d_logprob && y >= 0 && !empty ? p.tau * p.d_logprob[r] + nan_or_0 : 0.0f;
+    const float b = p.d_entropy && !empty ? p.tau * p.d_entropy[r] : 0.0f;
     q.hot = a;
     q.A = fmaf(b, H, a);
     q.B = b * kLn2;
     return q;
 }
 
-template <typename T>
-__device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q, int64_t first)
+// The gradient of one granule; hot: the element that is the token, or -1.
+template <typename T, bool ENTROPY>
+__device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q, int hot)
 {
     constexpr int kPer = Num<T>::kPer;
     float x[kPer];
@@ -309,28 +313,23 @@ __device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q, int64_t
         const float2 d = add2(make_float2(x[i], x[i + 1]), both(-q.m));
         const float2 l = fma2(d, both(q.c), both(-q.log2_s));
         const float2 e = make_float2(exp2_1(l.x), exp2_1(l.y));
-        float2 f = both(q.A);
-        if (q.B != 0.0f) f = fma2(both(q.B), make_float2(fmaxf(l.x, kLowest2), fmaxf(l.y, kLowest2)), f);
-        const float2 o = mul2(make_float2(-e.x, -e.y), f);
+        float2 f = both(-q.A);
+        if (ENTROPY) f = fma2(both(-q.B), make_float2(fmaxf(l.x, kLowest2), fmaxf(l.y, kLowest2)), f);
+        const float2 o = mul2(e, f);
         x[i] = o.x; x[i + 1] = o.y;
     }
-    const int64_t at = q.y - first;
-    if (at >= 0 && at < kPer && q.hot != 0.0f) {
+    if (hot >= 0) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] += i == int(at) ? q.hot : 0.0f;
+        for (int i = 0; i < kPer; ++i) x[i] += i == hot ? q.hot : 0.0f;
     }
     return Num<T>::narrow(x);
 }
 
-// Writes the granule whose element 0 has row index `first`; `vector`: the output row lies like the input row modulo 16 bytes.
+// Writes a granule element by element; `first`: row index of its element 0.
 template <typename T>
-__device__ __forceinline__ void put_granule(T *out_row, int64_t vocab, int64_t first, bool vector, uint4 w)
+__device__ __noinline__ void put_elements(T *out_row, int64_t vocab, int64_t first, uint4 w)
 {
     constexpr int kPer = Num<T>::kPer;
-    if (vector && first >= 0 && first + kPer <= vocab) {
-        *reinterpret_cast<uint4 *>(out_row + first) = w;
-        return;
-    }
     union { uint4 w; T e[kPer]; } u;
     u.w = w;
 #pragma unroll
@@ -344,49 +343,39 @@ __device__ __forceinline__ bool same_phase(const T *a, const T *b)
     return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// One row per cluster.  TOP: alternatives are wanted; GRAD: d_logits is.
-template <typename T, bool STASH, bool TOP, bool GRAD>
-__global__ void __launch_bounds__(kMaxThreads) logprob_kernel(const LogprobParams p, const int cluster)
+// Where the token lies in a slice: its granule (or -1) and its place there.
+struct HotSpot { int granule, place; };
+template <int PER>
+__device__ __forceinline__ HotSpot hot_spot(const RowGrad &q, int64_t first0, int n)
+{
+    const int64_t at = q.y - first0;
+    if (q.y < 0 || q.hot == 0.0f || at < 0 || at >= int64_t(n) * PER) return HotSpot{-1, -1};
+    return HotSpot{int(at / PER), int(at % PER)};
+}
+
+// Gradient of a thread's granules of a slice.
+template <typename T, bool STASH, int NT, bool ENTROPY>
+__device__ __forceinline__ void write_grad(const Slice<T, STASH, NT> &sl, T *out, const RowGrad &q)
+{
+    const HotSpot hot = hot_spot<Num<T>::kPer>(q, sl.first0, sl.n);
+    // 16-byte stores where the output row lies like the input row modulo 16 bytes
+    const bool vector = same_phase<T>(sl.row, out);
+    char *const dst = reinterpret_cast<char *>(out) + sl.first0 * int64_t(sizeof(T));
+#pragma unroll 2
+    for (int i = threadIdx.x; i < sl.n; i += NT) {
+        const uint4 w = granule_grad<T, ENTROPY>(sl.get(i), q, i == hot.granule ? hot.place : -1);
+        if (vector && sl.whole(i)) *reinterpret_cast<uint4 *>(dst + int64_t(i) * 16) = w;
+        else put_elements<T>(out, sl.vocab, sl.first(i), w);
+    }
+}
+
+// Adds the slice's e = 2^z (and e z), z = c (x - base), to the thread's sums.
+template <typename T, bool STASH, int NT, bool ENTROPY>
+__device__ __forceinline__ void add_terms(const Slice<T, STASH, NT> &sl, float base, float c, float2 &s2, float2 &t2)
 {
     constexpr int kPer = Num<T>::kPer;
-    extern __shared__ uint4 stash[];
-    __shared__ Shared sh;
-    __shared__ typename std::conditional<TOP, TopShared, int>::type top_sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-    const int64_t r = blockIdx.x / cluster;
-    const int rank = int(blockIdx.x % cluster);
-
-    Slice<T, STASH> sl;
-    sl.row = static_cast<const T *>(p.logits) + r * p.stride;
-    const uintptr_t address = reinterpret_cast<uintptr_t>(sl.row);
-    sl.base = reinterpret_cast<const char *>(address & ~uintptr_t(15));
-    sl.head = int((address & 15u) / sizeof(T));
-    sl.vocab = p.vocab;
-    sl.stash = stash;
-    const int64_t granules = (sl.head + p.vocab + kPer - 1) / kPer;
-    sl.g0 = granules * rank / cluster;
-    sl.g1 = granules * (rank + 1) / cluster;
-    const int64_t y = p.tokens[r];
-    float token_logit = 0.0f;
-    if (tid == 0 && rank == 0 && y >= 0) token_logit = y < p.vocab ? Num<T>::to_float(sl.row[y]) : quiet_nan();
-
-    // a block's shared memory may only be written by another once both run: announced here, awaited before the first write
-    if (TOP && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    sl.fetch();
-    // largest logit of the slice, NaN if there is one
-    float thread_max = -infinity();
-    for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) thread_max = Num<T>::max_of(thread_max, sl.get(g));
-    float m = warp_max_nan(thread_max);
-    if (warps > 1) {
-        if (lane == 0) sh.m[warp] = m;
-        __syncthreads();
-        m = sh.m[0];
-        for (int i = 1; i < warps; ++i) m = max_nan(m, sh.m[i]);
-    }
-    // sums relative to it
-    const float base = m == -infinity() ? 0.0f : m, c = p.tau_log2e;
-    float2 s2 = both(0.0f), t2 = both(0.0f);
-    for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x) {
+#pragma unroll 2
+    for (int g = threadIdx.x; g < sl.n; g += NT) {
         float x[kPer];
         Num<T>::widen(x, sl.get(g));
 #pragma unroll
@@ -394,19 +383,59 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(const LogprobParam
             const float2 z = mul2(add2(make_float2(x[i], x[i + 1]), both(-base)), both(c));
             const float2 e = make_float2(exp2_1(z.x), exp2_1(z.y));
             s2 = add2(s2, e);
-            t2 = fma2(e, make_float2(fmaxf(z.x, kLowest2), fmaxf(z.y, kLowest2)), t2);
+            if (ENTROPY) t2 = fma2(e, make_float2(fmaxf(z.x, kLowest2), fmaxf(z.y, kLowest2)), t2);
         }
     }
+}
+
+// One row per cluster.  TOP: alternatives are wanted; GRAD: d_logits is.
+template <typename T, bool STASH, int NT, bool TOP, bool GRAD>
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_constant__ LogprobParams p, const int log2_cluster)
+{
+    constexpr int kPer = Num<T>::kPer;
+    extern __shared__ uint4 stash[];
+    __shared__ Shared sh;
+    __shared__ typename std::conditional<TOP, TopShared, int>::type top_sh;
+    constexpr int warps = NT / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cluster = 1 << log2_cluster;
+    const int64_t r = blockIdx.x >> log2_cluster;
+    const int rank = int(blockIdx.x) & (cluster - 1);
+
+    const T *const row = static_cast<const T *>(p.logits) + r * p.stride;
+    const Slice<T, STASH, NT> sl(row, p.vocab, rank, log2_cluster, stash);
+    const int64_t y = p.tokens[r];
+    float token_logit = 0.0f;
+    if (tid == 0 && rank == 0 && y >= 0) token_logit = y < p.vocab ? Num<T>::to_float(row[y]) : quiet_nan();
+
+    // a block's shared memory may only be written by another once both run: announced here, awaited before the first write
+    if (TOP && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    sl.fetch();
+    // largest logit of the slice, NaN if there is one
+    typename Num<T>::Max running = Num<T>::nothing();
+#pragma unroll 4
+    for (int i = tid; i < sl.n; i += NT) running = Num<T>::max_of(running, sl.get(i));
+    const float thread_max = Num<T>::value(running);
+    float m = warp_max_nan(thread_max);
+    if (warps > 1) {
+        if (lane == 0) sh.m[warp] = m;
+        __syncthreads();
+        m = warp_max_nan(sh.m[lane < warps ? lane : 0]);
+    }
+    // sums relative to it
+    const float base = m == -infinity() ? 0.0f : m, c = p.tau_log2e;
+    float2 s2 = both(0.0f), t2 = both(0.0f);
+    if (p.entropy || p.d_entropy) add_terms<T, STASH, NT, true>(sl, base, c, s2, t2);
+    else add_terms<T, STASH, NT, false>(sl, base, c, s2, t2);
     float s = warp_sum(s2.x + s2.y), t = warp_sum(t2.x + t2.y);
     if (warps > 1) {
         if (lane == 0) { sh.s[warp] = s; sh.t[warp] = t; }
         __syncthreads();
-        s = t = 0.0f;
-        for (int i = 0; i < warps; ++i) { s += sh.s[i]; t += sh.t[i]; }
+        s = warp_sum(lane < warps ? sh.s[lane] : 0.0f);
+        t = warp_sum(lane < warps ? sh.t[lane] : 0.0f);
     }
     Sums all{m, s, t};
     if (!(m < infinity())) all.m = all.s = quiet_nan();       // a NaN or +inf: the row is NaN
-    if (TOP) slice_top<T, STASH>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(m));
+    if (TOP) slice_top<T, STASH, NT>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(m));
     if (cluster > 1) {
         cg::cluster_group cl = cg::this_cluster();
         if (tid == 0) sh.part = all;
@@ -436,7 +465,7 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(const LogprobParam
             TopShared &mine = reinterpret_cast<TopShared &>(top_sh);
             if (cluster > 1) {
                 const int n = cluster * p.n_top;
-                for (int i = tid; i < n; i += blockDim.x) {
+                for (int i = tid; i < n; i += NT) {
                     const unsigned long long key = mine.gathered[i];
                     int place = 0;
                     for (int j = 0; j < n; ++j) place += mine.gathered[j] > key;
@@ -454,113 +483,121 @@ __global__ void __launch_bounds__(kMaxThreads) logprob_kernel(const LogprobParam
     if (GRAD) {
         __syncthreads();              // d_logits may be the logits: the token's logit has been read
         const RowGrad q = row_grad(p, r, y, all.m, ln_s, H, y < p.vocab ? 0.0f : quiet_nan());
-        T *out = static_cast<T *>(p.d_logits) + r * p.d_stride;
-        const bool vector = same_phase<T>(sl.row, out);
-        for (int64_t g = sl.g0 + tid; g < sl.g1; g += blockDim.x)
-            put_granule<T>(out, p.vocab, sl.first(g), vector, granule_grad<T>(sl.get(g), q, sl.first(g)));
+        T *const out = static_cast<T *>(p.d_logits) + r * p.d_stride;
+        if (q.B == 0.0f) write_grad<T, STASH, NT, false>(sl, out, q);
+        else write_grad<T, STASH, NT, true>(sl, out, q);
     }
 }
 
-constexpr int kGradThreads = 256;
 constexpr int kGradPer = 4;                   // granules in flight per thread
 
-// The gradient alone, from the statistics of an earlier call.  Grid: parts of a row by rows.
-template <typename T>
-__global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const LogprobParams p, const int parts)
+// The gradient alone, from the statistics of an earlier call.  Grid: 2^log2_parts parts of a row by rows.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT) logprob_grad_kernel(const __grid_constant__ LogprobParams p, const int log2_parts)
 {
-    constexpr int kPer = Num<T>::kPer;
-    const int64_t r = blockIdx.x / parts;
-    const int part = int(blockIdx.x % parts);
-    Slice<T, false> sl;
-    sl.row = static_cast<const T *>(p.logits) + r * p.stride;
-    const uintptr_t address = reinterpret_cast<uintptr_t>(sl.row);
-    sl.base = reinterpret_cast<const char *>(address & ~uintptr_t(15));
-    sl.head = int((address & 15u) / sizeof(T));
-    sl.vocab = p.vocab;
-    const int64_t granules = (sl.head + p.vocab + kPer - 1) / kPer;
-    const int64_t g0 = granules * part / parts + threadIdx.x, g1 = granules * (part + 1) / parts;
+    const int64_t r = blockIdx.x >> log2_parts;
+    const T *const row = static_cast<const T *>(p.logits) + r * p.stride;
+    const Slice<T, false, NT> sl(row, p.vocab, int(blockIdx.x) & ((1 << log2_parts) - 1), log2_parts, nullptr);
+    constexpr int step = NT;
+    const int begin = threadIdx.x;
     uint4 w[kGradPer];
 #pragma unroll
-    for (int i = 0; i < kGradPer; ++i)
-        if (g0 + i * int64_t(blockDim.x) < g1) w[i] = sl.from_global(g0 + i * int64_t(blockDim.x));
+    for (int k = 0; k < kGradPer; ++k)
+        if (begin + k * step < sl.n) w[k] = sl.from_global(begin + k * step);
     const int64_t y = p.tokens[r];
     const RowGrad q = row_grad(p, r, y, p.stats[2 * r], p.stats[2 * r + 1], p.d_entropy ? p.entropy[r] : 0.0f,
                                y < p.vocab ? 0.0f : quiet_nan());
-    T *out = static_cast<T *>(p.d_logits) + r * p.d_stride;
-    const bool vector = same_phase<T>(sl.row, out);
+    T *const out = static_cast<T *>(p.d_logits) + r * p.d_stride;
+    const HotSpot hot = hot_spot<Num<T>::kPer>(q, sl.first0, sl.n);
+    const bool vector = same_phase<T>(row, out);
+    char *const dst = reinterpret_cast<char *>(out) + sl.first0 * int64_t(sizeof(T));
 #pragma unroll
-    for (int i = 0; i < kGradPer; ++i) {
-        const int64_t g = g0 + i * int64_t(blockDim.x);
-        if (g < g1) put_granule<T>(out, p.vocab, sl.first(g), vector, granule_grad<T>(w[i], q, sl.first(g)));
+    for (int k = 0; k < kGradPer; ++k) {
+        const int i = begin + k * step;
+        if (i < sl.n) {
+            const int place = i == hot.granule ? hot.place : -1;
+            const uint4 d = q.B == 0.0f ? granule_grad<T, false>(w[k], q, place) : granule_grad<T, true>(w[k], q, place);
+            if (vector && sl.whole(i)) *reinterpret_cast<uint4 *>(dst + int64_t(i) * 16) = d;
+            else put_elements<T>(out, p.vocab, sl.first(i), d);
+        }
     }
 }
 
-constexpr int64_t kSliceBytes = 64 * 1024;    // three blocks of such a slice share a multiprocessor
+constexpr int64_t kSliceBytes = 110 * 1024;   // two blocks of such a slice share a multiprocessor
 constexpr int64_t kStashMax = 200 * 1024;
 constexpr int kMultiprocessors = 148;
 
-struct Shape { int cluster, threads; int64_t smem; };
+struct Shape { int log2_cluster, threads; int64_t smem; };
 
 Shape shape_of(const LogprobParams &p, int element)
 {
     const int64_t bytes = (p.vocab * element + 15 + 15) / 16 * 16;
     Shape s;
-    s.cluster = 1;
-    while (s.cluster < kMaxCluster && (bytes > kSliceBytes * s.cluster ||
-                                       (p.rows * s.cluster * 2 <= kMultiprocessors && bytes >= 8192 * s.cluster)))
-        s.cluster *= 2;
-    const int64_t granules = (bytes / 16 + s.cluster - 1) / s.cluster + 1;
-    const int64_t each = p.rows * s.cluster <= kMultiprocessors ? 4 : 8;       // granules per thread
-    s.threads = 32;
-    while (s.threads < kMaxThreads && s.threads * each < granules) s.threads *= 2;
+    s.log2_cluster = 0;
+    while (1 << s.log2_cluster < kMaxCluster &&
+           (bytes > kSliceBytes << s.log2_cluster || ((p.rows << s.log2_cluster) * 2 <= kMultiprocessors && bytes >= int64_t(8192) << s.log2_cluster)))
+        s.log2_cluster++;
+    const int64_t granules = ((bytes / 16 - 1) >> s.log2_cluster) + 2;
+    s.threads = granules <= 256 ? 32 : granules <= 1024 ? 128 : 256;
     s.smem = granules * 16;
     return s;
 }
 
-template <typename T, bool STASH, bool TOP, bool GRAD>
+template <typename T, bool STASH, int NT, bool TOP, bool GRAD>
 int launch_instance(const LogprobParams &p, const Shape &s, cudaStream_t st)
 {
-    const auto kernel = logprob_kernel<T, STASH, TOP, GRAD>;
+    const auto kernel = logprob_kernel<T, STASH, NT, TOP, GRAD>;
     const size_t smem = STASH ? size_t(s.smem) : 0;
-    if (smem > 32 * 1024)
-        if (cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem))) return int(err);
+    if (smem > 32 * 1024) {
+        static std::atomic<uint64_t> raised{0};           // devices on which this instance may use kStashMax
+        if (int err = allow_shared(reinterpret_cast<const void *>(kernel), int(kStashMax), raised)) return err;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(p.rows * s.cluster));
-    cfg.blockDim = dim3(unsigned(s.threads));
+    cfg.gridDim = dim3(unsigned(p.rows << s.log2_cluster));
+    cfg.blockDim = dim3(NT);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = unsigned(s.cluster);
+    attr[0].val.clusterDim.x = 1u << s.log2_cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = s.cluster > 1 ? 1 : 0;
-    return int(cudaLaunchKernelEx(&cfg, kernel, p, s.cluster));
+    cfg.numAttrs = s.log2_cluster > 0 ? 1 : 0;
+    return int(cudaLaunchKernelEx(&cfg, kernel, p, s.log2_cluster));
+}
+
+template <typename T, bool STASH, int NT>
+int launch_outputs(const LogprobParams &p, const Shape &s, cudaStream_t st)
+{
+    if (p.n_top > 0) return p.d_logits ? launch_instance<T, STASH, NT, true, true>(p, s, st) : launch_instance<T, STASH, NT, true, false>(p, s, st);
+    return p.d_logits ? launch_instance<T, STASH, NT, false, true>(p, s, st) : launch_instance<T, STASH, NT, false, false>(p, s, st);
 }
 
 template <typename T>
 int launch_typed(const LogprobParams &p, cudaStream_t st)
 {
     const Shape s = shape_of(p, int(sizeof(T)));
-    const bool stash = s.smem <= kStashMax, top = p.n_top > 0, grad = p.d_logits != nullptr;
-    if (stash) {
-        if (top) return grad ? launch_instance<T, true, true, true>(p, s, st) : launch_instance<T, true, true, false>(p, s, st);
-        return grad ? launch_instance<T, true, false, true>(p, s, st) : launch_instance<T, true, false, false>(p, s, st);
-    }
-    if (top) return grad ? launch_instance<T, false, true, true>(p, s, st) : launch_instance<T, false, true, false>(p, s, st);
-    return grad ? launch_instance<T, false, false, true>(p, s, st) : launch_instance<T, false, false, false>(p, s, st);
+    if (s.smem > kStashMax) return launch_outputs<T, false, 256>(p, s, st);
+    if (s.threads == 32) return launch_outputs<T, true, 32>(p, s, st);
+    if (s.threads == 128) return launch_outputs<T, true, 128>(p, s, st);
+    return launch_outputs<T, true, 256>(p, s, st);
+}
+
+template <typename T, int NT>
+int launch_grad_instance(const LogprobParams &p, int64_t granules, cudaStream_t st)
+{
+    int log2_parts = 0;
+    while ((granules >> log2_parts) + 1 > NT * kGradPer) log2_parts++;
+    if (p.rows > (0x7fffffff >> log2_parts)) return int(cudaErrorInvalidConfiguration);
+    logprob_grad_kernel<T, NT><<<unsigned(p.rows << log2_parts), NT, 0, st>>>(p, log2_parts);
+    return int(cudaGetLastError());
 }
 
 template <typename T>
 int launch_grad_typed(const LogprobParams &p, cudaStream_t st)
 {
     const int64_t granules = (p.vocab * int64_t(sizeof(T)) + 15 + 15) / 16;
-    int threads = 32;
-    while (threads < kGradThreads && threads * kGradPer < granules) threads *= 2;
-    const int64_t parts = (granules + threads * kGradPer - 1) / (threads * kGradPer);
-    if (parts * p.rows > 0x7fffffff) return int(cudaErrorInvalidConfiguration);
-    logprob_grad_kernel<T><<<unsigned(parts * p.rows), threads, 0, st>>>(p, int(parts));
-    return int(cudaGetLastError());
+    return granules <= 32 * kGradPer ? launch_grad_instance<T, 32>(p, granules, st) : launch_grad_instance<T, 256>(p, granules, st);
 }
 
 }  // namespace
