@@ -21,11 +21,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kMaxWarps = 8;
+constexpr int kMaxWarps = 16;
 constexpr int kMaxCluster = 8;
 constexpr int kCandidates = 1024;
+constexpr int kGroup = 4;                    // granules a thread loads and sums up at a time
 constexpr int kGroups = 64;                  // groups of threads whose maxima bound the n-th largest logit from below
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kFastMax = 1e30f;            // logits (and scaled ones) below this leave room for every difference and product
 constexpr float kLowest2 = -200.0f;          // 2^-200 = 0 in fp32: log2-probabilities below are raised to it, so that 0 * (-inf) never forms
 
 template <typename T> struct Num;            // how sixteen bytes of a type are taken apart
@@ -159,6 +161,7 @@ struct Slice {
         n = int(g1 - g0);
         lo = first0 < 0 ? 1 : 0;
         hi = first0 + int64_t(n) * kPer > v ? n - 1 : n;
+        if (hi < lo) hi = lo;                                           // one granule, partial at both ends
     }
     __device__ __forceinline__ int64_t first(int i) const { return first0 + int64_t(i) * kPer; }
     __device__ __forceinline__ bool whole(int i) const { return unsigned(i - lo) < unsigned(hi - lo); }
@@ -167,22 +170,42 @@ struct Slice {
     {
         return whole(i) ? *reinterpret_cast<const uint4 *>(src + int64_t(i) * 16) : partial(i);
     }
+    // Starts the copies of the thread's granules, kGroup to a group; only the thread itself reads them back.
     __device__ __forceinline__ void fetch() const
     {
         if constexpr (STASH) {
-#pragma unroll 4
-            for (int i = threadIdx.x; i < n; i += NT) {
-                if (whole(i)) cp_async16(stash + i, src + int64_t(i) * 16);
-                else stash[i] = partial(i);
+            const char *from = src + threadIdx.x * 16;
+            uint4 *to = stash + threadIdx.x;
+            for (int i = threadIdx.x; i < n; i += kGroup * NT, from += kGroup * NT * 16, to += kGroup * NT) {
+                if (i >= lo && i + (kGroup - 1) * NT < hi) {
+#pragma unroll
+                    for (int k = 0; k < kGroup; ++k) cp_async16(to + k * NT, from + k * NT * 16);
+                } else {
+                    for (int k = 0; k < kGroup; ++k) {
+                        const int g = i + k * NT;
+                        if (whole(g)) cp_async16(to + k * NT, from + k * NT * 16);
+                        else if (g < n) to[k * NT] = partial(g);
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");      // a thread's own copies: only it reads them back
+        }
+    }
+    // Until all but the `later` youngest groups have arrived.
+    __device__ __forceinline__ void wait(int later) const
+    {
+        if constexpr (STASH) {
+            if (later >= 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+            else if (later == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            else if (later == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
     }
     __device__ __forceinline__ uint4 get(int i) const { return STASH ? stash[i] : from_global(i); }
 };
 
 struct Shared {
-    float m[kMaxWarps], s[kMaxWarps], t[kMaxWarps];
+    float warp[3][kMaxWarps];                          // the warps' maxima and sums
     Sums part;                                         // this block's, read by the whole cluster
 };
 struct TopShared {
@@ -213,6 +236,7 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShar
     if (tid < groups && !has_nan) {
         const float mine = sh.group[tid];
         int rank = 0;
+#pragma unroll 16
         for (int i = 0; i < groups; ++i) rank += sh.group[i] > mine || (sh.group[i] == mine && i < tid);
         if (rank == k - 1) sh.threshold = mine;
     }
@@ -240,7 +264,8 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShar
         for (unsigned i = tid; i < count; i += NT) {
             const unsigned long long mine = sh.cand[i];
             int rank = 0;
-            for (unsigned j = 0; j < count && rank < k; ++j) rank += sh.cand[j] > mine;
+#pragma unroll 8
+            for (unsigned j = 0; j < count; ++j) rank += sh.cand[j] > mine;
             if (rank < k) sh.top[rank] = mine;
         }
         __syncthreads();
@@ -280,10 +305,13 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShar
     __syncthreads();
 }
 
-// Per-row scalars of the gradient: d = a [j = y] - p (A + B log2 p), p = 2^(z - log2 S).
+// Per-row scalars of the gradient: d = a [j = y] - p (A + B log2 p) with log2 p = c (x - m) - log2 S.
+// fast: log2 p = l - delta with l = c x - L in one operation, L a rounded c m + log2 S and delta what it lacks; delta goes
+// into A and B, so no accuracy is lost.
 struct RowGrad {
-    float m, log2_s, c, hot, A, B;
+    float m, log2_s, c, L, hot, A, B;
     int64_t y;
+    bool fast;
 };
 __device__ __forceinline__ RowGrad row_grad(const LogprobParams &p, int64_t r, int64_t y, float m, float ln_s, float H, float nan_or_0)
 {
@@ -298,30 +326,52 @@ __device__ __forceinline__ RowGrad row_grad(const LogprobParams &p, int64_t r, i
     q.hot = a;
     q.A = fmaf(b, H, a);
     q.B = b * kLn2;
+    const float K = q.c * q.m;
+    q.L = K + q.log2_s;
+    q.fast = fabsf(K) < kFastMax && fabsf(q.m) < kFastMax;
+    if (q.fast) {
+        // c m + log2 S - L, each step exact or as small as what it corrects
+        const float delta = fmaf(q.c, q.m, -K) + ((K - q.L) + q.log2_s), f = exp2_1(-delta);
+        q.A = f * fmaf(-q.B, delta, q.A);
+        q.B *= f;
+    }
     return q;
 }
 
-// The gradient of one granule; hot: the element that is the token, or -1.
-template <typename T, bool ENTROPY>
-__device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q, int hot)
+template <typename T, bool ENTROPY, bool FAST>
+__device__ __forceinline__ void grad_terms(float (&x)[Num<T>::kPer], uint4 w, const RowGrad &q)
 {
-    constexpr int kPer = Num<T>::kPer;
-    float x[kPer];
     Num<T>::widen(x, w);
 #pragma unroll
-    for (int i = 0; i < kPer; i += 2) {
-        const float2 d = add2(make_float2(x[i], x[i + 1]), both(-q.m));
-        const float2 l = fma2(d, both(q.c), both(-q.log2_s));
+    for (int i = 0; i < Num<T>::kPer; i += 2) {
+        const float2 v = make_float2(x[i], x[i + 1]);
+        const float2 l = FAST ? fma2(v, both(q.c), both(-q.L)) : fma2(add2(v, both(-q.m)), both(q.c), both(-q.log2_s));
         const float2 e = make_float2(exp2_1(l.x), exp2_1(l.y));
         float2 f = both(-q.A);
         if (ENTROPY) f = fma2(both(-q.B), make_float2(fmaxf(l.x, kLowest2), fmaxf(l.y, kLowest2)), f);
         const float2 o = mul2(e, f);
         x[i] = o.x; x[i + 1] = o.y;
     }
-    if (hot >= 0) {
+}
+// The gradient of one granule, the token's own term aside.
+template <typename T, bool ENTROPY, bool FAST>
+__device__ __forceinline__ uint4 granule_grad(uint4 w, const RowGrad &q)
+{
+    constexpr int kPer = Num<T>::kPer;
+    float x[kPer];
+    grad_terms<T, ENTROPY, FAST>(x, w, q);
+    return Num<T>::narrow(x);
+}
+// The gradient of the granule that holds the token, at `place`.
+template <typename T>
+__device__ __forceinline__ uint4 token_grad(uint4 w, const RowGrad &q, int place)
+{
+    constexpr int kPer = Num<T>::kPer;
+    float x[kPer];
+    if (q.fast) grad_terms<T, true, true>(x, w, q);
+    else grad_terms<T, true, false>(x, w, q);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] += i == hot ? q.hot : 0.0f;
-    }
+    for (int i = 0; i < kPer; ++i) x[i] += i == place ? q.hot : 0.0f;
     return Num<T>::narrow(x);
 }
 
@@ -353,51 +403,174 @@ __device__ __forceinline__ HotSpot hot_spot(const RowGrad &q, int64_t first0, in
     return HotSpot{int(at / PER), int(at % PER)};
 }
 
-// Gradient of a thread's granules of a slice.
-template <typename T, bool STASH, int NT, bool ENTROPY>
+// Gradient of a thread's granules of a slice.  The granule that holds the token is written twice, the second time with the
+// token's term, so that the loop need not look for it.
+template <typename T, bool STASH, int NT, bool ENTROPY, bool FAST>
 __device__ __forceinline__ void write_grad(const Slice<T, STASH, NT> &sl, T *out, const RowGrad &q)
 {
     const HotSpot hot = hot_spot<Num<T>::kPer>(q, sl.first0, sl.n);
+    const int tid = threadIdx.x;
+    const bool mine = hot.granule >= 0 && hot.granule % NT == tid;
+    uint4 token_granule = make_uint4(0u, 0u, 0u, 0u);
+    if (mine) token_granule = sl.get(hot.granule);            // before it is overwritten: out may be the logits
     // 16-byte stores where the output row lies like the input row modulo 16 bytes
     const bool vector = same_phase<T>(sl.row, out);
-    char *const dst = reinterpret_cast<char *>(out) + sl.first0 * int64_t(sizeof(T));
-#pragma unroll 2
-    for (int i = threadIdx.x; i < sl.n; i += NT) {
-        const uint4 w = granule_grad<T, ENTROPY>(sl.get(i), q, i == hot.granule ? hot.place : -1);
-        if (vector && sl.whole(i)) *reinterpret_cast<uint4 *>(dst + int64_t(i) * 16) = w;
-        else put_elements<T>(out, sl.vocab, sl.first(i), w);
+    if (vector) {
+        int i = tid < sl.lo ? tid + NT : tid;
+        char *dst = reinterpret_cast<char *>(out) + sl.first0 * int64_t(sizeof(T)) + int64_t(i) * 16;
+#pragma unroll 4
+        for (; i < sl.hi; i += NT, dst += NT * 16) *reinterpret_cast<uint4 *>(dst) = granule_grad<T, ENTROPY, FAST>(sl.get(i), q);
+        if (tid < sl.lo) put_elements<T>(out, sl.vocab, sl.first(0), granule_grad<T, ENTROPY, FAST>(sl.get(0), q));
+        if (sl.hi < sl.n && sl.hi % NT == tid)
+            put_elements<T>(out, sl.vocab, sl.first(sl.hi), granule_grad<T, ENTROPY, FAST>(sl.get(sl.hi), q));
+    } else {
+        for (int i = tid; i < sl.n; i += NT) put_elements<T>(out, sl.vocab, sl.first(i), granule_grad<T, ENTROPY, FAST>(sl.get(i), q));
     }
+    if (mine) put_elements<T>(out, sl.vocab, sl.first(hot.granule), token_grad<T>(token_granule, q, hot.place));
 }
 
-// Adds the slice's e = 2^z (and e z), z = c (x - base), to the thread's sums.
-template <typename T, bool STASH, int NT, bool ENTROPY>
-__device__ __forceinline__ void add_terms(const Slice<T, STASH, NT> &sl, float base, float c, float2 &s2, float2 &t2)
+// A thread's running maximum and sums: e = 2^z and e z with z = c x - K, K a rounded c m.  One operation forms z and nothing is
+// lost by it: the product is exact inside the fused multiply-add, and K is the same constant in every term; what K lacks of
+// c m is put back at the end (relative_to).  `odd`: a NaN, an infinity or a maximum so large that c x may overflow.
+template <bool ENTROPY>
+struct Running {
+    float m = -infinity(), K = 0.0f;
+    float2 s = make_float2(0.0f, 0.0f), t = make_float2(0.0f, 0.0f);
+    bool odd = false;
+
+    template <typename T, int N>
+    __device__ __forceinline__ void add(const uint4 (&w)[N], float c)
+    {
+        constexpr int kPer = Num<T>::kPer;
+        typename Num<T>::Max most = Num<T>::nothing();
+#pragma unroll
+        for (int k = 0; k < N; ++k) most = Num<T>::max_of(most, w[k]);
+        const float x = Num<T>::value(most);
+        if (!(x <= m)) {
+            const float K1 = x * c;
+            odd = odd || !(fabsf(x) < kFastMax) || !(fabsf(K1) < kFastMax);
+            if (m > -infinity()) shift(K - K1);
+            m = x;
+            K = K1;
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float v[kPer];
+            Num<T>::widen(v, w[k]);
+#pragma unroll
+            for (int i = 0; i < kPer; i += 2) {
+                const float2 z = fma2(make_float2(v[i], v[i + 1]), both(c), both(-K));
+                const float2 e = make_float2(exp2_1(z.x), exp2_1(z.y));
+                s = add2(s, e);
+                if (ENTROPY) t = fma2(e, make_float2(fmaxf(z.x, kLowest2), fmaxf(z.y, kLowest2)), t);
+            }
+        }
+    }
+    // Sums relative to a base d below the present one (d <= 0 where the base rises).
+    __device__ __forceinline__ void shift(float d)
+    {
+        const float f = exp2_1(d);
+        d = fmaxf(d, kLowest2);
+        if (ENTROPY) t = mul2(both(f), fma2(both(d), s, t));
+        s = mul2(both(f), s);
+    }
+    __device__ __forceinline__ Sums relative_to(float most, float c)
+    {
+        if (m > -infinity()) shift(fmaf(-c, most, K));
+        return Sums{most, s.x + s.y, t.x + t.y};
+    }
+};
+
+// The slow way for slices that are `odd`: the maximum first (NaN if there is one), then the terms with z = c (x - m).
+template <typename T, bool STASH, int NT>
+__device__ __forceinline__ Sums sums_of_odd(const Slice<T, STASH, NT> &sl, float c, Shared &sh)
 {
     constexpr int kPer = Num<T>::kPer;
-#pragma unroll 2
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    typename Num<T>::Max running = Num<T>::nothing();
+    for (int g = threadIdx.x; g < sl.n; g += NT) running = Num<T>::max_of(running, sl.get(g));
+    float m = warp_max_nan(Num<T>::value(running));
+    __syncthreads();
+    if (lane == 0) sh.warp[0][warp] = m;
+    __syncthreads();
+    m = warp_max_nan(sh.warp[0][lane < NT / 32 ? lane : 0]);
+    const float base = m == -infinity() ? 0.0f : m;
+    float s = 0.0f, t = 0.0f;
     for (int g = threadIdx.x; g < sl.n; g += NT) {
         float x[kPer];
         Num<T>::widen(x, sl.get(g));
 #pragma unroll
-        for (int i = 0; i < kPer; i += 2) {
-            const float2 z = mul2(add2(make_float2(x[i], x[i + 1]), both(-base)), both(c));
-            const float2 e = make_float2(exp2_1(z.x), exp2_1(z.y));
-            s2 = add2(s2, e);
-            if (ENTROPY) t2 = fma2(e, make_float2(fmaxf(z.x, kLowest2), fmaxf(z.y, kLowest2)), t2);
+        for (int i = 0; i < kPer; ++i) {
+            const float z = (x[i] - base) * c, e = exp2_1(z);
+            s += e;
+            t = fmaf(e, fmaxf(z, kLowest2), t);
         }
     }
+    s = warp_sum(s);
+    t = warp_sum(t);
+    if (lane == 0) { sh.warp[1][warp] = s; sh.warp[2][warp] = t; }
+    __syncthreads();
+    s = warp_sum(lane < NT / 32 ? sh.warp[1][lane] : 0.0f);
+    t = warp_sum(lane < NT / 32 ? sh.warp[2][lane] : 0.0f);
+    Sums all{m, s, t};
+    if (!(m < infinity())) all.m = all.s = quiet_nan();       // a NaN or +inf: the row is NaN
+    return all;
+}
+
+// The slice's maximum and sums, the same in every thread of the block; thread_max: the thread's own maximum (NaNs aside).
+template <typename T, bool STASH, int NT, bool ENTROPY>
+__device__ __forceinline__ Sums sums_of(const Slice<T, STASH, NT> &sl, float c, Shared &sh, float &thread_max)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    Running<ENTROPY> run;
+    const int mine = sl.n > tid ? (sl.n - tid + NT - 1) / NT : 0;
+    int i = tid, later = (mine + kGroup - 1) / kGroup;
+    for (; i + (kGroup - 1) * NT < sl.n; i += kGroup * NT) {
+        sl.wait(--later);
+        uint4 w[kGroup];
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) w[k] = sl.get(i + k * NT);
+        run.template add<T>(w, c);
+    }
+    sl.wait(0);
+    for (; i < sl.n; i += NT) {
+        const uint4 w[1] = {sl.get(i)};
+        run.template add<T>(w, c);
+    }
+    thread_max = run.m;
+    const float m = warp_max(run.m);
+    Sums all = run.relative_to(m, c);
+    all.s = warp_sum(all.s);
+    if (ENTROPY) all.t = warp_sum(all.t);
+    bool odd = run.odd;
+    if (NT == 32) odd = __any_sync(0xffffffffu, odd);
+    else {
+        if (lane == 0) { sh.warp[0][warp] = all.m; sh.warp[1][warp] = all.s; sh.warp[2][warp] = all.t; }
+        odd = __syncthreads_or(odd);
+        all.m = -infinity();
+        all.s = all.t = 0.0f;
+        if (lane < NT / 32) all = Sums{sh.warp[0][lane], sh.warp[1][lane], sh.warp[2][lane]};
+        const float most = warp_max(all.m);
+        if (all.s > 0.0f) {
+            const float d = (all.m - most) * c, f = exp2_1(d);
+            all.t = f * fmaf(fmaxf(d, kLowest2), all.s, all.t);
+            all.s *= f;
+        }
+        all.m = most;
+        all.s = warp_sum(all.s);
+        all.t = warp_sum(all.t);
+    }
+    return odd ? sums_of_odd<T, STASH, NT>(sl, c, sh) : all;
 }
 
 // One row per cluster.  TOP: alternatives are wanted; GRAD: d_logits is.
 template <typename T, bool STASH, int NT, bool TOP, bool GRAD>
 __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_constant__ LogprobParams p, const int log2_cluster)
 {
-    constexpr int kPer = Num<T>::kPer;
     extern __shared__ uint4 stash[];
     __shared__ Shared sh;
     __shared__ typename std::conditional<TOP, TopShared, int>::type top_sh;
-    constexpr int warps = NT / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cluster = 1 << log2_cluster;
+    const int tid = threadIdx.x, cluster = 1 << log2_cluster;
     const int64_t r = blockIdx.x >> log2_cluster;
     const int rank = int(blockIdx.x) & (cluster - 1);
 
@@ -410,32 +583,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
     // a block's shared memory may only be written by another once both run: announced here, awaited before the first write
     if (TOP && cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     sl.fetch();
-    // largest logit of the slice, NaN if there is one
-    typename Num<T>::Max running = Num<T>::nothing();
-#pragma unroll 4
-    for (int i = tid; i < sl.n; i += NT) running = Num<T>::max_of(running, sl.get(i));
-    const float thread_max = Num<T>::value(running);
-    float m = warp_max_nan(thread_max);
-    if (warps > 1) {
-        if (lane == 0) sh.m[warp] = m;
-        __syncthreads();
-        m = warp_max_nan(sh.m[lane < warps ? lane : 0]);
-    }
-    // sums relative to it
-    const float base = m == -infinity() ? 0.0f : m, c = p.tau_log2e;
-    float2 s2 = both(0.0f), t2 = both(0.0f);
-    if (p.entropy || p.d_entropy) add_terms<T, STASH, NT, true>(sl, base, c, s2, t2);
-    else add_terms<T, STASH, NT, false>(sl, base, c, s2, t2);
-    float s = warp_sum(s2.x + s2.y), t = warp_sum(t2.x + t2.y);
-    if (warps > 1) {
-        if (lane == 0) { sh.s[warp] = s; sh.t[warp] = t; }
-        __syncthreads();
-        s = warp_sum(lane < warps ? sh.s[lane] : 0.0f);
-        t = warp_sum(lane < warps ? sh.t[lane] : 0.0f);
-    }
-    Sums all{m, s, t};
-    if (!(m < infinity())) all.m = all.s = quiet_nan();       // a NaN or +inf: the row is NaN
-    if (TOP) slice_top<T, STASH, NT>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(m));
+    const float c = p.tau_log2e;
+    float thread_max;
+    Sums all = p.entropy || p.d_entropy ? sums_of<T, STASH, NT, true>(sl, c, sh, thread_max) : sums_of<T, STASH, NT, false>(sl, c, sh, thread_max);
+    if (TOP) slice_top<T, STASH, NT>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(all.m));
     if (cluster > 1) {
         cg::cluster_group cl = cg::this_cluster();
         if (tid == 0) sh.part = all;
@@ -468,6 +619,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
                 for (int i = tid; i < n; i += NT) {
                     const unsigned long long key = mine.gathered[i];
                     int place = 0;
+#pragma unroll 8
                     for (int j = 0; j < n; ++j) place += mine.gathered[j] > key;
                     if (key != 0ull && place < p.n_top) mine.top[place] = key;
                 }
@@ -484,8 +636,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
         __syncthreads();              // d_logits may be the logits: the token's logit has been read
         const RowGrad q = row_grad(p, r, y, all.m, ln_s, H, y < p.vocab ? 0.0f : quiet_nan());
         T *const out = static_cast<T *>(p.d_logits) + r * p.d_stride;
-        if (q.B == 0.0f) write_grad<T, STASH, NT, false>(sl, out, q);
-        else write_grad<T, STASH, NT, true>(sl, out, q);
+        if (!q.fast) write_grad<T, STASH, NT, true, false>(sl, out, q);
+        else if (q.B == 0.0f) write_grad<T, STASH, NT, false, true>(sl, out, q);
+        else write_grad<T, STASH, NT, true, true>(sl, out, q);
     }
 }
 
@@ -515,8 +668,9 @@ __global__ void __launch_bounds__(NT) logprob_grad_kernel(const __grid_constant_
     for (int k = 0; k < kGradPer; ++k) {
         const int i = begin + k * step;
         if (i < sl.n) {
-            const int place = i == hot.granule ? hot.place : -1;
-            const uint4 d = q.B == 0.0f ? granule_grad<T, false>(w[k], q, place) : granule_grad<T, true>(w[k], q, place);
+            uint4 d = !q.fast ? granule_grad<T, true, false>(w[k], q)
+                      : q.B == 0.0f ? granule_grad<T, false, true>(w[k], q) : granule_grad<T, true, true>(w[k], q);
+            if (i == hot.granule) d = token_grad<T>(w[k], q, hot.place);
             if (vector && sl.whole(i)) *reinterpret_cast<uint4 *>(dst + int64_t(i) * 16) = d;
             else put_elements<T>(out, p.vocab, sl.first(i), d);
         }
@@ -538,7 +692,7 @@ Shape shape_of(const LogprobParams &p, int element)
            (bytes > kSliceBytes << s.log2_cluster || ((p.rows << s.log2_cluster) * 2 <= kMultiprocessors && bytes >= int64_t(8192) << s.log2_cluster)))
         s.log2_cluster++;
     const int64_t granules = ((bytes / 16 - 1) >> s.log2_cluster) + 2;
-    s.threads = granules <= 256 ? 32 : granules <= 1024 ? 128 : 256;
+    s.threads = granules <= 256 ? 32 : granules <= 1024 ? 128 : granules <= 4608 ? 256 : 512;
     s.smem = granules * 16;
     return s;
 }
@@ -552,6 +706,10 @@ int launch_instance(const LogprobParams &p, const Shape &s, cudaStream_t st)
         static std::atomic<uint64_t> raised{0};           // devices on which this instance may use kStashMax
         if (int err = allow_shared(reinterpret_cast<const void *>(kernel), int(kStashMax), raised)) return err;
     }
+    if (s.log2_cluster == 0) {
+        kernel<<<unsigned(p.rows), NT, smem, st>>>(p, 0);
+        return int(cudaGetLastError());
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(p.rows << s.log2_cluster));
     cfg.blockDim = dim3(NT);
@@ -562,7 +720,7 @@ int launch_instance(const LogprobParams &p, const Shape &s, cudaStream_t st)
     attr[0].val.clusterDim.x = 1u << s.log2_cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = s.log2_cluster > 0 ? 1 : 0;
+    cfg.numAttrs = 1;
     return int(cudaLaunchKernelEx(&cfg, kernel, p, s.log2_cluster));
 }
 
@@ -577,10 +735,11 @@ template <typename T>
 int launch_typed(const LogprobParams &p, cudaStream_t st)
 {
     const Shape s = shape_of(p, int(sizeof(T)));
-    if (s.smem > kStashMax) return launch_outputs<T, false, 256>(p, s, st);
+    if (s.smem > kStashMax) return launch_outputs<T, false, 512>(p, s, st);
     if (s.threads == 32) return launch_outputs<T, true, 32>(p, s, st);
     if (s.threads == 128) return launch_outputs<T, true, 128>(p, s, st);
-    return launch_outputs<T, true, 256>(p, s, st);
+    if (s.threads == 256) return launch_outputs<T, true, 256>(p, s, st);
+    return launch_outputs<T, true, 512>(p, s, st);
 }
 
 template <typename T, int NT>
