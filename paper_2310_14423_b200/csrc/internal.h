@@ -133,6 +133,7 @@ int launch_sync_static(const SyncParams &p, const LaunchShape &shape, int device
 struct ListTensor {           // one tensor, in the device table
     void *param, *copy, *m, *v;
     float *m_scale, *v_scale;
+    int64_t numel;
     int32_t param_type, grad_type, copy_type;
     float wd_scale;
 };
@@ -164,7 +165,7 @@ struct ListSyncParams {
     const ListTensor *tensors;
     const ListChunk *chunks;
     int32_t workers, tensors_per_worker;
-    float divisor;
+    float divisor, inverse;   // K; 1 / K where that is exact, otherwise 0
 };
 // How a list's step is launched.  8-bit states: a warp keeps `stages` blocks of 256 elements in shared memory, stage_bytes each
 // (parameter, gradient and codes of the list's widest tensor); fp32 states: both 0.

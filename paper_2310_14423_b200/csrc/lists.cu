@@ -58,22 +58,26 @@ __device__ __forceinline__ float code_of(float x, float inv, bool positive)
     return positive && q > 0.0f ? fmaxf(q, kCodeMin) : q;
 }
 
-// Eight codes of a lane: two words when the lane owns eight consecutive elements, single bytes otherwise.
+// Eight codes of a lane: two words when the lane owns eight consecutive elements, otherwise single bytes packed the same way.
 template <bool VEC>
-__device__ __forceinline__ void load_codes(float (&x)[8], const uint8_t *base, int64_t e0, int n, int lane)
+__device__ __forceinline__ uint2 load_codes_raw(const uint8_t *base, int64_t e0, int n, int lane)
 {
-    if (VEC) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(base + e0 + lane * 8);
-        const uint32_t ws[2] = {w.x, w.y};
+    if (VEC) return *reinterpret_cast<const uint2 *>(base + e0 + lane * 8);
+    uint2 w = make_uint2(0u, 0u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = from_e4m3x2((ws[i >> 1] >> (16 * (i & 1))) & 0xffffu);
-            x[2 * i] = f.x; x[2 * i + 1] = f.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = lane + 32 * i < n ? from_e4m3x2(base[e0 + lane + 32 * i]).x : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        if (lane + 32 * i < n) w.x |= uint32_t(base[e0 + lane + 32 * i]) << (8 * i);
+        if (lane + 32 * (i + 4) < n) w.y |= uint32_t(base[e0 + lane + 32 * (i + 4)]) << (8 * i);
     }
+    return w;
+}
+__device__ __forceinline__ void widen_codes(float (&x)[8], uint2 w)
+{
+    float2 f[4];
+    from_e4m3x4(f[0], f[1], w.x);
+    from_e4m3x4(f[2], f[3], w.y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = f[i].x; x[2 * i + 1] = f[i].y; }
 }
 template <bool VEC>
 __device__ __forceinline__ void store_codes(uint8_t *base, int64_t e0, int n, int lane, const float (&x)[8], float inv, bool positive)
@@ -168,8 +172,8 @@ __device__ __noinline__ void step_block_codes_any(const ListStepParams &p, int t
     const int64_t b = e0 >> 8;
     const float ms = t.m_scale[b], vs = t.v_scale[b];
     float m[8], u[8];
-    load_codes<false>(m, static_cast<const uint8_t *>(t.m), e0, n, lane);
-    load_codes<false>(u, static_cast<const uint8_t *>(t.v), e0, n, lane);
+    widen_codes(m, load_codes_raw<false>(static_cast<const uint8_t *>(t.m), e0, n, lane));
+    widen_codes(u, load_codes_raw<false>(static_cast<const uint8_t *>(t.v), e0, n, lane));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (lane + 32 * i >= n) { m[i] = u[i] = 0.0f; continue; }
@@ -333,12 +337,30 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
     return make_float2(bm.scale, bu.scale);
 }
 
-template <bool S8>
 __device__ __forceinline__ bool step_aligned(const ListTensor &t, const void *grad)
 {
-    return aligned_to(t.param, bytes_of_8(t.param_type)) && aligned_to(grad, bytes_of_8(t.grad_type)) &&
-           aligned_to(t.m, S8 ? 8 : 32) && aligned_to(t.v, S8 ? 8 : 32) &&
-           (t.copy_type == QSR_NONE || aligned_to(t.copy, bytes_of_8(t.copy_type)));
+    return aligned_to(t.param, bytes_of_8(t.param_type)) && aligned_to(grad, bytes_of_8(t.grad_type)) && aligned_to(t.m, 8) &&
+           aligned_to(t.v, 8) && (t.copy_type == QSR_NONE || aligned_to(t.copy, bytes_of_8(t.copy_type)));
+}
+
+// How many elements a pointer lies past the last place where eight of them may be accessed at once.
+__device__ __forceinline__ int phase_of(const void *p, int type)
+{
+    const unsigned a = unsigned(reinterpret_cast<uintptr_t>(p));
+    return type == QSR_F32 ? (a & 31u) >> 2 : (a & 15u) >> 1;
+}
+// A chunk of a tensor whose operands all have the same phase moves up to the next place where that access is allowed (and
+// over its end by as much, unless the tensor ends there); the tensor's first elements become a block of their own.
+// Tensors cut out of one buffer at odd offsets then run at full width: 6.4 instead of 3.0 TB/s.
+struct Span { int64_t begin; int n, head; };
+__device__ __forceinline__ Span span_of(const ListChunk &c, int64_t numel, int phase)
+{
+    Span s;
+    s.head = (8 - phase) & 7;
+    s.begin = c.offset + s.head;
+    const int64_t end = c.offset + c.n == numel ? numel : c.offset + c.n + s.head;
+    s.n = int(max(int64_t(0), min(end, numel) - s.begin));
+    return s;
 }
 
 __global__ void __launch_bounds__(kThreads) list_step_kernel(const __grid_constant__ ListStepParams p)
@@ -349,13 +371,18 @@ __global__ void __launch_bounds__(kThreads) list_step_kernel(const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float g_scale = p.clip ? p.grad_scale * p.clip[c.tensor / p.tensors_per_worker] : p.grad_scale;
     const float eta_wd = p.eta_wd * t.wd_scale;
-    const bool vec = step_aligned<false>(t, grad);
-    for (int b = warp; b * 256 < c.n; b += kWarps) {
-        const int64_t e0 = c.offset + b * 256;
-        const int n = min(256, c.n - b * 256);
+    const int phase = phase_of(t.param, t.param_type);
+    const bool vec = phase_of(grad, t.grad_type) == phase && phase_of(t.m, QSR_F32) == phase && phase_of(t.v, QSR_F32) == phase &&
+                     (t.copy_type == QSR_NONE || phase_of(t.copy, t.copy_type) == phase);
+    const Span s = span_of(c, t.numel, vec ? phase : 0);
+    for (int b = warp; b * 256 < s.n; b += kWarps) {
+        const int64_t e0 = s.begin + b * 256;
+        const int n = min(256, s.n - b * 256);
         if (vec && n == 256) step_block_f32<true>(p, t, grad, e0, n, lane, g_scale, eta_wd);
         else step_block_f32<false>(p, t, grad, e0, n, lane, g_scale, eta_wd);
     }
+    if (c.offset == 0 && s.head > 0 && warp == kWarps - 1)
+        step_block_f32<false>(p, t, grad, 0, int(min(int64_t(s.head), t.numel)), lane, g_scale, eta_wd);
 }
 
 // States in 8 bits.  A warp starts the copies of all its blocks (at most kListStages) into shared memory before it works on the
@@ -369,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 4) list_step_codes_kernel(const __gr
     const ListTensor &tensor = p.tensors[c.tensor];
     const void *const grad = p.grads[c.tensor];
     const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool vec = step_aligned<true>(tensor, grad);
+    const bool vec = step_aligned(tensor, grad);
     Chunk<PT, GT> t;
     t.param_type_ = tensor.param_type; t.grad_type_ = tensor.grad_type; t.copy_type = tensor.copy_type;
     t.param = static_cast<char *>(tensor.param) + c.offset * bytes_of(t.param_type());
@@ -437,25 +464,30 @@ __global__ void __launch_bounds__(kThreads) list_norm_kernel(const ListNormParam
     const int type = p.tensors[c.tensor].grad_type;
     const void *grad = p.grads[c.tensor];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool vec = aligned_to(grad, bytes_of_8(type));
+    const Span span = span_of(c, p.tensors[c.tensor].numel, phase_of(grad, type));
     float s = 0.0f;
-    for (int b = warp; b * 256 < c.n; b += kWarps) {
-        const int64_t e0 = c.offset + b * 256;
-        const int n = min(256, c.n - b * 256);
-        Raw8 r;
+    auto add = [&](const Raw8 &r, bool vec) {
         float g[8];
-        if (vec && n == 256) {
-            load_raw<true>(r, grad, e0, n, lane, type);
-            widen<true>(g, r, type);
-        } else {
-            load_raw<false>(r, grad, e0, n, lane, type);
-            widen<false>(g, r, type);
-        }
+        if (vec) widen<true>(g, r, type);
+        else widen<false>(g, r, type);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float x = g[i] * p.grad_scale;
             s = fmaf(x, x, s);
         }
+    };
+    for (int b = warp; b * 256 < span.n; b += kWarps) {
+        const int64_t e0 = span.begin + b * 256;
+        const int n = min(256, span.n - b * 256);
+        Raw8 r;
+        if (n == 256) load_raw<true>(r, grad, e0, n, lane, type);
+        else load_raw<false>(r, grad, e0, n, lane, type);
+        add(r, n == 256);
+    }
+    if (c.offset == 0 && span.head > 0 && warp == kWarps - 1) {
+        Raw8 r;
+        load_raw<false>(r, grad, 0, int(min(int64_t(span.head), p.tensors[c.tensor].numel)), lane, type);
+        add(r, false);
     }
     s = block_sum(s, part);
     const int worker = blockIdx.x / p.chunks_per_worker;
@@ -487,136 +519,257 @@ __global__ void __launch_bounds__(kThreads) list_norm_kernel(const ListNormParam
 
 // ---------------------------------------------------------------------------------------------- replica mean
 
-// Address of operand A of worker k's tensor: 0 parameter, 1 m, 2 v.
+// What lane k knows of worker k0 + k's tensor: where operand A (0 parameter, 1 m, 2 v) lies, its working copy, its scales.
+struct Place { char *data, *copy; float *scale; };
 template <int A>
-__device__ __forceinline__ void *operand(const ListTensor &t) { return A == 0 ? t.param : A == 1 ? t.m : t.v; }
-
-__device__ __forceinline__ void *shfl_ptr(const void *p, int lane)
+__device__ __forceinline__ Place place_of(const ListSyncParams &p, int tensor, int k)
 {
-    return reinterpret_cast<void *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(p), lane));
+    const ListTensor &t = p.tensors[min(k, p.workers - 1) * p.tensors_per_worker + tensor];
+    return Place{static_cast<char *>(A == 0 ? t.param : A == 1 ? t.m : t.v), static_cast<char *>(t.copy), A == 1 ? t.m_scale : t.v_scale};
+}
+__device__ __forceinline__ char *of_lane(char *p, int lane)
+{
+    return reinterpret_cast<char *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(p), lane));
 }
 
-// Mean over the workers of 256 elements in the caller's type, written back to every worker (and to the working copies).
-template <int A, bool VEC>
-__device__ __forceinline__ void mean_block(const ListSyncParams &p, int tensor, int type, int copy_type, int64_t e0, int n, int lane)
+// Four elements of a lane as they lie in memory: adjacent ones (VEC; 16 bytes of fp32, 8 of a 16-bit type), otherwise lane,
+// lane + 32, ... of the warp's 128, n of which are valid.
+template <bool F32, bool VEC>
+__device__ __forceinline__ uint4 load_quad(const char *base, int64_t e0, int n, int lane)
 {
-    float s[8];
+    uint4 r = make_uint4(0u, 0u, 0u, 0u);
+    if (VEC && F32) {
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(base + (e0 + lane * 4) * 4) : "memory");
+    } else if (VEC) {
+        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(base + (e0 + lane * 4) * 2) : "memory");
+    } else {
+        const int type = F32 ? QSR_F32 : QSR_BF16;            // the width is what counts here
+        if (lane < n) r.x = load1(base, e0 + lane, type);
+        if (lane + 32 < n) r.y = load1(base, e0 + lane + 32, type);
+        if (lane + 64 < n) r.z = load1(base, e0 + lane + 64, type);
+        if (lane + 96 < n) r.w = load1(base, e0 + lane + 96, type);
+    }
+    return r;
+}
+template <bool F32, bool VEC>
+__device__ __forceinline__ void add_quad(float (&s)[4], uint4 r, int type)
+{
+    if (F32) {
+        s[0] += __uint_as_float(r.x); s[1] += __uint_as_float(r.y); s[2] += __uint_as_float(r.z); s[3] += __uint_as_float(r.w);
+    } else if (VEC) {
+        const float2 a = widen2(r.x, type), b = widen2(r.y, type);
+        s[0] += a.x; s[1] += a.y; s[2] += b.x; s[3] += b.y;
+    } else {
+        s[0] += widen1(r.x, type); s[1] += widen1(r.y, type); s[2] += widen1(r.z, type); s[3] += widen1(r.w, type);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_quad(char *base, int64_t e0, int n, int lane, const float (&s)[4], int type)
+{
+    if (VEC && type == QSR_F32) *reinterpret_cast<float4 *>(base + (e0 + lane * 4) * 4) = make_float4(s[0], s[1], s[2], s[3]);
+    else if (VEC) *reinterpret_cast<uint2 *>(base + (e0 + lane * 4) * 2) = make_uint2(narrow2(s[0], s[1], type), narrow2(s[2], s[3], type));
+    else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = 0.0f;
+        for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < n) store1(base, e0 + lane + 32 * i, s[i], type);
+    }
+}
+
+// Adds N workers' elements, k ascending, all N loads started before the first is waited for.
+template <bool F32, bool VEC, int N>
+__device__ __forceinline__ void add_workers(float (&s)[4], char *data, int k, int64_t e0, int n, int lane, int type)
+{
+    uint4 r[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = load_quad<F32, VEC>(of_lane(data, k + j), e0, n, lane);
+#pragma unroll
+    for (int j = 0; j < N; ++j) add_quad<F32, VEC>(s, r[j], type);
+}
+
+__device__ __forceinline__ float mean_of(float sum, const ListSyncParams &p) { return p.inverse > 0.0f ? sum * p.inverse : sum / p.divisor; }
+
+// Mean over the workers of 128 elements in the caller's type, written back to every worker (parameters: to the working copies
+// too).  `mine`: the first 32 workers' places, loaded anew where there are more.
+template <int A, bool F32, bool VEC>
+__device__ __forceinline__ void mean_block(const ListSyncParams &p, Place mine, int tensor, int type, int copy_type, int64_t e0, int n, int lane)
+{
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k0 = 0; k0 < p.workers; k0 += 32) {
-        const int kl = k0 + lane < p.workers ? k0 + lane : k0;
-        const void *mine = operand<A>(p.tensors[kl * p.tensors_per_worker + tensor]);
+        if (p.workers > 32) mine = place_of<A>(p, tensor, k0 + lane);
         const int here = min(32, p.workers - k0);
         int k = 0;
-        for (; k + 4 <= here; k += 4) {
-            Raw8 r[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) load_raw<VEC>(r[j], shfl_ptr(mine, k + j), e0, n, lane, type);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[8];
-                widen<VEC>(x, r[j], type);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[i] += x[i];
-            }
-        }
-        for (; k < here; ++k) {
-            Raw8 r;
-            float x[8];
-            load_raw<VEC>(r, shfl_ptr(mine, k), e0, n, lane, type);
-            widen<VEC>(x, r, type);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += x[i];
-        }
+        for (; k + 8 <= here; k += 8) add_workers<F32, VEC, 8>(s, mine.data, k, e0, n, lane, type);
+        if (here & 4) { add_workers<F32, VEC, 4>(s, mine.data, k, e0, n, lane, type); k += 4; }
+        if ((here & 3) == 3) add_workers<F32, VEC, 3>(s, mine.data, k, e0, n, lane, type);
+        else if (here & 2) add_workers<F32, VEC, 2>(s, mine.data, k, e0, n, lane, type);
+        else if (here & 1) add_workers<F32, VEC, 1>(s, mine.data, k, e0, n, lane, type);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = s[i] / p.divisor;
+    for (int i = 0; i < 4; ++i) s[i] = mean_of(s[i], p);
     for (int k0 = 0; k0 < p.workers; k0 += 32) {
-        const int kl = k0 + lane < p.workers ? k0 + lane : k0;
-        const ListTensor &t = p.tensors[kl * p.tensors_per_worker + tensor];
-        void *mine = operand<A>(t), *copy = t.copy;
+        if (p.workers > 32) mine = place_of<A>(p, tensor, k0 + lane);
         const int here = min(32, p.workers - k0);
         for (int k = 0; k < here; ++k) {
-            store<VEC>(shfl_ptr(mine, k), e0, n, lane, s, type);
-            if (A == 0 && copy_type != QSR_NONE) store<VEC>(shfl_ptr(copy, k), e0, n, lane, s, copy_type);
+            store_quad<VEC>(of_lane(mine.data, k), e0, n, lane, s, F32 ? QSR_F32 : type);
+            if (A == 0 && copy_type != QSR_NONE) store_quad<VEC>(of_lane(mine.copy, k), e0, n, lane, s, copy_type);
         }
     }
 }
 
-// The same for a block of 8-bit states: the mean of the values they stand for (of the squares of v's codes), rounded to 8
-// bits once.
-template <int A, bool VEC>
-__device__ __forceinline__ void mean_codes(const ListSyncParams &p, int tensor, int64_t e0, int n, int lane)
+// Adds N workers' 8-bit states, 4 * WORDS codes of a lane: the values they stand for (of v: the squares of its codes).
+template <int A, int WORDS>
+__device__ __forceinline__ void add_codes(float (&s)[4 * WORDS], const uint32_t (&w)[WORDS], float scale)
 {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+        float2 f[2];
+        from_e4m3x4(f[0], f[1], w[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float y = __fmul_rn(j & 1 ? f[j >> 1].y : f[j >> 1].x, scale);
+            s[4 * i + j] = __fadd_rn(s[4 * i + j], A == 1 ? y : __fmul_rn(y, y));
+        }
+    }
+}
+template <int A, int N>
+__device__ __forceinline__ float finish_states(float (&s)[N], const ListSyncParams &p)
+{
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        s[i] = mean_of(s[i], p);
+        if (A == 2) s[i] = __fsqrt_rn(s[i]);
+        amax = fmaxf(amax, finite_or_0(fabsf(s[i])));
+    }
+    return amax;
+}
+
+// Mean of a block of 256 8-bit states, rounded to 8 bits once: ragged blocks and unaligned tensors, byte by byte.
+template <int A>
+__device__ __noinline__ void mean_codes_any(const ListSyncParams &p, int tensor, int64_t e0, int n, int lane)
+{
+    const int64_t b = e0 >> 8;
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = 0.0f;
-    const int64_t b = e0 >> 8;
     for (int k = 0; k < p.workers; ++k) {
-        const ListTensor &t = p.tensors[k * p.tensors_per_worker + tensor];
-        const float scale = (A == 1 ? t.m_scale : t.v_scale)[b];
-        float x[8];
-        load_codes<VEC>(x, static_cast<const uint8_t *>(operand<A>(t)), e0, n, lane);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = __fmul_rn(x[i], scale);
-            s[i] = __fadd_rn(s[i], A == 1 ? x[i] : __fmul_rn(x[i], x[i]));
-        }
+        const Place x = place_of<A>(p, tensor, k);
+        const uint2 r = load_codes_raw<false>(reinterpret_cast<const uint8_t *>(x.data), e0, n, lane);
+        const uint32_t w[2] = {r.x, r.y};
+        add_codes<A, 2>(s, w, x.scale[b]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        s[i] = s[i] / p.divisor;
-        if (A == 2) s[i] = __fsqrt_rn(s[i]);
-    }
-    const BlockScale q = block_scale(block_amax(s));
+    const BlockScale q = block_scale(warp_max(finish_states<A, 8>(s, p)));
     for (int k = 0; k < p.workers; ++k) {
-        const ListTensor &t = p.tensors[k * p.tensors_per_worker + tensor];
-        store_codes<VEC>(static_cast<uint8_t *>(operand<A>(t)), e0, n, lane, s, q.inv, A == 2);
-        if (lane == 0) (A == 1 ? t.m_scale : t.v_scale)[b] = q.scale;
+        const Place x = place_of<A>(p, tensor, k);
+        store_codes<false>(reinterpret_cast<uint8_t *>(x.data), e0, n, lane, s, q.inv, A == 2);
+        if (lane == 0) x.scale[b] = q.scale;
     }
 }
 
-// Whether every worker's operand may be accessed eight elements at a time.
+// Two whole blocks of 256 at once: sixteen adjacent codes per lane, a block per half warp, so that a warp reads 512 bytes of each
+// worker at a time and has eight workers' loads on their way.
+template <int A, int N>
+__device__ __forceinline__ void add_codes_of(float (&s)[16], char *data, float scale0, float scale1, int k, int64_t e0, int lane)
+{
+    uint4 r[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = load_quad<true, true>(of_lane(data, k + j) + e0, 0, 128, lane);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float a = __shfl_sync(0xffffffffu, scale0, k + j), b = __shfl_sync(0xffffffffu, scale1, k + j);
+        const uint32_t w[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+        add_codes<A, 4>(s, w, lane < 16 ? a : b);
+    }
+}
+template <int A>
+__device__ __forceinline__ void mean_codes(const ListSyncParams &p, Place mine, int tensor, int64_t e0, int lane)
+{
+    const int64_t b = e0 >> 8;
+    float s[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    for (int k0 = 0; k0 < p.workers; k0 += 32) {
+        if (p.workers > 32) mine = place_of<A>(p, tensor, k0 + lane);
+        const int here = min(32, p.workers - k0);
+        const float scale0 = lane < here ? mine.scale[b] : 0.0f, scale1 = lane < here ? mine.scale[b + 1] : 0.0f;
+        int k = 0;
+        for (; k + 8 <= here; k += 8) add_codes_of<A, 8>(s, mine.data, scale0, scale1, k, e0, lane);
+        if (here & 4) { add_codes_of<A, 4>(s, mine.data, scale0, scale1, k, e0, lane); k += 4; }
+        for (; k < here; ++k) add_codes_of<A, 1>(s, mine.data, scale0, scale1, k, e0, lane);
+    }
+    float amax = finish_states<A, 16>(s, p);
+#pragma unroll
+    for (int d = 8; d; d >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+    const BlockScale q = block_scale(amax);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = to_e4m3x4(make_float2(code_of(s[4 * i], q.inv, A == 2), code_of(s[4 * i + 1], q.inv, A == 2)),
+                         make_float2(code_of(s[4 * i + 2], q.inv, A == 2), code_of(s[4 * i + 3], q.inv, A == 2)));
+    const float scale0 = __shfl_sync(0xffffffffu, q.scale, 0), scale1 = __shfl_sync(0xffffffffu, q.scale, 16);
+    for (int k0 = 0; k0 < p.workers; k0 += 32) {
+        if (p.workers > 32) mine = place_of<A>(p, tensor, k0 + lane);
+        const int here = min(32, p.workers - k0);
+        for (int k = 0; k < here; ++k)
+            *reinterpret_cast<uint4 *>(of_lane(mine.data, k) + e0 + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (lane < here) { mine.scale[b] = scale0; mine.scale[b + 1] = scale1; }
+    }
+}
+
+// Whether every worker's operand may be accessed four (codes: sixteen) elements at a time.
 template <int A>
 __device__ __forceinline__ bool sync_aligned(const ListSyncParams &p, int tensor, int type, int copy_type, bool codes, int lane)
 {
     bool ok = true;
     for (int k = lane; k < p.workers; k += 32) {
-        const ListTensor &t = p.tensors[k * p.tensors_per_worker + tensor];
-        ok = ok && aligned_to(operand<A>(t), codes ? 8u : bytes_of_8(type));
-        if (A == 0 && copy_type != QSR_NONE) ok = ok && aligned_to(t.copy, bytes_of_8(copy_type));
+        const Place x = place_of<A>(p, tensor, k);
+        ok = ok && aligned_to(x.data, codes ? 16u : bytes_of_8(type) / 2);
+        if (A == 0 && copy_type != QSR_NONE) ok = ok && aligned_to(x.copy, bytes_of_8(copy_type) / 2);
     }
     return __all_sync(0xffffffffu, ok);
 }
 
-template <int A, bool CODES>
-__device__ __forceinline__ void sync_chunk(const ListSyncParams &p)
+template <int A, bool F32>
+__device__ __forceinline__ void sync_blocks(const ListSyncParams &p, const ListChunk &c, int type, int copy_type)
 {
-    const ListChunk c = p.chunks[blockIdx.x];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int type = A == 0 ? p.tensors[c.tensor].param_type : QSR_F32;
-    const int copy_type = p.tensors[c.tensor].copy_type;
-    const bool vec = sync_aligned<A>(p, c.tensor, type, copy_type, CODES, lane);
-    for (int b = warp; b * 256 < c.n; b += kWarps) {
-        const int64_t e0 = c.offset + b * 256;
-        const int n = min(256, c.n - b * 256);
-        if (CODES) {
-            if (vec && n == 256) mean_codes<A, true>(p, c.tensor, e0, n, lane);
-            else mean_codes<A, false>(p, c.tensor, e0, n, lane);
-        } else {
-            if (vec && n == 256) mean_block<A, true>(p, c.tensor, type, copy_type, e0, n, lane);
-            else mean_block<A, false>(p, c.tensor, type, copy_type, e0, n, lane);
-        }
+    const Place mine = place_of<A>(p, c.tensor, lane);
+    const bool vec = sync_aligned<A>(p, c.tensor, type, copy_type, false, lane);
+    for (int b = warp; b * 128 < c.n; b += kWarps) {
+        const int64_t e0 = c.offset + b * 128;
+        const int n = min(128, c.n - b * 128);
+        if (vec && n == 128) mean_block<A, F32, true>(p, mine, c.tensor, type, copy_type, e0, n, lane);
+        else mean_block<A, F32, false>(p, mine, c.tensor, type, copy_type, e0, n, lane);
     }
+}
+template <int A>
+__device__ __forceinline__ void sync_codes(const ListSyncParams &p, const ListChunk &c)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Place mine = place_of<A>(p, c.tensor, lane);
+    const int pairs = sync_aligned<A>(p, c.tensor, QSR_F32, QSR_NONE, true, lane) ? c.n / 512 : 0;
+    for (int b = warp; b < pairs; b += kWarps) mean_codes<A>(p, mine, c.tensor, c.offset + b * 512, lane);
+    for (int b = 2 * pairs + warp; b * 256 < c.n; b += kWarps)
+        mean_codes_any<A>(p, c.tensor, c.offset + b * 256, min(256, c.n - b * 256), lane);
+}
+template <int A, bool S8>
+__device__ __forceinline__ void sync_states(const ListSyncParams &p, const ListChunk &c)
+{
+    if (S8) sync_codes<A>(p, c);
+    else sync_blocks<A, true>(p, c, QSR_F32, QSR_NONE);
 }
 
 // Grid: worker 0's chunks by 1 (parameters) or 3 (parameters, m, v).
 template <bool S8>
-__global__ void __launch_bounds__(kThreads) list_sync_kernel(const ListSyncParams p)
+__global__ void __launch_bounds__(kThreads, S8 ? 3 : 4) list_sync_kernel(const __grid_constant__ ListSyncParams p)
 {
-    if (blockIdx.y == 0) sync_chunk<0, false>(p);
-    else if (blockIdx.y == 1) sync_chunk<1, S8>(p);
-    else sync_chunk<2, S8>(p);
+    const ListChunk c = p.chunks[blockIdx.x];
+    const int type = p.tensors[c.tensor].param_type, copy_type = p.tensors[c.tensor].copy_type;
+    if (blockIdx.y == 0) {
+        if (type == QSR_F32) sync_blocks<0, true>(p, c, type, copy_type);
+        else sync_blocks<0, false>(p, c, type, copy_type);
+    } else if (blockIdx.y == 1) sync_states<1, S8>(p, c);
+    else sync_states<2, S8>(p, c);
 }
 
 // Zeroes m and v (and their scales) of every worker.  Grid: all chunks.

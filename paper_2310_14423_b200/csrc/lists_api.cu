@@ -197,7 +197,7 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     chunks.reserve(size_t(l.n_chunks));
     for (int32_t i = 0; i < n; ++i) {
         const qsr_tensor &x = t[i];
-        table[size_t(i)] = qsr::ListTensor{x.param, x.copy, x.m, x.v, x.m_scale, x.v_scale, x.param_type, x.grad_type, x.copy_type, x.wd_scale};
+        table[size_t(i)] = qsr::ListTensor{x.param, x.copy, x.m, x.v, x.m_scale, x.v_scale, x.numel, x.param_type, x.grad_type, x.copy_type, x.wd_scale};
         grads[size_t(i)] = x.grad;
         for (int64_t o = 0; o < x.numel; o += l.chunk)
             chunks.push_back(qsr::ListChunk{i, int32_t(std::min(l.chunk, x.numel - o)), o});
@@ -327,6 +327,7 @@ int qsr_list_sync(qsr_list *list, int32_t state_sync)
     p.tensors = list->tensors; p.chunks = list->chunk_table;
     p.workers = c.workers; p.tensors_per_worker = c.n_tensors / c.workers;
     p.divisor = float(c.workers);
+    p.inverse = (c.workers & (c.workers - 1)) == 0 ? 1.0f / float(c.workers) : 0.0f;
     const bool codes = c.states == QSR_STATES_E4M3;
     list->launches++;
     if (int err = qsr::launch_list_sync(p, codes, state_sync == QSR_STATE_AVERAGE, list->chunks_per_worker, list->stream))
