@@ -36,22 +36,6 @@ __device__ __forceinline__ BlockScale block_scale(float amax)
 
 __device__ __forceinline__ float finite_or_0(float a) { return a < infinity() ? a : 0.0f; }
 
-// Largest finite magnitude of the warp's 256 values.  Infinities are rare: only a block that holds one pays for the test.
-__device__ __forceinline__ float block_amax(const float (&x)[8])
-{
-    float a = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(x[i]));
-    a = warp_max(a);
-    if (a == infinity()) {
-        a = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_or_0(fabsf(x[i])));
-        a = warp_max(a);
-    }
-    return a;
-}
-
 __device__ __forceinline__ float code_of(float x, float inv, bool positive)
 {
     const float q = __fmul_rn(x, inv);
@@ -70,14 +54,6 @@ __device__ __forceinline__ uint2 load_codes_raw(const uint8_t *base, int64_t e0,
         if (lane + 32 * (i + 4) < n) w.y |= uint32_t(base[e0 + lane + 32 * (i + 4)]) << (8 * i);
     }
     return w;
-}
-__device__ __forceinline__ void widen_codes(float (&x)[8], uint2 w)
-{
-    float2 f[4];
-    from_e4m3x4(f[0], f[1], w.x);
-    from_e4m3x4(f[2], f[3], w.y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = f[i].x; x[2 * i + 1] = f[i].y; }
 }
 template <bool VEC>
 __device__ __forceinline__ void store_codes(uint8_t *base, int64_t e0, int n, int lane, const float (&x)[8], float inv, bool positive)
@@ -163,35 +139,6 @@ __device__ __forceinline__ void step_block_f32(const ListStepParams &p, const Li
     store<VEC>(t.v, e0, n, lane, v, QSR_F32);
 }
 
-// The same with states in 8 bits, one element at a time: ragged blocks and unaligned tensors.
-// Not inlined, so that the registers of this rare path do not count against the common one.
-__device__ __noinline__ void step_block_codes_any(const ListStepParams &p, int tensor, int64_t e0, int n, int lane, float g_scale, float eta_wd)
-{
-    const ListTensor &t = p.tensors[tensor];
-    const void *const grad = p.grads[tensor];
-    const int64_t b = e0 >> 8;
-    const float ms = t.m_scale[b], vs = t.v_scale[b];
-    float m[8], u[8];
-    widen_codes(m, load_codes_raw<false>(static_cast<const uint8_t *>(t.m), e0, n, lane));
-    widen_codes(u, load_codes_raw<false>(static_cast<const uint8_t *>(t.v), e0, n, lane));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (lane + 32 * i >= n) { m[i] = u[i] = 0.0f; continue; }
-        const int64_t e = e0 + lane + 32 * i;
-        const float g = __fmul_rn(widen1(load1(grad, e, t.grad_type), t.grad_type), g_scale);
-        const float m0 = __fmul_rn(m[i], ms), u0 = __fmul_rn(u[i], vs), v0 = __fmul_rn(u0, u0);
-        m[i] = __fadd_rn(m0, __fmul_rn(p.omb1, __fsub_rn(g, m0)));
-        u[i] = __fsqrt_rn(__fadd_rn(v0, __fmul_rn(p.omb2, __fsub_rn(__fmul_rn(g, g), v0))));
-        const float th = step_theta(p, widen1(load1(t.param, e, t.param_type), t.param_type), m[i], u[i], eta_wd);
-        store1(t.param, e, th, t.param_type);
-        if (t.copy_type != QSR_NONE) store1(t.copy, e, th, t.copy_type);
-    }
-    const BlockScale bm = block_scale(block_amax(m)), bu = block_scale(block_amax(u));
-    store_codes<false>(static_cast<uint8_t *>(t.m), e0, n, lane, m, bm.inv, false);
-    store_codes<false>(static_cast<uint8_t *>(t.v), e0, n, lane, u, bu.inv, true);
-    if (lane == 0) { t.m_scale[b] = bm.scale; t.v_scale[b] = bu.scale; }
-}
-
 // Two fp32 operations per instruction (sm_100), each rounded like its scalar form.  Sums are written as fused multiply-adds with
 // a factor of one: nvcc 12.9 makes one fused operation of a packed product and the packed sum that takes it (also of
 // mul.rn.f32x2 and add.rn.f32x2), and the codes would not be those of the formulas (the tests compare them bit for bit).
@@ -251,6 +198,29 @@ __device__ __forceinline__ void read_operand(float (&x)[8], const char *smem, un
     widen8(x, r, type);
 }
 
+// The same element by element, zeros beyond n: ragged blocks and unaligned tensors.
+__device__ __forceinline__ char *element_of(char *smem, unsigned e, int type)
+{
+    return type == QSR_F32 ? smem + piece(e >> 2) * 16 + (e & 3) * 4 : smem + e * 2;
+}
+__device__ __forceinline__ void fill_operand(char *smem, const char *chunk, unsigned at, int n, int lane, int type)
+{
+    Raw8 r;
+    load_raw<false>(r, chunk, at, n, lane, type);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        char *const to = element_of(smem, lane + 32 * i, type);
+        if (type == QSR_F32) *reinterpret_cast<uint32_t *>(to) = r.w[i];
+        else *reinterpret_cast<uint16_t *>(to) = uint16_t(r.w[i]);
+    }
+}
+__device__ __forceinline__ void fill_codes(char *smem, const char *chunk, unsigned at, int n, int lane)
+{
+    const uint2 w = load_codes_raw<false>(reinterpret_cast<const uint8_t *>(chunk), at, n, lane);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) smem[lane + 32 * i] = char((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+}
+
 // The operands of a chunk: addresses of its first element (the same for the whole thread block) and types.  PT, GT: the types
 // of parameters and gradients where the whole list has the same, known to the compiler then, or -1.
 template <int PT, int GT>
@@ -262,14 +232,15 @@ struct Chunk {
     __device__ __forceinline__ int grad_type() const { return GT >= 0 ? GT : grad_type_; }
 };
 
-// A whole aligned block whose operands have arrived in shared memory (parameter, gradient, codes of m, codes of v): eight
-// consecutive elements per lane, in pairs.  ms, vs: the block's scales before; returned: after.
+// A block whose operands have arrived in shared memory (parameter, gradient, codes of m, codes of v): eight consecutive
+// elements per lane, in pairs.  ms, vs: the block's scales before; returned: after.  Without `vec` the results go through the
+// same shared memory and are written element by element, the first n of them.
 template <int PT, int GT>
-__device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, const Chunk<PT, GT> &t, const char *stage, unsigned at, unsigned lane,
-                                                   float ms, float vs, float g_scale, float eta_wd)
+__device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, const Chunk<PT, GT> &t, char *stage, unsigned at, int n, bool vec,
+                                                   unsigned lane, float ms, float vs, float g_scale, float eta_wd)
 {
     float g[8];
-    const char *const s_grad = stage + 256 * bytes_of(t.param_type()), *const s_codes = s_grad + 256 * bytes_of(t.grad_type());
+    char *const s_grad = stage + 256 * bytes_of(t.param_type()), *const s_codes = s_grad + 256 * bytes_of(t.grad_type());
     read_operand(g, s_grad, lane, t.grad_type());
     const uint2 mw = *reinterpret_cast<const uint2 *>(s_codes + lane * 8), vw = *reinterpret_cast<const uint2 *>(s_codes + 256 + lane * 8);
     float2 m[4], u[4];
@@ -309,8 +280,14 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
         au = max3_abs(au, u[i].x, u[i].y);
     }
     const unsigned mine = at + lane * 8;
-    store8(t.param + mine * bytes_of(t.param_type()), 0, th, t.param_type());
-    if (t.copy_type != QSR_NONE) store8(t.copy + mine * bytes_of(t.copy_type), 0, th, t.copy_type);
+    if (vec) {
+        store8(t.param + mine * bytes_of(t.param_type()), 0, th, t.param_type());
+        if (t.copy_type != QSR_NONE) store8(t.copy + mine * bytes_of(t.copy_type), 0, th, t.copy_type);
+    } else {
+        __syncwarp();                                 // parameter and gradient have been read: 1024 bytes at least
+        *reinterpret_cast<float4 *>(stage + piece(2 * lane) * 16) = make_float4(th[0], th[1], th[2], th[3]);
+        *reinterpret_cast<float4 *>(stage + piece(2 * lane + 1) * 16) = make_float4(th[4], th[5], th[6], th[7]);
+    }
     am = warp_max(am);
     au = warp_max(au);
     if (fmaxf(am, au) == infinity()) {                // only finite values make the scale
@@ -332,8 +309,23 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
         if (!tiny) u[i] = make_float2(max_nan(u[i].x, kCodeMin), max_nan(u[i].y, kCodeMin));
         else u[i] = make_float2(u[i].x > 0.0f ? fmaxf(u[i].x, kCodeMin) : u[i].x, u[i].y > 0.0f ? fmaxf(u[i].y, kCodeMin) : u[i].y);
     }
-    *reinterpret_cast<uint2 *>(t.m + mine) = make_uint2(to_e4m3x4(m[0], m[1]), to_e4m3x4(m[2], m[3]));
-    *reinterpret_cast<uint2 *>(t.v + mine) = make_uint2(to_e4m3x4(u[0], u[1]), to_e4m3x4(u[2], u[3]));
+    const uint2 m_codes = make_uint2(to_e4m3x4(m[0], m[1]), to_e4m3x4(m[2], m[3])), v_codes = make_uint2(to_e4m3x4(u[0], u[1]), to_e4m3x4(u[2], u[3]));
+    if (vec) {
+        *reinterpret_cast<uint2 *>(t.m + mine) = m_codes;
+        *reinterpret_cast<uint2 *>(t.v + mine) = v_codes;
+    } else {
+        *reinterpret_cast<uint2 *>(s_codes + lane * 8) = m_codes;
+        *reinterpret_cast<uint2 *>(s_codes + 256 + lane * 8) = v_codes;
+        __syncwarp();
+#pragma unroll 1
+        for (int e = lane; e < n; e += 32) {
+            const float x = *reinterpret_cast<const float *>(element_of(stage, e, QSR_F32));
+            store1(t.param, at + e, x, t.param_type());
+            if (t.copy_type != QSR_NONE) store1(t.copy, at + e, x, t.copy_type);
+            t.m[at + e] = s_codes[e];
+            t.v[at + e] = s_codes[256 + e];
+        }
+    }
     return make_float2(bm.scale, bu.scale);
 }
 
@@ -404,17 +396,24 @@ __global__ void __launch_bounds__(kThreads, 4) list_step_codes_kernel(const __gr
     t.copy = static_cast<char *>(tensor.copy) + c.offset * bytes_of(t.copy_type);
     t.m = static_cast<char *>(tensor.m) + c.offset;
     t.v = static_cast<char *>(tensor.v) + c.offset;
-    const unsigned whole = vec ? c.n >> 8 : 0;            // whole blocks on the fast path: 0 .. whole - 1
-    const unsigned mine = whole > warp ? (whole - warp + kWarps - 1) / kWarps : 0;
-    const char *const my_stages = reinterpret_cast<const char *>(stages) + warp * n_stages * stage_bytes;
-    const unsigned smem = unsigned(__cvta_generic_to_shared(my_stages));
+    const unsigned blocks = unsigned(c.n + 255) >> 8, mine = blocks > warp ? (blocks - warp + kWarps - 1) / kWarps : 0;
+    char *const my_stages = reinterpret_cast<char *>(stages) + warp * n_stages * stage_bytes;
     for (unsigned i = 0; i < mine; ++i) {
         const unsigned at = (warp + i * kWarps) * 256;
-        const unsigned s_param = smem + i * stage_bytes, s_grad = s_param + 256 * bytes_of(t.param_type()), s_codes = s_grad + 256 * bytes_of(t.grad_type());
-        fetch_operand(s_param, t.param, at, lane, t.param_type());
-        fetch_operand(s_grad, t.grad, at, lane, t.grad_type());
-        copy_async<8>(s_codes + lane * 8, t.m + (at + lane * 8));
-        copy_async<8>(s_codes + 256 + lane * 8, t.v + (at + lane * 8));
+        const int n = c.n - int(at);
+        char *const s_param = my_stages + i * stage_bytes, *const s_grad = s_param + 256 * bytes_of(t.param_type()), *const s_codes = s_grad + 256 * bytes_of(t.grad_type());
+        if (vec && n >= 256) {
+            const unsigned to = unsigned(__cvta_generic_to_shared(s_param)), grad_at = unsigned(s_grad - s_param), codes_at = unsigned(s_codes - s_param);
+            fetch_operand(to, t.param, at, lane, t.param_type());
+            fetch_operand(to + grad_at, t.grad, at, lane, t.grad_type());
+            copy_async<8>(to + codes_at + lane * 8, t.m + (at + lane * 8));
+            copy_async<8>(to + codes_at + 256 + lane * 8, t.v + (at + lane * 8));
+        } else {
+            fill_operand(s_param, t.param, at, n, lane, t.param_type());
+            fill_operand(s_grad, t.grad, at, n, lane, t.grad_type());
+            fill_codes(s_codes, t.m, at, n, lane);
+            fill_codes(s_codes + 256, t.v, at, n, lane);
+        }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // lane i holds the scales of the warp's i-th block
@@ -430,13 +429,13 @@ __global__ void __launch_bounds__(kThreads, 4) list_step_codes_kernel(const __gr
         else if (later == 1) copy_wait<1>();
         else copy_wait<0>();
         __syncwarp();
-        const float2 s = step_block_codes(p, t, my_stages + i * stage_bytes, (warp + i * kWarps) * 256, lane,
-                                          __shfl_sync(0xffffffffu, ms, i), __shfl_sync(0xffffffffu, vs, i), g_scale, eta_wd);
+        const unsigned at = (warp + i * kWarps) * 256;
+        const int n = c.n - int(at);
+        const float2 s = step_block_codes(p, t, my_stages + i * stage_bytes, at, min(n, 256), vec && n >= 256, lane, __shfl_sync(0xffffffffu, ms, i),
+                                          __shfl_sync(0xffffffffu, vs, i), g_scale, eta_wd);
         if (lane == i) { ms = s.x; vs = s.y; }
     }
     if (lane < mine) { m_scale[warp + lane * kWarps] = ms; v_scale[warp + lane * kWarps] = vs; }
-    for (unsigned b = whole + warp; b * 256 < unsigned(c.n); b += kWarps)
-        step_block_codes_any(p, c.tensor, c.offset + b * 256, min(256, c.n - int(b * 256)), lane, g_scale, eta_wd);
 }
 
 // ---------------------------------------------------------------------------------------------- clipping
@@ -652,17 +651,28 @@ __device__ __noinline__ void mean_codes_any(const ListSyncParams &p, int tensor,
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = 0.0f;
-    for (int k = 0; k < p.workers; ++k) {
-        const Place x = place_of<A>(p, tensor, k);
-        const uint2 r = load_codes_raw<false>(reinterpret_cast<const uint8_t *>(x.data), e0, n, lane);
-        const uint32_t w[2] = {r.x, r.y};
-        add_codes<A, 2>(s, w, x.scale[b]);
+    for (int k0 = 0; k0 < p.workers; k0 += 32) {
+        const Place mine = place_of<A>(p, tensor, k0 + lane);
+        const int here = min(32, p.workers - k0);
+        const float scale = mine.scale[b];
+        for (int k = 0; k < here; k += 4) {
+            uint2 r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = load_codes_raw<false>(reinterpret_cast<const uint8_t *>(of_lane(mine.data, min(k + j, here - 1))), e0, n, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w[2] = {r[j].x, r[j].y};
+                const float sc = __shfl_sync(0xffffffffu, scale, k + j);
+                if (k + j < here) add_codes<A, 2>(s, w, sc);
+            }
+        }
     }
     const BlockScale q = block_scale(warp_max(finish_states<A, 8>(s, p)));
-    for (int k = 0; k < p.workers; ++k) {
-        const Place x = place_of<A>(p, tensor, k);
-        store_codes<false>(reinterpret_cast<uint8_t *>(x.data), e0, n, lane, s, q.inv, A == 2);
-        if (lane == 0) x.scale[b] = q.scale;
+    for (int k0 = 0; k0 < p.workers; k0 += 32) {
+        const Place mine = place_of<A>(p, tensor, k0 + lane);
+        const int here = min(32, p.workers - k0);
+        for (int k = 0; k < here; ++k) store_codes<false>(reinterpret_cast<uint8_t *>(of_lane(mine.data, k)), e0, n, lane, s, q.inv, A == 2);
+        if (lane < here) mine.scale[b] = q.scale;
     }
 }
 
