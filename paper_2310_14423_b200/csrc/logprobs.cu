@@ -23,7 +23,6 @@ namespace cg = cooperative_groups;
 
 constexpr int kMaxWarps = 16;
 constexpr int kMaxCluster = 8;
-constexpr int kCandidates = 1024;
 constexpr int kGroup = 4;                    // granules a thread loads and sums up at a time
 constexpr int kGroups = 64;                  // groups of threads whose maxima bound the n-th largest logit from below
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -208,13 +207,16 @@ struct Shared {
     float warp[3][kMaxWarps];                          // the warps' maxima and sums
     Sums part;                                         // this block's, read by the whole cluster
 };
+template <int NT>
 struct TopShared {
+    // one warp has short rows (and no cluster): with little shared memory more of them fit a multiprocessor
+    static constexpr int kCandidates = NT == 32 ? 128 : 1024, kGathered = NT == 32 ? 1 : kMaxCluster * QSR_MAX_TOP;
     float group[kGroups];
     unsigned count;
     float threshold;
     unsigned long long best, warp_best[kMaxWarps];
     unsigned long long top[QSR_MAX_TOP];
-    unsigned long long gathered[kMaxCluster * QSR_MAX_TOP];
+    unsigned long long gathered[kGathered];
     unsigned long long cand[kCandidates];
 };
 
@@ -222,9 +224,10 @@ struct TopShared {
 // the k-th largest element from below, and few elements reach it unless many are equal; those that do are ranked by
 // counting.  If they do not fit (masked or constant rows), or a NaN is about, k rounds of "largest below the last one" follow.
 template <typename T, bool STASH, int NT>
-__device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShared &sh, int k, float thread_max, bool has_nan)
+__device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShared<NT> &sh, int k, float thread_max, bool has_nan)
 {
     constexpr int kPer = Num<T>::kPer;
+    constexpr unsigned kCandidates = TopShared<NT>::kCandidates;
     const int tid = threadIdx.x, lane = tid & 31;
     constexpr int per_group = NT > kGroups ? NT / kGroups : 1, groups = NT / per_group;
     float gm = thread_max;
@@ -248,14 +251,20 @@ __device__ __forceinline__ void slice_top(const Slice<T, STASH, NT> &sl, TopShar
             if (Num<T>::value(Num<T>::max_of(Num<T>::nothing(), w)) < thr) continue;
             float x[kPer];
             Num<T>::widen(x, w);
+            unsigned hits = 0u;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const int64_t j = sl.first(g) + i;
-                if (x[i] >= thr && j >= 0 && j < sl.vocab) {
-                    const unsigned at = atomicAdd(&sh.count, 1u);
-                    if (at < kCandidates) sh.cand[at] = key_of(x[i], uint32_t(j));
-                }
+                if (x[i] >= thr && j >= 0 && j < sl.vocab) hits |= 1u << i;
             }
+            if (hits == 0u) continue;
+            unsigned at = atomicAdd(&sh.count, unsigned(__popc(hits)));      // one for all of the granule: it is the slow part
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (hits >> i & 1u) {
+                    if (at < kCandidates) sh.cand[at] = key_of(x[i], uint32_t(sl.first(g) + i));
+                    ++at;
+                }
         }
     }
     __syncthreads();
@@ -569,7 +578,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
 {
     extern __shared__ uint4 stash[];
     __shared__ Shared sh;
-    __shared__ typename std::conditional<TOP, TopShared, int>::type top_sh;
+    __shared__ typename std::conditional<TOP, TopShared<NT>, int>::type top_sh;
     const int tid = threadIdx.x, cluster = 1 << log2_cluster;
     const int64_t r = blockIdx.x >> log2_cluster;
     const int rank = int(blockIdx.x) & (cluster - 1);
@@ -586,13 +595,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
     const float c = p.tau_log2e;
     float thread_max;
     Sums all = p.entropy || p.d_entropy ? sums_of<T, STASH, NT, true>(sl, c, sh, thread_max) : sums_of<T, STASH, NT, false>(sl, c, sh, thread_max);
-    if (TOP) slice_top<T, STASH, NT>(sl, reinterpret_cast<TopShared &>(top_sh), p.n_top, thread_max, isnan(all.m));
+    if (TOP) slice_top<T, STASH, NT>(sl, reinterpret_cast<TopShared<NT> &>(top_sh), p.n_top, thread_max, isnan(all.m));
     if (cluster > 1) {
         cg::cluster_group cl = cg::this_cluster();
         if (tid == 0) sh.part = all;
         if (TOP) {
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-            TopShared &mine = reinterpret_cast<TopShared &>(top_sh);
+            TopShared<NT> &mine = reinterpret_cast<TopShared<NT> &>(top_sh);
             unsigned long long *gather = cl.map_shared_rank(mine.gathered, 0);
             if (tid < p.n_top) gather[rank * p.n_top + tid] = mine.top[tid];
         }
@@ -613,7 +622,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
             if (p.stats) { p.stats[2 * r] = all.m; p.stats[2 * r + 1] = ln_s; }
         }
         if (TOP) {
-            TopShared &mine = reinterpret_cast<TopShared &>(top_sh);
+            TopShared<NT> &mine = reinterpret_cast<TopShared<NT> &>(top_sh);
             if (cluster > 1) {
                 const int n = cluster * p.n_top;
                 for (int i = tid; i < n; i += NT) {
@@ -692,7 +701,7 @@ Shape shape_of(const LogprobParams &p, int element)
            (bytes > kSliceBytes << s.log2_cluster || ((p.rows << s.log2_cluster) * 2 <= kMultiprocessors && bytes >= int64_t(8192) << s.log2_cluster)))
         s.log2_cluster++;
     const int64_t granules = ((bytes / 16 - 1) >> s.log2_cluster) + 2;
-    s.threads = granules <= 256 ? 32 : granules <= 1024 ? 128 : granules <= 4608 ? 256 : 512;
+    s.threads = granules <= 256 && s.log2_cluster == 0 ? 32 : granules <= 1024 ? 128 : granules <= 4608 ? 256 : 512;
     s.smem = granules * 16;
     return s;
 }
