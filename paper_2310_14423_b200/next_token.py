@@ -56,7 +56,7 @@ def logits_of(weights: List[torch.Tensor], tokens: torch.Tensor) -> torch.Tensor
     return h @ head
 
 
-def train(workers: int = 4, steps: int = 400, vocab: int = 1000, width: int = 128, rows: int = 16, length: int = 32, states: str = "e4m3",
+def train(workers: int = 4, steps: int = 400, vocab: int = 1000, width: int = 128, rows: int = 64, length: int = 32, states: str = "e4m3",
           state_sync: str = "keep", eta_max: float = 8e-3, alpha: float = 0.0175, h_base: int = 4, clip: float = 1.0, seed: int = 1,
           log=None) -> Dict[str, float]:
     """One run; returns the last held-out loss, the chain's entropy rate, rounds and kernel launches."""
