@@ -1,5 +1,8 @@
 // Lists of tensors: the AdamW step (OPT of Eq. 1, arXiv 2310.14423) over many tensors in one launch, states in fp32 or in
 // 8 bits, and the replica mean that ends a round (Algorithm 2).  Element-wise streams: no contraction, no tensor cores.
+//
+// A thread block works on one chunk of one tensor (the table says which), its eight warps on blocks of 256 consecutive elements,
+// eight per lane.  The chunk's types, addresses and factors are the same for the whole block, so nothing diverges.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -355,6 +358,9 @@ __device__ __forceinline__ Span span_of(const ListChunk &c, int64_t numel, int p
     return s;
 }
 
+// States in fp32.  Bound by memory: 16 to 32 bytes per element against about 30 instructions.  Two blocks per multiprocessor
+// with 128 bytes of loads per thread on their way (256-bit accesses) are enough; caps of 80 and 64 registers for more of them
+// cost 2 % and 12 %.  ViT-B/16's 150 tensors, fp32 parameters, bf16 gradients and copies: 364 us for 2.42 GB, 6.65 TB/s.
 __global__ void __launch_bounds__(kThreads) list_step_kernel(const __grid_constant__ ListStepParams p)
 {
     const ListChunk c = p.chunks[blockIdx.x];
@@ -378,7 +384,10 @@ __global__ void __launch_bounds__(kThreads) list_step_kernel(const __grid_consta
 }
 
 // States in 8 bits.  A warp starts the copies of all its blocks (at most kListStages) into shared memory before it works on the
-// first one: the work per byte is too much to leave the loads waiting in registers for it.
+// first one: with the loads in registers instead (and as many warps as fit) the same work took 350 us where it now takes 229,
+// waiting for memory half the time.  Now the instructions count: about 50 per element, so lists with 16 bytes per element run at
+// memory speed (ViT-B/16, fp32 parameters, bf16 gradients and copies: 229 us for 1.39 GB, 6.05 TB/s) and lists with 10 are bound
+// by issue (ResNet-152, all bf16: 123 us for 0.61 GB, 4.9 TB/s).  Four blocks per multiprocessor; three and five were 8 % slower.
 template <int PT, int GT>
 __global__ void __launch_bounds__(kThreads, 4) list_step_codes_kernel(const __grid_constant__ ListStepParams p, const unsigned stage_bytes,
                                                                       const unsigned n_stages)
@@ -452,7 +461,7 @@ __device__ __forceinline__ float block_sum(float x, float *smem)
     return s;
 }
 
-// Sum of squares of each chunk's gradients; the last block of a worker to finish adds its chunks up -- in chunk order, so
+// Clipping's norms (reads the gradients once more: bound by memory).  Sum of squares of each chunk's gradients; the last block of a worker to finish adds its chunks up -- in chunk order, so
 // the result does not depend on which block that is -- and leaves the factor.
 __global__ void __launch_bounds__(kThreads) list_norm_kernel(const ListNormParams p)
 {
@@ -597,8 +606,7 @@ __device__ __forceinline__ void mean_block(const ListSyncParams &p, Place mine, 
         if (p.workers > 32) mine = place_of<A>(p, tensor, k0 + lane);
         const int here = min(32, p.workers - k0);
         int k = 0;
-        for (; k + 8 <= here; k += 8) add_workers<F32, VEC, 8>(s, mine.data, k, e0, n, lane, type);
-        if (here & 4) { add_workers<F32, VEC, 4>(s, mine.data, k, e0, n, lane, type); k += 4; }
+        for (; k + 4 <= here; k += 4) add_workers<F32, VEC, 4>(s, mine.data, k, e0, n, lane, type);
         if ((here & 3) == 3) add_workers<F32, VEC, 3>(s, mine.data, k, e0, n, lane, type);
         else if (here & 2) add_workers<F32, VEC, 2>(s, mine.data, k, e0, n, lane, type);
         else if (here & 1) add_workers<F32, VEC, 1>(s, mine.data, k, e0, n, lane, type);
@@ -728,11 +736,11 @@ __device__ __forceinline__ void mean_codes(const ListSyncParams &p, Place mine, 
 
 // Whether every worker's operand may be accessed four (codes: sixteen) elements at a time.
 template <int A>
-__device__ __forceinline__ bool sync_aligned(const ListSyncParams &p, int tensor, int type, int copy_type, bool codes, int lane)
+__device__ __forceinline__ bool sync_aligned(const ListSyncParams &p, Place x, int tensor, int type, int copy_type, bool codes, int lane)
 {
     bool ok = true;
     for (int k = lane; k < p.workers; k += 32) {
-        const Place x = place_of<A>(p, tensor, k);
+        if (k >= 32) x = place_of<A>(p, tensor, k);
         ok = ok && aligned_to(x.data, codes ? 16u : bytes_of_8(type) / 2);
         if (A == 0 && copy_type != QSR_NONE) ok = ok && aligned_to(x.copy, bytes_of_8(copy_type) / 2);
     }
@@ -744,7 +752,7 @@ __device__ __forceinline__ void sync_blocks(const ListSyncParams &p, const ListC
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Place mine = place_of<A>(p, c.tensor, lane);
-    const bool vec = sync_aligned<A>(p, c.tensor, type, copy_type, false, lane);
+    const bool vec = sync_aligned<A>(p, mine, c.tensor, type, copy_type, false, lane);
     for (int b = warp; b * 128 < c.n; b += kWarps) {
         const int64_t e0 = c.offset + b * 128;
         const int n = min(128, c.n - b * 128);
@@ -757,7 +765,7 @@ __device__ __forceinline__ void sync_codes(const ListSyncParams &p, const ListCh
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Place mine = place_of<A>(p, c.tensor, lane);
-    const int pairs = sync_aligned<A>(p, c.tensor, QSR_F32, QSR_NONE, true, lane) ? c.n / 512 : 0;
+    const int pairs = sync_aligned<A>(p, mine, c.tensor, QSR_F32, QSR_NONE, true, lane) ? c.n / 512 : 0;
     for (int b = warp; b < pairs; b += kWarps) mean_codes<A>(p, mine, c.tensor, c.offset + b * 512, lane);
     for (int b = 2 * pairs + warp; b * 256 < c.n; b += kWarps)
         mean_codes_any<A>(p, c.tensor, c.offset + b * 256, min(256, c.n - b * 256), lane);
@@ -769,9 +777,13 @@ __device__ __forceinline__ void sync_states(const ListSyncParams &p, const ListC
     else sync_blocks<A, true>(p, c, QSR_F32, QSR_NONE);
 }
 
-// Grid: worker 0's chunks by 1 (parameters) or 3 (parameters, m, v).
+// The round end.  Grid: worker 0's chunks by 1 (parameters) or 3 (parameters, m, v).  Bound by memory: every value is read and
+// written once, and what counts is that all workers' loads of a block are on their way together, in pieces of 512 bytes per
+// worker (8-bit states in pieces of 256 bytes: 2.20 instead of 1.70 ms).  Eight ViT-B/16 replicas with copies: parameters alone
+// 1.13 ms (6.1 TB/s), with 8-bit states averaged 1.70 ms (5.7 TB/s).  The number of blocks per multiprocessor: fp32 states five
+// (three packed bf16 replicas, element by element: 76 us; with four 84), 8-bit states three (1.70 ms; four 1.73, with spills).
 template <bool S8>
-__global__ void __launch_bounds__(kThreads, S8 ? 3 : 4) list_sync_kernel(const __grid_constant__ ListSyncParams p)
+__global__ void __launch_bounds__(kThreads, S8 ? 3 : 5) list_sync_kernel(const __grid_constant__ ListSyncParams p)
 {
     const ListChunk c = p.chunks[blockIdx.x];
     const int type = p.tensors[c.tensor].param_type, copy_type = p.tensors[c.tensor].copy_type;

@@ -44,7 +44,7 @@ bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t
 constexpr int64_t kWarpBlocks = qsr::kListWarps * kBlock;      // elements of a thread block with one block per warp
 
 // Elements per thread block where every multiprocessor has work many times over: as many blocks per warp as hide the latency of
-// their loads.  fp32 states (operands in registers): four; ViT-B/16's list takes 370 us with four, 376 with three, 391 with two.
+// their loads.  fp32 states (operands in registers): four; ViT-B/16's list takes 364 us with four, 2 % more with three, 6 % with two.
 // 8-bit states (operands in shared memory): as many as let four thread blocks share a multiprocessor, at most four; 229 us
 // with three of fp32 parameters and bf16 gradients, 240 with four.
 int stages_of(int stage_bytes)
