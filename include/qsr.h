@@ -305,7 +305,7 @@ int qsr_train_host(const qsr_config *cfg, const float *theta0_host, const float 
  * The optimizer step and the round end over a model's own tensors, wherever they lie, instead of over [K, P] slabs: AdamW
  * (OPT of Eq. 1 as at qsr_config) on bf16, fp16 or fp32 parameters and gradients with fp32 or 8-bit states, and the
  * All-Reduce line of Algorithm 2 over K copies of the same tensors.  A list is made once from the tensors' addresses and
- * used every step; all tensors are handled by one launch (three with clipping on).
+ * used every step; all tensors are handled by one launch (two with clipping on).
  *
  * Per element, with g = grad_scale * grad (times the worker's clipping factor) and everything in fp32:
  *   m <- m + (1-beta1)*(g - m);  v <- v + (1-beta2)*(g*g - v);
@@ -364,7 +364,8 @@ int64_t qsr_list_workspace_bytes(const int64_t *numel_host, int32_t n_tensors, i
  * qsr_list_destroy; it is filled by copies enqueued on cuda_stream, on which all later work of the list is enqueued too.
  * QSR_EINVAL: NULL, unknown type, numbers that are not finite, betas outside [0, 1), sizes or types that differ between
  * workers, or a written range that overlaps any other range of the list (tied weights: list them once); QSR_EALIGN: a pointer
- * not aligned to its element; QSR_ERANGE: workspace too small.  No tensor is written. */
+ * not aligned to its element; QSR_ERANGE: workspace too small; QSR_ESTATE: the stream is being captured (the tables' copies
+ * would be replayed from memory that is gone).  No tensor is written. */
 int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor *tensors_host, void *workspace_dev,
                     int64_t workspace_bytes, void *cuda_stream);
 
@@ -372,7 +373,8 @@ int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor
 int qsr_list_destroy(qsr_list *list);
 
 /* New gradient addresses (host array of n_tensors device pointers, read during the call), same types: for training loops
- * whose gradients are allocated anew every step.  One small copy on the stream; asynchronous. */
+ * whose gradients are allocated anew every step.  They must not overlap what the list writes.  One small copy on the stream;
+ * asynchronous.  QSR_ESTATE: the stream is being captured, or another device than the list's is current. */
 int qsr_list_set_grads(qsr_list *list, const void *const *grads_host);
 
 /* One AdamW step of every tensor, formula above; n >= 1 counts the steps the states have seen (t + 1 - t_state_origin),
@@ -429,7 +431,7 @@ typedef struct qsr_logprob_args {
 
 /* The forward quantities, and, if d_logits is not NULL, the gradient in the same pass over the logits (for losses whose
  * d_logprob and d_entropy are known beforehand, such as cross entropy).  No context; one launch on cuda_stream (none for
- * rows = 0); asynchronous. */
+ * rows = 0) of the current device, where all arrays lie; asynchronous. */
 int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream);
 
 /* The gradient by itself, for losses whose d_logprob depends on logprob: reads logits, tokens, row_stats (and entropy if

@@ -143,6 +143,13 @@ cudaError_t upload(void *dst, const void *src, size_t bytes, cudaStream_t st)
     return bytes ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaSuccess;
 }
 
+// A captured copy from pageable memory would read it at every replay.
+bool capturing(cudaStream_t st)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    return cudaStreamIsCapturing(st, &status) == cudaSuccess && status != cudaStreamCaptureStatusNone;
+}
+
 bool on_own_device(const qsr_list &x)
 {
     int dev = -1;
@@ -206,6 +213,7 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return QSR_ECUDA; }
+    if (capturing(static_cast<cudaStream_t>(cuda_stream))) return QSR_ESTATE;
     qsr_list *x = new qsr_list;
     char *ws = static_cast<char *>(workspace);
     x->cfg = cfg;
@@ -276,7 +284,7 @@ int qsr_list_set_grads(qsr_list *list, const void *const *grads_host)
 {
     if (!list || !grads_host) return QSR_EINVAL;
     if (int rc = check_grads(list->cfg, list->host.data(), grads_host)) return rc;
-    if (!on_own_device(*list)) return QSR_ESTATE;
+    if (!on_own_device(*list) || capturing(list->stream)) return QSR_ESTATE;
     const int rc = cuda_rc(upload(list->grads, grads_host, size_t(list->cfg.n_tensors) * sizeof(void *), list->stream));
     list->has_grads = rc == QSR_OK;
     return rc;

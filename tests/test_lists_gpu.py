@@ -449,3 +449,26 @@ def test_many_chunks_and_offsets_beyond_32_bits():
     for a, b in ((p[at:], small[0]), (m[at:].view(torch.uint8), small[2].view(torch.uint8)), (vs[at // 256:], small[5])):
         assert torch.equal(a, b)
     assert bool((p[:1 << 20] == 0).all()) and float(ms[:at // 256].abs().max()) == 0.0
+
+
+def test_tables_are_not_uploaded_during_a_capture():
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        L = Lists([300])
+        side.synchronize()
+        ws = torch.empty_like(L.workspace)
+        status = []
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            for call in (lambda: L.list.qsr_list_set_grads(L.g),
+                         lambda: B.TensorList([torch.zeros_like(x) for x in L.p], None, L.m, L.v, workspace=ws, stream=_stream())):
+                try:
+                    call()
+                    status.append(0)
+                except B.QsrError as e:
+                    status.append(e.status)
+            L.list.qsr_list_step(6, 1e-2)
+        graph.replay()
+        side.synchronize()
+    assert status == [B.QSR_ESTATE, B.QSR_ESTATE]
+    check_step(L, expected(L, 6, 1e-2, 0.0))
