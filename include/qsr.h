@@ -406,8 +406,8 @@ int64_t qsr_list_launch_count(const qsr_list *list);
  *   d_logits[j] = tau * ( d_logprob*([j = y] - p_j) - d_entropy*p_j*(ln p_j + H) ),  rounded once to the logits' type.
  * Logits of -inf are masked tokens: p = 0 and no gradient.  A row with nothing but -inf: logprob -inf, H = 0, top_logprob
  * -inf (tokens 0, 1, ...), gradient 0.  A token < 0 marks a row without a score: logprob 0 and no d_logprob term.  A token
- * >= vocab, a NaN or a +inf in the row: NaN.  Sums are kept in fp32, (x - M) is formed before it is scaled, so rows that
- * hold the type's lowest value are treated like any other.
+ * >= vocab, a NaN or a +inf in the row: NaN.  Sums are kept in fp32 and tau*(x - M) is as accurate for large logits as for
+ * small ones, so rows masked with -1e10, say, or with the type's lowest value are treated like any other.
  */
 typedef struct qsr_logprob_args {
     const void *logits;      /* device, logits_type, [rows, row_stride], any element alignment                  */

@@ -35,7 +35,9 @@ constexpr int kMaxCluster = 8;
 constexpr int kGroup = 4;                    // granules a thread loads and sums up at a time
 constexpr int kGroups = 64;                  // groups of threads whose maxima bound the n-th largest logit from below
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kFastMax = 1e30f;            // logits (and scaled ones) below this leave room for every difference and product
+// The fast exponents c x - K take a rounded K = c m, so the largest term's own is up to ulp(K) / 2 instead of 0.
+constexpr float kBaseMax = 0x1p31f;          // sums: at most 64, so terms stay within 2^64 of what they are relative to m
+constexpr float kGradMax = 0x1p24f;          // gradient, whose constant holds log2 S too: at most 2, so nothing cancels in A and B
 constexpr float kLowest2 = -200.0f;          // 2^-200 = 0 in fp32: log2-probabilities below are raised to it, so that 0 * (-inf) never forms
 
 template <typename T> struct Num;            // how sixteen bytes of a type are taken apart
@@ -346,7 +348,7 @@ __device__ __forceinline__ RowGrad row_grad(const LogprobParams &p, int64_t r, i
     q.B = b * kLn2;
     const float K = q.c * q.m;
     q.L = K + q.log2_s;
-    q.fast = fabsf(K) < kFastMax && fabsf(q.m) < kFastMax;
+    q.fast = fabsf(K) < kGradMax;
     if (q.fast) {
         // c m + log2 S - L, each step exact or as small as what it corrects
         const float delta = fmaf(q.c, q.m, -K) + ((K - q.L) + q.log2_s), f = exp2_1(-delta);
@@ -449,7 +451,9 @@ __device__ __forceinline__ void write_grad(const Slice<T, STASH, NT> &sl, T *out
 
 // A thread's running maximum and sums: e = 2^z and e z with z = c x - K, K a rounded c m.  One operation forms z and nothing is
 // lost by it: the product is exact inside the fused multiply-add, and K is the same constant in every term; what K lacks of
-// c m is put back at the end (relative_to).  `odd`: a NaN, an infinity or a maximum so large that c x may overflow.
+// c m is put back at the end (relative_to).  That holds while |K| < kBaseMax.  A maximum below that range (a thread that
+// has only seen a mask of -1e10, say) takes K = -kBaseMax: its sums are then 0 or something finite, and count for nothing next to
+// a maximum inside the range.  `odd`: a NaN or a maximum above the range.
 template <bool ENTROPY>
 struct Running {
     float m = -infinity(), K = 0.0f;
@@ -465,8 +469,8 @@ struct Running {
         for (int k = 0; k < N; ++k) most = Num<T>::max_of(most, w[k]);
         const float x = Num<T>::value(most);
         if (!(x <= m)) {
-            const float K1 = x * c;
-            odd = odd || !(fabsf(x) < kFastMax) || !(fabsf(K1) < kFastMax);
+            const float cx = x * c, K1 = fmaxf(cx, -kBaseMax);
+            odd = odd || !(cx < kBaseMax);
             if (m > -infinity()) shift(K - K1);
             m = x;
             K = K1;
@@ -494,12 +498,13 @@ struct Running {
     }
     __device__ __forceinline__ Sums relative_to(float most, float c)
     {
-        if (m > -infinity()) shift(fmaf(-c, most, K));
+        if (m > -infinity()) shift(fminf(fmaf(-c, most, K), 64.0f));      // 64 at most inside the range
         return Sums{most, s.x + s.y, t.x + t.y};
     }
 };
 
-// The slow way for slices that are `odd`: the maximum first (NaN if there is one), then the terms with z = c (x - m).
+// The slow way for slices whose maximum is a NaN or out of the fast exponents' range: the maximum first (NaN if there is one),
+// then the terms with z = c (x - m).
 template <typename T, bool STASH, int NT>
 __device__ __forceinline__ Sums sums_of_odd(const Slice<T, STASH, NT> &sl, float c, Shared &sh)
 {
@@ -578,6 +583,8 @@ __device__ __forceinline__ Sums sums_of(const Slice<T, STASH, NT> &sl, float c, 
         all.s = warp_sum(all.s);
         all.t = warp_sum(all.t);
     }
+    // the slice's maximum itself below the range, or so near its end that threads below may count
+    odd = odd || (all.m > -infinity() && !(all.m * c > 4096.0f - kBaseMax));
     return odd ? sums_of_odd<T, STASH, NT>(sl, c, sh) : all;
 }
 
@@ -662,9 +669,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const __grid_con
 
 constexpr int kGradPer = 4;                   // granules in flight per thread
 
-// The gradient alone, from the statistics of an earlier call.  Grid: 2^log2_parts parts of a row by rows.
+// The gradient alone, from the statistics of an earlier call.  Grid: 2^log2_parts parts of a row by rows.  Six blocks of 256
+// threads per multiprocessor (40 registers): with 43 and five blocks the two calls on 2048 x 50001 bf16 took 150 us instead of 146.
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT) logprob_grad_kernel(const __grid_constant__ LogprobParams p, const int log2_parts)
+__global__ void __launch_bounds__(NT, NT == 256 ? 6 : 1) logprob_grad_kernel(const __grid_constant__ LogprobParams p, const int log2_parts)
 {
     const int64_t r = blockIdx.x >> log2_parts;
     const T *const row = static_cast<const T *>(p.logits) + r * p.stride;

@@ -346,3 +346,59 @@ def test_no_rows_and_python_refusals():
     with pytest.raises(B.QsrError) as e:
         B.qsr_token_logprobs_grad(x, y, f(3, 2), f(3, 5), d_entropy=o)      # entropy is needed
     assert e.value.status == B.QSR_EINVAL
+
+
+FAR = [-1e9, -1e10, -1e12, -1e15, -1e20, -1e29]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [37, 1024, 20001, 140000, 300000])
+def test_logits_far_from_zero(kind, V):
+    """Masks and whole rows of large magnitude, short of the type's lowest value: scattered, over whole threads, warps and
+    slices, several of them in one row, and rows whose largest logit is itself far below or above zero."""
+    rng = np.random.default_rng(V)
+    at, base = np.arange(V), rng.normal(0, 2, V)
+    rows, y = [], []
+
+    def add(row, token):
+        rows.append(np.broadcast_to(np.asarray(row, np.float64), (V,)).copy())
+        y.append(token)
+
+    for far in FAR if V < 50000 else FAR[1::3]:
+        add(np.where(rng.random(V) < 0.9, far, base), int(rng.integers(V)))
+        add(np.where(at < V - V // 8 - 1, far, base), V - 1)
+        add(np.where(at > V // 8, far, base), 0)
+        add(np.where(at == V // 2, base, far), V // 2)
+        add(far, V // 3)
+        add(np.where(at % 3 == 0, far, -math.inf), 0)
+        add(np.where(at % 2 == 0, far, 4 * far), 1)
+        add(-far, V // 2)
+        add(np.where(at == V // 2, -far, base), V // 2)
+        add(np.where(at < V // 2, -far, far), 0)
+    add(np.where(at < V // 2, base, np.asarray(FAR)[at % len(FAR)]), 0)
+    x = np.stack(rows)
+    a, b = rng.normal(0, 1, len(rows)), rng.normal(0, 1, len(rows))
+    for first in range(0, len(rows), 12):                 # few rows at a time: long ones are shared out over clusters then
+        s = slice(first, first + 12)
+        for fused in (True, False):
+            c = Call(x[s], y[s], kind)
+            c.forward(1.0, top=min(V, 5), a=a[s], b=b[s], fused=fused)
+            if not fused:
+                c.backward(1.0)
+            c.check(1.0, top=min(V, 5), a=a[s], b=b[s], gradient=True)
+
+
+@pytest.mark.parametrize("tau", [1e-9, 0.5, 1e6, 1e9])
+@pytest.mark.parametrize("V", [1024, 60000])
+def test_temperatures_far_from_one(V, tau):
+    """Scaled logits far from zero: ordinary logits and ones that differ by little, about ten and about minus ten."""
+    rng = np.random.default_rng(7)
+    near = rng.integers(-8, 8, (3, V)) * 2.0 ** -20
+    x = np.concatenate([rng.normal(0, 3, (2, V)), 10 + near, near - 10, np.where(rng.random((2, V)) < 0.9, -1e9, rng.normal(0, 3, (2, V)))])
+    y, a, b = rng.integers(0, V, len(x)), rng.normal(0, 1, len(x)), rng.normal(0, 1, len(x))
+    for fused in (True, False):
+        c = Call(x, y, "f32")
+        c.forward(tau, top=3, a=a, b=b, fused=fused)
+        if not fused:
+            c.backward(tau)
+        c.check(tau, top=3, a=a, b=b, gradient=True)
