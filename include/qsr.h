@@ -317,7 +317,8 @@ int qsr_train_host(const qsr_config *cfg, const float *theta0_host, const float 
  * can span a factor of 2^35 in v), scale = fl(amax * fl(1/448)) with amax the block's largest finite magnitude; codes are
  * fl(x * fl(1/scale)) rounded to nearest even, saturating at 448.  A positive sqrt(v) never becomes 0 (its smallest code is
  * 2^-9), because a vanished denominator would turn a small m into a huge step.  A block whose amax is below 2^-100 is
- * stored as zeros.  The scale is a full fp32 number, not a power of two, so that the largest element of a block decays as it
+ * stored as zeros.  An infinite m or sqrt(v) (a finite gradient whose square overflows has the latter) is stored as the saturated
+ * code, in a block of scale 0 as 0.  The scale is a full fp32 number, not a power of two, so that the largest element of a block decays as it
  * would in fp32 and takes the others along; three mantissa bits alone would hold 0.999*v at v.  The update itself uses the new
  * m and v before they are rounded to 8 bits.  A NaN in one element stays in that element.
  *

@@ -37,7 +37,19 @@ __device__ __forceinline__ BlockScale block_scale(float amax)
     return b;
 }
 
-__device__ __forceinline__ float finite_or_0(float a) { return a < infinity() ? a : 0.0f; }
+// The largest magnitude of a lane's N values; infinities (a sum or a square beyond fp32) do not count, and become the largest
+// finite number, whose code is 448 as theirs, or 0 where the scale is 0 (infinity * 0 would be NaN).
+template <int N>
+__device__ __forceinline__ float amax_of_finite(float (&x)[N])
+{
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (fabsf(x[i]) == infinity()) x[i] = copysignf(3.402823466e38f, x[i]);
+        else amax = fmaxf(amax, fabsf(x[i]));
+    }
+    return amax;
+}
 
 __device__ __forceinline__ float code_of(float x, float inv, bool positive)
 {
@@ -151,7 +163,7 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __
 __device__ __forceinline__ float2 add2(float2 a, float2 b, float one) { return __ffma2_rn(b, both(one), a); }
 __device__ __forceinline__ float2 sub2(float2 a, float2 b) { return __ffma2_rn(b, both(-1.0f), a); }
 
-// sqrt(v) rounded to nearest for v >= 2^-100: one Newton step on s = v * rsqrt(v) with the residual v - s^2 formed by a fused
+// sqrt(v) rounded to nearest for finite v >= 2^-100: one Newton step on s = v * rsqrt(v) with the residual v - s^2 formed by a fused
 // multiply-add (Markstein, IBM J. Res. Dev. 34, 1990).  Half the instructions of the general root, which also has to deal
 // with the operands excluded here.
 __device__ __forceinline__ float2 root2(float2 v)
@@ -251,7 +263,7 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
     from_e4m3x4(m[2], m[3], mw.y);
     from_e4m3x4(u[0], u[1], vw.x);
     from_e4m3x4(u[2], u[3], vw.y);
-    float least = infinity();
+    float least = infinity(), most = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float2 gi = make_float2(g[2 * i], g[2 * i + 1]);
@@ -260,9 +272,10 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
         m[i] = add2(m0, mul2(both(p.omb1), sub2(gi, m0)), p.one);
         u[i] = add2(v0, mul2(both(p.omb2), sub2(mul2(gi, gi), v0)), p.one);
         least = min3(least, u[i].x, u[i].y);
+        most = max3_abs(most, u[i].x, u[i].y);
     }
-    const bool tiny = least < 0x1p-100f;
-    if (!tiny) {
+    const bool general = least < 0x1p-100f || most == infinity();       // g * g may overflow where g does not
+    if (!general) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = root2(u[i]);
     } else {
@@ -291,25 +304,17 @@ __device__ __forceinline__ float2 step_block_codes(const ListStepParams &p, cons
         *reinterpret_cast<float4 *>(stage + piece(2 * lane) * 16) = make_float4(th[0], th[1], th[2], th[3]);
         *reinterpret_cast<float4 *>(stage + piece(2 * lane + 1) * 16) = make_float4(th[4], th[5], th[6], th[7]);
     }
-    am = warp_max(am);
-    au = warp_max(au);
     if (fmaxf(am, au) == infinity()) {                // only finite values make the scale
-        am = au = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            am = fmaxf(am, fmaxf(finite_or_0(fabsf(m[i].x)), finite_or_0(fabsf(m[i].y))));
-            au = fmaxf(au, fmaxf(finite_or_0(u[i].x), finite_or_0(u[i].y)));
-        }
-        am = warp_max(am);
-        au = warp_max(au);
+        am = amax_of_finite(reinterpret_cast<float (&)[8]>(m));
+        au = amax_of_finite(reinterpret_cast<float (&)[8]>(u));
     }
-    const BlockScale bm = block_scale(am), bu = block_scale(au);
+    const BlockScale bm = block_scale(warp_max(am)), bu = block_scale(warp_max(au));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         m[i] = mul2(m[i], both(bm.inv));
         u[i] = mul2(u[i], both(bu.inv));
         // what is positive stays positive; a lane without zeros need not ask which elements are
-        if (!tiny) u[i] = make_float2(max_nan(u[i].x, kCodeMin), max_nan(u[i].y, kCodeMin));
+        if (!general) u[i] = make_float2(max_nan(u[i].x, kCodeMin), max_nan(u[i].y, kCodeMin));
         else u[i] = make_float2(u[i].x > 0.0f ? fmaxf(u[i].x, kCodeMin) : u[i].x, u[i].y > 0.0f ? fmaxf(u[i].y, kCodeMin) : u[i].y);
     }
     const uint2 m_codes = make_uint2(to_e4m3x4(m[0], m[1]), to_e4m3x4(m[2], m[3])), v_codes = make_uint2(to_e4m3x4(u[0], u[1]), to_e4m3x4(u[2], u[3]));
@@ -646,9 +651,9 @@ __device__ __forceinline__ float finish_states(float (&s)[N], const ListSyncPara
     for (int i = 0; i < N; ++i) {
         s[i] = mean_of(s[i], p);
         if (A == 2) s[i] = __fsqrt_rn(s[i]);
-        amax = fmaxf(amax, finite_or_0(fabsf(s[i])));
+        amax = fmaxf(amax, fabsf(s[i]));
     }
-    return amax;
+    return amax == infinity() ? amax_of_finite(s) : amax;
 }
 
 // Mean of a block of 256 8-bit states, rounded to 8 bits once: ragged blocks and unaligned tensors, byte by byte.

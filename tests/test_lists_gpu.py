@@ -472,3 +472,91 @@ def test_tables_are_not_uploaded_during_a_capture():
         side.synchronize()
     assert status == [B.QSR_ESTATE, B.QSR_ESTATE]
     check_step(L, expected(L, 6, 1e-2, 0.0))
+
+
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("lead", [64, 1])
+def test_gradients_whose_square_overflows(lead, grad, states):
+    """Gradients of 3e19 (finite) and infinite ones, among ordinary neighbours and zeros, in whole blocks and ragged ends.  The
+    formula in fp32: v and its root are infinite, so a finite gradient's update is 0; the root saturates at 448 in 8 bits."""
+    n, lr, wd = 1300, 1e-2, 0.1
+    big = {3: 3e19, 300: -3e19, 600: 3e19, 700: math.inf, 900: -math.inf, 1290: 3e19}
+    L = Lists([n], grad=grad, states=states, lead=lead, weight_decay=wd, seed=11)
+    L.wd[0] = 1.0
+    L.list = B.TensorList(L.p, L.g, L.m, L.v, m_scale=L.ms, v_scale=L.vs, workspace=L.workspace, stream=_stream(), weight_decay=wd)
+    codes = states == "e4m3"
+    for lo, hi in ((296, 304), (512, 768)):                # zero neighbours: a lane's eight; a whole block, of gradients and states
+        for x in (L.g, L.m, L.v):
+            x[0][lo:hi].view(torch.uint8).zero_()
+    for i, g in big.items():
+        L.g[0][i] = g
+    L.before = L.numpy()
+    finite = [i for i in big if math.isfinite(big[i])]
+    infinite = [i for i in big if not math.isfinite(big[i])]
+    ordinary = np.setdiff1d(np.arange(n), list(big))
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = expected(L, 6, lr, wd)
+    L.list.qsr_list_step(6, lr)
+    got = L.numpy()
+    theta = L.before["p"][0]
+    assert np.isnan(got["p"][0][infinite]).all()
+    # the decay: factor and product rounded, then the difference
+    assert np.all(np.abs(got["p"][0][finite] - theta[finite] * (1 - lr * wd)) <= 4 * U * np.abs(theta[finite]))
+    assert np.all(np.abs(got["p"][0][ordinary] - want[0][0][ordinary]) <= want[0][3][ordinary] + TINY["f32"])
+    m = np.asarray([0.1 * L.before["g"][0][i] for i in finite])
+    if not codes:
+        assert np.isposinf(got["v"][0][list(big)]).all() and np.isfinite(got["v"][0][ordinary]).all()
+        assert np.all(np.abs(got["m"][0][finite] - m) <= 1e-6 * np.abs(m)) and np.isinf(got["m"][0][infinite]).all()
+    else:
+        block_of = lambda i: i // 256                      # noqa: E731
+        assert np.isfinite(got["ms"][0]).all() and np.isfinite(got["vs"][0]).all()
+        assert not np.isnan(got["m"][0]).any() and not np.isnan(got["v"][0]).any()
+        assert np.all(np.abs(got["ms"][0][[block_of(i) for i in finite]] - np.abs(m) / 448) <= 1e-6 * np.abs(m) / 448)
+        assert [got["m"][0][i] for i in finite] == [math.copysign(448.0, big[i]) for i in finite]
+        # the block of 512..767 has no finite root above 0: it is stored as zeros
+        assert [got["v"][0][i] for i in big] == [0.0 if block_of(i) == 2 else 448.0 for i in big]
+        assert got["m"][0][900] == -448.0 and got["vs"][0][2] == 0 and (got["v"][0][512:768] == 0).all()
+        amax = np.sqrt(blocks(np.where(np.isin(np.arange(n), list(big)), 0.0, want[0][2])).max(1))
+        assert np.all(np.abs(got["vs"][0] - amax / 448) <= 16 * U * amax / 448)
+    L.assert_guards()
+    L.g[0].zero_()
+    L.list.qsr_list_step(7, lr)
+    after = L.numpy()
+    assert np.isfinite(after["p"][0][ordinary]).all() and np.isnan(after["p"][0][infinite]).all()
+    assert not codes or not (np.isnan(after["m"][0]).any() or np.isnan(after["v"][0]).any())
+
+
+@pytest.mark.parametrize("lead", [64, 1])
+def test_averaged_states_whose_sum_overflows(lead):
+    """8-bit states: sums of m and of v beyond fp32 saturate at 448 in their element, or vanish with a block of zeros."""
+    n, K = 1300, 3
+    L = Lists([n], K=K, states="e4m3", lead=lead, seed=12)
+    for k in range(K):
+        for x, s, top in ((L.m[k], L.ms[k], 2.0e38), (L.v[k], L.vs[k], 1.7e19)):
+            byte = x.view(torch.uint8)
+            byte[:256] = torch.arange(256, device=DEV) % 16 + 0x30          # 0.5 .. 1.9
+            byte[512:768] = 0
+            byte[1024:] = 0
+            for i in (5, 600, 1290):
+                byte[i] = 0x7e + 0x80 * (x is L.m[k] and i != 600)           # 448, or -448
+                s[i // 256] = top / 448
+    before = L.numpy()
+    L.list.qsr_list_sync("average")
+    got = L.numpy()
+    for name, scale, sign in (("m", "ms", -1.0), ("v", "vs", 1.0)):
+        ordinary = [np.setdiff1d(np.arange(256), [5]), np.arange(256, 512), np.arange(768, 1024)]
+        for k in range(K):
+            assert np.isfinite(got[scale][k]).all() and not np.isnan(got[name][k]).any()
+            assert got[name][k][5] == sign * 448.0
+            for block in (2, 5):
+                assert got[scale][k][block] == 0 and (got[name][k][block * 256:(block + 1) * 256] == 0).all()
+            assert np.array_equal(got[name][k], got[name][0]) and np.array_equal(got[scale][k], got[scale][0])
+        for span in ordinary:
+            x = np.stack([dequantise(before[name][k], before[scale][k])[span] for k in range(K)])
+            e = (K + 4) * U * np.abs(x).max(0)
+            x = x.mean(0) if name == "m" else np.sqrt((x * x).mean(0))
+            s = got[scale][0][span[0] // 256]
+            assert abs(s - np.abs(x).max() / 448) <= e.max() / 448 + 2 * U * np.abs(x).max() / 448
+            assert np.all(np.abs(got[name][0][span] * s - x) <= e + np.abs(x) * (2.0 ** -4 + 8 * U) + s * 2.0 ** -9)
+    L.assert_guards()
