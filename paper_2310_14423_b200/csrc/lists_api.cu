@@ -137,7 +137,8 @@ int check_list(const qsr_list_config &c, const qsr_tensor *t)
     return QSR_OK;
 }
 
-// Enqueues a copy from pageable host memory: such a copy is staged before the call returns, so the source may be freed.
+// Enqueues a copy from pageable host memory: such a copy is staged before the call returns, so the source may be freed.  A copy from
+// page-locked memory would read it whenever the stream gets there.
 cudaError_t upload(void *dst, const void *src, size_t bytes, cudaStream_t st)
 {
     return bytes ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaSuccess;
@@ -285,9 +286,14 @@ int qsr_list_set_grads(qsr_list *list, const void *const *grads_host)
     if (!list || !grads_host) return QSR_EINVAL;
     if (int rc = check_grads(list->cfg, list->host.data(), grads_host)) return rc;
     if (!on_own_device(*list) || capturing(list->stream)) return QSR_ESTATE;
-    const int rc = cuda_rc(upload(list->grads, grads_host, size_t(list->cfg.n_tensors) * sizeof(void *), list->stream));
-    list->has_grads = rc == QSR_OK;
-    return rc;
+    try {              // a copy of the caller's array, which may be page-locked: see upload
+        const std::vector<const void *> table(grads_host, grads_host + list->cfg.n_tensors);
+        const int rc = cuda_rc(upload(list->grads, table.data(), table.size() * sizeof(void *), list->stream));
+        list->has_grads = rc == QSR_OK;
+        return rc;
+    } catch (...) {    // out of host memory
+        return QSR_EINVAL;
+    }
 }
 
 int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale)

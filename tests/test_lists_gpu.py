@@ -560,3 +560,19 @@ def test_averaged_states_whose_sum_overflows(lead):
             assert abs(s - np.abs(x).max() / 448) <= e.max() / 448 + 2 * U * np.abs(x).max() / 448
             assert np.all(np.abs(got[name][0][span] * s - x) <= e + np.abs(x) * (2.0 ** -4 + 8 * U) + s * 2.0 ** -9)
     L.assert_guards()
+
+
+def test_gradient_table_in_page_locked_memory():
+    """The table is read during the call only, whatever memory it lies in: it is overwritten while the stream is still busy."""
+    L = Lists([100, 5000], grad="bf16", weight_decay=0.1)
+    fresh = [torch.randn(n, device=DEV).to(torch.bfloat16) for n in L.sizes]
+    others = [torch.zeros_like(g) for g in fresh]
+    table = torch.tensor([g.data_ptr() for g in fresh], dtype=torch.int64).pin_memory()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)                         # about 50 ms
+    assert B.lib().qsr_list_set_grads(L.list._h, table.data_ptr()) == B.QSR_OK
+    table.copy_(torch.tensor([g.data_ptr() for g in others], dtype=torch.int64))
+    L.list.qsr_list_step(6, 1e-2)
+    L.g = fresh
+    L.before["g"] = [g.double().cpu().numpy() for g in fresh]
+    check_step(L, expected(L, 6, 1e-2, 0.1))
