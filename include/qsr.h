@@ -366,7 +366,7 @@ int64_t qsr_list_workspace_bytes(const int64_t *numel_host, int32_t n_tensors, i
  * QSR_EINVAL: NULL, unknown type, numbers that are not finite, betas outside [0, 1), sizes or types that differ between
  * workers, or a written range that overlaps any other range of the list (tied weights: list them once); QSR_EALIGN: a pointer
  * not aligned to its element; QSR_ERANGE: workspace too small; QSR_ESTATE: the stream is being captured (the tables' copies
- * would be replayed from memory that is gone).  No tensor is written. */
+ * would be replayed from memory that is gone), or it is the legacy default stream while a blocking stream is.  No tensor is written. */
 int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor *tensors_host, void *workspace_dev,
                     int64_t workspace_bytes, void *cuda_stream);
 
@@ -375,7 +375,8 @@ int qsr_list_destroy(qsr_list *list);
 
 /* New gradient addresses (host array of n_tensors device pointers, read during the call), same types: for training loops
  * whose gradients are allocated anew every step.  They must not overlap what the list writes.  One small copy on the stream;
- * asynchronous.  QSR_ESTATE: the stream is being captured, or another device than the list's is current. */
+ * asynchronous.  QSR_ESTATE: the stream is being captured (as at qsr_list_create), or another device than the list's is
+ * current. */
 int qsr_list_set_grads(qsr_list *list, const void *const *grads_host);
 
 /* One AdamW step of every tensor, formula above; n >= 1 counts the steps the states have seen (t + 1 - t_state_origin),

@@ -144,11 +144,19 @@ cudaError_t upload(void *dst, const void *src, size_t bytes, cudaStream_t st)
     return bytes ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaSuccess;
 }
 
-// A captured copy from pageable memory would read it at every replay.
-bool capturing(cudaStream_t st)
+// QSR_ESTATE during a capture: a captured copy from pageable memory would read it at every replay.  The legacy default stream
+// takes no work while a blocking stream is being captured; the query says so with an error of its own, and an attempt would
+// invalidate that capture.
+int not_capturing(cudaStream_t st)
 {
     cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-    return cudaStreamIsCapturing(st, &status) == cudaSuccess && status != cudaStreamCaptureStatusNone;
+    const cudaError_t err = cudaStreamIsCapturing(st, &status);
+    if (err == cudaErrorStreamCaptureImplicit) {
+        cudaGetLastError();
+        return QSR_ESTATE;
+    }
+    if (err != cudaSuccess) return cuda_rc(err);
+    return status == cudaStreamCaptureStatusNone ? QSR_OK : QSR_ESTATE;
 }
 
 bool on_own_device(const qsr_list &x)
@@ -214,7 +222,7 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return QSR_ECUDA; }
-    if (capturing(static_cast<cudaStream_t>(cuda_stream))) return QSR_ESTATE;
+    if (int rc = not_capturing(static_cast<cudaStream_t>(cuda_stream))) return rc;
     qsr_list *x = new qsr_list;
     char *ws = static_cast<char *>(workspace);
     x->cfg = cfg;
@@ -285,7 +293,8 @@ int qsr_list_set_grads(qsr_list *list, const void *const *grads_host)
 {
     if (!list || !grads_host) return QSR_EINVAL;
     if (int rc = check_grads(list->cfg, list->host.data(), grads_host)) return rc;
-    if (!on_own_device(*list) || capturing(list->stream)) return QSR_ESTATE;
+    if (!on_own_device(*list)) return QSR_ESTATE;
+    if (int rc = not_capturing(list->stream)) return rc;
     try {              // a copy of the caller's array, which may be page-locked: see upload
         const std::vector<const void *> table(grads_host, grads_host + list->cfg.n_tensors);
         const int rc = cuda_rc(upload(list->grads, table.data(), table.size() * sizeof(void *), list->stream));

@@ -1,5 +1,6 @@
 """Tensor lists on the GPU -- AdamW steps with states in 32 and 8 bits, clipping, replica means -- against the formulas of
 include/qsr.h in binary64 (numpy).  Tolerances are sums of the roundings each quantity goes through (u = 2^-24)."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -576,3 +577,35 @@ def test_gradient_table_in_page_locked_memory():
     L.g = fresh
     L.before["g"] = [g.double().cpu().numpy() for g in fresh]
     check_step(L, expected(L, 6, 1e-2, 0.1))
+
+
+def test_no_upload_while_a_blocking_stream_is_captured():
+    """A list on the legacy default stream while another, blocking stream is being captured: refused, and the capture goes on."""
+    L = Lists([300])
+    lst = B.TensorList(L.p, L.g, L.m, L.v, workspace=L.workspace)           # stream 0
+    torch.cuda.synchronize()
+    raw = C.c_void_p()
+    assert int(torch.cuda.cudart().cudaStreamCreate(C.addressof(raw))) == 0
+    blocking = torch.cuda.ExternalStream(raw.value)
+    x, other = torch.zeros(8, device=DEV), torch.empty_like(L.workspace)
+    spare = [torch.zeros_like(t) for t in L.p]
+    status = []
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=blocking):
+        x.add_(1.0)
+        for call in (lambda: lst.qsr_list_set_grads(L.g), lambda: B.TensorList(spare, None, L.m, L.v, workspace=other)):
+            try:
+                call()
+                status.append(0)
+            except B.QsrError as e:
+                status.append(e.status)
+        x.add_(1.0)
+    x.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert status == [B.QSR_ESTATE, B.QSR_ESTATE] and bool((x == 2.0).all())
+    lst.qsr_list_step(6, 1e-2)
+    torch.cuda.synchronize()
+    check_step(L, expected(L, 6, 1e-2, 0.0))
