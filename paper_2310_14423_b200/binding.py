@@ -4,7 +4,7 @@ Every step of the path runs in the library's CUDA kernels.  There is no CPU fall
 the library has not been built (`python -m paper_2310_14423_b200.build`), and calls that need a device return
 the library's error codes, raised here as QsrError.
 
-torch is used by callers for device memory and streams; this module only needs `tensor.data_ptr()`.
+torch is used by callers for device memory and streams; this module asks tensors for their address, layout and device.
 """
 from __future__ import annotations
 
@@ -216,6 +216,14 @@ class _Names(dict):
 _NAMES = _Names()
 
 
+def _current_device() -> int:
+    """Index of the device that the library's launches go to (torch is initialised: callers hold a CUDA tensor)."""
+    global _current_device
+    from torch._C import _cuda_getDevice
+    _current_device = _cuda_getDevice          # from now on without the way round through Python
+    return _current_device()
+
+
 def _dptr(t) -> Optional[int]:
     """Device address of a torch tensor (or None)."""
     if t is None:
@@ -399,11 +407,17 @@ class TensorList:
         if codes and (m_scale is None or v_scale is None):
             raise ValueError("states in 8 bits need m_scale and v_scale")
         state_types = {"torch.float8_e4m3fn": 0} if codes else {"torch.float32": 0}
+        device = params[0].get_device() if n else -1
+        for what, t in [("workspace", workspace), ("grad_norm", grad_norm)]:
+            if t is not None and n and t.get_device() != device:
+                raise ValueError(f"{what}: expected a CUDA tensor on cuda:{device}")
         entries = (QsrTensor * max(1, n))()
         for i, p in enumerate(params):
             e = entries[i]
             e.numel, e.param_type, e.wd_scale = p.numel(), DTYPE.get(str(p.dtype), QSR_NONE), 1.0 if wd_scale is None else wd_scale[i]
             e.param = _element(p, p, f"params[{i}]")
+            if p.get_device() != device:
+                raise ValueError(f"params[{i}]: expected a CUDA tensor on cuda:{device}")
             e.m, e.v = _element(m[i], p, f"m[{i}]", state_types), _element(v[i], p, f"v[{i}]", state_types)
             e.copy_type = QSR_NONE
             if copies is not None and copies[i] is not None:
@@ -415,11 +429,13 @@ class TensorList:
                 e.grad_type = e.param_type
             if codes:
                 for name, scales in (("m_scale", m_scale), ("v_scale", v_scale)):
-                    if str(scales[i].dtype) != "torch.float32" or scales[i].numel() != (p.numel() + 255) // 256:
-                        raise ValueError(f"{name}[{i}]: one float32 per 256 elements is expected")
+                    if str(scales[i].dtype) != "torch.float32" or scales[i].numel() != (p.numel() + 255) // 256 or scales[i].get_device() != device:
+                        raise ValueError(f"{name}[{i}]: one float32 per 256 elements is expected, on cuda:{device}")
                     setattr(e, name, _dptr(scales[i]) if p.numel() else None)
         if grad_norm is not None and (str(grad_norm.dtype) != "torch.float32" or grad_norm.numel() != workers):
             raise ValueError("grad_norm: one float32 per worker is expected")
+        if n and device != _current_device():
+            raise ValueError(f"the tensors are on cuda:{device}, which is not the current device")
         cfg = QsrListConfig(n_tensors=n, workers=int(workers), states=STATES["e4m3" if codes else "f32"], beta1=beta1, beta2=beta2,
                             eps=eps, weight_decay=weight_decay, clip_norm=clip_norm, grad_norm=_dptr(grad_norm))
         nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
@@ -463,19 +479,19 @@ class TensorList:
 
 # ---- log probabilities of given tokens ------------------------------------------------------------------
 
-def _vector(t, what: str, n: int, dtype: str) -> Optional[int]:
-    """Device address of a contiguous CUDA tensor of n elements of `dtype`; None for None."""
+def _vector(t, what: str, n: int, dtype: str, device: int) -> Optional[int]:
+    """Device address of a contiguous tensor of n elements of `dtype` on the CUDA device of that index; None for None."""
     if t is None:
         return None
-    if _NAMES[t.dtype] != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {n} x {dtype} is expected")
+    if _NAMES[t.dtype] != dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous tensor of {n} x {dtype} on cuda:{device} is expected")
     return t.data_ptr()
 
 
-def _matrix(t, shape, what: str):
-    """Row stride of a CUDA matrix with adjacent columns (that of a single row means nothing)."""
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{what}: a CUDA matrix is expected")
+def _matrix(t, shape, what: str, device: int):
+    """Row stride of a matrix with adjacent columns (that of a single row means nothing) on the CUDA device of that index."""
+    if len(shape) != 2 or device < 0 or t.get_device() != device:
+        raise ValueError(f"{what}: a CUDA matrix is expected, all tensors on the same device")
     if t.is_contiguous():
         return shape[1]
     stride = t.stride()
@@ -484,38 +500,40 @@ def _matrix(t, shape, what: str):
     return max(stride[0], shape[1]) if shape[0] <= 1 else stride[0]
 
 
-def _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits) -> QsrLogprobArgs:
-    shape = logits.shape
-    stride, kind = _matrix(logits, shape, "logits"), DTYPE.get(_NAMES[logits.dtype])
+def _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits) -> Tuple[QsrLogprobArgs, int, int]:
+    """Arguments that both calls share, with the number of rows and the index of the device."""
+    shape, device = logits.shape, logits.get_device()
+    stride, kind = _matrix(logits, shape, "logits", device), DTYPE.get(_NAMES[logits.dtype])
     if kind is None:
         raise ValueError(f"logits: {logits.dtype} is not supported (one of {', '.join(sorted(DTYPE))})")
     R, V = shape
     f32 = "torch.float32"
-    a = QsrLogprobArgs(logits.data_ptr(), _vector(tokens, "tokens", R, "torch.int64"), R, V, stride, kind, 0, inv_temperature, None,
-                       _vector(entropy, "entropy", R, f32), _vector(row_stats, "row_stats", 2 * R, f32), None, None,
-                       _vector(d_logprob, "d_logprob", R, f32), _vector(d_entropy, "d_entropy", R, f32))
+    if device != _current_device():
+        raise ValueError(f"the logits are on cuda:{device}, which is not the current device")
+    a = QsrLogprobArgs(logits.data_ptr(), _vector(tokens, "tokens", R, "torch.int64", device), R, V, stride, kind, 0, inv_temperature, None,
+                       _vector(entropy, "entropy", R, f32, device), _vector(row_stats, "row_stats", 2 * R, f32, device), None, None,
+                       _vector(d_logprob, "d_logprob", R, f32, device), _vector(d_entropy, "d_entropy", R, f32, device))
     if d_logits is not None:
         if d_logits.shape != shape or d_logits.dtype != logits.dtype:
             raise ValueError("d_logits: shape and type of the logits are expected")
-        a.d_logits, a.d_row_stride = d_logits.data_ptr(), _matrix(d_logits, shape, "d_logits")
-    return a
+        a.d_logits, a.d_row_stride = d_logits.data_ptr(), _matrix(d_logits, shape, "d_logits", device)
+    return a, R, device
 
 
 def qsr_token_logprobs(logits, tokens, logprob, entropy=None, row_stats=None, top_logprob=None, top_token=None,
                        inv_temperature: float = 1.0, d_logprob=None, d_entropy=None, d_logits=None, stream: int = 0) -> None:
     """Log probability of each row's token, with optional entropy, row statistics, top alternatives ([rows, n] tensors, n at
     most QSR_MAX_TOP) and, if d_logits is given, the gradient in the same pass.  All tensors are the caller's."""
-    a = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
-    R = a.rows
-    a.logprob = _vector(logprob, "logprob", R, "torch.float32")
+    a, R, device = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
+    a.logprob = _vector(logprob, "logprob", R, "torch.float32", device)
     if (top_logprob is None) != (top_token is None):
         raise ValueError("top_logprob and top_token come together")
     if top_token is not None:
         if top_token.dim() != 2:
             raise ValueError("top_token: [rows, n] is expected")
         a.n_top = n = top_token.shape[1]
-        a.top_logprob = _vector(top_logprob, "top_logprob", R * n, "torch.float32")
-        a.top_token = _vector(top_token, "top_token", R * n, "torch.int64")
+        a.top_logprob = _vector(top_logprob, "top_logprob", R * n, "torch.float32", device)
+        a.top_token = _vector(top_token, "top_token", R * n, "torch.int64", device)
     _check(lib().qsr_token_logprobs(C.byref(a), stream), "qsr_token_logprobs")
 
 
@@ -523,7 +541,7 @@ def qsr_token_logprobs_grad(logits, tokens, row_stats, d_logits, d_logprob=None,
                             inv_temperature: float = 1.0, stream: int = 0) -> None:
     """Gradient of sum(d_logprob * logprob + d_entropy * entropy) with respect to the logits, from the row_stats (and entropy)
     that qsr_token_logprobs wrote for the same logits and temperature."""
-    a = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
+    a, _, _ = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
     _check(lib().qsr_token_logprobs_grad(C.byref(a), stream), "qsr_token_logprobs_grad")
 
 

@@ -3,6 +3,7 @@ import ctypes as C
 import math
 
 import pytest
+import torch
 
 from paper_2310_14423_b200 import binding as B
 
@@ -120,3 +121,79 @@ def test_logprob_calls_refuse():
     assert grad(d_logits=None) == B.QSR_EINVAL
     assert grad(row_stats=None) == B.QSR_EINVAL
     assert grad(d_entropy=1 << 25) == B.QSR_EINVAL
+
+
+class Placed:
+    """What the binding asks of a tensor, for one that lies on a device of this index at an address that nothing reads."""
+
+    def __init__(self, *shape, dtype=torch.float32, device=0):
+        self.shape, self.dtype, self.index, self.device = torch.Size(shape), dtype, device, torch.device("cuda", device)
+        self.is_cuda = True
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return self.index
+
+    def is_contiguous(self):
+        return True
+
+    def element_size(self):
+        return torch.empty(0, dtype=self.dtype).element_size()
+
+    def data_ptr(self):
+        return 1 << 30
+
+
+class Reached(Exception):
+    pass
+
+
+@pytest.fixture
+def no_library(monkeypatch):
+    """Every argument has passed when the library is asked for."""
+    def reached():
+        raise Reached
+    monkeypatch.setattr(B, "lib", reached)
+    monkeypatch.setattr(B, "_current_device", lambda: 0, raising=False)
+
+
+def test_lists_want_all_tensors_on_the_current_device(no_library):
+    def make(states, **other):
+        """A list of two tensors, some of its operands on device 1."""
+        t = lambda n, name, dtype=torch.float32: Placed(n, dtype=dtype, device=other.get(name, 0))        # noqa: E731
+        f8 = torch.float8_e4m3fn if states == "e4m3" else torch.float32
+        scale = lambda name: [t(2, name), t(1, name)] if states == "e4m3" else None                        # noqa: E731
+        B.TensorList([t(300, "first"), t(5, "param")], [t(300, "grad"), t(5, "grad")], [t(300, "m", f8), t(5, "m", f8)],
+                     [t(300, "v", f8), t(5, "v", f8)], m_scale=scale("m_scale"), v_scale=scale("v_scale"),
+                     copies=[t(300, "copy", torch.bfloat16), t(5, "copy", torch.bfloat16)], grad_norm=t(1, "grad_norm"),
+                     workspace=t(4096, "workspace", torch.uint8))
+
+    for states in ("f32", "e4m3"):
+        with pytest.raises(Reached):
+            make(states)
+        for name in ("first", "param", "grad", "m", "v", "copy", "grad_norm", "workspace") + (("m_scale", "v_scale") if states == "e4m3" else ()):
+            with pytest.raises(ValueError):
+                make(states, **{name: 1})
+        with pytest.raises(ValueError):       # all of them on a device that is not the current one
+            make(states, first=1, param=1, grad=1, m=1, v=1, copy=1, grad_norm=1, workspace=1, m_scale=1, v_scale=1)
+
+
+def test_log_probabilities_want_all_tensors_on_the_current_device(no_library):
+    i64 = torch.int64
+    own = dict(logits=Placed(3, 7), tokens=Placed(3, dtype=i64))
+    forward = dict(own, logprob=Placed(3), entropy=Placed(3), row_stats=Placed(3, 2), top_logprob=Placed(3, 2), top_token=Placed(3, 2, dtype=i64),
+                   d_logprob=Placed(3), d_entropy=Placed(3), d_logits=Placed(3, 7))
+    grad = dict(own, row_stats=Placed(3, 2), d_logits=Placed(3, 7), d_logprob=Placed(3), d_entropy=Placed(3), entropy=Placed(3))
+    for call, args in ((B.qsr_token_logprobs, forward), (B.qsr_token_logprobs_grad, grad)):
+        with pytest.raises(Reached):
+            call(**args)
+        for name, t in args.items():
+            with pytest.raises(ValueError):
+                call(**{**args, name: Placed(*t.shape, dtype=t.dtype, device=1)})
+        with pytest.raises(ValueError):
+            call(**{name: Placed(*t.shape, dtype=t.dtype, device=1) for name, t in args.items()})
