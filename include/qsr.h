@@ -425,7 +425,8 @@ typedef struct qsr_logprob_args {
     int64_t *top_token;      /* device [rows, n_top]; output                                                     */
     const float *d_logprob;  /* device [rows] or NULL (no such term)                                             */
     const float *d_entropy;  /* device [rows] or NULL                                                            */
-    void *d_logits;          /* device, logits_type, [rows, d_row_stride]: output; may be the logits themselves  */
+    void *d_logits;          /* device, logits_type, [rows, d_row_stride]: output; the logits themselves, or     */
+                             /* nothing of them (columns of one buffer with the same stride are fine)            */
     int64_t d_row_stride;    /* vocab <= d_row_stride; equal to row_stride if d_logits is logits                 */
 } qsr_logprob_args;
 

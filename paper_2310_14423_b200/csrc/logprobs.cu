@@ -816,6 +816,20 @@ namespace {
 
 bool element_aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// Whether two matrices of rows x vocab elements of e bytes (strides in elements; not the same matrix) share one.  With equal
+// strides, as columns of one buffer have them, rows meet exactly if the distance modulo the stride is less than a row from
+// either side; otherwise matrices that lie in and out of one another count as sharing.
+bool share_bytes(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int64_t rows, int64_t vocab, int e)
+{
+    typedef __int128 wide;                          // strides have no upper limit
+    const wide x = wide(reinterpret_cast<uintptr_t>(a)), y = wide(reinterpret_cast<uintptr_t>(b));
+    const wide row = wide(vocab) * e, xs = wide(a_stride) * e, ys = wide(b_stride) * e;
+    if (x + (rows - 1) * xs + row <= y || y + (rows - 1) * ys + row <= x) return false;
+    if (xs != ys || rows == 1) return true;
+    const wide d = (x > y ? x - y : y - x) % xs;
+    return d < row || d > xs - row;
+}
+
 // Checks what both calls share and fills the kernel's arguments.
 int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &p)
 {
@@ -838,6 +852,9 @@ int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &
         return QSR_EALIGN;
     if (forward && (!element_aligned(a->logprob, 4) || (a->n_top > 0 && (!element_aligned(a->top_logprob, 4) || !element_aligned(a->top_token, 8)))))
         return QSR_EALIGN;
+    if (a->rows > 0 && a->d_logits && a->d_logits != a->logits &&
+        share_bytes(a->logits, a->row_stride, a->d_logits, a->d_row_stride, a->rows, a->vocab, int(e)))
+        return QSR_EINVAL;
     p.logits = a->logits; p.tokens = a->tokens;
     p.logprob = a->logprob; p.entropy = a->entropy; p.stats = a->row_stats;
     p.top_logprob = a->top_logprob; p.top_token = a->top_token;

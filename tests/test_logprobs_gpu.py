@@ -402,3 +402,22 @@ def test_temperatures_far_from_one(V, tau):
         if not fused:
             c.backward(tau)
         c.check(tau, top=3, a=a, b=b, gradient=True)
+
+
+@pytest.mark.parametrize("V,stride,at", [(100, 200, 100), (100, 250, 100), (100, 250, 150), (1001, 2003, 1002)])
+def test_gradient_in_other_columns_of_the_logits_buffer(V, stride, at):
+    x, y, a, b = draw(6, V, "bf16")
+    want = Call(x, y, "bf16")
+    want.forward(1.0, a=a, b=b, fused=True)
+    buffer = torch.full((6, stride), 5.0, device=DEV, dtype=torch.bfloat16)
+    for fused in (True, False):
+        c = Call(x, y, "bf16")
+        buffer[:, :V] = c.x
+        c.x, c.d = buffer[:, :V], buffer[:, at:at + V]
+        c.forward(1.0, a=a, b=b, fused=fused)
+        if not fused:
+            c.backward(1.0)
+        assert torch.equal(c.x, want.x) and torch.allclose(c.d.float(), want.d.float(), rtol=2.0 ** -7, atol=1e-6)
+        used = torch.zeros(stride, dtype=torch.bool, device=DEV)
+        used[:V] = used[at:at + V] = True
+        assert bool((buffer[:, ~used] == 5.0).all())

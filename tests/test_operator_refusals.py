@@ -197,3 +197,17 @@ def test_log_probabilities_want_all_tensors_on_the_current_device(no_library):
                 call(**{**args, name: Placed(*t.shape, dtype=t.dtype, device=1)})
         with pytest.raises(ValueError):
             call(**{name: Placed(*t.shape, dtype=t.dtype, device=1) for name, t in args.items()})
+
+
+def test_gradients_that_overlap_the_logits_without_being_them():
+    """fp32 logits of 4 x 100 at 2^20, rows 100 or 250 apart.  Accepted layouts are tested on the GPU."""
+    at = 1 << 20
+    for kw in (dict(d_logits=at + 4), dict(d_logits=at - 4), dict(d_logits=at + 4 * 399), dict(d_logits=at - 4 * 399),
+               dict(d_logits=at + 4 * 100), dict(d_logits=at, d_row_stride=100, row_stride=100, logits=at + 40),
+               dict(row_stride=250, d_row_stride=250, d_logits=at + 4 * 99), dict(row_stride=250, d_row_stride=250, d_logits=at + 4 * 151),
+               dict(row_stride=250, d_row_stride=250, d_logits=at - 4 * (250 + 99)), dict(row_stride=250, d_row_stride=250, d_logits=at + 4 * (750 + 99)),
+               dict(row_stride=250, d_row_stride=251, d_logits=at + 4 * 100), dict(row_stride=1 << 62, d_row_stride=1 << 62, d_logits=at + 4),
+               dict(rows=1, d_logits=at + 4 * 99), dict(rows=1, row_stride=500, d_row_stride=600, d_logits=at - 4 * 99)):
+        args = {**dict(d_row_stride=100, row_stats=1 << 24), **kw}
+        assert B.lib().qsr_token_logprobs(C.byref(_args(**args)), None) == B.QSR_EINVAL, kw
+        assert B.lib().qsr_token_logprobs_grad(C.byref(_args(**args)), None) == B.QSR_EINVAL, kw
