@@ -417,7 +417,7 @@ typedef struct qsr_logprob_args {
     int64_t rows, vocab, row_stride;   /* 0 <= rows < 2^28, 1 <= vocab < 2^31, vocab <= row_stride (elements)    */
     int32_t logits_type;     /* QSR_F32, QSR_BF16 or QSR_F16                                                     */
     int32_t n_top;           /* 0..QSR_MAX_TOP, at most vocab                                                    */
-    double inv_temperature;  /* > 0, finite                                                                      */
+    double inv_temperature;  /* above 0 in fp32, at most 2e38                                                    */
     float *logprob;          /* device [rows]; output                                                            */
     float *entropy;          /* device [rows] or NULL; output (an input of the _grad call with d_entropy)        */
     float *row_stats;        /* device [rows, 2] or NULL; output (an input of the _grad call), 8-byte aligned    */

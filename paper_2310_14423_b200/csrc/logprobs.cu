@@ -835,8 +835,8 @@ int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &
 {
     if (!a) return QSR_EINVAL;
     if (a->logits_type != QSR_F32 && a->logits_type != QSR_BF16 && a->logits_type != QSR_F16) return QSR_EINVAL;
-    if (!std::isfinite(a->inv_temperature) || !(float(a->inv_temperature) > 0.0f) || !std::isfinite(float(a->inv_temperature)))
-        return QSR_EINVAL;
+    const float tau = float(a->inv_temperature), tau_log2e = float(a->inv_temperature * 1.4426950408889634);
+    if (!(tau > 0.0f) || !std::isfinite(tau_log2e)) return QSR_EINVAL;
     if (a->rows < 0 || a->rows >= (int64_t(1) << 28) || a->vocab < 1 || a->vocab > 0x7fffffff || a->row_stride < a->vocab) return QSR_ERANGE;
     if (forward && (a->n_top < 0 || a->n_top > QSR_MAX_TOP || a->n_top > a->vocab)) return QSR_ERANGE;
     if (a->d_logits && (a->d_row_stride < a->vocab || (a->d_logits == a->logits && a->d_row_stride != a->row_stride))) return QSR_ERANGE;
@@ -861,8 +861,8 @@ int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &
     p.d_logprob = a->d_logprob; p.d_entropy = a->d_entropy; p.d_logits = a->d_logits;
     p.rows = a->rows; p.vocab = a->vocab; p.stride = a->row_stride; p.d_stride = a->d_row_stride;
     p.type = a->logits_type; p.n_top = a->n_top;
-    p.tau = float(a->inv_temperature);
-    p.tau_log2e = float(a->inv_temperature * 1.4426950408889634);
+    p.tau = tau;
+    p.tau_log2e = tau_log2e;
     return QSR_OK;
 }
 

@@ -211,3 +211,11 @@ def test_gradients_that_overlap_the_logits_without_being_them():
         args = {**dict(d_row_stride=100, row_stats=1 << 24), **kw}
         assert B.lib().qsr_token_logprobs(C.byref(_args(**args)), None) == B.QSR_EINVAL, kw
         assert B.lib().qsr_token_logprobs_grad(C.byref(_args(**args)), None) == B.QSR_EINVAL, kw
+
+
+def test_temperatures_whose_base_two_factor_overflows():
+    """exp(tau z) is 2^(c z) with c = tau log2(e), which has to be finite in fp32."""
+    for tau in (2.5e38, 3.4e38):
+        assert B.lib().qsr_token_logprobs(C.byref(_args(inv_temperature=tau)), None) == B.QSR_EINVAL
+        assert B.lib().qsr_token_logprobs(C.byref(_args(inv_temperature=tau, rows=0)), None) == B.QSR_EINVAL
+    assert B.lib().qsr_token_logprobs(C.byref(_args(inv_temperature=2e38, rows=0)), None) == B.QSR_OK
