@@ -374,8 +374,9 @@ int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor
 int qsr_list_destroy(qsr_list *list);
 
 /* New gradient addresses (host array of n_tensors device pointers, read during the call), same types: for training loops
- * whose gradients are allocated anew every step.  They must not overlap what the list writes.  One small copy on the stream;
- * asynchronous.  QSR_ESTATE: the stream is being captured (as at qsr_list_create), or another device than the list's is
+ * whose gradients are allocated anew every step.  They must not overlap what the list writes.  The table goes to the device by one
+ * copy on the stream, which is staged during the call (for tables above 64 KB the host may wait for the stream).  The
+ * gradients before have to stay until the steps enqueued so far have read them.  QSR_ESTATE: the stream is being captured (as at qsr_list_create), or another device than the list's is
  * current. */
 int qsr_list_set_grads(qsr_list *list, const void *const *grads_host);
 

@@ -359,19 +359,20 @@ def _dense(t) -> bool:
     return True
 
 
-def _element(t, like, what: str, dtypes=DTYPE):
-    """Device address of one operand of a list entry: a dense CUDA tensor with as many elements as the parameter, in the
+def _element(t, like, what: str, i: int, dtypes=DTYPE):
+    """Device address of operand `what` of list entry i: a dense CUDA tensor with as many elements as the parameter, in the
     same order in memory."""
-    name = str(t.dtype)
+    name, device = _NAMES[t.dtype], like.get_device()
     if name not in dtypes:
-        raise ValueError(f"{what}: {name} is not supported (one of {', '.join(sorted(dtypes))})")
-    if not t.is_cuda or t.device != like.device:
-        raise ValueError(f"{what}: expected a CUDA tensor on {like.device}")
-    if t.numel() != like.numel():
-        raise ValueError(f"{what}: {t.numel()} elements for a parameter of {like.numel()}")
+        raise ValueError(f"{what}[{i}]: {name} is not supported (one of {', '.join(sorted(dtypes))})")
+    if device < 0 or t.get_device() != device:
+        raise ValueError(f"{what}[{i}]: expected a CUDA tensor on {like.device}")
+    numel = t.numel()
+    if numel != like.numel():
+        raise ValueError(f"{what}[{i}]: {numel} elements for a parameter of {like.numel()}")
     if not (t.is_contiguous() and like.is_contiguous()) and not (t.shape == like.shape and t.stride() == like.stride() and _dense(t)):
-        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} does not lie in memory like its parameter")
-    return int(t.data_ptr()) if t.numel() else None
+        raise ValueError(f"{what}[{i}]: shape {tuple(t.shape)} with strides {t.stride()} does not lie in memory like its parameter")
+    return t.data_ptr() if numel else None
 
 
 def qsr_list_workspace_bytes(numels, workers: int = 1) -> int:
@@ -390,7 +391,11 @@ class TensorList:
     places); with several workers, worker 0's tensors first, then worker 1's, and so on.  m, v: float32 tensors, or
     float8_e4m3fn with m_scale / v_scale (float32, one per 256 elements, in memory order).  wd_scale: a factor on the
     weight decay per tensor (default 1).  workspace: a CUDA tensor of qsr_list_workspace_bytes bytes.  Keeps references
-    to the tensors whose memory the library borrows."""
+    to the tensors whose memory the library borrows.
+
+    Work goes to `stream`, and the caller orders it after what fills the tensors.  Gradients that qsr_list_set_grads replaces are
+    marked as in use there (Tensor.record_stream), so that their memory is not given out again while an enqueued step reads
+    it.  All other tensors, and the last gradients, are let go with the list: with `stream` idle, or recorded by the caller."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None, wd_scale=None, workers: int = 1,
                  beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
@@ -415,16 +420,16 @@ class TensorList:
         for i, p in enumerate(params):
             e = entries[i]
             e.numel, e.param_type, e.wd_scale = p.numel(), DTYPE.get(str(p.dtype), QSR_NONE), 1.0 if wd_scale is None else wd_scale[i]
-            e.param = _element(p, p, f"params[{i}]")
+            e.param = _element(p, p, "params", i)
             if p.get_device() != device:
                 raise ValueError(f"params[{i}]: expected a CUDA tensor on cuda:{device}")
-            e.m, e.v = _element(m[i], p, f"m[{i}]", state_types), _element(v[i], p, f"v[{i}]", state_types)
+            e.m, e.v = _element(m[i], p, "m", i, state_types), _element(v[i], p, "v", i, state_types)
             e.copy_type = QSR_NONE
             if copies is not None and copies[i] is not None:
-                e.copy, e.copy_type = _element(copies[i], p, f"copies[{i}]"), DTYPE[str(copies[i].dtype)]
+                e.copy, e.copy_type = _element(copies[i], p, "copies", i), DTYPE[str(copies[i].dtype)]
             g = None if grads is None else grads[i]
             if g is not None:
-                e.grad, e.grad_type = _element(g, p, f"grads[{i}]"), DTYPE[str(g.dtype)]
+                e.grad, e.grad_type = _element(g, p, "grads", i), DTYPE[str(g.dtype)]
             else:
                 e.grad_type = e.param_type
             if codes:
@@ -440,8 +445,8 @@ class TensorList:
                             eps=eps, weight_decay=weight_decay, clip_norm=clip_norm, grad_norm=_dptr(grad_norm))
         nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
         self._params, self._grad_types = list(params), [entries[i].grad_type for i in range(n)]
-        self._keep = (list(m), list(v), m_scale, v_scale, copies, grad_norm, workspace)
-        self._grads = grads
+        self._keep = [None if x is None else list(x) for x in (m, v, m_scale, v_scale, copies)] + [grad_norm, workspace]
+        self._grads, self._stream = None if grads is None else list(grads), int(stream)
         _check(lib().qsr_list_create(C.byref(self._h), C.byref(cfg), entries, _dptr(workspace), nbytes, C.c_void_p(stream)),
                "qsr_list_create")
 
@@ -460,11 +465,18 @@ class TensorList:
         """New gradient tensors (one per parameter, of the types the list was made with)."""
         if len(grads) != len(self._params):
             raise ValueError(f"{len(grads)} gradients for {len(self._params)} parameters")
-        names = {v: k for k, v in DTYPE.items()}
+        only = {v: {k: 0} for k, v in DTYPE.items()}
         table = (C.c_void_p * max(1, len(grads)))()
         for i, (g, p) in enumerate(zip(grads, self._params)):
-            table[i] = _element(g, p, f"grads[{i}]", {names[self._grad_types[i]]: 0})
+            table[i] = _element(g, p, "grads", i, only[self._grad_types[i]])
         _check(lib().qsr_list_set_grads(self._h, table), "qsr_list_set_grads")
+        if self._grads is not None:
+            import torch
+            device = self._params[0].device
+            stream = torch.cuda.ExternalStream(self._stream, device) if self._stream else torch.cuda.default_stream(device)
+            for g in self._grads:
+                if g is not None:
+                    g.record_stream(stream)
         self._grads = list(grads)
 
     def qsr_list_step(self, n: int, lr: float, grad_scale: float = 1.0) -> None:

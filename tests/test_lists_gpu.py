@@ -609,3 +609,31 @@ def test_no_upload_while_a_blocking_stream_is_captured():
     lst.qsr_list_step(6, 1e-2)
     torch.cuda.synchronize()
     check_step(L, expected(L, 6, 1e-2, 0.0))
+
+
+@pytest.mark.parametrize("again", [False, True])
+def test_replaced_gradients_stay_until_the_list_has_read_them(again):
+    """Gradients of another stream than the list's, dropped by everybody when they are replaced: their memory is not given out
+    again while the list's stream has yet to read them."""
+    L = Lists([100, 5000], weight_decay=0.1)
+    side = torch.cuda.Stream()
+    lst = B.TensorList(L.p, L.g, L.m, L.v, wd_scale=L.wd, workspace=L.workspace, stream=side.cuda_stream, weight_decay=0.1)
+    values = [torch.randn(n, device=DEV) for n in L.sizes]
+    torch.cuda.synchronize()
+    if again:                                              # gradients that the list was given by the call, not when it was made
+        lst.qsr_list_set_grads([x.clone() for x in values])
+    else:
+        grads = [x.clone() for x in values]
+        lst = B.TensorList(L.p, grads, L.m, L.v, wd_scale=L.wd, workspace=L.workspace, stream=side.cuda_stream, weight_decay=0.1)
+        grads.clear()                                      # the list keeps the tensors, not the caller's container
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                     # about 50 ms
+    lst.qsr_list_step(6, 1e-2)
+    # memory of the current stream
+    lst.qsr_list_set_grads([torch.zeros(n, device=DEV) for n in L.sizes])
+    taken = [torch.full((n,), math.nan, device=DEV) for n in L.sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    L.before["g"] = [x.double().cpu().numpy() for x in values]
+    check_step(L, expected(L, 6, 1e-2, 0.1))
+    assert all(bool(x.isnan().all()) for x in taken)
