@@ -637,3 +637,92 @@ def test_replaced_gradients_stay_until_the_list_has_read_them(again):
     L.before["g"] = [x.double().cpu().numpy() for x in values]
     check_step(L, expected(L, 6, 1e-2, 0.1))
     assert all(bool(x.isnan().all()) for x in taken)
+
+
+LARGE = [1_900_003, 8191, 8192, 8193, 600_000, 33, 0, 24_577]      # beyond 2,424,832 elements a warp has several blocks
+
+
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("lead,types", [(64, TYPES[1]), (1, TYPES[3]), (3, TYPES[0]), (8, TYPES[4])])
+def test_step_of_a_large_list(lead, types, states):
+    param, grad, copy = types
+    L = Lists(LARGE, param=param, grad=grad, copy=copy, states=states, lead=lead, weight_decay=0.1, seed=20 + lead)
+    L.list.qsr_list_step(6, 1e-2)
+    check_step(L, expected(L, 6, 1e-2, 0.1))
+
+
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("lead", [64, 5])
+def test_clipping_of_a_large_list(lead, states):
+    norms = torch.zeros(2, device=DEV)
+    L = Lists([1_300_001, 8192, 24_577, 7], K=2, grad="bf16", copy="bf16", states=states, lead=lead, clip_norm=0.5, grad_norm=norms, weight_decay=0.05,
+              seed=30)
+    L.list.qsr_list_step(4, 1e-3)
+    check_step(L, expected(L, 4, 1e-3, 0.05, clip=0.5))
+    want = [math.sqrt(sum(float((g * g).sum()) for g in L.before["g"][4 * k:4 * k + 4])) for k in range(2)]
+    assert np.allclose(norms.cpu().numpy(), want, rtol=64 * U, atol=0)
+
+
+@pytest.mark.parametrize("mode", ["keep", "average", "reset"])
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("lead,types", [(64, TYPES[1]), (1, TYPES[3])])
+def test_sync_of_a_large_list_equals_a_list_per_tensor(lead, types, states, mode):
+    """The same bits, whatever the chunks: workers are added in ascending order.  Lists of one tensor here are small ones."""
+    param, grad, copy = types
+    sizes, K = [750_001, 8193, 100_000, 33], 3
+    one, many = (Lists(sizes, K=K, param=param, grad=grad, copy=copy, states=states, lead=lead, seed=40) for _ in range(2))
+    one.list.qsr_list_sync(mode)
+    for j in range(len(sizes)):
+        pick = lambda xs: None if xs is None else xs[j::len(sizes)]      # noqa: E731
+        ws = torch.empty(B.qsr_list_workspace_bytes([sizes[j]] * K, K), dtype=torch.uint8, device=DEV)
+        lst = B.TensorList(pick(many.p), None, pick(many.m), pick(many.v), m_scale=pick(many.ms), v_scale=pick(many.vs), copies=pick(many.c), workers=K,
+                           workspace=ws, stream=_stream())
+        lst.qsr_list_sync(mode)
+    a, b = one.numpy(), many.numpy()
+    for name in ("p", "c", "m", "v", "ms", "vs"):
+        assert a[name] is None or all(np.array_equal(x, y) for x, y in zip(a[name], b[name])), name
+    mean = np.mean([one.before["p"][k * len(sizes)] for k in range(K)], 0)
+    e = (K + 1) * U * np.abs(mean).max() * 4
+    assert np.all(np.abs(a["p"][0] - mean) <= e + HALF_ULP[param] * (np.abs(mean) + e) + TINY[param])
+    one.assert_guards()
+    many.assert_guards()
+
+
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("lead", [64, 3])
+def test_several_types_in_one_list(lead, states):
+    """fp32 vectors beside bf16 and fp16 matrices, with gradients and copies of their own types, in one step and one mean."""
+    K = 2
+    groups = [Lists(sizes, K=K, param=t[0], grad=t[1], copy=t[2], states=states, lead=lead, seed=50 + i)
+              for i, (sizes, t) in enumerate((([7, 300, 2049], TYPES[0]), ([4100, 33], TYPES[3]), ([8200, 1], TYPES[1]), ([513], TYPES[4]), ([777], TYPES[5])))]
+
+    def merged(name):
+        """Worker 0's tensors of all groups, then worker 1's."""
+        out = []
+        for k in range(K):
+            for L in groups:
+                n, xs = len(L.sizes), getattr(L, name)
+                out += [None] * n if xs is None else xs[k * n:(k + 1) * n]
+        return out
+
+    codes = states == "e4m3"
+    every = [x.numel() for x in merged("p")]
+    ws = torch.empty(B.qsr_list_workspace_bytes(every, K), dtype=torch.uint8, device=DEV)
+    lst = B.TensorList(merged("p"), merged("g"), merged("m"), merged("v"), m_scale=merged("ms") if codes else None,
+                       v_scale=merged("vs") if codes else None, copies=merged("c"), wd_scale=merged("wd"), workers=K, workspace=ws, stream=_stream(),
+                       weight_decay=0.1)
+    lst.qsr_list_step(6, 1e-2)
+    for L in groups:
+        check_step(L, expected(L, 6, 1e-2, 0.1))
+    before = [L.numpy() for L in groups]
+    lst.qsr_list_sync("average")
+    for L, b in zip(groups, before):
+        got, n = L.numpy(), len(L.sizes)
+        for j in range(n):
+            th = np.stack([b["p"][k * n + j] for k in range(K)])
+            e = (K + 1) * U * np.abs(th).mean(0)
+            param = L.types[0]
+            for k in range(K):
+                assert np.all(np.abs(got["p"][k * n + j] - th.mean(0)) <= e + HALF_ULP[param] * (np.abs(th.mean(0)) + e) + TINY[param])
+                assert all(got[x] is None or np.array_equal(got[x][k * n + j], got[x][j]) for x in ("p", "c", "m", "v", "ms", "vs"))
+        L.assert_guards()
