@@ -317,10 +317,10 @@ int qsr_train_host(const qsr_config *cfg, const float *theta0_host, const float 
  * can span a factor of 2^35 in v), scale = fl(amax * fl(1/448)) with amax the block's largest finite magnitude; codes are
  * fl(x * fl(1/scale)) rounded to nearest even, saturating at 448.  A positive sqrt(v) never becomes 0 (its smallest code is
  * 2^-9), because a vanished denominator would turn a small m into a huge step.  A block whose amax is below 2^-100 is
- * stored as zeros.  An infinite m or sqrt(v) (a finite gradient whose square overflows has the latter) is stored as the saturated
- * code, in a block of scale 0 as 0.  The scale is a full fp32 number, not a power of two, so that the largest element of a block decays as it
- * would in fp32 and takes the others along; three mantissa bits alone would hold 0.999*v at v.  The update itself uses the new
- * m and v before they are rounded to 8 bits.  A NaN in one element stays in that element.
+ * stored as zeros.  An infinite m or sqrt(v) (a finite gradient whose square overflows has the latter) is stored as the
+ * saturated code, in a block of scale 0 as 0.  The scale is a full fp32 number, not a power of two, so that the largest
+ * element of a block decays as it would in fp32 and takes the others along; three mantissa bits alone would hold 0.999*v at
+ * v.  The update itself uses the new m and v before they are rounded to 8 bits.  A NaN in one element stays in that element.
  *
  * Tensors are worker-major: entry k*(n_tensors/workers) + j is tensor j of worker k, and the same j has the same numel,
  * param_type and copy_type for every worker.  Any element alignment works; the fast path needs each tensor of an entry
@@ -366,7 +366,8 @@ int64_t qsr_list_workspace_bytes(const int64_t *numel_host, int32_t n_tensors, i
  * QSR_EINVAL: NULL, unknown type, numbers that are not finite, betas outside [0, 1), sizes or types that differ between
  * workers, or a written range that overlaps any other range of the list (tied weights: list them once); QSR_EALIGN: a pointer
  * not aligned to its element; QSR_ERANGE: workspace too small; QSR_ESTATE: the stream is being captured (the tables' copies
- * would be replayed from memory that is gone), or it is the legacy default stream while a blocking stream is.  No tensor is written. */
+ * would be replayed from memory that is gone), or it is the legacy default stream while a blocking stream is.  No tensor is
+ * written. */
 int qsr_list_create(qsr_list **out, const qsr_list_config *cfg, const qsr_tensor *tensors_host, void *workspace_dev,
                     int64_t workspace_bytes, void *cuda_stream);
 
@@ -376,14 +377,15 @@ int qsr_list_destroy(qsr_list *list);
 /* New gradient addresses (host array of n_tensors device pointers, read during the call), same types: for training loops
  * whose gradients are allocated anew every step.  They must not overlap what the list writes.  The table goes to the device by one
  * copy on the stream, which is staged during the call (for tables above 64 KB the host may wait for the stream).  The
- * gradients before have to stay until the steps enqueued so far have read them.  QSR_ESTATE: the stream is being captured (as at qsr_list_create), or another device than the list's is
- * current. */
+ * gradients before have to stay until the steps enqueued so far have read them.  QSR_ESTATE: the stream is being captured
+ * (as at qsr_list_create), or another device than the list's is current. */
 int qsr_list_set_grads(qsr_list *list, const void *const *grads_host);
 
 /* One AdamW step of every tensor, formula above; n >= 1 counts the steps the states have seen (t + 1 - t_state_origin),
  * lr is the learning rate of this step (qsr_config_learning_rate gives the schedules').  grad_scale multiplies every
  * gradient first (1 / loss scale, or 1 / accumulated batches).  QSR_ESTATE: no gradients set, or another device than the
- * list's is current.  Asynchronous. */
+ * list's is current.  Asynchronous.  n, lr and grad_scale are arguments of the launch: a step that was captured in a CUDA graph
+ * repeats them, bias corrections included, at every replay, so a training loop does not advance by replaying one. */
 int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale);
 
 /* End of a round (All-Reduce line of Algorithm 2) over the list's K workers: every parameter becomes
@@ -407,10 +409,11 @@ int64_t qsr_list_launch_count(const qsr_list *list);
  *   probabilities (no gradient flows through these).
  * Gradient of  sum_r d_logprob[r]*logprob[r] + d_entropy[r]*H[r]  with respect to the logits:
  *   d_logits[j] = tau * ( d_logprob*([j = y] - p_j) - d_entropy*p_j*(ln p_j + H) ),  rounded once to the logits' type.
- * Logits of -inf are masked tokens: p = 0 and no gradient.  A row with nothing but -inf: logprob -inf, H = 0, top_logprob
- * -inf (tokens 0, 1, ...), gradient 0.  A token < 0 marks a row without a score: logprob 0 and no d_logprob term.  A token
- * >= vocab, a NaN or a +inf in the row: NaN.  Sums are kept in fp32 and tau*(x - M) is as accurate for large logits as for
- * small ones, so rows masked with -1e10, say, or with the type's lowest value are treated like any other.
+ * Logits of -inf are masked tokens: p = 0 and no gradient, but for the scored token's own term tau*d_logprob.  A row with
+ * nothing but -inf: logprob -inf, H = 0, top_logprob -inf (tokens 0, 1, ...), gradient 0.  A token < 0 marks a row without a
+ * score: logprob 0 and no d_logprob term.  A token >= vocab, a NaN or a +inf in the row: NaN.  Sums are kept in fp32 and
+ * tau*(x - M) is as accurate for large logits as for small ones, so rows masked with -1e10, say, or with the type's lowest
+ * value are treated like any other.
  */
 typedef struct qsr_logprob_args {
     const void *logits;      /* device, logits_type, [rows, row_stride], any element alignment                  */

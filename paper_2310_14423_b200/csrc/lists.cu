@@ -786,7 +786,8 @@ __device__ __forceinline__ void sync_states(const ListSyncParams &p, const ListC
 // written once, and what counts is that all workers' loads of a block are on their way together, in pieces of 512 bytes per
 // worker (8-bit states in pieces of 256 bytes: 2.20 instead of 1.70 ms).  Eight ViT-B/16 replicas with copies: parameters alone
 // 1.13 ms (6.1 TB/s), with 8-bit states averaged 1.70 ms (5.7 TB/s).  The number of blocks per multiprocessor: fp32 states five
-// (three packed bf16 replicas, element by element: 76 us; with four 84), 8-bit states three (1.70 ms; four 1.73, with spills).
+// (three packed bf16 replicas, element by element: 76 us with 48 bytes of spills; with four blocks 84 and none), 8-bit states
+// three (1.70 ms with 28 bytes of spills; with four 1.73 and 360 bytes).
 template <bool S8>
 __global__ void __launch_bounds__(kThreads, S8 ? 3 : 5) list_sync_kernel(const __grid_constant__ ListSyncParams p)
 {

@@ -703,7 +703,9 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 6 : 1) logprob_grad_kernel(con
     }
 }
 
-constexpr int64_t kSliceBytes = 110 * 1024;   // two blocks of such a slice share a multiprocessor
+// Two blocks of such a slice share a multiprocessor.  With alternatives, for which a block has 11 KB of its own, they do up to 102
+// KB; slices between the two bounds run one block at a time there.
+constexpr int64_t kSliceBytes = 110 * 1024;
 constexpr int64_t kStashMax = 200 * 1024;
 constexpr int kMultiprocessors = 148;
 
