@@ -446,6 +446,83 @@ int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream);
  * ignored.  One launch; asynchronous. */
 int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream);
 
+/* ---- layer norm ------------------------------------------------------------------------------------------ */
+
+/*
+ * The normalisation between a model's products.  For each row x[0..width), everything in fp32:
+ *   mean = sum x / width;  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps);  hat = (x - mean)*rstd;  y = hat*weight + bias,
+ * y rounded once to the rows' type.  Backwards, with g = d_y*weight:
+ *   d_x = rstd*(g - (sum g)/width - hat*(sum g*hat)/width);  d_weight = sum over rows of d_y*hat;  d_bias = sum over rows of d_y.
+ * Sums over rows are added in a fixed order, so that results repeat bit for bit.  Infinities and NaN stay in their row, and
+ * in the columns' sums.
+ */
+typedef struct qsr_layer_norm_args {
+    const void *x;           /* device, type, [rows, x_stride], any element alignment                            */
+    const void *weight;      /* device, weight_type, [width], or NULL (ones)                                     */
+    const void *bias;        /* device, weight_type, [width], or NULL (zeros)                                    */
+    float *mean, *rstd;      /* device [rows]: outputs of the forward call (NULL: not wanted), inputs of the other */
+    int64_t rows, width;     /* 0 <= rows < 2^31, 1 <= width <= 2^24                                             */
+    int64_t x_stride;        /* elements, at least width                                                         */
+    int32_t type;            /* of x, y, d_y and d_x: QSR_F32, QSR_BF16 or QSR_F16                               */
+    int32_t weight_type;     /* of weight, bias, d_weight and d_bias                                             */
+    double eps;              /* >= 0; forward call                                                               */
+    void *y;                 /* forward: [rows, y_stride]; x itself, or nothing of it                            */
+    int64_t y_stride;
+    const void *d_y;         /* backward: [rows, d_y_stride]                                                     */
+    int64_t d_y_stride;
+    void *d_x;               /* backward: [rows, d_x_stride] or NULL; x or d_y itself, or nothing of them        */
+    int64_t d_x_stride;
+    void *d_weight, *d_bias; /* backward: [width] or NULL; written, not added to                                 */
+    void *workspace;         /* backward with d_weight or d_bias: device memory, 256-byte aligned, in use until  */
+    int64_t workspace_bytes; /* the call's work is done; qsr_layer_norm_workspace_bytes(rows, width)             */
+} qsr_layer_norm_args;
+
+/* Forward.  No context; one launch on cuda_stream (none for rows = 0) of the current device, where all arrays lie;
+ * asynchronous. */
+int qsr_layer_norm(const qsr_layer_norm_args *args, void *cuda_stream);
+
+/* Bytes of workspace for d_weight and d_bias. */
+int64_t qsr_layer_norm_workspace_bytes(int64_t rows, int64_t width);
+
+/* Backward, from the mean and rstd that the forward call left.  Up to three launches; asynchronous.  With rows = 0 the sums over
+ * rows are zero. */
+int qsr_layer_norm_grad(const qsr_layer_norm_args *args, void *cuda_stream);
+
+/* ---- embedding ------------------------------------------------------------------------------------------- */
+
+/*
+ * A model's input end: out[r] = scale * table[tokens[r]], and the gradient of the table, d_table[v] = scale * (sum of d_out[r] over
+ * the rows r whose token is v).  Products and sums in fp32, one rounding at the end.  The rows of a token are added in an order
+ * that depends on the tokens alone (no floating-point atomics), so that results repeat bit for bit.  A token < 0 marks a row
+ * without one: zeros, no gradient.  A token >= vocab: NaN, no gradient.
+ */
+typedef struct qsr_embed_args {
+    void *table;             /* device, table_type, [vocab, table_stride]: input of qsr_embed; d_table, the output of */
+                             /* qsr_embed_grad                                                                   */
+    const int64_t *tokens;   /* device [rows]                                                                    */
+    void *out;               /* device, out_type, [rows, out_stride]: output of qsr_embed; d_out, the input of   */
+                             /* qsr_embed_grad.  Shares nothing with the table                                   */
+    int64_t rows, vocab, width;        /* 0 <= rows < 2^31, 1 <= vocab < 2^31 - 1, 1 <= width <= 2^20             */
+    int64_t table_stride, out_stride;  /* elements, at least width; any element alignment                        */
+    int32_t table_type, out_type;      /* QSR_F32, QSR_BF16 or QSR_F16                                            */
+    double scale;            /* finite in fp32                                                                   */
+    int32_t accumulate;      /* qsr_embed_grad: 0 writes the whole table's gradient (zeros where a token does not occur), */
+                             /* 1 adds to the rows of tokens that occur and touches no other                     */
+    int32_t reserved;        /* 0                                                                                */
+    void *workspace;         /* qsr_embed_grad: device memory, 256-byte aligned, in use until the call's work is done */
+    int64_t workspace_bytes; /* at least qsr_embed_workspace_bytes(rows, vocab, width)                           */
+} qsr_embed_args;
+
+/* The lookup.  No context; one launch on cuda_stream (none for rows = 0) of the current device, where all arrays lie;
+ * asynchronous. */
+int qsr_embed(const qsr_embed_args *args, void *cuda_stream);
+
+/* Bytes of workspace of the gradient.  Negative qsr_status on error. */
+int64_t qsr_embed_workspace_bytes(int64_t rows, int64_t vocab, int64_t width);
+
+/* The gradient.  Several launches; asynchronous. */
+int qsr_embed_grad(const qsr_embed_args *args, void *cuda_stream);
+
 /* ---- test hook ---------------------------------------------------------------------------------------- */
 
 /* The two halves of the Box-Muller transform that turns generator words into the synthetic gradient's noise (the

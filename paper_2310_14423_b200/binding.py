@@ -33,7 +33,8 @@ EXPORTS = ("qsr_config_check", "qsr_row_stride_hint", "qsr_config_learning_rate"
            "qsr_workspace_bytes", "qsr_init", "qsr_destroy", "qsr_round_length", "qsr_set_tensor_table", "qsr_clip_workspace_floats", "qsr_set_grad_clip", "qsr_set_params", "qsr_local_step",
            "qsr_local_step_sync", "qsr_parallel_step", "qsr_sync", "qsr_sync_sum_floats", "qsr_sync_partial", "qsr_local_step_partial", "qsr_sync_finish", "qsr_sync_static", "qsr_run", "qsr_launch_count",
            "qsr_set_launch_shape", "qsr_set_graph_replay", "qsr_set_resident_steps", "qsr_train_host", "qsr_list_workspace_bytes", "qsr_list_create", "qsr_list_destroy", "qsr_list_set_grads",
-           "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
+           "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_layer_norm",
+           "qsr_layer_norm_workspace_bytes", "qsr_layer_norm_grad", "qsr_embed", "qsr_embed_workspace_bytes", "qsr_embed_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
 
 
 class QsrConfig(C.Structure):
@@ -69,6 +70,23 @@ class QsrLogprobArgs(C.Structure):
                 ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("row_stats", C.c_void_p), ("top_logprob", C.c_void_p),
                 ("top_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_entropy", C.c_void_p), ("d_logits", C.c_void_p),
                 ("d_row_stride", C.c_int64)]
+
+
+class QsrLayerNormArgs(C.Structure):
+    """Mirror of `qsr_layer_norm_args`."""
+    _fields_ = [("x", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p),
+                ("rows", C.c_int64), ("width", C.c_int64), ("x_stride", C.c_int64), ("type", C.c_int32), ("weight_type", C.c_int32),
+                ("eps", C.c_double), ("y", C.c_void_p), ("y_stride", C.c_int64), ("d_y", C.c_void_p), ("d_y_stride", C.c_int64),
+                ("d_x", C.c_void_p), ("d_x_stride", C.c_int64), ("d_weight", C.c_void_p), ("d_bias", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class QsrEmbedArgs(C.Structure):
+    """Mirror of `qsr_embed_args`."""
+    _fields_ = [("table", C.c_void_p), ("tokens", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64),
+                ("width", C.c_int64), ("table_stride", C.c_int64), ("out_stride", C.c_int64), ("table_type", C.c_int32),
+                ("out_type", C.c_int32), ("scale", C.c_double), ("accumulate", C.c_int32), ("reserved", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
 class QsrError(RuntimeError):
@@ -127,6 +145,12 @@ def lib():
             "qsr_list_launch_count": (i64, [vp]),
             "qsr_token_logprobs": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
             "qsr_token_logprobs_grad": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
+            "qsr_layer_norm": (C.c_int, [C.POINTER(QsrLayerNormArgs), vp]),
+            "qsr_layer_norm_workspace_bytes": (i64, [i64, i64]),
+            "qsr_layer_norm_grad": (C.c_int, [C.POINTER(QsrLayerNormArgs), vp]),
+            "qsr_embed": (C.c_int, [C.POINTER(QsrEmbedArgs), vp]),
+            "qsr_embed_workspace_bytes": (i64, [i64, i64, i64]),
+            "qsr_embed_grad": (C.c_int, [C.POINTER(QsrEmbedArgs), vp]),
             "qsr_debug_box_muller": (C.c_int, [vp, i64, vp, vp, vp, vp]),
             "qsr_debug_fast_math": (C.c_int, [vp, i64, vp, vp, vp]),
             "qsr_strerror": (C.c_char_p, [C.c_int]),
@@ -555,6 +579,116 @@ def qsr_token_logprobs_grad(logits, tokens, row_stats, d_logits, d_logprob=None,
     that qsr_token_logprobs wrote for the same logits and temperature."""
     a, _, _ = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
     _check(lib().qsr_token_logprobs_grad(C.byref(a), stream), "qsr_token_logprobs_grad")
+
+
+# ---- layer norm and embedding ---------------------------------------------------------------------------
+
+def _kind(t, what: str) -> int:
+    kind = DTYPE.get(_NAMES[t.dtype])
+    if kind is None:
+        raise ValueError(f"{what}: {t.dtype} is not supported (one of {', '.join(sorted(DTYPE))})")
+    return kind
+
+
+def _workspace(t, device: int) -> Tuple[Optional[int], int]:
+    """Address and bytes of a workspace on the CUDA device of that index."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on cuda:{device} is expected")
+    return t.data_ptr(), int(t.numel() * t.element_size())
+
+
+def _on_current(device: int, what: str) -> None:
+    if device != _current_device():
+        raise ValueError(f"{what} on cuda:{device}, which is not the current device")
+
+
+def _like(t, x, what: str, device: int) -> Tuple[Optional[int], int]:
+    """Address and row stride of a matrix of the shape and type of x; (None, its columns) for None."""
+    if t is None:
+        return None, x.shape[1]
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise ValueError(f"{what}: shape and type of x are expected")
+    return t.data_ptr(), _matrix(t, t.shape, what, device)
+
+
+def _layer_norm_args(x, weight, others, mean, rstd) -> Tuple[QsrLayerNormArgs, int]:
+    """Arguments that both calls share.  others: {field: vector of the weight's type}."""
+    shape, device = x.shape, x.get_device()
+    stride = _matrix(x, shape, "x", device)
+    _on_current(device, "x is")
+    R, N = shape
+    given = [t for t in (weight, *others.values()) if t is not None]
+    a = QsrLayerNormArgs(x=x.data_ptr(), x_stride=stride, rows=R, width=N, type=_kind(x, "x"), weight_type=_kind(given[0] if given else x, "weight"),
+                         mean=_vector(mean, "mean", R, "torch.float32", device), rstd=_vector(rstd, "rstd", R, "torch.float32", device))
+    kind = _NAMES[given[0].dtype] if given else ""
+    a.weight = _vector(weight, "weight", N, kind, device)
+    for name, t in others.items():
+        setattr(a, name, _vector(t, name, N, kind, device))
+    return a, device
+
+
+def qsr_layer_norm(x, y, weight=None, bias=None, mean=None, rstd=None, eps: float = 1e-5, stream: int = 0) -> None:
+    """Layer norm of each row of x into y (x itself is fine), with optional weight and bias (one type), and the rows' statistics
+    (float32) that qsr_layer_norm_grad takes.  Matrices may be columns of wider buffers.  All tensors are the caller's."""
+    a, device = _layer_norm_args(x, weight, {"bias": bias}, mean, rstd)
+    a.y, a.y_stride = _like(y, x, "y", device)
+    a.eps = eps
+    _check(lib().qsr_layer_norm(C.byref(a), stream), "qsr_layer_norm")
+
+
+def qsr_layer_norm_workspace_bytes(rows: int, width: int) -> int:
+    """Bytes of device workspace for the gradients of weight and bias."""
+    n = int(lib().qsr_layer_norm_workspace_bytes(rows, width))
+    if n < 0:
+        raise QsrError(n, "qsr_layer_norm_workspace_bytes")
+    return n
+
+
+def qsr_layer_norm_grad(x, d_y, mean, rstd, d_x=None, weight=None, d_weight=None, d_bias=None, workspace=None, stream: int = 0) -> None:
+    """Gradients of layer norm from the statistics that qsr_layer_norm wrote: of x (x or d_y may be written over), and of weight and
+    bias (of the weight's type, with a workspace of qsr_layer_norm_workspace_bytes bytes), each if it is given."""
+    a, device = _layer_norm_args(x, weight, {"d_weight": d_weight, "d_bias": d_bias}, mean, rstd)
+    a.d_y, a.d_y_stride = _like(d_y, x, "d_y", device)
+    a.d_x, a.d_x_stride = _like(d_x, x, "d_x", device)
+    a.workspace, a.workspace_bytes = _workspace(workspace, device)
+    _check(lib().qsr_layer_norm_grad(C.byref(a), stream), "qsr_layer_norm_grad")
+
+
+def _embed_args(table, tokens, out, scale, table_name: str, out_name: str) -> Tuple[QsrEmbedArgs, int]:
+    device = table.get_device()
+    stride, out_stride = _matrix(table, table.shape, table_name, device), _matrix(out, out.shape, out_name, device)
+    _on_current(device, f"{table_name} is")
+    (V, N), R = table.shape, out.shape[0]
+    if out.shape[1] != N:
+        raise ValueError(f"{out_name}: {out.shape[1]} columns for a table of {N}")
+    return QsrEmbedArgs(table=table.data_ptr(), tokens=_vector(tokens, "tokens", R, "torch.int64", device), out=out.data_ptr(), rows=R, vocab=V,
+                        width=N, table_stride=stride, out_stride=out_stride, table_type=_kind(table, table_name),
+                        out_type=_kind(out, out_name), scale=scale), device
+
+
+def qsr_embed(table, tokens, out, scale: float = 1.0, stream: int = 0) -> None:
+    """out[r] = scale * table[tokens[r]] (zeros where a token is negative).  The matrices may differ in type, and be columns of
+    wider buffers."""
+    a, _ = _embed_args(table, tokens, out, scale, "table", "out")
+    _check(lib().qsr_embed(C.byref(a), stream), "qsr_embed")
+
+
+def qsr_embed_workspace_bytes(rows: int, vocab: int, width: int) -> int:
+    """Bytes of device workspace for qsr_embed_grad."""
+    n = int(lib().qsr_embed_workspace_bytes(rows, vocab, width))
+    if n < 0:
+        raise QsrError(n, "qsr_embed_workspace_bytes")
+    return n
+
+
+def qsr_embed_grad(d_out, tokens, d_table, scale: float = 1.0, accumulate: bool = False, workspace=None, stream: int = 0) -> None:
+    """Gradient of qsr_embed's table: written whole, or (accumulate) added to the rows of tokens that occur."""
+    a, device = _embed_args(d_table, tokens, d_out, scale, "d_table", "d_out")
+    a.accumulate = 1 if accumulate else 0
+    a.workspace, a.workspace_bytes = _workspace(workspace, device)
+    _check(lib().qsr_embed_grad(C.byref(a), stream), "qsr_embed_grad")
 
 
 def qsr_debug_box_muller(words, radius, sine, cosine, stream: int = 0) -> None:

@@ -12,8 +12,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqsr.so")
-SOURCES = ["schedule.cpp", "kernels.cu", "api.cu", "lists.cu", "lists_api.cu", "logprobs.cu"]
-HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "wide.cuh"), os.path.join(os.path.dirname(HERE), "include", "qsr.h")]
+SOURCES = ["schedule.cpp", "kernels.cu", "api.cu", "lists.cu", "lists_api.cu", "logprobs.cu", "layernorm.cu", "embed.cu"]
+HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "checks.h", "wide.cuh", "rows.cuh")] + [os.path.join(os.path.dirname(HERE), "include", "qsr.h")]
 
 
 def _nvcc() -> str:

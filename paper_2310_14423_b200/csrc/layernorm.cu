@@ -1,0 +1,531 @@
+// Layer norm over the rows of a matrix: forward, and backward with the gradients of weight and bias.  See include/qsr.h.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "checks.h"
+#include "rows.cuh"
+
+namespace qsr {
+
+namespace {
+
+constexpr int kBlocks = 296;          // most partial sums of the weight's gradient: two blocks on each of 148 multiprocessors
+constexpr int kMaxHeld = 4;           // most granules of eight elements that a thread holds of a row
+constexpr int kMaxThreads = 1024;
+
+struct Params {
+    const void *x, *dy;
+    void *y, *dx;
+    const void *w, *b;
+    float *mean, *rstd;
+    float *partial;                   // [blocks, 2, width]
+    int64_t rows, x_stride, y_stride, dy_stride, dx_stride;
+    int32_t width, granules, wtype;
+    int32_t wvec;                     // weight and bias aligned to eight elements
+    int32_t want_weight, want_bias;
+    float eps, divisor;
+};
+
+// Weights and biases: read by every row, so through the cache.
+template <bool VEC>
+__device__ __forceinline__ void weights(float (&v)[8], const void *base, float otherwise, int lane, int lanes, int k, int width, int type, bool vec)
+{
+    const int c0 = column<VEC>(lane, lanes, k, 0);
+    if (!base) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = otherwise;
+    } else if (VEC && vec && c0 + 8 <= width) {
+        Raw8 r;
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + size_t(c0) * (type == QSR_F32 ? 4 : 2));
+        const uint4 lo = __ldg(p), hi = type == QSR_F32 ? __ldg(p + 1) : make_uint4(0, 0, 0, 0);
+        r.w[0] = lo.x; r.w[1] = lo.y; r.w[2] = lo.z; r.w[3] = lo.w;
+        r.w[4] = hi.x; r.w[5] = hi.y; r.w[6] = hi.z; r.w[7] = hi.w;
+        widen8(v, r, type);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = column<VEC>(lane, lanes, k, j);
+            v[j] = c < width ? widen1(load1(base, c, type), type) : otherwise;
+        }
+    }
+}
+
+// Sum over the lanes that share a row: 2^n lanes of a warp, or all threads of the block (scratch: a float per warp).
+__device__ __forceinline__ float row_sum(float v, int lanes, float *scratch)
+{
+    for (int d = min(lanes, 32) >> 1; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (lanes <= 32) return v;
+    __syncthreads();                              // the sums before this one have been read
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int n = lanes >> 5;
+    v = (threadIdx.x & 31) < n ? scratch[threadIdx.x & 31] : 0.0f;
+    return warp_sum(v);
+}
+
+// Rows that fit in registers: HELD granules a thread, `lanes` threads a row (a power of two up to 32, or the whole block).  Mean and
+// variance take two passes over the registers, so that rows far from zero lose nothing.
+template <typename T, int HELD, bool VEC>
+__global__ void __launch_bounds__(kMaxThreads) forward_kernel(const __grid_constant__ Params p, int lanes)
+{
+    __shared__ float scratch[32];
+    constexpr int TYPE = Kind<T>::type;
+    const int lane = int(threadIdx.x) & (lanes - 1);
+    const int64_t row = int64_t(blockIdx.x) * (int(blockDim.x) / lanes) + int(threadIdx.x) / lanes;
+    const bool live = row < p.rows;
+    float x[HELD][8];
+    float s = 0.0f;
+    {
+        Raw8 raw[HELD];
+        const void *from = row_of<T>(p.x, live ? row : 0, p.x_stride);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) fetch<VEC>(raw[k], from, lane, lanes, k, live ? p.width : 0, TYPE);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            widen8(x[k], raw[k], TYPE);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += x[k][j];
+        }
+    }
+    const float mean = row_sum(s, lanes, scratch) / p.divisor;
+    float q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[k][j] -= mean;
+            if (column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[k][j], x[k][j], q);
+        }
+    const float rstd = 1.0f / sqrtf(row_sum(q, lanes, scratch) / p.divisor + p.eps);
+    if (!live) return;
+    if (lane == 0) {
+        if (p.mean) p.mean[row] = mean;
+        if (p.rstd) p.rstd[row] = rstd;
+    }
+    void *to = row_of<T>(p.y, row, p.y_stride);
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        if (column<VEC>(lane, lanes, k, 0) >= p.width) break;
+        float w[8], b[8];
+        weights<VEC>(w, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+        weights<VEC>(b, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = fmaf(x[k][j] * rstd, w[j], b[j]);
+        put<VEC>(to, w, lane, lanes, k, p.width, TYPE);
+    }
+}
+
+// Rows of any length, read three times (from the caches after the first); one block a row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kMaxThreads) forward_long_kernel(const __grid_constant__ Params p)
+{
+    __shared__ float scratch[32];
+    constexpr int TYPE = Kind<T>::type;
+    const int lane = threadIdx.x, lanes = blockDim.x, steps = (p.granules + lanes - 1) / lanes;
+    const void *from = row_of<T>(p.x, blockIdx.x, p.x_stride);
+    float s = 0.0f, q = 0.0f, x[8];
+    Raw8 r;
+    for (int k = 0; k < steps; ++k) {
+        fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
+        widen8(x, r, TYPE);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += x[j];
+    }
+    const float mean = row_sum(s, lanes, scratch) / p.divisor;
+    for (int k = 0; k < steps; ++k) {
+        fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
+        widen8(x, r, TYPE);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[j] - mean, x[j] - mean, q);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum(q, lanes, scratch) / p.divisor + p.eps);
+    if (lane == 0) {
+        if (p.mean) p.mean[blockIdx.x] = mean;
+        if (p.rstd) p.rstd[blockIdx.x] = rstd;
+    }
+    void *to = row_of<T>(p.y, blockIdx.x, p.y_stride);
+    for (int k = 0; k < steps; ++k) {
+        fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
+        widen8(x, r, TYPE);
+        float w[8], b[8];
+        weights<VEC>(w, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+        weights<VEC>(b, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = fmaf((x[j] - mean) * rstd, w[j], b[j]);
+        put<VEC>(to, w, lane, lanes, k, p.width, TYPE);
+    }
+}
+
+__device__ __forceinline__ void group_barrier(int group, int threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+}
+
+// Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take R rows at a time, each
+// thread the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which
+// leaves one partial sum for each column.
+template <typename T, bool VEC, int R, int THREADS>
+__global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
+{
+    extern __shared__ float shared[];             // a group's row sums: [groups][2][warps of a group][2 R]; then column sums
+    constexpr int TYPE = Kind<T>::type;
+    const int groups = int(blockDim.x) / lanes, group = int(threadIdx.x) / lanes, lane = int(threadIdx.x) - group * lanes;
+    const int warps = lanes >> 5;
+    const bool mine = column<VEC>(lane, lanes, 0, 0) < p.width;
+    float w[8], dw[8], db[8];
+    weights<VEC>(w, p.w, 1.0f, lane, lanes, 0, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[j] = db[j] = 0.0f;
+    const float inverse = 1.0f / p.divisor;
+    int turn = 0;
+    for (int64_t base = int64_t(blockIdx.x) * groups * R; base < p.rows; base += int64_t(gridDim.x) * groups * R) {
+        const int64_t row0 = base + group * R;
+        Raw8 x[R], dy[R];
+        float mean[R], rstd[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool live = row0 + r < p.rows && mine;
+            const int64_t row = live ? row0 + r : 0;
+            fetch<VEC>(x[r], row_of<T>(p.x, row, p.x_stride), lane, lanes, 0, live ? p.width : 0, TYPE);
+            fetch<VEC>(dy[r], row_of<T>(p.dy, row, p.dy_stride), lane, lanes, 0, live ? p.width : 0, TYPE);
+            mean[r] = live ? p.mean[row] : 0.0f;
+            rstd[r] = live ? p.rstd[row] : 0.0f;
+        }
+        float s[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float a[8], d[8];
+            widen8(a, x[r], TYPE);
+            widen8(d, dy[r], TYPE);
+            float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                // beyond the row both are zero: a finite statistic gives no sum, one that is not finite is kept out
+                const float hat = column<VEC>(lane, lanes, 0, j) < p.width ? (a[j] - mean[r]) * rstd[r] : 0.0f;
+                dw[j] = fmaf(d[j], hat, dw[j]);
+                db[j] += d[j];
+                const float g = d[j] * w[j];
+                s1 += g;
+                s2 = fmaf(g, hat, s2);
+            }
+            s[2 * r] = s1;
+            s[2 * r + 1] = s2;
+        }
+        if (p.dx) {
+#pragma unroll
+            for (int i = 0; i < 2 * R; ++i)
+                for (int d = min(lanes, 32) >> 1; d; d >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
+            if (lanes > 32) {
+                float *at = shared + (group * 2 + turn) * warps * 2 * R;
+                turn ^= 1;
+                if ((lane & 31) == 0) {
+#pragma unroll
+                    for (int i = 0; i < 2 * R; ++i) at[(lane >> 5) * 2 * R + i] = s[i];
+                }
+                group_barrier(group, lanes);
+#pragma unroll
+                for (int i = 0; i < 2 * R; ++i) {
+                    s[i] = 0.0f;
+                    for (int v = 0; v < warps; ++v) s[i] += at[v * 2 * R + i];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (row0 + r >= p.rows || !mine) continue;
+                float a[8], d[8];
+                widen8(a, x[r], TYPE);
+                widen8(d, dy[r], TYPE);
+                const float c1 = s[2 * r] * inverse, c2 = s[2 * r + 1] * inverse;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float hat = (a[j] - mean[r]) * rstd[r];
+                    d[j] = (fmaf(d[j], w[j], -c1) - hat * c2) * rstd[r];
+                }
+                put<VEC>(row_of<T>(p.dx, row0 + r, p.dx_stride), d, lane, lanes, 0, p.width, TYPE);
+            }
+        }
+    }
+    if (!p.partial) return;
+    float *out = p.partial + int64_t(blockIdx.x) * 2 * p.width;
+    for (int pass = 0; pass < 2; ++pass) {
+        float (&v)[8] = pass ? db : dw;
+        if (groups > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) shared[j * blockDim.x + threadIdx.x] = v[j];
+            __syncthreads();
+            if (group == 0)
+                for (int g = 1; g < groups; ++g)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += shared[j * blockDim.x + g * lanes + lane];
+        }
+        if (group == 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = column<VEC>(lane, lanes, 0, j);
+                if (c < p.width) out[int64_t(pass) * p.width + c] = v[j];
+            }
+    }
+}
+
+// Longer rows: their gradient by a block a row, which reads the row twice ...
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kMaxThreads) backward_long_kernel(const __grid_constant__ Params p)
+{
+    __shared__ float scratch[32];
+    constexpr int TYPE = Kind<T>::type;
+    const int lane = threadIdx.x, lanes = blockDim.x, steps = (p.granules + lanes - 1) / lanes;
+    const void *xr = row_of<T>(p.x, blockIdx.x, p.x_stride), *dr = row_of<T>(p.dy, blockIdx.x, p.dy_stride);
+    void *to = row_of<T>(p.dx, blockIdx.x, p.dx_stride);
+    const float mean = p.mean[blockIdx.x], rstd = p.rstd[blockIdx.x];
+    float s1 = 0.0f, s2 = 0.0f, a[8], d[8], w[8];
+    Raw8 rx, rd;
+    for (int k = 0; k < steps; ++k) {
+        fetch<VEC>(rx, xr, lane, lanes, k, p.width, TYPE);
+        fetch<VEC>(rd, dr, lane, lanes, k, p.width, TYPE);
+        widen8(a, rx, TYPE);
+        widen8(d, rd, TYPE);
+        weights<VEC>(w, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (column<VEC>(lane, lanes, k, j) < p.width) {
+                s1 = fmaf(d[j], w[j], s1);
+                s2 = fmaf(d[j] * w[j], (a[j] - mean) * rstd, s2);
+            }
+    }
+    const float c1 = row_sum(s1, lanes, scratch) / p.divisor, c2 = row_sum(s2, lanes, scratch) / p.divisor;
+    for (int k = 0; k < steps; ++k) {
+        fetch<VEC>(rx, xr, lane, lanes, k, p.width, TYPE);
+        fetch<VEC>(rd, dr, lane, lanes, k, p.width, TYPE);
+        widen8(a, rx, TYPE);
+        widen8(d, rd, TYPE);
+        weights<VEC>(w, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = (fmaf(d[j], w[j], -c1) - (a[j] - mean) * rstd * c2) * rstd;
+        put<VEC>(to, d, lane, lanes, k, p.width, TYPE);
+    }
+}
+
+// ... and the column sums by blocks of 256 granules over a part of the rows.  Runs first, since the gradient may be
+// written over its operands.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) column_sums_kernel(const __grid_constant__ Params p)
+{
+    constexpr int TYPE = Kind<T>::type;
+    const int lanes = int(gridDim.x) * 256, lane = int(blockIdx.x) * 256 + int(threadIdx.x);
+    if (column<VEC>(lane, lanes, 0, 0) >= p.width) return;
+    float dw[8], db[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw[j] = db[j] = 0.0f;
+#pragma unroll 2
+    for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        Raw8 rx, rd;
+        float a[8], d[8];
+        fetch<VEC>(rx, row_of<T>(p.x, row, p.x_stride), lane, lanes, 0, p.width, TYPE);
+        fetch<VEC>(rd, row_of<T>(p.dy, row, p.dy_stride), lane, lanes, 0, p.width, TYPE);
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        widen8(a, rx, TYPE);
+        widen8(d, rd, TYPE);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            dw[j] = fmaf(d[j], (a[j] - mean) * rstd, dw[j]);
+            db[j] += d[j];
+        }
+    }
+    float *out = p.partial + int64_t(blockIdx.y) * 2 * p.width;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = column<VEC>(lane, lanes, 0, j);
+        if (c < p.width) {
+            out[c] = dw[j];
+            out[p.width + c] = db[j];
+        }
+    }
+}
+
+// Adds the blocks' partial sums, always in the same order: 32 columns a block, eight threads a column.
+__global__ void __launch_bounds__(256) finish_kernel(const float *partial, int blocks, int width, void *dw, void *db, int type)
+{
+    __shared__ float part[8][33];
+    const int64_t c = int64_t(blockIdx.x) * 32 + (threadIdx.x & 31), all = int64_t(2) * width;
+    const int y = threadIdx.x >> 5;
+    float s = 0.0f;
+    if (c < all)
+#pragma unroll 8
+        for (int b = y; b < blocks; b += 8) s += partial[b * all + c];
+    part[y][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (y != 0 || c >= all) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += part[i][threadIdx.x & 31];
+    void *to = c < width ? dw : db;
+    if (to) store1(to, c < width ? c : c - width, s, type);
+}
+
+template <typename T, int HELD, bool VEC>
+int launch_held(const Params &p, int lanes, cudaStream_t st)
+{
+    const int threads = std::max(lanes, 128), rows = threads / lanes;
+    forward_kernel<T, HELD, VEC><<<unsigned((p.rows + rows - 1) / rows), unsigned(threads), 0, st>>>(p, lanes);
+    return int(cudaGetLastError());
+}
+
+template <typename T, bool VEC>
+int launch_forward(const Params &p, cudaStream_t st)
+{
+    // a warp a row up to 1024 elements, then the smallest block that holds a row in its registers
+    int lanes = p.granules <= 32 ? power_of_two(p.granules) : 32;
+    if (p.granules > 32 * kMaxHeld) lanes = 128;
+    while (lanes >= 128 && p.granules > lanes * kMaxHeld) lanes *= 2;
+    if (lanes > kMaxThreads) {
+        forward_long_kernel<T, VEC><<<unsigned(p.rows), kMaxThreads, 0, st>>>(p);
+        return int(cudaGetLastError());
+    }
+    switch ((p.granules + lanes - 1) / lanes) {
+    case 1: return launch_held<T, 1, VEC>(p, lanes, st);
+    case 2: return launch_held<T, 2, VEC>(p, lanes, st);
+    case 3: return launch_held<T, 3, VEC>(p, lanes, st);
+    default: return launch_held<T, 4, VEC>(p, lanes, st);
+    }
+}
+
+template <typename T, bool VEC>
+int launch_backward(const Params &p, void *dw, void *db, cudaStream_t st)
+{
+    int blocks = 0;
+    if (p.granules <= kMaxThreads) {
+        // rows at a time: as many as the registers of a block of this size allow
+        const int lanes = p.granules <= 32 ? power_of_two(p.granules) : (p.granules + 31) / 32 * 32;
+        const int groups = lanes >= 256 ? 1 : lanes <= 32 ? 256 / lanes : 384 / lanes;
+        constexpr int many = sizeof(T) == 4 ? 2 : 4;
+        const int threads = groups * lanes, R = threads <= 384 ? many : many / 2;
+        const int64_t turns = (p.rows + int64_t(groups) * R - 1) / (int64_t(groups) * R);
+        blocks = int(std::min<int64_t>(turns, kBlocks));
+        const size_t sums = size_t(groups) * 2 * size_t(lanes / 32) * 2 * size_t(R) * 4, columns = groups > 1 ? size_t(threads) * 8 * 4 : 0;
+        if (threads <= 384) backward_kernel<T, VEC, many, 384><<<unsigned(blocks), unsigned(threads), std::max(sums, columns), st>>>(p, lanes);
+        else backward_kernel<T, VEC, many / 2, kMaxThreads><<<unsigned(blocks), unsigned(threads), std::max(sums, columns), st>>>(p, lanes);
+    } else {
+        if (p.partial) {
+            const int wide = (p.granules + 255) / 256;
+            blocks = int(std::min<int64_t>(std::max(1, 2 * kBlocks / wide), std::min<int64_t>(p.rows, kBlocks)));
+            column_sums_kernel<T, VEC><<<dim3(unsigned(wide), unsigned(blocks)), 256, 0, st>>>(p);
+            if (cudaError_t err = cudaGetLastError()) return int(err);
+        }
+        if (p.dx) backward_long_kernel<T, VEC><<<unsigned(p.rows), kMaxThreads, 0, st>>>(p);
+    }
+    if (cudaError_t err = cudaGetLastError()) return int(err);
+    if (!p.partial) return 0;
+    finish_kernel<<<unsigned((int64_t(2) * p.width + 31) / 32), 256, 0, st>>>(p.partial, blocks, p.width, dw, db, p.wtype);
+    return int(cudaGetLastError());
+}
+
+constexpr int64_t kMaxWidth = int64_t(1) << 24;      // up to which a width is a number in fp32
+
+int shared_checks(const qsr_layer_norm_args &a)
+{
+    if (!type_bytes(a.type) || !type_bytes(a.weight_type)) return QSR_EINVAL;
+    if (a.rows < 0 || a.rows > 0x7fffffff || a.width < 1 || a.width > kMaxWidth || a.x_stride < a.width) return QSR_ERANGE;
+    const unsigned e = unsigned(type_bytes(a.type)), w = unsigned(type_bytes(a.weight_type));
+    if (!aligned_to(a.x, e) || !aligned_to(a.weight, w) || !aligned_to(a.mean, 4) || !aligned_to(a.rstd, 4)) return QSR_EALIGN;
+    return QSR_OK;
+}
+
+Params params_of(const qsr_layer_norm_args &a)
+{
+    Params p = {};
+    p.x = a.x; p.x_stride = a.x_stride;
+    p.w = a.weight; p.wtype = a.weight_type;
+    p.mean = a.mean; p.rstd = a.rstd;
+    p.rows = a.rows; p.width = int32_t(a.width);
+    p.granules = int32_t((a.width + 7) / 8);
+    p.divisor = float(a.width);
+    return p;
+}
+
+}  // namespace
+
+}  // namespace qsr
+
+extern "C" {
+
+int qsr_layer_norm(const qsr_layer_norm_args *a, void *cuda_stream)
+{
+    using namespace qsr;
+    if (!a || !(a->eps >= 0.0) || !std::isfinite(float(a->eps))) return QSR_EINVAL;
+    if (int rc = shared_checks(*a)) return rc;
+    if (a->y_stride < a->width || (a->y == a->x && a->rows > 1 && a->y_stride != a->x_stride)) return QSR_ERANGE;
+    if (a->rows == 0) return QSR_OK;
+    if (!a->x || !a->y) return QSR_EINVAL;
+    const int e = type_bytes(a->type), we = type_bytes(a->weight_type);
+    if (!aligned_to(a->y, unsigned(e)) || !aligned_to(a->bias, unsigned(we))) return QSR_EALIGN;
+    if (a->y != a->x && share_bytes(a->x, a->x_stride, a->width, e, a->rows, a->y, a->y_stride, a->width, e, a->rows)) return QSR_EINVAL;
+    Params p = params_of(*a);
+    p.y = a->y; p.y_stride = a->y_stride;
+    p.b = a->bias;
+    p.eps = float(a->eps);
+    p.wvec = aligned_to(a->weight, 16) && aligned_to(a->bias, 16);
+    const bool vec = rows_aligned(a->x, a->x_stride, a->rows, e) && rows_aligned(a->y, a->y_stride, a->rows, e);
+    const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    int err;
+    if (a->type == QSR_F32) err = vec ? launch_forward<float, true>(p, st) : launch_forward<float, false>(p, st);
+    else if (a->type == QSR_BF16) err = vec ? launch_forward<__nv_bfloat16, true>(p, st) : launch_forward<__nv_bfloat16, false>(p, st);
+    else err = vec ? launch_forward<__half, true>(p, st) : launch_forward<__half, false>(p, st);
+    return launch_status(err);
+}
+
+int64_t qsr_layer_norm_workspace_bytes(int64_t rows, int64_t width)
+{
+    if (rows < 0 || rows > 0x7fffffff || width < 1 || width > qsr::kMaxWidth) return QSR_ERANGE;
+    return std::max<int64_t>(256, std::min<int64_t>(std::max<int64_t>(rows, 1), qsr::kBlocks) * 2 * width * 4);
+}
+
+int qsr_layer_norm_grad(const qsr_layer_norm_args *a, void *cuda_stream)
+{
+    using namespace qsr;
+    if (!a) return QSR_EINVAL;
+    if (int rc = shared_checks(*a)) return rc;
+    if (a->d_y_stride < a->width || (a->d_x && a->d_x_stride < a->width)) return QSR_ERANGE;
+    const int e = type_bytes(a->type), we = type_bytes(a->weight_type);
+    const bool sums = a->d_weight || a->d_bias;
+    if (!aligned_to(a->d_weight, unsigned(we)) || !aligned_to(a->d_bias, unsigned(we)) || !aligned_to(a->d_y, unsigned(e)) || !aligned_to(a->d_x, unsigned(e)))
+        return QSR_EALIGN;
+    if (sums) {
+        if (!a->workspace) return QSR_EINVAL;
+        if (!aligned_to(a->workspace, 256)) return QSR_EALIGN;
+        if (a->workspace_bytes < qsr_layer_norm_workspace_bytes(a->rows, a->width)) return QSR_ERANGE;
+    }
+    const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (a->rows == 0) {               // sums over nothing
+        if (a->d_weight)
+            if (cudaError_t err = cudaMemsetAsync(a->d_weight, 0, size_t(a->width) * size_t(we), st)) return launch_status(int(err));
+        if (a->d_bias)
+            if (cudaError_t err = cudaMemsetAsync(a->d_bias, 0, size_t(a->width) * size_t(we), st)) return launch_status(int(err));
+        return QSR_OK;
+    }
+    if (!a->x || !a->d_y || !a->mean || !a->rstd) return QSR_EINVAL;
+    if (!sums && !a->d_x) return QSR_OK;
+    if (a->d_x) {
+        const struct { const void *p; int64_t stride; } of[2] = {{a->x, a->x_stride}, {a->d_y, a->d_y_stride}};
+        for (const auto &o : of) {
+            if (o.p == a->d_x && (o.stride == a->d_x_stride || a->rows == 1)) continue;      // in place
+            if (share_bytes(o.p, o.stride, a->width, e, a->rows, a->d_x, a->d_x_stride, a->width, e, a->rows)) return QSR_EINVAL;
+        }
+    }
+    Params p = params_of(*a);
+    p.dy = a->d_y; p.dy_stride = a->d_y_stride;
+    p.dx = a->d_x; p.dx_stride = a->d_x_stride;
+    p.partial = sums ? static_cast<float *>(a->workspace) : nullptr;
+    p.wvec = aligned_to(a->weight, 16);
+    const bool vec = rows_aligned(a->x, a->x_stride, a->rows, e) && rows_aligned(a->d_y, a->d_y_stride, a->rows, e) &&
+                     (!a->d_x || rows_aligned(a->d_x, a->d_x_stride, a->rows, e));
+    int err;
+    if (a->type == QSR_F32) err = vec ? launch_backward<float, true>(p, a->d_weight, a->d_bias, st) : launch_backward<float, false>(p, a->d_weight, a->d_bias, st);
+    else if (a->type == QSR_BF16) err = vec ? launch_backward<__nv_bfloat16, true>(p, a->d_weight, a->d_bias, st) : launch_backward<__nv_bfloat16, false>(p, a->d_weight, a->d_bias, st);
+    else err = vec ? launch_backward<__half, true>(p, a->d_weight, a->d_bias, st) : launch_backward<__half, false>(p, a->d_weight, a->d_bias, st);
+    return launch_status(err);
+}
+
+}  // extern "C"

@@ -23,6 +23,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "checks.h"
 #include "wide.cuh"
 
 namespace qsr {
@@ -816,21 +817,9 @@ int launch_logprobs_grad(const LogprobParams &p, void *stream)
 
 namespace {
 
-bool element_aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
-// Whether two matrices of rows x vocab elements of e bytes (strides in elements; not the same matrix) share one.  With equal
-// strides, as columns of one buffer have them, rows meet exactly if the distance modulo the stride is less than a row from
-// either side; otherwise matrices that lie in and out of one another count as sharing.
-bool share_bytes(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int64_t rows, int64_t vocab, int e)
-{
-    typedef __int128 wide;                          // strides have no upper limit
-    const wide x = wide(reinterpret_cast<uintptr_t>(a)), y = wide(reinterpret_cast<uintptr_t>(b));
-    const wide row = wide(vocab) * e, xs = wide(a_stride) * e, ys = wide(b_stride) * e;
-    if (x + (rows - 1) * xs + row <= y || y + (rows - 1) * ys + row <= x) return false;
-    if (xs != ys || rows == 1) return true;
-    const wide d = (x > y ? x - y : y - x) % xs;
-    return d < row || d > xs - row;
-}
+using qsr::aligned_to;
+using qsr::launch_status;
+using qsr::share_bytes;
 
 // Checks what both calls share and fills the kernel's arguments.
 int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &p)
@@ -848,14 +837,14 @@ int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &
         if (!forward && (!a->d_logits || !a->row_stats || (a->d_entropy && !a->entropy))) return QSR_EINVAL;
     }
     const unsigned e = a->logits_type == QSR_F32 ? 4 : 2;
-    if (!element_aligned(a->logits, e) || !element_aligned(a->d_logits, e) || !element_aligned(a->tokens, 8) ||
-        !element_aligned(a->entropy, 4) || !element_aligned(a->row_stats, 8) || !element_aligned(a->d_logprob, 4) ||
-        !element_aligned(a->d_entropy, 4))
+    if (!aligned_to(a->logits, e) || !aligned_to(a->d_logits, e) || !aligned_to(a->tokens, 8) ||
+        !aligned_to(a->entropy, 4) || !aligned_to(a->row_stats, 8) || !aligned_to(a->d_logprob, 4) ||
+        !aligned_to(a->d_entropy, 4))
         return QSR_EALIGN;
-    if (forward && (!element_aligned(a->logprob, 4) || (a->n_top > 0 && (!element_aligned(a->top_logprob, 4) || !element_aligned(a->top_token, 8)))))
+    if (forward && (!aligned_to(a->logprob, 4) || (a->n_top > 0 && (!aligned_to(a->top_logprob, 4) || !aligned_to(a->top_token, 8)))))
         return QSR_EALIGN;
     if (a->rows > 0 && a->d_logits && a->d_logits != a->logits &&
-        share_bytes(a->logits, a->row_stride, a->d_logits, a->d_row_stride, a->rows, a->vocab, int(e)))
+        share_bytes(a->logits, a->row_stride, a->vocab, int(e), a->rows, a->d_logits, a->d_row_stride, a->vocab, int(e), a->rows))
         return QSR_EINVAL;
     p.logits = a->logits; p.tokens = a->tokens;
     p.logprob = a->logprob; p.entropy = a->entropy; p.stats = a->row_stats;
@@ -868,13 +857,6 @@ int logprob_params(const qsr_logprob_args *a, bool forward, qsr::LogprobParams &
     return QSR_OK;
 }
 
-int launched(int err)
-{
-    if (err == 0) return QSR_OK;
-    cudaGetLastError();
-    return QSR_ECUDA;
-}
-
 }  // namespace
 
 extern "C" {
@@ -883,14 +865,14 @@ int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream)
 {
     qsr::LogprobParams p;
     if (int rc = logprob_params(args, true, p)) return rc;
-    return p.rows == 0 ? QSR_OK : launched(qsr::launch_logprobs(p, cuda_stream));
+    return p.rows == 0 ? QSR_OK : qsr::launch_status(qsr::launch_logprobs(p, cuda_stream));
 }
 
 int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream)
 {
     qsr::LogprobParams p;
     if (int rc = logprob_params(args, false, p)) return rc;
-    return p.rows == 0 ? QSR_OK : launched(qsr::launch_logprobs_grad(p, cuda_stream));
+    return p.rows == 0 ? QSR_OK : qsr::launch_status(qsr::launch_logprobs_grad(p, cuda_stream));
 }
 
 }  // extern "C"
