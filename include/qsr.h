@@ -446,6 +446,86 @@ int qsr_token_logprobs(const qsr_logprob_args *args, void *cuda_stream);
  * ignored.  One launch; asynchronous. */
 int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream);
 
+/* ---- matrices stepped by their orthogonalised momentum --------------------------------------------------- */
+
+/*
+ * The optimizer step of a model's hidden matrices in which the update has (nearly) equal singular values, beside qsr_list_step
+ * for its vectors, embeddings and heads; and the round end over K copies of the same matrices.  Per matrix of r x c elements, row
+ * by row without gaps, k = min(r, c), with g = grad_scale * grad:
+ *   m <- m + (1-beta)*(g - m);   u = nesterov ? g + beta*(m - g) : m;   X = u / (norm(u) + eps), norm: root of the sum of squares
+ *   `iterations` times:  A = X X^T (X^T X if r > c);  C = a I + b A + c A^2;  X <- C X (X C),  a, b, c = 3.4445, -4.7750, 2.0315
+ *   theta <- theta - (lr*weight_decay*wd_scale*theta + lr*update_scale*X),
+ * theta rounded once to the parameter's type and once, from the same fp32 value, to the working copy's.  The polynomial
+ * takes singular values above about 0.005 to [0.68, 1.21] in five iterations; it does not converge to one.
+ * Products are taken by the tensor cores on fp16 numbers with sums in fp32; X, A and C are held at powers of two that keep them in
+ * fp16's range.  products = 1 rounds each of them to fp16: the update is off by about 1e-3 of its norm (an eighth of what bf16
+ * would give).  products = 3 holds them as sums of two fp16 numbers and takes three products for each: off by 2e-6 to 2e-5, at
+ * about three times the cost; for fp32 parameters that are compared with an fp32 step.  Norms are summed in binary64.  No
+ * floating-point atomics: results repeat bit for bit.  A NaN or an infinity in a gradient makes its whole matrix NaN, and no
+ * other.  A matrix of zeros has the update zero.
+ *
+ * Matrices are worker-major, as tensors of a qsr_list: entry k*(n_matrices/workers) + j is matrix j of worker k.
+ */
+#define QSR_MUON_MAX_ITERATIONS 16
+
+typedef struct qsr_muon qsr_muon; /* opaque; host memory owned by the library */
+
+/* One matrix: DEVICE pointers to rows*cols consecutive elements each (NULL is accepted where that is 0). */
+typedef struct qsr_matrix {
+    void *param;          /* param_type, any element alignment                                                   */
+    void *copy;           /* copy_type: written by every step and synchronization; NULL where QSR_NONE           */
+    const void *grad;     /* grad_type; may be NULL until qsr_muon_set_grads                                     */
+    float *momentum;      /* m                                                                                   */
+    int64_t rows, cols;   /* 0 .. 2^20 each, the shorter side at most 32768                                      */
+    int32_t param_type;   /* QSR_F32, QSR_BF16 or QSR_F16                                                        */
+    int32_t grad_type;
+    int32_t copy_type;    /* the same, or QSR_NONE                                                               */
+    float wd_scale;       /* factor on the weight decay                                                          */
+    float update_scale;   /* factor on the update, sqrt(max(1, r/c)) for instance                                */
+    int32_t reserved;     /* 0                                                                                   */
+} qsr_matrix;
+
+typedef struct qsr_muon_config {
+    int32_t n_matrices;   /* entries, a multiple of workers                                                      */
+    int32_t workers;      /* K                                                                                   */
+    int32_t products;     /* 1 or 3, above                                                                       */
+    int32_t iterations;   /* 1 .. QSR_MUON_MAX_ITERATIONS, 5 as published                                        */
+    int32_t nesterov;     /* 0 or 1                                                                              */
+    int32_t reserved;     /* 0                                                                                   */
+    double beta, eps, weight_decay;
+} qsr_muon_config;
+
+/* Bytes of device workspace for matrices of these sizes (host arrays): about 4 bytes an element with one product, 8 with three,
+ * plus as much for the square of the shorter side.  Negative qsr_status on error. */
+int64_t qsr_muon_workspace_bytes(const int64_t *rows_host, const int64_t *cols_host, int32_t n_matrices, int32_t workers, int32_t products);
+
+/* Makes a list over caller-owned matrices; arguments, stream, workspace and refusals as at qsr_list_create.  The workspace belongs
+ * to this list alone, and so does a captured step: two lists, or two graphs of one list that can overlap on the GPU, must not
+ * share it. */
+int qsr_muon_create(qsr_muon **out, const qsr_muon_config *cfg, const qsr_matrix *matrices_host, void *workspace_dev, int64_t workspace_bytes,
+                    void *cuda_stream);
+
+/* Frees the list (host memory only).  NULL is accepted. */
+int qsr_muon_destroy(qsr_muon *muon);
+
+/* New gradient addresses, as qsr_list_set_grads. */
+int qsr_muon_set_grads(qsr_muon *muon, const void *const *grads_host);
+
+/* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  2 + 3 * iterations
+ * launches, whatever the number of matrices; asynchronous.  It may be captured; lr and grad_scale are then those of the capture. */
+int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale);
+
+/* End of a round over the list's K workers, as qsr_list_sync: every parameter becomes the mean (sum over k = 0..K-1 in fp32) / K;
+ * QSR_STATE_KEEP leaves m alone, QSR_STATE_AVERAGE replaces it by its mean, QSR_STATE_RESET zeroes it. */
+int qsr_muon_sync(qsr_muon *muon, int32_t state_sync);
+
+/* Waits for the list's stream.  QSR_ECUDA: a wait inside an earlier step's kernels ran out (they are bounded, so that a kernel
+ * always ends); that step's results are not valid.  QSR_ESTATE as at qsr_list_set_grads. */
+int qsr_muon_check(qsr_muon *muon);
+
+/* Kernel launches issued through this list so far. */
+int64_t qsr_muon_launch_count(const qsr_muon *muon);
+
 /* ---- layer norm ------------------------------------------------------------------------------------------ */
 
 /*

@@ -33,7 +33,8 @@ EXPORTS = ("qsr_config_check", "qsr_row_stride_hint", "qsr_config_learning_rate"
            "qsr_workspace_bytes", "qsr_init", "qsr_destroy", "qsr_round_length", "qsr_set_tensor_table", "qsr_clip_workspace_floats", "qsr_set_grad_clip", "qsr_set_params", "qsr_local_step",
            "qsr_local_step_sync", "qsr_parallel_step", "qsr_sync", "qsr_sync_sum_floats", "qsr_sync_partial", "qsr_local_step_partial", "qsr_sync_finish", "qsr_sync_static", "qsr_run", "qsr_launch_count",
            "qsr_set_launch_shape", "qsr_set_graph_replay", "qsr_set_resident_steps", "qsr_train_host", "qsr_list_workspace_bytes", "qsr_list_create", "qsr_list_destroy", "qsr_list_set_grads",
-           "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_layer_norm",
+           "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_muon_workspace_bytes",
+           "qsr_muon_create", "qsr_muon_destroy", "qsr_muon_set_grads", "qsr_muon_step", "qsr_muon_sync", "qsr_muon_check", "qsr_muon_launch_count", "qsr_layer_norm",
            "qsr_layer_norm_workspace_bytes", "qsr_layer_norm_grad", "qsr_embed", "qsr_embed_workspace_bytes", "qsr_embed_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
 
 
@@ -70,6 +71,19 @@ class QsrLogprobArgs(C.Structure):
                 ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("row_stats", C.c_void_p), ("top_logprob", C.c_void_p),
                 ("top_token", C.c_void_p), ("d_logprob", C.c_void_p), ("d_entropy", C.c_void_p), ("d_logits", C.c_void_p),
                 ("d_row_stride", C.c_int64)]
+
+
+class QsrMatrix(C.Structure):
+    """Mirror of `qsr_matrix`."""
+    _fields_ = [("param", C.c_void_p), ("copy", C.c_void_p), ("grad", C.c_void_p), ("momentum", C.c_void_p), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("wd_scale", C.c_float),
+                ("update_scale", C.c_float), ("reserved", C.c_int32)]
+
+
+class QsrMuonConfig(C.Structure):
+    """Mirror of `qsr_muon_config`."""
+    _fields_ = [("n_matrices", C.c_int32), ("workers", C.c_int32), ("products", C.c_int32), ("iterations", C.c_int32), ("nesterov", C.c_int32),
+                ("reserved", C.c_int32), ("beta", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double)]
 
 
 class QsrLayerNormArgs(C.Structure):
@@ -145,6 +159,14 @@ def lib():
             "qsr_list_launch_count": (i64, [vp]),
             "qsr_token_logprobs": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
             "qsr_token_logprobs_grad": (C.c_int, [C.POINTER(QsrLogprobArgs), vp]),
+            "qsr_muon_workspace_bytes": (i64, [vp, vp, i32, i32, i32]),
+            "qsr_muon_create": (C.c_int, [C.POINTER(vp), C.POINTER(QsrMuonConfig), C.POINTER(QsrMatrix), vp, i64, vp]),
+            "qsr_muon_destroy": (C.c_int, [vp]),
+            "qsr_muon_set_grads": (C.c_int, [vp, vp]),
+            "qsr_muon_step": (C.c_int, [vp, C.c_double, C.c_double]),
+            "qsr_muon_sync": (C.c_int, [vp, i32]),
+            "qsr_muon_check": (C.c_int, [vp]),
+            "qsr_muon_launch_count": (i64, [vp]),
             "qsr_layer_norm": (C.c_int, [C.POINTER(QsrLayerNormArgs), vp]),
             "qsr_layer_norm_workspace_bytes": (i64, [i64, i64]),
             "qsr_layer_norm_grad": (C.c_int, [C.POINTER(QsrLayerNormArgs), vp]),
@@ -408,6 +430,15 @@ def qsr_list_workspace_bytes(numels, workers: int = 1) -> int:
     return n
 
 
+def _in_use(tensors, stream: int, device) -> None:
+    """Keeps the tensors' memory from being given out again before `stream` has done its work so far."""
+    import torch
+    on = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(on)
+
+
 class TensorList:
     """Owner of one `qsr_list`: AdamW steps and replica means over a model's own tensors.
 
@@ -495,12 +526,7 @@ class TensorList:
             table[i] = _element(g, p, "grads", i, only[self._grad_types[i]])
         _check(lib().qsr_list_set_grads(self._h, table), "qsr_list_set_grads")
         if self._grads is not None:
-            import torch
-            device = self._params[0].device
-            stream = torch.cuda.ExternalStream(self._stream, device) if self._stream else torch.cuda.default_stream(device)
-            for g in self._grads:
-                if g is not None:
-                    g.record_stream(stream)
+            _in_use(self._grads, self._stream, self._params[0].device)
         self._grads = list(grads)
 
     def qsr_list_step(self, n: int, lr: float, grad_scale: float = 1.0) -> None:
@@ -579,6 +605,113 @@ def qsr_token_logprobs_grad(logits, tokens, row_stats, d_logits, d_logprob=None,
     that qsr_token_logprobs wrote for the same logits and temperature."""
     a, _, _ = _logprob_args(logits, tokens, inv_temperature, entropy, row_stats, d_logprob, d_entropy, d_logits)
     _check(lib().qsr_token_logprobs_grad(C.byref(a), stream), "qsr_token_logprobs_grad")
+
+
+# ---- matrices stepped by their orthogonalised momentum --------------------------------------------------
+
+def qsr_muon_workspace_bytes(shapes, workers: int = 1, products: int = 1) -> int:
+    """Bytes of device workspace for a MuonList over matrices of these (rows, columns) (all workers' matrices)."""
+    rows, cols = (np.ascontiguousarray([int(s[i]) for s in shapes], np.int64) for i in (0, 1))
+    n = int(lib().qsr_muon_workspace_bytes(rows.ctypes.data, cols.ctypes.data, rows.size, int(workers), int(products)))
+    if n < 0:
+        raise QsrError(n, "qsr_muon_workspace_bytes")
+    return n
+
+
+def _entry(t, like, what: str, i: int, dtypes=DTYPE):
+    """Device address of operand `what` of matrix i: contiguous and of the parameter's shape."""
+    if t.shape != like.shape or not t.is_contiguous():
+        raise ValueError(f"{what}[{i}]: a contiguous matrix of shape {tuple(like.shape)} is expected")
+    return _element(t, like, what, i, dtypes)
+
+
+class MuonList:
+    """Owner of one `qsr_muon`: steps of matrices by their orthogonalised momentum, and replica means over them.
+
+    params / grads / copies: lists of contiguous 2-D CUDA tensors in float32, bfloat16 or float16 (grads and copies may be None, or
+    None in places); momentum: float32; with several workers, worker 0's matrices first, then worker 1's, and so on.
+    wd_scale, update_scale: factors on the weight decay and on the update per matrix (default: 1, and sqrt(max(1, rows / columns))).
+    products: 1 (fp16) or 3 (nearly fp32).  workspace: a CUDA tensor of qsr_muon_workspace_bytes bytes.  Keeps references to the
+    tensors whose memory the library borrows; streams and lifetimes as at TensorList."""
+
+    def __init__(self, params, grads, momentum, copies=None, wd_scale=None, update_scale=None, workers: int = 1, beta: float = 0.95,
+                 nesterov: bool = True, weight_decay: float = 0.0, eps: float = 1e-7, iterations: int = 5, products: int = 1,
+                 workspace=None, stream: int = 0):
+        self._h = C.c_void_p()
+        n = len(params)
+        for what, column in (("grads", grads), ("momentum", momentum), ("copies", copies), ("wd_scale", wd_scale), ("update_scale", update_scale)):
+            if column is None and what == "momentum":
+                raise ValueError("momentum is required")
+            if column is not None and len(column) != n:
+                raise ValueError(f"{what}: {len(column)} entries for {n} matrices")
+        device = params[0].get_device() if n else -1
+        if workspace is not None and n and workspace.get_device() != device:
+            raise ValueError(f"workspace: expected a CUDA tensor on cuda:{device}")
+        entries = (QsrMatrix * max(1, n))()
+        for i, p in enumerate(params):
+            if p.dim() != 2:
+                raise ValueError(f"params[{i}]: a matrix is expected")
+            e = entries[i]
+            e.rows, e.cols = p.shape
+            e.param, e.param_type = _entry(p, p, "params", i), DTYPE.get(_NAMES[p.dtype], QSR_NONE)
+            if p.get_device() != device:
+                raise ValueError(f"params[{i}]: expected a CUDA tensor on cuda:{device}")
+            e.momentum = _entry(momentum[i], p, "momentum", i, {"torch.float32": 0})
+            e.copy_type = QSR_NONE
+            if copies is not None and copies[i] is not None:
+                e.copy, e.copy_type = _entry(copies[i], p, "copies", i), DTYPE[_NAMES[copies[i].dtype]]
+            g = None if grads is None else grads[i]
+            e.grad_type = e.param_type
+            if g is not None:
+                e.grad, e.grad_type = _entry(g, p, "grads", i), DTYPE[_NAMES[g.dtype]]
+            e.wd_scale = 1.0 if wd_scale is None else wd_scale[i]
+            e.update_scale = max(1.0, e.rows / max(1, e.cols)) ** 0.5 if update_scale is None else update_scale[i]
+        if n:
+            _on_current(device, "the matrices are")
+        cfg = QsrMuonConfig(n_matrices=n, workers=int(workers), products=int(products), iterations=int(iterations), nesterov=int(bool(nesterov)),
+                            beta=beta, eps=eps, weight_decay=weight_decay)
+        nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
+        self._params, self._grad_types = list(params), [entries[i].grad_type for i in range(n)]
+        self._keep = [None if x is None else list(x) for x in (momentum, copies)] + [workspace]
+        self._grads, self._stream = None if grads is None else list(grads), int(stream)
+        _check(lib().qsr_muon_create(C.byref(self._h), C.byref(cfg), entries, _dptr(workspace), nbytes, C.c_void_p(stream)), "qsr_muon_create")
+
+    def close(self) -> None:
+        if self._h:
+            lib().qsr_muon_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def qsr_muon_set_grads(self, grads) -> None:
+        """New gradient tensors (one per matrix, of the types the list was made with)."""
+        if len(grads) != len(self._params):
+            raise ValueError(f"{len(grads)} gradients for {len(self._params)} matrices")
+        only = {v: {k: 0} for k, v in DTYPE.items()}
+        table = (C.c_void_p * max(1, len(grads)))()
+        for i, (g, p) in enumerate(zip(grads, self._params)):
+            table[i] = _entry(g, p, "grads", i, only[self._grad_types[i]])
+        _check(lib().qsr_muon_set_grads(self._h, table), "qsr_muon_set_grads")
+        if self._grads is not None:
+            _in_use(self._grads, self._stream, self._params[0].device)
+        self._grads = list(grads)
+
+    def qsr_muon_step(self, lr: float, grad_scale: float = 1.0) -> None:
+        _check(lib().qsr_muon_step(self._h, lr, grad_scale), "qsr_muon_step")
+
+    def qsr_muon_sync(self, state_sync: str = "keep") -> None:
+        _check(lib().qsr_muon_sync(self._h, STATE[state_sync]), "qsr_muon_sync")
+
+    def qsr_muon_check(self) -> None:
+        """Waits for the stream; raises if a wait inside an earlier step ran out."""
+        _check(lib().qsr_muon_check(self._h), "qsr_muon_check")
+
+    def qsr_muon_launch_count(self) -> int:
+        return int(lib().qsr_muon_launch_count(self._h))
 
 
 # ---- layer norm and embedding ---------------------------------------------------------------------------

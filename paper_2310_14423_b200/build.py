@@ -12,7 +12,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqsr.so")
-SOURCES = ["schedule.cpp", "kernels.cu", "api.cu", "lists.cu", "lists_api.cu", "logprobs.cu", "layernorm.cu", "embed.cu"]
+SOURCES = ["schedule.cpp", "kernels.cu", "api.cu", "lists.cu", "lists_api.cu", "logprobs.cu", "layernorm.cu", "embed.cu", "muon.cu", "muon_api.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "checks.h", "wide.cuh", "rows.cuh")] + [os.path.join(os.path.dirname(HERE), "include", "qsr.h")]
 
 

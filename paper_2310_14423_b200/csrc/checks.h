@@ -4,7 +4,9 @@
 
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
+#include <vector>
 
 #include "../../include/qsr.h"
 
@@ -48,6 +50,43 @@ inline int launch_status(int err)
     if (err == 0) return QSR_OK;
     cudaGetLastError();
     return QSR_ECUDA;
+}
+
+struct Range { uintptr_t begin, end; bool written; };
+
+// Two ranges that share a byte, one of them written.
+inline bool overlap(std::vector<Range> &r)
+{
+    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    uintptr_t end_any = 0, end_written = 0;
+    for (const Range &x : r) {
+        if (x.begin < end_written || (x.written && x.begin < end_any)) return true;
+        end_any = std::max(end_any, x.end);
+        if (x.written) end_written = std::max(end_written, x.end);
+    }
+    return false;
+}
+
+// Enqueues a copy from pageable host memory: such a copy is staged before the call returns, so the source may be freed.  A copy from
+// page-locked memory would read it whenever the stream gets there.
+inline cudaError_t upload(void *dst, const void *src, size_t bytes, cudaStream_t st)
+{
+    return bytes ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaSuccess;
+}
+
+// QSR_ESTATE during a capture: a captured copy from pageable memory would read it at every replay.  The legacy default stream
+// takes no work while a blocking stream is being captured; the query says so with an error of its own, and an attempt would
+// invalidate that capture.
+inline int not_capturing(cudaStream_t st)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    const cudaError_t err = cudaStreamIsCapturing(st, &status);
+    if (err == cudaErrorStreamCaptureImplicit) {
+        cudaGetLastError();
+        return QSR_ESTATE;
+    }
+    if (err != cudaSuccess) return launch_status(int(err));
+    return status == cudaStreamCaptureStatusNone ? QSR_OK : QSR_ESTATE;
 }
 
 }  // namespace qsr

@@ -184,6 +184,43 @@ int launch_list_reset(const ListSyncParams &p, bool states8, int64_t chunks, voi
 // Raises a kernel's limit of dynamic shared memory, once per device (`raised`: a bit for each of the first 64 devices).
 int allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &raised);
 
+// ---- matrices stepped by their orthogonalised momentum (muon.cu, muon_api.cu) ----
+
+struct MuonMatrix {           // one matrix, in the device table; m <= n are its sides
+    void *param, *copy;
+    float *momentum;
+    int64_t rows, cols;
+    uint16_t *x[2];           // fp16 blocks of 64 x 64: the iterate of m x n (column of blocks by column), before and after a product
+    uint16_t *gram, *factor;  // the same of m x m
+    int32_t m, n, mb, nb;     // mb, nb: blocks along m and n
+    int32_t tall;             // rows > cols: the iterate is the transpose
+    int32_t param_type, copy_type, grad_type;
+    float wd_scale, update_scale;
+    float scale;              // power of two that the iterate is held at
+    int32_t first_chunk, chunks;
+};
+struct MuonTile { int32_t matrix, i, j, pad; };      // 128 x 256 elements of a product: 128-row tile i, 256-column tile j
+struct MuonBlock { int32_t matrix, p, q, pad; };     // a block of 64 x 64
+struct MuonChunk { int32_t matrix, n; int64_t offset; };   // n consecutive elements
+struct MuonParams {
+    const MuonMatrix *matrices;
+    const void *const *grads;
+    const MuonChunk *chunks;
+    const MuonBlock *blocks;
+    double *partial;          // [chunks]: sums of squares
+    float *factor;            // [matrices]: scale / (norm + eps)
+    unsigned *arrived;        // [matrices], zero between launches
+    unsigned *late;           // set where a wait ran out
+    float one_minus_beta, beta, grad_scale, eps;
+    float lr, lr_decay;
+    int32_t nesterov, products, iterations;
+};
+int launch_muon_clear(const MuonParams &p, int64_t chunks, void *stream);      // momentum <- 0
+int launch_muon_momentum(const MuonParams &p, int64_t chunks, void *stream);
+int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream);
+// One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate, 3 last iterate and update of the parameters.
+int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
+
 // ---- log probabilities of given tokens (logprobs.cu) ----
 
 struct LogprobParams {

@@ -8,6 +8,7 @@
 #include <new>
 #include <vector>
 
+#include "checks.h"
 #include "internal.h"
 
 struct qsr_list {
@@ -28,18 +29,11 @@ struct qsr_list {
 
 namespace {
 
+using namespace qsr;
+
 constexpr int64_t kBlock = 256;            // elements that share a scale in 8 bits: chunks are whole blocks
 
-int cuda_rc(cudaError_t err)
-{
-    if (err == cudaSuccess) return QSR_OK;
-    cudaGetLastError();
-    return QSR_ECUDA;
-}
-
-int element_bytes(int type) { return type == QSR_F32 ? 4 : type == QSR_BF16 || type == QSR_F16 ? 2 : 0; }
-bool known(int type) { return element_bytes(type) != 0; }
-bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+bool known(int type) { return type_bytes(type) != 0; }
 
 constexpr int64_t kWarpBlocks = qsr::kListWarps * kBlock;      // elements of a thread block with one block per warp
 
@@ -84,27 +78,12 @@ Layout layout_of(const int64_t *numel, int32_t n, int32_t workers, int stages)
     return l;
 }
 
-struct Range { uintptr_t begin, end; bool written; };
-
-// Two ranges that share a byte, one of them written.
-bool overlap(std::vector<Range> &r)
-{
-    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.begin < b.begin; });
-    uintptr_t end_any = 0, end_written = 0;
-    for (const Range &x : r) {
-        if (x.begin < end_written || (x.written && x.begin < end_any)) return true;
-        end_any = std::max(end_any, x.end);
-        if (x.written) end_written = std::max(end_written, x.end);
-    }
-    return false;
-}
-
 int check_grads(const qsr_list_config &c, const qsr_tensor *t, const void *const *grads)
 {
     for (int32_t i = 0; i < c.n_tensors; ++i) {
         if (t[i].numel == 0) continue;
         if (!grads[i]) return QSR_EINVAL;
-        if (!aligned(grads[i], unsigned(element_bytes(t[i].grad_type)))) return QSR_EALIGN;
+        if (!aligned_to(grads[i], unsigned(type_bytes(t[i].grad_type)))) return QSR_EALIGN;
     }
     return QSR_OK;
 }
@@ -117,7 +96,7 @@ int check_list(const qsr_list_config &c, const qsr_tensor *t)
     if (c.states != QSR_STATES_F32 && c.states != QSR_STATES_E4M3) return QSR_EINVAL;
     if (!unit_interval(c.beta1) || !unit_interval(c.beta2) || !std::isfinite(c.eps) || c.eps < 0.0 || !std::isfinite(c.weight_decay))
         return QSR_EINVAL;
-    if (!aligned(c.grad_norm, 4)) return QSR_EALIGN;
+    if (!aligned_to(c.grad_norm, 4)) return QSR_EALIGN;
     const bool codes = c.states == QSR_STATES_E4M3;
     const int32_t per = c.n_tensors / c.workers;
     for (int32_t i = 0; i < c.n_tensors; ++i) {
@@ -128,35 +107,13 @@ int check_list(const qsr_list_config &c, const qsr_tensor *t)
         if (x.numel != first.numel || x.param_type != first.param_type || x.copy_type != first.copy_type) return QSR_EINVAL;
         if (x.numel == 0) continue;
         if (!x.param || !x.m || !x.v || (codes && (!x.m_scale || !x.v_scale)) || (x.copy_type != QSR_NONE && !x.copy)) return QSR_EINVAL;
-        if (!aligned(x.param, unsigned(element_bytes(x.param_type))) || (!codes && (!aligned(x.m, 4) || !aligned(x.v, 4))) ||
-            (codes && (!aligned(x.m_scale, 4) || !aligned(x.v_scale, 4))) ||
-            (x.copy_type != QSR_NONE && !aligned(x.copy, unsigned(element_bytes(x.copy_type)))) ||
-            !aligned(x.grad, unsigned(element_bytes(x.grad_type))))
+        if (!aligned_to(x.param, unsigned(type_bytes(x.param_type))) || (!codes && (!aligned_to(x.m, 4) || !aligned_to(x.v, 4))) ||
+            (codes && (!aligned_to(x.m_scale, 4) || !aligned_to(x.v_scale, 4))) ||
+            (x.copy_type != QSR_NONE && !aligned_to(x.copy, unsigned(type_bytes(x.copy_type)))) ||
+            !aligned_to(x.grad, unsigned(type_bytes(x.grad_type))))
             return QSR_EALIGN;
     }
     return QSR_OK;
-}
-
-// Enqueues a copy from pageable host memory: such a copy is staged before the call returns, so the source may be freed.  A copy from
-// page-locked memory would read it whenever the stream gets there.
-cudaError_t upload(void *dst, const void *src, size_t bytes, cudaStream_t st)
-{
-    return bytes ? cudaMemcpyAsync(dst, src, bytes, cudaMemcpyHostToDevice, st) : cudaSuccess;
-}
-
-// QSR_ESTATE during a capture: a captured copy from pageable memory would read it at every replay.  The legacy default stream
-// takes no work while a blocking stream is being captured; the query says so with an error of its own, and an attempt would
-// invalidate that capture.
-int not_capturing(cudaStream_t st)
-{
-    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-    const cudaError_t err = cudaStreamIsCapturing(st, &status);
-    if (err == cudaErrorStreamCaptureImplicit) {
-        cudaGetLastError();
-        return QSR_ESTATE;
-    }
-    if (err != cudaSuccess) return cuda_rc(err);
-    return status == cudaStreamCaptureStatusNone ? QSR_OK : QSR_ESTATE;
 }
 
 bool on_own_device(const qsr_list &x)
@@ -174,12 +131,12 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     qsr::ListShape shape{0, 0, 0, t[0].param_type, t[0].grad_type};
     for (int32_t i = 0; i < n; ++i) {
         if (t[i].param_type != t[0].param_type || t[i].grad_type != t[0].grad_type) shape.param_type = shape.grad_type = QSR_NONE;
-        if (codes) shape.stage_bytes = std::max(shape.stage_bytes, int(kBlock) * (element_bytes(t[i].param_type) + element_bytes(t[i].grad_type) + 2));
+        if (codes) shape.stage_bytes = std::max(shape.stage_bytes, int(kBlock) * (type_bytes(t[i].param_type) + type_bytes(t[i].grad_type) + 2));
     }
     shape.stages = stages_of(shape.stage_bytes);
     const Layout l = layout_of(numel.data(), n, cfg.workers, shape.stages);
     if (l.n_chunks < 0) return int(l.n_chunks);
-    if (!aligned(workspace, 256)) return QSR_EALIGN;
+    if (!aligned_to(workspace, 256)) return QSR_EALIGN;
     if (workspace_bytes < l.bytes) return QSR_ERANGE;
 
     shape.chunks = l.n_chunks;
@@ -193,15 +150,15 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     for (int32_t i = 0; i < n; ++i) {
         const qsr_tensor &x = t[i];
         const int64_t scales = (x.numel + kBlock - 1) / kBlock * 4, state = x.numel * (codes ? 1 : 4);
-        add(x.param, x.numel * element_bytes(x.param_type), true);
-        if (x.copy_type != QSR_NONE) add(x.copy, x.numel * element_bytes(x.copy_type), true);
+        add(x.param, x.numel * type_bytes(x.param_type), true);
+        if (x.copy_type != QSR_NONE) add(x.copy, x.numel * type_bytes(x.copy_type), true);
         add(x.m, state, true);
         add(x.v, state, true);
         if (codes) {
             add(x.m_scale, scales, true);
             add(x.v_scale, scales, true);
         }
-        add(x.grad, x.numel * element_bytes(x.grad_type), false);
+        add(x.grad, x.numel * type_bytes(x.grad_type), false);
         has_grads = has_grads && (x.grad || x.numel == 0);
     }
     add(workspace, l.bytes, true);
@@ -252,7 +209,7 @@ int create(qsr_list **out, const qsr_list_config &cfg, const qsr_tensor *t, void
     if (err == cudaSuccess) err = cudaMemsetAsync(x->arrived, 0, size_t(cfg.workers) * sizeof(unsigned), x->stream);
     if (err != cudaSuccess) {
         delete x;
-        return cuda_rc(err);
+        return launch_status(err);
     }
     *out = x;
     return QSR_OK;
@@ -297,7 +254,7 @@ int qsr_list_set_grads(qsr_list *list, const void *const *grads_host)
     if (int rc = not_capturing(list->stream)) return rc;
     try {              // a copy of the caller's array, which may be page-locked: see upload
         const std::vector<const void *> table(grads_host, grads_host + list->cfg.n_tensors);
-        const int rc = cuda_rc(upload(list->grads, table.data(), table.size() * sizeof(void *), list->stream));
+        const int rc = launch_status(upload(list->grads, table.data(), table.size() * sizeof(void *), list->stream));
         list->has_grads = rc == QSR_OK;
         return rc;
     } catch (...) {    // out of host memory
@@ -334,11 +291,11 @@ int qsr_list_step(qsr_list *list, int64_t n, double lr, double grad_scale)
         q.chunks_per_worker = int32_t(list->chunks_per_worker);
         q.max_norm = float(c.clip_norm); q.grad_scale = p.grad_scale;
         list->launches++;
-        if (int err = qsr::launch_list_norm(q, list->chunks, list->stream)) return cuda_rc(cudaError_t(err));
+        if (int err = qsr::launch_list_norm(q, list->chunks, list->stream)) return launch_status(err);
         p.clip = list->clip;
     }
     list->launches++;
-    return cuda_rc(cudaError_t(qsr::launch_list_step(p, list->shape, list->stream)));
+    return launch_status(qsr::launch_list_step(p, list->shape, list->stream));
 }
 
 int qsr_list_sync(qsr_list *list, int32_t state_sync)
@@ -355,10 +312,10 @@ int qsr_list_sync(qsr_list *list, int32_t state_sync)
     const bool codes = c.states == QSR_STATES_E4M3;
     list->launches++;
     if (int err = qsr::launch_list_sync(p, codes, state_sync == QSR_STATE_AVERAGE, list->chunks_per_worker, list->stream))
-        return cuda_rc(cudaError_t(err));
+        return launch_status(err);
     if (state_sync != QSR_STATE_RESET) return QSR_OK;
     list->launches++;
-    return cuda_rc(cudaError_t(qsr::launch_list_reset(p, codes, list->chunks, list->stream)));
+    return launch_status(qsr::launch_list_reset(p, codes, list->chunks, list->stream));
 }
 
 int64_t qsr_list_launch_count(const qsr_list *list) { return list ? list->launches : int64_t(QSR_EINVAL); }

@@ -1,0 +1,409 @@
+// C ABI of the matrices stepped by their orthogonalised momentum: checks, device tables, launches.  See include/qsr.h.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <numeric>
+#include <vector>
+
+#include "checks.h"
+#include "internal.h"
+
+struct qsr_muon {
+    qsr_muon_config cfg;
+    cudaStream_t stream;
+    int device, multiprocessors;
+    qsr::MuonParams params;                     // tables; the step's numbers are filled in by each call
+    const void **grads;
+    const qsr::MuonTile *half, *whole;          // tiles of a symmetric result, and of the iterate
+    const qsr::ListTensor *sync_tensors;
+    const qsr::ListChunk *sync_chunks;
+    int64_t chunks, blocks, n_half, n_whole, param_sync_chunks, all_sync_chunks;
+    std::vector<qsr_matrix> host;
+    bool has_grads;
+    int64_t launches;
+};
+
+namespace {
+
+using namespace qsr;
+
+constexpr int64_t kChunk = 16384;                                  // elements that a block adds to the momentum
+constexpr int64_t kSyncChunk = int64_t(kListWarps) * 256 * kListStages;
+constexpr int64_t kMaxSide = int64_t(1) << 20, kMaxShortSide = 32768;
+constexpr int64_t kBlockBytes = 64 * 64 * 2;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Sides { int64_t m, n, mb, nb; };
+Sides sides_of(int64_t rows, int64_t cols)
+{
+    const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
+    return Sides{m, n, ceil_div(m, 64), ceil_div(n, 64)};
+}
+int64_t half_tiles(const Sides &s)              // 128 x 256 tiles of an m x m matrix that reach the diagonal's tiles or lie above
+{
+    int64_t count = 0;
+    for (int64_t j = 0; j * 4 < s.mb; ++j) count += std::min(ceil_div(s.mb, 2), 2 * j + 2);
+    return count;
+}
+int64_t whole_tiles(const Sides &s) { return ceil_div(s.mb, 2) * ceil_div(s.nb, 4); }
+
+struct Layout {
+    int64_t matrices, grads, chunks, blocks, half, whole, sync_tensors, sync_chunks, partial, factor, arrived, late, data, bytes;
+    int64_t n_chunks, n_blocks, n_half, n_whole, n_sync, n_param_sync;
+    int status;
+};
+
+// Where everything lies in the workspace, from the matrices' sizes.
+Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t workers, int32_t products)
+{
+    Layout l;
+    std::memset(&l, 0, sizeof l);
+    int64_t data = 0;
+    const int64_t parts = products == 3 ? 2 : 1;
+    for (int32_t i = 0; i < n; ++i) {
+        if (rows[i] < 0 || cols[i] < 0) { l.status = QSR_EINVAL; return l; }
+        if (rows[i] > kMaxSide || cols[i] > kMaxSide || std::min(rows[i], cols[i]) > kMaxShortSide) { l.status = QSR_ERANGE; return l; }
+        const int64_t size = rows[i] * cols[i];
+        if (size == 0) continue;
+        const Sides s = sides_of(rows[i], cols[i]);
+        l.n_chunks += ceil_div(size, kChunk);
+        l.n_blocks += s.mb * s.nb;
+        l.n_half += half_tiles(s);
+        l.n_whole += whole_tiles(s);
+        if (i < n / workers) l.n_param_sync += ceil_div(size, kSyncChunk);
+        data += (2 * s.mb * s.nb + 2 * s.mb * s.mb) * parts * kBlockBytes;
+    }
+    l.n_sync = 2 * l.n_param_sync;
+    if (l.n_chunks > 0x7fffffff || l.n_blocks > 0x7fffffff || l.n_whole > 0x7fffffff || l.n_half > 0x7fffffff) { l.status = QSR_ERANGE; return l; }
+    int64_t at = 0;
+    auto take = [&at](int64_t bytes) { const int64_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    l.matrices = take(int64_t(n) * int64_t(sizeof(MuonMatrix)));
+    l.grads = take(int64_t(n) * int64_t(sizeof(void *)));
+    l.chunks = take(l.n_chunks * int64_t(sizeof(MuonChunk)));
+    l.blocks = take(l.n_blocks * int64_t(sizeof(MuonBlock)));
+    l.half = take(l.n_half * int64_t(sizeof(MuonTile)));
+    l.whole = take(l.n_whole * int64_t(sizeof(MuonTile)));
+    l.sync_tensors = take(2 * int64_t(n) * int64_t(sizeof(ListTensor)));
+    l.sync_chunks = take(l.n_sync * int64_t(sizeof(ListChunk)));
+    l.partial = take(l.n_chunks * int64_t(sizeof(double)));
+    l.factor = take(int64_t(n) * int64_t(sizeof(float)));
+    l.arrived = take(int64_t(n) * int64_t(sizeof(unsigned)));
+    l.late = take(int64_t(sizeof(unsigned)));
+    l.data = take(data);
+    l.bytes = std::max<int64_t>(at, 256);
+    return l;
+}
+
+bool products_known(int32_t products) { return products == 1 || products == 3; }
+
+int check_config(const qsr_muon_config &c)
+{
+    if (c.n_matrices < 1 || c.workers < 1 || c.n_matrices % c.workers != 0 || c.reserved != 0) return QSR_EINVAL;
+    if (!products_known(c.products) || (c.nesterov != 0 && c.nesterov != 1)) return QSR_EINVAL;
+    if (c.iterations < 1 || c.iterations > QSR_MUON_MAX_ITERATIONS) return QSR_ERANGE;
+    if (!std::isfinite(c.beta) || c.beta < 0.0 || c.beta >= 1.0 || !std::isfinite(c.eps) || c.eps < 0.0 || !std::isfinite(c.weight_decay)) return QSR_EINVAL;
+    return QSR_OK;
+}
+
+int check_matrices(const qsr_muon_config &c, const qsr_matrix *t)
+{
+    const int32_t per = c.n_matrices / c.workers;
+    for (int32_t i = 0; i < c.n_matrices; ++i) {
+        const qsr_matrix &x = t[i], &first = t[i % per];
+        if (x.rows < 0 || x.cols < 0 || !type_bytes(x.param_type) || !type_bytes(x.grad_type) || (x.copy_type != QSR_NONE && !type_bytes(x.copy_type)) ||
+            !std::isfinite(x.wd_scale) || !std::isfinite(x.update_scale) || x.reserved != 0)
+            return QSR_EINVAL;
+        if (x.rows != first.rows || x.cols != first.cols || x.param_type != first.param_type || x.copy_type != first.copy_type) return QSR_EINVAL;
+        if (x.rows == 0 || x.cols == 0) continue;
+        if (!x.param || !x.momentum || (x.copy_type != QSR_NONE && !x.copy)) return QSR_EINVAL;
+        if (!aligned_to(x.param, unsigned(type_bytes(x.param_type))) || !aligned_to(x.momentum, 4) || !aligned_to(x.grad, unsigned(type_bytes(x.grad_type))) ||
+            (x.copy_type != QSR_NONE && !aligned_to(x.copy, unsigned(type_bytes(x.copy_type)))))
+            return QSR_EALIGN;
+    }
+    return QSR_OK;
+}
+
+int check_grads(const qsr_muon &x, const void *const *grads)
+{
+    for (size_t i = 0; i < x.host.size(); ++i) {
+        if (x.host[i].rows == 0 || x.host[i].cols == 0) continue;
+        if (!grads[i]) return QSR_EINVAL;
+        if (!aligned_to(grads[i], unsigned(type_bytes(x.host[i].grad_type)))) return QSR_EALIGN;
+    }
+    return QSR_OK;
+}
+
+bool on_own_device(const qsr_muon &x)
+{
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == x.device;
+}
+
+int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    const int32_t n = cfg.n_matrices, per = n / cfg.workers;
+    std::vector<int64_t> rows(static_cast<size_t>(n)), cols(static_cast<size_t>(n));
+    for (int32_t i = 0; i < n; ++i) { rows[size_t(i)] = t[i].rows; cols[size_t(i)] = t[i].cols; }
+    const Layout l = layout_of(rows.data(), cols.data(), n, cfg.workers, cfg.products);
+    if (l.status) return l.status;
+    if (!aligned_to(workspace, 256)) return QSR_EALIGN;
+    if (workspace_bytes < l.bytes) return QSR_ERANGE;
+
+    std::vector<Range> ranges;
+    auto add = [&ranges](const void *p, int64_t bytes, bool written) {
+        const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes > 0) ranges.push_back(Range{b, b + uintptr_t(bytes), written});
+    };
+    bool has_grads = true;
+    for (int32_t i = 0; i < n; ++i) {
+        const int64_t size = t[i].rows * t[i].cols;
+        add(t[i].param, size * type_bytes(t[i].param_type), true);
+        if (t[i].copy_type != QSR_NONE) add(t[i].copy, size * type_bytes(t[i].copy_type), true);
+        add(t[i].momentum, size * 4, true);
+        add(t[i].grad, size * type_bytes(t[i].grad_type), false);
+        has_grads = has_grads && (t[i].grad || size == 0);
+    }
+    add(workspace, l.bytes, true);
+    if (overlap(ranges)) return QSR_EINVAL;
+
+    char *ws = static_cast<char *>(workspace);
+    std::vector<MuonMatrix> matrices(static_cast<size_t>(n));
+    std::vector<const void *> grads(static_cast<size_t>(n));
+    std::vector<MuonChunk> chunks;
+    std::vector<MuonBlock> blocks;
+    std::vector<MuonTile> half, whole;
+    std::vector<ListTensor> sync_tensors(size_t(n) * 2);
+    std::vector<ListChunk> sync_chunks;
+    chunks.reserve(size_t(l.n_chunks));
+    blocks.reserve(size_t(l.n_blocks));
+    half.reserve(size_t(l.n_half));
+    whole.reserve(size_t(l.n_whole));
+    sync_chunks.reserve(size_t(l.n_sync));
+    const int64_t parts = cfg.products == 3 ? 2 : 1;
+    char *at = ws + l.data;
+    auto take = [&at, parts](int64_t count) {
+        uint16_t *here = reinterpret_cast<uint16_t *>(at);
+        at += count * parts * kBlockBytes;
+        return here;
+    };
+    for (int32_t i = 0; i < n; ++i) {
+        const qsr_matrix &x = t[i];
+        MuonMatrix &y = matrices[size_t(i)];
+        std::memset(&y, 0, sizeof y);
+        grads[size_t(i)] = x.grad;
+        const int32_t k = i / per, j = i % per;          // worker by worker: its parameters, then its momenta
+        sync_tensors[size_t(2 * k * per + j)] = ListTensor{x.param, x.copy, nullptr, nullptr, nullptr, nullptr, x.rows * x.cols, x.param_type, QSR_NONE, x.copy_type, 0.0f};
+        sync_tensors[size_t((2 * k + 1) * per + j)] = ListTensor{x.momentum, nullptr, nullptr, nullptr, nullptr, nullptr, x.rows * x.cols, QSR_F32, QSR_NONE, QSR_NONE, 0.0f};
+        if (x.rows == 0 || x.cols == 0) continue;
+        const Sides s = sides_of(x.rows, x.cols);
+        y.param = x.param; y.copy = x.copy; y.momentum = x.momentum;
+        y.rows = x.rows; y.cols = x.cols;
+        y.m = int32_t(s.m); y.n = int32_t(s.n); y.mb = int32_t(s.mb); y.nb = int32_t(s.nb);
+        y.tall = x.rows > x.cols;
+        y.param_type = x.param_type; y.copy_type = x.copy_type; y.grad_type = x.grad_type;
+        y.wd_scale = x.wd_scale; y.update_scale = x.update_scale;
+        // entries of the iterate have a root mean square of about one where it is sqrt(m n); fp16 holds up to 65504
+        y.scale = float(std::ldexp(1.0, std::min(15, int(std::floor(0.5 * std::log2(double(s.m) * double(s.n)))))));
+        y.x[0] = take(s.mb * s.nb);
+        y.x[1] = take(s.mb * s.nb);
+        y.gram = take(s.mb * s.mb);
+        y.factor = take(s.mb * s.mb);
+        y.first_chunk = int32_t(chunks.size());
+        for (int64_t o = 0; o < x.rows * x.cols; o += kChunk) chunks.push_back(MuonChunk{i, int32_t(std::min(kChunk, x.rows * x.cols - o)), o});
+        y.chunks = int32_t(chunks.size()) - y.first_chunk;
+        // in the order of the matrix's own rows
+        for (int64_t a = 0; a < (y.tall ? s.nb : s.mb); ++a)
+            for (int64_t b = 0; b < (y.tall ? s.mb : s.nb); ++b) blocks.push_back(MuonBlock{i, int32_t(y.tall ? b : a), int32_t(y.tall ? a : b), 0});
+    }
+    for (int part = 0; part < 2; ++part)
+        for (int32_t j = 0; j < per; ++j)
+            for (int64_t o = 0; o < t[j].rows * t[j].cols; o += kSyncChunk)
+                sync_chunks.push_back(ListChunk{part * per + j, int32_t(std::min(kSyncChunk, t[j].rows * t[j].cols - o)), o});
+    // long products first, so that short ones fill the end
+    std::vector<int32_t> order(static_cast<size_t>(n));
+    std::iota(order.begin(), order.end(), 0);
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].nb > matrices[size_t(b)].nb; });
+    for (int32_t i : order) {
+        const MuonMatrix &y = matrices[size_t(i)];
+        for (int32_t j = 0; j * 4 < y.mb; ++j)
+            for (int32_t r = 0; r < std::min((y.mb + 1) / 2, 2 * j + 2); ++r) half.push_back(MuonTile{i, r, j, 0});
+    }
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].mb > matrices[size_t(b)].mb; });
+    for (int32_t i : order) {
+        const MuonMatrix &y = matrices[size_t(i)];
+        for (int32_t j = 0; j * 4 < y.nb; ++j)
+            for (int32_t r = 0; r * 2 < y.mb; ++r) whole.push_back(MuonTile{i, r, j, 0});
+    }
+    if (int64_t(half.size()) != l.n_half || int64_t(whole.size()) != l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
+        int64_t(sync_chunks.size()) != l.n_sync || at > ws + l.bytes)
+        return QSR_EINVAL;                               // the tables do not fit what was reserved for them
+
+    int dev = 0, multiprocessors = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&multiprocessors, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return QSR_ECUDA;
+    }
+    const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (int rc = not_capturing(st)) return rc;
+    qsr_muon *x = new qsr_muon;
+    try {
+        x->host.assign(t, t + n);
+    } catch (...) {
+        delete x;
+        throw;
+    }
+    x->cfg = cfg;
+    x->stream = st;
+    x->device = dev;
+    x->multiprocessors = multiprocessors;
+    x->grads = reinterpret_cast<const void **>(ws + l.grads);
+    x->half = reinterpret_cast<const MuonTile *>(ws + l.half);
+    x->whole = reinterpret_cast<const MuonTile *>(ws + l.whole);
+    x->sync_tensors = reinterpret_cast<const ListTensor *>(ws + l.sync_tensors);
+    x->sync_chunks = reinterpret_cast<const ListChunk *>(ws + l.sync_chunks);
+    x->chunks = l.n_chunks; x->blocks = l.n_blocks; x->n_half = l.n_half; x->n_whole = l.n_whole;
+    x->param_sync_chunks = l.n_param_sync; x->all_sync_chunks = l.n_sync;
+    x->has_grads = has_grads;
+    x->launches = 0;
+    MuonParams &p = x->params;
+    std::memset(&p, 0, sizeof p);
+    p.matrices = reinterpret_cast<const MuonMatrix *>(ws + l.matrices);
+    p.grads = x->grads;
+    p.chunks = reinterpret_cast<const MuonChunk *>(ws + l.chunks);
+    p.blocks = reinterpret_cast<const MuonBlock *>(ws + l.blocks);
+    p.partial = reinterpret_cast<double *>(ws + l.partial);
+    p.factor = reinterpret_cast<float *>(ws + l.factor);
+    p.arrived = reinterpret_cast<unsigned *>(ws + l.arrived);
+    p.late = reinterpret_cast<unsigned *>(ws + l.late);
+    p.one_minus_beta = float(1.0 - cfg.beta);
+    p.beta = float(cfg.beta);
+    p.eps = float(cfg.eps);
+    p.nesterov = cfg.nesterov; p.products = cfg.products; p.iterations = cfg.iterations;
+    cudaError_t err = upload(ws + l.matrices, matrices.data(), matrices.size() * sizeof(MuonMatrix), st);
+    if (err == cudaSuccess) err = upload(ws + l.grads, grads.data(), grads.size() * sizeof(void *), st);
+    if (err == cudaSuccess) err = upload(ws + l.chunks, chunks.data(), chunks.size() * sizeof(MuonChunk), st);
+    if (err == cudaSuccess) err = upload(ws + l.blocks, blocks.data(), blocks.size() * sizeof(MuonBlock), st);
+    if (err == cudaSuccess) err = upload(ws + l.half, half.data(), half.size() * sizeof(MuonTile), st);
+    if (err == cudaSuccess) err = upload(ws + l.whole, whole.data(), whole.size() * sizeof(MuonTile), st);
+    if (err == cudaSuccess) err = upload(ws + l.sync_tensors, sync_tensors.data(), sync_tensors.size() * sizeof(ListTensor), st);
+    if (err == cudaSuccess) err = upload(ws + l.sync_chunks, sync_chunks.data(), sync_chunks.size() * sizeof(ListChunk), st);
+    if (err == cudaSuccess) err = cudaMemsetAsync(p.arrived, 0, size_t(n) * sizeof(unsigned), st);
+    if (err == cudaSuccess) err = cudaMemsetAsync(p.late, 0, sizeof(unsigned), st);
+    if (err != cudaSuccess) {
+        delete x;
+        return launch_status(int(err));
+    }
+    *out = x;
+    return QSR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t qsr_muon_workspace_bytes(const int64_t *rows_host, const int64_t *cols_host, int32_t n_matrices, int32_t workers, int32_t products)
+{
+    if (!rows_host || !cols_host || n_matrices < 1 || workers < 1 || n_matrices % workers != 0 || !products_known(products)) return QSR_EINVAL;
+    const Layout l = layout_of(rows_host, cols_host, n_matrices, workers, products);
+    return l.status ? l.status : l.bytes;
+}
+
+int qsr_muon_create(qsr_muon **out, const qsr_muon_config *cfg, const qsr_matrix *matrices_host, void *workspace_dev, int64_t workspace_bytes,
+                    void *cuda_stream)
+{
+    if (!out) return QSR_EINVAL;
+    *out = nullptr;
+    if (!cfg || !matrices_host || !workspace_dev) return QSR_EINVAL;
+    if (int rc = check_config(*cfg)) return rc;
+    if (int rc = check_matrices(*cfg, matrices_host)) return rc;
+    try {
+        return create(out, *cfg, matrices_host, workspace_dev, workspace_bytes, cuda_stream);
+    } catch (...) {        // out of host memory
+        return QSR_EINVAL;
+    }
+}
+
+int qsr_muon_destroy(qsr_muon *muon)
+{
+    delete muon;
+    return QSR_OK;
+}
+
+int qsr_muon_set_grads(qsr_muon *muon, const void *const *grads_host)
+{
+    if (!muon || !grads_host) return QSR_EINVAL;
+    if (int rc = check_grads(*muon, grads_host)) return rc;
+    if (!on_own_device(*muon)) return QSR_ESTATE;
+    if (int rc = not_capturing(muon->stream)) return rc;
+    try {              // a copy of the caller's array, which may be page-locked: see upload
+        const std::vector<const void *> table(grads_host, grads_host + muon->cfg.n_matrices);
+        const int rc = launch_status(int(upload(muon->grads, table.data(), table.size() * sizeof(void *), muon->stream)));
+        muon->has_grads = rc == QSR_OK;
+        return rc;
+    } catch (...) {    // out of host memory
+        return QSR_EINVAL;
+    }
+}
+
+int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale)
+{
+    if (!muon || !std::isfinite(float(lr)) || !std::isfinite(float(grad_scale)) || !std::isfinite(float(lr * muon->cfg.weight_decay))) return QSR_EINVAL;
+    if (!muon->has_grads || !on_own_device(*muon)) return QSR_ESTATE;
+    if (muon->chunks == 0) return QSR_OK;
+    MuonParams p = muon->params;
+    p.grad_scale = float(grad_scale);
+    p.lr = float(lr);
+    p.lr_decay = float(lr * muon->cfg.weight_decay);
+    muon->launches++;
+    if (int err = launch_muon_momentum(p, muon->chunks, muon->stream)) return launch_status(err);
+    muon->launches++;
+    if (int err = launch_muon_pack(p, muon->blocks, muon->stream)) return launch_status(err);
+    for (int i = 0; i < muon->cfg.iterations; ++i)
+        for (int kind = 0; kind < 3; ++kind) {
+            const bool last = kind == 2 && i + 1 == muon->cfg.iterations;
+            muon->launches++;
+            if (int err = launch_muon_product(p, last ? 3 : kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
+                                              muon->multiprocessors, muon->stream))
+                return launch_status(err);
+        }
+    return QSR_OK;
+}
+
+int qsr_muon_sync(qsr_muon *muon, int32_t state_sync)
+{
+    if (!muon || state_sync < QSR_STATE_KEEP || state_sync > QSR_STATE_RESET) return QSR_EINVAL;
+    if (!on_own_device(*muon)) return QSR_ESTATE;
+    if (muon->chunks == 0) return QSR_OK;
+    const int32_t K = muon->cfg.workers;
+    ListSyncParams p;
+    p.tensors = muon->sync_tensors; p.chunks = muon->sync_chunks;
+    p.workers = K; p.tensors_per_worker = 2 * (muon->cfg.n_matrices / K);
+    p.divisor = float(K);
+    p.inverse = (K & (K - 1)) == 0 ? 1.0f / float(K) : 0.0f;
+    muon->launches++;
+    const int64_t chunks = state_sync == QSR_STATE_AVERAGE ? muon->all_sync_chunks : muon->param_sync_chunks;
+    if (int err = launch_list_sync(p, false, false, chunks, muon->stream)) return launch_status(err);
+    if (state_sync != QSR_STATE_RESET) return QSR_OK;
+    muon->launches++;
+    return launch_status(launch_muon_clear(muon->params, muon->chunks, muon->stream));
+}
+
+int qsr_muon_check(qsr_muon *muon)
+{
+    if (!muon) return QSR_EINVAL;
+    if (!on_own_device(*muon)) return QSR_ESTATE;
+    if (int rc = not_capturing(muon->stream)) return rc;
+    unsigned late = 0;
+    cudaError_t err = cudaMemcpyAsync(&late, muon->params.late, sizeof late, cudaMemcpyDeviceToHost, muon->stream);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(muon->stream);
+    if (err != cudaSuccess) return launch_status(int(err));
+    return late ? QSR_ECUDA : QSR_OK;
+}
+
+int64_t qsr_muon_launch_count(const qsr_muon *muon) { return muon ? muon->launches : int64_t(QSR_EINVAL); }
+
+}  // extern "C"

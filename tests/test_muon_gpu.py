@@ -1,0 +1,325 @@
+"""Steps by orthogonalised momentum on the GPU against the formulas in binary64, with a bound on the iteration's error that is
+carried along with the binary64 iterates.
+
+One iteration maps singular values by p(s) = a s + b s^3 + c s^5, and to first order a perturbation of an iterate grows at most by the
+largest of (p(s) - p(t)) / (s - t), (p(s) + p(t)) / (s + t) and p(s) / s over its singular values.  Added to it, in the 2-norm of all entries:
+the roundings of X, A and C where they are held (E relative to each entry), and those of the three products (G relative to the
+product of absolute values).  E = 2^-11 for fp16, 2^-22 for a sum of two, which also leaves out products of 2^-22; the tensor cores
+add 16 products and the accumulator at a time and may cut off the result, 2^-23 each: `sums` / 16 times with one product,
+at most 12 times with three before fp32 registers take over (2^-24 each)."""
+import math
+
+import pytest
+import torch
+
+from paper_2310_14423_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+T = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}
+a, b, c = 3.4445, -4.7750, 2.0315
+
+
+def growth(s):
+    """The largest divided difference of p over the singular values s."""
+    x, y = s[:, None], s[None, :]
+    even = x * x + x * y + y * y                                    # (x^3 - y^3) / (x - y)
+    fifth = x ** 4 + x ** 3 * y + x * x * y * y + x * y ** 3 + y ** 4
+    odd_even = x * x - x * y + y * y                                # (x^3 + y^3) / (x + y)
+    odd_fifth = x ** 4 - x ** 3 * y + x * x * y * y - x * y ** 3 + y ** 4
+    return max(float((a + b * even + c * fifth).abs().max()), float((a + b * odd_even + c * odd_fifth).abs().max()),
+               float((a + b * s ** 2 + c * s ** 4).abs().max()))
+
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def orthogonal64(u, iterations, eps, products):
+    """(X, bound on the 2-norm of the entries' error) for one matrix in binary64, rounded where X, A and C are held in fp16."""
+    X = u / (torch.linalg.vector_norm(u) + eps)
+    tall = X.shape[0] > X.shape[1]
+    X = X.T if tall else X
+    m, n = X.shape
+    # With one product the reference rounds where the kernels do, at the same powers of two.  What is left are entries that lie nearer to
+    # a boundary than the products' error G (below 2^-17 of them, 2^-7 of a step) and fall to its other side: one in 2^6, each a
+    # step off, which is 2^-3 of a step in the mean over many entries and up to a whole one over few.
+    e = 2.0 ** -11 * min(1.0, 0.25 + 4.0 / math.sqrt(m * n)) if products == 1 else 2.0 ** -22
+    scale = 2.0 ** min(15, math.floor(0.5 * math.log2(m * n)))
+    held = (lambda M, at: (M * at).half().double() / at) if products == 1 else (lambda M, at: M)
+    gamma = (lambda k: (k / 16 + 1) * 2.0 ** -23) if products == 1 else (lambda k: 12 * 2.0 ** -23 + (k / 64 + 2) * 2.0 ** -24 + 2.0 ** -22)
+    norm = lambda M: float(torch.linalg.vector_norm(M))                # noqa: E731
+    grain = 2.0 ** -25 * 2                                             # fp16's smallest step against entries of about one
+    X = held(X, scale)
+    err = e * norm(X) + 8 * U * norm(X) + grain
+    eye = torch.eye(m, device=DEV, dtype=torch.float64)
+    for _ in range(iterations):
+        A = held(X @ X.T, 2.0 ** 14)
+        singular = torch.linalg.eigvalsh(A).clamp_min(0.0).sqrt()
+        two = float(singular[-1]) * 1.01
+        d_A = e * norm(A) + gamma(n) * norm(X.abs() @ X.T.abs())
+        C = held(a * eye + b * A + c * A @ A, 2.0 ** 14)
+        d_C = (abs(b) + 2 * c * two * two) * d_A + c * gamma(m) * norm(A.abs() @ A.abs()) + 4 * U * norm(abs(b) * A.abs() + 4 * eye)
+        new = held(C @ X, scale) if _ + 1 < iterations else C @ X
+        local = d_C * two + (e + gamma(m)) * norm(C.abs() @ X.abs()) + e * norm(new) + grain
+        # the perturbation so far goes through this iteration; that of A and C is local
+        err = growth(singular) * err + local
+        X = new
+    return (X.T if tall else X), 1.05 * err
+
+
+class Case:
+    """K workers' matrices of the given shapes with their operands, and the list over them."""
+
+    def __init__(self, shapes, workers=1, param="f32", grad="bf16", copy=None, shift=0, seed=0, **kw):
+        g = gen(seed)
+        self.shapes, self.param, self.copy_kind, self.K = shapes, param, copy, workers
+
+        def make(kind, size):
+            out = []
+            for _ in range(workers):
+                for r, cc in shapes:
+                    flat = torch.empty(r * cc + shift, device=DEV, dtype=T[kind])
+                    out.append(flat[shift:].view(r, cc))
+                    out[-1].copy_(torch.randn(r, cc, device=DEV, generator=g) * size)
+            return out
+
+        self.p, self.g, self.m = make(param, 0.1), make(grad, 1e-3), make("f32", 1e-3)
+        self.c = [x.to(T[copy]) for x in self.p] if copy else None
+        self.kw = dict(beta=0.95, nesterov=True, weight_decay=0.1, eps=1e-7, iterations=5, products=1) | kw
+        self.scale = [1.0 + 0.5 * i for i in range(len(self.p))]
+        self.wd = [float(i % 2) for i in range(len(self.p))]
+        self.ws = torch.full((B.qsr_muon_workspace_bytes([x.shape for x in self.p], workers, self.kw["products"]),), 255, dtype=torch.uint8, device=DEV)
+        self.list = B.MuonList(self.p, self.g, self.m, copies=self.c, wd_scale=self.wd, update_scale=self.scale, workers=workers, workspace=self.ws,
+                               stream=stream(), **self.kw)
+
+    def step_and_compare(self, lr=0.02, grad_scale=1.0):
+        before = [(x.double(), g.float() * grad_scale, m.clone()) for x, g, m in zip(self.p, self.g, self.m)]
+        self.list.qsr_muon_step(lr, grad_scale)
+        self.list.qsr_muon_check()
+        kw = self.kw
+        beta = float(torch.tensor(kw["beta"], dtype=torch.float32))
+        omb = float(torch.tensor(1.0 - kw["beta"], dtype=torch.float32))
+        for i, (theta, g, m) in enumerate(before):
+            if theta.numel() == 0:
+                continue
+            g, m = g.double(), m.double()
+            want = m + omb * (g - m)
+            tol = 2 * U * ((g - m).abs() + want.abs()) + TINY["f32"]
+            assert not ((self.m[i].double() - want).abs() > tol).any()
+            held = self.m[i].double()                      # the direction is taken from the momentum as it is held
+            u = g + beta * (held - g) if kw["nesterov"] else held
+            X, err = orthogonal64(u, kw["iterations"], kw["eps"], kw["products"])
+            s = lr * self.scale[i]
+            new = theta - lr * kw["weight_decay"] * self.wd[i] * theta - s * X
+            kind = self.param
+            off = float(torch.linalg.vector_norm(self.p[i].double() - new))
+            bound = s * err * (1 + HALF_ULP[kind]) + (HALF_ULP[kind] + 4 * U) * float(torch.linalg.vector_norm(new.abs() + (s * X).abs())) + TINY[kind] * theta.numel()
+            assert off <= bound, (i, tuple(theta.shape), off / bound)
+            assert err < 0.5 * float(torch.linalg.vector_norm(X))      # the bound says something
+            if self.c is not None:
+                if kind == "f32":
+                    assert torch.equal(self.c[i], self.p[i].to(self.c[i].dtype))
+                ck = self.copy_kind
+                assert not ((self.c[i].double() - self.p[i].double()).abs() > (HALF_ULP[ck] + HALF_ULP[kind]) * 1.01 * new.abs().clamp_min(float(err * s)) + TINY[ck] * 2).any()
+
+
+SHAPES = [(1, 1), (1, 5), (7, 1), (2, 2), (1, 640), (63, 65), (64, 64), (65, 63), (128, 128), (100, 300), (300, 100), (129, 257), (256, 256), (257, 128),
+          (512, 260), (320, 700)]
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_one_matrix(shape, products):
+    Case([shape], products=products).step_and_compare()
+
+
+@pytest.mark.parametrize("param,grad,copy,products", [("f32", "bf16", "bf16", 3), ("f32", "f32", "f16", 1), ("bf16", "bf16", None, 1), ("f16", "f16", None, 1),
+                                                      ("bf16", "f32", "f32", 3), ("f32", "f16", None, 3)])
+def test_types_and_several_matrices(param, grad, copy, products):
+    x = Case([(70, 200), (200, 70), (0, 5), (64, 256), (256, 65)], workers=2, param=param, grad=grad, copy=copy, products=products)
+    x.step_and_compare()
+    x.step_and_compare(lr=0.01, grad_scale=0.5)
+    assert x.list.qsr_muon_launch_count() == 2 * 17
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape", [(768, 768), (768, 2304), (2304, 768), (1023, 2047), (1537, 77), (1300, 1100)])
+def test_larger_matrices(shape, products):
+    Case([shape], products=products, copy="bf16").step_and_compare()
+
+
+@pytest.mark.parametrize("kw", [dict(nesterov=False), dict(iterations=1), dict(iterations=2), dict(iterations=6), dict(beta=0.0), dict(weight_decay=0.0), dict(eps=0.0),
+                                dict(eps=1.0)])
+def test_settings(kw):
+    Case([(150, 90), (90, 150)], products=3, **kw).step_and_compare()
+
+
+@pytest.mark.parametrize("param,copy", [("f32", "bf16"), ("bf16", None)])
+@pytest.mark.parametrize("shift", [1, 3, 8])
+def test_unaligned(param, copy, shift):
+    x = Case([(96, 200), (201, 96), (33, 130)], param=param, copy=copy, shift=shift, products=3)
+    x.step_and_compare()
+
+
+def test_many_small_matrices():
+    Case([(5 + i % 40, 3 + 7 * i % 50) for i in range(300)], products=3).step_and_compare()
+
+
+@pytest.mark.parametrize("products", [1, 3])
+def test_low_rank_and_badly_scaled(products):
+    x = Case([(200, 300), (200, 300), (200, 300)], products=products, nesterov=False, beta=0.0, grad="f32")
+    x.g[0].copy_(torch.randn(200, 2, device=DEV, generator=gen(1)) @ torch.randn(2, 300, device=DEV, generator=gen(2)))
+    x.g[1].mul_(1e15)
+    x.g[2].zero_()
+    x.g[2][17, 200] = 1e-3            # a single element
+    x.step_and_compare()
+
+
+def test_zeros_have_no_update():
+    for eps in (1e-7, 0.0):
+        x = Case([(70, 90)], weight_decay=0.0, eps=eps)
+        x.g[0].zero_()
+        x.m[0].zero_()
+        before = x.p[0].clone()
+        x.list.qsr_muon_step(0.1)
+        assert torch.equal(x.p[0], before) and not x.m[0].any()
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_stay_in_their_matrix(value):
+    clean = Case([(70, 90), (130, 60), (64, 64)], products=3, grad="f32")
+    dirty = Case([(70, 90), (130, 60), (64, 64)], products=3, grad="f32")
+    dirty.g[1][100, 3] = value
+    for x in (clean, dirty):
+        x.list.qsr_muon_step(0.1)
+    assert torch.equal(clean.p[0], dirty.p[0]) and torch.equal(clean.p[2], dirty.p[2])
+    assert torch.isnan(dirty.p[1]).all()
+
+
+def test_the_same_bits_again():
+    runs = []
+    for _ in range(2):
+        x = Case([(300, 500), (77, 1000)], products=3, copy="bf16")
+        for _ in range(3):
+            x.list.qsr_muon_step(0.02)
+        runs.append(x)
+    for name in ("p", "m", "c"):
+        assert all(torch.equal(s, t) for s, t in zip(getattr(runs[0], name), getattr(runs[1], name)))
+
+
+@pytest.mark.parametrize("param,copy", [("f32", "bf16"), ("bf16", None)])
+@pytest.mark.parametrize("mode", ["keep", "average", "reset"])
+@pytest.mark.parametrize("workers", [1, 3, 4])
+def test_round_end(mode, workers, param, copy):
+    x = Case([(33, 70), (0, 9), (200, 101)], workers=workers, param=param, copy=copy)
+    p0, m0 = [t.clone() for t in x.p], [t.clone() for t in x.m]
+    x.list.qsr_muon_sync(mode)
+    n = len(x.shapes)
+
+    def mean(ts, j):
+        total = ts[j].float()
+        for k in range(1, workers):
+            total = total + ts[k * n + j].float()
+        return total / torch.full_like(total, workers)        # a division by a Python number is a product with its rounded reciprocal
+    for k in range(workers):
+        for j in range(n):
+            i, value = k * n + j, mean(p0, j)
+            assert torch.equal(x.p[i], value.to(x.p[i].dtype))
+            if copy:
+                assert torch.equal(x.c[i], value.to(x.c[i].dtype))
+            want = {"keep": m0[i], "average": mean(m0, j), "reset": torch.zeros_like(m0[i])}[mode]
+            assert torch.equal(x.m[i], want)
+
+
+def test_new_gradients():
+    x, y = Case([(70, 90), (90, 70)], seed=1), Case([(70, 90), (90, 70)], seed=1)
+    other = [torch.randn_like(g) for g in x.g]
+    x.list.qsr_muon_set_grads(other)
+    for g, o in zip(y.g, other):
+        g.copy_(o)
+    x.list.qsr_muon_step(0.1)
+    y.list.qsr_muon_step(0.1)
+    assert all(torch.equal(s, t) for s, t in zip(x.p, y.p))
+
+
+def test_without_gradients_a_step_is_refused():
+    p, m = torch.zeros(8, 8, device=DEV), torch.zeros(8, 8, device=DEV)
+    ws = torch.empty(B.qsr_muon_workspace_bytes([(8, 8)]), dtype=torch.uint8, device=DEV)
+    x = B.MuonList([p], None, [m], workspace=ws, stream=stream())
+    with pytest.raises(B.QsrError) as e:
+        x.qsr_muon_step(0.1)
+    assert e.value.status == B.QSR_ESTATE
+    x.qsr_muon_set_grads([torch.ones(8, 8, device=DEV)])
+    x.qsr_muon_step(0.1)
+    x.qsr_muon_check()
+
+
+def test_captured_and_replayed():
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        x, y = Case([(200, 300), (64, 30)], products=3, seed=3), Case([(200, 300), (64, 30)], products=3, seed=3)
+        x.list.qsr_muon_step(0.02)                     # outside a graph first
+        y.list.qsr_muon_step(0.02)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            x.list.qsr_muon_step(0.02)
+            with pytest.raises(B.QsrError) as e:
+                x.list.qsr_muon_set_grads(x.g)
+            assert e.value.status == B.QSR_ESTATE
+        for _ in range(3):
+            x.g[0].mul_(-1.1)
+            y.g[0].mul_(-1.1)
+            graph.replay()
+            y.list.qsr_muon_step(0.02)
+        side.synchronize()
+    assert all(torch.equal(s, t) for s, t in zip(x.p + x.m, y.p + y.m))
+
+
+def test_two_lists_at_once():
+    """Two lists with their own workspaces on two streams."""
+    alone = [Case([(500, 700)] * 4, products=3, seed=s) for s in (1, 2)]
+    for x in alone:
+        for _ in range(5):
+            x.list.qsr_muon_step(0.02)
+    torch.cuda.synchronize()
+    together, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s, st in zip((1, 2), streams):
+        with torch.cuda.stream(st):
+            together.append(Case([(500, 700)] * 4, products=3, seed=s))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x in together:
+            x.list.qsr_muon_step(0.02)
+    torch.cuda.synchronize()
+    for x, y in zip(alone, together):
+        assert all(torch.equal(s, t) for s, t in zip(x.p, y.p))
+
+
+def test_offsets_beyond_32_bits():
+    """512 copies of one 2048 x 2048 matrix below one another, 2^31 elements: the orthogonal factor of a stack is the stack of the
+    factors over sqrt(512), up to the polynomial, which sees the same A."""
+    n, side = 512, 2048
+    y = torch.randn(side, side, device=DEV, generator=gen(1)).bfloat16()
+    g = y.repeat(n, 1)
+    p, m = torch.zeros(n * side, side, device=DEV, dtype=torch.bfloat16), torch.zeros(n * side, side, device=DEV)
+    ws = torch.empty(B.qsr_muon_workspace_bytes([p.shape]), dtype=torch.uint8, device=DEV)
+    x = B.MuonList([p], [g], [m], beta=0.0, update_scale=[n ** 0.5], workspace=ws, stream=stream())
+    x.qsr_muon_step(1.0)
+    x.qsr_muon_check()
+    want, err = orthogonal64(y.double(), 5, 0.0, 1)
+    for part in (0, 255, 511):
+        got = -p[part * side:(part + 1) * side].double()
+        assert float(torch.linalg.vector_norm(got - want)) <= err + 2.0 ** -8 * float(torch.linalg.vector_norm(want))
+    assert torch.equal(m[-side:], y.float())
