@@ -199,7 +199,7 @@ struct MuonMatrix {           // one matrix, in the device table; m <= n are its
     float scale;              // power of two that the iterate is held at
     int32_t first_chunk, chunks;
 };
-struct MuonTile { int32_t matrix, i, j, pad; };      // 128 x 256 elements of a product: 128-row tile i, 256-column tile j
+struct MuonTile { int32_t matrix, i, j, pad; };      // 256 x 256 elements of a product: row tile i, column tile j
 struct MuonBlock { int32_t matrix, p, q, pad; };     // a block of 64 x 64
 struct MuonChunk { int32_t matrix, n; int64_t offset; };   // n consecutive elements
 struct MuonParams {

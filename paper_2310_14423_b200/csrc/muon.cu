@@ -172,11 +172,11 @@ enum { GRAM = 0, FACTOR = 1, ITERATE = 2, UPDATE = 3 };
 
 constexpr int kProductThreads = 384;         // warps: 0 copies, 1 products, 2 accumulators' allocation, 4 to 11 results
 constexpr int kBlockBytes = kBlockElements * 2;
-constexpr int kOperandBlocks = 6;            // of a stage: two of the 128-row tile, four of the 256-column tile
-constexpr int kStageBlocks = 24;             // shared memory for operands: 4 stages of one product, 2 of three
+constexpr int kOperandBlocks = 4;            // of a stage in each block of a pair: two of its 128 rows, two of its 128 columns
+constexpr int kStageBlocks = 24;             // shared memory for operands: 6 stages of one product, 3 of three
 constexpr int kTurn = 1;                     // blocks along the sum that tensor memory adds up, with three products
 constexpr unsigned kAccumulators = 512;      // columns of tensor memory: two tiles of 256
-constexpr unsigned long long kPatience = 4000000000ull;      // nanoseconds that a wait may take
+constexpr long long kPatience = 6000000000;  // clocks that a wait may take, some seconds
 
 __device__ __forceinline__ uint32_t shared_address(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
 
@@ -185,6 +185,15 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, unsigned count)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// The barrier at the same place in the shared memory of the pair's first block.
+__device__ __forceinline__ void barrier_arrive_first(uint32_t bar)
+{
+    asm volatile("{.reg .b32 a; mapa.shared::cluster.u32 a, %0, 0; mbarrier.arrive.shared::cluster.b64 _, [a];}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ void barrier_expect(uint32_t bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -196,25 +205,25 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, unsigned parity)
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ unsigned long long nanoseconds()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
 // False, with *stop set, if the phase does not end in time; false too where another role has given up, if `heed`.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, unsigned parity, volatile unsigned *stop, bool heed = true)
 {
     if (barrier_try(bar, parity)) return true;
-    const unsigned long long begin = nanoseconds();
+    const long long begin = clock64();
     for (;;) {
-        for (int i = 0; i < 32; ++i)
+        for (int i = 0; i < 64; ++i)
             if (barrier_try(bar, parity)) return true;
         if (heed && *stop) return false;
-        if (nanoseconds() - begin > kPatience) break;
+        if (clock64() - begin > kPatience) break;
     }
     *stop = 1;
     return false;
+}
+__device__ __forceinline__ bool elected()
+{
+    uint32_t e;
+    asm volatile("{.reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p;}" : "=r"(e));
+    return e != 0;
 }
 __device__ __forceinline__ void copy_block(uint32_t to, const void *from, uint32_t bar)
 {
@@ -228,19 +237,20 @@ __device__ __forceinline__ uint64_t operand(uint32_t address)
 {
     return uint64_t((address >> 4) & 0x3fff) | uint64_t(kBlockBytes >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
-// Instruction descriptor: fp16 operands, fp32 accumulators, 128 x n; outer_a / outer_b: the operand's rows in memory run along the sum.
+// Instruction descriptor: fp16 operands, fp32 accumulators, 256 x n over the pair; outer_a / outer_b: the operand's rows in memory run along the sum.
 __device__ __forceinline__ uint32_t instruction(int n, bool outer_a, bool outer_b)
 {
-    return 1u << 4 | uint32_t(outer_a) << 15 | uint32_t(outer_b) << 16 | uint32_t(n >> 3) << 17 | uint32_t(128 >> 4) << 24;
+    return 1u << 4 | uint32_t(outer_a) << 15 | uint32_t(outer_b) << 16 | uint32_t(n >> 3) << 17 | uint32_t(256 >> 4) << 24;
 }
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
-    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b),
+    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b),
                  "r"(idesc), "r"(uint32_t(add)) : "memory");
 }
+// Arrives at both blocks' barriers when the products issued so far are done.
 __device__ __forceinline__ void commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(uint16_t(3)) : "memory");
 }
 __device__ __forceinline__ void load_accumulators(float (&v)[16], uint32_t address)
 {
@@ -269,7 +279,7 @@ __device__ __forceinline__ void load_accumulators(float (&v)[32], uint32_t addre
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Whether the block in row tile P, column tile T (256 elements each) of a symmetric matrix is held; otherwise its mirror image is.
+// Whether the blocks in row tile P, column tile T (256 elements each) of a symmetric matrix are held; otherwise their mirror images are.
 __device__ __forceinline__ bool held(int P, int T) { return P <= T; }
 
 // Half a row of a block, 32 elements: where 16-byte pair `pair` (0 or 1) of it lies, in elements.
@@ -315,59 +325,58 @@ __device__ __forceinline__ void add_half(float (&v)[32], const uint16_t *block, 
     }
 }
 
-__device__ __forceinline__ float stepped(const MuonParams &p, float theta, float decay, float step, float x)
+// Eight elements of the parameter that belong to columns col.. of a row of the iterate, as they lie in memory: adjacent (`vec`), or
+// one to a word.
+__device__ __forceinline__ void fetch_theta(Raw8 &r, const MuonMatrix &t, int row, int col, bool vec)
 {
-    return theta - fmaf(decay, theta, step * x);
-}
-
-// theta <- theta - (lr wd theta + lr update_scale X) for 32 elements of one row of the iterate.
-__device__ __forceinline__ void update(const MuonParams &p, const MuonMatrix &t, int64_t row, int64_t col, const float (&x)[32])
-{
-    const float decay = p.lr_decay * t.wd_scale, step = p.lr * t.update_scale / t.scale;
-    const int type = t.param_type, ct = t.copy_type;
-    if (row >= t.m) return;
-    if (t.tall) {                             // lanes are neighbours in memory
-        const int64_t pitch = t.cols;
-        int64_t at = col * pitch + row;
-#pragma unroll
-        for (int k0 = 0; k0 < 32; k0 += 8) {
-            uint32_t old[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) old[k] = col + k0 + k < t.n ? load1(t.param, at + k * pitch, type) : 0u;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (col + k0 + k < t.n) {
-                    const float theta = stepped(p, widen1(old[k], type), decay, step, x[k0 + k]);
-                    store1(t.param, at + k * pitch, theta, type);
-                    if (ct != QSR_NONE) store1(t.copy, at + k * pitch, theta, ct);
-                }
-            at += 8 * pitch;
-        }
+    const int type = t.param_type;
+    if (row >= t.m || col >= t.n) return;
+    if (vec) {
+        load8(r, t.param, int64_t(row) * t.cols + col, type);
         return;
     }
-    const int64_t at = row * t.cols + col;
-    const bool vec = t.cols % 8 == 0 && address_aligned(t.param, type == QSR_F32 ? 32 : 16) && (ct == QSR_NONE || address_aligned(t.copy, ct == QSR_F32 ? 32 : 16));
+    const int64_t step = t.tall ? t.cols : 1, at = t.tall ? col * t.cols + row : row * t.cols + col;
 #pragma unroll
-    for (int k = 0; k < 32; k += 8) {
-        if (vec && col + k + 8 <= t.n) {
-            Raw8 r;
-            float theta[8];
-            load8(r, t.param, at + k, type);
-            widen8(theta, r, type);
+    for (int j = 0; j < 8; ++j) r.w[j] = col + j < t.n ? load1(t.param, at + j * step, type) : 0u;
+}
+// 32 rows (row: this lane's) and 128 columns of the iterate: the parameter's elements into the second-level cache.
+__device__ __forceinline__ void prefetch_theta(const MuonMatrix &t, int row, int col)
+{
+    const int bytes = t.param_type == QSR_F32 ? 4 : 2, lane = threadIdx.x & 31;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) theta[j] = stepped(p, theta[j], decay, step, x[k + j]);
-            store8(t.param, at + k, theta, type);
-            if (ct != QSR_NONE) store8(t.copy, at + k, theta, ct);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + k + j < t.n) {
-                    const float theta = stepped(p, widen1(load1(t.param, at + k + j, type), type), decay, step, x[k + j]);
-                    store1(t.param, at + k + j, theta, type);
-                    if (ct != QSR_NONE) store1(t.copy, at + k + j, theta, ct);
-                }
-        }
+    for (int q = 0; q < 4; ++q) {
+        const int m = t.tall ? row - lane : row, n = col + q * 32 + (t.tall ? lane : 0);
+        if (m >= t.m || n >= t.n) continue;
+        const char *at = static_cast<const char *>(t.param) + (t.tall ? int64_t(n) * t.cols + m : int64_t(m) * t.cols + n) * bytes;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
     }
+}
+// theta <- theta - (decay theta + step X) for the eight elements.
+__device__ __forceinline__ void update_theta(const Raw8 &r, const MuonMatrix &t, int row, int col, bool vec, float decay, float step, const float *x)
+{
+    const int type = t.param_type, copy = t.copy_type;
+    if (row >= t.m || col >= t.n) return;
+    float theta[8];
+    if (vec) widen8(theta, r, type);
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) theta[j] = widen1(r.w[j], type);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) theta[j] -= fmaf(decay, theta[j], step * x[j]);
+    if (vec) {
+        const int64_t at = int64_t(row) * t.cols + col;
+        store8(t.param, at, theta, type);
+        if (copy != QSR_NONE) store8(t.copy, at, theta, copy);
+        return;
+    }
+    const int64_t pitch = t.tall ? t.cols : 1, at = t.tall ? col * t.cols + row : row * t.cols + col;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (col + j < t.n) {
+            store1(t.param, at + j * pitch, theta[j], type);
+            if (copy != QSR_NONE) store1(t.copy, at + j * pitch, theta[j], copy);
+        }
 }
 
 // What becomes of 32 sums of a tile: row `row` of block (bp, bq), its first or second half.
@@ -394,23 +403,24 @@ __device__ __forceinline__ void result(const MuonParams &p, const MuonMatrix &t,
     } else {
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= 1.0f / kFactorScale;
-        if (KIND == ITERATE)
-            store_half(t.x[from ^ 1] + block * kBlockElements, t.x[from ^ 1] + (int64_t(mb) * t.nb + block) * kBlockElements, row, half, v, PRODUCTS == 3);
-        else update(p, t, int64_t(bp) * 64 + row, int64_t(bq) * 64 + half * 32, v);
+        store_half(t.x[from ^ 1] + block * kBlockElements, t.x[from ^ 1] + (int64_t(mb) * t.nb + block) * kBlockElements, row, half, v, PRODUCTS == 3);
     }
 }
 
 struct Shared {
-    uint64_t full[4], empty[4], ready[2], drained[2];
+    uint64_t full[6], other[6], empty[6], ready[2], drained[2];
     uint32_t tensor_memory;
     unsigned stop;
 };
 
-// A block per multiprocessor takes tiles of 128 x 256 elements, blockIdx.x, + gridDim.x, ...: one warp brings blocks of 64 along the
-// sum into a ring of stages, one thread issues the products into one half of tensor memory, eight warps take the tile before out
-// of the other half.
+// A pair of blocks (one per multiprocessor) takes tiles of 256 x 256 elements, pair, + pairs, ...; each has 128 of the tile's rows and
+// 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  One warp of
+// each block copies; one thread of the first block issues the products of both (in the second block that thread tells the first
+// when a stage has arrived); eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
+// single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.
 template <int KIND, int PRODUCTS>
-__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int n_tiles, int from)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int n_tiles, int from)
 {
     extern __shared__ char raw[];
     __shared__ Shared sh;
@@ -419,26 +429,29 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     const uint32_t stage0 = (shared_address(raw) + 1023u) & ~1023u;
     constexpr uint32_t kStage = kOperandBlocks * PARTS * kBlockBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = int(blockIdx.x & 1), pair = int(blockIdx.x >> 1), pairs = int(gridDim.x >> 1);
     volatile unsigned *stop = &sh.stop;
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             barrier_init(shared_address(&sh.full[i]), 1);
+            barrier_init(shared_address(&sh.other[i]), 1);
             barrier_init(shared_address(&sh.empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(shared_address(&sh.ready[i]), 1);
-            barrier_init(shared_address(&sh.drained[i]), 8);
+            barrier_init(shared_address(&sh.drained[i]), 16);
         }
         sh.stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    __syncthreads();
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&sh.tensor_memory)), "r"(kAccumulators) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&sh.tensor_memory)), "r"(kAccumulators) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     fence_before();
-    __syncthreads();
+    pair_sync();
     fence_after();
     const uint32_t accumulators = sh.tensor_memory;
 
@@ -446,12 +459,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         int stage = 0, issued = 0;
         unsigned phase = 0;
         bool going = true;
-        for (int tile = blockIdx.x; tile < n_tiles && going; tile += gridDim.x) {
+        for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = tiles[tile];
             const MuonMatrix &t = p.matrices[w.matrix];
             const int mb = t.mb, nb = t.nb, sums = KIND == GRAM ? nb : mb;
-            const int p0 = w.i * 2, q0 = w.j * 4, columns = KIND >= ITERATE ? nb : mb;
-            const int rows = min(2, mb - p0), cols = min(4, columns - q0);
+            const int columns = KIND >= ITERATE ? nb : mb, wide = columns - w.j * 4 > 2;
+            const int p0 = w.i * 4 + rank * 2, q0 = w.j * 4 + (wide ? rank * 2 : rank);
+            const int rows = max(0, min(2, mb - p0)), cols = max(0, min(wide ? 2 : 1, columns - q0));
             const uint16_t *left = KIND == GRAM ? t.x[from] : KIND == FACTOR ? t.gram : t.factor;
             const uint16_t *right = KIND == FACTOR ? t.gram : t.x[from];
             const int64_t left_lo = int64_t(mb) * (KIND == GRAM ? nb : mb), right_lo = int64_t(mb) * (KIND == FACTOR ? mb : nb);
@@ -468,7 +482,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 __syncwarp();
                 if (mine) {
                     bool direct;               // block (at, k), or its mirror image (k, at)
-                    if (is_left) direct = KIND == GRAM || held(w.i >> 1, k >> 2);
+                    if (is_left) direct = KIND == GRAM || held(w.i, k >> 2);
                     else direct = KIND == GRAM || (KIND == FACTOR && held(w.j, k >> 2));
                     const int64_t index = direct ? int64_t(k) * mb + at : int64_t(at) * mb + k;
                     copy_block(stage0 + stage * kStage + (part * kOperandBlocks + slot) * kBlockBytes, base + index * kBlockElements, bar);
@@ -485,39 +499,49 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             barrier_wait(shared_address(&sh.full[last % STAGES]), parity, stop, false);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0, buffer = 0;
-            unsigned phase = 0, buffer_phase = 0;
-            bool going = true;
-            for (int tile = blockIdx.x; tile < n_tiles && going; tile += gridDim.x) {
-                const MuonTile w = tiles[tile];
-                const MuonMatrix &t = p.matrices[w.matrix];
-                const int sums = KIND == GRAM ? t.nb : t.mb, cols = min(4, (KIND >= ITERATE ? t.nb : t.mb) - w.j * 4);
-                for (int k = 0; k < sums; ++k) {
-                    const int part = k % TURN;                     // of what is added up in tensor memory
-                    const uint32_t d = accumulators + unsigned(buffer) * 256u;
-                    if (part == 0 && !barrier_wait(shared_address(&sh.drained[buffer]), buffer_phase ^ 1u, stop)) { going = false; break; }
-                    if (!barrier_wait(shared_address(&sh.full[stage]), phase, stop)) { going = false; break; }
-                    fence_after();
-                    const bool outer_a = KIND != GRAM && !held(w.i >> 1, k >> 2);
-                    const bool outer_b = KIND >= ITERATE || (KIND == FACTOR && !held(w.j, k >> 2));
-                    const uint32_t idesc = instruction(cols * 64, outer_a, outer_b);
-                    const uint32_t a0 = stage0 + stage * kStage, b0 = a0 + 2 * kBlockBytes;
-                    const uint64_t a = operand(a0), b = operand(b0);
-                    const uint64_t a_step = outer_a ? 2048 >> 4 : 32 >> 4, b_step = outer_b ? 2048 >> 4 : 32 >> 4;
-                    constexpr uint64_t lo = (kOperandBlocks * kBlockBytes) >> 4;
+        // the whole warp runs through the loop, so that descriptors are computed once for it, and one elected thread issues
+        int stage = 0, buffer = 0;
+        unsigned phase = 0, buffer_phase = 0;
+        const bool one = elected();
+        bool going = true;
+        for (int tile = pair; tile < n_tiles && going; tile += pairs) {
+            const MuonTile w = tiles[tile];
+            const MuonMatrix &t = p.matrices[w.matrix];
+            const int sums = KIND == GRAM ? t.nb : t.mb, wide = (KIND >= ITERATE ? t.nb : t.mb) - w.j * 4 > 2;
+            for (int k = 0; k < sums; ++k) {
+                const uint32_t full = shared_address(&sh.full[stage]), other = shared_address(&sh.other[stage]);
+                if (rank == 1) {
+                    if (!barrier_wait(full, phase, stop)) { going = false; break; }
+                    if (one) barrier_arrive_first(other);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    continue;
+                }
+                const int part = k % TURN;                     // of what is added up in tensor memory
+                const uint32_t d = accumulators + unsigned(buffer) * 256u;
+                if (part == 0 && !barrier_wait(shared_address(&sh.drained[buffer]), buffer_phase ^ 1u, stop)) { going = false; break; }
+                if (!barrier_wait(full, phase, stop) || !barrier_wait(other, phase, stop)) { going = false; break; }
+                fence_after();
+                const bool outer_a = KIND != GRAM && !held(w.i, k >> 2);
+                const bool outer_b = KIND >= ITERATE || (KIND == FACTOR && !held(w.j, k >> 2));
+                const uint32_t idesc = instruction(wide ? 256 : 128, outer_a, outer_b);
+                const uint32_t a0 = stage0 + stage * kStage, b0 = a0 + 2 * kBlockBytes;
+                const uint64_t a = operand(a0), b = operand(b0);
+                const uint64_t a_step = outer_a ? 2048 >> 4 : 32 >> 4, b_step = outer_b ? 2048 >> 4 : 32 >> 4;
+                constexpr uint64_t lo = (kOperandBlocks * kBlockBytes) >> 4;
+                if (one) {
 #pragma unroll
                     for (int q = PRODUCTS - 1; q >= 0; --q)        // hi lo, lo hi, hi hi
 #pragma unroll
                         for (int s = 0; s < 4; ++s)
                             multiply(d, a + (q == 1 ? lo : 0) + s * a_step, b + (q == 2 ? lo : 0) + s * b_step, idesc, part > 0 || q < PRODUCTS - 1 || s > 0);
                     commit(shared_address(&sh.empty[stage]));
-                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-                    if (part == TURN - 1 || k == sums - 1) {
-                        commit(shared_address(&sh.ready[buffer]));
-                        buffer ^= 1;
-                        if (buffer == 0) buffer_phase ^= 1u;
-                    }
+                    if (part == TURN - 1 || k == sums - 1) commit(shared_address(&sh.ready[buffer]));
+                }
+                __syncwarp();
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                if (part == TURN - 1 || k == sums - 1) {
+                    buffer ^= 1;
+                    if (buffer == 0) buffer_phase ^= 1u;
                 }
             }
         }
@@ -528,16 +552,37 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         const auto next = [&] {
             fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(shared_address(&sh.drained[buffer]));
+            if (lane == 0) barrier_arrive_first(shared_address(&sh.drained[buffer]));
             buffer ^= 1;
             if (buffer == 0) buffer_phase ^= 1u;
         };
         bool going = true;
-        for (int tile = blockIdx.x; tile < n_tiles && going; tile += gridDim.x) {
+        for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = tiles[tile];
             const MuonMatrix &t = p.matrices[w.matrix];
-            const int row = (group & 1) * 32 + lane, bp = w.i * 2 + (group >> 1);      // in block row bp
+            const int row = (group & 1) * 32 + lane, bp = w.i * 4 + rank * 2 + (group >> 1);      // in block row bp
+            const int bq = w.j * 4 + part * 2;
             const uint32_t from_lane = accumulators + unsigned(part * 128) + (unsigned(group * 32) << 16);
+            // the last product of a step: a pipeline over eight columns of the parameter at a time
+            constexpr int DEPTH = PRODUCTS == 3 ? 2 : 4;
+            Raw8 theta[KIND == UPDATE ? DEPTH : 1];
+            const int r = bp * 64 + row, c = bq * 64;
+            bool vec = false;
+            float decay = 0.0f, step = 0.0f;
+            if (KIND == UPDATE) {
+                if (tile + pairs < n_tiles) {
+                    const MuonTile ahead = tiles[tile + pairs];
+                    prefetch_theta(p.matrices[ahead.matrix], (ahead.i * 4 + rank * 2 + (group >> 1)) * 64 + row, (ahead.j * 4 + part * 2) * 64);
+                }
+                const int type = t.param_type, copy = t.copy_type;
+                vec = !t.tall && t.cols % 8 == 0 && address_aligned(t.param, type == QSR_F32 ? 32 : 16) &&
+                      (copy == QSR_NONE || address_aligned(t.copy, copy == QSR_F32 ? 32 : 16));
+                decay = p.lr_decay * t.wd_scale;
+                step = p.lr * t.update_scale / (t.scale * kFactorScale);
+                if (PRODUCTS == 1)
+#pragma unroll
+                    for (int g = 0; g < DEPTH; ++g) fetch_theta(theta[g], t, r, c + g * 8, vec);
+            }
             if (PRODUCTS == 1) {
                 if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) break;
                 fence_after();
@@ -545,7 +590,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int h = 0; h < 4; ++h) {                    // 32 columns each
                     float v[32];
                     load_accumulators(v, from_lane + unsigned(buffer * 256 + h * 32));
-                    result<KIND, PRODUCTS>(p, t, bp, w.j * 4 + part * 2 + (h >> 1), row, h & 1, from, v);
+                    if (KIND != UPDATE) result<KIND, PRODUCTS>(p, t, bp, bq + (h >> 1), row, h & 1, from, v);
+                    else
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            update_theta(theta[g % DEPTH], t, r, c + h * 32 + g * 8, vec, decay, step, v + g * 8);
+                            if (h < 3) fetch_theta(theta[g % DEPTH], t, r, c + h * 32 + 32 + g * 8, vec);
+                        }
                 }
                 next();
             } else {
@@ -569,18 +620,28 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     next();
                 }
                 if (!going) break;
+                if (KIND != UPDATE) {
 #pragma unroll
-                for (int h = 0; h < 4; ++h) result<KIND, PRODUCTS>(p, t, bp, w.j * 4 + part * 2 + (h >> 1), row, h & 1, from, v[h]);
+                    for (int h = 0; h < 4; ++h) result<KIND, PRODUCTS>(p, t, bp, bq + (h >> 1), row, h & 1, from, v[h]);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < DEPTH; ++g) fetch_theta(theta[g % DEPTH], t, r, c + g * 8, vec);
+#pragma unroll
+                    for (int g = 0; g < 16; ++g) {
+                        update_theta(theta[g % DEPTH], t, r, c + g * 8, vec, decay, step, v[g / 4] + g % 4 * 8);
+                        if (g + DEPTH < 16) fetch_theta(theta[g % DEPTH], t, r, c + (g + DEPTH) * 8, vec);
+                    }
+                }
             }
         }
     }
     __syncwarp();
     fence_before();
-    __syncthreads();
     if (threadIdx.x == 0 && sh.stop) *p.late = 1u;
+    pair_sync();                         // the other block's products read this one's shared memory and write its tensor memory
     if (warp == 2) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(accumulators), "r"(kAccumulators) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(accumulators), "r"(kAccumulators) : "memory");
     }
 }
 
@@ -619,7 +680,7 @@ int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream)
 int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
 {
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int n = int(n_tiles), blocks = n < multiprocessors ? n : multiprocessors;
+    const int n = int(n_tiles), blocks = 2 * (n < multiprocessors / 2 ? n : multiprocessors / 2);
     if (p.products == 3) {
         if (kind == GRAM) return launch_product<GRAM, 3>(p, from, tiles, n, blocks, st);
         if (kind == FACTOR) return launch_product<FACTOR, 3>(p, from, tiles, n, blocks, st);

@@ -43,13 +43,12 @@ Sides sides_of(int64_t rows, int64_t cols)
     const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
     return Sides{m, n, ceil_div(m, 64), ceil_div(n, 64)};
 }
-int64_t half_tiles(const Sides &s)              // 128 x 256 tiles of an m x m matrix that reach the diagonal's tiles or lie above
+int64_t half_tiles(const Sides &s)              // 256 x 256 tiles of an m x m matrix on and above the diagonal
 {
-    int64_t count = 0;
-    for (int64_t j = 0; j * 4 < s.mb; ++j) count += std::min(ceil_div(s.mb, 2), 2 * j + 2);
-    return count;
+    const int64_t t = ceil_div(s.mb, 4);
+    return t * (t + 1) / 2;
 }
-int64_t whole_tiles(const Sides &s) { return ceil_div(s.mb, 2) * ceil_div(s.nb, 4); }
+int64_t whole_tiles(const Sides &s) { return ceil_div(s.mb, 4) * ceil_div(s.nb, 4); }
 
 struct Layout {
     int64_t matrices, grads, chunks, blocks, half, whole, sync_tensors, sync_chunks, partial, factor, arrived, late, data, bytes;
@@ -230,13 +229,13 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
         for (int32_t j = 0; j * 4 < y.mb; ++j)
-            for (int32_t r = 0; r < std::min((y.mb + 1) / 2, 2 * j + 2); ++r) half.push_back(MuonTile{i, r, j, 0});
+            for (int32_t r = 0; r <= j; ++r) half.push_back(MuonTile{i, r, j, 0});
     }
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].mb > matrices[size_t(b)].mb; });
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
         for (int32_t j = 0; j * 4 < y.nb; ++j)
-            for (int32_t r = 0; r * 2 < y.mb; ++r) whole.push_back(MuonTile{i, r, j, 0});
+            for (int32_t r = 0; r * 4 < y.mb; ++r) whole.push_back(MuonTile{i, r, j, 0});
     }
     if (int64_t(half.size()) != l.n_half || int64_t(whole.size()) != l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
         int64_t(sync_chunks.size()) != l.n_sync || at > ws + l.bytes)
