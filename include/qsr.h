@@ -511,7 +511,7 @@ int qsr_muon_destroy(qsr_muon *muon);
 /* New gradient addresses, as qsr_list_set_grads. */
 int qsr_muon_set_grads(qsr_muon *muon, const void *const *grads_host);
 
-/* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  2 + 3 * iterations
+/* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  3 + 3 * iterations
  * launches, whatever the number of matrices; asynchronous.  It may be captured; lr and grad_scale are then those of the capture. */
 int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale);
 

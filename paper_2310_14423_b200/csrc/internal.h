@@ -190,16 +190,21 @@ struct MuonMatrix {           // one matrix, in the device table; m <= n are its
     void *param, *copy;
     float *momentum;
     int64_t rows, cols;
-    uint16_t *x[2];           // fp16 blocks of 64 x 64: the iterate of m x n (column of blocks by column), before and after a product
+    uint16_t *x[2];           // fp16 blocks of 64 x 64: the iterate (column of blocks by column), before and after a product
     uint16_t *gram, *factor;  // the same of m x m
-    int32_t m, n, mb, nb;     // mb, nb: blocks along m and n
-    int32_t tall;             // rows > cols: the iterate is the transpose
+    int32_t rb, cb, mb, nb;   // blocks along rows, columns, m and n
+    int32_t tall;             // rows > cols
     int32_t param_type, copy_type, grad_type;
     float wd_scale, update_scale;
     float scale;              // power of two that the iterate is held at
     int32_t first_chunk, chunks;
 };
-struct MuonTile { int32_t matrix, i, j, pad; };      // 256 x 256 elements of a product: row tile i, column tile j
+struct alignas(16) MuonTile {  // 256 x 256 elements of a product: row tile i, column tile j
+    int32_t matrix, i, j;
+    int32_t tall;             // of the matrix
+    int32_t rows, columns;    // of the product's result, in blocks
+    int32_t longer, shorter;  // the matrix's sides in blocks
+};
 struct MuonBlock { int32_t matrix, p, q, pad; };     // a block of 64 x 64
 struct MuonChunk { int32_t matrix, n; int64_t offset; };   // n consecutive elements
 struct MuonParams {
@@ -218,7 +223,8 @@ struct MuonParams {
 int launch_muon_clear(const MuonParams &p, int64_t chunks, void *stream);      // momentum <- 0
 int launch_muon_momentum(const MuonParams &p, int64_t chunks, void *stream);
 int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream);
-// One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate, 3 last iterate and update of the parameters.
+int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream);
+// One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate.
 int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
 
 // ---- log probabilities of given tokens (logprobs.cu) ----

@@ -1,11 +1,12 @@
 // Orthogonalised momentum: the kernels.  See include/qsr.h for the formulas and muon_api.cu for the launches.
 //
-// The iterate X (m x n, m <= n: the transpose of a tall matrix) and the symmetric m x m matrices A = X X^T and C = a I + b A + c A^2
-// are held as fp16 blocks of 64 x 64 (8 KB), each exactly as a tensor-core operand wants it in shared memory (rows of 128 bytes,
-// 16-byte pieces exchanged by the row number's low three bits).  A block is one untiled bulk copy, needs no tensor map, and serves as an
-// operand with either side along the products' sum: rows along it if read as it is, columns along it if the instruction is told so
-// ("major" bit).  So X X^T and C X read the same blocks of X, and of A and C only the tiles on and above the diagonal are
-// computed; what lies below is read from its mirror image.  Blocks are padded with zeros, hence any m and n.
+// The iterate X (rows x cols) and the symmetric m x m matrices A = X X^T (X^T X if there are more rows than columns; m is the shorter
+// side) and C = a I + b A + c A^2 are held as fp16 blocks of 64 x 64 (8 KB), each exactly as a tensor-core operand wants it in
+// shared memory (rows of 128 bytes, 16-byte pieces exchanged by the row number's low three bits).  A block is one untiled bulk copy, needs
+// no tensor map, and serves as an operand with either side along the products' sum: columns along it as it is, rows along it if
+// the instruction is told so ("outer").  So X X^T and C X, or X^T X and X C, read the same blocks of X, no matrix is ever transposed,
+// and of A and C only the tiles on and above the diagonal are computed; what lies below is read from its mirror image.
+// Blocks are padded with zeros, hence any sizes.
 //
 // With three products per multiplication, X, A and C are sums of two fp16 numbers and hi hi + hi lo + lo hi are accumulated.
 #include <cuda_runtime.h>
@@ -41,14 +42,15 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
     const MuonMatrix &t = p.matrices[c.matrix];
     const void *grad = p.grads[c.matrix];
     const int gt = t.grad_type;
-    const bool vec = address_aligned(grad, gt == QSR_F32 ? 32 : 16) && address_aligned(t.momentum, 32);
+    float *momentum = t.momentum;
+    const bool vec = address_aligned(grad, gt == QSR_F32 ? 32 : 16) && address_aligned(momentum, 32);
     double s = 0.0;
     if (vec) {
 #pragma unroll 2
         for (int i = int(threadIdx.x) * 8; i + 8 <= c.n; i += kMomentumThreads * 8) {
             Raw8 rg, rm;
             load8(rg, grad, c.offset + i, gt);
-            load32(rm, t.momentum + c.offset + i);
+            load32(rm, momentum + c.offset + i);
             float g[8], m[8];
             widen8(g, rg, gt);
             widen8(m, rm, QSR_F32);
@@ -59,14 +61,28 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
                 const double u = double(direction(p, m[j], gs));
                 s = fma(u, u, s);
             }
-            store8(t.momentum, c.offset + i, m, QSR_F32);
+            store8(momentum, c.offset + i, m, QSR_F32);
         }
     }
-    for (int i = (vec ? c.n & ~7 : 0) + int(threadIdx.x); i < c.n; i += kMomentumThreads) {
-        const float gs = widen1(load1(grad, c.offset + i, gt), gt) * p.grad_scale, m = updated(p, t.momentum[c.offset + i], gs);
-        const double u = double(direction(p, m, gs));
-        s = fma(u, u, s);
-        t.momentum[c.offset + i] = m;
+    for (int i0 = (vec ? c.n & ~7 : 0) + int(threadIdx.x); i0 < c.n; i0 += 8 * kMomentumThreads) {
+        uint32_t g[8];
+        float m[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * kMomentumThreads;
+            g[j] = i < c.n ? load1(grad, c.offset + i, gt) : 0u;
+            m[j] = i < c.n ? momentum[c.offset + i] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * kMomentumThreads;
+            const float gs = widen1(g[j], gt) * p.grad_scale, to = updated(p, m[j], gs);
+            const double u = double(direction(p, to, gs));
+            if (i < c.n) {
+                s = fma(u, u, s);
+                momentum[c.offset + i] = to;
+            }
+        }
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
@@ -109,66 +125,166 @@ __global__ void __launch_bounds__(kMomentumThreads) clear_kernel(const __grid_co
 
 constexpr int kBlockElements = 64 * 64;
 
-// Two fp16 numbers whose sum is x to 22 bits (hi alone: 11).
-__device__ __forceinline__ void split(float x, __half &hi, __half &lo)
-{
-    hi = __float2half_rn(x);
-    lo = __float2half_rn(x - __half2float(hi));
-}
+// Where a block of 64 x 64 holds its element (r, c).
+__device__ __forceinline__ int place(int r, int c) { return r * 64 + ((c >> 3) ^ (r & 7)) * 8 + (c & 7); }
 
-// One block of the first iterate: u from the new momentum, times scale / (norm + eps).
-__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonParams p)
+// A thread's elements of a block, sixteen in two halves of eight.  WIDE: eight adjacent ones of a row, eight threads to a row (the
+// matrix's rows are aligned to eight elements); otherwise eight of a column, 64 threads side by side.
+template <bool WIDE> __device__ __forceinline__ int row_in(int half) { return WIDE ? half * 32 + (int(threadIdx.x) >> 3) : (int(threadIdx.x) >> 6) * 16 + half * 8; }
+template <bool WIDE> __device__ __forceinline__ int column_in() { return WIDE ? (int(threadIdx.x) & 7) * 8 : int(threadIdx.x) & 63; }
+
+// A half: how many of its elements the matrix has, the first one's place, and the distance from one to the next.
+struct Half { int64_t at, step; int n; };
+template <bool WIDE>
+__device__ __forceinline__ Half half_of(const MuonMatrix &t, const MuonBlock &b, int half)
 {
-    __shared__ __align__(16) __half hi[kBlockElements], lo[kBlockElements];
-    const MuonBlock b = p.blocks[blockIdx.x];
-    const MuonMatrix &t = p.matrices[b.matrix];
-    const void *grad = p.grads[b.matrix];
+    const int64_t r = int64_t(b.p) * 64 + row_in<WIDE>(half), c = int64_t(b.q) * 64 + column_in<WIDE>(), rows = t.rows, cols = t.cols;
+    return Half{r * cols + c, WIDE ? 1 : cols, c >= cols || r >= rows ? 0 : WIDE ? 8 : int(min(rows - r, int64_t(8)))};
+}
+template <bool WIDE>
+__device__ __forceinline__ void take(Raw8 &raw, const void *base, int type, const Half &o)
+{
+    if (WIDE && o.n) {
+        load8(raw, base, o.at, type);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) raw.w[k] = !WIDE && k < o.n ? load1(base, o.at + k * o.step, type) : 0u;
+}
+template <bool WIDE>
+__device__ __forceinline__ void widen(float (&x)[8], const Raw8 &raw, int type)
+{
+    if (WIDE) widen8(x, raw, type);
+    else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = widen1(raw.w[k], type);
+}
+template <bool WIDE>
+__device__ __forceinline__ void give(void *base, const float (&x)[8], int type, const Half &o)
+{
+    if (WIDE) {
+        if (o.n) store8(base, o.at, x, type);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k < o.n) store1(base, o.at + k * o.step, x[k], type);
+}
+__device__ __forceinline__ bool wide_rows(const MuonMatrix &t, const void *base, int type) { return t.cols % 8 == 0 && address_aligned(base, type == QSR_F32 ? 32 : 16); }
+
+// One block of the first iterate: u from the new momentum, times scale / (norm + eps); zeros beyond the matrix.
+template <bool WIDE>
+__device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b, const void *grad)
+{
+    const bool both = p.products == 3;
+    uint16_t *block = t.x[0] + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
+    const int64_t lo = int64_t(t.rb) * t.cb * kBlockElements;
+    const int grad_type = t.grad_type;
+    const float *momentum = t.momentum;
     const float factor = p.factor[b.matrix];
-    const int gt = t.grad_type;
-    // the matrix's rows r0.. and columns c0.. in its own orientation
-    const int64_t r0 = int64_t(t.tall ? b.q : b.p) * 64, c0 = int64_t(t.tall ? b.p : b.q) * 64;
-    const bool vec = t.cols % 8 == 0 && address_aligned(grad, gt == QSR_F32 ? 32 : 16) && address_aligned(t.momentum, 32);
+    Half o[2];
+    Raw8 g[2], m[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int r = h * 32 + int(threadIdx.x) / 8, c = (int(threadIdx.x) & 7) * 8;
-        const int64_t at = (r0 + r) * t.cols + c0 + c;
-        float g[8], m[8];
-        if (vec && r0 + r < t.rows && c0 + c < t.cols) {
-            Raw8 rg, rm;
-            load8(rg, grad, at, gt);
-            load32(rm, t.momentum + at);
-            widen8(g, rg, gt);
-            widen8(m, rm, QSR_F32);
+        o[h] = half_of<WIDE>(t, b, h);
+        take<WIDE>(g[h], grad, grad_type, o[h]);
+        take<WIDE>(m[h], momentum, QSR_F32, o[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float gs[8], x[8];
+        widen<WIDE>(gs, g[h], grad_type);
+        widen<WIDE>(x, m[h], QSR_F32);
+        Raw8 hi, rest;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k < o[h].n ? direction(p, x[k], gs[k] * p.grad_scale) * factor : 0.0f;      // whatever the factor
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            const __half2 f = __floats2half2_rn(x[k], x[k + 1]);
+            const float2 back = __half22float2(f);
+            hi.w[k / 2] = *reinterpret_cast<const uint32_t *>(&f);
+            rest.w[k / 2] = narrow2(x[k] - back.x, x[k + 1] - back.y, QSR_F16);
+        }
+        if (WIDE) {
+            uint16_t *to = block + place(row_in<true>(h), column_in<true>());
+            store16(to, hi);
+            if (both) store16(to + lo, rest);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = r0 + r < t.rows && c0 + c + j < t.cols;
-                g[j] = in ? widen1(load1(grad, at + j, gt), gt) : 0.0f;
-                m[j] = in ? t.momentum[at + j] : 0.0f;
+            for (int k = 0; k < 8; ++k) {
+                uint16_t *to = block + place(row_in<false>(h) + k, column_in<false>());
+                *to = uint16_t(hi.w[k / 2] >> (k % 2 * 16));
+                if (both) to[lo] = uint16_t(rest.w[k / 2] >> (k % 2 * 16));
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int row = t.tall ? c + j : r, col = t.tall ? r : c + j;      // in the block
-            const bool in = r0 + r < t.rows && c0 + c + j < t.cols;            // padding stays zero, whatever the factor
-            const int to = row * 64 + ((col / 8) ^ (row & 7)) * 8 + (col & 7);
-            split(in ? direction(p, m[j], g[j] * p.grad_scale) * factor : 0.0f, hi[to], lo[to]);
-        }
     }
-    __syncthreads();
-    uint4 *out = reinterpret_cast<uint4 *>(t.x[0] + (int64_t(b.q) * t.mb + b.p) * kBlockElements);
-    uint4 *out_lo = out + int64_t(t.mb) * t.nb * (kBlockElements / 8);
+}
+// The blocks are taken from the last one on: the end of what the launch before has written is still in the second-level cache.
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonParams p)
+{
+    const MuonBlock b = p.blocks[gridDim.x - 1 - blockIdx.x];
+    const MuonMatrix &t = p.matrices[b.matrix];
+    const void *grad = p.grads[b.matrix];
+    if (wide_rows(t, grad, t.grad_type) && wide_rows(t, t.momentum, QSR_F32)) pack_block<true>(p, t, b, grad);
+    else pack_block<false>(p, t, b, grad);
+}
+
+// theta <- theta - (lr wd theta + lr update_scale X) for one block of the last iterate.
+template <bool WIDE>
+__device__ __forceinline__ void apply_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b, int from)
+{
+    const bool both = p.products == 3;
+    const float decay = p.lr_decay * t.wd_scale, step = p.lr * t.update_scale / t.scale;
+    const uint16_t *block = t.x[from] + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
+    const int64_t lo = int64_t(t.rb) * t.cb * kBlockElements;
+    const int type = t.param_type, copy_type = t.copy_type;
+    void *param = t.param, *copy = t.copy;
+    Half o[2];
+    Raw8 old[2], hi[2], rest[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int i = h * 256 + int(threadIdx.x);
-        out[i] = reinterpret_cast<const uint4 *>(hi)[i];
-        if (p.products == 3) out_lo[i] = reinterpret_cast<const uint4 *>(lo)[i];
+        o[h] = half_of<WIDE>(t, b, h);
+        take<WIDE>(old[h], param, type, o[h]);
+        if (WIDE) {
+            const uint16_t *x = block + place(row_in<true>(h), column_in<true>());
+            load16(hi[h], x);
+            if (both) load16(rest[h], x + lo);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint16_t *x = block + place(row_in<false>(h) + k, column_in<false>());
+                hi[h].w[k] = *x;
+                if (both) rest[h].w[k] = x[lo];
+            }
+        }
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float theta[8], x[8], more[8];
+        widen<WIDE>(theta, old[h], type);
+        widen<WIDE>(x, hi[h], QSR_F16);
+        if (both) {
+            widen<WIDE>(more, rest[h], QSR_F16);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] += more[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) theta[k] -= fmaf(decay, theta[k], step * x[k]);
+        give<WIDE>(param, theta, type, o[h]);
+        if (copy_type != QSR_NONE) give<WIDE>(copy, theta, copy_type, o[h]);
+    }
+}
+__global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ MuonParams p, int from)
+{
+    const MuonBlock b = p.blocks[gridDim.x - 1 - blockIdx.x];
+    const MuonMatrix &t = p.matrices[b.matrix];
+    if (wide_rows(t, t.param, t.param_type) && (t.copy_type == QSR_NONE || wide_rows(t, t.copy, t.copy_type))) apply_block<true>(p, t, b, from);
+    else apply_block<false>(p, t, b, from);
 }
 
 // ---- products --------------------------------------------------------------------------------------------
 
-enum { GRAM = 0, FACTOR = 1, ITERATE = 2, UPDATE = 3 };
+enum { GRAM = 0, FACTOR = 1, ITERATE = 2 };
 
 constexpr int kProductThreads = 384;         // warps: 0 copies, 1 products, 2 accumulators' allocation, 4 to 11 results
 constexpr int kBlockBytes = kBlockElements * 2;
@@ -184,7 +300,6 @@ __device__ __forceinline__ void barrier_init(uint32_t bar, unsigned count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
-__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // The barrier at the same place in the shared memory of the pair's first block.
 __device__ __forceinline__ void barrier_arrive_first(uint32_t bar)
 {
@@ -279,133 +394,111 @@ __device__ __forceinline__ void load_accumulators(float (&v)[32], uint32_t addre
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Whether the blocks in row tile P, column tile T (256 elements each) of a symmetric matrix are held; otherwise their mirror images are.
-__device__ __forceinline__ bool held(int P, int T) { return P <= T; }
+// What a product is made of, in blocks: rows x sums times sums x columns.  An operand is the iterate or a symmetric matrix; it is
+// "outer" at step k if its blocks there have the sum along their rows.  Of a symmetric matrix the blocks in row tile P, column
+// tile T (four blocks each) are held where P <= T; elsewhere their mirror images are read, the other way round.
+struct Shape {
+    int rows, sums, columns;
+    bool left_x, right_x, outer_left_x, outer_right_x;
+    __device__ __forceinline__ bool outer_left(int i, int k) const { return left_x ? outer_left_x : i > (k >> 2); }
+    __device__ __forceinline__ bool outer_right(int j, int k) const { return right_x ? outer_right_x : j > (k >> 2); }
+};
+template <int KIND>
+__device__ __forceinline__ Shape shape_of(const MuonTile &w)
+{
+    const bool tall = w.tall;
+    if (KIND == GRAM) return Shape{w.rows, w.longer, w.columns, true, true, tall, tall};                 // X X^T, or X^T X
+    if (KIND == FACTOR) return Shape{w.rows, w.shorter, w.columns, false, false, false, false};         // A A
+    return Shape{w.rows, w.shorter, w.columns, tall, !tall, false, true};                                // C X, or X C
+}
 
-// Half a row of a block, 32 elements: where 16-byte pair `pair` (0 or 1) of it lies, in elements.
-__device__ __forceinline__ int pair_at(int row, int half, int pair) { return row * 64 + ((half * 2 + pair) ^ ((row & 7) >> 1)) * 16; }
-
-__device__ __forceinline__ void store_half(uint16_t *block, uint16_t *block_lo, int row, int half, const float (&v)[32], bool both)
+// A warp's 32 rows of a block pass through 4 KB of its own in shared memory, which hold them as the block does: a thread has a row in
+// its registers, but a warp's accesses to global memory are adjacent (rows of 128 bytes a thread apart take eight times as long).
+// Half: 32 of the row's 64 elements, as 16 words.
+__device__ __forceinline__ char *piece(char *buffer, int lane, int half, int k) { return buffer + lane * 128 + (((half * 4 + k) ^ (lane & 7)) * 16); }
+__device__ __forceinline__ void stage_half(char *buffer, int lane, int half, const uint32_t (&w)[16])
 {
 #pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-        Raw8 hi, lo;
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4 *>(piece(buffer, lane, half, k)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+}
+__device__ __forceinline__ void unstage_half(uint32_t (&w)[16], char *buffer, int lane, int half)
+{
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float a = v[pair * 16 + 2 * k], b = v[pair * 16 + 2 * k + 1];
-            const __half2 h = __floats2half2_rn(a, b);
-            const float2 f = __half22float2(h);
-            hi.w[k] = *reinterpret_cast<const uint32_t *>(&h);
-            if (both) lo.w[k] = narrow2(a - f.x, b - f.y, QSR_F16);
+    for (int k = 0; k < 4; ++k) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(piece(buffer, lane, half, k));
+        w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+    }
+}
+__device__ __forceinline__ void flush(char *buffer, int lane, uint16_t *to)
+{
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(to)[k * 32 + lane] = reinterpret_cast<const uint4 *>(buffer)[k * 32 + lane];
+    __syncwarp();
+}
+__device__ __forceinline__ void fill(char *buffer, int lane, const uint16_t *from)
+{
+    uint4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const uint4 *>(from)[k * 32 + lane];
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(buffer)[k * 32 + lane] = v[k];
+    __syncwarp();
+}
+// What fp16 leaves of x, if `rest`; otherwise x in fp16.
+__device__ __forceinline__ void narrow_half(uint32_t (&w)[16], const float (&x)[32], bool rest)
+{
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        w[k] = narrow2(x[2 * k], x[2 * k + 1], QSR_F16);
+        if (rest) {
+            const float2 f = widen2(w[k], QSR_F16);
+            w[k] = narrow2(x[2 * k] - f.x, x[2 * k + 1] - f.y, QSR_F16);
         }
-        if (row & 1) {                       // odd rows: the two pieces of a pair change places
+    }
+}
+__device__ __forceinline__ void add_half(float (&x)[32], const uint32_t (&w)[16], float factor)
+{
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t x = hi.w[k]; hi.w[k] = hi.w[k + 4]; hi.w[k + 4] = x;
-                if (both) { x = lo.w[k]; lo.w[k] = lo.w[k + 4]; lo.w[k + 4] = x; }
-            }
-        }
-        store32(block + pair_at(row, half, pair), hi);
-        if (both) store32(block_lo + pair_at(row, half, pair), lo);
+    for (int k = 0; k < 16; ++k) {
+        const float2 f = widen2(w[k], QSR_F16);
+        x[2 * k] = fmaf(factor, f.x, x[2 * k]);
+        x[2 * k + 1] = fmaf(factor, f.y, x[2 * k + 1]);
     }
 }
 
-__device__ __forceinline__ void add_half(float (&v)[32], const uint16_t *block, int row, int half, float factor)
+// From sums to what is held: all but the polynomial's middle term.
+template <int KIND>
+__device__ __forceinline__ void finish_half(float (&x)[32], float factor, int diagonal)
 {
 #pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-        Raw8 r;
-        load32(r, block + pair_at(row, half, pair));
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float2 f = widen2((row & 1) ? r.w[k ^ 4] : r.w[k], QSR_F16);
-            v[pair * 16 + 2 * k] = fmaf(factor, f.x, v[pair * 16 + 2 * k]);
-            v[pair * 16 + 2 * k + 1] = fmaf(factor, f.y, v[pair * 16 + 2 * k + 1]);
-        }
-    }
+    for (int k = 0; k < 32; ++k) x[k] = KIND == FACTOR ? x[k] * factor + (k == diagonal ? kA * kFactorScale : 0.0f) : x[k] * factor;
 }
+constexpr float kMiddle = kB * kFactorScale / kGramScale;
 
-// Eight elements of the parameter that belong to columns col.. of a row of the iterate, as they lie in memory: adjacent (`vec`), or
-// one to a word.
-__device__ __forceinline__ void fetch_theta(Raw8 &r, const MuonMatrix &t, int row, int col, bool vec)
-{
-    const int type = t.param_type;
-    if (row >= t.m || col >= t.n) return;
-    if (vec) {
-        load8(r, t.param, int64_t(row) * t.cols + col, type);
-        return;
+// Where a warp's part of a tile goes: 32 rows of blocks (bp, bq) and (bp, bq + 1).
+template <int KIND>
+struct Target {
+    int blocks, diagonal;              // of the two, how many there are; where this thread's row meets the diagonal, in their columns
+    uint16_t *to;
+    const uint16_t *gram;              // FACTOR: the same elements of A
+    int64_t column, lo;                // from a block to the next, and to what fp16 leaves
+    float factor;
+    __device__ __forceinline__ Target(const MuonTile &w, const MuonParams &p, int from, int rank, int group, int part, int lane)
+    {
+        const MuonMatrix &t = p.matrices[w.matrix];
+        const int bp = w.i * 4 + rank * 2 + (group >> 1), bq = w.j * 4 + part * 2;
+        blocks = bp < w.rows ? min(2, w.columns - bq) : 0;
+        diagonal = (bp - bq) * 64 + (group & 1) * 32 + lane;
+        const int64_t at = (int64_t(bq) * w.rows + bp) * kBlockElements + (group & 1) * (kBlockElements / 2);
+        to = (KIND == GRAM ? t.gram : KIND == FACTOR ? t.factor : t.x[from ^ 1]) + at;
+        gram = t.gram + at;
+        column = int64_t(w.rows) * kBlockElements;
+        lo = int64_t(w.columns) * column;
+        factor = KIND == GRAM ? kGramScale / (t.scale * t.scale) : KIND == FACTOR ? kC * kFactorScale / (kGramScale * kGramScale) : 1.0f / kFactorScale;
     }
-    const int64_t step = t.tall ? t.cols : 1, at = t.tall ? col * t.cols + row : row * t.cols + col;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.w[j] = col + j < t.n ? load1(t.param, at + j * step, type) : 0u;
-}
-// 32 rows (row: this lane's) and 128 columns of the iterate: the parameter's elements into the second-level cache.
-__device__ __forceinline__ void prefetch_theta(const MuonMatrix &t, int row, int col)
-{
-    const int bytes = t.param_type == QSR_F32 ? 4 : 2, lane = threadIdx.x & 31;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int m = t.tall ? row - lane : row, n = col + q * 32 + (t.tall ? lane : 0);
-        if (m >= t.m || n >= t.n) continue;
-        const char *at = static_cast<const char *>(t.param) + (t.tall ? int64_t(n) * t.cols + m : int64_t(m) * t.cols + n) * bytes;
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
-    }
-}
-// theta <- theta - (decay theta + step X) for the eight elements.
-__device__ __forceinline__ void update_theta(const Raw8 &r, const MuonMatrix &t, int row, int col, bool vec, float decay, float step, const float *x)
-{
-    const int type = t.param_type, copy = t.copy_type;
-    if (row >= t.m || col >= t.n) return;
-    float theta[8];
-    if (vec) widen8(theta, r, type);
-    else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) theta[j] = widen1(r.w[j], type);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) theta[j] -= fmaf(decay, theta[j], step * x[j]);
-    if (vec) {
-        const int64_t at = int64_t(row) * t.cols + col;
-        store8(t.param, at, theta, type);
-        if (copy != QSR_NONE) store8(t.copy, at, theta, copy);
-        return;
-    }
-    const int64_t pitch = t.tall ? t.cols : 1, at = t.tall ? col * t.cols + row : row * t.cols + col;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (col + j < t.n) {
-            store1(t.param, at + j * pitch, theta[j], type);
-            if (copy != QSR_NONE) store1(t.copy, at + j * pitch, theta[j], copy);
-        }
-}
-
-// What becomes of 32 sums of a tile: row `row` of block (bp, bq), its first or second half.
-template <int KIND, int PRODUCTS>
-__device__ __forceinline__ void result(const MuonParams &p, const MuonMatrix &t, int bp, int bq, int row, int half, int from, float (&v)[32])
-{
-    const int mb = t.mb;
-    if (bp >= mb || bq >= (KIND >= ITERATE ? t.nb : mb)) return;
-    const int64_t block = int64_t(bq) * mb + bp;
-    if (KIND == GRAM) {
-        const float f = kGramScale / (t.scale * t.scale);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] *= f;
-        store_half(t.gram + block * kBlockElements, t.gram + (int64_t(mb) * mb + block) * kBlockElements, row, half, v, PRODUCTS == 3);
-    } else if (KIND == FACTOR) {
-        const uint16_t *gram = t.gram + block * kBlockElements;
-        constexpr float f = kC * kFactorScale / (kGramScale * kGramScale), g = kB * kFactorScale / kGramScale;
-        const int diagonal = (bp - bq) * 64 + row - half * 32;      // which of them is on the diagonal
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = v[k] * f + (k == diagonal ? kA * kFactorScale : 0.0f);
-        add_half(v, gram, row, half, g);
-        if (PRODUCTS == 3) add_half(v, gram + int64_t(mb) * mb * kBlockElements, row, half, g);
-        store_half(t.factor + block * kBlockElements, t.factor + (int64_t(mb) * mb + block) * kBlockElements, row, half, v, PRODUCTS == 3);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] *= 1.0f / kFactorScale;
-        store_half(t.x[from ^ 1] + block * kBlockElements, t.x[from ^ 1] + (int64_t(mb) * t.nb + block) * kBlockElements, row, half, v, PRODUCTS == 3);
-    }
-}
+};
 
 struct Shared {
     uint64_t full[6], other[6], empty[6], ready[2], drained[2];
@@ -459,36 +552,40 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
         int stage = 0, issued = 0;
         unsigned phase = 0;
         bool going = true;
+        // a tile's description and its matrix's addresses are read while the tile before is copied
+        MuonTile ahead = tiles[min(pair, n_tiles - 1)];
+        const uint16_t *x = p.matrices[ahead.matrix].x[from], *symmetric = KIND == FACTOR ? p.matrices[ahead.matrix].gram : p.matrices[ahead.matrix].factor;
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
-            const MuonTile w = tiles[tile];
-            const MuonMatrix &t = p.matrices[w.matrix];
-            const int mb = t.mb, nb = t.nb, sums = KIND == GRAM ? nb : mb;
-            const int columns = KIND >= ITERATE ? nb : mb, wide = columns - w.j * 4 > 2;
+            const MuonTile w = ahead;
+            const Shape z = shape_of<KIND>(w);
+            const int wide = z.columns - w.j * 4 > 2, sums = z.sums;
             const int p0 = w.i * 4 + rank * 2, q0 = w.j * 4 + (wide ? rank * 2 : rank);
-            const int rows = max(0, min(2, mb - p0)), cols = max(0, min(wide ? 2 : 1, columns - q0));
-            const uint16_t *left = KIND == GRAM ? t.x[from] : KIND == FACTOR ? t.gram : t.factor;
-            const uint16_t *right = KIND == FACTOR ? t.gram : t.x[from];
-            const int64_t left_lo = int64_t(mb) * (KIND == GRAM ? nb : mb), right_lo = int64_t(mb) * (KIND == FACTOR ? mb : nb);
+            const int rows = max(0, min(2, z.rows - p0)), cols = max(0, min(wide ? 2 : 1, z.columns - q0));
             // this lane's block of each stage: part, then rows of the left or columns of the right operand
             const int part = lane / kOperandBlocks, slot = lane % kOperandBlocks;
-            const bool is_left = slot < 2;
+            const bool is_left = slot < 2, iterate = is_left ? z.left_x : z.right_x;
             const bool mine = part < PARTS && (is_left ? slot < rows : slot - 2 < cols);
-            const int at = is_left ? p0 + slot : q0 + slot - 2;
-            const uint16_t *base = is_left ? left + part * left_lo * kBlockElements : right + part * right_lo * kBlockElements;
+            const int at = is_left ? p0 + slot : q0 + slot - 2, pitch = iterate && w.tall ? w.longer : w.shorter;
+            const uint16_t *base = (iterate ? x : symmetric) + part * int64_t(w.shorter) * (iterate ? w.longer : w.shorter) * kBlockElements;
+            ahead = tiles[min(tile + pairs, n_tiles - 1)];
             for (int k = 0; k < sums; ++k) {
                 if (!barrier_wait(shared_address(&sh.empty[stage]), phase ^ 1u, stop)) { going = false; break; }
                 const uint32_t bar = shared_address(&sh.full[stage]);
                 if (lane == 0) barrier_expect(bar, unsigned((rows + cols) * PARTS * kBlockBytes));
                 __syncwarp();
                 if (mine) {
-                    bool direct;               // block (at, k), or its mirror image (k, at)
-                    if (is_left) direct = KIND == GRAM || held(w.i, k >> 2);
-                    else direct = KIND == GRAM || (KIND == FACTOR && held(w.j, k >> 2));
-                    const int64_t index = direct ? int64_t(k) * mb + at : int64_t(at) * mb + k;
+                    // block (at, k), or block (k, at): of a symmetric matrix, its mirror image
+                    const bool outer = is_left ? z.outer_left(w.i, k) : z.outer_right(w.j, k);
+                    const int64_t index = outer ? int64_t(at) * pitch + k : int64_t(k) * pitch + at;
                     copy_block(stage0 + stage * kStage + (part * kOperandBlocks + slot) * kBlockBytes, base + index * kBlockElements, bar);
                 }
                 issued++;
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                if (k == 0) {
+                    const MuonMatrix &t = p.matrices[ahead.matrix];
+                    x = t.x[from];
+                    symmetric = KIND == FACTOR ? t.gram : t.factor;
+                }
             }
         }
         // when the block ends nothing may be copying into its shared memory, or reading it: wait for the last stages
@@ -504,10 +601,12 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
         unsigned phase = 0, buffer_phase = 0;
         const bool one = elected();
         bool going = true;
+        MuonTile ahead = tiles[min(pair, n_tiles - 1)];
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
-            const MuonTile w = tiles[tile];
-            const MuonMatrix &t = p.matrices[w.matrix];
-            const int sums = KIND == GRAM ? t.nb : t.mb, wide = (KIND >= ITERATE ? t.nb : t.mb) - w.j * 4 > 2;
+            const MuonTile w = ahead;
+            ahead = tiles[min(tile + pairs, n_tiles - 1)];
+            const Shape z = shape_of<KIND>(w);
+            const int sums = z.sums, wide = z.columns - w.j * 4 > 2;
             for (int k = 0; k < sums; ++k) {
                 const uint32_t full = shared_address(&sh.full[stage]), other = shared_address(&sh.other[stage]);
                 if (rank == 1) {
@@ -521,8 +620,7 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
                 if (part == 0 && !barrier_wait(shared_address(&sh.drained[buffer]), buffer_phase ^ 1u, stop)) { going = false; break; }
                 if (!barrier_wait(full, phase, stop) || !barrier_wait(other, phase, stop)) { going = false; break; }
                 fence_after();
-                const bool outer_a = KIND != GRAM && !held(w.i, k >> 2);
-                const bool outer_b = KIND >= ITERATE || (KIND == FACTOR && !held(w.j, k >> 2));
+                const bool outer_a = z.outer_left(w.i, k), outer_b = z.outer_right(w.j, k);
                 const uint32_t idesc = instruction(wide ? 256 : 128, outer_a, outer_b);
                 const uint32_t a0 = stage0 + stage * kStage, b0 = a0 + 2 * kBlockBytes;
                 const uint64_t a = operand(a0), b = operand(b0);
@@ -547,6 +645,7 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
         }
     } else if (warp >= 4) {
         const int group = warp & 3, part = (warp - 4) >> 2;      // lanes 32 group.. of tensor memory, columns 128 part..
+        char *buffer_own = raw + (stage0 - shared_address(raw)) + kStageBlocks * kBlockBytes + (warp - 4) * 4096;
         int buffer = 0;
         unsigned buffer_phase = 0;
         const auto next = [&] {
@@ -556,47 +655,30 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
             buffer ^= 1;
             if (buffer == 0) buffer_phase ^= 1u;
         };
+        const uint32_t from_lane = accumulators + unsigned(part * 128) + (unsigned(group * 32) << 16);
         bool going = true;
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
-            const MuonTile w = tiles[tile];
-            const MuonMatrix &t = p.matrices[w.matrix];
-            const int row = (group & 1) * 32 + lane, bp = w.i * 4 + rank * 2 + (group >> 1);      // in block row bp
-            const int bq = w.j * 4 + part * 2;
-            const uint32_t from_lane = accumulators + unsigned(part * 128) + (unsigned(group * 32) << 16);
-            // the last product of a step: a pipeline over eight columns of the parameter at a time
-            constexpr int DEPTH = PRODUCTS == 3 ? 2 : 4;
-            Raw8 theta[KIND == UPDATE ? DEPTH : 1];
-            const int r = bp * 64 + row, c = bq * 64;
-            bool vec = false;
-            float decay = 0.0f, step = 0.0f;
-            if (KIND == UPDATE) {
-                if (tile + pairs < n_tiles) {
-                    const MuonTile ahead = tiles[tile + pairs];
-                    prefetch_theta(p.matrices[ahead.matrix], (ahead.i * 4 + rank * 2 + (group >> 1)) * 64 + row, (ahead.j * 4 + part * 2) * 64);
-                }
-                const int type = t.param_type, copy = t.copy_type;
-                vec = !t.tall && t.cols % 8 == 0 && address_aligned(t.param, type == QSR_F32 ? 32 : 16) &&
-                      (copy == QSR_NONE || address_aligned(t.copy, copy == QSR_F32 ? 32 : 16));
-                decay = p.lr_decay * t.wd_scale;
-                step = p.lr * t.update_scale / (t.scale * kFactorScale);
-                if (PRODUCTS == 1)
-#pragma unroll
-                    for (int g = 0; g < DEPTH; ++g) fetch_theta(theta[g], t, r, c + g * 8, vec);
-            }
             if (PRODUCTS == 1) {
+                const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
+                if (KIND == FACTOR && o.blocks > 0) fill(buffer_own, lane, o.gram);
                 if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) break;
                 fence_after();
 #pragma unroll 1
-                for (int h = 0; h < 4; ++h) {                    // 32 columns each
+                for (int h = 0; h < 2 * o.blocks; ++h) {         // 32 columns each
                     float v[32];
+                    uint32_t words[16];
                     load_accumulators(v, from_lane + unsigned(buffer * 256 + h * 32));
-                    if (KIND != UPDATE) result<KIND, PRODUCTS>(p, t, bp, bq + (h >> 1), row, h & 1, from, v);
-                    else
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            update_theta(theta[g % DEPTH], t, r, c + h * 32 + g * 8, vec, decay, step, v + g * 8);
-                            if (h < 3) fetch_theta(theta[g % DEPTH], t, r, c + h * 32 + 32 + g * 8, vec);
-                        }
+                    finish_half<KIND>(v, o.factor, o.diagonal - h * 32);
+                    if (KIND == FACTOR) {
+                        unstage_half(words, buffer_own, lane, h & 1);
+                        add_half(v, words, kMiddle);
+                    }
+                    narrow_half(words, v, false);
+                    stage_half(buffer_own, lane, h & 1, words);
+                    if (h & 1) {
+                        flush(buffer_own, lane, o.to + (h >> 1) * o.column);
+                        if (KIND == FACTOR && h + 1 < 2 * o.blocks) fill(buffer_own, lane, o.gram + o.column);
+                    }
                 }
                 next();
             } else {
@@ -605,9 +687,9 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[h][k] = 0.0f;
-                const int turns = ((KIND == GRAM ? t.nb : t.mb) + TURN - 1) / TURN;
+                int turns = ((KIND == GRAM ? tiles[tile].longer : tiles[tile].shorter) + TURN - 1) / TURN;
 #pragma unroll 1
-                for (int turn = 0; turn < turns; ++turn) {
+                for (; turns > 0; --turns) {
                     if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) { going = false; break; }
                     fence_after();
 #pragma unroll
@@ -620,16 +702,32 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
                     next();
                 }
                 if (!going) break;
-                if (KIND != UPDATE) {
+                const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) result<KIND, PRODUCTS>(p, t, bp, bq + (h >> 1), row, h & 1, from, v[h]);
-                } else {
+                for (int q = 0; q < 2; ++q) {                    // blocks
+                    if (q >= o.blocks) break;
+                    uint32_t words[16];
 #pragma unroll
-                    for (int g = 0; g < DEPTH; ++g) fetch_theta(theta[g % DEPTH], t, r, c + g * 8, vec);
+                    for (int h = 0; h < 2; ++h) finish_half<KIND>(v[2 * q + h], o.factor, o.diagonal - (2 * q + h) * 32);
+                    if (KIND == FACTOR)
 #pragma unroll
-                    for (int g = 0; g < 16; ++g) {
-                        update_theta(theta[g % DEPTH], t, r, c + g * 8, vec, decay, step, v[g / 4] + g % 4 * 8);
-                        if (g + DEPTH < 16) fetch_theta(theta[g % DEPTH], t, r, c + (g + DEPTH) * 8, vec);
+                        for (int s = 0; s < 2; ++s) {
+                            fill(buffer_own, lane, o.gram + q * o.column + s * o.lo);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                unstage_half(words, buffer_own, lane, h);
+                                add_half(v[2 * q + h], words, kMiddle);
+                            }
+                        }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {                // fp16, and what it leaves
+                        __syncwarp();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            narrow_half(words, v[2 * q + h], s == 1);
+                            stage_half(buffer_own, lane, h, words);
+                        }
+                        flush(buffer_own, lane, o.to + q * o.column + s * o.lo);
                     }
                 }
             }
@@ -645,7 +743,7 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
     }
 }
 
-constexpr int kProductShared = kStageBlocks * kBlockBytes + 1024;
+constexpr int kProductShared = kStageBlocks * kBlockBytes + 8 * 4096 + 1024;
 
 template <int KIND, int PRODUCTS>
 int launch_product(const MuonParams &p, int from, const MuonTile *tiles, int n, int blocks, cudaStream_t st)
@@ -677,6 +775,12 @@ int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream)
     return int(cudaGetLastError());
 }
 
+int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream)
+{
+    apply_kernel<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(p, from);
+    return int(cudaGetLastError());
+}
+
 int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
 {
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -684,13 +788,11 @@ int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile 
     if (p.products == 3) {
         if (kind == GRAM) return launch_product<GRAM, 3>(p, from, tiles, n, blocks, st);
         if (kind == FACTOR) return launch_product<FACTOR, 3>(p, from, tiles, n, blocks, st);
-        if (kind == ITERATE) return launch_product<ITERATE, 3>(p, from, tiles, n, blocks, st);
-        return launch_product<UPDATE, 3>(p, from, tiles, n, blocks, st);
+        return launch_product<ITERATE, 3>(p, from, tiles, n, blocks, st);
     }
     if (kind == GRAM) return launch_product<GRAM, 1>(p, from, tiles, n, blocks, st);
     if (kind == FACTOR) return launch_product<FACTOR, 1>(p, from, tiles, n, blocks, st);
-    if (kind == ITERATE) return launch_product<ITERATE, 1>(p, from, tiles, n, blocks, st);
-    return launch_product<UPDATE, 1>(p, from, tiles, n, blocks, st);
+    return launch_product<ITERATE, 1>(p, from, tiles, n, blocks, st);
 }
 
 }  // namespace qsr

@@ -201,8 +201,9 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
         const Sides s = sides_of(x.rows, x.cols);
         y.param = x.param; y.copy = x.copy; y.momentum = x.momentum;
         y.rows = x.rows; y.cols = x.cols;
-        y.m = int32_t(s.m); y.n = int32_t(s.n); y.mb = int32_t(s.mb); y.nb = int32_t(s.nb);
         y.tall = x.rows > x.cols;
+        y.mb = int32_t(s.mb); y.nb = int32_t(s.nb);
+        y.rb = y.tall ? y.nb : y.mb; y.cb = y.tall ? y.mb : y.nb;
         y.param_type = x.param_type; y.copy_type = x.copy_type; y.grad_type = x.grad_type;
         y.wd_scale = x.wd_scale; y.update_scale = x.update_scale;
         // entries of the iterate have a root mean square of about one where it is sqrt(m n); fp16 holds up to 65504
@@ -214,9 +215,8 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
         y.first_chunk = int32_t(chunks.size());
         for (int64_t o = 0; o < x.rows * x.cols; o += kChunk) chunks.push_back(MuonChunk{i, int32_t(std::min(kChunk, x.rows * x.cols - o)), o});
         y.chunks = int32_t(chunks.size()) - y.first_chunk;
-        // in the order of the matrix's own rows
-        for (int64_t a = 0; a < (y.tall ? s.nb : s.mb); ++a)
-            for (int64_t b = 0; b < (y.tall ? s.mb : s.nb); ++b) blocks.push_back(MuonBlock{i, int32_t(y.tall ? b : a), int32_t(y.tall ? a : b), 0});
+        for (int32_t a = 0; a < y.rb; ++a)
+            for (int32_t b = 0; b < y.cb; ++b) blocks.push_back(MuonBlock{i, a, b, 0});
     }
     for (int part = 0; part < 2; ++part)
         for (int32_t j = 0; j < per; ++j)
@@ -229,13 +229,14 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
         for (int32_t j = 0; j * 4 < y.mb; ++j)
-            for (int32_t r = 0; r <= j; ++r) half.push_back(MuonTile{i, r, j, 0});
+            for (int32_t r = 0; r <= j; ++r) half.push_back(MuonTile{i, r, j, y.tall, y.mb, y.mb, y.nb, y.mb});
     }
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].mb > matrices[size_t(b)].mb; });
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
-        for (int32_t j = 0; j * 4 < y.nb; ++j)
-            for (int32_t r = 0; r * 4 < y.mb; ++r) whole.push_back(MuonTile{i, r, j, 0});
+        // neighbours share what is longer: the iterate's tile, not the factor's
+        for (int32_t u = 0; u * 4 < y.nb; ++u)
+            for (int32_t v = 0; v * 4 < y.mb; ++v) whole.push_back(MuonTile{i, y.tall ? u : v, y.tall ? v : u, y.tall, y.rb, y.cb, y.nb, y.mb});
     }
     if (int64_t(half.size()) != l.n_half || int64_t(whole.size()) != l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
         int64_t(sync_chunks.size()) != l.n_sync || at > ws + l.bytes)
@@ -363,13 +364,13 @@ int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale)
     if (int err = launch_muon_pack(p, muon->blocks, muon->stream)) return launch_status(err);
     for (int i = 0; i < muon->cfg.iterations; ++i)
         for (int kind = 0; kind < 3; ++kind) {
-            const bool last = kind == 2 && i + 1 == muon->cfg.iterations;
             muon->launches++;
-            if (int err = launch_muon_product(p, last ? 3 : kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
+            if (int err = launch_muon_product(p, kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
                                               muon->multiprocessors, muon->stream))
                 return launch_status(err);
         }
-    return QSR_OK;
+    muon->launches++;
+    return launch_status(launch_muon_apply(p, muon->cfg.iterations & 1, muon->blocks, muon->stream));
 }
 
 int qsr_muon_sync(qsr_muon *muon, int32_t state_sync)

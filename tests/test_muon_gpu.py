@@ -150,7 +150,7 @@ def test_types_and_several_matrices(param, grad, copy, products):
     x = Case([(70, 200), (200, 70), (0, 5), (64, 256), (256, 65)], workers=2, param=param, grad=grad, copy=copy, products=products)
     x.step_and_compare()
     x.step_and_compare(lr=0.01, grad_scale=0.5)
-    assert x.list.qsr_muon_launch_count() == 2 * 17
+    assert x.list.qsr_muon_launch_count() == 2 * 18
 
 
 @pytest.mark.parametrize("products", [1, 3])
