@@ -216,6 +216,7 @@ struct MuonParams {
     float *factor;            // [matrices]: scale / (norm + eps)
     unsigned *arrived;        // [matrices], zero between launches
     unsigned *late;           // set where a wait ran out
+    const uint16_t *data;     // all matrices' blocks
     float one_minus_beta, beta, grad_scale, eps;
     float lr, lr_decay;
     int32_t nesterov, products, iterations;
@@ -225,7 +226,9 @@ int launch_muon_momentum(const MuonParams &p, int64_t chunks, void *stream);
 int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream);
 int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream);
 // One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate.
-int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
+// tensor_maps: two CUtensorMaps over the blocks at MuonParams::data.
+int encode_muon_maps(void *tensor_maps, const void *data, int64_t bytes);
+int launch_muon_product(const MuonParams &p, const void *tensor_maps, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
 
 // ---- log probabilities of given tokens (logprobs.cu) ----
 

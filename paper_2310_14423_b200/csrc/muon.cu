@@ -2,13 +2,14 @@
 //
 // The iterate X (rows x cols) and the symmetric m x m matrices A = X X^T (X^T X if there are more rows than columns; m is the shorter
 // side) and C = a I + b A + c A^2 are held as fp16 blocks of 64 x 64 (8 KB), each exactly as a tensor-core operand wants it in
-// shared memory (rows of 128 bytes, 16-byte pieces exchanged by the row number's low three bits).  A block is one untiled bulk copy, needs
-// no tensor map, and serves as an operand with either side along the products' sum: columns along it as it is, rows along it if
+// shared memory (rows of 128 bytes, 16-byte pieces exchanged by the row number's low three bits).  A block is one copy of 8 KB in a row
+// and serves as an operand with either side along the products' sum: columns along it as it is, rows along it if
 // the instruction is told so ("outer").  So X X^T and C X, or X^T X and X C, read the same blocks of X, no matrix is ever transposed,
 // and of A and C only the tiles on and above the diagonal are computed; what lies below is read from its mirror image.
 // Blocks are padded with zeros, hence any sizes.
 //
 // With three products per multiplication, X, A and C are sums of two fp16 numbers and hi hi + hi lo + lo hi are accumulated.
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "wide.cuh"
@@ -286,11 +287,14 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Muon
 
 enum { GRAM = 0, FACTOR = 1, ITERATE = 2 };
 
-constexpr int kProductThreads = 384;         // warps: 0 copies, 1 products, 2 accumulators' allocation, 4 to 11 results
+struct Maps { CUtensorMap single, pair; };
+
+constexpr int kResultWarps = 8;
+constexpr int kProductThreads = 128 + kResultWarps * 32;      // warps: 0 and 3 copies, 1 products, 2 accumulators' allocation, then results
 constexpr int kBlockBytes = kBlockElements * 2;
 constexpr int kOperandBlocks = 4;            // of a stage in each block of a pair: two of its 128 rows, two of its 128 columns
 constexpr int kStageBlocks = 24;             // shared memory for operands: 6 stages of one product, 3 of three
-constexpr int kTurn = 1;                     // blocks along the sum that tensor memory adds up, with three products
+constexpr int kTurn = 2;                     // blocks along the sum that tensor memory adds up, with three products
 constexpr unsigned kAccumulators = 512;      // columns of tensor memory: two tiles of 256
 constexpr long long kPatience = 6000000000;  // clocks that a wait may take, some seconds
 
@@ -340,10 +344,13 @@ __device__ __forceinline__ bool elected()
     asm volatile("{.reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p;}" : "=r"(e));
     return e != 0;
 }
-__device__ __forceinline__ void copy_block(uint32_t to, const void *from, uint32_t bar)
+// Blocks of 64 x 64 into this thread block's shared memory, one (`single`) or two neighbours (`pair`), reported to the barrier at that
+// place in the pair's first thread block.  The maps see the workspace's blocks as rows of 128 bytes, and a copy is 64 or 128 whole
+// rows: the tiled form is used because only that one may report to the other thread block's barrier.
+__device__ __forceinline__ void copy_blocks(uint32_t to, const CUtensorMap *map, int row, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(kBlockBytes), "r"(bar)
-                 : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map),
+                 "r"(0), "r"(row), "r"(bar & 0xfeffffffu) : "memory");
 }
 
 // Operand descriptor: rows of 128 bytes with 128-byte swizzle, groups of eight rows 1024 bytes apart; with the sum along the
@@ -412,59 +419,61 @@ __device__ __forceinline__ Shape shape_of(const MuonTile &w)
     return Shape{w.rows, w.shorter, w.columns, tall, !tall, false, true};                                // C X, or X C
 }
 
-// A warp's 32 rows of a block pass through 4 KB of its own in shared memory, which hold them as the block does: a thread has a row in
-// its registers, but a warp's accesses to global memory are adjacent (rows of 128 bytes a thread apart take eight times as long).
-// Half: 32 of the row's 64 elements, as 16 words.
-__device__ __forceinline__ char *piece(char *buffer, int lane, int half, int k) { return buffer + lane * 128 + (((half * 4 + k) ^ (lane & 7)) * 16); }
-__device__ __forceinline__ void stage_half(char *buffer, int lane, int half, const uint32_t (&w)[16])
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4 *>(piece(buffer, lane, half, k)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-}
-__device__ __forceinline__ void unstage_half(uint32_t (&w)[16], char *buffer, int lane, int half)
+// Half a row of a block, 32 elements: where 32-byte pair `pair` (0 or 1) of it lies, in elements.  A thread has a row in its registers and
+// writes it 32 bytes at a time, a sector each.  (Passing the tile through shared memory, so that a warp's accesses are adjacent, was
+// slower: the operands' copies and the products take most of what shared memory can do.)
+__device__ __forceinline__ int pair_at(int row, int half, int pair) { return row * 64 + ((half * 2 + pair) ^ ((row & 7) >> 1)) * 16; }
+// The words of 16 elements, in the order in which odd rows and even rows hold their two 16-byte pieces.
+__device__ __forceinline__ void exchange(Raw8 &r, bool odd)
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(piece(buffer, lane, half, k));
-        w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+        const uint32_t a = r.w[k], b = r.w[k + 4];
+        r.w[k] = odd ? b : a;
+        r.w[k + 4] = odd ? a : b;
     }
 }
-__device__ __forceinline__ void flush(char *buffer, int lane, uint16_t *to)
-{
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(to)[k * 32 + lane] = reinterpret_cast<const uint4 *>(buffer)[k * 32 + lane];
-    __syncwarp();
-}
-__device__ __forceinline__ void fill(char *buffer, int lane, const uint16_t *from)
-{
-    uint4 v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = reinterpret_cast<const uint4 *>(from)[k * 32 + lane];
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 8; ++k) reinterpret_cast<uint4 *>(buffer)[k * 32 + lane] = v[k];
-    __syncwarp();
-}
-// What fp16 leaves of x, if `rest`; otherwise x in fp16.
-__device__ __forceinline__ void narrow_half(uint32_t (&w)[16], const float (&x)[32], bool rest)
+// 32 elements in fp16, and what fp16 leaves of them `lo` elements further.
+template <bool REST>
+__device__ __forceinline__ void store_half(uint16_t *block, int64_t lo, int row, int half, const float (&v)[32])
 {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        w[k] = narrow2(x[2 * k], x[2 * k + 1], QSR_F16);
-        if (rest) {
-            const float2 f = widen2(w[k], QSR_F16);
-            w[k] = narrow2(x[2 * k] - f.x, x[2 * k + 1] - f.y, QSR_F16);
+    for (int pair = 0; pair < 2; ++pair) {
+        uint16_t *to = block + pair_at(row, half, pair);
+        Raw8 hi, rest;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float a = v[pair * 16 + 2 * k], b = v[pair * 16 + 2 * k + 1];
+            hi.w[k] = narrow2(a, b, QSR_F16);
+            if (REST) {
+                const float2 f = widen2(hi.w[k], QSR_F16);
+                rest.w[k] = narrow2(a - f.x, b - f.y, QSR_F16);
+            }
+        }
+        exchange(hi, row & 1);
+        store32(to, hi);
+        if (REST) {
+            exchange(rest, row & 1);
+            store32(to + lo, rest);
         }
     }
 }
-__device__ __forceinline__ void add_half(float (&x)[32], const uint32_t (&w)[16], float factor)
+__device__ __forceinline__ void load_half(Raw8 (&r)[2], const uint16_t *block, int row, int half)
 {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const float2 f = widen2(w[k], QSR_F16);
-        x[2 * k] = fmaf(factor, f.x, x[2 * k]);
-        x[2 * k + 1] = fmaf(factor, f.y, x[2 * k + 1]);
+    for (int pair = 0; pair < 2; ++pair) load32(r[pair], block + pair_at(row, half, pair));
+}
+__device__ __forceinline__ void add_half(float (&v)[32], Raw8 (&r)[2], int row, float factor)
+{
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+        exchange(r[pair], row & 1);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float2 f = widen2(r[pair].w[k], QSR_F16);
+            v[pair * 16 + 2 * k] = fmaf(factor, f.x, v[pair * 16 + 2 * k]);
+            v[pair * 16 + 2 * k + 1] = fmaf(factor, f.y, v[pair * 16 + 2 * k + 1]);
+        }
     }
 }
 
@@ -477,21 +486,23 @@ __device__ __forceinline__ void finish_half(float (&x)[32], float factor, int di
 }
 constexpr float kMiddle = kB * kFactorScale / kGramScale;
 
-// Where a warp's part of a tile goes: 32 rows of blocks (bp, bq) and (bp, bq + 1).
+// Where a warp's part of a tile goes: 32 rows of blocks (bp, bq) and (bp, bq + 1), a row to a thread.
 template <int KIND>
 struct Target {
-    int blocks, diagonal;              // of the two, how many there are; where this thread's row meets the diagonal, in their columns
+    int blocks;                        // of the two, how many the result has
+    int row, diagonal;                 // in its block; where it meets the matrix's diagonal, in their columns
     uint16_t *to;
     const uint16_t *gram;              // FACTOR: the same elements of A
-    int64_t column, lo;                // from a block to the next, and to what fp16 leaves
+    int64_t column, lo;                // from a block to the next, from fp16 to what it leaves
     float factor;
     __device__ __forceinline__ Target(const MuonTile &w, const MuonParams &p, int from, int rank, int group, int part, int lane)
     {
         const MuonMatrix &t = p.matrices[w.matrix];
         const int bp = w.i * 4 + rank * 2 + (group >> 1), bq = w.j * 4 + part * 2;
         blocks = bp < w.rows ? min(2, w.columns - bq) : 0;
-        diagonal = (bp - bq) * 64 + (group & 1) * 32 + lane;
-        const int64_t at = (int64_t(bq) * w.rows + bp) * kBlockElements + (group & 1) * (kBlockElements / 2);
+        row = (group & 1) * 32 + lane;
+        diagonal = (bp - bq) * 64 + row;
+        const int64_t at = (int64_t(bq) * w.rows + bp) * kBlockElements;
         to = (KIND == GRAM ? t.gram : KIND == FACTOR ? t.factor : t.x[from ^ 1]) + at;
         gram = t.gram + at;
         column = int64_t(w.rows) * kBlockElements;
@@ -501,24 +512,23 @@ struct Target {
 };
 
 struct Shared {
-    uint64_t full[6], other[6], empty[6], ready[2], drained[2];
+    uint64_t full[6], empty[6], ready[2], drained[2];
     uint32_t tensor_memory;
     unsigned stop;
 };
 
 // A pair of blocks (one per multiprocessor) takes tiles of 256 x 256 elements, pair, + pairs, ...; each has 128 of the tile's rows and
-// 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  One warp of
-// each block copies; one thread of the first block issues the products of both (in the second block that thread tells the first
-// when a stage has arrived); eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
+// 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  Two warps of
+// each block copy; one thread of the first block issues the products of both; eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
 // single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.
 template <int KIND, int PRODUCTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
-product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int n_tiles, int from)
+product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Maps maps, const MuonTile *tiles, int n_tiles, int from)
 {
     extern __shared__ char raw[];
     __shared__ Shared sh;
     constexpr int PARTS = PRODUCTS == 3 ? 2 : 1, STAGES = kStageBlocks / (kOperandBlocks * PARTS);
-    constexpr int TURN = PRODUCTS == 3 ? kTurn : 1 << 30;
+    constexpr int STEPS = PRODUCTS == 3 ? kTurn : 1;
     const uint32_t stage0 = (shared_address(raw) + 1023u) & ~1023u;
     constexpr uint32_t kStage = kOperandBlocks * PARTS * kBlockBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -527,12 +537,11 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             barrier_init(shared_address(&sh.full[i]), 1);
-            barrier_init(shared_address(&sh.other[i]), 1);
             barrier_init(shared_address(&sh.empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(shared_address(&sh.ready[i]), 1);
-            barrier_init(shared_address(&sh.drained[i]), 16);
+            barrier_init(shared_address(&sh.drained[i]), 2 * kResultWarps);
         }
         sh.stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -548,43 +557,54 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
     fence_after();
     const uint32_t accumulators = sh.tensor_memory;
 
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
+        // Copies: warp 0 those of the left operand, warp 3 those of the right one.  Everything is the same for the whole warp and one elected
+        // thread issues: copies issued by several threads of a warp go out one by one, at a hundred clocks and more each.
+        const bool left = warp == 0, one = elected();
         int stage = 0, issued = 0;
         unsigned phase = 0;
         bool going = true;
-        // a tile's description and its matrix's addresses are read while the tile before is copied
+        // a tile's description and its matrix's places are read while the tile before is copied
+        const auto block_of = [&](const uint16_t *at) { return int((at - p.data) / kBlockElements); };
         MuonTile ahead = tiles[min(pair, n_tiles - 1)];
-        const uint16_t *x = p.matrices[ahead.matrix].x[from], *symmetric = KIND == FACTOR ? p.matrices[ahead.matrix].gram : p.matrices[ahead.matrix].factor;
+        int x = block_of(p.matrices[ahead.matrix].x[from]), symmetric = block_of(KIND == FACTOR ? p.matrices[ahead.matrix].gram : p.matrices[ahead.matrix].factor);
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = ahead;
             const Shape z = shape_of<KIND>(w);
-            const int wide = z.columns - w.j * 4 > 2, sums = z.sums;
-            const int p0 = w.i * 4 + rank * 2, q0 = w.j * 4 + (wide ? rank * 2 : rank);
-            const int rows = max(0, min(2, z.rows - p0)), cols = max(0, min(wide ? 2 : 1, z.columns - q0));
-            // this lane's block of each stage: part, then rows of the left or columns of the right operand
-            const int part = lane / kOperandBlocks, slot = lane % kOperandBlocks;
-            const bool is_left = slot < 2, iterate = is_left ? z.left_x : z.right_x;
-            const bool mine = part < PARTS && (is_left ? slot < rows : slot - 2 < cols);
-            const int at = is_left ? p0 + slot : q0 + slot - 2, pitch = iterate && w.tall ? w.longer : w.shorter;
-            const uint16_t *base = (iterate ? x : symmetric) + part * int64_t(w.shorter) * (iterate ? w.longer : w.shorter) * kBlockElements;
+            const int sums = z.sums, wide = z.columns - w.j * 4 > 2;
+            const int at = left ? w.i * 4 + rank * 2 : w.j * 4 + (wide ? rank * 2 : rank);           // first of up to two blocks
+            const int here = max(0, left ? min(2, z.rows - at) : min(wide ? 2 : 1, z.columns - at));
+            const int both = min(4, z.rows - w.i * 4) + min(4, z.columns - w.j * 4);                // blocks that the pair copies
+            const bool iterate = left ? z.left_x : z.right_x;
+            const int pitch = iterate && w.tall ? w.longer : w.shorter, lo = w.shorter * (iterate ? w.longer : w.shorter);
+            const int base = iterate ? x : symmetric;
             ahead = tiles[min(tile + pairs, n_tiles - 1)];
             for (int k = 0; k < sums; ++k) {
                 if (!barrier_wait(shared_address(&sh.empty[stage]), phase ^ 1u, stop)) { going = false; break; }
-                const uint32_t bar = shared_address(&sh.full[stage]);
-                if (lane == 0) barrier_expect(bar, unsigned((rows + cols) * PARTS * kBlockBytes));
-                __syncwarp();
-                if (mine) {
-                    // block (at, k), or block (k, at): of a symmetric matrix, its mirror image
-                    const bool outer = is_left ? z.outer_left(w.i, k) : z.outer_right(w.j, k);
-                    const int64_t index = outer ? int64_t(at) * pitch + k : int64_t(k) * pitch + at;
-                    copy_block(stage0 + stage * kStage + (part * kOperandBlocks + slot) * kBlockBytes, base + index * kBlockElements, bar);
+                const uint32_t bar = shared_address(&sh.full[stage]), to = stage0 + stage * kStage + (left ? 0 : 2) * kBlockBytes;
+                // blocks (at, k), (at + 1, k), which are neighbours, or blocks (k, at), (k, at + 1): of a symmetric matrix, their mirror images
+                const bool outer = left ? z.outer_left(w.i, k) : z.outer_right(w.j, k);
+                const int first = base + (outer ? at * pitch + k : k * pitch + at);
+                if (one) {
+                    if (left && rank == 0) barrier_expect(bar, unsigned(both * PARTS * kBlockBytes));
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        const uint32_t into = to + part * kOperandBlocks * kBlockBytes;
+                        const int row = (first + part * lo) * 64;
+                        if (here == 2 && !outer) copy_blocks(into, &maps.pair, row, bar);
+                        else {
+                            if (here > 0) copy_blocks(into, &maps.single, row, bar);
+                            if (here > 1) copy_blocks(into + kBlockBytes, &maps.single, row + pitch * 64, bar);
+                        }
+                    }
                 }
+                __syncwarp();
                 issued++;
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 if (k == 0) {
                     const MuonMatrix &t = p.matrices[ahead.matrix];
-                    x = t.x[from];
-                    symmetric = KIND == FACTOR ? t.gram : t.factor;
+                    x = block_of(t.x[from]);
+                    symmetric = block_of(KIND == FACTOR ? t.gram : t.factor);
                 }
             }
         }
@@ -593,9 +613,9 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
             const int last = issued - 1 - s;
             const unsigned parity = unsigned(last / STAGES) & 1u;
             barrier_wait(shared_address(&sh.empty[last % STAGES]), parity, stop);
-            barrier_wait(shared_address(&sh.full[last % STAGES]), parity, stop, false);
+            if (rank == 0) barrier_wait(shared_address(&sh.full[last % STAGES]), parity, stop, false);
         }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // the whole warp runs through the loop, so that descriptors are computed once for it, and one elected thread issues
         int stage = 0, buffer = 0;
         unsigned phase = 0, buffer_phase = 0;
@@ -607,37 +627,51 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
             ahead = tiles[min(tile + pairs, n_tiles - 1)];
             const Shape z = shape_of<KIND>(w);
             const int sums = z.sums, wide = z.columns - w.j * 4 > 2;
-            for (int k = 0; k < sums; ++k) {
-                const uint32_t full = shared_address(&sh.full[stage]), other = shared_address(&sh.other[stage]);
-                if (rank == 1) {
-                    if (!barrier_wait(full, phase, stop)) { going = false; break; }
-                    if (one) barrier_arrive_first(other);
-                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-                    continue;
-                }
-                const int part = k % TURN;                     // of what is added up in tensor memory
+            for (int k = 0; k < sums; k += STEPS) {
+                // STEPS stages at a time (with three products one turn of what tensor memory adds up), the smaller products of all of
+                // them first: the fewer sums are added to an accumulator that has grown, the less is cut off
+                const int steps = min(STEPS, sums - k);
+                const bool last = k + steps == sums, begins = PRODUCTS == 3 || k == 0;
                 const uint32_t d = accumulators + unsigned(buffer) * 256u;
-                if (part == 0 && !barrier_wait(shared_address(&sh.drained[buffer]), buffer_phase ^ 1u, stop)) { going = false; break; }
-                if (!barrier_wait(full, phase, stop) || !barrier_wait(other, phase, stop)) { going = false; break; }
-                fence_after();
-                const bool outer_a = z.outer_left(w.i, k), outer_b = z.outer_right(w.j, k);
-                const uint32_t idesc = instruction(wide ? 256 : 128, outer_a, outer_b);
-                const uint32_t a0 = stage0 + stage * kStage, b0 = a0 + 2 * kBlockBytes;
-                const uint64_t a = operand(a0), b = operand(b0);
-                const uint64_t a_step = outer_a ? 2048 >> 4 : 32 >> 4, b_step = outer_b ? 2048 >> 4 : 32 >> 4;
+                if (begins && !barrier_wait(shared_address(&sh.drained[buffer]), buffer_phase ^ 1u, stop)) { going = false; break; }
+                uint64_t a[STEPS], b[STEPS], a_step[STEPS], b_step[STEPS];
+                uint32_t idesc[STEPS], empty[STEPS];
                 constexpr uint64_t lo = (kOperandBlocks * kBlockBytes) >> 4;
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    if (i >= steps) break;
+                    if (!barrier_wait(shared_address(&sh.full[stage]), phase, stop)) { going = false; break; }
+                    fence_after();
+                    const bool outer_a = z.outer_left(w.i, k + i), outer_b = z.outer_right(w.j, k + i);
+                    const uint32_t a0 = stage0 + stage * kStage;
+                    idesc[i] = instruction(wide ? 256 : 128, outer_a, outer_b);
+                    a[i] = operand(a0);
+                    b[i] = operand(a0 + 2 * kBlockBytes);
+                    a_step[i] = outer_a ? 2048 >> 4 : 32 >> 4;
+                    b_step[i] = outer_b ? 2048 >> 4 : 32 >> 4;
+                    empty[i] = shared_address(&sh.empty[stage]);
+                    if (PRODUCTS == 3 && one)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)              // hi lo, lo hi
+#pragma unroll
+                            for (int s = 0; s < 4; ++s)
+                                multiply(d, a[i] + q * lo + s * a_step[i], b[i] + (1 - q) * lo + s * b_step[i], idesc[i], i + q + s > 0);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (!going) break;
                 if (one) {
 #pragma unroll
-                    for (int q = PRODUCTS - 1; q >= 0; --q)        // hi lo, lo hi, hi hi
+                    for (int i = 0; i < STEPS; ++i) {
+                        if (i >= steps) break;
 #pragma unroll
                         for (int s = 0; s < 4; ++s)
-                            multiply(d, a + (q == 1 ? lo : 0) + s * a_step, b + (q == 2 ? lo : 0) + s * b_step, idesc, part > 0 || q < PRODUCTS - 1 || s > 0);
-                    commit(shared_address(&sh.empty[stage]));
-                    if (part == TURN - 1 || k == sums - 1) commit(shared_address(&sh.ready[buffer]));
+                            multiply(d, a[i] + s * a_step[i], b[i] + s * b_step[i], idesc[i], PRODUCTS == 3 || k + i + s > 0);
+                        commit(empty[i]);
+                    }
+                    if (PRODUCTS == 3 || last) commit(shared_address(&sh.ready[buffer]));
                 }
                 __syncwarp();
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-                if (part == TURN - 1 || k == sums - 1) {
+                if (PRODUCTS == 3 || last) {
                     buffer ^= 1;
                     if (buffer == 0) buffer_phase ^= 1u;
                 }
@@ -645,7 +679,6 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
         }
     } else if (warp >= 4) {
         const int group = warp & 3, part = (warp - 4) >> 2;      // lanes 32 group.. of tensor memory, columns 128 part..
-        char *buffer_own = raw + (stage0 - shared_address(raw)) + kStageBlocks * kBlockBytes + (warp - 4) * 4096;
         int buffer = 0;
         unsigned buffer_phase = 0;
         const auto next = [&] {
@@ -660,25 +693,20 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             if (PRODUCTS == 1) {
                 const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
-                if (KIND == FACTOR && o.blocks > 0) fill(buffer_own, lane, o.gram);
+                Raw8 gram[2];
+                if (KIND == FACTOR && o.blocks > 0) load_half(gram, o.gram, o.row, 0);
                 if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) break;
                 fence_after();
 #pragma unroll 1
                 for (int h = 0; h < 2 * o.blocks; ++h) {         // 32 columns each
                     float v[32];
-                    uint32_t words[16];
                     load_accumulators(v, from_lane + unsigned(buffer * 256 + h * 32));
                     finish_half<KIND>(v, o.factor, o.diagonal - h * 32);
                     if (KIND == FACTOR) {
-                        unstage_half(words, buffer_own, lane, h & 1);
-                        add_half(v, words, kMiddle);
+                        add_half(v, gram, o.row, kMiddle);
+                        if (h + 1 < 2 * o.blocks) load_half(gram, o.gram + ((h + 1) >> 1) * o.column, o.row, (h + 1) & 1);
                     }
-                    narrow_half(words, v, false);
-                    stage_half(buffer_own, lane, h & 1, words);
-                    if (h & 1) {
-                        flush(buffer_own, lane, o.to + (h >> 1) * o.column);
-                        if (KIND == FACTOR && h + 1 < 2 * o.blocks) fill(buffer_own, lane, o.gram + o.column);
-                    }
+                    store_half<false>(o.to + (h >> 1) * o.column, 0, o.row, h & 1, v);
                 }
                 next();
             } else {
@@ -687,7 +715,7 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[h][k] = 0.0f;
-                int turns = ((KIND == GRAM ? tiles[tile].longer : tiles[tile].shorter) + TURN - 1) / TURN;
+                int turns = ((KIND == GRAM ? tiles[tile].longer : tiles[tile].shorter) + STEPS - 1) / STEPS;
 #pragma unroll 1
                 for (; turns > 0; --turns) {
                     if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) { going = false; break; }
@@ -704,31 +732,18 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
                 if (!going) break;
                 const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {                    // blocks
-                    if (q >= o.blocks) break;
-                    uint32_t words[16];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) finish_half<KIND>(v[2 * q + h], o.factor, o.diagonal - (2 * q + h) * 32);
-                    if (KIND == FACTOR)
+                for (int h = 0; h < 4; ++h) {                    // 32 columns each
+                    if (h >= 2 * o.blocks) break;
+                    finish_half<KIND>(v[h], o.factor, o.diagonal - h * 32);
+                    if (KIND == FACTOR) {
+                        Raw8 gram[2];
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
-                            fill(buffer_own, lane, o.gram + q * o.column + s * o.lo);
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                unstage_half(words, buffer_own, lane, h);
-                                add_half(v[2 * q + h], words, kMiddle);
-                            }
+                            load_half(gram, o.gram + (h >> 1) * o.column + s * o.lo, o.row, h & 1);
+                            add_half(v[h], gram, o.row, kMiddle);
                         }
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {                // fp16, and what it leaves
-                        __syncwarp();
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            narrow_half(words, v[2 * q + h], s == 1);
-                            stage_half(buffer_own, lane, h, words);
-                        }
-                        flush(buffer_own, lane, o.to + q * o.column + s * o.lo);
                     }
+                    store_half<true>(o.to + (h >> 1) * o.column, o.lo, o.row, h & 1, v[h]);
                 }
             }
         }
@@ -743,19 +758,39 @@ product_kernel(const __grid_constant__ MuonParams p, const MuonTile *tiles, int 
     }
 }
 
-constexpr int kProductShared = kStageBlocks * kBlockBytes + 8 * 4096 + 1024;
+constexpr int kProductShared = kStageBlocks * kBlockBytes + 1024;
 
 template <int KIND, int PRODUCTS>
-int launch_product(const MuonParams &p, int from, const MuonTile *tiles, int n, int blocks, cudaStream_t st)
+int launch_product(const MuonParams &p, const Maps &maps, int from, const MuonTile *tiles, int n, int blocks, cudaStream_t st)
 {
     const auto kernel = product_kernel<KIND, PRODUCTS>;
     static std::atomic<uint64_t> raised{0};
     if (int err = allow_shared(reinterpret_cast<const void *>(kernel), kProductShared, raised)) return err;
-    kernel<<<unsigned(blocks), kProductThreads, kProductShared, st>>>(p, tiles, n, from);
+    kernel<<<unsigned(blocks), kProductThreads, kProductShared, st>>>(p, maps, tiles, n, from);
     return int(cudaGetLastError());
 }
 
 }  // namespace
+
+// The driver's function is looked up at run time: the library is not linked against the driver.
+int encode_muon_maps(void *tensor_maps, const void *data, int64_t bytes)
+{
+    void *entry = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaError_t err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found)) return int(err);
+    if (found != cudaDriverEntryPointSuccess || !entry) return int(cudaErrorNotSupported);
+    const cuuint64_t size[2] = {64, cuuint64_t(bytes / 128)}, pitch[1] = {128};
+    const cuuint32_t step[2] = {1, 1};
+    Maps &maps = *static_cast<Maps *>(tensor_maps);
+    for (cuuint32_t blocks = 1; blocks <= 2; ++blocks) {
+        const cuuint32_t box[2] = {64, 64 * blocks};
+        const CUresult err = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(entry)(
+            blocks == 1 ? &maps.single : &maps.pair, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(data), size, pitch, box, step,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (err != CUDA_SUCCESS) return int(cudaErrorInvalidValue);
+    }
+    return 0;
+}
 
 int launch_muon_clear(const MuonParams &p, int64_t chunks, void *stream)
 {
@@ -781,18 +816,19 @@ int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *strea
     return int(cudaGetLastError());
 }
 
-int launch_muon_product(const MuonParams &p, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
+int launch_muon_product(const MuonParams &p, const void *tensor_maps, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
 {
+    const Maps &maps = *static_cast<const Maps *>(tensor_maps);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int n = int(n_tiles), blocks = 2 * (n < multiprocessors / 2 ? n : multiprocessors / 2);
     if (p.products == 3) {
-        if (kind == GRAM) return launch_product<GRAM, 3>(p, from, tiles, n, blocks, st);
-        if (kind == FACTOR) return launch_product<FACTOR, 3>(p, from, tiles, n, blocks, st);
-        return launch_product<ITERATE, 3>(p, from, tiles, n, blocks, st);
+        if (kind == GRAM) return launch_product<GRAM, 3>(p, maps, from, tiles, n, blocks, st);
+        if (kind == FACTOR) return launch_product<FACTOR, 3>(p, maps, from, tiles, n, blocks, st);
+        return launch_product<ITERATE, 3>(p, maps, from, tiles, n, blocks, st);
     }
-    if (kind == GRAM) return launch_product<GRAM, 1>(p, from, tiles, n, blocks, st);
-    if (kind == FACTOR) return launch_product<FACTOR, 1>(p, from, tiles, n, blocks, st);
-    return launch_product<ITERATE, 1>(p, from, tiles, n, blocks, st);
+    if (kind == GRAM) return launch_product<GRAM, 1>(p, maps, from, tiles, n, blocks, st);
+    if (kind == FACTOR) return launch_product<FACTOR, 1>(p, maps, from, tiles, n, blocks, st);
+    return launch_product<ITERATE, 1>(p, maps, from, tiles, n, blocks, st);
 }
 
 }  // namespace qsr

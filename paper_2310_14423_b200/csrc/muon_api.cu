@@ -24,6 +24,7 @@ struct qsr_muon {
     std::vector<qsr_matrix> host;
     bool has_grads;
     int64_t launches;
+    alignas(64) unsigned char maps[256];        // two CUtensorMaps
 };
 
 namespace {
@@ -279,10 +280,16 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     p.factor = reinterpret_cast<float *>(ws + l.factor);
     p.arrived = reinterpret_cast<unsigned *>(ws + l.arrived);
     p.late = reinterpret_cast<unsigned *>(ws + l.late);
+    p.data = reinterpret_cast<const uint16_t *>(ws + l.data);
     p.one_minus_beta = float(1.0 - cfg.beta);
     p.beta = float(cfg.beta);
     p.eps = float(cfg.eps);
     p.nesterov = cfg.nesterov; p.products = cfg.products; p.iterations = cfg.iterations;
+    if (l.bytes > l.data)
+        if (int bad = encode_muon_maps(x->maps, p.data, l.bytes - l.data)) {
+            delete x;
+            return launch_status(bad);
+        }
     cudaError_t err = upload(ws + l.matrices, matrices.data(), matrices.size() * sizeof(MuonMatrix), st);
     if (err == cudaSuccess) err = upload(ws + l.grads, grads.data(), grads.size() * sizeof(void *), st);
     if (err == cudaSuccess) err = upload(ws + l.chunks, chunks.data(), chunks.size() * sizeof(MuonChunk), st);
@@ -365,7 +372,7 @@ int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale)
     for (int i = 0; i < muon->cfg.iterations; ++i)
         for (int kind = 0; kind < 3; ++kind) {
             muon->launches++;
-            if (int err = launch_muon_product(p, kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
+            if (int err = launch_muon_product(p, muon->maps, kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
                                               muon->multiprocessors, muon->stream))
                 return launch_status(err);
         }
