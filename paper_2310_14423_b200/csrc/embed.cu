@@ -57,113 +57,204 @@ __global__ void __launch_bounds__(256) lookup_kernel(const __grid_constant__ Loo
 
 // ---- sorting the tokens ----------------------------------------------------------------------------------
 
-// A stable radix sort of (token, row), lowest digits first.  Each pass takes two launches: the blocks count their digits, then every
-// block finds its places from all blocks' counts.  Tokens that are not in the vocabulary sort behind it.
+// A stable radix sort of (token, row), lowest digits first.  Few rows: all passes by one block, in shared memory.  Many: the blocks
+// count their first digits, then there is one launch for each pass, in which every block finds its places from all blocks' counts
+// and counts the next digits of what it places where they land.  Tokens that are not in the vocabulary sort behind it.
+//
+// The launches of a gradient follow one another closely: each is started before the one before it has ended and waits for that.
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 constexpr int kMaxDigit = 10;          // bits
-constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32;
-constexpr int kMaxSortBlocks = 256;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+constexpr int kSortPer = 4;            // keys that a thread holds at a time
+constexpr int kMaxSortBlocks = 128;
+constexpr int kFew = 4096, kFewThreads = 1024, kFewDigit = 8;
 
 struct SortParams {
     const int64_t *tokens;             // first pass; otherwise keys and rows
     const uint32_t *keys, *rows;
     uint32_t *keys_out, *rows_out;
-    uint32_t *counts;                  // [blocks, 1 << bits]
+    uint32_t *counts, *next_counts;    // [blocks, 1 << bits]; the next pass's, or NULL
     int64_t n, per_warp;               // per_warp: a multiple of 32
     uint32_t vocab;
-    int32_t shift, bits;
+    int32_t shift, bits, passes;
 };
 
-__device__ __forceinline__ uint32_t key_at(const SortParams &p, int64_t i)
-{
-    if (!p.tokens) return p.keys[i];
-    const int64_t t = p.tokens[i];
-    return t >= 0 && t < int64_t(p.vocab) ? uint32_t(t) : p.vocab;
-}
+__device__ __forceinline__ uint32_t key_of(int64_t token, uint32_t vocab) { return token >= 0 && token < int64_t(vocab) ? uint32_t(token) : vocab; }
+__device__ __forceinline__ uint32_t key_at(const SortParams &p, int64_t i) { return p.tokens ? key_of(p.tokens[i], p.vocab) : p.keys[i]; }
 
 __global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_constant__ SortParams p)
 {
     __shared__ uint32_t count[1 << kMaxDigit];
+    let_next_launch_start();
     const int digits = 1 << p.bits;
     for (int d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
     __syncthreads();
     const int64_t begin = int64_t(blockIdx.x) * p.per_warp * kSortWarps, end = min(p.n, begin + p.per_warp * kSortWarps);
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&count[(key_at(p, i) >> p.shift) & (digits - 1)], 1u);
+    for (int64_t i0 = begin + threadIdx.x; i0 < end; i0 += kSortPer * kSortThreads) {
+        uint32_t key[kSortPer];
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k) key[k] = i0 + k * kSortThreads < end ? key_at(p, i0 + k * kSortThreads) : 0u;
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k)
+            if (i0 + k * kSortThreads < end) atomicAdd(&count[key[k] & uint32_t(digits - 1)], 1u);
+    }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += kSortThreads) p.counts[int64_t(blockIdx.x) * digits + d] = count[d];
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+        p.counts[int64_t(blockIdx.x) * digits + d] = count[d];
+        for (int pass = 1; pass < p.passes; ++pass) p.next_counts[(int64_t(pass - 1) * gridDim.x + blockIdx.x) * digits + d] = 0;
+    }
 }
 
-// Sum over the threads before this one, of a block of kSortThreads.
+// Sum over the threads before this one.
+template <int THREADS>
 __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t *scratch)
 {
     uint32_t s = v;
+#pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         const uint32_t u = __shfl_up_sync(0xffffffffu, s, d);
         if (int(threadIdx.x & 31) >= d) s += u;
     }
     if ((threadIdx.x & 31) == 31) scratch[threadIdx.x >> 5] = s;
     __syncthreads();
-    uint32_t before = 0;
-    for (int w = 0; w < int(threadIdx.x >> 5); ++w) before += scratch[w];
-    return before + s - v;
+    uint32_t w = (threadIdx.x & 31) < THREADS / 32 ? scratch[threadIdx.x & 31] : 0u;
+    w = (threadIdx.x & 31) < (threadIdx.x >> 5) ? w : 0u;
+    return __reduce_add_sync(0xffffffffu, w) + s - v;
+}
+
+// Places of a warp's keys: `place` holds the next place of each digit for this warp and is moved on.
+__device__ __forceinline__ uint32_t take_place(uint32_t *place, uint32_t digit, bool live, int lane)
+{
+    const uint32_t same = __match_any_sync(0xffffffffu, live ? digit : 0xffffffffu);
+    const int rank = __popc(same & ((1u << lane) - 1u));
+    const uint32_t to = live ? place[digit] + uint32_t(rank) : 0u;
+    __syncwarp();
+    if (live && rank == 0) place[digit] += uint32_t(__popc(same));
+    __syncwarp();
+    return to;
 }
 
 __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_constant__ SortParams p)
 {
-    __shared__ uint32_t place[kSortWarps][1 << kMaxDigit];      // next place of each digit, warp by warp
+    extern __shared__ uint32_t places[];                        // [warps][digits]: next place of each digit, warp by warp
     __shared__ uint32_t scratch[kSortWarps];
     const int digits = 1 << p.bits, mask = digits - 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < kSortWarps << kMaxDigit; i += kSortThreads) (&place[0][0])[i] = 0;
+    uint32_t *place = places + warp * digits;
+    for (int i = threadIdx.x; i < kSortWarps * digits; i += kSortThreads) places[i] = 0;
     __syncthreads();
+    wait_for_launch_before();
+    let_next_launch_start();
     const int64_t begin = (int64_t(blockIdx.x) * kSortWarps + warp) * p.per_warp, end = min(p.n, begin + p.per_warp);
-    for (int64_t i = begin + lane; i < end; i += 32) atomicAdd(&place[warp][(key_at(p, i) >> p.shift) & mask], 1u);
-
-    // this thread's digits: consecutive ones, so that a scan over threads is one over digits
+    for (int64_t i0 = begin + lane; i0 < end; i0 += 32 * kSortPer) {
+        uint32_t key[kSortPer];
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k) key[k] = i0 + k * 32 < end ? key_at(p, i0 + k * 32) : 0u;
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k)
+            if (i0 + k * 32 < end) atomicAdd(&place[(key[k] >> p.shift) & mask], 1u);
+    }
+    // each digit's total and its share in the blocks before this one; consecutive digits to a thread, so that a scan over
+    // threads is one over digits
     constexpr int kPer = (1 << kMaxDigit) / kSortThreads;
     const int per = max(1, digits / kSortThreads), d0 = int(threadIdx.x) * per;
     uint32_t total[kPer], earlier[kPer], all = 0;
+#pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        total[k] = earlier[k] = 0;
+        uint32_t t = 0, e = 0;
         if (k < per && d0 + k < digits) {
-            uint32_t t = 0, e = 0;
-#pragma unroll 8
+#pragma unroll 16
             for (int b = 0; b < int(gridDim.x); ++b) {
-                const uint32_t c = p.counts[int64_t(b) * digits + d0 + k];
+                const uint32_t c = __ldcg(&p.counts[int64_t(b) * digits + d0 + k]);
                 t += c;
                 e += b < int(blockIdx.x) ? c : 0u;
             }
-            total[k] = t; earlier[k] = e;
         }
-        all += total[k];
+        total[k] = t; earlier[k] = e;
+        all += t;
     }
-    uint32_t at = exclusive_scan(all, scratch);
+    uint32_t at = exclusive_scan<kSortThreads>(all, scratch);
     __syncthreads();                                            // all warps have counted
+#pragma unroll
     for (int k = 0; k < kPer; ++k)
         if (k < per && d0 + k < digits) {
             uint32_t next = at + earlier[k];
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = place[w][d0 + k];
-                place[w][d0 + k] = next;
+                const uint32_t c = places[w * digits + d0 + k];
+                places[w * digits + d0 + k] = next;
                 next += c;
             }
             at += total[k];
         }
     __syncthreads();
-    for (int64_t i0 = begin; i0 < end; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const bool live = i < end;
-        const uint32_t key = live ? key_at(p, i) : 0u, row = p.tokens ? uint32_t(i) : live ? p.rows[i] : 0u;
-        const uint32_t digit = live ? (key >> p.shift) & uint32_t(mask) : 0xffffffffu;
-        const uint32_t same = __match_any_sync(0xffffffffu, digit);
-        const int rank = __popc(same & ((1u << lane) - 1u));
-        uint32_t to = 0;
-        if (live) to = place[warp][digit] + uint32_t(rank);
-        __syncwarp();
-        if (live && rank == 0) place[warp][digit] += uint32_t(__popc(same));
-        __syncwarp();
-        if (live) {
-            p.keys_out[to] = key;
-            p.rows_out[to] = row;
+    const uint32_t per_block = uint32_t(p.per_warp * kSortWarps);
+    for (int64_t i0 = begin; i0 < end; i0 += 32 * kSortPer) {
+        uint32_t key[kSortPer], row[kSortPer];
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k) {
+            const int64_t i = i0 + k * 32 + lane;
+            key[k] = i < end ? key_at(p, i) : 0u;
+            row[k] = p.tokens ? uint32_t(i) : i < end ? p.rows[i] : 0u;
         }
+#pragma unroll
+        for (int k = 0; k < kSortPer; ++k) {
+            const bool live = i0 + k * 32 + lane < end;
+            const uint32_t to = take_place(place, (key[k] >> p.shift) & uint32_t(mask), live, lane);
+            if (!live) continue;
+            p.keys_out[to] = key[k];
+            p.rows_out[to] = row[k];
+            if (p.next_counts) atomicAdd(&p.next_counts[int64_t(to / per_block) * digits + ((key[k] >> (p.shift + p.bits)) & mask)], 1u);
+        }
+    }
+}
+
+// Up to kFew rows: all passes of a sort by up to 8 bits at a time.
+__global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const __grid_constant__ SortParams p)
+{
+    extern __shared__ uint32_t few[];                            // two sets of keys and rows, then [warps][digits]
+    __shared__ uint32_t scratch[32];
+    let_next_launch_start();
+    const int n = int(p.n), digits = 1 << p.bits, mask = digits - 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t *keys[2] = {few, few + 2 * kFew}, *rows[2] = {few + kFew, few + 3 * kFew}, *places = few + 4 * kFew, *place = places + warp * digits;
+    const int per_warp = ((n + 1023) / 1024) * 32, begin = warp * per_warp, end = min(n, begin + per_warp);
+    for (int i = begin + lane; i < end; i += 32) {
+        keys[0][i] = key_of(p.tokens[i], p.vocab);
+        rows[0][i] = uint32_t(i);
+    }
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const uint32_t *key = keys[pass & 1], *row = rows[pass & 1];
+        const int shift = pass * p.bits;
+        for (int i = threadIdx.x; i < 32 * digits; i += kFewThreads) places[i] = 0;
+        __syncthreads();
+        for (int i = begin + lane; i < end; i += 32) atomicAdd(&place[(key[i] >> shift) & mask], 1u);
+        __syncthreads();
+        uint32_t total = 0;
+        if (int(threadIdx.x) < digits)
+#pragma unroll
+            for (int w = 0; w < 32; ++w) total += places[w * digits + threadIdx.x];
+        uint32_t at = exclusive_scan<kFewThreads>(total, scratch);
+        if (int(threadIdx.x) < digits)
+#pragma unroll
+            for (int w = 0; w < 32; ++w) {
+                const uint32_t c = places[w * digits + threadIdx.x];
+                places[w * digits + threadIdx.x] = at;
+                at += c;
+            }
+        __syncthreads();
+        const bool last = pass + 1 == p.passes;
+        uint32_t *key_to = last ? p.keys_out : keys[(pass & 1) ^ 1], *row_to = last ? p.rows_out : rows[(pass & 1) ^ 1];
+        for (int i0 = begin; i0 < end; i0 += 32) {
+            const int i = i0 + lane;
+            const bool live = i < end;
+            const uint32_t k = live ? key[i] : 0u, r = live ? row[i] : 0u, to = take_place(place, (k >> shift) & uint32_t(mask), live, lane);
+            if (live) {
+                key_to[to] = k;
+                row_to[to] = r;
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -178,12 +269,13 @@ struct SumParams {
     int32_t width, table_type, accumulate;
     int32_t chunk, chunks;             // sorted positions that one group of threads adds up
     int32_t lanes, tiles;              // threads of a group, parts of a row
+    int32_t join_lanes;                // the same where partial sums are joined
     int32_t sum_blocks;
     float scale;
 };
 
 constexpr int kSumThreads = 128;
-constexpr int kAhead = 8;              // rows whose loads are under way together
+constexpr int kRing = 8;               // rows that a thread has under way
 
 template <bool VEC>
 __device__ __forceinline__ void write_row(const SumParams &p, uint32_t token, const float (&s)[8], int lane, int lanes, int first)
@@ -229,10 +321,59 @@ __device__ void clear_rows(const SumParams &p, int64_t first)
     }
 }
 
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)       // of 16; the rest reads as zeros
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+// A thread's rows on their way: kRing of them by asynchronous copies into its own slots of shared memory (aligned rows), which needs
+// no registers for them and no loop that is written out; otherwise one, in registers.
+template <typename T, bool VEC>
+struct Ring {
+    static constexpr int BYTES = 8 * int(sizeof(T)), SHARED = VEC ? kRing * kSumThreads * BYTES : 16;
+    uint32_t slots;
+    int left;                                        // columns from this thread's first one on
+    Raw8 next;
+    __device__ __forceinline__ Ring(char *shared, int left_) : slots(uint32_t(__cvta_generic_to_shared(shared)) + threadIdx.x * 16), left(left_) {}
+    // row: this thread's first column of it (VEC), or the group's first column; NULL: nothing
+    __device__ __forceinline__ void issue(int slot, const T *row, int lane, int lanes)
+    {
+        if (VEC) {
+            if (row && left > 0) {
+                const uint32_t to = slots + slot * (kSumThreads * BYTES);
+#pragma unroll
+                for (int h = 0; h < BYTES / 16; ++h) {
+                    const int n = max(0, min(16, (left - h * (16 / int(sizeof(T)))) * int(sizeof(T))));
+                    copy_async(to + h * (kSumThreads * 16), row + (n > 0 ? h * (16 / int(sizeof(T))) : 0), n);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else fetch<false>(next, row, lane, lanes, 0, row ? left : 0, Kind<T>::type);
+    }
+    __device__ __forceinline__ void take(float (&x)[8], int slot)
+    {
+        if (!VEC) {
+            widen8(x, next, Kind<T>::type);
+            return;
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+        Raw8 r;
+        const uint32_t from = slots + slot * (kSumThreads * BYTES);
+#pragma unroll
+        for (int h = 0; h < BYTES / 16; ++h)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[4 * h]), "=r"(r.w[4 * h + 1]), "=r"(r.w[4 * h + 2]), "=r"(r.w[4 * h + 3])
+                         : "r"(from + h * (kSumThreads * 16)) : "memory");
+        widen8(x, r, Kind<T>::type);
+    }
+};
+
 // A group of threads adds the rows of one chunk of sorted positions, run by run; the first blocks.  The others clear rows.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ SumParams p)
 {
+    __shared__ __align__(16) char ring_memory[Ring<T, VEC>::SHARED];
+    wait_for_launch_before();
+    let_next_launch_start();
     if (int(blockIdx.x) >= p.sum_blocks) {
         const int64_t first = (int64_t(int(blockIdx.x) - p.sum_blocks) * (kSumThreads / 32) + (threadIdx.x >> 5)) * 32;
         if (first < p.vocab) clear_rows<VEC>(p, first);
@@ -243,108 +384,139 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
     const int64_t c = unit / p.tiles;
     if (c >= p.chunks) return;
     const int first = int(unit - c * p.tiles) * p.lanes * 8, width = p.width - first;
-    const int64_t begin = c * p.chunk, end = min(p.n, begin + p.chunk);
-    const uint32_t none = uint32_t(p.vocab);
-    uint32_t token = p.keys[begin];
+    const int64_t begin = c * p.chunk;
+    const int count = int(min(p.n - begin, int64_t(p.chunk)));
+    const uint32_t none = uint32_t(p.vocab), *keys = p.keys + begin, *rows = p.rows + begin;
+    uint32_t token = keys[0];
     if (token == none) return;
-    bool whole = begin == 0 || p.keys[begin - 1] != token;      // the run begins in this chunk
+    bool whole = begin == 0 || keys[-1] != token;               // the run begins in this chunk
+    const int mine = VEC ? lane * 8 : 0;
+    Ring<T, VEC> ring(ring_memory, width - mine);
+    const T *base = static_cast<const T *>(p.d_out) + first + mine;
+    const auto issue = [&](int i) { ring.issue(i & (kRing - 1), i < count ? base + int64_t(rows[i]) * p.d_out_stride : nullptr, lane, p.lanes); };
+    constexpr int AHEAD = VEC ? kRing : 1;
+    for (int i = 0; i < AHEAD; ++i) issue(i);
     float s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = 0.0f;
     float *part = p.partial + c * 2 * p.width + first;
-    auto keep = [&](int slot) {
+    const auto leave = [&](int slot) {                          // -1: the run lies in this chunk alone
+        if (slot < 0) {
+            write_row<VEC>(p, token, s, lane, p.lanes, first);
+            return;
+        }
+        float *to = part + int64_t(slot) * p.width;
+        if (VEC && p.width % 8 == 0) {
+            if (lane * 8 < width) store8(to, lane * 8, s, QSR_F32);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int col = column<VEC>(lane, p.lanes, 0, j);
-            if (col < width) part[int64_t(slot) * p.width + col] = s[j];
+            if (col < width) to[col] = s[j];
         }
     };
-    for (int64_t i0 = begin; i0 < end; i0 += kAhead) {
-        uint32_t key[kAhead];
-        Raw8 raw[kAhead];
+    for (int i = 0; i < count; ++i) {
+        const uint32_t key = keys[i];
+        if (key != token) {
+            leave(whole ? -1 : 0);
+            token = key;
+            whole = true;
+            if (key == none) break;
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const bool live = i0 + a < end;
-            key[a] = live ? p.keys[i0 + a] : none;
-            const int64_t row = live ? int64_t(p.rows[i0 + a]) : 0;
-            fetch<VEC>(raw[a], static_cast<const T *>(p.d_out) + row * p.d_out_stride + first, lane, p.lanes, 0, key[a] != none ? width : 0, Kind<T>::type);
+            for (int j = 0; j < 8; ++j) s[j] = 0.0f;
         }
+        float x[8];
+        ring.take(x, i & (kRing - 1));
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            if (key[a] != token) {
-                if (token != none) {
-                    if (whole) write_row<VEC>(p, token, s, lane, p.lanes, first);
-                    else keep(0);
-                }
-                token = key[a];
-                whole = true;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] = 0.0f;
-            }
-            float x[8];
-            widen8(x, raw[a], Kind<T>::type);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += x[j];
-        }
+        for (int j = 0; j < 8; ++j) s[j] += x[j];
+        issue(i + AHEAD);
     }
-    // a chunk shorter than a multiple of kAhead has met `none` above and has nothing left
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (token == none) return;
-    const bool goes_on = end < p.n && p.keys[end] == token;
-    if (!whole) keep(0);
-    else if (goes_on) keep(1);
-    else write_row<VEC>(p, token, s, lane, p.lanes, first);
+    const bool goes_on = begin + count < p.n && keys[count] == token;
+    leave(!whole ? 0 : goes_on ? 1 : -1);
 }
 
-// Runs over several chunks: the block of the chunk that a run begins in adds up the partial sums, warp w those of chunks w,
-// w + 8, ... behind it, and the warps' sums in their order.
+// Runs over several chunks: the block of the chunk that a run begins in adds up its partial sums, each of `ways` groups of threads those
+// of every ways-th chunk behind it, and then the groups' sums in their order.
+constexpr int kJoinThreads = 512;
 template <bool VEC>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumParams p)
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ SumParams p)
 {
-    __shared__ float shared[8][8][32];
+    __shared__ float shared[8][kJoinThreads];
+    wait_for_launch_before();
     const int64_t c = int64_t(blockIdx.x), begin = c * p.chunk, end = begin + p.chunk;
     if (end >= p.n) return;
-    const uint32_t token = p.keys[end - 1];
-    if (token == uint32_t(p.vocab) || p.keys[end] != token || (begin > 0 && p.keys[begin] == token && p.keys[begin - 1] == token)) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = int(blockIdx.y) * 256, width = p.width - first;
+    const uint32_t token = p.keys[end - 1], behind = p.keys[end], at_begin = p.keys[begin], before = begin > 0 ? p.keys[begin - 1] : uint32_t(p.vocab);
+    if (token == uint32_t(p.vocab) || behind != token || (at_begin == token && before == token)) return;
+    const int lanes = p.join_lanes, ways = kJoinThreads / lanes, lane = int(threadIdx.x) & (lanes - 1), way = int(threadIdx.x) / lanes;
+    const int first = int(blockIdx.y) * lanes * 8, width = p.width - first, col = column<VEC>(lane, lanes, 0, 0);
+    // the last chunk that begins with this token
+    int64_t lo = c + 1, hi = p.chunks - 1;
+    if (lo < hi && p.keys[(lo + 1) * p.chunk] != token) hi = lo;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        if (p.keys[mid * p.chunk] == token) lo = mid;
+        else hi = mid - 1;
+    }
     float s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = 0.0f;
-    auto add = [&](int64_t chunk, int slot) {
+    const bool aligned = VEC && p.width % 8 == 0;
+    const auto load = [&](Raw8 &r, int64_t chunk, int slot) {
         const float *part = p.partial + (chunk * 2 + slot) * p.width + first;
+        if (aligned && col < width) load32(r, part + col);
+        else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int col = column<VEC>(lane, 32, 0, j);
-            if (col < width) s[j] += part[col];
-        }
+            for (int j = 0; j < 8; ++j) r.w[j] = column<VEC>(lane, lanes, 0, j) < width ? __float_as_uint(part[column<VEC>(lane, lanes, 0, j)]) : 0u;
     };
-    if (warp == 0) add(c, 1);
-    for (int64_t k = c + 1 + warp; k < p.chunks && p.keys[k * p.chunk] == token; k += 8) add(k, 0);
+    const auto add = [&](const Raw8 &r) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) shared[warp][j][lane] = s[j];
+        for (int j = 0; j < 8; ++j) s[j] += __uint_as_float(r.w[j]);
+    };
+    if (way == 0) {
+        Raw8 r;
+        load(r, c, 1);
+        add(r);
+    }
+    for (int64_t k = c + 1 + way; k <= lo; k += 4 * ways) {
+        Raw8 r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i * ways <= lo) load(r[i], k + i * ways, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i * ways <= lo) add(r[i]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) shared[j][threadIdx.x] = s[j];
     __syncthreads();
-    if (warp) return;
-    for (int w = 1; w < 8; ++w)
+    if (way) return;
+    for (int w = 1; w < ways; ++w)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += shared[w][j][lane];
-    if (column<VEC>(lane, 32, 0, 0) < width) write_row<VEC>(p, token, s, lane, 32, first);
+        for (int j = 0; j < 8; ++j) s[j] += shared[j][w * lanes + lane];
+    if (col < width) write_row<VEC>(p, token, s, lane, lanes, first);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------
 
 constexpr int64_t kMaxWidth = int64_t(1) << 20;
 
-struct Layout { int64_t keys[2], rows[2], counts, partial, bytes; int32_t chunk, chunks, blocks, passes, bits; int64_t per_warp; };
+struct Layout { int64_t keys[2], rows[2], counts, partial, bytes; int32_t chunk, chunks, blocks, passes, bits; bool few; int64_t per_warp; };
 
 Layout layout_of(int64_t rows, int64_t vocab, int64_t width)
 {
     Layout l = {};
-    // chunks: short enough that every multiprocessor has several, at most 64 (partial sums: 1/32 of a chunk's rows)
+    // chunks: short enough that every multiprocessor has several, at most 32 (partial sums: two for a chunk's rows)
     l.chunk = 8;
-    while (l.chunk < 64 && rows / l.chunk > 148 * 8) l.chunk *= 2;
+    while (l.chunk < 32 && rows / l.chunk > 148 * 8) l.chunk *= 2;
     l.chunks = int32_t((rows + l.chunk - 1) / l.chunk);
     int bits = 1;
     while ((vocab >> bits) != 0) bits++;                        // of `vocab` itself, which stands for no token
-    l.passes = (bits + kMaxDigit - 1) / kMaxDigit;
+    l.few = rows <= kFew;
+    const int most = l.few ? kFewDigit : kMaxDigit;
+    l.passes = (bits + most - 1) / most;
     l.bits = (bits + l.passes - 1) / l.passes;
     l.blocks = int32_t(std::min<int64_t>(std::max<int64_t>(1, (rows + 2047) / 2048), kMaxSortBlocks));
     l.per_warp = std::max<int64_t>(32, ((rows + l.blocks - 1) / l.blocks + kSortThreads - 1) / kSortThreads * 32);
@@ -355,7 +527,7 @@ Layout layout_of(int64_t rows, int64_t vocab, int64_t width)
         l.keys[i] = take(rows * 4);
         l.rows[i] = take(rows * 4);
     }
-    l.counts = take(int64_t(l.blocks) * (int64_t(4) << l.bits));
+    l.counts = take(int64_t(l.passes) * l.blocks * (int64_t(4) << l.bits));
     l.partial = take(int64_t(l.chunks) * 2 * width * 4);
     l.bytes = std::max<int64_t>(at, 256);
     return l;
@@ -370,15 +542,60 @@ int launch_lookup(const LookupParams &p, cudaStream_t st)
     return int(cudaGetLastError());
 }
 
+// A launch that may start before the one before it on the stream has ended (its kernel waits for that).
+template <typename P>
+int launch_close(void (*kernel)(P), dim3 grid, unsigned threads, size_t shared, const P &p, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return int(cudaLaunchKernelEx(&cfg, kernel, p));
+}
+
 template <typename T>
 int launch_sums(SumParams p, bool vec, int64_t sum_blocks, int64_t clear_blocks, cudaStream_t st)
 {
     if (sum_blocks + clear_blocks > 0x7fffffff) return int(cudaErrorInvalidConfiguration);
     p.sum_blocks = int32_t(sum_blocks);
-    const unsigned grid = unsigned(sum_blocks + clear_blocks);
-    if (vec) sum_kernel<T, true><<<grid, kSumThreads, 0, st>>>(p);
-    else sum_kernel<T, false><<<grid, kSumThreads, 0, st>>>(p);
-    return int(cudaGetLastError());
+    return launch_close(vec ? sum_kernel<T, true> : sum_kernel<T, false>, dim3(unsigned(sum_blocks + clear_blocks)), kSumThreads, 0, p, st);
+}
+
+int launch_sort(SortParams &s, const Layout &l, uint32_t *const *keys, uint32_t *const *rows, cudaStream_t st)
+{
+    if (l.few) {
+        const size_t shared = size_t(4 * kFew + (32 << l.bits)) * 4;
+        static std::atomic<uint64_t> raised{0};
+        if (int err = allow_shared(reinterpret_cast<const void *>(sort_few_kernel), (4 * kFew + (32 << kFewDigit)) * 4, raised)) return err;
+        s.keys_out = keys[0]; s.rows_out = rows[0];
+        sort_few_kernel<<<1, kFewThreads, shared, st>>>(s);
+        s.keys = keys[0]; s.rows = rows[0];
+        return int(cudaGetLastError());
+    }
+    const int64_t counts = int64_t(l.blocks) << l.bits;
+    uint32_t *const first = s.counts;
+    s.next_counts = first + counts;
+    count_kernel<<<unsigned(l.blocks), kSortThreads, 0, st>>>(s);
+    if (cudaError_t err = cudaGetLastError()) return int(err);
+    const size_t shared = size_t(kSortWarps) * (size_t(4) << l.bits);
+    static std::atomic<uint64_t> raised{0};
+    if (int err = allow_shared(reinterpret_cast<const void *>(place_kernel), kSortWarps * (4 << kMaxDigit), raised)) return err;
+    for (int pass = 0; pass < l.passes; ++pass) {
+        s.shift = pass * l.bits;
+        s.counts = first + pass * counts;
+        s.next_counts = pass + 1 < l.passes ? s.counts + counts : nullptr;
+        s.keys_out = keys[pass & 1]; s.rows_out = rows[pass & 1];
+        if (int err = launch_close(place_kernel, dim3(unsigned(l.blocks)), kSortThreads, shared, s, st)) return err;
+        s.tokens = nullptr;
+        s.keys = s.keys_out; s.rows = s.rows_out;
+    }
+    return 0;
 }
 
 int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
@@ -393,19 +610,9 @@ int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
     SortParams s = {};
     s.tokens = a.tokens;
     s.counts = reinterpret_cast<uint32_t *>(ws + l.counts);
-    s.n = a.rows; s.per_warp = l.per_warp; s.vocab = uint32_t(a.vocab); s.bits = l.bits;
-    int at = 0;
-    for (int pass = 0; pass < l.passes && a.rows > 0; ++pass) {
-        s.shift = pass * l.bits;
-        s.keys_out = keys[at]; s.rows_out = rows[at];
-        count_kernel<<<unsigned(l.blocks), kSortThreads, 0, st>>>(s);
-        if (cudaError_t err = cudaGetLastError()) return int(err);
-        place_kernel<<<unsigned(l.blocks), kSortThreads, 0, st>>>(s);
-        if (cudaError_t err = cudaGetLastError()) return int(err);
-        s.tokens = nullptr;
-        s.keys = keys[at]; s.rows = rows[at];
-        at ^= 1;
-    }
+    s.n = a.rows; s.per_warp = l.per_warp; s.vocab = uint32_t(a.vocab); s.bits = l.bits; s.passes = l.passes;
+    if (a.rows > 0)
+        if (int err = launch_sort(s, l, keys, rows, st)) return err;
     SumParams p = {};
     p.d_out = a.out; p.d_table = a.table;
     p.keys = s.keys; p.rows = s.rows;
@@ -426,10 +633,9 @@ int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
         if (err) return err;
     }
     if (l.chunks < 2) return 0;
-    const dim3 grid(unsigned(l.chunks), unsigned((granules + 31) / 32));
-    if (vec) join_kernel<true><<<grid, 256, 0, st>>>(p);
-    else join_kernel<false><<<grid, 256, 0, st>>>(p);
-    return int(cudaGetLastError());
+    p.join_lanes = p.lanes;
+    const dim3 grid(unsigned(l.chunks), unsigned((granules + p.join_lanes - 1) / p.join_lanes));
+    return launch_close(vec ? join_kernel<true> : join_kernel<false>, grid, kJoinThreads, 0, p, st);
 }
 
 int shared_checks(const qsr_embed_args *a)

@@ -199,11 +199,12 @@ struct MuonMatrix {           // one matrix, in the device table; m <= n are its
     float scale;              // power of two that the iterate is held at
     int32_t first_chunk, chunks;
 };
-struct alignas(16) MuonTile {  // 256 x 256 elements of a product: row tile i, column tile j
-    int32_t matrix, i, j;
+struct alignas(16) MuonTile {  // of a product: row tile i (256 elements), and the columns of `width` blocks (4 or 2) from block q on
+    int32_t matrix, i, q, width;
     int32_t tall;             // of the matrix
     int32_t rows, columns;    // of the product's result, in blocks
     int32_t longer, shorter;  // the matrix's sides in blocks
+    int32_t pad[3];
 };
 struct MuonBlock { int32_t matrix, p, q, pad; };     // a block of 64 x 64
 struct MuonChunk { int32_t matrix, n; int64_t offset; };   // n consecutive elements
@@ -224,6 +225,10 @@ struct MuonParams {
 int launch_muon_clear(const MuonParams &p, int64_t chunks, void *stream);      // momentum <- 0
 int launch_muon_momentum(const MuonParams &p, int64_t chunks, void *stream);
 int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream);
+// Matrices whose steps one block each takes, all products in one launch; shared_blocks: most blocks that one of them needs, columns: of
+// tensor memory.
+constexpr int kMuonSmallBlocks = 26;
+int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, void *stream);
 int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream);
 // One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate.
 // tensor_maps: two CUtensorMaps over the blocks at MuonParams::data.

@@ -33,6 +33,13 @@ __device__ __forceinline__ float updated(const MuonParams &p, float m, float g) 
 // What is orthogonalised, from the new momentum.
 __device__ __forceinline__ float direction(const MuonParams &p, float m, float g) { return p.nesterov ? fmaf(p.beta, m - g, g) : m; }
 
+// scale / (norm + eps); nothing to scale where that is 0.
+__device__ __forceinline__ float scale_factor(float scale, double squares, float eps)
+{
+    const double length = sqrt(squares) + double(eps);
+    return length == 0.0 ? 0.0f : float(isnan(length) ? length : fmin(double(scale) / length, 3.0e38));
+}
+
 // m <- m + (1 - beta)(g - m) and the sum of squares of u, chunk by chunk; the matrix's last chunk adds them in their order.
 // Squares and sums in binary64: the norm neither overflows nor loses small elements.
 __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid_constant__ MuonParams p)
@@ -109,8 +116,7 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
     if (threadIdx.x == 0) {
         s = scratch[0];
         for (int w = 1; w < kMomentumThreads / 32; ++w) s += scratch[w];
-        const double length = sqrt(s) + double(p.eps);            // 0: nothing to scale
-        p.factor[c.matrix] = length == 0.0 ? 0.0f : float(isnan(length) ? length : fmin(double(t.scale) / length, 3.0e38));
+        p.factor[c.matrix] = scale_factor(t.scale, s, p.eps);
         p.arrived[c.matrix] = 0;
     }
 }
@@ -354,15 +360,15 @@ __device__ __forceinline__ void copy_blocks(uint32_t to, const CUtensorMap *map,
 }
 
 // Operand descriptor: rows of 128 bytes with 128-byte swizzle, groups of eight rows 1024 bytes apart; with the sum along the
-// columns of blocks ("outer"), the next 64 rows or columns of the operand are a block further.
-__device__ __forceinline__ uint64_t operand(uint32_t address)
+// columns of blocks ("outer"), the next 64 rows or columns of the operand are `next` bytes further (otherwise right behind).
+__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t next = kBlockBytes)
 {
-    return uint64_t((address >> 4) & 0x3fff) | uint64_t(kBlockBytes >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+    return uint64_t((address >> 4) & 0x3fff) | uint64_t(next >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
-// Instruction descriptor: fp16 operands, fp32 accumulators, 256 x n over the pair; outer_a / outer_b: the operand's rows in memory run along the sum.
-__device__ __forceinline__ uint32_t instruction(int n, bool outer_a, bool outer_b)
+// Instruction descriptor: fp16 operands, fp32 accumulators, m x n; outer_a / outer_b: the operand's rows in memory run along the sum.
+__device__ __forceinline__ uint32_t instruction(int m, int n, bool outer_a, bool outer_b)
 {
-    return 1u << 4 | uint32_t(outer_a) << 15 | uint32_t(outer_b) << 16 | uint32_t(n >> 3) << 17 | uint32_t(256 >> 4) << 24;
+    return 1u << 4 | uint32_t(outer_a) << 15 | uint32_t(outer_b) << 16 | uint32_t(n >> 3) << 17 | uint32_t(m >> 4) << 24;
 }
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
@@ -408,7 +414,7 @@ struct Shape {
     int rows, sums, columns;
     bool left_x, right_x, outer_left_x, outer_right_x;
     __device__ __forceinline__ bool outer_left(int i, int k) const { return left_x ? outer_left_x : i > (k >> 2); }
-    __device__ __forceinline__ bool outer_right(int j, int k) const { return right_x ? outer_right_x : j > (k >> 2); }
+    __device__ __forceinline__ bool outer_right(int q, int k) const { return right_x ? outer_right_x : (q >> 2) > (k >> 2); }
 };
 template <int KIND>
 __device__ __forceinline__ Shape shape_of(const MuonTile &w)
@@ -498,8 +504,8 @@ struct Target {
     __device__ __forceinline__ Target(const MuonTile &w, const MuonParams &p, int from, int rank, int group, int part, int lane)
     {
         const MuonMatrix &t = p.matrices[w.matrix];
-        const int bp = w.i * 4 + rank * 2 + (group >> 1), bq = w.j * 4 + part * 2;
-        blocks = bp < w.rows ? min(2, w.columns - bq) : 0;
+        const int bp = w.i * 4 + rank * 2 + (group >> 1), bq = w.q + part * 2;
+        blocks = bp < w.rows ? min(2, min(w.columns, w.q + w.width) - bq) : 0;
         row = (group & 1) * 32 + lane;
         diagonal = (bp - bq) * 64 + row;
         const int64_t at = (int64_t(bq) * w.rows + bp) * kBlockElements;
@@ -517,7 +523,7 @@ struct Shared {
     unsigned stop;
 };
 
-// A pair of blocks (one per multiprocessor) takes tiles of 256 x 256 elements, pair, + pairs, ...; each has 128 of the tile's rows and
+// A pair of blocks (one per multiprocessor) takes tiles of 256 x 256 elements (or 256 x 128), pair, + pairs, ...; each has 128 of the tile's rows and
 // 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  Two warps of
 // each block copy; one thread of the first block issues the products of both; eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
 // single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.
@@ -571,10 +577,10 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = ahead;
             const Shape z = shape_of<KIND>(w);
-            const int sums = z.sums, wide = z.columns - w.j * 4 > 2;
-            const int at = left ? w.i * 4 + rank * 2 : w.j * 4 + (wide ? rank * 2 : rank);           // first of up to two blocks
-            const int here = max(0, left ? min(2, z.rows - at) : min(wide ? 2 : 1, z.columns - at));
-            const int both = min(4, z.rows - w.i * 4) + min(4, z.columns - w.j * 4);                // blocks that the pair copies
+            const int columns = min(w.width, z.columns - w.q), sums = z.sums, wide = columns > 2;
+            const int at = left ? w.i * 4 + rank * 2 : w.q + (wide ? rank * 2 : rank);           // first of up to two blocks
+            const int here = max(0, left ? min(2, z.rows - at) : min(wide ? 2 : 1, w.q + columns - at));
+            const int both = min(4, z.rows - w.i * 4) + columns;                // blocks that the pair copies
             const bool iterate = left ? z.left_x : z.right_x;
             const int pitch = iterate && w.tall ? w.longer : w.shorter, lo = w.shorter * (iterate ? w.longer : w.shorter);
             const int base = iterate ? x : symmetric;
@@ -583,7 +589,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                 if (!barrier_wait(shared_address(&sh.empty[stage]), phase ^ 1u, stop)) { going = false; break; }
                 const uint32_t bar = shared_address(&sh.full[stage]), to = stage0 + stage * kStage + (left ? 0 : 2) * kBlockBytes;
                 // blocks (at, k), (at + 1, k), which are neighbours, or blocks (k, at), (k, at + 1): of a symmetric matrix, their mirror images
-                const bool outer = left ? z.outer_left(w.i, k) : z.outer_right(w.j, k);
+                const bool outer = left ? z.outer_left(w.i, k) : z.outer_right(w.q, k);
                 const int first = base + (outer ? at * pitch + k : k * pitch + at);
                 if (one) {
                     if (left && rank == 0) barrier_expect(bar, unsigned(both * PARTS * kBlockBytes));
@@ -626,7 +632,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
             const MuonTile w = ahead;
             ahead = tiles[min(tile + pairs, n_tiles - 1)];
             const Shape z = shape_of<KIND>(w);
-            const int sums = z.sums, wide = z.columns - w.j * 4 > 2;
+            const int sums = z.sums, wide = min(w.width, z.columns - w.q) > 2;
             for (int k = 0; k < sums; k += STEPS) {
                 // STEPS stages at a time (with three products one turn of what tensor memory adds up), the smaller products of all of
                 // them first: the fewer sums are added to an accumulator that has grown, the less is cut off
@@ -642,9 +648,9 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                     if (i >= steps) break;
                     if (!barrier_wait(shared_address(&sh.full[stage]), phase, stop)) { going = false; break; }
                     fence_after();
-                    const bool outer_a = z.outer_left(w.i, k + i), outer_b = z.outer_right(w.j, k + i);
+                    const bool outer_a = z.outer_left(w.i, k + i), outer_b = z.outer_right(w.q, k + i);
                     const uint32_t a0 = stage0 + stage * kStage;
-                    idesc[i] = instruction(wide ? 256 : 128, outer_a, outer_b);
+                    idesc[i] = instruction(256, wide ? 256 : 128, outer_a, outer_b);
                     a[i] = operand(a0);
                     b[i] = operand(a0 + 2 * kBlockBytes);
                     a_step[i] = outer_a ? 2048 >> 4 : 32 >> 4;
@@ -758,6 +764,301 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
     }
 }
 
+// ---- small matrices --------------------------------------------------------------------------------------
+
+// A whole step of one matrix by one block: its shorter side is at most 128, its longer one at most 512, and X and A fit in shared memory,
+// where they stay through all iterations (C takes the place of A, every product that of its operand, once all sums are in tensor
+// memory).  The general way takes a launch for every product, whatever its size: 18 of 4 to 9 us each, against one.
+constexpr int kSmallThreads = 512;
+
+template <int PRODUCTS>
+struct Resident {
+    static constexpr int PARTS = PRODUCTS == 3 ? 2 : 1;
+    char *x, *a;                          // blocks of X (rb x cb), then of A (mb x mb), column of blocks by column; the second part behind the first
+    int rb, cb, mb;
+    __device__ __forceinline__ int x_part() const { return rb * cb * kBlockBytes; }
+    __device__ __forceinline__ int a_part() const { return mb * mb * kBlockBytes; }
+};
+
+// Issues D = left right for all its rows, 128 at a time into `columns` columns of tensor memory each.  Operands: address of their first
+// block, bytes from a part to the next, blocks in a column (pitch), and whether the sum runs along the blocks' rows.
+struct Operand { uint32_t at; int part, pitch; bool outer; };
+template <int PRODUCTS>
+__device__ __forceinline__ void issue_all(uint32_t d, const Operand &l, const Operand &r, int row_blocks, int column_blocks, int sums)
+{
+    for (int i = 0; i < row_blocks; i += 2)
+        for (int j = 0; j < column_blocks; j += 4) {
+            const int n = min(4, column_blocks - j) * 64;
+            const uint32_t idesc = instruction(128, n, l.outer, r.outer), to = d + unsigned(i / 2 * column_blocks * 64 + j * 64);
+            const uint64_t l_step = l.outer ? 2048 >> 4 : 32 >> 4, r_step = r.outer ? 2048 >> 4 : 32 >> 4;
+            bool add = false;
+            for (int q = PRODUCTS == 3 ? 2 : 0; q >= 0; --q)           // the small products first, over the whole sum
+                for (int k = 0; k < sums; ++k) {
+                    const uint64_t a = operand(l.at + (q == 1 ? l.part : 0) + (l.outer ? i * l.pitch + k : k * l.pitch + i) * kBlockBytes,
+                                               i + 1 < row_blocks ? l.pitch * kBlockBytes : 0);       // no second block: the first once more
+                    const uint64_t b = operand(r.at + (q == 2 ? r.part : 0) + (r.outer ? j * r.pitch + k : k * r.pitch + j) * kBlockBytes, r.pitch * kBlockBytes);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(to), "l"(a + s * l_step),
+                                     "l"(b + s * r_step), "r"(idesc), "r"(uint32_t(add)) : "memory");
+                        add = true;
+                    }
+                }
+        }
+}
+
+// 32 numbers of a row, half a block's, into a block in shared memory: fp16, and what it leaves.
+template <int PRODUCTS>
+__device__ __forceinline__ void keep_half(char *block, int part, int row, int half, const float (&v)[32])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint4 hi, rest;
+        uint32_t *h = &hi.x, *l = &rest.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = v[k * 8 + 2 * i], b = v[k * 8 + 2 * i + 1];
+            h[i] = narrow2(a, b, QSR_F16);
+            if (PRODUCTS == 3) {
+                const float2 f = widen2(h[i], QSR_F16);
+                l[i] = narrow2(a - f.x, b - f.y, QSR_F16);
+            }
+        }
+        char *to = block + row * 128 + ((half * 4 + k) ^ (row & 7)) * 16;
+        *reinterpret_cast<uint4 *>(to) = hi;
+        if (PRODUCTS == 3) *reinterpret_cast<uint4 *>(to + part) = rest;
+    }
+}
+__device__ __forceinline__ void add_kept(float (&v)[32], const char *block, int row, int half, float factor)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(block + row * 128 + ((half * 4 + k) ^ (row & 7)) * 16);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = widen2(u[i], QSR_F16);
+            v[k * 8 + 2 * i] = fmaf(factor, f.x, v[k * 8 + 2 * i]);
+            v[k * 8 + 2 * i + 1] = fmaf(factor, f.y, v[k * 8 + 2 * i + 1]);
+        }
+    }
+}
+
+// A thread's eight elements of block (p, q): adjacent ones of a row, or of a column where rows are not aligned.
+template <bool WIDE>
+__device__ __forceinline__ Half eighth_of(const MuonMatrix &t, int p, int q, int &row, int &col)
+{
+    row = WIDE ? int(threadIdx.x) >> 3 : (int(threadIdx.x) >> 6) * 8;
+    col = WIDE ? (int(threadIdx.x) & 7) * 8 : int(threadIdx.x) & 63;
+    const int64_t r = p * 64 + row, c = q * 64 + col, rows = t.rows, cols = t.cols;
+    return Half{r * cols + c, WIDE ? 1 : cols, c >= cols || r >= rows ? 0 : WIDE ? 8 : int(min(rows - r, int64_t(8)))};
+}
+// Momentum, and the sum of squares of what is orthogonalised.
+template <bool WIDE>
+__device__ __forceinline__ double small_momentum(const MuonParams &p, const MuonMatrix &t, const void *grad)
+{
+    double s = 0.0;
+    const int blocks = t.rb * t.cb, rb = t.rb, gt = t.grad_type;
+    float *momentum = t.momentum;
+#pragma unroll 2
+    for (int b = 0; b < blocks; ++b) {
+        int row, col;
+        const Half o = eighth_of<WIDE>(t, b % rb, b / rb, row, col);
+        Raw8 g, m;
+        take<WIDE>(g, grad, gt, o);
+        take<WIDE>(m, momentum, QSR_F32, o);
+        float gs[8], ms[8];
+        widen<WIDE>(gs, g, gt);
+        widen<WIDE>(ms, m, QSR_F32);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = gs[k] * p.grad_scale;
+            ms[k] = updated(p, ms[k], x);
+            const double u = double(direction(p, ms[k], x));
+            if (k < o.n) s = fma(u, u, s);
+        }
+        give<WIDE>(momentum, ms, QSR_F32, o);
+    }
+    return s;
+}
+// The first iterate.
+template <bool WIDE, int PRODUCTS>
+__device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix &t, const void *grad, const Resident<PRODUCTS> &z, float factor)
+{
+    const int blocks = t.rb * t.cb, rb = t.rb, gt = t.grad_type;
+#pragma unroll 2
+    for (int b = 0; b < blocks; ++b) {
+        int row, col;
+        const Half o = eighth_of<WIDE>(t, b % rb, b / rb, row, col);
+        Raw8 g, m;
+        take<WIDE>(g, grad, gt, o);
+        take<WIDE>(m, t.momentum, QSR_F32, o);
+        float gs[8], x[8];
+        widen<WIDE>(gs, g, gt);
+        widen<WIDE>(x, m, QSR_F32);
+        uint32_t hi[4], rest[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k < o.n ? direction(p, x[k], gs[k] * p.grad_scale) * factor : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            hi[k] = narrow2(x[2 * k], x[2 * k + 1], QSR_F16);
+            const float2 f = widen2(hi[k], QSR_F16);
+            rest[k] = narrow2(x[2 * k] - f.x, x[2 * k + 1] - f.y, QSR_F16);
+        }
+        uint16_t *block = reinterpret_cast<uint16_t *>(z.x + b * kBlockBytes);
+        const int lo = z.x_part() / 2;
+        if (WIDE) {
+            uint16_t *to = block + place(row, col);
+            *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if (PRODUCTS == 3) *reinterpret_cast<uint4 *>(to + lo) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                uint16_t *to = block + place(row + k, col);
+                *to = uint16_t(hi[k / 2] >> (k % 2 * 16));
+                if (PRODUCTS == 3) to[lo] = uint16_t(rest[k / 2] >> (k % 2 * 16));
+            }
+        }
+    }
+}
+template <bool WIDE, int PRODUCTS>
+__device__ __forceinline__ void small_apply(const MuonParams &p, const MuonMatrix &t, const Resident<PRODUCTS> &z)
+{
+    const float decay = p.lr_decay * t.wd_scale, step = p.lr * t.update_scale / t.scale;
+    const int blocks = t.rb * t.cb, rb = t.rb, type = t.param_type, copy_type = t.copy_type;
+    void *param = t.param, *copy = t.copy;
+#pragma unroll 2
+    for (int b = 0; b < blocks; ++b) {
+        int row, col;
+        const Half o = eighth_of<WIDE>(t, b % rb, b / rb, row, col);
+        Raw8 old;
+        take<WIDE>(old, param, type, o);
+        const __half *block = reinterpret_cast<const __half *>(z.x + b * kBlockBytes);
+        const int lo = z.x_part() / 2;
+        float theta[8];
+        widen<WIDE>(theta, old, type);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const __half *x = block + place(WIDE ? row : row + k, WIDE ? col + k : col);
+            const float v = __half2float(x[0]) + (PRODUCTS == 3 ? __half2float(x[lo]) : 0.0f);
+            theta[k] -= fmaf(decay, theta[k], step * v);
+        }
+        give<WIDE>(param, theta, type, o);
+        if (copy_type != QSR_NONE) give<WIDE>(copy, theta, copy_type, o);
+    }
+}
+
+template <int PRODUCTS>
+__global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_constant__ MuonParams p, const int32_t *which, unsigned columns)
+{
+    extern __shared__ char raw[];
+    __shared__ double sums[kSmallThreads / 32];
+    __shared__ float factor;
+    __shared__ uint64_t done;
+    __shared__ uint32_t tensor_memory;
+    __shared__ unsigned stop_flag;
+    constexpr int PARTS = Resident<PRODUCTS>::PARTS;
+    const int matrix = which[blockIdx.x], warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const MuonMatrix t = p.matrices[matrix];
+    const void *grad = p.grads[matrix];
+    Resident<PRODUCTS> z;
+    z.rb = t.rb; z.cb = t.cb; z.mb = t.mb;
+    z.x = raw + (((shared_address(raw) + 1023u) & ~1023u) - shared_address(raw));
+    z.a = z.x + PARTS * z.x_part();
+    if (threadIdx.x == 0) {
+        barrier_init(shared_address(&done), 1);
+        stop_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&tensor_memory)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    const bool wide = wide_rows(t, grad, t.grad_type) && wide_rows(t, t.momentum, QSR_F32);
+    double s = wide ? small_momentum<true>(p, t, grad) : small_momentum<false>(p, t, grad);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) sums[warp] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = sums[0];
+        for (int w = 1; w < kSmallThreads / 32; ++w) s += sums[w];
+        factor = scale_factor(t.scale, s, p.eps);
+    }
+    __syncthreads();
+    if (wide) small_pack<true, PRODUCTS>(p, t, grad, z, factor);
+    else small_pack<false, PRODUCTS>(p, t, grad, z, factor);
+
+    const uint32_t accumulators = tensor_memory, x_at = shared_address(z.x), a_at = shared_address(z.a);
+    const bool tall = t.tall;
+    const int group = warp & 3, share = warp >> 2;          // lanes 32 group.., every fourth half of a block's columns
+    const float gram_factor = kGramScale / (t.scale * t.scale);
+    constexpr float factor_factor = kC * kFactorScale / (kGramScale * kGramScale);
+    unsigned phase = 0;
+    for (int product = 0; product < 3 * p.iterations; ++product) {
+        const int kind = product % 3;
+        const int rows = kind == ITERATE ? z.rb : z.mb, cols = kind == ITERATE ? z.cb : z.mb;
+        // what has been written to shared memory is read by the tensor cores
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_before();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            fence_after();
+            const Operand x{x_at, z.x_part(), z.rb, false}, x_outer{x_at, z.x_part(), z.rb, true}, a{a_at, z.a_part(), z.mb, false};
+            if (kind == GRAM) issue_all<PRODUCTS>(accumulators, tall ? x_outer : x, tall ? x_outer : x, z.mb, z.mb, tall ? z.rb : z.cb);
+            else if (kind == FACTOR) issue_all<PRODUCTS>(accumulators, a, a, z.mb, z.mb, z.mb);
+            else issue_all<PRODUCTS>(accumulators, tall ? x : a, tall ? a : x_outer, z.rb, z.cb, z.mb);
+            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(&done)) : "memory");
+        }
+        barrier_wait(shared_address(&done), phase, &stop_flag);
+        phase ^= 1u;
+        fence_after();
+        const int halves = (rows + 1) / 2 * cols * 2;       // 128 rows x 32 columns each
+        for (int u = share; u < halves; u += 4) {
+            const int i = u / (cols * 2) * 2 + (group >> 1), h = u % (cols * 2), j = h >> 1, half = h & 1, row = (group & 1) * 32 + lane;
+            float v[32];
+            load_accumulators(v, accumulators + unsigned(u * 32) + (unsigned(group * 32) << 16));
+            if (i >= rows) continue;
+            char *block = (kind == ITERATE ? z.x : z.a) + (j * rows + i) * kBlockBytes;
+            if (kind == GRAM) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] *= gram_factor;
+                keep_half<PRODUCTS>(block, z.a_part(), row, half, v);
+            } else if (kind == FACTOR) {
+                finish_half<FACTOR>(v, factor_factor, (i - j) * 64 + row - half * 32);
+                add_kept(v, block, row, half, kMiddle);
+                if (PRODUCTS == 3) add_kept(v, block + z.a_part(), row, half, kMiddle);
+                keep_half<PRODUCTS>(block, z.a_part(), row, half, v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] *= 1.0f / kFactorScale;
+                keep_half<PRODUCTS>(block, z.x_part(), row, half, v);
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (wide_rows(t, t.param, t.param_type) && (t.copy_type == QSR_NONE || wide_rows(t, t.copy, t.copy_type))) small_apply<true, PRODUCTS>(p, t, z);
+    else small_apply<false, PRODUCTS>(p, t, z);
+    if (threadIdx.x == 0 && stop_flag) *p.late = 1u;
+    if (warp == 0) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(accumulators), "r"(columns) : "memory");
+    }
+}
+
+template <int PRODUCTS>
+int launch_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, cudaStream_t st)
+{
+    const auto kernel = small_kernel<PRODUCTS>;
+    static std::atomic<uint64_t> raised{0};
+    // a block more than the matrix has: where an operand has an odd number of them, the products read one behind it (and nobody the result)
+    if (int err = allow_shared(reinterpret_cast<const void *>(kernel), (kMuonSmallBlocks + 1) * kBlockBytes + 1024, raised)) return err;
+    kernel<<<unsigned(n), kSmallThreads, size_t(shared_blocks + 1) * kBlockBytes + 1024, st>>>(p, which, columns);
+    return int(cudaGetLastError());
+}
+
 constexpr int kProductShared = kStageBlocks * kBlockBytes + 1024;
 
 template <int KIND, int PRODUCTS>
@@ -814,6 +1115,12 @@ int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *strea
 {
     apply_kernel<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(p, from);
     return int(cudaGetLastError());
+}
+
+int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, void *stream)
+{
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return p.products == 3 ? launch_small<3>(p, which, n, shared_blocks, columns, st) : launch_small<1>(p, which, n, shared_blocks, columns, st);
 }
 
 int launch_muon_product(const MuonParams &p, const void *tensor_maps, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)

@@ -5,7 +5,6 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
-#include <numeric>
 #include <vector>
 
 #include "checks.h"
@@ -18,9 +17,12 @@ struct qsr_muon {
     qsr::MuonParams params;                     // tables; the step's numbers are filled in by each call
     const void **grads;
     const qsr::MuonTile *half, *whole;          // tiles of a symmetric result, and of the iterate
+    const int32_t *small;                       // matrices that one block each steps
+    int32_t n_small, small_blocks;
+    unsigned small_columns;
     const qsr::ListTensor *sync_tensors;
     const qsr::ListChunk *sync_chunks;
-    int64_t chunks, blocks, n_half, n_whole, param_sync_chunks, all_sync_chunks;
+    int64_t chunks, large_chunks, blocks, n_half, n_whole, param_sync_chunks, all_sync_chunks;
     std::vector<qsr_matrix> host;
     bool has_grads;
     int64_t launches;
@@ -44,14 +46,33 @@ Sides sides_of(int64_t rows, int64_t cols)
     const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
     return Sides{m, n, ceil_div(m, 64), ceil_div(n, 64)};
 }
-int64_t half_tiles(const Sides &s)              // 256 x 256 tiles of an m x m matrix on and above the diagonal
+// Tiles of 256 rows and `width` blocks of columns: those of an m x m matrix that reach the diagonal's 256 x 256 tiles or lie above,
+// and those of an r x c matrix (blocks).
+int64_t half_tiles(const Sides &s, int64_t width)
 {
-    const int64_t t = ceil_div(s.mb, 4);
-    return t * (t + 1) / 2;
+    int64_t count = 0;
+    for (int64_t q = 0; q < s.mb; q += width) count += q / 4 + 1;
+    return count;
 }
-int64_t whole_tiles(const Sides &s) { return ceil_div(s.mb, 4) * ceil_div(s.nb, 4); }
+int64_t whole_tiles(int64_t rb, int64_t cb, int64_t width) { return ceil_div(rb, 4) * ceil_div(cb, width); }
+
+// Columns of a tile, in blocks: two instead of four where that ends earlier on `pairs` pairs of multiprocessors.  A narrow tile takes
+// about 0.65 of a wide one's time (its products take half, but it copies three quarters as much).  Two workers' ragged list, 1023 x 2047
+// the largest, takes 432 us by this rule, 515 with wide tiles alone and 457 with narrow ones; ViT-B/16's bf16 list 1661 us with wide
+// tiles, 2045 with narrow ones.
+int32_t tile_width(int64_t wide, int64_t narrow, int64_t pairs) { return ceil_div(narrow, pairs) * 65 < ceil_div(wide, pairs) * 100 ? 2 : 4; }
+
+// Blocks of shared memory and columns of tensor memory that a matrix stepped by one block needs; whether it is one.
+bool is_small(int64_t rows, int64_t cols, int64_t parts, int64_t &blocks, int64_t &columns)
+{
+    const Sides s = sides_of(rows, cols);
+    blocks = (s.mb * s.nb + s.mb * s.mb) * parts;
+    columns = std::max(s.mb, rows > cols ? (s.nb + 1) / 2 * s.mb : s.nb) * 64;
+    return s.mb <= 2 && s.nb <= 8 && blocks <= kMuonSmallBlocks;
+}
 
 struct Layout {
+    int64_t small, n_small;
     int64_t matrices, grads, chunks, blocks, half, whole, sync_tensors, sync_chunks, partial, factor, arrived, late, data, bytes;
     int64_t n_chunks, n_blocks, n_half, n_whole, n_sync, n_param_sync;
     int status;
@@ -70,11 +91,16 @@ Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t wo
         const int64_t size = rows[i] * cols[i];
         if (size == 0) continue;
         const Sides s = sides_of(rows[i], cols[i]);
+        int64_t blocks, columns;
         l.n_chunks += ceil_div(size, kChunk);
-        l.n_blocks += s.mb * s.nb;
-        l.n_half += half_tiles(s);
-        l.n_whole += whole_tiles(s);
         if (i < n / workers) l.n_param_sync += ceil_div(size, kSyncChunk);
+        if (is_small(rows[i], cols[i], parts, blocks, columns)) {
+            l.n_small++;
+            continue;
+        }
+        l.n_blocks += s.mb * s.nb;
+        l.n_half += half_tiles(s, 2);
+        l.n_whole += whole_tiles(s.mb, s.nb, 2) + whole_tiles(s.nb, s.mb, 2);       // room for either
         data += (2 * s.mb * s.nb + 2 * s.mb * s.mb) * parts * kBlockBytes;
     }
     l.n_sync = 2 * l.n_param_sync;
@@ -87,6 +113,7 @@ Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t wo
     l.blocks = take(l.n_blocks * int64_t(sizeof(MuonBlock)));
     l.half = take(l.n_half * int64_t(sizeof(MuonTile)));
     l.whole = take(l.n_whole * int64_t(sizeof(MuonTile)));
+    l.small = take(l.n_small * int64_t(sizeof(int32_t)));
     l.sync_tensors = take(2 * int64_t(n) * int64_t(sizeof(ListTensor)));
     l.sync_chunks = take(l.n_sync * int64_t(sizeof(ListChunk)));
     l.partial = take(l.n_chunks * int64_t(sizeof(double)));
@@ -170,10 +197,18 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     add(workspace, l.bytes, true);
     if (overlap(ranges)) return QSR_EINVAL;
 
+    int dev = 0, multiprocessors = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&multiprocessors, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return QSR_ECUDA;
+    }
+
     char *ws = static_cast<char *>(workspace);
     std::vector<MuonMatrix> matrices(static_cast<size_t>(n));
     std::vector<const void *> grads(static_cast<size_t>(n));
-    std::vector<MuonChunk> chunks;
+    std::vector<MuonChunk> chunks, small_chunks;
+    std::vector<int32_t> small;
+    int64_t small_blocks = 0, small_columns = 32;
     std::vector<MuonBlock> blocks;
     std::vector<MuonTile> half, whole;
     std::vector<ListTensor> sync_tensors(size_t(n) * 2);
@@ -209,13 +244,22 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
         y.wd_scale = x.wd_scale; y.update_scale = x.update_scale;
         // entries of the iterate have a root mean square of about one where it is sqrt(m n); fp16 holds up to 65504
         y.scale = float(std::ldexp(1.0, std::min(15, int(std::floor(0.5 * std::log2(double(s.m) * double(s.n)))))));
+        int64_t need, columns;
+        const bool alone = is_small(x.rows, x.cols, parts, need, columns);
+        std::vector<MuonChunk> &to = alone ? small_chunks : chunks;
+        y.first_chunk = int32_t(to.size());
+        for (int64_t o = 0; o < x.rows * x.cols; o += kChunk) to.push_back(MuonChunk{i, int32_t(std::min(kChunk, x.rows * x.cols - o)), o});
+        y.chunks = int32_t(to.size()) - y.first_chunk;
+        if (alone) {
+            small.push_back(i);
+            small_blocks = std::max(small_blocks, need);
+            while (small_columns < columns) small_columns *= 2;
+            continue;
+        }
         y.x[0] = take(s.mb * s.nb);
         y.x[1] = take(s.mb * s.nb);
         y.gram = take(s.mb * s.mb);
         y.factor = take(s.mb * s.mb);
-        y.first_chunk = int32_t(chunks.size());
-        for (int64_t o = 0; o < x.rows * x.cols; o += kChunk) chunks.push_back(MuonChunk{i, int32_t(std::min(kChunk, x.rows * x.cols - o)), o});
-        y.chunks = int32_t(chunks.size()) - y.first_chunk;
         for (int32_t a = 0; a < y.rb; ++a)
             for (int32_t b = 0; b < y.cb; ++b) blocks.push_back(MuonBlock{i, a, b, 0});
     }
@@ -223,31 +267,45 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
         for (int32_t j = 0; j < per; ++j)
             for (int64_t o = 0; o < t[j].rows * t[j].cols; o += kSyncChunk)
                 sync_chunks.push_back(ListChunk{part * per + j, int32_t(std::min(kSyncChunk, t[j].rows * t[j].cols - o)), o});
+    std::vector<int32_t> order;
+    for (int32_t i = 0; i < n; ++i)
+        if (matrices[size_t(i)].x[0]) order.push_back(i);
+    const int64_t large_chunks = int64_t(chunks.size());
+    chunks.insert(chunks.end(), small_chunks.begin(), small_chunks.end());       // momentum and norm of the others only; all are cleared
+    int64_t wide_half = 0, narrow_half = 0, wide_whole = 0, narrow_whole = 0;
+    for (int32_t i : order) {
+        const MuonMatrix &y = matrices[size_t(i)];
+        const Sides s = sides_of(y.rows, y.cols);
+        wide_half += half_tiles(s, 4);
+        narrow_half += half_tiles(s, 2);
+        wide_whole += whole_tiles(y.rb, y.cb, 4);
+        narrow_whole += whole_tiles(y.rb, y.cb, 2);
+    }
+    const int64_t pairs = std::max(1, multiprocessors / 2);
+    const int32_t half_width = tile_width(wide_half, narrow_half, pairs), whole_width = tile_width(wide_whole, narrow_whole, pairs);
     // long products first, so that short ones fill the end
-    std::vector<int32_t> order(static_cast<size_t>(n));
-    std::iota(order.begin(), order.end(), 0);
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].nb > matrices[size_t(b)].nb; });
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
-        for (int32_t j = 0; j * 4 < y.mb; ++j)
-            for (int32_t r = 0; r <= j; ++r) half.push_back(MuonTile{i, r, j, y.tall, y.mb, y.mb, y.nb, y.mb});
+        for (int32_t q = 0; q < y.mb; q += half_width)
+            for (int32_t r = 0; r <= q / 4; ++r) half.push_back(MuonTile{i, r, q, half_width, y.tall, y.mb, y.mb, y.nb, y.mb, {}});
     }
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].mb > matrices[size_t(b)].mb; });
     for (int32_t i : order) {
         const MuonMatrix &y = matrices[size_t(i)];
         // neighbours share what is longer: the iterate's tile, not the factor's
-        for (int32_t u = 0; u * 4 < y.nb; ++u)
-            for (int32_t v = 0; v * 4 < y.mb; ++v) whole.push_back(MuonTile{i, y.tall ? u : v, y.tall ? v : u, y.tall, y.rb, y.cb, y.nb, y.mb});
+        if (y.tall) {
+            for (int32_t r = 0; r * 4 < y.rb; ++r)
+                for (int32_t q = 0; q < y.cb; q += whole_width) whole.push_back(MuonTile{i, r, q, whole_width, y.tall, y.rb, y.cb, y.nb, y.mb, {}});
+        } else {
+            for (int32_t q = 0; q < y.cb; q += whole_width)
+                for (int32_t r = 0; r * 4 < y.rb; ++r) whole.push_back(MuonTile{i, r, q, whole_width, y.tall, y.rb, y.cb, y.nb, y.mb, {}});
+        }
     }
-    if (int64_t(half.size()) != l.n_half || int64_t(whole.size()) != l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
-        int64_t(sync_chunks.size()) != l.n_sync || at > ws + l.bytes)
+    if (int64_t(half.size()) > l.n_half || int64_t(whole.size()) > l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
+        int64_t(sync_chunks.size()) != l.n_sync || int64_t(small.size()) != l.n_small || at > ws + l.bytes)
         return QSR_EINVAL;                               // the tables do not fit what was reserved for them
 
-    int dev = 0, multiprocessors = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&multiprocessors, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-        cudaGetLastError();
-        return QSR_ECUDA;
-    }
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (int rc = not_capturing(st)) return rc;
     qsr_muon *x = new qsr_muon;
@@ -266,7 +324,9 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     x->whole = reinterpret_cast<const MuonTile *>(ws + l.whole);
     x->sync_tensors = reinterpret_cast<const ListTensor *>(ws + l.sync_tensors);
     x->sync_chunks = reinterpret_cast<const ListChunk *>(ws + l.sync_chunks);
-    x->chunks = l.n_chunks; x->blocks = l.n_blocks; x->n_half = l.n_half; x->n_whole = l.n_whole;
+    x->small = reinterpret_cast<const int32_t *>(ws + l.small);
+    x->n_small = int32_t(l.n_small); x->small_blocks = int32_t(small_blocks); x->small_columns = unsigned(small_columns);
+    x->chunks = l.n_chunks; x->large_chunks = large_chunks; x->blocks = l.n_blocks; x->n_half = int64_t(half.size()); x->n_whole = int64_t(whole.size());
     x->param_sync_chunks = l.n_param_sync; x->all_sync_chunks = l.n_sync;
     x->has_grads = has_grads;
     x->launches = 0;
@@ -285,7 +345,7 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     p.beta = float(cfg.beta);
     p.eps = float(cfg.eps);
     p.nesterov = cfg.nesterov; p.products = cfg.products; p.iterations = cfg.iterations;
-    if (l.bytes > l.data)
+    if (l.n_whole > 0)
         if (int bad = encode_muon_maps(x->maps, p.data, l.bytes - l.data)) {
             delete x;
             return launch_status(bad);
@@ -296,6 +356,7 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     if (err == cudaSuccess) err = upload(ws + l.blocks, blocks.data(), blocks.size() * sizeof(MuonBlock), st);
     if (err == cudaSuccess) err = upload(ws + l.half, half.data(), half.size() * sizeof(MuonTile), st);
     if (err == cudaSuccess) err = upload(ws + l.whole, whole.data(), whole.size() * sizeof(MuonTile), st);
+    if (err == cudaSuccess) err = upload(ws + l.small, small.data(), small.size() * sizeof(int32_t), st);
     if (err == cudaSuccess) err = upload(ws + l.sync_tensors, sync_tensors.data(), sync_tensors.size() * sizeof(ListTensor), st);
     if (err == cudaSuccess) err = upload(ws + l.sync_chunks, sync_chunks.data(), sync_chunks.size() * sizeof(ListChunk), st);
     if (err == cudaSuccess) err = cudaMemsetAsync(p.arrived, 0, size_t(n) * sizeof(unsigned), st);
@@ -365,8 +426,13 @@ int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale)
     p.grad_scale = float(grad_scale);
     p.lr = float(lr);
     p.lr_decay = float(lr * muon->cfg.weight_decay);
+    if (muon->n_small > 0) {
+        muon->launches++;
+        if (int err = launch_muon_small(p, muon->small, muon->n_small, muon->small_blocks, muon->small_columns, muon->stream)) return launch_status(err);
+    }
+    if (muon->large_chunks == 0) return QSR_OK;
     muon->launches++;
-    if (int err = launch_muon_momentum(p, muon->chunks, muon->stream)) return launch_status(err);
+    if (int err = launch_muon_momentum(p, muon->large_chunks, muon->stream)) return launch_status(err);
     muon->launches++;
     if (int err = launch_muon_pack(p, muon->blocks, muon->stream)) return launch_status(err);
     for (int i = 0; i < muon->cfg.iterations; ++i)

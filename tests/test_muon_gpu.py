@@ -135,7 +135,7 @@ class Case:
 
 
 SHAPES = [(1, 1), (1, 5), (7, 1), (2, 2), (1, 640), (63, 65), (64, 64), (65, 63), (128, 128), (100, 300), (300, 100), (129, 257), (256, 256), (257, 128),
-          (512, 260), (320, 700)]
+          (512, 260), (320, 700), (64, 512), (512, 65), (63, 500), (129, 64), (128, 512), (130, 300), (600, 513)]
 
 
 @pytest.mark.parametrize("products", [1, 3])
@@ -147,14 +147,14 @@ def test_one_matrix(shape, products):
 @pytest.mark.parametrize("param,grad,copy,products", [("f32", "bf16", "bf16", 3), ("f32", "f32", "f16", 1), ("bf16", "bf16", None, 1), ("f16", "f16", None, 1),
                                                       ("bf16", "f32", "f32", 3), ("f32", "f16", None, 3)])
 def test_types_and_several_matrices(param, grad, copy, products):
-    x = Case([(70, 200), (200, 70), (0, 5), (64, 256), (256, 65)], workers=2, param=param, grad=grad, copy=copy, products=products)
+    x = Case([(70, 200), (200, 70), (0, 5), (64, 256), (600, 650), (256, 65)], workers=2, param=param, grad=grad, copy=copy, products=products)
     x.step_and_compare()
     x.step_and_compare(lr=0.01, grad_scale=0.5)
-    assert x.list.qsr_muon_launch_count() == 2 * 18
+    assert x.list.qsr_muon_launch_count() == 2 * (1 + 18)
 
 
 @pytest.mark.parametrize("products", [1, 3])
-@pytest.mark.parametrize("shape", [(768, 768), (768, 2304), (2304, 768), (1023, 2047), (1537, 77), (1300, 1100)])
+@pytest.mark.parametrize("shape", [(768, 768), (768, 2304), (2304, 768), (1023, 2047), (1537, 77), (1300, 1100), (2600, 2500)])
 def test_larger_matrices(shape, products):
     Case([shape], products=products, copy="bf16").step_and_compare()
 
