@@ -445,21 +445,20 @@ template <bool VEC>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ SumParams p)
 {
     __shared__ float shared[8][kJoinThreads];
-    wait_for_launch_before();
+    // The sorted keys are those of the launch before the one before, which had ended before that one let this one start: what there is
+    // to join is found out while the sums are still being taken.
     const int64_t c = int64_t(blockIdx.x), begin = c * p.chunk, end = begin + p.chunk;
     if (end >= p.n) return;
     const uint32_t token = p.keys[end - 1], behind = p.keys[end], at_begin = p.keys[begin], before = begin > 0 ? p.keys[begin - 1] : uint32_t(p.vocab);
     if (token == uint32_t(p.vocab) || behind != token || (at_begin == token && before == token)) return;
     const int lanes = p.join_lanes, ways = kJoinThreads / lanes, lane = int(threadIdx.x) & (lanes - 1), way = int(threadIdx.x) / lanes;
     const int first = int(blockIdx.y) * lanes * 8, width = p.width - first, col = column<VEC>(lane, lanes, 0, 0);
-    // the last chunk that begins with this token
-    int64_t lo = c + 1, hi = p.chunks - 1;
-    if (lo < hi && p.keys[(lo + 1) * p.chunk] != token) hi = lo;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (p.keys[mid * p.chunk] == token) lo = mid;
-        else hi = mid - 1;
+    int64_t lo = c;                              // the last chunk that begins with this token; they follow one another
+    for (int same = 32; same == 32; lo += same) {
+        const int64_t k = lo + 1 + (threadIdx.x & 31);
+        same = __popc(__ballot_sync(0xffffffffu, k < p.chunks && p.keys[k * p.chunk] == token));
     }
+    wait_for_launch_before();
     float s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[j] = 0.0f;
