@@ -737,37 +737,27 @@ def _on_current(device: int, what: str) -> None:
         raise ValueError(f"{what} on cuda:{device}, which is not the current device")
 
 
-def _like(t, x, what: str, device: int) -> Tuple[Optional[int], int]:
-    """Address and row stride of a matrix of the shape and type of x; (None, its columns) for None."""
-    if t is None:
-        return None, x.shape[1]
-    if t.shape != x.shape or t.dtype != x.dtype:
+def _like(t, x, shape, what: str, device: int) -> Tuple[int, int]:
+    """Address and row stride of a matrix of the shape and type of x."""
+    if t.shape != shape or t.dtype != x.dtype:
         raise ValueError(f"{what}: shape and type of x are expected")
-    return t.data_ptr(), _matrix(t, t.shape, what, device)
-
-
-def _layer_norm_args(x, weight, others, mean, rstd) -> Tuple[QsrLayerNormArgs, int]:
-    """Arguments that both calls share.  others: {field: vector of the weight's type}."""
-    shape, device = x.shape, x.get_device()
-    stride = _matrix(x, shape, "x", device)
-    _on_current(device, "x is")
-    R, N = shape
-    given = [t for t in (weight, *others.values()) if t is not None]
-    a = QsrLayerNormArgs(x=x.data_ptr(), x_stride=stride, rows=R, width=N, type=_kind(x, "x"), weight_type=_kind(given[0] if given else x, "weight"),
-                         mean=_vector(mean, "mean", R, "torch.float32", device), rstd=_vector(rstd, "rstd", R, "torch.float32", device))
-    kind = _NAMES[given[0].dtype] if given else ""
-    a.weight = _vector(weight, "weight", N, kind, device)
-    for name, t in others.items():
-        setattr(a, name, _vector(t, name, N, kind, device))
-    return a, device
+    return t.data_ptr(), _matrix(t, shape, what, device)
 
 
 def qsr_layer_norm(x, y, weight=None, bias=None, mean=None, rstd=None, eps: float = 1e-5, stream: int = 0) -> None:
     """Layer norm of each row of x into y (x itself is fine), with optional weight and bias (one type), and the rows' statistics
     (float32) that qsr_layer_norm_grad takes.  Matrices may be columns of wider buffers.  All tensors are the caller's."""
-    a, device = _layer_norm_args(x, weight, {"bias": bias}, mean, rstd)
-    a.y, a.y_stride = _like(y, x, "y", device)
-    a.eps = eps
+    shape, device = x.shape, x.get_device()
+    stride = _matrix(x, shape, "x", device)
+    _on_current(device, "x is")
+    R, N = shape
+    kind = _kind(x, "x")
+    given = weight if weight is not None else bias
+    weight_kind, name = (kind, "") if given is None else (_kind(given, "weight"), _NAMES[given.dtype])
+    to, y_stride = _like(y, x, shape, "y", device)
+    a = QsrLayerNormArgs(x.data_ptr(), _vector(weight, "weight", N, name, device), _vector(bias, "bias", N, name, device),
+                         _vector(mean, "mean", R, "torch.float32", device), _vector(rstd, "rstd", R, "torch.float32", device), R, N, stride, kind,
+                         weight_kind, eps, to, y_stride)
     _check(lib().qsr_layer_norm(C.byref(a), stream), "qsr_layer_norm")
 
 
@@ -782,23 +772,31 @@ def qsr_layer_norm_workspace_bytes(rows: int, width: int) -> int:
 def qsr_layer_norm_grad(x, d_y, mean, rstd, d_x=None, weight=None, d_weight=None, d_bias=None, workspace=None, stream: int = 0) -> None:
     """Gradients of layer norm from the statistics that qsr_layer_norm wrote: of x (x or d_y may be written over), and of weight and
     bias (of the weight's type, with a workspace of qsr_layer_norm_workspace_bytes bytes), each if it is given."""
-    a, device = _layer_norm_args(x, weight, {"d_weight": d_weight, "d_bias": d_bias}, mean, rstd)
-    a.d_y, a.d_y_stride = _like(d_y, x, "d_y", device)
-    a.d_x, a.d_x_stride = _like(d_x, x, "d_x", device)
-    a.workspace, a.workspace_bytes = _workspace(workspace, device)
+    shape, device = x.shape, x.get_device()
+    stride = _matrix(x, shape, "x", device)
+    _on_current(device, "x is")
+    R, N = shape
+    kind = _kind(x, "x")
+    given = weight if weight is not None else d_weight if d_weight is not None else d_bias
+    weight_kind, name = (kind, "") if given is None else (_kind(given, "weight"), _NAMES[given.dtype])
+    dy, dy_stride = _like(d_y, x, shape, "d_y", device)
+    dx, dx_stride = (None, N) if d_x is None else _like(d_x, x, shape, "d_x", device)
+    at, nbytes = _workspace(workspace, device)
+    a = QsrLayerNormArgs(x.data_ptr(), _vector(weight, "weight", N, name, device), None, _vector(mean, "mean", R, "torch.float32", device),
+                         _vector(rstd, "rstd", R, "torch.float32", device), R, N, stride, kind, weight_kind, 0.0, None, N, dy, dy_stride, dx, dx_stride,
+                         _vector(d_weight, "d_weight", N, name, device), _vector(d_bias, "d_bias", N, name, device), at, nbytes)
     _check(lib().qsr_layer_norm_grad(C.byref(a), stream), "qsr_layer_norm_grad")
 
 
 def _embed_args(table, tokens, out, scale, table_name: str, out_name: str) -> Tuple[QsrEmbedArgs, int]:
     device = table.get_device()
-    stride, out_stride = _matrix(table, table.shape, table_name, device), _matrix(out, out.shape, out_name, device)
+    (V, N), (R, columns) = shape, out_shape = table.shape, out.shape
+    stride, out_stride = _matrix(table, shape, table_name, device), _matrix(out, out_shape, out_name, device)
     _on_current(device, f"{table_name} is")
-    (V, N), R = table.shape, out.shape[0]
-    if out.shape[1] != N:
-        raise ValueError(f"{out_name}: {out.shape[1]} columns for a table of {N}")
-    return QsrEmbedArgs(table=table.data_ptr(), tokens=_vector(tokens, "tokens", R, "torch.int64", device), out=out.data_ptr(), rows=R, vocab=V,
-                        width=N, table_stride=stride, out_stride=out_stride, table_type=_kind(table, table_name),
-                        out_type=_kind(out, out_name), scale=scale), device
+    if columns != N:
+        raise ValueError(f"{out_name}: {columns} columns for a table of {N}")
+    return QsrEmbedArgs(table.data_ptr(), _vector(tokens, "tokens", R, "torch.int64", device), out.data_ptr(), R, V, N, stride, out_stride,
+                        _kind(table, table_name), _kind(out, out_name), scale), device
 
 
 def qsr_embed(table, tokens, out, scale: float = 1.0, stream: int = 0) -> None:

@@ -317,13 +317,13 @@ __device__ __forceinline__ float spread_sum(const float (&v)[N], int lane)
     return a[0];
 }
 
-// Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take R rows at a time, each
-// thread the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which
-// leaves one partial sum for each column.  The next R rows are loaded while the present ones are worked on.
-template <typename T, bool VEC, bool FULL, int R, int THREADS>
+// Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take a row at a time, each thread
+// the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which leaves
+// one partial sum for each column.  The next DEPTH rows are loaded while one is worked on.
+template <typename T, bool VEC, bool FULL, int DEPTH, int THREADS>
 __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
 {
-    extern __shared__ float shared[];             // a group's row sums: [groups][2][warps of a group][2 R]; then column sums
+    extern __shared__ float shared[];             // a group's row sums: [groups][2][warps of a group][2]; then column sums
     constexpr int TYPE = Kind<T>::type;
     const int groups = int(blockDim.x) / lanes, group = int(threadIdx.x) / lanes, lane = int(threadIdx.x) - group * lanes;
     const int warps = lanes >> 5;
@@ -338,104 +338,88 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
             dw[j] = db[j] = make_float2(0.0f, 0.0f);
         }
     }
-    const float inverse = p.inverse;
-    Raw8 next_x[R], next_dy[R];
-    float next_mean[R], next_rstd[R];
-    const auto load = [&](int64_t row0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const bool live = row0 + r < p.rows && mine;
-            const int64_t row = live ? row0 + r : 0;
-            fetch_row<VEC, FULL>(next_x[r], row_of<T>(p.x, row, p.x_stride), lane, lanes, 0, live, p.width, TYPE);
-            fetch_row<VEC, FULL>(next_dy[r], row_of<T>(p.dy, row, p.dy_stride), lane, lanes, 0, live, p.width, TYPE);
-            next_mean[r] = live ? p.mean[row] : 0.0f;
-            next_rstd[r] = live ? p.rstd[row] : 0.0f;
-        }
+    Raw8 x[DEPTH], dy[DEPTH];
+    float means[DEPTH], rstds[DEPTH];
+    const auto load = [&](int i, int64_t row) {
+        const bool live = row < p.rows && mine;
+        const int64_t r = live ? row : 0;
+        fetch_row<VEC, FULL>(x[i], row_of<T>(p.x, r, p.x_stride), lane, lanes, 0, live, p.width, TYPE);
+        fetch_row<VEC, FULL>(dy[i], row_of<T>(p.dy, r, p.dy_stride), lane, lanes, 0, live, p.width, TYPE);
+        means[i] = live ? p.mean[r] : 0.0f;
+        rstds[i] = live ? p.rstd[r] : 0.0f;
     };
     int turn = 0;
-    const int64_t step = int64_t(gridDim.x) * groups * R;
-    load(int64_t(blockIdx.x) * groups * R + group * R);
-    for (int64_t base = int64_t(blockIdx.x) * groups * R; base < p.rows; base += step) {
-        const int64_t row0 = base + group * R;
-        Raw8 x[R], dy[R];
-        float mean[R], rstd[R];
+    const int64_t step = int64_t(gridDim.x) * groups;
+    int64_t row = int64_t(blockIdx.x) * groups + group;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            x[r] = next_x[r]; dy[r] = next_dy[r];
-            mean[r] = next_mean[r]; rstd[r] = next_rstd[r];
-        }
-        load(row0 + step);
-        float s[2 * R];
+    for (int i = 0; i < DEPTH; ++i) load(i, row + i * step);
+    for (int64_t base = int64_t(blockIdx.x) * groups; base < p.rows; base += DEPTH * step) {       // `base`: the same for the block
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int i = 0; i < DEPTH; ++i, row += step) {
             Pairs a, d;
-            widen_pairs(a, x[r], TYPE);
-            widen_pairs(d, dy[r], TYPE);
-            const float2 minus = make_float2(-mean[r], -mean[r]), times = make_float2(rstd[r], rstd[r]);
+            widen_pairs(a, x[i], TYPE);
+            widen_pairs(d, dy[i], TYPE);
+            const float mean = means[i], rstd = rstds[i];
+            load(i, row + DEPTH * step);
+            const float2 minus = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
             float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float2 hat = mul2(add2(a.v[j], minus), times);
+                a.v[j] = add2(a.v[j], minus);
+                float2 hat = mul2(a.v[j], times);
                 if (!FULL) {       // beyond the row both are zero: a finite statistic gives no sum, one that is not finite is kept out
                     if (column<VEC>(lane, lanes, 0, 2 * j) >= p.width) hat.x = 0.0f;
                     if (column<VEC>(lane, lanes, 0, 2 * j + 1) >= p.width) hat.y = 0.0f;
                 }
                 dw[j] = fma2(d.v[j], hat, dw[j]);
                 db[j] = add2(db[j], d.v[j]);
-                const float2 g = mul2(d.v[j], w[j]);
-                s1 = add2(s1, g);
-                s2 = fma2(g, hat, s2);
+                d.v[j] = mul2(d.v[j], w[j]);
+                s1 = add2(s1, d.v[j]);
+                s2 = fma2(d.v[j], hat, s2);
             }
-            s[2 * r] = s1.x + s1.y;
-            s[2 * r + 1] = s2.x + s2.y;
-        }
-        if (!p.dx) continue;
-        if (lanes >= 32) {
-            const float v = spread_sum(s, lane & 31);
-            if (lanes == 32) {
-#pragma unroll
-                for (int i = 0; i < 2 * R; ++i) s[i] = __shfl_sync(0xffffffffu, v, i * (32 / (2 * R)));
-            } else {
-                float *at = shared + (group * 2 + turn) * warps * 2 * R;
-                turn ^= 1;
-                if ((lane & (32 / (2 * R) - 1)) == 0) at[(lane >> 5) * 2 * R + (lane & 31) / (32 / (2 * R))] = v;
-                group_barrier(group, lanes);
-                if (warps <= 4) {
-#pragma unroll
-                    for (int i = 0; i < 2 * R; ++i) s[i] = 0.0f;
-                    for (int u = 0; u < warps; ++u)
-#pragma unroll
-                        for (int i = 0; i < 2 * R; ++i) s[i] += at[u * 2 * R + i];
+            if (!p.dx) continue;
+            float s[2] = {s1.x + s1.y, s2.x + s2.y};
+            if (lanes >= 32) {
+                const float v = spread_sum(s, lane & 31);
+                if (lanes == 32) {
+                    s[0] = __shfl_sync(0xffffffffu, v, 0);
+                    s[1] = __shfl_sync(0xffffffffu, v, 16);
                 } else {
-                    const int u = lane & 31;
-#pragma unroll
-                    for (int i = 0; i < 2 * R; ++i) s[i] = u < warps ? at[u * 2 * R + i] : 0.0f;
-                    const float all = spread_sum(s, u);
-#pragma unroll
-                    for (int i = 0; i < 2 * R; ++i) s[i] = __shfl_sync(0xffffffffu, all, i * (32 / (2 * R)));
+                    float *at = shared + (group * 2 + turn) * warps * 2;
+                    turn ^= 1;
+                    if ((lane & 15) == 0) at[(lane >> 5) * 2 + ((lane >> 4) & 1)] = v;
+                    group_barrier(group, lanes);
+                    if (warps <= 4) {
+                        s[0] = s[1] = 0.0f;
+                        for (int u = 0; u < warps; ++u) {
+                            s[0] += at[u * 2];
+                            s[1] += at[u * 2 + 1];
+                        }
+                    } else {
+                        const int u = lane & 31;
+                        s[0] = u < warps ? at[u * 2] : 0.0f;
+                        s[1] = u < warps ? at[u * 2 + 1] : 0.0f;
+                        const float all = spread_sum(s, u);
+                        s[0] = __shfl_sync(0xffffffffu, all, 0);
+                        s[1] = __shfl_sync(0xffffffffu, all, 16);
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    for (int e = lanes >> 1; e; e >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], e);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2 * R; ++i)
-                for (int d = lanes >> 1; d; d >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], d);
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (row0 + r >= p.rows || !mine) continue;
-            Pairs a, d;
-            widen_pairs(a, x[r], TYPE);
-            widen_pairs(d, dy[r], TYPE);
-            const float c1 = -s[2 * r] * inverse, c2 = -s[2 * r + 1] * inverse * rstd[r];
-            const float2 minus = make_float2(-mean[r], -mean[r]), times = make_float2(rstd[r], rstd[r]), along = make_float2(c2, c2), level = make_float2(c1, c1);
+            if (row >= p.rows || !mine) continue;
+            const float c1 = -s[0] * p.inverse, c2 = -s[1] * p.inverse * rstd;
+            const float2 along = make_float2(c2, c2), level = make_float2(c1, c1);
             float out[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 v = mul2(fma2(add2(a.v[j], minus), along, fma2(d.v[j], w[j], level)), times);
+                const float2 v = mul2(fma2(a.v[j], along, add2(d.v[j], level)), times);
                 out[2 * j] = v.x;
                 out[2 * j + 1] = v.y;
             }
-            put_row<VEC, FULL>(row_of<T>(p.dx, row0 + r, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+            put_row<VEC, FULL>(row_of<T>(p.dx, row, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
         }
     }
     if (!p.partial) return;
@@ -607,16 +591,16 @@ int launch_backward(const Params &p, void *dw, void *db, cudaStream_t st)
 {
     int blocks = 0;
     if (p.granules <= kMaxThreads) {
-        // groups enough for 768 threads, one block on a multiprocessor; rows at a time: as many as their registers allow
-        constexpr int R = sizeof(T) == 4 ? 1 : 2;
+        // as many groups as fit 768 threads, one block on a multiprocessor; rows that need more threads have fewer registers
+        constexpr int DEPTH = 1;
         const int lanes = p.granules <= 32 ? power_of_two(p.granules) : (p.granules + 31) / 32 * 32;
         const int groups = std::max(1, lanes <= 32 ? 512 / lanes : std::min(768 / lanes, 15)), threads = groups * lanes;
-        const int64_t turns = (p.rows + int64_t(groups) * R - 1) / (int64_t(groups) * R);
-        blocks = int(std::min<int64_t>(turns, kBlocks));
-        const size_t sums = size_t(groups) * 2 * size_t(lanes / 32) * 2 * size_t(R) * 4, columns = groups > 1 ? size_t(threads) * 8 * 4 : 0;
+        blocks = int(std::min<int64_t>((p.rows + groups - 1) / groups, kBlocks));
+        const size_t sums = size_t(groups) * size_t(lanes / 32) * 16, columns = groups > 1 ? size_t(threads) * 8 * 4 : 0;
         const bool full = VEC && p.width == lanes * 8;
         const auto kernel = threads > 768 ? (full ? backward_kernel<T, true, true, 1, kMaxThreads> : backward_kernel<T, VEC, false, 1, kMaxThreads>)
-                                          : (full ? backward_kernel<T, true, true, R, 768> : backward_kernel<T, VEC, false, R, 768>);
+                            : threads > 640 ? (full ? backward_kernel<T, true, true, DEPTH, 768> : backward_kernel<T, VEC, false, DEPTH, 768>)
+                                            : (full ? backward_kernel<T, true, true, DEPTH, 640> : backward_kernel<T, VEC, false, DEPTH, 640>);
         kernel<<<unsigned(blocks), unsigned(threads), std::max(sums, columns), st>>>(p, lanes);
     } else {
         if (p.partial) {
