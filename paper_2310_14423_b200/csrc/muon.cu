@@ -23,6 +23,10 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 // maximum on [0, 1.2025]), so entries of A stay below 1.45 and those of C, whose eigenvalues lie in [0.63, 3.45], below 3.45.
 constexpr float kGramScale = 16384.0f, kFactorScale = 16384.0f;
 
+// The launches of a step follow one another closely: each is started before the one before it has ended, and waits for that.
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---- momentum and norms ----------------------------------------------------------------------------------
 
 __device__ __forceinline__ bool address_aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -46,6 +50,7 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
 {
     __shared__ double scratch[kMomentumThreads / 32];
     __shared__ bool last;
+    let_next_launch_start();
     const MuonChunk c = p.chunks[blockIdx.x];
     const MuonMatrix &t = p.matrices[c.matrix];
     const void *grad = p.grads[c.matrix];
@@ -229,9 +234,11 @@ __device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix
 // The blocks are taken from the last one on: the end of what the launch before has written is still in the second-level cache.
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonParams p)
 {
+    let_next_launch_start();
     const MuonBlock b = p.blocks[gridDim.x - 1 - blockIdx.x];
     const MuonMatrix &t = p.matrices[b.matrix];
     const void *grad = p.grads[b.matrix];
+    wait_for_launch_before();
     if (wide_rows(t, grad, t.grad_type) && wide_rows(t, t.momentum, QSR_F32)) pack_block<true>(p, t, b, grad);
     else pack_block<false>(p, t, b, grad);
 }
@@ -285,6 +292,7 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Muon
 {
     const MuonBlock b = p.blocks[gridDim.x - 1 - blockIdx.x];
     const MuonMatrix &t = p.matrices[b.matrix];
+    wait_for_launch_before();
     if (wide_rows(t, t.param, t.param_type) && (t.copy_type == QSR_NONE || wide_rows(t, t.copy, t.copy_type))) apply_block<true>(p, t, b, from);
     else apply_block<false>(p, t, b, from);
 }
@@ -540,6 +548,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = int(blockIdx.x & 1), pair = int(blockIdx.x >> 1), pairs = int(gridDim.x >> 1);
     volatile unsigned *stop = &sh.stop;
+    let_next_launch_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             barrier_init(shared_address(&sh.full[i]), 1);
@@ -562,6 +571,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
     pair_sync();
     fence_after();
     const uint32_t accumulators = sh.tensor_memory;
+    wait_for_launch_before();
 
     if (warp == 0 || warp == 3) {
         // Copies: warp 0 those of the left operand, warp 3 those of the right one.  Everything is the same for the whole warp and one elected
@@ -784,26 +794,33 @@ struct Resident {
 // block, bytes from a part to the next, blocks in a column (pitch), and whether the sum runs along the blocks' rows.
 struct Operand { uint32_t at; int part, pitch; bool outer; };
 template <int PRODUCTS>
-__device__ __forceinline__ void issue_all(uint32_t d, const Operand &l, const Operand &r, int row_blocks, int column_blocks, int sums)
+__device__ __forceinline__ void issue_all(bool one, uint32_t d, const Operand &l, const Operand &r, int row_blocks, int column_blocks, int sums)
 {
+    const uint64_t l_step = l.outer ? 2048 >> 4 : 32 >> 4, r_step = r.outer ? 2048 >> 4 : 32 >> 4;                       // 16 along the sum
+    const uint64_t l_next = uint64_t(l.outer ? 1 : l.pitch) * (kBlockBytes >> 4), r_next = uint64_t(r.outer ? 1 : r.pitch) * (kBlockBytes >> 4);      // 64
     for (int i = 0; i < row_blocks; i += 2)
         for (int j = 0; j < column_blocks; j += 4) {
-            const int n = min(4, column_blocks - j) * 64;
-            const uint32_t idesc = instruction(128, n, l.outer, r.outer), to = d + unsigned(i / 2 * column_blocks * 64 + j * 64);
-            const uint64_t l_step = l.outer ? 2048 >> 4 : 32 >> 4, r_step = r.outer ? 2048 >> 4 : 32 >> 4;
-            bool add = false;
-            for (int q = PRODUCTS == 3 ? 2 : 0; q >= 0; --q)           // the small products first, over the whole sum
-                for (int k = 0; k < sums; ++k) {
-                    const uint64_t a = operand(l.at + (q == 1 ? l.part : 0) + (l.outer ? i * l.pitch + k : k * l.pitch + i) * kBlockBytes,
-                                               i + 1 < row_blocks ? l.pitch * kBlockBytes : 0);       // no second block: the first once more
-                    const uint64_t b = operand(r.at + (q == 2 ? r.part : 0) + (r.outer ? j * r.pitch + k : k * r.pitch + j) * kBlockBytes, r.pitch * kBlockBytes);
+            const uint32_t idesc = instruction(128, min(4, column_blocks - j) * 64, l.outer, r.outer), to = d + unsigned(i / 2 * column_blocks * 64 + j * 64);
+            // no second block of 64 rows: the first once more
+            const uint64_t l0 = operand(l.at + (l.outer ? i * l.pitch : i) * kBlockBytes, i + 1 < row_blocks ? l.pitch * kBlockBytes : 0);
+            const uint64_t r0 = operand(r.at + (r.outer ? j * r.pitch : j) * kBlockBytes, r.pitch * kBlockBytes);
+            uint32_t add = 0;
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(to), "l"(a + s * l_step),
-                                     "l"(b + s * r_step), "r"(idesc), "r"(uint32_t(add)) : "memory");
-                        add = true;
-                    }
+            for (int q = PRODUCTS == 3 ? 2 : 0; q >= 0; --q) {         // the small products first, over the whole sum
+                uint64_t a = l0 + (q == 1 ? uint64_t(l.part >> 4) : 0), b = r0 + (q == 2 ? uint64_t(r.part >> 4) : 0);
+                for (int k = 0; k < sums; ++k) {
+                    if (one)
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(to), "l"(a + s * l_step),
+                                         "l"(b + s * r_step), "r"(idesc), "r"(add) : "memory");
+                            add = 1;
+                        }
+                    a += l_next;
+                    b += r_next;
                 }
+            }
+            __syncwarp();
         }
 }
 
@@ -853,15 +870,45 @@ __device__ __forceinline__ Half eighth_of(const MuonMatrix &t, int p, int q, int
     const int64_t r = p * 64 + row, c = q * 64 + col, rows = t.rows, cols = t.cols;
     return Half{r * cols + c, WIDE ? 1 : cols, c >= cols || r >= rows ? 0 : WIDE ? 8 : int(min(rows - r, int64_t(8)))};
 }
-// Momentum, and the sum of squares of what is orthogonalised.
+// Momentum, and the sum of squares of what is orthogonalised, which is kept for the first kKept blocks.
+constexpr int kKept = 4;
+struct Kept { float u[kKept][8]; };
 template <bool WIDE>
-__device__ __forceinline__ double small_momentum(const MuonParams &p, const MuonMatrix &t, const void *grad)
+__device__ __forceinline__ double small_momentum(const MuonParams &p, const MuonMatrix &t, const void *grad, Kept &kept)
 {
     double s = 0.0;
     const int blocks = t.rb * t.cb, rb = t.rb, gt = t.grad_type;
     float *momentum = t.momentum;
+    {
+        Half o[kKept];
+        Raw8 g[kKept], m[kKept];
+        int bp = 0, bq = 0;
+#pragma unroll
+        for (int b = 0; b < kKept; ++b) {
+            int row, col;
+            o[b] = eighth_of<WIDE>(t, bp, bq, row, col);
+            if (b >= blocks) o[b].n = 0;
+            take<WIDE>(g[b], grad, gt, o[b]);
+            take<WIDE>(m[b], momentum, QSR_F32, o[b]);
+            if (++bp == rb) { bp = 0; ++bq; }
+        }
+#pragma unroll
+        for (int b = 0; b < kKept; ++b) {
+            float gs[8], ms[8];
+            widen<WIDE>(gs, g[b], gt);
+            widen<WIDE>(ms, m[b], QSR_F32);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x = gs[k] * p.grad_scale;
+                ms[k] = updated(p, ms[k], x);
+                kept.u[b][k] = k < o[b].n ? direction(p, ms[k], x) : 0.0f;
+                s = fma(double(kept.u[b][k]), double(kept.u[b][k]), s);
+            }
+            give<WIDE>(momentum, ms, QSR_F32, o[b]);
+        }
+    }
 #pragma unroll 2
-    for (int b = 0; b < blocks; ++b) {
+    for (int b = kKept; b < blocks; ++b) {
         int row, col;
         const Half o = eighth_of<WIDE>(t, b % rb, b / rb, row, col);
         Raw8 g, m;
@@ -883,12 +930,46 @@ __device__ __forceinline__ double small_momentum(const MuonParams &p, const Muon
 }
 // The first iterate.
 template <bool WIDE, int PRODUCTS>
-__device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix &t, const void *grad, const Resident<PRODUCTS> &z, float factor)
+__device__ __forceinline__ void pack_eighth(const Resident<PRODUCTS> &z, int b, int row, int col, const float (&x)[8])
+{
+    uint32_t hi[4], rest[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        hi[k] = narrow2(x[2 * k], x[2 * k + 1], QSR_F16);
+        const float2 f = widen2(hi[k], QSR_F16);
+        rest[k] = narrow2(x[2 * k] - f.x, x[2 * k + 1] - f.y, QSR_F16);
+    }
+    uint16_t *block = reinterpret_cast<uint16_t *>(z.x + b * kBlockBytes);
+    const int lo = z.x_part() / 2;
+    if (WIDE) {
+        uint16_t *to = block + place(row, col);
+        *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (PRODUCTS == 3) *reinterpret_cast<uint4 *>(to + lo) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            uint16_t *to = block + place(row + k, col);
+            *to = uint16_t(hi[k / 2] >> (k % 2 * 16));
+            if (PRODUCTS == 3) to[lo] = uint16_t(rest[k / 2] >> (k % 2 * 16));
+        }
+    }
+}
+template <bool WIDE, int PRODUCTS>
+__device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix &t, const void *grad, const Resident<PRODUCTS> &z, float factor, const Kept &kept)
 {
     const int blocks = t.rb * t.cb, rb = t.rb, gt = t.grad_type;
+    int row, col;
+    eighth_of<WIDE>(t, 0, 0, row, col);
+#pragma unroll
+    for (int b = 0; b < kKept; ++b) {
+        if (b >= blocks) break;
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = kept.u[b][k] == 0.0f ? 0.0f : kept.u[b][k] * factor;        // padding stays zero, whatever the factor
+        pack_eighth<WIDE, PRODUCTS>(z, b, row, col, x);
+    }
 #pragma unroll 2
-    for (int b = 0; b < blocks; ++b) {
-        int row, col;
+    for (int b = kKept; b < blocks; ++b) {
         const Half o = eighth_of<WIDE>(t, b % rb, b / rb, row, col);
         Raw8 g, m;
         take<WIDE>(g, grad, gt, o);
@@ -896,29 +977,9 @@ __device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix
         float gs[8], x[8];
         widen<WIDE>(gs, g, gt);
         widen<WIDE>(x, m, QSR_F32);
-        uint32_t hi[4], rest[4];
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = k < o.n ? direction(p, x[k], gs[k] * p.grad_scale) * factor : 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            hi[k] = narrow2(x[2 * k], x[2 * k + 1], QSR_F16);
-            const float2 f = widen2(hi[k], QSR_F16);
-            rest[k] = narrow2(x[2 * k] - f.x, x[2 * k + 1] - f.y, QSR_F16);
-        }
-        uint16_t *block = reinterpret_cast<uint16_t *>(z.x + b * kBlockBytes);
-        const int lo = z.x_part() / 2;
-        if (WIDE) {
-            uint16_t *to = block + place(row, col);
-            *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            if (PRODUCTS == 3) *reinterpret_cast<uint4 *>(to + lo) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                uint16_t *to = block + place(row + k, col);
-                *to = uint16_t(hi[k / 2] >> (k % 2 * 16));
-                if (PRODUCTS == 3) to[lo] = uint16_t(rest[k / 2] >> (k % 2 * 16));
-            }
-        }
+        pack_eighth<WIDE, PRODUCTS>(z, b, row, col, x);
     }
 }
 template <bool WIDE, int PRODUCTS>
@@ -976,7 +1037,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     const bool wide = wide_rows(t, grad, t.grad_type) && wide_rows(t, t.momentum, QSR_F32);
-    double s = wide ? small_momentum<true>(p, t, grad) : small_momentum<false>(p, t, grad);
+    Kept kept;
+    double s = wide ? small_momentum<true>(p, t, grad, kept) : small_momentum<false>(p, t, grad, kept);
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
     if (lane == 0) sums[warp] = s;
@@ -987,8 +1049,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         factor = scale_factor(t.scale, s, p.eps);
     }
     __syncthreads();
-    if (wide) small_pack<true, PRODUCTS>(p, t, grad, z, factor);
-    else small_pack<false, PRODUCTS>(p, t, grad, z, factor);
+    if (wide) small_pack<true, PRODUCTS>(p, t, grad, z, factor, kept);
+    else small_pack<false, PRODUCTS>(p, t, grad, z, factor, kept);
 
     const uint32_t accumulators = tensor_memory, x_at = shared_address(z.x), a_at = shared_address(z.a);
     const bool tall = t.tall;
@@ -1003,20 +1065,25 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         fence_before();
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (warp == 0) {                                    // one elected thread issues, the whole warp computes with it
             fence_after();
+            const bool one = elected();
             const Operand x{x_at, z.x_part(), z.rb, false}, x_outer{x_at, z.x_part(), z.rb, true}, a{a_at, z.a_part(), z.mb, false};
-            if (kind == GRAM) issue_all<PRODUCTS>(accumulators, tall ? x_outer : x, tall ? x_outer : x, z.mb, z.mb, tall ? z.rb : z.cb);
-            else if (kind == FACTOR) issue_all<PRODUCTS>(accumulators, a, a, z.mb, z.mb, z.mb);
-            else issue_all<PRODUCTS>(accumulators, tall ? x : a, tall ? a : x_outer, z.rb, z.cb, z.mb);
-            asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(&done)) : "memory");
+            if (kind == GRAM) issue_all<PRODUCTS>(one, accumulators, tall ? x_outer : x, tall ? x_outer : x, z.mb, z.mb, tall ? z.rb : z.cb);
+            else if (kind == FACTOR) issue_all<PRODUCTS>(one, accumulators, a, a, z.mb, z.mb, z.mb);
+            else issue_all<PRODUCTS>(one, accumulators, tall ? x : a, tall ? a : x_outer, z.rb, z.cb, z.mb);
+            if (one) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(&done)) : "memory");
+            __syncwarp();
         }
         barrier_wait(shared_address(&done), phase, &stop_flag);
         phase ^= 1u;
         fence_after();
-        const int halves = (rows + 1) / 2 * cols * 2;       // 128 rows x 32 columns each
-        for (int u = share; u < halves; u += 4) {
-            const int i = u / (cols * 2) * 2 + (group >> 1), h = u % (cols * 2), j = h >> 1, half = h & 1, row = (group & 1) * 32 + lane;
+        const int row = (group & 1) * 32 + lane;
+        int first = 0, h = share;                           // 128 rows from block `first` on, x 32 columns each
+        for (int u = share;; u += 4, h += 4) {
+            for (; h >= cols * 2; h -= cols * 2) first += 2;
+            if (first >= rows) break;
+            const int i = first + (group >> 1), j = h >> 1, half = h & 1;
             float v[32];
             load_accumulators(v, accumulators + unsigned(u * 32) + (unsigned(group * 32) << 16));
             if (i >= rows) continue;
@@ -1059,6 +1126,22 @@ int launch_small(const MuonParams &p, const int32_t *which, int n, int shared_bl
     return int(cudaGetLastError());
 }
 
+template <typename... A>
+int launch_close(void (*kernel)(A...), unsigned blocks, unsigned threads, size_t shared, cudaStream_t st, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return int(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
+
 constexpr int kProductShared = kStageBlocks * kBlockBytes + 1024;
 
 template <int KIND, int PRODUCTS>
@@ -1067,8 +1150,7 @@ int launch_product(const MuonParams &p, const Maps &maps, int from, const MuonTi
     const auto kernel = product_kernel<KIND, PRODUCTS>;
     static std::atomic<uint64_t> raised{0};
     if (int err = allow_shared(reinterpret_cast<const void *>(kernel), kProductShared, raised)) return err;
-    kernel<<<unsigned(blocks), kProductThreads, kProductShared, st>>>(p, maps, tiles, n, from);
-    return int(cudaGetLastError());
+    return launch_close(kernel, unsigned(blocks), kProductThreads, kProductShared, st, p, maps, tiles, n, from);
 }
 
 }  // namespace
@@ -1107,14 +1189,12 @@ int launch_muon_momentum(const MuonParams &p, int64_t chunks, void *stream)
 
 int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream)
 {
-    pack_kernel<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return int(cudaGetLastError());
+    return launch_close(pack_kernel, unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream), p);
 }
 
 int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream)
 {
-    apply_kernel<<<unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream)>>>(p, from);
-    return int(cudaGetLastError());
+    return launch_close(apply_kernel, unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream), p, from);
 }
 
 int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, void *stream)
