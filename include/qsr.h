@@ -456,7 +456,8 @@ int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream);
  *   `iterations` times:  A = X X^T (X^T X if r > c);  C = a I + b A + c A^2;  X <- C X (X C),  a, b, c = 3.4445, -4.7750, 2.0315
  *   theta <- theta - (lr*weight_decay*wd_scale*theta + lr*update_scale*X),
  * theta rounded once to the parameter's type and once, from the same fp32 value, to the working copy's.  The polynomial
- * takes singular values above about 0.005 to [0.68, 1.21] in five iterations; it does not converge to one.
+ * takes singular values above about 0.005 to [0.68, 1.21] in five iterations; it does not converge to one.  Where one side is at
+ * least twice the other, the last three iterations are X <- (C3 C2 C1) X with A <- C A C in between: the same with fewer operations.
  * Products are taken by the tensor cores on fp16 numbers with sums in fp32; X, A and C are held at powers of two that keep them in
  * fp16's range.  products = 1 rounds each of them to fp16: the update is off by about 1e-3 of its norm (an eighth of what bf16
  * would give).  products = 3 holds them as sums of two fp16 numbers and takes three products for each: off by 2e-6 to 2e-5, at
@@ -496,7 +497,7 @@ typedef struct qsr_muon_config {
 } qsr_muon_config;
 
 /* Bytes of device workspace for matrices of these sizes (host arrays): about 4 bytes an element with one product, 8 with three,
- * plus as much for the square of the shorter side.  Negative qsr_status on error. */
+ * plus up to two and a half times as much for the square of the shorter side.  Negative qsr_status on error. */
 int64_t qsr_muon_workspace_bytes(const int64_t *rows_host, const int64_t *cols_host, int32_t n_matrices, int32_t workers, int32_t products);
 
 /* Makes a list over caller-owned matrices; arguments, stream, workspace and refusals as at qsr_list_create.  The workspace belongs
@@ -511,8 +512,9 @@ int qsr_muon_destroy(qsr_muon *muon);
 /* New gradient addresses, as qsr_list_set_grads. */
 int qsr_muon_set_grads(qsr_muon *muon, const void *const *grads_host);
 
-/* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  3 + 3 * iterations
- * launches, whatever the number of matrices; asynchronous.  It may be captured; lr and grad_scale are then those of the capture. */
+/* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  One launch
+ * for all matrices that one multiprocessor holds (up to 128 x 512), and for all others 3 + 3 * iterations, or one more, whatever
+ * their number; asynchronous.  It may be captured; lr and grad_scale are then those of the capture. */
 int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale);
 
 /* End of a round over the list's K workers, as qsr_list_sync: every parameter becomes the mean (sum over k = 0..K-1 in fp32) / K;

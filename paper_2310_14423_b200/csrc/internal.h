@@ -190,8 +190,7 @@ struct MuonMatrix {           // one matrix, in the device table; m <= n are its
     void *param, *copy;
     float *momentum;
     int64_t rows, cols;
-    uint16_t *x[2];           // fp16 blocks of 64 x 64: the iterate (column of blocks by column), before and after a product
-    uint16_t *gram, *factor;  // the same of m x m
+    uint16_t *x, *x_last;     // fp16 blocks of 64 x 64, column of blocks by column: the first iterate, and the last one
     int32_t rb, cb, mb, nb;   // blocks along rows, columns, m and n
     int32_t tall;             // rows > cols
     int32_t param_type, copy_type, grad_type;
@@ -199,13 +198,25 @@ struct MuonMatrix {           // one matrix, in the device table; m <= n are its
     float scale;              // power of two that the iterate is held at
     int32_t first_chunk, chunks;
 };
-struct alignas(16) MuonTile {  // of a product: row tile i (256 elements), and the columns of `width` blocks (4 or 2) from block q on
-    int32_t matrix, i, q, width;
-    int32_t tall;             // of the matrix
-    int32_t rows, columns;    // of the product's result, in blocks
-    int32_t longer, shorter;  // the matrix's sides in blocks
-    int32_t pad[3];
+// A tile of a product of blocks, result = factor * (left right): its row tile i (256 elements), and the columns of `width` blocks (4 or 2) from
+// block q on.  Places are numbers of blocks from MuonParams::data on; `pitch`: blocks in a column of them, `lo`: to what fp16 leaves.
+struct alignas(16) MuonTile {
+    int32_t i, q, width;
+    int32_t flags;
+    int32_t rows, columns, sums;              // of the product, in blocks
+    float factor;
+    int32_t left, left_pitch, left_lo;
+    int32_t right, right_pitch, right_lo;
+    int32_t to;                               // rows x columns blocks
+    int32_t gram;                             // polynomial: A, whose A A this product is
 };
+// An operand is the iterate, whose blocks all lie with the sum along their rows (OUTER) or all do not, or a symmetric matrix, of which the
+// tiles on and above the diagonal are held.
+enum { MUON_LEFT_ITERATE = 1, MUON_LEFT_OUTER = 2, MUON_RIGHT_ITERATE = 4, MUON_RIGHT_OUTER = 8 };
+// Powers of two that A and C are held at, for fp16's range: singular values of X stay below 1.2025 (the polynomial's maximum on
+// [0, 1.2025]), so entries of A stay below 1.45 and those of C, whose eigenvalues lie in [0.63, 3.45], below 3.45.
+constexpr float kMuonGramScale = 16384.0f, kMuonFactorScale = 16384.0f;
+constexpr float kMuonA = 3.4445f, kMuonB = -4.7750f, kMuonC = 2.0315f;
 struct MuonBlock { int32_t matrix, p, q, pad; };     // a block of 64 x 64
 struct MuonChunk { int32_t matrix, n; int64_t offset; };   // n consecutive elements
 struct MuonParams {
@@ -217,7 +228,7 @@ struct MuonParams {
     float *factor;            // [matrices]: scale / (norm + eps)
     unsigned *arrived;        // [matrices], zero between launches
     unsigned *late;           // set where a wait ran out
-    const uint16_t *data;     // all matrices' blocks
+    uint16_t *data;     // all matrices' blocks
     float one_minus_beta, beta, grad_scale, eps;
     float lr, lr_decay;
     int32_t nesterov, products, iterations;
@@ -229,11 +240,11 @@ int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream);
 // tensor memory.
 constexpr int kMuonSmallBlocks = 26;
 int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, void *stream);
-int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream);
-// One product of all matrices: 0 gram, 1 polynomial of it, 2 iterate.
+int launch_muon_apply(const MuonParams &p, int64_t blocks, void *stream);
 // tensor_maps: two CUtensorMaps over the blocks at MuonParams::data.
 int encode_muon_maps(void *tensor_maps, const void *data, int64_t bytes);
-int launch_muon_product(const MuonParams &p, const void *tensor_maps, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
+// Products of any number of matrices; polynomial: the tiles' results are C = a I + b A + c A A.
+int launch_muon_product(const MuonParams &p, const void *tensor_maps, bool polynomial, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream);
 
 // ---- log probabilities of given tokens (logprobs.cu) ----
 

@@ -6,7 +6,8 @@
 // and serves as an operand with either side along the products' sum: columns along it as it is, rows along it if
 // the instruction is told so ("outer").  So X X^T and C X, or X^T X and X C, read the same blocks of X, no matrix is ever transposed,
 // and of A and C only the tiles on and above the diagonal are computed; what lies below is read from its mirror image.
-// Blocks are padded with zeros, hence any sizes.
+// Blocks are padded with zeros, hence any sizes.  Products of C with A or with another C, for which the last iterations of long matrices are
+// taken (muon_api.cu), are symmetric too, since all of them are polynomials of the same A.
 //
 // With three products per multiplication, X, A and C are sums of two fp16 numbers and hi hi + hi lo + lo hi are accumulated.
 #include <cuda.h>
@@ -18,10 +19,7 @@ namespace qsr {
 
 namespace {
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-// Powers of two that A and C are held at, for fp16's range: singular values of X stay below 1.2025 (the polynomial's
-// maximum on [0, 1.2025]), so entries of A stay below 1.45 and those of C, whose eigenvalues lie in [0.63, 3.45], below 3.45.
-constexpr float kGramScale = 16384.0f, kFactorScale = 16384.0f;
+constexpr float kA = kMuonA, kB = kMuonB, kC = kMuonC, kGramScale = kMuonGramScale, kFactorScale = kMuonFactorScale;
 
 // The launches of a step follow one another closely: each is started before the one before it has ended, and waits for that.
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -189,7 +187,7 @@ template <bool WIDE>
 __device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b, const void *grad)
 {
     const bool both = p.products == 3;
-    uint16_t *block = t.x[0] + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
+    uint16_t *block = t.x + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
     const int64_t lo = int64_t(t.rb) * t.cb * kBlockElements;
     const int grad_type = t.grad_type;
     const float *momentum = t.momentum;
@@ -245,11 +243,11 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonP
 
 // theta <- theta - (lr wd theta + lr update_scale X) for one block of the last iterate.
 template <bool WIDE>
-__device__ __forceinline__ void apply_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b, int from)
+__device__ __forceinline__ void apply_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b)
 {
     const bool both = p.products == 3;
     const float decay = p.lr_decay * t.wd_scale, step = p.lr * t.update_scale / t.scale;
-    const uint16_t *block = t.x[from] + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
+    const uint16_t *block = t.x_last + (int64_t(b.q) * t.rb + b.p) * kBlockElements;
     const int64_t lo = int64_t(t.rb) * t.cb * kBlockElements;
     const int type = t.param_type, copy_type = t.copy_type;
     void *param = t.param, *copy = t.copy;
@@ -288,13 +286,13 @@ __device__ __forceinline__ void apply_block(const MuonParams &p, const MuonMatri
         if (copy_type != QSR_NONE) give<WIDE>(copy, theta, copy_type, o[h]);
     }
 }
-__global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ MuonParams p, int from)
+__global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ MuonParams p)
 {
     const MuonBlock b = p.blocks[gridDim.x - 1 - blockIdx.x];
     const MuonMatrix &t = p.matrices[b.matrix];
     wait_for_launch_before();
-    if (wide_rows(t, t.param, t.param_type) && (t.copy_type == QSR_NONE || wide_rows(t, t.copy, t.copy_type))) apply_block<true>(p, t, b, from);
-    else apply_block<false>(p, t, b, from);
+    if (wide_rows(t, t.param, t.param_type) && (t.copy_type == QSR_NONE || wide_rows(t, t.copy, t.copy_type))) apply_block<true>(p, t, b);
+    else apply_block<false>(p, t, b);
 }
 
 // ---- products --------------------------------------------------------------------------------------------
@@ -415,23 +413,10 @@ __device__ __forceinline__ void load_accumulators(float (&v)[32], uint32_t addre
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// What a product is made of, in blocks: rows x sums times sums x columns.  An operand is the iterate or a symmetric matrix; it is
-// "outer" at step k if its blocks there have the sum along their rows.  Of a symmetric matrix the blocks in row tile P, column
-// tile T (four blocks each) are held where P <= T; elsewhere their mirror images are read, the other way round.
-struct Shape {
-    int rows, sums, columns;
-    bool left_x, right_x, outer_left_x, outer_right_x;
-    __device__ __forceinline__ bool outer_left(int i, int k) const { return left_x ? outer_left_x : i > (k >> 2); }
-    __device__ __forceinline__ bool outer_right(int q, int k) const { return right_x ? outer_right_x : (q >> 2) > (k >> 2); }
-};
-template <int KIND>
-__device__ __forceinline__ Shape shape_of(const MuonTile &w)
-{
-    const bool tall = w.tall;
-    if (KIND == GRAM) return Shape{w.rows, w.longer, w.columns, true, true, tall, tall};                 // X X^T, or X^T X
-    if (KIND == FACTOR) return Shape{w.rows, w.shorter, w.columns, false, false, false, false};         // A A
-    return Shape{w.rows, w.shorter, w.columns, tall, !tall, false, true};                                // C X, or X C
-}
+// Whether an operand's blocks at step k of the sum lie with the sum along their rows ("outer").  Of a symmetric matrix the blocks in row
+// tile P, column tile T (four blocks each) are held where P <= T; elsewhere their mirror images are read, the other way round.
+__device__ __forceinline__ bool outer_left(const MuonTile &w, int k) { return w.flags & MUON_LEFT_ITERATE ? (w.flags & MUON_LEFT_OUTER) != 0 : w.i > (k >> 2); }
+__device__ __forceinline__ bool outer_right(const MuonTile &w, int k) { return w.flags & MUON_RIGHT_ITERATE ? (w.flags & MUON_RIGHT_OUTER) != 0 : (w.q >> 2) > (k >> 2); }
 
 // Half a row of a block, 32 elements: where 32-byte pair `pair` (0 or 1) of it lies, in elements.  A thread has a row in its registers and
 // writes it 32 bytes at a time, a sector each.  (Passing the tile through shared memory, so that a warp's accesses are adjacent, was
@@ -492,36 +477,34 @@ __device__ __forceinline__ void add_half(float (&v)[32], Raw8 (&r)[2], int row, 
 }
 
 // From sums to what is held: all but the polynomial's middle term.
-template <int KIND>
+template <bool POLYNOMIAL>
 __device__ __forceinline__ void finish_half(float (&x)[32], float factor, int diagonal)
 {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) x[k] = KIND == FACTOR ? x[k] * factor + (k == diagonal ? kA * kFactorScale : 0.0f) : x[k] * factor;
+    for (int k = 0; k < 32; ++k) x[k] = POLYNOMIAL ? x[k] * factor + (k == diagonal ? kA * kFactorScale : 0.0f) : x[k] * factor;
 }
 constexpr float kMiddle = kB * kFactorScale / kGramScale;
 
 // Where a warp's part of a tile goes: 32 rows of blocks (bp, bq) and (bp, bq + 1), a row to a thread.
-template <int KIND>
 struct Target {
     int blocks;                        // of the two, how many the result has
     int row, diagonal;                 // in its block; where it meets the matrix's diagonal, in their columns
     uint16_t *to;
-    const uint16_t *gram;              // FACTOR: the same elements of A
+    const uint16_t *gram;              // polynomial: the same elements of A
     int64_t column, lo;                // from a block to the next, from fp16 to what it leaves
     float factor;
-    __device__ __forceinline__ Target(const MuonTile &w, const MuonParams &p, int from, int rank, int group, int part, int lane)
+    __device__ __forceinline__ Target(const MuonTile &w, const MuonParams &p, int rank, int group, int part, int lane)
     {
-        const MuonMatrix &t = p.matrices[w.matrix];
         const int bp = w.i * 4 + rank * 2 + (group >> 1), bq = w.q + part * 2;
         blocks = bp < w.rows ? min(2, min(w.columns, w.q + w.width) - bq) : 0;
         row = (group & 1) * 32 + lane;
         diagonal = (bp - bq) * 64 + row;
-        const int64_t at = (int64_t(bq) * w.rows + bp) * kBlockElements;
-        to = (KIND == GRAM ? t.gram : KIND == FACTOR ? t.factor : t.x[from ^ 1]) + at;
-        gram = t.gram + at;
+        const int64_t at = int64_t(bq) * w.rows + bp;
+        to = p.data + (w.to + at) * kBlockElements;
+        gram = p.data + (w.gram + at) * kBlockElements;
         column = int64_t(w.rows) * kBlockElements;
         lo = int64_t(w.columns) * column;
-        factor = KIND == GRAM ? kGramScale / (t.scale * t.scale) : KIND == FACTOR ? kC * kFactorScale / (kGramScale * kGramScale) : 1.0f / kFactorScale;
+        factor = w.factor;
     }
 };
 
@@ -535,9 +518,9 @@ struct Shared {
 // 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  Two warps of
 // each block copy; one thread of the first block issues the products of both; eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
 // single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.
-template <int KIND, int PRODUCTS>
+template <bool POLYNOMIAL, int PRODUCTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
-product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Maps maps, const MuonTile *tiles, int n_tiles, int from)
+product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Maps maps, const MuonTile *tiles, int n_tiles)
 {
     extern __shared__ char raw[];
     __shared__ Shared sh;
@@ -580,26 +563,20 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
         int stage = 0, issued = 0;
         unsigned phase = 0;
         bool going = true;
-        // a tile's description and its matrix's places are read while the tile before is copied
-        const auto block_of = [&](const uint16_t *at) { return int((at - p.data) / kBlockElements); };
-        MuonTile ahead = tiles[min(pair, n_tiles - 1)];
-        int x = block_of(p.matrices[ahead.matrix].x[from]), symmetric = block_of(KIND == FACTOR ? p.matrices[ahead.matrix].gram : p.matrices[ahead.matrix].factor);
+        MuonTile ahead = tiles[min(pair, n_tiles - 1)];          // read while the tile before is copied
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = ahead;
-            const Shape z = shape_of<KIND>(w);
-            const int columns = min(w.width, z.columns - w.q), sums = z.sums, wide = columns > 2;
+            const int columns = min(w.width, w.columns - w.q), sums = w.sums, wide = columns > 2;
             const int at = left ? w.i * 4 + rank * 2 : w.q + (wide ? rank * 2 : rank);           // first of up to two blocks
-            const int here = max(0, left ? min(2, z.rows - at) : min(wide ? 2 : 1, w.q + columns - at));
-            const int both = min(4, z.rows - w.i * 4) + columns;                // blocks that the pair copies
-            const bool iterate = left ? z.left_x : z.right_x;
-            const int pitch = iterate && w.tall ? w.longer : w.shorter, lo = w.shorter * (iterate ? w.longer : w.shorter);
-            const int base = iterate ? x : symmetric;
+            const int here = max(0, left ? min(2, w.rows - at) : min(wide ? 2 : 1, w.q + columns - at));
+            const int both = min(4, w.rows - w.i * 4) + columns;                // blocks that the pair copies
+            const int base = left ? w.left : w.right, pitch = left ? w.left_pitch : w.right_pitch, lo = left ? w.left_lo : w.right_lo;
             ahead = tiles[min(tile + pairs, n_tiles - 1)];
             for (int k = 0; k < sums; ++k) {
                 if (!barrier_wait(shared_address(&sh.empty[stage]), phase ^ 1u, stop)) { going = false; break; }
                 const uint32_t bar = shared_address(&sh.full[stage]), to = stage0 + stage * kStage + (left ? 0 : 2) * kBlockBytes;
                 // blocks (at, k), (at + 1, k), which are neighbours, or blocks (k, at), (k, at + 1): of a symmetric matrix, their mirror images
-                const bool outer = left ? z.outer_left(w.i, k) : z.outer_right(w.q, k);
+                const bool outer = left ? outer_left(w, k) : outer_right(w, k);
                 const int first = base + (outer ? at * pitch + k : k * pitch + at);
                 if (one) {
                     if (left && rank == 0) barrier_expect(bar, unsigned(both * PARTS * kBlockBytes));
@@ -617,11 +594,6 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                 __syncwarp();
                 issued++;
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-                if (k == 0) {
-                    const MuonMatrix &t = p.matrices[ahead.matrix];
-                    x = block_of(t.x[from]);
-                    symmetric = block_of(KIND == FACTOR ? t.gram : t.factor);
-                }
             }
         }
         // when the block ends nothing may be copying into its shared memory, or reading it: wait for the last stages
@@ -641,8 +613,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             const MuonTile w = ahead;
             ahead = tiles[min(tile + pairs, n_tiles - 1)];
-            const Shape z = shape_of<KIND>(w);
-            const int sums = z.sums, wide = min(w.width, z.columns - w.q) > 2;
+            const int sums = w.sums, wide = min(w.width, w.columns - w.q) > 2;
             for (int k = 0; k < sums; k += STEPS) {
                 // STEPS stages at a time (with three products one turn of what tensor memory adds up), the smaller products of all of
                 // them first: the fewer sums are added to an accumulator that has grown, the less is cut off
@@ -658,7 +629,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                     if (i >= steps) break;
                     if (!barrier_wait(shared_address(&sh.full[stage]), phase, stop)) { going = false; break; }
                     fence_after();
-                    const bool outer_a = z.outer_left(w.i, k + i), outer_b = z.outer_right(w.q, k + i);
+                    const bool outer_a = outer_left(w, k + i), outer_b = outer_right(w, k + i);
                     const uint32_t a0 = stage0 + stage * kStage;
                     idesc[i] = instruction(256, wide ? 256 : 128, outer_a, outer_b);
                     a[i] = operand(a0);
@@ -708,17 +679,17 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
         bool going = true;
         for (int tile = pair; tile < n_tiles && going; tile += pairs) {
             if (PRODUCTS == 1) {
-                const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
+                const Target o(tiles[tile], p, rank, group, part, lane);
                 Raw8 gram[2];
-                if (KIND == FACTOR && o.blocks > 0) load_half(gram, o.gram, o.row, 0);
+                if (POLYNOMIAL && o.blocks > 0) load_half(gram, o.gram, o.row, 0);
                 if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) break;
                 fence_after();
 #pragma unroll 1
                 for (int h = 0; h < 2 * o.blocks; ++h) {         // 32 columns each
                     float v[32];
                     load_accumulators(v, from_lane + unsigned(buffer * 256 + h * 32));
-                    finish_half<KIND>(v, o.factor, o.diagonal - h * 32);
-                    if (KIND == FACTOR) {
+                    finish_half<POLYNOMIAL>(v, o.factor, o.diagonal - h * 32);
+                    if (POLYNOMIAL) {
                         add_half(v, gram, o.row, kMiddle);
                         if (h + 1 < 2 * o.blocks) load_half(gram, o.gram + ((h + 1) >> 1) * o.column, o.row, (h + 1) & 1);
                     }
@@ -731,7 +702,7 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[h][k] = 0.0f;
-                int turns = ((KIND == GRAM ? tiles[tile].longer : tiles[tile].shorter) + STEPS - 1) / STEPS;
+                int turns = (tiles[tile].sums + STEPS - 1) / STEPS;
 #pragma unroll 1
                 for (; turns > 0; --turns) {
                     if (!barrier_wait(shared_address(&sh.ready[buffer]), buffer_phase, stop)) { going = false; break; }
@@ -746,12 +717,12 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
                     next();
                 }
                 if (!going) break;
-                const Target<KIND> o(tiles[tile], p, from, rank, group, part, lane);
+                const Target o(tiles[tile], p, rank, group, part, lane);
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {                    // 32 columns each
                     if (h >= 2 * o.blocks) break;
-                    finish_half<KIND>(v[h], o.factor, o.diagonal - h * 32);
-                    if (KIND == FACTOR) {
+                    finish_half<POLYNOMIAL>(v[h], o.factor, o.diagonal - h * 32);
+                    if (POLYNOMIAL) {
                         Raw8 gram[2];
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
@@ -1093,7 +1064,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
                 for (int k = 0; k < 32; ++k) v[k] *= gram_factor;
                 keep_half<PRODUCTS>(block, z.a_part(), row, half, v);
             } else if (kind == FACTOR) {
-                finish_half<FACTOR>(v, factor_factor, (i - j) * 64 + row - half * 32);
+                finish_half<true>(v, factor_factor, (i - j) * 64 + row - half * 32);
                 add_kept(v, block, row, half, kMiddle);
                 if (PRODUCTS == 3) add_kept(v, block + z.a_part(), row, half, kMiddle);
                 keep_half<PRODUCTS>(block, z.a_part(), row, half, v);
@@ -1144,13 +1115,13 @@ int launch_close(void (*kernel)(A...), unsigned blocks, unsigned threads, size_t
 
 constexpr int kProductShared = kStageBlocks * kBlockBytes + 1024;
 
-template <int KIND, int PRODUCTS>
-int launch_product(const MuonParams &p, const Maps &maps, int from, const MuonTile *tiles, int n, int blocks, cudaStream_t st)
+template <bool POLYNOMIAL, int PRODUCTS>
+int launch_product(const MuonParams &p, const Maps &maps, const MuonTile *tiles, int n, int blocks, cudaStream_t st)
 {
-    const auto kernel = product_kernel<KIND, PRODUCTS>;
+    const auto kernel = product_kernel<POLYNOMIAL, PRODUCTS>;
     static std::atomic<uint64_t> raised{0};
     if (int err = allow_shared(reinterpret_cast<const void *>(kernel), kProductShared, raised)) return err;
-    return launch_close(kernel, unsigned(blocks), kProductThreads, kProductShared, st, p, maps, tiles, n, from);
+    return launch_close(kernel, unsigned(blocks), kProductThreads, kProductShared, st, p, maps, tiles, n);
 }
 
 }  // namespace
@@ -1192,9 +1163,9 @@ int launch_muon_pack(const MuonParams &p, int64_t blocks, void *stream)
     return launch_close(pack_kernel, unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream), p);
 }
 
-int launch_muon_apply(const MuonParams &p, int from, int64_t blocks, void *stream)
+int launch_muon_apply(const MuonParams &p, int64_t blocks, void *stream)
 {
-    return launch_close(apply_kernel, unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream), p, from);
+    return launch_close(apply_kernel, unsigned(blocks), 256, 0, static_cast<cudaStream_t>(stream), p);
 }
 
 int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shared_blocks, unsigned columns, void *stream)
@@ -1203,19 +1174,13 @@ int launch_muon_small(const MuonParams &p, const int32_t *which, int n, int shar
     return p.products == 3 ? launch_small<3>(p, which, n, shared_blocks, columns, st) : launch_small<1>(p, which, n, shared_blocks, columns, st);
 }
 
-int launch_muon_product(const MuonParams &p, const void *tensor_maps, int kind, int from, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
+int launch_muon_product(const MuonParams &p, const void *tensor_maps, bool polynomial, const MuonTile *tiles, int64_t n_tiles, int multiprocessors, void *stream)
 {
     const Maps &maps = *static_cast<const Maps *>(tensor_maps);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int n = int(n_tiles), blocks = 2 * (n < multiprocessors / 2 ? n : multiprocessors / 2);
-    if (p.products == 3) {
-        if (kind == GRAM) return launch_product<GRAM, 3>(p, maps, from, tiles, n, blocks, st);
-        if (kind == FACTOR) return launch_product<FACTOR, 3>(p, maps, from, tiles, n, blocks, st);
-        return launch_product<ITERATE, 3>(p, maps, from, tiles, n, blocks, st);
-    }
-    if (kind == GRAM) return launch_product<GRAM, 1>(p, maps, from, tiles, n, blocks, st);
-    if (kind == FACTOR) return launch_product<FACTOR, 1>(p, maps, from, tiles, n, blocks, st);
-    return launch_product<ITERATE, 1>(p, maps, from, tiles, n, blocks, st);
+    if (p.products == 3) return polynomial ? launch_product<true, 3>(p, maps, tiles, n, blocks, st) : launch_product<false, 3>(p, maps, tiles, n, blocks, st);
+    return polynomial ? launch_product<true, 1>(p, maps, tiles, n, blocks, st) : launch_product<false, 1>(p, maps, tiles, n, blocks, st);
 }
 
 }  // namespace qsr

@@ -10,19 +10,22 @@
 #include "checks.h"
 #include "internal.h"
 
+struct MuonLaunch { int64_t first, n; bool polynomial; };          // which tiles
+
 struct qsr_muon {
     qsr_muon_config cfg;
     cudaStream_t stream;
     int device, multiprocessors;
     qsr::MuonParams params;                     // tables; the step's numbers are filled in by each call
     const void **grads;
-    const qsr::MuonTile *half, *whole;          // tiles of a symmetric result, and of the iterate
+    const qsr::MuonTile *tiles;
+    std::vector<MuonLaunch> products;               // of a step, in their order
     const int32_t *small;                       // matrices that one block each steps
     int32_t n_small, small_blocks;
     unsigned small_columns;
     const qsr::ListTensor *sync_tensors;
     const qsr::ListChunk *sync_chunks;
-    int64_t chunks, large_chunks, blocks, n_half, n_whole, param_sync_chunks, all_sync_chunks;
+    int64_t chunks, large_chunks, blocks, param_sync_chunks, all_sync_chunks;
     std::vector<qsr_matrix> host;
     bool has_grads;
     int64_t launches;
@@ -48,19 +51,123 @@ Sides sides_of(int64_t rows, int64_t cols)
 }
 // Tiles of 256 rows and `width` blocks of columns: those of an m x m matrix that reach the diagonal's 256 x 256 tiles or lie above,
 // and those of an r x c matrix (blocks).
-int64_t half_tiles(const Sides &s, int64_t width)
+int64_t half_tiles(int64_t mb, int64_t width)
 {
     int64_t count = 0;
-    for (int64_t q = 0; q < s.mb; q += width) count += q / 4 + 1;
+    for (int64_t q = 0; q < mb; q += width) count += q / 4 + 1;
     return count;
 }
 int64_t whole_tiles(int64_t rb, int64_t cb, int64_t width) { return ceil_div(rb, 4) * ceil_div(cb, width); }
+
+// Iterations whose products of X and C are saved.  X_k = P_k X with symmetric m x m matrices that are all polynomials of A: C_k' = C_k ... C_j,
+// and A_(k+1) = C_k A_k C_k.  With the last r iterations on these alone, m x m x m products take the place of 2 (r - 1) with m x m x n: for
+// five iterations and r = 3, in units of m^3 and with n = rho m, 10 rho + 15 instead of 17 rho + 7.  The first iterations stay products with
+// X, because A holds small singular values by their squares: after two of them the rounding of A no longer shows (the update is as
+// near to the formula's as with r = 0 on matrices of low rank over noise, and loses an order of magnitude with one iteration less).
+// From rho = 2 on: six 1024 x 2048 take 298 us against 322 with r = 0 (three products: 652 and 737), eight 1024 x 1280 406 against 387
+// (831 and 844), and ViT-B/16's list, whose three matrices in four have rho of 3 or 4, 1307 against 1646 (3208 and 3960).
+int64_t short_iterations(const Sides &s, int32_t iterations) { return s.nb >= 2 * s.mb && iterations >= 4 ? std::min(3, iterations - 2) : 0; }
+// Symmetric matrices that a matrix needs: A and C, or A, C A, two of C and their product.
+int64_t squares(int64_t r) { return r ? 5 : 2; }
 
 // Columns of a tile, in blocks: two instead of four where that ends earlier on `pairs` pairs of multiprocessors.  A narrow tile takes
 // about 0.65 of a wide one's time (its products take half, but it copies three quarters as much).  Two workers' ragged list, 1023 x 2047
 // the largest, takes 432 us by this rule, 515 with wide tiles alone and 457 with narrow ones; ViT-B/16's bf16 list 1661 us with wide
 // tiles, 2045 with narrow ones.
 int32_t tile_width(int64_t wide, int64_t narrow, int64_t pairs) { return ceil_div(narrow, pairs) * 65 < ceil_div(wide, pairs) * 100 ? 2 : 4; }
+
+// The products of a step.  Three slots an iteration -- A, C, and what takes C -- and one more for matrices whose last iterations are short.
+struct Operand { int32_t at, pitch, lo; bool iterate, outer; };
+struct Product { Operand left, right; int32_t to, gram, rows, columns, sums; bool symmetric; float factor; };
+class Plan {
+public:
+    explicit Plan(int32_t iterations) : iterations_(iterations), slots_(size_t(3 * iterations + 1)) {}
+
+    // All products of a matrix with the last r iterations short; x, square: its iterates' and symmetric matrices' places.  Returns which of the
+    // two iterates is the last.
+    int add(const MuonMatrix &y, const int32_t *x, const int32_t *square, int32_t r)
+    {
+        const int32_t mb = y.mb, lo = mb * mb, first_short = r ? iterations_ - r : iterations_;
+        const auto whole = [&](int k, bool outer) { return Operand{x[k], y.rb, y.rb * y.cb, true, outer}; };
+        const auto half = [&](int32_t at) { return Operand{at, mb, lo, false, false}; };
+        const float to_gram = kMuonGramScale / (y.scale * y.scale), keep = 1.0f / kMuonFactorScale;
+        const auto square_product = [&](int slot, int32_t a, int32_t b, int32_t to, float factor) {
+            slots_[size_t(slot)].push_back(Product{half(a), half(b), to, to, mb, mb, mb, true, factor});
+        };
+        const auto iterate = [&](int slot, int from, int32_t c, float factor) {
+            const Operand l = y.tall ? whole(from, false) : half(c), right = y.tall ? half(c) : whole(from, true);      // X C, or C X
+            slots_[size_t(slot)].push_back(Product{l, right, x[from ^ 1], 0, y.rb, y.cb, mb, false, factor});
+        };
+        const int32_t a = square[0], ca = square[2];
+        int32_t c = square[1], spare = r ? square[3] : 0, product = 0, free = r ? square[4] : 0;
+        int now = 0;
+        float scale = kMuonFactorScale;               // that `product` is held at: its entries grow by up to 3.45 with each C
+        for (int32_t k = 0; k < iterations_; ++k) {
+            const int slot = 3 * k;
+            if (k <= first_short) slots_[size_t(slot)].push_back(Product{whole(now, y.tall), whole(now, y.tall), a, 0, mb, mb, y.nb, true, to_gram});
+            else square_product(slot, c, ca, a, keep);                                   // A <- C (C A)
+            if (k > first_short) std::swap(c, spare);                                      // the last C may still be wanted
+            slots_[size_t(slot + 1)].push_back(Product{half(a), half(a), c, a, mb, mb, mb, true, kMuonC * kMuonFactorScale / (kMuonGramScale * kMuonGramScale)});
+            if (k < first_short) {
+                iterate(slot + 2, now, c, keep);
+                now ^= 1;
+                continue;
+            }
+            if (k + 1 < iterations_) square_product(slot + 2, c, a, ca, keep);            // C A
+            if (k == first_short) product = c;
+            else {                                                                       // C_k ... C_first
+                const int32_t to = k == first_short + 1 ? free : spare;
+                square_product(slot + 2, c, product, to, 0.25f * keep);
+                scale *= 0.25f;
+                product = to;
+            }
+        }
+        if (r) {
+            iterate(3 * iterations_, now, product, 1.0f / scale);
+            now ^= 1;
+        }
+        return now;
+    }
+
+    // The launches' tiles, one launch for each slot that has products; their places are numbers for now.
+    void tiles(std::vector<MuonTile> &out, std::vector<MuonLaunch> &launches, int64_t pairs)
+    {
+        for (size_t slot = 0; slot < slots_.size(); ++slot) {
+            std::vector<Product> &all = slots_[slot];
+            if (all.empty()) continue;
+            int64_t wide = 0, narrow = 0;
+            for (const Product &p : all) {
+                wide += p.symmetric ? half_tiles(p.rows, 4) : whole_tiles(p.rows, p.columns, 4);
+                narrow += p.symmetric ? half_tiles(p.rows, 2) : whole_tiles(p.rows, p.columns, 2);
+            }
+            const int32_t width = tile_width(wide, narrow, pairs);
+            // long products first, so that short ones fill the end
+            std::stable_sort(all.begin(), all.end(), [](const Product &a, const Product &b) { return a.sums > b.sums; });
+            const size_t begin = out.size();
+            for (const Product &p : all) {
+                const auto tile = [&](int32_t i, int32_t q) {
+                    const int32_t flags = (p.left.iterate ? MUON_LEFT_ITERATE : 0) | (p.left.outer ? MUON_LEFT_OUTER : 0) |
+                                          (p.right.iterate ? MUON_RIGHT_ITERATE : 0) | (p.right.outer ? MUON_RIGHT_OUTER : 0);
+                    out.push_back(MuonTile{i, q, width, flags, p.rows, p.columns, p.sums, p.factor, p.left.at, p.left.pitch, p.left.lo, p.right.at,
+                                           p.right.pitch, p.right.lo, p.to, p.gram});
+                };
+                // neighbours share what is longer: the iterate's tile, not the factor's
+                if (p.rows > p.columns) {
+                    for (int32_t i = 0; i * 4 < p.rows; ++i)
+                        for (int32_t q = 0; q < p.columns; q += width) tile(i, q);
+                } else {
+                    for (int32_t q = 0; q < p.columns; q += width)
+                        for (int32_t i = 0; i * 4 < p.rows && (!p.symmetric || i <= q / 4); ++i) tile(i, q);
+                }
+            }
+            launches.push_back(MuonLaunch{int64_t(begin), int64_t(out.size() - begin), slot % 3 == 1});
+        }
+    }
+
+private:
+    int32_t iterations_;
+    std::vector<std::vector<Product>> slots_;
+};
 
 // Blocks of shared memory and columns of tensor memory that a matrix stepped by one block needs; whether it is one.
 bool is_small(int64_t rows, int64_t cols, int64_t parts, int64_t &blocks, int64_t &columns)
@@ -73,13 +180,13 @@ bool is_small(int64_t rows, int64_t cols, int64_t parts, int64_t &blocks, int64_
 
 struct Layout {
     int64_t small, n_small;
-    int64_t matrices, grads, chunks, blocks, half, whole, sync_tensors, sync_chunks, partial, factor, arrived, late, data, bytes;
-    int64_t n_chunks, n_blocks, n_half, n_whole, n_sync, n_param_sync;
+    int64_t matrices, grads, chunks, blocks, tiles, sync_tensors, sync_chunks, partial, factor, arrived, late, data, bytes;
+    int64_t n_chunks, n_blocks, n_tiles, n_sync, n_param_sync;
     int status;
 };
 
 // Where everything lies in the workspace, from the matrices' sizes.
-Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t workers, int32_t products)
+Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t workers, int32_t products, int32_t iterations)
 {
     Layout l;
     std::memset(&l, 0, sizeof l);
@@ -98,21 +205,20 @@ Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t wo
             l.n_small++;
             continue;
         }
+        const int64_t r = short_iterations(s, iterations), half = half_tiles(s.mb, 2), whole = std::max(whole_tiles(s.mb, s.nb, 2), whole_tiles(s.nb, s.mb, 2));
         l.n_blocks += s.mb * s.nb;
-        l.n_half += half_tiles(s, 2);
-        l.n_whole += whole_tiles(s.mb, s.nb, 2) + whole_tiles(s.nb, s.mb, 2);       // room for either
-        data += (2 * s.mb * s.nb + 2 * s.mb * s.mb) * parts * kBlockBytes;
+        l.n_tiles += iterations * (2 * half + whole) + (r ? 4 * half + whole : 0);       // room for tiles of either width
+        data += (2 * s.mb * s.nb + squares(r) * s.mb * s.mb) * parts * kBlockBytes;
     }
     l.n_sync = 2 * l.n_param_sync;
-    if (l.n_chunks > 0x7fffffff || l.n_blocks > 0x7fffffff || l.n_whole > 0x7fffffff || l.n_half > 0x7fffffff) { l.status = QSR_ERANGE; return l; }
+    if (l.n_chunks > 0x7fffffff || l.n_blocks > 0x7fffffff || l.n_tiles > 0x7fffffff || data / kBlockBytes > (int64_t(1) << 25)) { l.status = QSR_ERANGE; return l; }
     int64_t at = 0;
     auto take = [&at](int64_t bytes) { const int64_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     l.matrices = take(int64_t(n) * int64_t(sizeof(MuonMatrix)));
     l.grads = take(int64_t(n) * int64_t(sizeof(void *)));
     l.chunks = take(l.n_chunks * int64_t(sizeof(MuonChunk)));
     l.blocks = take(l.n_blocks * int64_t(sizeof(MuonBlock)));
-    l.half = take(l.n_half * int64_t(sizeof(MuonTile)));
-    l.whole = take(l.n_whole * int64_t(sizeof(MuonTile)));
+    l.tiles = take(l.n_tiles * int64_t(sizeof(MuonTile)));
     l.small = take(l.n_small * int64_t(sizeof(int32_t)));
     l.sync_tensors = take(2 * int64_t(n) * int64_t(sizeof(ListTensor)));
     l.sync_chunks = take(l.n_sync * int64_t(sizeof(ListChunk)));
@@ -175,7 +281,7 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     const int32_t n = cfg.n_matrices, per = n / cfg.workers;
     std::vector<int64_t> rows(static_cast<size_t>(n)), cols(static_cast<size_t>(n));
     for (int32_t i = 0; i < n; ++i) { rows[size_t(i)] = t[i].rows; cols[size_t(i)] = t[i].cols; }
-    const Layout l = layout_of(rows.data(), cols.data(), n, cfg.workers, cfg.products);
+    const Layout l = layout_of(rows.data(), cols.data(), n, cfg.workers, cfg.products, cfg.iterations);
     if (l.status) return l.status;
     if (!aligned_to(workspace, 256)) return QSR_EALIGN;
     if (workspace_bytes < l.bytes) return QSR_ERANGE;
@@ -210,13 +316,14 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     std::vector<int32_t> small;
     int64_t small_blocks = 0, small_columns = 32;
     std::vector<MuonBlock> blocks;
-    std::vector<MuonTile> half, whole;
+    std::vector<MuonTile> tiles;
+    std::vector<MuonLaunch> launches;
+    Plan plan(cfg.iterations);
     std::vector<ListTensor> sync_tensors(size_t(n) * 2);
     std::vector<ListChunk> sync_chunks;
     chunks.reserve(size_t(l.n_chunks));
     blocks.reserve(size_t(l.n_blocks));
-    half.reserve(size_t(l.n_half));
-    whole.reserve(size_t(l.n_whole));
+    tiles.reserve(size_t(l.n_tiles));
     sync_chunks.reserve(size_t(l.n_sync));
     const int64_t parts = cfg.products == 3 ? 2 : 1;
     char *at = ws + l.data;
@@ -256,10 +363,19 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
             while (small_columns < columns) small_columns *= 2;
             continue;
         }
-        y.x[0] = take(s.mb * s.nb);
-        y.x[1] = take(s.mb * s.nb);
-        y.gram = take(s.mb * s.mb);
-        y.factor = take(s.mb * s.mb);
+        const int64_t r = short_iterations(s, cfg.iterations);
+        int32_t whole[2], square[5] = {0, 0, 0, 0, 0};
+        uint16_t *iterate[2];
+        for (int k = 0; k < 2; ++k) {
+            whole[k] = int32_t((at - (ws + l.data)) / kBlockBytes);
+            iterate[k] = take(s.mb * s.nb);
+        }
+        for (int64_t k = 0; k < squares(r); ++k) {
+            square[k] = int32_t((at - (ws + l.data)) / kBlockBytes);
+            take(s.mb * s.mb);
+        }
+        y.x = iterate[0];
+        y.x_last = iterate[plan.add(y, whole, square, int32_t(r))];
         for (int32_t a = 0; a < y.rb; ++a)
             for (int32_t b = 0; b < y.cb; ++b) blocks.push_back(MuonBlock{i, a, b, 0});
     }
@@ -267,42 +383,10 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
         for (int32_t j = 0; j < per; ++j)
             for (int64_t o = 0; o < t[j].rows * t[j].cols; o += kSyncChunk)
                 sync_chunks.push_back(ListChunk{part * per + j, int32_t(std::min(kSyncChunk, t[j].rows * t[j].cols - o)), o});
-    std::vector<int32_t> order;
-    for (int32_t i = 0; i < n; ++i)
-        if (matrices[size_t(i)].x[0]) order.push_back(i);
     const int64_t large_chunks = int64_t(chunks.size());
     chunks.insert(chunks.end(), small_chunks.begin(), small_chunks.end());       // momentum and norm of the others only; all are cleared
-    int64_t wide_half = 0, narrow_half = 0, wide_whole = 0, narrow_whole = 0;
-    for (int32_t i : order) {
-        const MuonMatrix &y = matrices[size_t(i)];
-        const Sides s = sides_of(y.rows, y.cols);
-        wide_half += half_tiles(s, 4);
-        narrow_half += half_tiles(s, 2);
-        wide_whole += whole_tiles(y.rb, y.cb, 4);
-        narrow_whole += whole_tiles(y.rb, y.cb, 2);
-    }
-    const int64_t pairs = std::max(1, multiprocessors / 2);
-    const int32_t half_width = tile_width(wide_half, narrow_half, pairs), whole_width = tile_width(wide_whole, narrow_whole, pairs);
-    // long products first, so that short ones fill the end
-    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].nb > matrices[size_t(b)].nb; });
-    for (int32_t i : order) {
-        const MuonMatrix &y = matrices[size_t(i)];
-        for (int32_t q = 0; q < y.mb; q += half_width)
-            for (int32_t r = 0; r <= q / 4; ++r) half.push_back(MuonTile{i, r, q, half_width, y.tall, y.mb, y.mb, y.nb, y.mb, {}});
-    }
-    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return matrices[size_t(a)].mb > matrices[size_t(b)].mb; });
-    for (int32_t i : order) {
-        const MuonMatrix &y = matrices[size_t(i)];
-        // neighbours share what is longer: the iterate's tile, not the factor's
-        if (y.tall) {
-            for (int32_t r = 0; r * 4 < y.rb; ++r)
-                for (int32_t q = 0; q < y.cb; q += whole_width) whole.push_back(MuonTile{i, r, q, whole_width, y.tall, y.rb, y.cb, y.nb, y.mb, {}});
-        } else {
-            for (int32_t q = 0; q < y.cb; q += whole_width)
-                for (int32_t r = 0; r * 4 < y.rb; ++r) whole.push_back(MuonTile{i, r, q, whole_width, y.tall, y.rb, y.cb, y.nb, y.mb, {}});
-        }
-    }
-    if (int64_t(half.size()) > l.n_half || int64_t(whole.size()) > l.n_whole || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
+    plan.tiles(tiles, launches, std::max(1, multiprocessors / 2));
+    if (int64_t(tiles.size()) > l.n_tiles || int64_t(chunks.size()) != l.n_chunks || int64_t(blocks.size()) != l.n_blocks ||
         int64_t(sync_chunks.size()) != l.n_sync || int64_t(small.size()) != l.n_small || at > ws + l.bytes)
         return QSR_EINVAL;                               // the tables do not fit what was reserved for them
 
@@ -320,13 +404,13 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     x->device = dev;
     x->multiprocessors = multiprocessors;
     x->grads = reinterpret_cast<const void **>(ws + l.grads);
-    x->half = reinterpret_cast<const MuonTile *>(ws + l.half);
-    x->whole = reinterpret_cast<const MuonTile *>(ws + l.whole);
+    x->tiles = reinterpret_cast<const MuonTile *>(ws + l.tiles);
+    x->products = std::move(launches);
     x->sync_tensors = reinterpret_cast<const ListTensor *>(ws + l.sync_tensors);
     x->sync_chunks = reinterpret_cast<const ListChunk *>(ws + l.sync_chunks);
     x->small = reinterpret_cast<const int32_t *>(ws + l.small);
     x->n_small = int32_t(l.n_small); x->small_blocks = int32_t(small_blocks); x->small_columns = unsigned(small_columns);
-    x->chunks = l.n_chunks; x->large_chunks = large_chunks; x->blocks = l.n_blocks; x->n_half = int64_t(half.size()); x->n_whole = int64_t(whole.size());
+    x->chunks = l.n_chunks; x->large_chunks = large_chunks; x->blocks = l.n_blocks;
     x->param_sync_chunks = l.n_param_sync; x->all_sync_chunks = l.n_sync;
     x->has_grads = has_grads;
     x->launches = 0;
@@ -340,12 +424,12 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     p.factor = reinterpret_cast<float *>(ws + l.factor);
     p.arrived = reinterpret_cast<unsigned *>(ws + l.arrived);
     p.late = reinterpret_cast<unsigned *>(ws + l.late);
-    p.data = reinterpret_cast<const uint16_t *>(ws + l.data);
+    p.data = reinterpret_cast<uint16_t *>(ws + l.data);
     p.one_minus_beta = float(1.0 - cfg.beta);
     p.beta = float(cfg.beta);
     p.eps = float(cfg.eps);
     p.nesterov = cfg.nesterov; p.products = cfg.products; p.iterations = cfg.iterations;
-    if (l.n_whole > 0)
+    if (l.n_tiles > 0)
         if (int bad = encode_muon_maps(x->maps, p.data, l.bytes - l.data)) {
             delete x;
             return launch_status(bad);
@@ -354,8 +438,7 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
     if (err == cudaSuccess) err = upload(ws + l.grads, grads.data(), grads.size() * sizeof(void *), st);
     if (err == cudaSuccess) err = upload(ws + l.chunks, chunks.data(), chunks.size() * sizeof(MuonChunk), st);
     if (err == cudaSuccess) err = upload(ws + l.blocks, blocks.data(), blocks.size() * sizeof(MuonBlock), st);
-    if (err == cudaSuccess) err = upload(ws + l.half, half.data(), half.size() * sizeof(MuonTile), st);
-    if (err == cudaSuccess) err = upload(ws + l.whole, whole.data(), whole.size() * sizeof(MuonTile), st);
+    if (err == cudaSuccess) err = upload(ws + l.tiles, tiles.data(), tiles.size() * sizeof(MuonTile), st);
     if (err == cudaSuccess) err = upload(ws + l.small, small.data(), small.size() * sizeof(int32_t), st);
     if (err == cudaSuccess) err = upload(ws + l.sync_tensors, sync_tensors.data(), sync_tensors.size() * sizeof(ListTensor), st);
     if (err == cudaSuccess) err = upload(ws + l.sync_chunks, sync_chunks.data(), sync_chunks.size() * sizeof(ListChunk), st);
@@ -376,7 +459,7 @@ extern "C" {
 int64_t qsr_muon_workspace_bytes(const int64_t *rows_host, const int64_t *cols_host, int32_t n_matrices, int32_t workers, int32_t products)
 {
     if (!rows_host || !cols_host || n_matrices < 1 || workers < 1 || n_matrices % workers != 0 || !products_known(products)) return QSR_EINVAL;
-    const Layout l = layout_of(rows_host, cols_host, n_matrices, workers, products);
+    const Layout l = layout_of(rows_host, cols_host, n_matrices, workers, products, QSR_MUON_MAX_ITERATIONS);
     return l.status ? l.status : l.bytes;
 }
 
@@ -435,15 +518,12 @@ int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale)
     if (int err = launch_muon_momentum(p, muon->large_chunks, muon->stream)) return launch_status(err);
     muon->launches++;
     if (int err = launch_muon_pack(p, muon->blocks, muon->stream)) return launch_status(err);
-    for (int i = 0; i < muon->cfg.iterations; ++i)
-        for (int kind = 0; kind < 3; ++kind) {
-            muon->launches++;
-            if (int err = launch_muon_product(p, muon->maps, kind, i & 1, kind == 2 ? muon->whole : muon->half, kind == 2 ? muon->n_whole : muon->n_half,
-                                              muon->multiprocessors, muon->stream))
-                return launch_status(err);
-        }
+    for (const MuonLaunch &x : muon->products) {
+        muon->launches++;
+        if (int err = launch_muon_product(p, muon->maps, x.polynomial, muon->tiles + x.first, x.n, muon->multiprocessors, muon->stream)) return launch_status(err);
+    }
     muon->launches++;
-    return launch_status(launch_muon_apply(p, muon->cfg.iterations & 1, muon->blocks, muon->stream));
+    return launch_status(launch_muon_apply(p, muon->blocks, muon->stream));
 }
 
 int qsr_muon_sync(qsr_muon *muon, int32_t state_sync)

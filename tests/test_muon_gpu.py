@@ -307,6 +307,124 @@ def test_two_lists_at_once():
         assert all(torch.equal(s, t) for s, t in zip(x.p, y.p))
 
 
+def short64(u, iterations, short, products):
+    """What orthogonal64 gives, with the last `short` iterations on A alone: A <- C (C A), P <- C P and one product P X at the end, rounded
+    where the kernels round."""
+    X = u / torch.linalg.vector_norm(u)
+    tall = X.shape[0] > X.shape[1]
+    X = X.T if tall else X
+    m, n = X.shape
+    e = 2.0 ** -11 * min(1.0, 0.25 + 4.0 / math.sqrt(m * n)) if products == 1 else 2.0 ** -22
+    scale = 2.0 ** min(15, math.floor(0.5 * math.log2(m * n)))
+    held = (lambda M, at: (M * at).half().double() / at) if products == 1 else (lambda M, at: M)
+    gamma = (lambda k: (k / 16 + 1) * 2.0 ** -23) if products == 1 else (lambda k: 12 * 2.0 ** -23 + (k / 64 + 2) * 2.0 ** -24 + 2.0 ** -22)
+    norm = lambda M: float(torch.linalg.vector_norm(M))                # noqa: E731
+    two = lambda M: float(torch.linalg.matrix_norm(M, 2))              # noqa: E731
+    grain = 2.0 ** -25 * 2
+    tile = torch.arange(m, device=DEV) // 256
+    above = tile[:, None] <= tile[None, :]                            # of a symmetric matrix, the 256 x 256 tiles that are held
+    both = lambda M: torch.where(above, M, M.T)                        # noqa: E731
+    eye = torch.eye(m, device=DEV, dtype=torch.float64)
+    X = held(X, scale)
+    err = e * norm(X) + 8 * U * norm(X) + grain
+    terms = []                                                         # errors of the products C_j ... C_first, times X
+    for k in range(iterations):
+        on_x = k <= iterations - short
+        if on_x:
+            A = held(X @ X.T, 2.0 ** 14)
+            d_A = e * norm(A) + gamma(n) * norm(X.abs() @ X.T.abs())
+        t = torch.linalg.eigvalsh(A).clamp_min(0.0)
+        top, singular = float(t[-1]) * 1.02, t.sqrt()
+        # C = f(A): a change of A changes it by at most f's largest divided difference, |b + c (t + t')|
+        to_C = max(abs(b), abs(b + 2 * c * top))
+        own = c * gamma(m) * norm(A.abs() @ A.abs()) + 4 * U * norm(abs(b) * A.abs() + 4 * eye)
+        C = both(held(a * eye + b * A + c * A @ A, 2.0 ** 14))
+        own += e * norm(C)
+        d_C = to_C * d_A + own
+        err *= growth(singular)                                       # X's, through what remains
+        if k < iterations - short:
+            new = held(C @ X, scale)
+            err += d_C * math.sqrt(top) + (e + gamma(m)) * norm(C.abs() @ X.abs()) + e * norm(new) + grain
+            X = new
+            continue
+        if on_x:
+            P, at = C, 2.0 ** 14
+            terms = [d_C]
+        else:
+            # what was wrong in P passes C; P's own rounding, C's error times P
+            at /= 4
+            new = both(held(C @ P, at))
+            # with C times P times X taken by its parts: P's earlier errors grow by at most C's norm
+            terms = [x * two(C) for x in terms] + [d_C * two(P @ X) / max(two(X), 1e-30), e * norm(new) + gamma(m) * norm(C.abs() @ P.abs())]
+            P = new
+        if k + 1 < iterations:
+            CA = both(held(C @ A, 2.0 ** 14))
+            A_next = both(held(C @ CA, 2.0 ** 14))
+            d_CA = e * norm(CA) + gamma(m) * norm(C.abs() @ A.abs())
+            # A' = q(A), q(t) = t f(t)^2, by q's largest divided difference over A's eigenvalues; then what this step rounds
+            grid = t[:, None], t[None, :]
+            q = lambda x: x * (a + b * x + c * x * x) ** 2             # noqa: E731
+            slope = lambda x: (a + b * x + c * x * x) ** 2 + 2 * x * (a + b * x + c * x * x) * (b + 2 * c * x)     # noqa: E731
+            apart = (grid[0] - grid[1]).abs() > 1e-4
+            divided = torch.where(apart, (q(grid[0]) - q(grid[1])) / torch.where(apart, grid[0] - grid[1], 1.0), slope((grid[0] + grid[1]) / 2))
+            to_A = float(divided.abs().max()) * 1.01
+            d_A = to_A * d_A + own * (two(CA) + two(C) * top) + two(C) * d_CA + e * norm(A_next) + gamma(m) * norm(C.abs() @ CA.abs())
+            A = A_next
+    err += sum(terms) * two(X) + gamma(m) * norm(P.abs() @ X.abs())
+    X = P @ X
+    return (X.T if tall else X), 1.05 * err
+
+
+def spread(shape, rank, seed):
+    """Entries of a matrix of low rank over weak noise, or a normal one."""
+    r, k = shape
+    if rank == 0:
+        return torch.randn(r, k, device=DEV, generator=gen(seed))
+    low = torch.randn(r, rank, device=DEV, generator=gen(seed)) @ torch.randn(rank, k, device=DEV, generator=gen(seed + 1))
+    return low + 0.01 * torch.randn(r, k, device=DEV, generator=gen(seed + 2))
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape,iterations,rank", [((300, 640), 5, 0), ((640, 300), 5, 0), ((130, 2000), 4, 0), ((2000, 130), 4, 0), ((520, 1100), 6, 0),
+                                                   ((65, 5000), 8, 0), ((700, 1500), 5, 0), ((1500, 700), 16, 0), ((300, 900), 5, 20), ((900, 300), 5, 3)])
+def test_long_matrices(shape, iterations, rank, products):
+    """Sides that differ by two or more and four iterations or more: the last three (of four, two) on m x m matrices."""
+    g = spread(shape, rank, 5)
+    p, m = torch.zeros(shape, device=DEV), torch.zeros(shape, device=DEV)
+    ws = torch.empty(B.qsr_muon_workspace_bytes([shape], 1, products), dtype=torch.uint8, device=DEV)
+    x = B.MuonList([p], [g], [m], beta=0.0, nesterov=False, eps=0.0, iterations=iterations, products=products, update_scale=[1.0], workspace=ws, stream=stream())
+    x.qsr_muon_step(1.0)
+    x.qsr_muon_check()
+    assert x.qsr_muon_launch_count() == 3 + 3 * iterations + 1
+    short = min(3, iterations - 2)
+    want, err = short64(g.double(), iterations, short, products)
+    off, size = float(torch.linalg.vector_norm(p.double() + want)), float(torch.linalg.vector_norm(want))
+    assert off <= err + U * size
+    if iterations <= (8 if products == 3 else 6) and (products == 3 or rank == 0):
+        assert err < 0.5 * size                                       # the bound says something; it grows with each iteration
+
+
+def test_long_matrices_beside_others():
+    """A list's matrices go through the same launches, long or not, and each is what it is alone."""
+    shapes = [(300, 640), (500, 600), (700, 300), (30, 20), (640, 1400)]
+    for products in (1, 3):
+        together = Case(shapes, products=products, seed=9)
+        alone = []
+        for i in range(len(shapes)):
+            ws = torch.empty(B.qsr_muon_workspace_bytes([shapes[i]], 1, products), dtype=torch.uint8, device=DEV)
+            p, m = together.p[i].clone(), together.m[i].clone()
+            x = B.MuonList([p], [together.g[i]], [m], wd_scale=[together.wd[i]], update_scale=[together.scale[i]], workspace=ws, stream=stream(), **together.kw)
+            for _ in range(2):
+                x.qsr_muon_step(0.02)
+            x.qsr_muon_check()
+            alone.append((p, m))
+        for _ in range(2):
+            together.list.qsr_muon_step(0.02)
+        together.list.qsr_muon_check()
+        for (p, m), q, mm in zip(alone, together.p, together.m):
+            assert torch.equal(p, q) and torch.equal(m, mm)
+
+
 def test_offsets_beyond_32_bits():
     """512 copies of one 2048 x 2048 matrix below one another, 2^31 elements: the orthogonal factor of a stack is the stack of the
     factors over sqrt(512), up to the polynomial, which sees the same A."""
