@@ -57,8 +57,7 @@ __global__ void __launch_bounds__(256) lookup_kernel(const __grid_constant__ Loo
 
 // ---- sorting the tokens ----------------------------------------------------------------------------------
 
-// A stable radix sort of (token, row), lowest digits first.  Few rows: all passes by one block, in shared memory.  Many: the blocks
-// count their first digits, then there is one launch for each pass, in which every block finds its places from all blocks' counts
+// Many rows: a stable radix sort of (token, row), lowest digits first.  The blocks count their first digits, then there is one launch for each pass, in which every block finds its places from all blocks' counts
 // and counts the next digits of what it places where they land.  Tokens that are not in the vocabulary sort behind it.
 //
 // The launches of a gradient follow one another closely: each is started before the one before it has ended and waits for that.
@@ -69,7 +68,6 @@ constexpr int kMaxDigit = 10;          // bits
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
 constexpr int kSortPer = 4;            // keys that a thread holds at a time
 constexpr int kMaxSortBlocks = 128;
-constexpr int kFew = 4096, kFewThreads = 1024, kFewDigit = 8;
 
 struct SortParams {
     const int64_t *tokens;             // first pass; otherwise keys and rows
@@ -207,54 +205,6 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
             p.rows_out[to] = row[k];
             if (p.next_counts) atomicAdd(&p.next_counts[int64_t(to / per_block) * digits + ((key[k] >> (p.shift + p.bits)) & mask)], 1u);
         }
-    }
-}
-
-// Up to kFew rows: all passes of a sort by up to 8 bits at a time.
-__global__ void __launch_bounds__(kFewThreads) sort_few_kernel(const __grid_constant__ SortParams p)
-{
-    extern __shared__ uint32_t few[];                            // two sets of keys and rows, then [warps][digits]
-    __shared__ uint32_t scratch[32];
-    let_next_launch_start();
-    const int n = int(p.n), digits = 1 << p.bits, mask = digits - 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint32_t *keys[2] = {few, few + 2 * kFew}, *rows[2] = {few + kFew, few + 3 * kFew}, *places = few + 4 * kFew, *place = places + warp * digits;
-    const int per_warp = ((n + 1023) / 1024) * 32, begin = warp * per_warp, end = min(n, begin + per_warp);
-    for (int i = begin + lane; i < end; i += 32) {
-        keys[0][i] = key_of(p.tokens[i], p.vocab);
-        rows[0][i] = uint32_t(i);
-    }
-    for (int pass = 0; pass < p.passes; ++pass) {
-        const uint32_t *key = keys[pass & 1], *row = rows[pass & 1];
-        const int shift = pass * p.bits;
-        for (int i = threadIdx.x; i < 32 * digits; i += kFewThreads) places[i] = 0;
-        __syncthreads();
-        for (int i = begin + lane; i < end; i += 32) atomicAdd(&place[(key[i] >> shift) & mask], 1u);
-        __syncthreads();
-        uint32_t total = 0;
-        if (int(threadIdx.x) < digits)
-#pragma unroll
-            for (int w = 0; w < 32; ++w) total += places[w * digits + threadIdx.x];
-        uint32_t at = exclusive_scan<kFewThreads>(total, scratch);
-        if (int(threadIdx.x) < digits)
-#pragma unroll
-            for (int w = 0; w < 32; ++w) {
-                const uint32_t c = places[w * digits + threadIdx.x];
-                places[w * digits + threadIdx.x] = at;
-                at += c;
-            }
-        __syncthreads();
-        const bool last = pass + 1 == p.passes;
-        uint32_t *key_to = last ? p.keys_out : keys[(pass & 1) ^ 1], *row_to = last ? p.rows_out : rows[(pass & 1) ^ 1];
-        for (int i0 = begin; i0 < end; i0 += 32) {
-            const int i = i0 + lane;
-            const bool live = i < end;
-            const uint32_t k = live ? key[i] : 0u, r = live ? row[i] : 0u, to = take_place(place, (k >> shift) & uint32_t(mask), live, lane);
-            if (live) {
-                key_to[to] = k;
-                row_to[to] = r;
-            }
-        }
-        __syncthreads();
     }
 }
 
@@ -498,24 +448,224 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     if (col < width) write_row<VEC>(p, token, s, lane, lanes, first);
 }
 
+// ---- few rows --------------------------------------------------------------------------------------------
+
+// All in one launch, since launches and not bytes are what few rows cost.  A block has every 2^stride-th token (neighbours are often frequent
+// together) and up to 64 columns: it picks the rows of its tokens out of all rows in their order, sorts them (stable, a digit at a time, in
+// shared memory), and adds them.  A group of threads takes a token; the rows of one that occurs often are shared by all groups, whose
+// sums are added in their order.  2048 rows of 128 bf16 numbers, 1000 tokens, a quarter of the rows with the five most frequent: 7.0 us in a graph, of
+// which 2 are an empty launch's; what is left is the chain load, sort, load, add.
+struct FewParams {
+    SumParams sum;
+    const int64_t *tokens;
+    int32_t stride, passes, bits;      // stride: log2 of the blocks that share the tokens; of a token's number in its block, a pass's bits
+};
+constexpr int kFew = 4096, kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kFewBlocks = 384;        // 768 were slower with few columns (9.5 us for 6.4) and with many (49 for 43)
+constexpr int kFewLanes = 8;           // threads of a group, at most: 64 columns
+constexpr int kFewRange = 8192;        // tokens of a block, at most
+constexpr int kFewDigit = 7;           // bits
+constexpr int kFewTokens = 8;          // of a thread at a time
+constexpr int kOften = 16;             // rows from which on a token is everybody's: 32 take 8.0 us instead of 7.0 above, and 31 instead of
+                                       // 36 for 4096 rows of 4096
+
+// Adds rows list[first], list[first + step], ... of `count` to s.
+template <typename T, bool VEC, int AHEAD>
+__device__ __forceinline__ void add_rows(float (&s)[8], const SumParams &p, const T *base, const uint32_t *list, int first, int step, int count, int lane, int lanes, int width)
+{
+    for (int i = first; i < count; i += AHEAD * step) {
+        Raw8 r[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i + k * step < count) fetch<VEC>(r[k], base + int64_t(list[i + k * step]) * p.d_out_stride, lane, lanes, 0, width, Kind<T>::type);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (i + k * step >= count) break;
+            float x[8];
+            widen8(x, r[k], Kind<T>::type);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += x[j];
+        }
+    }
+}
+
+// The first of positions [from, to) whose key is not `key`, or `to`; those with it come first.
+__device__ __forceinline__ int end_of(const uint32_t *keys, uint32_t key, int from, int to)
+{
+    while (from < to) {
+        const int mid = (from + to) >> 1;
+        if (keys[mid] == key) from = mid + 1;
+        else to = mid;
+    }
+    return from;
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant__ FewParams f)
+{
+    extern __shared__ uint32_t memory[];                         // two sets of [n] keys and [n] rows
+    __shared__ uint32_t scratch[kFewWarps], found[kFewWarps], often[kFew / kOften], n_often, n_runs;
+    __shared__ uint32_t present[kFewRange / 32], places[kFewWarps << kFewDigit];
+    __shared__ float shared[8][kFewWarps][kFewLanes];
+    const SumParams &p = f.sum;
+    const int n = int(p.n), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t vocab = uint32_t(p.vocab), self = blockIdx.x, others = (1u << f.stride) - 1u;
+    const int range = self < vocab ? int(((vocab - 1u - self) >> f.stride) + 1u) : 0;       // tokens self, self + 2^stride, ...
+    uint32_t *keys = memory, *rows = keys + n, *keys_to = rows + n, *rows_to = keys_to + n;
+    for (int i = threadIdx.x; i < (range + 31) / 32; i += kFewThreads) present[i] = 0;
+    if (threadIdx.x == 0) n_often = n_runs = 0;
+    __syncthreads();
+    // a warp's share of the rows: those with the block's tokens to the front of its share, then all shares together
+    const int per_warp = ((n + kFewThreads - 1) / kFewThreads) * 32, from = warp * per_warp, to = min(n, from + per_warp);
+    int here = 0;
+    for (int i0 = from; i0 < to; i0 += 32 * kFewTokens) {
+        uint32_t token[kFewTokens];
+#pragma unroll
+        for (int k = 0; k < kFewTokens; ++k) {
+            const int i = i0 + k * 32 + lane;
+            token[k] = i < to ? key_of(f.tokens[i], vocab) : vocab;
+        }
+#pragma unroll
+        for (int k = 0; k < kFewTokens; ++k) {
+            const uint32_t t = token[k] >> f.stride;
+            const bool mine = token[k] < vocab && (token[k] & others) == self;
+            const uint32_t all = __ballot_sync(0xffffffffu, mine);
+            if (mine) {
+                const int at = from + here + __popc(all & ((1u << lane) - 1u));
+                keys_to[at] = t;
+                rows_to[at] = uint32_t(i0 + k * 32 + lane);
+                if (!p.accumulate && !(present[t >> 5] >> (t & 31) & 1u)) atomicOr(&present[t >> 5], 1u << (t & 31));
+            }
+            here += __popc(all);
+        }
+    }
+    if (lane == 0) found[warp] = uint32_t(here);
+    __syncthreads();
+    int before = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) {
+        before += w < warp ? int(found[w]) : 0;
+        count += int(found[w]);
+    }
+    for (int i = lane; i < here; i += 32) {
+        keys[before + i] = keys_to[from + i];
+        rows[before + i] = rows_to[from + i];
+    }
+    __syncthreads();
+    if (count > 1) {
+        const int digits = 1 << f.bits, mask = digits - 1, share = ((count + kFewThreads - 1) / kFewThreads) * 32, b = warp * share, e = min(count, b + share);
+        uint32_t *place = places + warp * digits;
+        for (int pass = 0; pass < f.passes; ++pass) {
+            const int shift = pass * f.bits;
+            for (int i = threadIdx.x; i < kFewWarps * digits; i += kFewThreads) places[i] = 0;
+            __syncthreads();
+            for (int i0 = b; i0 < e; i0 += 32) {                 // one addition for equal digits: a frequent token may be all there is
+                const int digit = i0 + lane < e ? int((keys[i0 + lane] >> shift) & uint32_t(mask)) : digits;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                if (digit < digits && lane == __ffs(int(same)) - 1) place[digit] += uint32_t(__popc(same));
+                __syncwarp();
+            }
+            __syncthreads();
+            uint32_t total = 0;
+            if (int(threadIdx.x) < digits)
+#pragma unroll
+                for (int w = 0; w < kFewWarps; ++w) total += places[w * digits + threadIdx.x];
+            uint32_t at = exclusive_scan<kFewThreads>(total, scratch);
+            if (int(threadIdx.x) < digits)
+#pragma unroll
+                for (int w = 0; w < kFewWarps; ++w) {
+                    const uint32_t c = places[w * digits + threadIdx.x];
+                    places[w * digits + threadIdx.x] = at;
+                    at += c;
+                }
+            __syncthreads();
+            for (int i0 = b; i0 < e; i0 += 32) {
+                const bool live = i0 + lane < e;
+                const uint32_t k = live ? keys[i0 + lane] : 0u, r = live ? rows[i0 + lane] : 0u, place_of = take_place(place, (k >> shift) & uint32_t(mask), live, lane);
+                if (live) {
+                    keys_to[place_of] = k;
+                    rows_to[place_of] = r;
+                }
+            }
+            __syncthreads();
+            uint32_t *const k = keys, *const r = rows;
+            keys = keys_to; rows = rows_to;
+            keys_to = k; rows_to = r;
+        }
+    }
+    const int lanes = p.lanes, groups = kFewThreads / lanes, group = int(threadIdx.x) / lanes, l = int(threadIdx.x) & (lanes - 1);
+    const int first = int(blockIdx.y) * lanes * 8, width = p.width - first;
+    const T *base = static_cast<const T *>(p.d_out) + first;
+    uint32_t *runs = keys_to;                                    // where a token's rows begin, in any order
+    for (int i = threadIdx.x; i < count; i += kFewThreads)
+        if (i == 0 || keys[i - 1] != keys[i]) runs[atomicAdd(&n_runs, 1u)] = uint32_t(i);
+    __syncthreads();
+    for (int k = group; k < int(n_runs); k += groups) {
+        const int i = int(runs[k]);
+        const uint32_t key = keys[i];
+        const int end = end_of(keys, key, i + 1, min(count, i + kOften));
+        if (end == i + kOften) {                                 // kOften rows or more
+            if (l == 0) often[atomicAdd(&n_often, 1u)] = uint32_t(i);
+            continue;
+        }
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add_rows<T, VEC, 4>(s, p, base, rows + i, 0, 1, end - i, l, lanes, width);
+        write_row<VEC>(p, (key << f.stride | self), s, l, lanes, first);
+    }
+    if (!p.accumulate) {
+        const float zero[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = group; t < range; t += groups)
+            if (!(present[t >> 5] >> (t & 31) & 1u)) write_row<VEC>(p, uint32_t(t) << f.stride | self, zero, l, lanes, first);
+    }
+    __syncthreads();
+    for (uint32_t o = 0; o < n_often; ++o) {
+        const int i = int(often[o]);
+        const uint32_t key = keys[i];
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        add_rows<T, VEC, 8>(s, p, base, rows + i, group, groups, end_of(keys, key, i + kOften, count) - i, l, lanes, width);
+        for (int d = lanes; d < 32; d *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += __shfl_xor_sync(0xffffffffu, s[j], d);
+        __syncthreads();
+        if (lane < lanes)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) shared[j][warp][l] = s[j];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int w = 1; w < kFewWarps; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += shared[j][w][l];
+            write_row<VEC>(p, (key << f.stride | self), s, l, lanes, first);
+        }
+    }
+}
+
 // ---- host side -------------------------------------------------------------------------------------------
 
 constexpr int64_t kMaxWidth = int64_t(1) << 20;
 
-struct Layout { int64_t keys[2], rows[2], counts, partial, bytes; int32_t chunk, chunks, blocks, passes, bits; bool few; int64_t per_warp; };
+struct Layout { int64_t keys[2], rows[2], counts, partial, bytes; int32_t chunk, chunks, blocks, passes, bits; int64_t per_warp; };
+
+// One launch for all, in which every block reads all tokens, instead of sorting them in launches of their own: 2048 x 128 (above) 7.0 us
+// against 17.0, 64 rows 4.4 against 12.2, 4096 x 4096 of 1000 tokens 36 against 49; the other way only where nearly all of the most rows have one
+// token, 27 against 24 us for 4096 x 512.
+bool is_few(int64_t rows, int64_t vocab) { return rows <= kFew && vocab <= int64_t(1) << 21; }
 
 Layout layout_of(int64_t rows, int64_t vocab, int64_t width)
 {
     Layout l = {};
+    if (is_few(rows, vocab)) {
+        l.bytes = 256;                                           // none is used
+        return l;
+    }
     // chunks: short enough that every multiprocessor has several, at most 32 (partial sums: two for a chunk's rows)
     l.chunk = 8;
     while (l.chunk < 32 && rows / l.chunk > 148 * 8) l.chunk *= 2;
     l.chunks = int32_t((rows + l.chunk - 1) / l.chunk);
     int bits = 1;
     while ((vocab >> bits) != 0) bits++;                        // of `vocab` itself, which stands for no token
-    l.few = rows <= kFew;
-    const int most = l.few ? kFewDigit : kMaxDigit;
-    l.passes = (bits + most - 1) / most;
+    l.passes = (bits + kMaxDigit - 1) / kMaxDigit;
     l.bits = (bits + l.passes - 1) / l.passes;
     l.blocks = int32_t(std::min<int64_t>(std::max<int64_t>(1, (rows + 2047) / 2048), kMaxSortBlocks));
     l.per_warp = std::max<int64_t>(32, ((rows + l.blocks - 1) / l.blocks + kSortThreads - 1) / kSortThreads * 32);
@@ -568,15 +718,6 @@ int launch_sums(SumParams p, bool vec, int64_t sum_blocks, int64_t clear_blocks,
 
 int launch_sort(SortParams &s, const Layout &l, uint32_t *const *keys, uint32_t *const *rows, cudaStream_t st)
 {
-    if (l.few) {
-        const size_t shared = size_t(4 * kFew + (32 << l.bits)) * 4;
-        static std::atomic<uint64_t> raised{0};
-        if (int err = allow_shared(reinterpret_cast<const void *>(sort_few_kernel), (4 * kFew + (32 << kFewDigit)) * 4, raised)) return err;
-        s.keys_out = keys[0]; s.rows_out = rows[0];
-        sort_few_kernel<<<1, kFewThreads, shared, st>>>(s);
-        s.keys = keys[0]; s.rows = rows[0];
-        return int(cudaGetLastError());
-    }
     const int64_t counts = int64_t(l.blocks) << l.bits;
     uint32_t *const first = s.counts;
     s.next_counts = first + counts;
@@ -597,8 +738,40 @@ int launch_sort(SortParams &s, const Layout &l, uint32_t *const *keys, uint32_t 
     return 0;
 }
 
+template <typename T, bool VEC>
+int launch_few(const FewParams &f, unsigned ranges, cudaStream_t st)
+{
+    const size_t shared = 4 * size_t(f.sum.n) * 4;
+    static std::atomic<uint64_t> raised{0};
+    if (int err = allow_shared(reinterpret_cast<const void *>(few_kernel<T, VEC>), 4 * kFew * 4, raised)) return err;
+    few_kernel<T, VEC><<<dim3(ranges, unsigned(f.sum.tiles)), kFewThreads, shared, st>>>(f);
+    return int(cudaGetLastError());
+}
+
 int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
 {
+    SumParams p = {};
+    p.d_out = a.out; p.d_table = a.table;
+    p.n = a.rows; p.vocab = a.vocab; p.d_out_stride = a.out_stride; p.d_table_stride = a.table_stride;
+    p.width = int32_t(a.width); p.table_type = a.table_type; p.accumulate = a.accumulate;
+    p.scale = float(a.scale);
+    const int granules = int((a.width + 7) / 8);
+    if (is_few(a.rows, a.vocab)) {
+        if (a.rows == 0 && a.accumulate) return 0;
+        p.lanes = std::min(kFewLanes, power_of_two(granules));
+        p.tiles = (granules + p.lanes - 1) / p.lanes;
+        FewParams f = {p, a.tokens, 0, 0, 0};
+        while ((int64_t(2) << f.stride) * p.tiles <= kFewBlocks && (int64_t(1) << f.stride) < a.vocab) f.stride++;
+        while ((a.vocab - 1) >> f.stride >= kFewRange) f.stride++;
+        int bits = 0;
+        while (((a.vocab - 1) >> f.stride) >> bits) bits++;
+        f.passes = (bits + kFewDigit - 1) / kFewDigit;
+        f.bits = f.passes ? (bits + f.passes - 1) / f.passes : 0;
+        const unsigned n = 1u << f.stride;
+        if (a.out_type == QSR_F32) return vec ? launch_few<float, true>(f, n, st) : launch_few<float, false>(f, n, st);
+        if (a.out_type == QSR_BF16) return vec ? launch_few<__nv_bfloat16, true>(f, n, st) : launch_few<__nv_bfloat16, false>(f, n, st);
+        return vec ? launch_few<__half, true>(f, n, st) : launch_few<__half, false>(f, n, st);
+    }
     const Layout l = layout_of(a.rows, a.vocab, a.width);
     char *ws = static_cast<char *>(a.workspace);
     uint32_t *keys[2], *rows[2];
@@ -612,15 +785,9 @@ int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
     s.n = a.rows; s.per_warp = l.per_warp; s.vocab = uint32_t(a.vocab); s.bits = l.bits; s.passes = l.passes;
     if (a.rows > 0)
         if (int err = launch_sort(s, l, keys, rows, st)) return err;
-    SumParams p = {};
-    p.d_out = a.out; p.d_table = a.table;
     p.keys = s.keys; p.rows = s.rows;
     p.partial = reinterpret_cast<float *>(ws + l.partial);
-    p.n = a.rows; p.vocab = a.vocab; p.d_out_stride = a.out_stride; p.d_table_stride = a.table_stride;
-    p.width = int32_t(a.width); p.table_type = a.table_type; p.accumulate = a.accumulate;
     p.chunk = l.chunk; p.chunks = l.chunks;
-    p.scale = float(a.scale);
-    const int granules = int((a.width + 7) / 8);
     p.lanes = std::min(kSumThreads, power_of_two(granules));
     p.tiles = (granules + p.lanes - 1) / p.lanes;
     const int64_t groups = kSumThreads / p.lanes, sum_blocks = (int64_t(l.chunks) * p.tiles + groups - 1) / groups;

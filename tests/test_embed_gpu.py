@@ -216,3 +216,14 @@ def test_captured_and_replayed_with_other_tokens():
     second = g.clone()
     B.qsr_embed_grad(d, t, g, workspace=ws, stream=stream())
     assert torch.equal(g, second) and not torch.equal(first, second)
+
+
+@pytest.mark.parametrize("kind,out", [("f32", "bf16"), ("bf16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("R,V,N", [(1, 2048, 3), (15, 3, 9), (16, 2049, 9), (17, 40, 64), (32, 1, 65), (33, 70000, 8), (257, 5000, 200), (4095, 6, 70), (4096, 300, 130), (4097, 300, 130),
+                                   (4096, 1 << 21, 2), (600, (1 << 21) + 1, 2)])
+def test_gradient_of_few_rows(R, V, N, kind, out, accumulate):
+    """One launch for up to 4096 rows and 2^21 tokens; the others sort."""
+    d = torch.randn(R, N, device=DEV, generator=gen(R)).to(T[out])
+    for how in ("zipf", "uniform", "same", "absent", "outside"):
+        check_grad(d, draw(R, V, R + V, how), V, 0.75, kind, accumulate)
