@@ -92,7 +92,8 @@ __device__ __forceinline__ float inverse_root(float x)
     return x > 1e-30f && x < 1e30f ? r * fmaf(-0.5f * x * r, r, 1.5f) : 1.0f / sqrtf(x);
 }
 
-// FULL kernels: every thread has all its elements (the row is lanes * HELD whole granules), so that nothing is compared with the width.
+// FULL kernels compare nothing with the width.  Forward: every thread has all its elements, the row is lanes * HELD whole granules.
+// Backward: the row is whole granules, and a thread has one or none.
 
 // Rows that fit in registers: HELD granules a thread, `lanes` threads a row (a power of two up to 32, or the whole block).  Mean and
 // variance take two passes over the registers, so that rows far from zero lose nothing.
@@ -317,119 +318,87 @@ __device__ __forceinline__ float spread_sum(const float (&v)[N], int lane)
     return a[0];
 }
 
-// Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take a row at a time, each thread
-// the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which leaves
-// one partial sum for each column.  The next DEPTH rows are loaded while one is worked on.
-template <typename T, bool VEC, bool FULL, int DEPTH, int THREADS>
-__global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
+// A thread's eight columns in the backward pass: weights, and the column sums that stay in its registers.
+struct Columns { float2 w[4], dw[4], db[4]; };
+template <bool VEC>
+__device__ __forceinline__ void start_columns(Columns &c, const Params &p, int lane, int lanes)
 {
-    extern __shared__ float shared[];             // a group's row sums: [groups][2][warps of a group][2]; then column sums
-    constexpr int TYPE = Kind<T>::type;
-    const int groups = int(blockDim.x) / lanes, group = int(threadIdx.x) / lanes, lane = int(threadIdx.x) - group * lanes;
-    const int warps = lanes >> 5;
-    const bool mine = FULL || column<VEC>(lane, lanes, 0, 0) < p.width;
-    float2 w[4], dw[4], db[4];
-    {
-        float v[8];
-        weights<VEC>(v, p.w, 1.0f, lane, lanes, 0, p.width, p.wtype, p.wvec != 0);
+    float v[8];
+    weights<VEC>(v, p.w, 1.0f, lane, lanes, 0, p.width, p.wtype, p.wvec != 0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j] = make_float2(v[2 * j], v[2 * j + 1]);
-            dw[j] = db[j] = make_float2(0.0f, 0.0f);
-        }
+    for (int j = 0; j < 4; ++j) {
+        c.w[j] = make_float2(v[2 * j], v[2 * j + 1]);
+        c.dw[j] = c.db[j] = make_float2(0.0f, 0.0f);
     }
-    Raw8 x[DEPTH], dy[DEPTH];
-    float means[DEPTH], rstds[DEPTH];
-    const auto load = [&](int i, int64_t row) {
-        const bool live = row < p.rows && mine;
-        const int64_t r = live ? row : 0;
-        fetch_row<VEC, FULL>(x[i], row_of<T>(p.x, r, p.x_stride), lane, lanes, 0, live, p.width, TYPE);
-        fetch_row<VEC, FULL>(dy[i], row_of<T>(p.dy, r, p.dy_stride), lane, lanes, 0, live, p.width, TYPE);
-        means[i] = live ? p.mean[r] : 0.0f;
-        rstds[i] = live ? p.rstd[r] : 0.0f;
-    };
-    int turn = 0;
-    const int64_t step = int64_t(gridDim.x) * groups;
-    int64_t row = int64_t(blockIdx.x) * groups + group;
+}
+// a: x becomes x - mean; d: dy becomes dy w; sum, product: this thread's shares of the row's two sums.
+template <bool VEC, bool FULL>
+__device__ __forceinline__ void add_columns(Pairs &a, Pairs &d, Columns &c, float &sum, float &product, float mean, float rstd, int lane, int lanes, int width)
+{
+    const float2 minus = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
+    float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
 #pragma unroll
-    for (int i = 0; i < DEPTH; ++i) load(i, row + i * step);
-    for (int64_t base = int64_t(blockIdx.x) * groups; base < p.rows; base += DEPTH * step) {       // `base`: the same for the block
-#pragma unroll
-        for (int i = 0; i < DEPTH; ++i, row += step) {
-            Pairs a, d;
-            widen_pairs(a, x[i], TYPE);
-            widen_pairs(d, dy[i], TYPE);
-            const float mean = means[i], rstd = rstds[i];
-            load(i, row + DEPTH * step);
-            const float2 minus = make_float2(-mean, -mean), times = make_float2(rstd, rstd);
-            float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                a.v[j] = add2(a.v[j], minus);
-                float2 hat = mul2(a.v[j], times);
-                if (!FULL) {       // beyond the row both are zero: a finite statistic gives no sum, one that is not finite is kept out
-                    if (column<VEC>(lane, lanes, 0, 2 * j) >= p.width) hat.x = 0.0f;
-                    if (column<VEC>(lane, lanes, 0, 2 * j + 1) >= p.width) hat.y = 0.0f;
-                }
-                dw[j] = fma2(d.v[j], hat, dw[j]);
-                db[j] = add2(db[j], d.v[j]);
-                d.v[j] = mul2(d.v[j], w[j]);
-                s1 = add2(s1, d.v[j]);
-                s2 = fma2(d.v[j], hat, s2);
-            }
-            if (!p.dx) continue;
-            float s[2] = {s1.x + s1.y, s2.x + s2.y};
-            if (lanes >= 32) {
-                const float v = spread_sum(s, lane & 31);
-                if (lanes == 32) {
-                    s[0] = __shfl_sync(0xffffffffu, v, 0);
-                    s[1] = __shfl_sync(0xffffffffu, v, 16);
-                } else {
-                    float *at = shared + (group * 2 + turn) * warps * 2;
-                    turn ^= 1;
-                    if ((lane & 15) == 0) at[(lane >> 5) * 2 + ((lane >> 4) & 1)] = v;
-                    group_barrier(group, lanes);
-                    if (warps <= 4) {
-                        s[0] = s[1] = 0.0f;
-                        for (int u = 0; u < warps; ++u) {
-                            s[0] += at[u * 2];
-                            s[1] += at[u * 2 + 1];
-                        }
-                    } else {
-                        const int u = lane & 31;
-                        s[0] = u < warps ? at[u * 2] : 0.0f;
-                        s[1] = u < warps ? at[u * 2 + 1] : 0.0f;
-                        const float all = spread_sum(s, u);
-                        s[0] = __shfl_sync(0xffffffffu, all, 0);
-                        s[1] = __shfl_sync(0xffffffffu, all, 16);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    for (int e = lanes >> 1; e; e >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], e);
-            }
-            if (row >= p.rows || !mine) continue;
-            const float c1 = -s[0] * p.inverse, c2 = -s[1] * p.inverse * rstd;
-            const float2 along = make_float2(c2, c2), level = make_float2(c1, c1);
-            float out[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 v = mul2(fma2(a.v[j], along, add2(d.v[j], level)), times);
-                out[2 * j] = v.x;
-                out[2 * j + 1] = v.y;
-            }
-            put_row<VEC, FULL>(row_of<T>(p.dx, row, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+    for (int j = 0; j < 4; ++j) {
+        a.v[j] = add2(a.v[j], minus);
+        float2 hat = mul2(a.v[j], times);
+        if (!FULL) {       // beyond the row both are zero: a finite statistic gives no sum, one that is not finite is kept out
+            if (column<VEC>(lane, lanes, 0, 2 * j) >= width) hat.x = 0.0f;
+            if (column<VEC>(lane, lanes, 0, 2 * j + 1) >= width) hat.y = 0.0f;
         }
+        c.dw[j] = fma2(d.v[j], hat, c.dw[j]);
+        c.db[j] = add2(c.db[j], d.v[j]);
+        d.v[j] = mul2(d.v[j], c.w[j]);
+        s1 = add2(s1, d.v[j]);
+        s2 = fma2(d.v[j], hat, s2);
     }
-    if (!p.partial) return;
+    sum = s1.x + s1.y;
+    product = s2.x + s2.y;
+}
+// N sums over the `warps` warps of a group; at: [warps][N] of shared memory, which calls use two of in turn.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&s)[N], float *at, int warps, int group, int lanes, int lane)
+{
+    constexpr int SHARE = 32 / N;                 // lanes that have the same value
+    const float v = spread_sum(s, lane & 31);
+    if ((lane & (SHARE - 1)) == 0) at[(lane >> 5) * N + (lane & 31) / SHARE] = v;
+    group_barrier(group, lanes);
+    if (warps <= 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = 0.0f;
+        for (int u = 0; u < warps; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[i] += at[u * N + i];
+    } else {
+        const int u = lane & 31;
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = u < warps ? at[u * N + i] : 0.0f;
+        const float all = spread_sum(s, u);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = __shfl_sync(0xffffffffu, all, i * SHARE);
+    }
+}
+__device__ __forceinline__ void row_gradient(float (&out)[8], const Pairs &a, const Pairs &d, float sum, float product, float inverse, float rstd)
+{
+    const float c1 = -sum * inverse, c2 = -product * inverse * rstd;
+    const float2 along = make_float2(c2, c2), level = make_float2(c1, c1), times = make_float2(rstd, rstd);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 v = mul2(fma2(a.v[j], along, add2(d.v[j], level)), times);
+        out[2 * j] = v.x;
+        out[2 * j + 1] = v.y;
+    }
+}
+// The groups' column sums, joined in their order, to the block's partial sums.  shared: eight floats a thread.
+template <bool VEC>
+__device__ __forceinline__ void leave_columns(const Params &p, const Columns &c, float *shared, int groups, int group, int lane, int lanes)
+{
     float *out = p.partial + int64_t(blockIdx.x) * 2 * p.width;
     for (int pass = 0; pass < 2; ++pass) {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            v[2 * j] = pass ? db[j].x : dw[j].x;
-            v[2 * j + 1] = pass ? db[j].y : dw[j].y;
+            v[2 * j] = pass ? c.db[j].x : c.dw[j].x;
+            v[2 * j + 1] = pass ? c.db[j].y : c.dw[j].y;
         }
         if (groups > 1) {
             __syncthreads();
@@ -444,10 +413,213 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
         if (group == 0)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = column<VEC>(lane, lanes, 0, j);
-                if (c < p.width) out[int64_t(pass) * p.width + c] = v[j];
+                const int col = column<VEC>(lane, lanes, 0, j);
+                if (col < p.width) out[int64_t(pass) * p.width + col] = v[j];
             }
     }
+}
+
+// Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take a row at a time, each thread
+// the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which leaves
+// one partial sum for each column.  The next row is loaded while one is worked on.
+template <typename T, bool VEC, bool FULL, int THREADS>
+__global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
+{
+    extern __shared__ float shared[];             // a group's row sums: [groups][2][warps of a group][2]; then column sums
+    constexpr int TYPE = Kind<T>::type;
+    const int groups = int(blockDim.x) / lanes, group = int(threadIdx.x) / lanes, lane = int(threadIdx.x) - group * lanes;
+    const int warps = lanes >> 5;
+    const bool mine = column<VEC>(lane, lanes, 0, 0) < p.width;
+    Columns c;
+    start_columns<VEC>(c, p, lane, lanes);
+    Raw8 x, dy;
+    float next_mean, next_rstd;
+    const auto load = [&](int64_t row) {
+        const bool live = row < p.rows && mine;
+        const int64_t r = live ? row : 0;
+        fetch_row<VEC, FULL>(x, row_of<T>(p.x, r, p.x_stride), lane, lanes, 0, live, p.width, TYPE);
+        fetch_row<VEC, FULL>(dy, row_of<T>(p.dy, r, p.dy_stride), lane, lanes, 0, live, p.width, TYPE);
+        next_mean = live ? p.mean[r] : 0.0f;
+        next_rstd = live ? p.rstd[r] : 0.0f;
+    };
+    int turn = 0;
+    const int64_t step = int64_t(gridDim.x) * groups;
+    int64_t row = int64_t(blockIdx.x) * groups + group;
+    load(row);
+    for (int64_t base = int64_t(blockIdx.x) * groups; base < p.rows; base += step, row += step) {       // `base`: the same for the block
+        Pairs a, d;
+        widen_pairs(a, x, TYPE);
+        widen_pairs(d, dy, TYPE);
+        const float mean = next_mean, rstd = next_rstd;
+        load(row + step);
+        float s[2];
+        add_columns<VEC, FULL>(a, d, c, s[0], s[1], mean, rstd, lane, lanes, p.width);
+        if (!p.dx) continue;
+        if (lanes > 32) {
+            group_sums(s, shared + (group * 2 + turn) * warps * 2, warps, group, lanes, lane);
+            turn ^= 1;
+        } else if (lanes == 32) {
+            const float v = spread_sum(s, lane);
+            s[0] = __shfl_sync(0xffffffffu, v, 0);
+            s[1] = __shfl_sync(0xffffffffu, v, 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                for (int e = lanes >> 1; e; e >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], e);
+        }
+        if (row >= p.rows || !mine) continue;
+        float out[8];
+        row_gradient(out, a, d, s[0], s[1], p.inverse, rstd);
+        put_row<VEC, FULL>(row_of<T>(p.dx, row, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+    }
+    if (p.partial) leave_columns<VEC>(p, c, shared, groups, group, lane, lanes);
+}
+
+// The same for aligned rows that a whole block takes: they come by bulk copies into a ring of shared memory, `stages` rows of x and dy
+// ahead, issued by one thread, and are worked on ROWS at a time, whose sums cross the block together.  So many rows under way would not
+// fit in registers beside the column sums.  Against the kernel above, which has one row ahead: 4099 x 5003 fp32 60 us instead of 66,
+// 8192 x 4096 bf16 55 instead of 59, 4096 x 8192 bf16 59 instead of 76.  A multiprocessor's bulk copies follow one another at a few hundred
+// clocks each, so that rows of which a block holds several at once gain nothing (12544 x 768 bf16: 21 to 24 us instead of 18.4).  Bound
+// by what a row costs its block in instructions and exchanges, beside the copies: 3.6 to 4.9 TB/s.
+constexpr int kMaxStages = 8;
+constexpr long long kPatience = 6000000000;       // clocks that a wait may take, some seconds
+
+__device__ __forceinline__ bool copied(uint32_t bar, unsigned parity)
+{
+    uint32_t done;
+    asm volatile("{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ bool wait_for_copy(uint32_t bar, unsigned parity)
+{
+    if (copied(bar, parity)) return true;
+    for (const long long begin = clock64(); clock64() - begin < kPatience;)
+        for (int i = 0; i < 64; ++i)
+            if (copied(bar, parity)) return true;
+    return false;
+}
+// Eight elements of a row in shared memory.  `left`: how many the row has from there on; behind it lies whatever follows it in memory.
+template <typename T, bool FULL>
+__device__ __forceinline__ void take_shared(Raw8 &r, uint32_t from, int left)
+{
+#pragma unroll
+    for (int h = 0; h < int(sizeof(T)) / 2; ++h)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[4 * h]), "=r"(r.w[4 * h + 1]), "=r"(r.w[4 * h + 2]), "=r"(r.w[4 * h + 3])
+                     : "r"(from + h * 16) : "memory");
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (j < left || (FULL && left > 0)) continue;
+        if (sizeof(T) == 4) r.w[j] = 0u;
+        else r.w[j / 2] &= j & 1 ? 0xffffu : 0xffff0000u;
+    }
+}
+
+template <typename T, bool FULL, int ROWS, int THREADS>
+__global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_constant__ Params p, int stages)
+{
+    extern __shared__ __align__(128) char ring[];                // [stages][x, dy]
+    __shared__ __align__(8) unsigned long long full[kMaxStages];
+    __shared__ float sums[2][THREADS / 32][2 * ROWS];     // used in turn
+    constexpr int TYPE = Kind<T>::type, BYTES = int(sizeof(T));
+    const int lanes = int(blockDim.x), lane = int(threadIdx.x), left = p.width - lane * 8, slot = lanes * 8 * BYTES;
+    const uint32_t bars = uint32_t(__cvta_generic_to_shared(full)), slots = uint32_t(__cvta_generic_to_shared(ring));
+    const int64_t step = gridDim.x;
+    // Copies are of 16 bytes and more: what follows a row up to there lies in the matrix, except behind the last row, whose end is
+    // read as it is wanted.
+    const auto issue = [&](int stage, int64_t row) {
+        const unsigned n = unsigned(row + 1 < p.rows ? (p.width * BYTES + 15) & ~15 : p.width * BYTES & ~15);
+        const uint32_t bar = bars + stage * 8, to = slots + stage * 2 * slot;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(2 * n) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(row_of<T>(p.x, row, p.x_stride)), "r"(n),
+                     "r"(bar) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + slot), "l"(row_of<T>(p.dy, row, p.dy_stride)),
+                     "r"(n), "r"(bar) : "memory");
+    };
+    int under_way = 0;
+    if (lane == 0) {
+        for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + i * 8) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
+        for (; under_way < stages && blockIdx.x + under_way * step < p.rows; ++under_way) issue(under_way, blockIdx.x + under_way * step);
+    }
+    Columns c;
+    start_columns<true>(c, p, lane, lanes);
+    float next_mean[ROWS], next_rstd[ROWS];
+    const auto statistics = [&](int64_t row) {                   // zeros where there is no row, or no column
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const bool live = row + r * step < p.rows && left > 0;
+            next_mean[r] = live ? p.mean[row + r * step] : 0.0f;
+            next_rstd[r] = live ? p.rstd[row + r * step] : 0.0f;
+        }
+    };
+    statistics(blockIdx.x);
+    __syncthreads();
+    int turn = 0, stage = 0;
+    unsigned phase = 0;
+    bool all_came = true;
+    for (int64_t row = blockIdx.x; row < p.rows; row += ROWS * step) {
+        const int live = row + step < p.rows ? ROWS : 1;         // of ROWS, one or two
+        float mean[ROWS], rstd[ROWS], s[2 * ROWS];
+        Pairs a[ROWS], d[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            mean[r] = next_mean[r];
+            rstd[r] = next_rstd[r];
+        }
+        statistics(row + ROWS * step);
+        int at = stage;
+        unsigned parity = phase;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            Raw8 x, dy;
+            if (r < live) {
+                all_came = all_came && wait_for_copy(bars + at * 8, parity);
+                const uint32_t from = slots + at * 2 * slot + lane * 8 * BYTES;
+                const int64_t here = row + r * step;
+                if (!FULL && left < 8 && here + 1 == p.rows) {
+                    fetch<true>(x, row_of<T>(p.x, here, p.x_stride), lane, lanes, 0, p.width, TYPE);
+                    fetch<true>(dy, row_of<T>(p.dy, here, p.dy_stride), lane, lanes, 0, p.width, TYPE);
+                } else {
+                    take_shared<T, FULL>(x, from, left);
+                    take_shared<T, FULL>(dy, from + slot, left);
+                }
+                if (++at == stages) { at = 0; parity ^= 1u; }
+            } else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x.w[j] = dy.w[j] = 0u;
+            widen_pairs(a[r], x, TYPE);
+            widen_pairs(d[r], dy, TYPE);
+            if (!all_came) d[r].v[0].x = quiet_nan();            // a wait ran out: no number passes for a gradient
+            add_columns<true, FULL>(a[r], d[r], c, s[2 * r], s[2 * r + 1], mean[r], rstd[r], lane, lanes, p.width);
+        }
+        if (p.dx) group_sums(s, sums[turn][0], lanes >> 5, 0, lanes, lane);
+        else __syncthreads();
+        turn ^= 1;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {                         // all threads have taken these rows
+            if (r >= live || !all_came) break;
+            under_way--;
+            const int64_t next = row + (r + stages) * step;
+            if (lane == 0 && next < p.rows) {
+                issue(stage, next);
+                under_way++;
+            }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+        if (!p.dx || left <= 0) continue;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (r >= live) break;
+            float out[8];
+            row_gradient(out, a[r], d[r], s[2 * r], s[2 * r + 1], p.inverse, rstd[r]);
+            put_row<true, FULL>(row_of<T>(p.dx, row + r * step, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+        }
+    }
+    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: no copy may outlive the block
+        wait_for_copy(bars + stage * 8, phase);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+    }
+    if (p.partial) leave_columns<true>(p, c, nullptr, 1, 0, lane, lanes);
 }
 
 // Longer rows: their gradient by a block a row, which reads the row twice ...
@@ -549,7 +721,7 @@ __global__ void __launch_bounds__(32 * kFinish) finish_kernel(const float *parti
 template <typename T, int HELD, bool VEC, bool FULL>
 int launch_held(const Params &p, int lanes, cudaStream_t st)
 {
-    // Warps that stay where each gets two rows and more: 12544 x 768 in bf16 takes 9.1 us, 14.4 with a warp for every row.
+    // Warps that stay where each gets two rows and more: 12544 x 768 in bf16 takes 8.8 us, 14.4 with a warp for every row.
     if (lanes <= 32 && p.rows >= int64_t(2) * kResident * (256 / lanes)) {
         forward_rows_kernel<T, HELD, VEC, FULL><<<unsigned(kResident), 256, 0, st>>>(p, lanes);
         return int(cudaGetLastError());
@@ -586,22 +758,44 @@ int launch_forward(const Params &p, cudaStream_t st)
     return launch_granules<T, VEC, false>(p, lanes, held, st);
 }
 
+constexpr int kRingBytes = 100 * 1024;
+template <typename T, bool FULL, int ROWS, int THREADS>
+int launch_ring(const Params &p, int lanes, int blocks, cudaStream_t st)
+{
+    const int row = lanes * 16 * int(sizeof(T)), stages = std::max(2 * ROWS, std::min(kMaxStages, kRingBytes / row));
+    const auto kernel = backward_ring_kernel<T, FULL, ROWS, THREADS>;
+    static std::atomic<uint64_t> raised{0};
+    if (int err = allow_shared(reinterpret_cast<const void *>(kernel), std::max(kRingBytes, 2 * ROWS * THREADS * 16 * int(sizeof(T))), raised)) return err;
+    kernel<<<unsigned(blocks), unsigned(lanes), size_t(stages) * row, st>>>(p, stages);
+    return int(cudaGetLastError());
+}
+template <typename T, bool FULL>
+int launch_ring(const Params &p, int lanes, int blocks, cudaStream_t st)
+{
+    return lanes > 768 ? launch_ring<T, FULL, 1, kMaxThreads>(p, lanes, blocks, st)
+           : lanes > 640 ? launch_ring<T, FULL, 2, 768>(p, lanes, blocks, st) : launch_ring<T, FULL, 2, 640>(p, lanes, blocks, st);
+}
+
 template <typename T, bool VEC>
 int launch_backward(const Params &p, void *dw, void *db, cudaStream_t st)
 {
     int blocks = 0;
     if (p.granules <= kMaxThreads) {
         // as many groups as fit 768 threads, one block on a multiprocessor; rows that need more threads have fewer registers
-        constexpr int DEPTH = 1;
         const int lanes = p.granules <= 32 ? power_of_two(p.granules) : (p.granules + 31) / 32 * 32;
         const int groups = std::max(1, lanes <= 32 ? 512 / lanes : std::min(768 / lanes, 15)), threads = groups * lanes;
         blocks = int(std::min<int64_t>((p.rows + groups - 1) / groups, kBlocks));
+        const bool full = VEC && p.width % 8 == 0;
         const size_t sums = size_t(groups) * size_t(lanes / 32) * 16, columns = groups > 1 ? size_t(threads) * 8 * 4 : 0;
-        const bool full = VEC && p.width == lanes * 8;
-        const auto kernel = threads > 768 ? (full ? backward_kernel<T, true, true, 1, kMaxThreads> : backward_kernel<T, VEC, false, 1, kMaxThreads>)
-                            : threads > 640 ? (full ? backward_kernel<T, true, true, DEPTH, 768> : backward_kernel<T, VEC, false, DEPTH, 768>)
-                                            : (full ? backward_kernel<T, true, true, DEPTH, 640> : backward_kernel<T, VEC, false, DEPTH, 640>);
-        kernel<<<unsigned(blocks), unsigned(threads), std::max(sums, columns), st>>>(p, lanes);
+        if (VEC && lanes > 768 / 2) {
+            const int err = full ? launch_ring<T, true>(p, lanes, blocks, st) : launch_ring<T, false>(p, lanes, blocks, st);
+            if (err) return err;
+        } else {
+            const auto kernel = threads > 768 ? backward_kernel<T, false, false, kMaxThreads>
+                                : threads > 640 ? (full ? backward_kernel<T, VEC, VEC, 768> : backward_kernel<T, VEC, false, 768>)
+                                                : (full ? backward_kernel<T, VEC, VEC, 640> : backward_kernel<T, VEC, false, 640>);
+            kernel<<<unsigned(blocks), unsigned(threads), std::max(sums, columns), st>>>(p, lanes);
+        }
     } else {
         if (p.partial) {
             const int wide = (p.granules + 255) / 256;

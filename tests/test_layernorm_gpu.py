@@ -273,3 +273,41 @@ def test_captured_and_on_a_stream_of_its_own():
     graph.replay()
     _, _, y64, _, _, tol = forward64(x, w, b)
     close(y, y64, rounded(tol, y64, "bf16"))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("R,N", [(1, 3080), (2, 3136), (148, 3081), (149, 4096), (297, 4100), (445, 5003), (300, 6144), (900, 3500), (450, 6145), (297, 8185), (151, 8192)])
+def test_wide_rows_in_aligned_buffers(R, N, kind):
+    """Rows that a block takes alone, several for each block, in buffers whose other columns are not numbers, and which end with the last row."""
+    x, dy, w, _ = inputs(R, N, kind, kind, R + N)
+    m64, r64 = forward64(x, None, None)[:2]
+    mean, rstd = m64[:, 0].float(), r64[:, 0].float()
+    pad = -N % 8
+
+    def wide(m):
+        flat = torch.full((R * (N + pad) - pad,), math.nan, device=DEV, dtype=T[kind])
+        out = flat.as_strided((R, N), (N + pad, 1))
+        out.copy_(m)
+        return out
+
+    xs, dys, dx = wide(x), wide(dy), wide(torch.zeros_like(x))
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    ws = torch.empty(B.qsr_layer_norm_workspace_bytes(R, N), dtype=torch.uint8, device=DEV)
+    B.qsr_layer_norm_grad(xs, dys, mean, rstd, d_x=dx, weight=w, d_weight=dw, d_bias=db, workspace=ws, stream=stream())
+    dx64, dw64, db64, tx, tw, tb = backward64(x, dy, mean, rstd, w)
+    close(dx, dx64, rounded(tx, dx64, kind))
+    close(dw, dw64, rounded(tw, dw64, kind))
+    close(db, db64, rounded(tb, db64, kind))
+    dw2 = torch.empty_like(w)
+    B.qsr_layer_norm_grad(xs, dys, mean, rstd, weight=w, d_weight=dw2, workspace=ws, stream=stream())
+    assert torch.equal(dw2, dw)
+    for over in (wide(x), wide(dy)):
+        a, d = (over, dys) if torch.equal(over, xs) else (xs, over)
+        B.qsr_layer_norm_grad(a, d, mean, rstd, d_x=over, weight=w, stream=stream())
+        assert torch.equal(over, dx)
+    if R > 2:
+        xs[R // 2, N - 1] = math.nan
+        dx2 = wide(torch.zeros_like(x))
+        B.qsr_layer_norm_grad(xs, dys, mean, rstd, d_x=dx2, weight=w, stream=stream())
+        rows = torch.arange(R, device=DEV) != R // 2
+        assert torch.equal(dx2[rows], dx[rows]) and torch.isnan(dx2[R // 2]).all()
