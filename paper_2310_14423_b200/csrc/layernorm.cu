@@ -421,7 +421,8 @@ __device__ __forceinline__ void leave_columns(const Params &p, const Columns &c,
 
 // Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take a row at a time, each thread
 // the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which leaves
-// one partial sum for each column.  The next row is loaded while one is worked on.
+// one partial sum for each column.  The next row is loaded while one is worked on.  12544 x 768 bf16: 16.3 us and 2 more for the sums of the blocks'
+// sums (58 MB, 3.5 TB/s): eleven rows for each group, whose chains of loads, exchanges and the joining at the end are what it waits for.
 template <typename T, bool VEC, bool FULL, int THREADS>
 __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
 {
@@ -758,7 +759,7 @@ int launch_forward(const Params &p, cudaStream_t st)
     return launch_granules<T, VEC, false>(p, lanes, held, st);
 }
 
-constexpr int kRingBytes = 100 * 1024;
+constexpr int kRingBytes = 100 * 1024;            // 200 KB are one to three per cent slower
 template <typename T, bool FULL, int ROWS, int THREADS>
 int launch_ring(const Params &p, int lanes, int blocks, cudaStream_t st)
 {
@@ -769,6 +770,7 @@ int launch_ring(const Params &p, int lanes, int blocks, cudaStream_t st)
     kernel<<<unsigned(blocks), unsigned(lanes), size_t(stages) * row, st>>>(p, stages);
     return int(cudaGetLastError());
 }
+// Two rows at a time (8192 x 4096 bf16 55.3 us, 58.6 one by one; 4096 x 4096 fp32 41.4 and 44.6), one where a thread has 64 registers.
 template <typename T, bool FULL>
 int launch_ring(const Params &p, int lanes, int blocks, cudaStream_t st)
 {

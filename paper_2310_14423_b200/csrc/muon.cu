@@ -43,7 +43,8 @@ __device__ __forceinline__ float scale_factor(float scale, double squares, float
 }
 
 // m <- m + (1 - beta)(g - m) and the sum of squares of u, chunk by chunk; the matrix's last chunk adds them in their order.
-// Squares and sums in binary64: the norm neither overflows nor loses small elements.
+// Squares and sums in binary64: the norm neither overflows nor loses small elements.  Bound by memory: 85 M elements with bf16 gradients (10 bytes
+// each) 143 us, 5.9 TB/s.
 __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid_constant__ MuonParams p)
 {
     __shared__ double scratch[kMomentumThreads / 32];
@@ -229,7 +230,8 @@ __device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix
         }
     }
 }
-// The blocks are taken from the last one on: the end of what the launch before has written is still in the second-level cache.
+// The blocks are taken from the last one on: the end of what the launch before has written is still in the second-level cache.  Bound by memory:
+// 85 M elements 129 us with one product (8 bytes each), 146 us with three (10 bytes).
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonParams p)
 {
     let_next_launch_start();
@@ -241,7 +243,9 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ MuonP
     else pack_block<false>(p, t, b, grad);
 }
 
-// theta <- theta - (lr wd theta + lr update_scale X) for one block of the last iterate.
+// theta <- theta - (lr wd theta + lr update_scale X) for one block of the last iterate.  85 M elements: 103 us in bf16 (6 bytes each), 178 us in fp32
+// with three products and bf16 copies (14 bytes, 6.7 TB/s).  The last product's threads doing this with the sums they have saves
+// 1 % of the step with one product, and costs 3 % with three, whose sums leave no registers for the parameters.
 template <bool WIDE>
 __device__ __forceinline__ void apply_block(const MuonParams &p, const MuonMatrix &t, const MuonBlock &b)
 {
@@ -517,7 +521,10 @@ struct Shared {
 // A pair of blocks (one per multiprocessor) takes tiles of 256 x 256 elements (or 256 x 128), pair, + pairs, ...; each has 128 of the tile's rows and
 // 128 of its columns in its shared memory, a stage at a time of 64 along the sum, and 128 x 256 sums in its tensor memory.  Two warps of
 // each block copy; one thread of the first block issues the products of both; eight warps take the tile before out of the other half of tensor memory.  Compared with 128 x 256 tiles of
-// single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.
+// single blocks, each multiprocessor copies and reads two thirds of the bytes for a product.  Bound by the tensor cores at the clock that the power limit
+// leaves (1.5 to 1.6 GHz): C X for 85 M elements with m = 768 takes 96 us, 1.36 PFLOP/s, and 293 us with three products (1.34); symmetric
+// m x m products, whose diagonal tiles are half wasted, 30 and 83 us for 48 matrices.  Staging results through shared memory and
+// sixteen warps for them were slower.
 template <bool POLYNOMIAL, int PRODUCTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
 product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Maps maps, const MuonTile *tiles, int n_tiles)
@@ -749,7 +756,8 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
 
 // A whole step of one matrix by one block: its shorter side is at most 128, its longer one at most 512, and X and A fit in shared memory,
 // where they stay through all iterations (C takes the place of A, every product that of its operand, once all sums are in tensor
-// memory).  The general way takes a launch for every product, whatever its size: 18 of 4 to 9 us each, against one.
+// memory).  The general way takes a launch for every product, whatever its size: 115 us for four of 128 x 128, 25 us this way, of which
+// fifteen products take 1.3 us each: one after the other, copies in and out of tensor memory included, and far from its rate.
 constexpr int kSmallThreads = 512;
 
 template <int PRODUCTS>
