@@ -623,6 +623,115 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
     if (p.partial) leave_columns<true>(p, c, nullptr, 1, 0, lane, lanes);
 }
 
+// Forward over many aligned rows, in the same way: blocks that stay, each thread with the weight and bias of its sixteen columns, so that a
+// row's exchanges are few beside its elements.  Mean and variance take two passes over the registers.
+template <typename T, bool FULL, int THREADS>
+__global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_kernel(const __grid_constant__ Params p, int stages)
+{
+    extern __shared__ __align__(128) char ring[];                // [stages] rows
+    __shared__ __align__(8) unsigned long long full[kMaxStages];
+    __shared__ float sums[2][THREADS / 32];                      // used in turn
+    constexpr int TYPE = Kind<T>::type, BYTES = int(sizeof(T)), HELD = 2;
+    const int lanes = int(blockDim.x), lane = int(threadIdx.x), warps = lanes >> 5, slot = HELD * lanes * 8 * BYTES;
+    const uint32_t bars = uint32_t(__cvta_generic_to_shared(full)), slots = uint32_t(__cvta_generic_to_shared(ring));
+    const int64_t step = gridDim.x;
+    const auto issue = [&](int stage, int64_t row) {             // of the last row, whole 16 bytes, as above
+        const unsigned n = unsigned(row + 1 < p.rows ? (p.width * BYTES + 15) & ~15 : p.width * BYTES & ~15);
+        const uint32_t bar = bars + stage * 8;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(slots + stage * slot),
+                     "l"(row_of<T>(p.x, row, p.x_stride)), "r"(n), "r"(bar) : "memory");
+    };
+    int under_way = 0;
+    if (lane == 0) {
+        for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + i * 8) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
+        for (; under_way < stages && blockIdx.x + under_way * step < p.rows; ++under_way) issue(under_way, blockIdx.x + under_way * step);
+    }
+    Pairs w[HELD], b[HELD];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        float v[8];
+        weights<true>(v, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
+        weights<true>(v, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
+    }
+    const auto left = [&](int k) { return p.width - (lane + k * lanes) * 8; };
+    const auto block_sum = [&](float2 v, float *at) {
+        const float mine = warp_sum(v.x + v.y);
+        if ((lane & 31) == 0) at[lane >> 5] = mine;
+        __syncthreads();
+        return warp_sum((lane & 31) < warps ? at[lane & 31] : 0.0f);
+    };
+    __syncthreads();
+    int stage = 0;
+    unsigned phase = 0;
+    bool all_came = true;
+    for (int64_t row = blockIdx.x; row < p.rows; row += step) {
+        all_came = all_came && wait_for_copy(bars + stage * 8, phase);
+        Pairs x[HELD];
+        float2 s = make_float2(0.0f, 0.0f), q = s;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            Raw8 raw;
+            if (!FULL && left(k) < 8 && row + 1 == p.rows) fetch<true>(raw, row_of<T>(p.x, row, p.x_stride), lane, lanes, k, p.width, TYPE);
+            else take_shared<T, FULL>(raw, slots + stage * slot + (lane + k * lanes) * 8 * BYTES, left(k));
+            widen_pairs(x[k], raw, TYPE);
+            if (!all_came) x[k].v[0].x = quiet_nan();            // a wait ran out: no number passes for a result
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s = add2(s, x[k].v[j]);
+        }
+        const float mean = block_sum(s, sums[0]) * p.inverse;
+        if (all_came) {                                          // and all threads have taken this row
+            under_way--;
+            if (lane == 0 && row + stages * step < p.rows) {
+                issue(stage, row + stages * step);
+                under_way++;
+            }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const float2 minus = FULL && left(k) <= 0 ? make_float2(0.0f, 0.0f) : make_float2(-mean, -mean);      // nothing beyond the row
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[k].v[j] = add2(x[k].v[j], minus);
+                if (!FULL) {
+                    if (2 * j >= left(k)) x[k].v[j].x = 0.0f;
+                    if (2 * j + 1 >= left(k)) x[k].v[j].y = 0.0f;
+                }
+                q = fma2(x[k].v[j], x[k].v[j], q);
+            }
+        }
+        const float rstd = inverse_root(fmaf(block_sum(q, sums[1]), p.inverse, p.eps));
+        if (lane == 0) {
+            if (p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+        void *to = row_of<T>(p.y, row, p.y_stride);
+        const float2 times = make_float2(rstd, rstd);
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            if (left(k) <= 0) break;
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 v = fma2(mul2(x[k].v[j], times), w[k].v[j], b[k].v[j]);
+                y[2 * j] = v.x;
+                y[2 * j + 1] = v.y;
+            }
+            put_row<true, FULL>(to, y, lane, lanes, k, p.width, TYPE);
+        }
+    }
+    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: no copy may outlive the block
+        wait_for_copy(bars + stage * 8, phase);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+    }
+}
+
 // Longer rows: their gradient by a block a row, which reads the row twice ...
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads) backward_long_kernel(const __grid_constant__ Params p)
@@ -743,9 +852,33 @@ int launch_granules(const Params &p, int lanes, int held, cudaStream_t st)
     }
 }
 
+template <typename T, bool FULL, int THREADS>
+int launch_forward_ring(const Params &p, int lanes, cudaStream_t st)
+{
+    constexpr int BLOCKS = kMaxThreads / THREADS, BYTES = 200 * 1024 / BLOCKS;         // on a multiprocessor; of each
+    const int slot = lanes * 16 * int(sizeof(T)), stages = std::min(kMaxStages, BYTES / slot);
+    const auto kernel = forward_ring_kernel<T, FULL, THREADS>;
+    static std::atomic<uint64_t> raised{0};
+    if (int err = allow_shared(reinterpret_cast<const void *>(kernel), BYTES, raised)) return err;
+    kernel<<<unsigned(kBlocks * BLOCKS), unsigned(lanes), size_t(stages) * slot, st>>>(p, stages);
+    return int(cudaGetLastError());
+}
+template <typename T, bool FULL>
+int launch_forward_ring(const Params &p, int lanes, cudaStream_t st)
+{
+    return lanes > 512 ? launch_forward_ring<T, FULL, 1024>(p, lanes, st)
+           : lanes > 256 ? launch_forward_ring<T, FULL, 512>(p, lanes, st)
+           : lanes > 128 ? launch_forward_ring<T, FULL, 256>(p, lanes, st) : launch_forward_ring<T, FULL, 128>(p, lanes, st);
+}
+
 template <typename T, bool VEC>
 int launch_forward(const Params &p, cudaStream_t st)
 {
+    if (VEC && p.granules > 32 * kMaxHeld && p.granules <= 2 * kMaxThreads) {
+        const int lanes = (p.granules + 63) / 64 * 32, blocks = kBlocks * (kMaxThreads / std::max(128, power_of_two(lanes)));
+        if (p.rows >= 4 * int64_t(blocks))
+            return p.width % 8 == 0 ? launch_forward_ring<T, true>(p, lanes, st) : launch_forward_ring<T, false>(p, lanes, st);
+    }
     // a warp a row up to 1024 elements, then the smallest block that holds a row in its registers
     int lanes = p.granules <= 32 ? power_of_two(p.granules) : 32;
     if (p.granules > 32 * kMaxHeld) lanes = 128;
