@@ -275,6 +275,32 @@ def test_captured_and_on_a_stream_of_its_own():
     close(y, y64, rounded(tol, y64, "bf16"))
 
 
+@pytest.mark.parametrize("kind,wkind", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("R,N", [(4800, 1032), (4736, 2048), (4735, 2045), (2400, 3001), (2369, 4096), (1200, 4101), (1185, 8192), (600, 8193), (593, 16384), (592, 16389)])
+def test_many_wide_rows(R, N, kind, wkind):
+    """Enough rows for blocks that stay, and a few less; buffers as below; in place."""
+    x, _, w, b = inputs(R, N, kind, wkind, R + N)
+    pad = -N % 8
+
+    def wide(m):
+        flat = torch.full((R * (N + pad) - pad,), math.nan, device=DEV, dtype=T[kind])
+        out = flat.as_strided((R, N), (N + pad, 1))
+        out.copy_(m)
+        return out
+
+    xs, y, mean, rstd = wide(x), wide(torch.zeros_like(x)), torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    B.qsr_layer_norm(xs, y, weight=w, bias=b, mean=mean, rstd=rstd, eps=EPS, stream=stream())
+    for rows in (slice(0, R // 2), slice(R // 2, R)):
+        m64, r64, y64, dm, dr, tol = forward64(x[rows], w, b)
+        close(mean[rows], m64[:, 0], dm[:, 0] + U * m64[:, 0].abs())
+        close(rstd[rows], r64[:, 0], dr[:, 0])
+        close(y[rows], y64, rounded(tol, y64, kind))
+    xs[R // 3, N - 1] = math.nan
+    B.qsr_layer_norm(xs, xs, weight=w, bias=b, eps=EPS, stream=stream())
+    rows = torch.arange(R, device=DEV) != R // 3
+    assert torch.equal(xs[rows], y[rows]) and torch.isnan(xs[R // 3]).all()
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("R,N", [(1, 3080), (2, 3136), (148, 3081), (149, 4096), (297, 4100), (445, 5003), (300, 6144), (900, 3500), (450, 6145), (297, 8185), (151, 8192)])
 def test_wide_rows_in_aligned_buffers(R, N, kind):
