@@ -421,8 +421,8 @@ __device__ __forceinline__ void leave_columns(const Params &p, const Columns &c,
 
 // Backward for rows of up to 8 x 1024 elements.  `lanes` threads (a power of two up to 32, or whole warps) take a row at a time, each thread
 // the same eight columns of every row, so that the column sums stay in its registers; groups of lanes share a block, which leaves
-// one partial sum for each column.  The next row is loaded while one is worked on.  12544 x 768 bf16: 16.3 us and 2 more for the sums of the blocks'
-// sums (58 MB, 3.5 TB/s): eleven rows for each group, whose chains of loads, exchanges and the joining at the end are what it waits for.
+// one partial sum for each column.  The next row is loaded while one is worked on.  12544 x 768 bf16: 15 us and 2 more for the sums of the blocks'
+// sums (58 MB, 3.8 TB/s): bound by instructions (issue 65 %), and by its beginning and end, since a group has but eleven rows.
 template <typename T, bool VEC, bool FULL, int THREADS>
 __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant__ Params p, int lanes)
 {
@@ -435,19 +435,25 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
     start_columns<VEC>(c, p, lane, lanes);
     Raw8 x, dy;
     float next_mean, next_rstd;
-    const auto load = [&](int64_t row) {
-        const bool live = row < p.rows && mine;
-        const int64_t r = live ? row : 0;
-        fetch_row<VEC, FULL>(x, row_of<T>(p.x, r, p.x_stride), lane, lanes, 0, live, p.width, TYPE);
-        fetch_row<VEC, FULL>(dy, row_of<T>(p.dy, r, p.dy_stride), lane, lanes, 0, live, p.width, TYPE);
-        next_mean = live ? p.mean[r] : 0.0f;
-        next_rstd = live ? p.rstd[r] : 0.0f;
+    // rows below 2^31, and pointers that are moved on: the loop is short of instructions
+    const unsigned rows = unsigned(p.rows), step = gridDim.x * unsigned(groups);
+    unsigned row = blockIdx.x * unsigned(groups) + unsigned(group);
+    const T *from_x = static_cast<const T *>(p.x) + int64_t(row) * p.x_stride, *from_dy = static_cast<const T *>(p.dy) + int64_t(row) * p.dy_stride;
+    T *to = static_cast<T *>(p.dx) + int64_t(row) * p.dx_stride;
+    const float *from_mean = p.mean + row, *from_rstd = p.rstd + row;
+    const int64_t x_step = step * p.x_stride, dy_step = step * p.dy_stride, dx_step = step * p.dx_stride;
+    const auto load = [&](unsigned at) {
+        const bool live = at < rows && mine;
+        fetch_row<VEC, FULL>(x, from_x, lane, lanes, 0, live, p.width, TYPE);
+        fetch_row<VEC, FULL>(dy, from_dy, lane, lanes, 0, live, p.width, TYPE);
+        next_mean = live ? *from_mean : 0.0f;
+        next_rstd = live ? *from_rstd : 0.0f;
+        from_x += x_step; from_dy += dy_step;
+        from_mean += step; from_rstd += step;
     };
     int turn = 0;
-    const int64_t step = int64_t(gridDim.x) * groups;
-    int64_t row = int64_t(blockIdx.x) * groups + group;
     load(row);
-    for (int64_t base = int64_t(blockIdx.x) * groups; base < p.rows; base += step, row += step) {       // `base`: the same for the block
+    for (unsigned base = blockIdx.x * unsigned(groups); base < rows; base += step, row += step, to += dx_step) {       // `base`: the same for the block
         Pairs a, d;
         widen_pairs(a, x, TYPE);
         widen_pairs(d, dy, TYPE);
@@ -468,10 +474,10 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
             for (int k = 0; k < 2; ++k)
                 for (int e = lanes >> 1; e; e >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], e);
         }
-        if (row >= p.rows || !mine) continue;
+        if (row >= rows || !mine) continue;
         float out[8];
         row_gradient(out, a, d, s[0], s[1], p.inverse, rstd);
-        put_row<VEC, FULL>(row_of<T>(p.dx, row, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+        put_row<VEC, FULL>(to, out, lane, lanes, 0, p.width, TYPE);
     }
     if (p.partial) leave_columns<VEC>(p, c, shared, groups, group, lane, lanes);
 }
@@ -479,8 +485,8 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
 // The same for aligned rows that a whole block takes: they come by bulk copies into a ring of shared memory, `stages` rows of x and dy
 // ahead, issued by one thread, and are worked on ROWS at a time, whose sums cross the block together.  So many rows under way would not
 // fit in registers beside the column sums.  Against the kernel above, which has one row ahead: 4099 x 5003 fp32 60 us instead of 66,
-// 8192 x 4096 bf16 55 instead of 59, 4096 x 8192 bf16 59 instead of 76.  A multiprocessor's bulk copies follow one another at a few hundred
-// clocks each, so that rows of which a block holds several at once gain nothing (12544 x 768 bf16: 21 to 24 us instead of 18.4).  Bound
+// 8192 x 4096 bf16 55 instead of 59, 4096 x 8192 bf16 56 instead of 76.  A multiprocessor's bulk copies follow one another at a few hundred
+// clocks each, so that rows of which a block holds several at once gain nothing (12544 x 768 bf16: 21 to 24 us, when the kernel above took 18.4).  Bound
 // by what a row costs its block in instructions and exchanges, beside the copies: 3.6 to 4.9 TB/s.
 constexpr int kMaxStages = 8;
 constexpr long long kPatience = 6000000000;       // clocks that a wait may take, some seconds
@@ -524,7 +530,6 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
     constexpr int TYPE = Kind<T>::type, BYTES = int(sizeof(T));
     const int lanes = int(blockDim.x), lane = int(threadIdx.x), left = p.width - lane * 8, slot = lanes * 8 * BYTES;
     const uint32_t bars = uint32_t(__cvta_generic_to_shared(full)), slots = uint32_t(__cvta_generic_to_shared(ring));
-    const int64_t step = gridDim.x;
     // Copies are of 16 bytes and more: what follows a row up to there lies in the matrix, except behind the last row, whose end is
     // read as it is wanted.
     const auto issue = [&](int stage, int64_t row) {
@@ -540,17 +545,23 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
     if (lane == 0) {
         for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + i * 8) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
-        for (; under_way < stages && blockIdx.x + under_way * step < p.rows; ++under_way) issue(under_way, blockIdx.x + under_way * step);
+        for (; under_way < stages && blockIdx.x + under_way * gridDim.x < p.rows; ++under_way) issue(under_way, blockIdx.x + under_way * gridDim.x);
     }
     Columns c;
     start_columns<true>(c, p, lane, lanes);
     float next_mean[ROWS], next_rstd[ROWS];
-    const auto statistics = [&](int64_t row) {                   // zeros where there is no row, or no column
+    const unsigned rows = unsigned(p.rows), step = gridDim.x;    // below 2^31, and pointers that are moved on: fewer instructions
+    const float *from_mean = p.mean + blockIdx.x, *from_rstd = p.rstd + blockIdx.x;
+    T *to = static_cast<T *>(p.dx) + int64_t(blockIdx.x) * p.dx_stride;
+    const int64_t dx_step = step * p.dx_stride;
+    const auto statistics = [&](unsigned row) {                  // zeros where there is no row, or no column
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const bool live = row + r * step < p.rows && left > 0;
-            next_mean[r] = live ? p.mean[row + r * step] : 0.0f;
-            next_rstd[r] = live ? p.rstd[row + r * step] : 0.0f;
+            const bool live = row + r * step < rows && left > 0;
+            next_mean[r] = live ? *from_mean : 0.0f;
+            next_rstd[r] = live ? *from_rstd : 0.0f;
+            from_mean += step;
+            from_rstd += step;
         }
     };
     statistics(blockIdx.x);
@@ -558,8 +569,8 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
     int turn = 0, stage = 0;
     unsigned phase = 0;
     bool all_came = true;
-    for (int64_t row = blockIdx.x; row < p.rows; row += ROWS * step) {
-        const int live = row + step < p.rows ? ROWS : 1;         // of ROWS, one or two
+    for (unsigned row = blockIdx.x; row < rows; row += ROWS * step) {
+        const int live = row + step < rows ? ROWS : 1;         // of ROWS, one or two
         float mean[ROWS], rstd[ROWS], s[2 * ROWS];
         Pairs a[ROWS], d[ROWS];
 #pragma unroll
@@ -576,8 +587,8 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
             if (r < live) {
                 all_came = all_came && wait_for_copy(bars + at * 8, parity);
                 const uint32_t from = slots + at * 2 * slot + lane * 8 * BYTES;
-                const int64_t here = row + r * step;
-                if (!FULL && left < 8 && here + 1 == p.rows) {
+                const unsigned here = row + r * step;
+                if (!FULL && left < 8 && here + 1 == rows) {
                     fetch<true>(x, row_of<T>(p.x, here, p.x_stride), lane, lanes, 0, p.width, TYPE);
                     fetch<true>(dy, row_of<T>(p.dy, here, p.dy_stride), lane, lanes, 0, p.width, TYPE);
                 } else {
@@ -600,8 +611,8 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
         for (int r = 0; r < ROWS; ++r) {                         // all threads have taken these rows
             if (r >= live || !all_came) break;
             under_way--;
-            const int64_t next = row + (r + stages) * step;
-            if (lane == 0 && next < p.rows) {
+            const unsigned next = row + unsigned(r + stages) * step;
+            if (lane == 0 && next < rows) {
                 issue(stage, next);
                 under_way++;
             }
@@ -609,11 +620,11 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
         }
         if (!p.dx || left <= 0) continue;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
+        for (int r = 0; r < ROWS; ++r, to += dx_step) {
             if (r >= live) break;
             float out[8];
             row_gradient(out, a[r], d[r], s[2 * r], s[2 * r + 1], p.inverse, rstd[r]);
-            put_row<true, FULL>(row_of<T>(p.dx, row + r * step, p.dx_stride), out, lane, lanes, 0, p.width, TYPE);
+            put_row<true, FULL>(to, out, lane, lanes, 0, p.width, TYPE);
         }
     }
     for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: no copy may outlive the block
