@@ -602,7 +602,8 @@ int qsr_embed(const qsr_embed_args *args, void *cuda_stream);
 /* Bytes of workspace of the gradient.  Negative qsr_status on error. */
 int64_t qsr_embed_workspace_bytes(int64_t rows, int64_t vocab, int64_t width);
 
-/* The gradient.  One launch for up to 4096 rows of up to 2^21 tokens (none if there is nothing to do), otherwise several; asynchronous. */
+/* The gradient.  One launch for few rows (4096; up to 16384 of up to 64 columns) of up to 2^21 tokens, none if there is nothing to do,
+ * otherwise several; asynchronous. */
 int qsr_embed_grad(const qsr_embed_args *args, void *cuda_stream);
 
 /* ---- test hook ---------------------------------------------------------------------------------------- */

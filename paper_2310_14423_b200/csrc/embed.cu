@@ -464,7 +464,7 @@ struct FewParams {
     const int64_t *tokens;
     int32_t stride, passes, bits;      // stride: log2 of the blocks that share the tokens; of a token's number in its block, a pass's bits
 };
-constexpr int kFew = 4096, kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kFew = 16384, kFewThreads = 256, kFewWarps = kFewThreads / 32;
 constexpr int kFewBlocks = 384;        // 768 were slower with few columns (9.5 us for 6.4) and with many (49 for 43)
 constexpr int kFewLanes = 8;           // threads of a group, at most: 64 columns
 constexpr int kFewRange = 8192;        // tokens of a block, at most
@@ -475,7 +475,7 @@ constexpr int kOften = 16;             // rows from which on a token is everybod
 
 // Adds rows list[first], list[first + step], ... of `count` to s.
 template <typename T, bool VEC, int AHEAD>
-__device__ __forceinline__ void add_rows(float (&s)[8], const SumParams &p, const T *base, const uint32_t *list, int first, int step, int count, int lane, int lanes, int width)
+__device__ __forceinline__ void add_rows(float (&s)[8], const SumParams &p, const T *base, const uint16_t *list, int first, int step, int count, int lane, int lanes, int width)
 {
     for (int i = first; i < count; i += AHEAD * step) {
         Raw8 r[AHEAD];
@@ -494,7 +494,7 @@ __device__ __forceinline__ void add_rows(float (&s)[8], const SumParams &p, cons
 }
 
 // The first of positions [from, to) whose key is not `key`, or `to`; those with it come first.
-__device__ __forceinline__ int end_of(const uint32_t *keys, uint32_t key, int from, int to)
+__device__ __forceinline__ int end_of(const uint16_t *keys, uint32_t key, int from, int to)
 {
     while (from < to) {
         const int mid = (from + to) >> 1;
@@ -507,7 +507,7 @@ __device__ __forceinline__ int end_of(const uint32_t *keys, uint32_t key, int fr
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant__ FewParams f)
 {
-    extern __shared__ uint32_t memory[];                         // two sets of [n] keys and [n] rows
+    extern __shared__ uint16_t memory[];                         // two sets of [n] keys and [n] rows, which are below 2^16
     __shared__ uint32_t scratch[kFewWarps], found[kFewWarps], often[kFew / kOften], n_often, n_runs;
     __shared__ uint32_t present[kFewRange / 32], places[kFewWarps << kFewDigit];
     __shared__ float shared[8][kFewWarps][kFewLanes];
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant_
     const int n = int(p.n), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t vocab = uint32_t(p.vocab), self = blockIdx.x, others = (1u << f.stride) - 1u;
     const int range = self < vocab ? int(((vocab - 1u - self) >> f.stride) + 1u) : 0;       // tokens self, self + 2^stride, ...
-    uint32_t *keys = memory, *rows = keys + n, *keys_to = rows + n, *rows_to = keys_to + n;
+    uint16_t *keys = memory, *rows = keys + n, *keys_to = rows + n, *rows_to = keys_to + n;
     for (int i = threadIdx.x; i < (range + 31) / 32; i += kFewThreads) present[i] = 0;
     if (threadIdx.x == 0) n_often = n_runs = 0;
     __syncthreads();
@@ -536,8 +536,8 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant_
             const uint32_t all = __ballot_sync(0xffffffffu, mine);
             if (mine) {
                 const int at = from + here + __popc(all & ((1u << lane) - 1u));
-                keys_to[at] = t;
-                rows_to[at] = uint32_t(i0 + k * 32 + lane);
+                keys_to[at] = uint16_t(t);
+                rows_to[at] = uint16_t(i0 + k * 32 + lane);
                 if (!p.accumulate && !(present[t >> 5] >> (t & 31) & 1u)) atomicOr(&present[t >> 5], 1u << (t & 31));
             }
             here += __popc(all);
@@ -587,12 +587,12 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant_
                 const bool live = i0 + lane < e;
                 const uint32_t k = live ? keys[i0 + lane] : 0u, r = live ? rows[i0 + lane] : 0u, place_of = take_place(place, (k >> shift) & uint32_t(mask), live, lane);
                 if (live) {
-                    keys_to[place_of] = k;
-                    rows_to[place_of] = r;
+                    keys_to[place_of] = uint16_t(k);
+                    rows_to[place_of] = uint16_t(r);
                 }
             }
             __syncthreads();
-            uint32_t *const k = keys, *const r = rows;
+            uint16_t *const k = keys, *const r = rows;
             keys = keys_to; rows = rows_to;
             keys_to = k; rows_to = r;
         }
@@ -600,9 +600,9 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const __grid_constant_
     const int lanes = p.lanes, groups = kFewThreads / lanes, group = int(threadIdx.x) / lanes, l = int(threadIdx.x) & (lanes - 1);
     const int first = int(blockIdx.y) * lanes * 8, width = p.width - first;
     const T *base = static_cast<const T *>(p.d_out) + first;
-    uint32_t *runs = keys_to;                                    // where a token's rows begin, in any order
+    uint16_t *runs = keys_to;                                    // where a token's rows begin, in any order
     for (int i = threadIdx.x; i < count; i += kFewThreads)
-        if (i == 0 || keys[i - 1] != keys[i]) runs[atomicAdd(&n_runs, 1u)] = uint32_t(i);
+        if (i == 0 || keys[i - 1] != keys[i]) runs[atomicAdd(&n_runs, 1u)] = uint16_t(i);
     __syncthreads();
     for (int k = group; k < int(n_runs); k += groups) {
         const int i = int(runs[k]);
@@ -652,14 +652,18 @@ constexpr int64_t kMaxWidth = int64_t(1) << 20;
 struct Layout { int64_t keys[2], rows[2], counts, partial, bytes; int32_t chunk, chunks, blocks, passes, bits; int64_t per_warp; };
 
 // One launch for all, in which every block reads all tokens, instead of sorting them in launches of their own: 2048 x 128 (above) 7.0 us
-// against 17.0, 64 rows 4.4 against 12.2, 4096 x 4096 of 1000 tokens 36 against 49; the other way only where nearly all of the most rows have one
-// token, 27 against 24 us for 4096 x 512.
-bool is_few(int64_t rows, int64_t vocab) { return rows <= kFew && vocab <= int64_t(1) << 21; }
+// against 17.0, 64 rows 4.4 against 12.2, 4096 x 4096 of 1000 tokens 36 against 49.  Up to kFew rows where few parts of a row read them: 8192 x
+// 128 14 against 20, 16384 x 15 of 57048 tokens 27 against 46; but 8192 x 1024 32 against 27, 16384 x 128 24 against 22.  The other way
+// too where most of so many rows have one token, whose block then has most of the work: 8192 x 128 of one token 43 against 22.
+bool is_few(int64_t rows, int64_t vocab, int64_t width)
+{
+    return (rows <= kFew / 4 || rows * ((width + 63) / 64) <= kFew) && vocab <= int64_t(1) << 21;
+}
 
 Layout layout_of(int64_t rows, int64_t vocab, int64_t width)
 {
     Layout l = {};
-    if (is_few(rows, vocab)) {
+    if (is_few(rows, vocab, width)) {
         l.bytes = 256;                                           // none is used
         return l;
     }
@@ -745,9 +749,9 @@ int launch_sort(SortParams &s, const Layout &l, uint32_t *const *keys, uint32_t 
 template <typename T, bool VEC>
 int launch_few(const FewParams &f, unsigned ranges, cudaStream_t st)
 {
-    const size_t shared = 4 * size_t(f.sum.n) * 4;
+    const size_t shared = 4 * size_t(f.sum.n) * 2;
     static std::atomic<uint64_t> raised{0};
-    if (int err = allow_shared(reinterpret_cast<const void *>(few_kernel<T, VEC>), 4 * kFew * 4, raised)) return err;
+    if (int err = allow_shared(reinterpret_cast<const void *>(few_kernel<T, VEC>), 4 * kFew * 2, raised)) return err;
     few_kernel<T, VEC><<<dim3(ranges, unsigned(f.sum.tiles)), kFewThreads, shared, st>>>(f);
     return int(cudaGetLastError());
 }
@@ -760,7 +764,7 @@ int launch_grad(const qsr_embed_args &a, bool vec, cudaStream_t st)
     p.width = int32_t(a.width); p.table_type = a.table_type; p.accumulate = a.accumulate;
     p.scale = float(a.scale);
     const int granules = int((a.width + 7) / 8);
-    if (is_few(a.rows, a.vocab)) {
+    if (is_few(a.rows, a.vocab, a.width)) {
         if (a.rows == 0 && a.accumulate) return 0;
         p.lanes = std::min(kFewLanes, power_of_two(granules));
         p.tiles = (granules + p.lanes - 1) / p.lanes;

@@ -221,9 +221,10 @@ def test_captured_and_replayed_with_other_tokens():
 @pytest.mark.parametrize("kind,out", [("f32", "bf16"), ("bf16", "f16"), ("f16", "f32")])
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("R,V,N", [(1, 2048, 3), (15, 3, 9), (16, 2049, 9), (17, 40, 64), (32, 1, 65), (33, 70000, 8), (257, 5000, 200), (4095, 6, 70), (4096, 300, 130), (4097, 300, 130),
-                                   (4096, 1 << 21, 2), (600, (1 << 21) + 1, 2)])
+                                   (4096, 1 << 21, 2), (600, (1 << 21) + 1, 2), (8192, 5000, 128), (8193, 5000, 128),
+                                   (8192, 3, 129), (16384, 30011, 64), (16383, 9, 33), (16385, 700, 64)])
 def test_gradient_of_few_rows(R, V, N, kind, out, accumulate):
-    """One launch for up to 4096 rows and 2^21 tokens; the others sort."""
+    """One launch for up to 4096 rows, or 16384 parts of 64 columns, and 2^21 tokens; the others sort."""
     d = torch.randn(R, N, device=DEV, generator=gen(R)).to(T[out])
     for how in ("zipf", "uniform", "same", "absent", "outside"):
         check_grad(d, draw(R, V, R + V, how), V, 0.75, kind, accumulate)
