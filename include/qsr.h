@@ -560,7 +560,8 @@ typedef struct qsr_layer_norm_args {
 } qsr_layer_norm_args;
 
 /* Forward.  No context; one launch on cuda_stream (none for rows = 0) of the current device, where all arrays lie;
- * asynchronous. */
+ * asynchronous.  (Here and backwards a wait for a copy inside the kernel has a limit of some seconds; rows after one that ran out
+ * are NaN.) */
 int qsr_layer_norm(const qsr_layer_norm_args *args, void *cuda_stream);
 
 /* Bytes of workspace for d_weight and d_bias. */
