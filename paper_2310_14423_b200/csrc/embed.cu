@@ -400,17 +400,21 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 {
     __shared__ float shared[8][kJoinThreads];
     // The sorted keys are those of the launch before the one before, which had ended before that one let this one start: what there is
-    // to join is found out while the sums are still being taken.
+    // to join is found out while the sums are still being taken.  They are read from the second-level cache, where that launch left them.
+    // Blocks without anything to join wait too: a launch none of whose blocks waits may end before the sums are written, and whatever is
+    // ordered behind this launch alone (the next node of a graph, say) would not find them.
     const int64_t c = int64_t(blockIdx.x), begin = c * p.chunk, end = begin + p.chunk;
-    if (end >= p.n) return;
-    const uint32_t token = p.keys[end - 1], behind = p.keys[end], at_begin = p.keys[begin], before = begin > 0 ? p.keys[begin - 1] : uint32_t(p.vocab);
-    if (token == uint32_t(p.vocab) || behind != token || (at_begin == token && before == token)) return;
+    const uint32_t none = uint32_t(p.vocab), token = end < p.n ? __ldcg(p.keys + end - 1) : none;
+    if (token == none || __ldcg(p.keys + end) != token || (begin > 0 && __ldcg(p.keys + begin) == token && __ldcg(p.keys + begin - 1) == token)) {
+        wait_for_launch_before();
+        return;
+    }
     const int lanes = p.join_lanes, ways = kJoinThreads / lanes, lane = int(threadIdx.x) & (lanes - 1), way = int(threadIdx.x) / lanes;
     const int first = int(blockIdx.y) * lanes * 8, width = p.width - first, col = column<VEC>(lane, lanes, 0, 0);
     int64_t lo = c;                              // the last chunk that begins with this token; they follow one another
     for (int same = 32; same == 32; lo += same) {
         const int64_t k = lo + 1 + (threadIdx.x & 31);
-        same = __popc(__ballot_sync(0xffffffffu, k < p.chunks && p.keys[k * p.chunk] == token));
+        same = __popc(__ballot_sync(0xffffffffu, k < p.chunks && __ldcg(p.keys + k * p.chunk) == token));
     }
     wait_for_launch_before();
     float s[8];

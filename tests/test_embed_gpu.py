@@ -228,3 +228,33 @@ def test_gradient_of_few_rows(R, V, N, kind, out, accumulate):
     d = torch.randn(R, N, device=DEV, generator=gen(R)).to(T[out])
     for how in ("zipf", "uniform", "same", "absent", "outside"):
         check_grad(d, draw(R, V, R + V, how), V, 0.75, kind, accumulate)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("R,V,N", [(20000, 30011, 64), (20000, 20000, 513), (70000, 70001, 24), (5000, (1 << 21) + 9, 8)])
+def test_sorted_gradient_in_a_graph_before_a_copy(R, V, N, accumulate):
+    """Rows that are sorted, none of whose tokens has rows in two chunks, so that nothing is joined: what follows the gradient in a graph finds it
+    complete.  All tokens different (positions, say): every sum is one product; padding alone: nothing is added."""
+    d = torch.randn(R, N, device=DEV, generator=gen(R)).bfloat16()
+    start = torch.randn(V, N, device=DEV, generator=gen(V)) if accumulate else None
+    for t in (torch.randperm(V, device=DEV, generator=gen(1))[:R], torch.full((R,), -1, device=DEV)):
+        g, copy = torch.zeros(V, N, device=DEV), torch.empty(V, N, device=DEV)
+        ws = torch.empty(B.qsr_embed_workspace_bytes(R, V, N), dtype=torch.uint8, device=DEV)
+        B.qsr_embed_grad(d, t, g, scale=0.5, accumulate=accumulate, workspace=ws, stream=stream())
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            if accumulate:
+                g.copy_(start)
+            else:
+                g.fill_(3.0)
+            B.qsr_embed_grad(d, t, g, scale=0.5, accumulate=accumulate, workspace=ws, stream=stream())
+            copy.copy_(g)
+        for _ in range(20):
+            d.mul_(-1.0).add_(0.25)
+            want = start.clone() if accumulate else torch.zeros(V, N, device=DEV)
+            some = t >= 0
+            want[t[some]] += 0.5 * d[some].float()
+            graph.replay()
+            assert torch.equal(copy, want) and torch.equal(g, want)
