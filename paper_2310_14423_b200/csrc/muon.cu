@@ -744,8 +744,8 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
     }
     __syncwarp();
     fence_before();
-    if (threadIdx.x == 0 && sh.stop) *p.late = 1u;
     pair_sync();                         // the other block's products read this one's shared memory and write its tensor memory
+    if (threadIdx.x == 0 && *stop) *p.late = 1u;          // behind the barrier: any warp may have been the last to give up
     if (warp == 2) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(accumulators), "r"(kAccumulators) : "memory");
