@@ -560,8 +560,8 @@ typedef struct qsr_layer_norm_args {
 } qsr_layer_norm_args;
 
 /* Forward.  No context; one launch on cuda_stream (none for rows = 0) of the current device, where all arrays lie;
- * asynchronous.  (Here and backwards a wait for a copy inside the kernel has a limit of some seconds; rows after one that ran out
- * are NaN.) */
+ * asynchronous.  (Here and backwards a wait for a copy inside the kernel has a limit of some seconds; rows from one that ran out
+ * on are NaN, and so are the sums over rows of the columns of the thread that waited.) */
 int qsr_layer_norm(const qsr_layer_norm_args *args, void *cuda_stream);
 
 /* Bytes of workspace for d_weight and d_bias. */
@@ -624,6 +624,11 @@ int qsr_debug_box_muller(const uint32_t *words_dev, int64_t n, float *radius_dev
  * sqrt_dev[i] = sqrt.approx.ftz(x_dev[i]), rcp_dev[i] = rcp.approx.ftz(x_dev[i]) for n floats (device arrays, 4-byte
  * aligned).  For tests that bound their error against binary64.  No context; one launch on cuda_stream; asynchronous. */
 int qsr_debug_fast_math(const float *x_dev, int64_t n, float *sqrt_dev, float *rcp_dev, void *cuda_stream);
+
+/* The limit of the waits for copies in layer norm's kernels, in clocks of a multiprocessor, for the calls from now on (all devices and
+ * threads of the process): 0 has every such wait run out at once, a negative number brings the library's own limit back.  For tests of
+ * what a call leaves where a wait ran out.  Copies under way are waited for in any case, with the library's own limit. */
+int qsr_debug_copy_patience(int64_t clocks);
 
 /* Text for a qsr_status. Never NULL. */
 const char *qsr_strerror(int status);

@@ -35,7 +35,8 @@ EXPORTS = ("qsr_config_check", "qsr_row_stride_hint", "qsr_config_learning_rate"
            "qsr_set_launch_shape", "qsr_set_graph_replay", "qsr_set_resident_steps", "qsr_train_host", "qsr_list_workspace_bytes", "qsr_list_create", "qsr_list_destroy", "qsr_list_set_grads",
            "qsr_list_step", "qsr_list_sync", "qsr_list_launch_count", "qsr_token_logprobs", "qsr_token_logprobs_grad", "qsr_muon_workspace_bytes",
            "qsr_muon_create", "qsr_muon_destroy", "qsr_muon_set_grads", "qsr_muon_step", "qsr_muon_sync", "qsr_muon_check", "qsr_muon_launch_count", "qsr_layer_norm",
-           "qsr_layer_norm_workspace_bytes", "qsr_layer_norm_grad", "qsr_embed", "qsr_embed_workspace_bytes", "qsr_embed_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_strerror")
+           "qsr_layer_norm_workspace_bytes", "qsr_layer_norm_grad", "qsr_embed", "qsr_embed_workspace_bytes", "qsr_embed_grad", "qsr_debug_box_muller", "qsr_debug_fast_math", "qsr_debug_copy_patience",
+           "qsr_strerror")
 
 
 class QsrConfig(C.Structure):
@@ -175,6 +176,7 @@ def lib():
             "qsr_embed_grad": (C.c_int, [C.POINTER(QsrEmbedArgs), vp]),
             "qsr_debug_box_muller": (C.c_int, [vp, i64, vp, vp, vp, vp]),
             "qsr_debug_fast_math": (C.c_int, [vp, i64, vp, vp, vp]),
+            "qsr_debug_copy_patience": (C.c_int, [i64]),
             "qsr_strerror": (C.c_char_p, [C.c_int]),
         }
         for name in EXPORTS:
@@ -833,3 +835,8 @@ def qsr_debug_fast_math(x, root, reciprocal, stream: int = 0) -> None:
     """Test hook: the library's single-instruction square root and reciprocal of each float of x (CUDA tensors)."""
     _check(lib().qsr_debug_fast_math(_dptr(x), int(x.numel()), _dptr(root), _dptr(reciprocal), C.c_void_p(stream)),
            "qsr_debug_fast_math")
+
+
+def qsr_debug_copy_patience(clocks: int = -1) -> None:
+    """Test hook: limit of the waits for copies in layer norm's kernels from now on; 0: they run out at once, negative: the usual one."""
+    _check(lib().qsr_debug_copy_patience(int(clocks)), "qsr_debug_copy_patience")

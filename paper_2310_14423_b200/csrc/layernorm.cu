@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "checks.h"
@@ -27,6 +28,7 @@ struct Params {
     int32_t wvec;                     // weight and bias aligned to eight elements
     int32_t want_weight, want_bias;
     float eps, inverse;            // inverse: one over the width
+    long long patience;               // clocks that a wait for a row's copy may take
 };
 
 // Weights and biases: read by every row, so through the cache.
@@ -490,6 +492,7 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const __grid_constant
 // by what a row costs its block in instructions and exchanges, beside the copies: 3.6 to 4.9 TB/s.
 constexpr int kMaxStages = 8;
 constexpr long long kPatience = 6000000000;       // clocks that a wait may take, some seconds
+std::atomic<long long> g_patience{kPatience};     // of the launches to come; other than that only by the test hook
 
 __device__ __forceinline__ bool copied(uint32_t bar, unsigned parity)
 {
@@ -497,10 +500,12 @@ __device__ __forceinline__ bool copied(uint32_t bar, unsigned parity)
     asm volatile("{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ bool wait_for_copy(uint32_t bar, unsigned parity)
+// A limit of zero has run out at once, whether the copy is there or not.
+__device__ __forceinline__ bool wait_for_copy(uint32_t bar, unsigned parity, long long patience)
 {
+    if (patience <= 0) return false;
     if (copied(bar, parity)) return true;
-    for (const long long begin = clock64(); clock64() - begin < kPatience;)
+    for (const long long begin = clock64(); clock64() - begin < patience;)
         for (int i = 0; i < 64; ++i)
             if (copied(bar, parity)) return true;
     return false;
@@ -585,7 +590,7 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
         for (int r = 0; r < ROWS; ++r) {
             Raw8 x, dy;
             if (r < live) {
-                all_came = all_came && wait_for_copy(bars + at * 8, parity);
+                all_came = all_came && wait_for_copy(bars + at * 8, parity, p.patience);
                 const uint32_t from = slots + at * 2 * slot + lane * 8 * BYTES;
                 const unsigned here = row + r * step;
                 if (!FULL && left < 8 && here + 1 == rows) {
@@ -601,7 +606,9 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
                 for (int j = 0; j < 8; ++j) x.w[j] = dy.w[j] = 0u;
             widen_pairs(a[r], x, TYPE);
             widen_pairs(d[r], dy, TYPE);
-            if (!all_came) d[r].v[0].x = quiet_nan();            // a wait ran out: no number passes for a gradient
+            if (!all_came)                                       // a wait ran out: no number passes for a gradient, the columns' sums included
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[r].v[j] = make_float2(quiet_nan(), quiet_nan());
             add_columns<true, FULL>(a[r], d[r], c, s[2 * r], s[2 * r + 1], mean[r], rstd[r], lane, lanes, p.width);
         }
         if (p.dx) group_sums(s, sums[turn][0], lanes >> 5, 0, lanes, lane);
@@ -627,8 +634,8 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
             put_row<true, FULL>(to, out, lane, lanes, 0, p.width, TYPE);
         }
     }
-    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: no copy may outlive the block
-        wait_for_copy(bars + stage * 8, phase);
+    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: the copies under way are waited for, each with the limit once more
+        wait_for_copy(bars + stage * 8, phase, kPatience);
         if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
     if (p.partial) leave_columns<true>(p, c, nullptr, 1, 0, lane, lanes);
@@ -685,7 +692,7 @@ __global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_k
     unsigned phase = 0;
     bool all_came = true;
     for (int64_t row = blockIdx.x; row < p.rows; row += step) {
-        all_came = all_came && wait_for_copy(bars + stage * 8, phase);
+        all_came = all_came && wait_for_copy(bars + stage * 8, phase, p.patience);
         Pairs x[HELD];
         float2 s = make_float2(0.0f, 0.0f), q = s;
 #pragma unroll
@@ -740,8 +747,8 @@ __global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_k
             put_row<true, FULL>(to, y, lane, lanes, k, p.width, TYPE);
         }
     }
-    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: no copy may outlive the block
-        wait_for_copy(bars + stage * 8, phase);
+    for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: the copies under way are waited for, each with the limit once more
+        wait_for_copy(bars + stage * 8, phase, kPatience);
         if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
 }
@@ -989,6 +996,7 @@ Params params_of(const qsr_layer_norm_args &a)
     p.rows = a.rows; p.width = int32_t(a.width);
     p.granules = int32_t((a.width + 7) / 8);
     p.inverse = 1.0f / float(a.width);
+    p.patience = g_patience.load(std::memory_order_relaxed);
     return p;
 }
 
@@ -1073,6 +1081,12 @@ int qsr_layer_norm_grad(const qsr_layer_norm_args *a, void *cuda_stream)
     else if (a->type == QSR_BF16) err = vec ? launch_backward<__nv_bfloat16, true>(p, a->d_weight, a->d_bias, st) : launch_backward<__nv_bfloat16, false>(p, a->d_weight, a->d_bias, st);
     else err = vec ? launch_backward<__half, true>(p, a->d_weight, a->d_bias, st) : launch_backward<__half, false>(p, a->d_weight, a->d_bias, st);
     return launch_status(err);
+}
+
+int qsr_debug_copy_patience(int64_t clocks)
+{
+    qsr::g_patience.store(clocks < 0 ? qsr::kPatience : clocks, std::memory_order_relaxed);
+    return QSR_OK;
 }
 
 }  // extern "C"
