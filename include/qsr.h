@@ -533,7 +533,8 @@ int64_t qsr_muon_launch_count(const qsr_muon *muon);
 /*
  * The normalisation between a model's products.  For each row x[0..width), everything in fp32:
  *   mean = sum x / width;  rstd = 1 / sqrt(sum (x - mean)^2 / width + eps);  hat = (x - mean)*rstd;  y = hat*weight + bias,
- * y rounded once to the rows' type.  Backwards, with g = d_y*weight:
+ * y rounded once to the rows' type.  (Of rows far from zero the mean is taken off in two parts, so that its rounding, which grows with
+ * the mean, does not show in y.)  Backwards, with g = d_y*weight:
  *   d_x = rstd*(g - (sum g)/width - hat*(sum g*hat)/width);  d_weight = sum over rows of d_y*hat;  d_bias = sum over rows of d_y.
  * Sums over rows are added in a fixed order, so that results repeat bit for bit.  Infinities and NaN stay in their row, and
  * in the columns' sums.

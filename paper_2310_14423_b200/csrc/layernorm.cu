@@ -97,8 +97,42 @@ __device__ __forceinline__ float inverse_root(float x)
 // FULL kernels compare nothing with the width.  Forward: every thread has all its elements, the row is lanes * HELD whole granules.
 // Backward: the row is whole granules, and a thread has one or none.
 
+// A mean is off by some 2^-24 of the row's values, and with it every x - mean by the same, which the division by the spread makes large
+// where the row is far from zero: 0.03 to 0.09 for rows of one value near 1000.  Rows whose mean is further from zero than so many
+// standard deviations have the mean of what is left taken off too, and the variance taken anew.  For the others the error is within a few
+// roundings: of fp32 from four on (some 2^-20), of fp16, whose roundings are 2^-11, from 64 on (2^-16).
+template <typename T>
+__device__ __forceinline__ bool far_from_zero(float mean, float rstd) { return fabsf(mean) * rstd > (sizeof(T) == 4 ? 4.0f : 64.0f); }
+
+// That for rows in registers; x: what is left.  All lanes of a warp come here together, with rows of their own.
+template <typename T, int HELD, bool VEC, bool FULL>
+__device__ __forceinline__ void settle_row(float (&x)[HELD][8], float &mean, float &rstd, const Params &p, int lane, int lanes, float *scratch)
+{
+    const bool far = far_from_zero<T>(mean, rstd);
+    if (!__any_sync(0xffffffffu, far)) return;                   // of rows that a block shares, the same for the block
+    float s = 0.0f, q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (FULL || column<VEC>(lane, lanes, k, j) < p.width) s += x[k][j];
+    const float left = row_sum(s, lanes, scratch) * p.inverse, rest = far ? left : 0.0f;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[k][j] -= rest;
+            if (FULL || column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[k][j], x[k][j], q);
+        }
+    const float anew = inverse_root(fmaf(row_sum(q, lanes, scratch), p.inverse, p.eps));
+    if (far) {
+        mean += rest;
+        rstd = anew;
+    }
+}
+
 // Rows that fit in registers: HELD granules a thread, `lanes` threads a row (a power of two up to 32, or the whole block).  Mean and
-// variance take two passes over the registers, so that rows far from zero lose nothing.
+// variance take two passes over the registers, and rows far from zero two more.
 template <typename T, int HELD, bool VEC, bool FULL>
 __global__ void __launch_bounds__(kMaxThreads) forward_kernel(const __grid_constant__ Params p, int lanes)
 {
@@ -121,7 +155,7 @@ __global__ void __launch_bounds__(kMaxThreads) forward_kernel(const __grid_const
             for (int j = 0; j < 8; ++j) s += x[k][j];
         }
     }
-    const float mean = row_sum(s, lanes, scratch) * p.inverse;
+    float mean = row_sum(s, lanes, scratch) * p.inverse;
     float q = 0.0f;
 #pragma unroll
     for (int k = 0; k < HELD; ++k)
@@ -130,7 +164,8 @@ __global__ void __launch_bounds__(kMaxThreads) forward_kernel(const __grid_const
             x[k][j] -= mean;
             if (FULL || column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[k][j], x[k][j], q);
         }
-    const float rstd = inverse_root(fmaf(row_sum(q, lanes, scratch), p.inverse, p.eps));
+    float rstd = inverse_root(fmaf(row_sum(q, lanes, scratch), p.inverse, p.eps));
+    settle_row<T, HELD, VEC, FULL>(x, mean, rstd, p, lane, lanes, scratch);
     if (!live) return;
     if (lane == 0) {
         if (p.mean) p.mean[row] = mean;
@@ -183,7 +218,7 @@ __global__ void __launch_bounds__(256, 4) forward_rows_kernel(const __grid_const
             for (int j = 0; j < 8; ++j) s += x[k][j];
         }
         load(row + step);
-        const float mean = row_sum(s, lanes, nullptr) * p.inverse;
+        float mean = row_sum(s, lanes, nullptr) * p.inverse;
 #pragma unroll
         for (int k = 0; k < HELD; ++k)
 #pragma unroll
@@ -191,7 +226,8 @@ __global__ void __launch_bounds__(256, 4) forward_rows_kernel(const __grid_const
                 x[k][j] -= mean;
                 if (FULL || column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[k][j], x[k][j], q);
             }
-        const float rstd = inverse_root(fmaf(row_sum(q, lanes, nullptr), p.inverse, p.eps));
+        float rstd = inverse_root(fmaf(row_sum(q, lanes, nullptr), p.inverse, p.eps));
+        settle_row<T, HELD, VEC, FULL>(x, mean, rstd, p, lane, lanes, nullptr);
         if (row >= p.rows) continue;
         if (lane == 0) {
             if (p.mean) p.mean[row] = mean;
@@ -224,7 +260,7 @@ __global__ void __launch_bounds__(256, 4) forward_rows_kernel(const __grid_const
     }
 }
 
-// Rows of any length, read three times (from the caches after the first); one block a row.
+// Rows of any length, read three times (from the caches after the first), five times if they are far from zero; one block a row.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMaxThreads) forward_long_kernel(const __grid_constant__ Params p)
 {
@@ -240,17 +276,34 @@ __global__ void __launch_bounds__(kMaxThreads) forward_long_kernel(const __grid_
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += x[j];
     }
-    const float mean = row_sum(s, lanes, scratch) * p.inverse;
-    for (int k = 0; k < steps; ++k) {
-        fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
-        widen8(x, r, TYPE);
+    const float mean = __fmul_rn(row_sum(s, lanes, scratch), p.inverse);          // one number in all that follows, not part of an fma
+    float rest = 0.0f, rstd;                                     // rest: the mean of what is left
+    const auto spread = [&] {
+        q = 0.0f;
+        for (int k = 0; k < steps; ++k) {
+            fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
+            widen8(x, r, TYPE);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[j] - mean, x[j] - mean, q);
+            for (int j = 0; j < 8; ++j)
+                if (column<VEC>(lane, lanes, k, j) < p.width) q = fmaf(x[j] - mean - rest, x[j] - mean - rest, q);
+        }
+        rstd = inverse_root(fmaf(row_sum(q, lanes, scratch), p.inverse, p.eps));
+    };
+    spread();
+    if (far_from_zero<T>(mean, rstd)) {                             // the same for the block
+        s = 0.0f;
+        for (int k = 0; k < steps; ++k) {
+            fetch<VEC>(r, from, lane, lanes, k, p.width, TYPE);
+            widen8(x, r, TYPE);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (column<VEC>(lane, lanes, k, j) < p.width) s += x[j] - mean;
+        }
+        rest = __fmul_rn(row_sum(s, lanes, scratch), p.inverse);
+        spread();
     }
-    const float rstd = inverse_root(fmaf(row_sum(q, lanes, scratch), p.inverse, p.eps));
     if (lane == 0) {
-        if (p.mean) p.mean[blockIdx.x] = mean;
+        if (p.mean) p.mean[blockIdx.x] = mean + rest;
         if (p.rstd) p.rstd[blockIdx.x] = rstd;
     }
     void *to = row_of<T>(p.y, blockIdx.x, p.y_stride);
@@ -261,7 +314,7 @@ __global__ void __launch_bounds__(kMaxThreads) forward_long_kernel(const __grid_
         weights<VEC>(w, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
         weights<VEC>(b, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = fmaf((x[j] - mean) * rstd, w[j], b[j]);
+        for (int j = 0; j < 8; ++j) w[j] = fmaf((x[j] - mean - rest) * rstd, w[j], b[j]);
         put<VEC>(to, w, lane, lanes, k, p.width, TYPE);
     }
 }
@@ -646,18 +699,25 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
 // 37 with the first kernel above, 8192 x 5120 39 instead of 56, 4096 x 5120 fp32 31 instead of 35 (5.4 TB/s); eight columns a thread, two rows at a
 // time: 37.  Bound by instructions (widening, exchanges, the loop) beside the copies.  (Backward, sixteen columns a thread leave
 // too few warps: 64 us for 4099 x 5003 fp32 instead of 60, 73 for 8192 x 4096 bf16 instead of 56.)
+//
+// Rows far from zero are noted and come after up to 256 rows of the block, read once more: the registers for them here, where there is none to
+// spare, would cost all rows (8192 x 5120 bf16 49 us instead of 40).  Nothing of such a row has been written, so that y may be x.  Where
+// all rows are far, 8192 x 4096 bf16 takes 88 us.
+constexpr int kFarRows = 256;
 template <typename T, bool FULL, int THREADS>
 __global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_kernel(const __grid_constant__ Params p, int stages)
 {
     extern __shared__ __align__(128) char ring[];                // [stages] rows
     __shared__ __align__(8) unsigned long long full[kMaxStages];
     __shared__ float sums[2][THREADS / 32];                      // used in turn
+    __shared__ unsigned far_rows[kFarRows], n_far;
+    __shared__ float far_means[kFarRows];
     constexpr int TYPE = Kind<T>::type, BYTES = int(sizeof(T)), HELD = 2;
     const int lanes = int(blockDim.x), lane = int(threadIdx.x), warps = lanes >> 5, slot = HELD * lanes * 8 * BYTES;
     const uint32_t bars = uint32_t(__cvta_generic_to_shared(full)), slots = uint32_t(__cvta_generic_to_shared(ring));
-    const int64_t step = gridDim.x;
-    const auto issue = [&](int stage, int64_t row) {             // of the last row, whole 16 bytes, as above
-        const unsigned n = unsigned(row + 1 < p.rows ? (p.width * BYTES + 15) & ~15 : p.width * BYTES & ~15);
+    const unsigned rows = unsigned(p.rows), step = gridDim.x;    // below 2^31
+    const auto issue = [&](int stage, unsigned row) {             // of the last row, whole 16 bytes, as above
+        const unsigned n = unsigned(row + 1 < rows ? (p.width * BYTES + 15) & ~15 : p.width * BYTES & ~15);
         const uint32_t bar = bars + stage * 8;
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(slots + stage * slot),
@@ -667,18 +727,7 @@ __global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_k
     if (lane == 0) {
         for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + i * 8) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
-        for (; under_way < stages && blockIdx.x + under_way * step < p.rows; ++under_way) issue(under_way, blockIdx.x + under_way * step);
-    }
-    Pairs w[HELD], b[HELD];
-#pragma unroll
-    for (int k = 0; k < HELD; ++k) {
-        float v[8];
-        weights<true>(v, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
-        weights<true>(v, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
+        for (; under_way < stages && blockIdx.x + under_way * step < rows; ++under_way) issue(under_way, blockIdx.x + under_way * step);
     }
     const auto left = [&](int k) { return p.width - (lane + k * lanes) * 8; };
     const auto block_sum = [&](float2 v, float *at) {
@@ -687,65 +736,129 @@ __global__ void __launch_bounds__(THREADS, kMaxThreads / THREADS) forward_ring_k
         __syncthreads();
         return warp_sum((lane & 31) < warps ? at[lane & 31] : 0.0f);
     };
+    if (lane == 0) n_far = 0;
     __syncthreads();
     int stage = 0;
     unsigned phase = 0;
     bool all_came = true;
-    for (int64_t row = blockIdx.x; row < p.rows; row += step) {
-        all_came = all_came && wait_for_copy(bars + stage * 8, phase, p.patience);
-        Pairs x[HELD];
-        float2 s = make_float2(0.0f, 0.0f), q = s;
+    for (unsigned row = blockIdx.x; row < rows;) {
+        const unsigned end = min(rows, row + kFarRows * step);
+        Pairs w[HELD], b[HELD];
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
-            Raw8 raw;
-            if (!FULL && left(k) < 8 && row + 1 == p.rows) fetch<true>(raw, row_of<T>(p.x, row, p.x_stride), lane, lanes, k, p.width, TYPE);
-            else take_shared<T, FULL>(raw, slots + stage * slot + (lane + k * lanes) * 8 * BYTES, left(k));
-            widen_pairs(x[k], raw, TYPE);
-            if (!all_came) x[k].v[0].x = quiet_nan();            // a wait ran out: no number passes for a result
+            float v[8];
+            weights<true>(v, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s = add2(s, x[k].v[j]);
+            for (int j = 0; j < 4; ++j) w[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
+            weights<true>(v, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[k].v[j] = make_float2(v[2 * j], v[2 * j + 1]);
         }
-        const float mean = block_sum(s, sums[0]) * p.inverse;
-        if (all_came) {                                          // and all threads have taken this row
-            under_way--;
-            if (lane == 0 && row + stages * step < p.rows) {
-                issue(stage, row + stages * step);
-                under_way++;
+        for (; row < end; row += step) {
+            all_came = all_came && wait_for_copy(bars + stage * 8, phase, p.patience);
+            Pairs x[HELD];
+            float2 s = make_float2(0.0f, 0.0f), q = s;
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                Raw8 raw;
+                if (!FULL && left(k) < 8 && row + 1 == rows) fetch<true>(raw, row_of<T>(p.x, row, p.x_stride), lane, lanes, k, p.width, TYPE);
+                else take_shared<T, FULL>(raw, slots + stage * slot + (lane + k * lanes) * 8 * BYTES, left(k));
+                widen_pairs(x[k], raw, TYPE);
+                if (!all_came) x[k].v[0].x = quiet_nan();        // a wait ran out: no number passes for a result
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s = add2(s, x[k].v[j]);
             }
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-#pragma unroll
-        for (int k = 0; k < HELD; ++k) {
-            const float2 minus = FULL && left(k) <= 0 ? make_float2(0.0f, 0.0f) : make_float2(-mean, -mean);      // nothing beyond the row
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[k].v[j] = add2(x[k].v[j], minus);
-                if (!FULL) {
-                    if (2 * j >= left(k)) x[k].v[j].x = 0.0f;
-                    if (2 * j + 1 >= left(k)) x[k].v[j].y = 0.0f;
+            const float mean = block_sum(s, sums[0]) * p.inverse;
+            if (all_came) {                                      // and all threads have taken this row
+                under_way--;
+                if (lane == 0 && row + stages * step < rows) {
+                    issue(stage, row + stages * step);
+                    under_way++;
                 }
-                q = fma2(x[k].v[j], x[k].v[j], q);
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+            }
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                if (FULL && left(k) <= 0) break;                 // nothing beyond the row
+                const float2 minus = make_float2(-mean, -mean);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[k].v[j] = add2(x[k].v[j], minus);
+                    if (!FULL) {
+                        if (2 * j >= left(k)) x[k].v[j].x = 0.0f;
+                        if (2 * j + 1 >= left(k)) x[k].v[j].y = 0.0f;
+                    }
+                    q = fma2(x[k].v[j], x[k].v[j], q);
+                }
+            }
+            const float rstd = inverse_root(fmaf(block_sum(q, sums[1]), p.inverse, p.eps));
+            const bool far = far_from_zero<T>(mean, rstd);       // the same for the block
+            if (lane == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+                if (far) {
+                    far_rows[n_far] = row;
+                    far_means[n_far++] = mean;
+                }
+            }
+            void *to = row_of<T>(p.y, row, p.y_stride);
+            const float2 times = make_float2(rstd, rstd);
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                if (left(k) <= 0 || far) break;
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 v = fma2(mul2(x[k].v[j], times), w[k].v[j], b[k].v[j]);
+                    y[2 * j] = v.x;
+                    y[2 * j + 1] = v.y;
+                }
+                put_row<true, FULL>(to, y, lane, lanes, k, p.width, TYPE);
             }
         }
-        const float rstd = inverse_root(fmaf(block_sum(q, sums[1]), p.inverse, p.eps));
-        if (lane == 0) {
-            if (p.mean) p.mean[row] = mean;
-            if (p.rstd) p.rstd[row] = rstd;
-        }
-        void *to = row_of<T>(p.y, row, p.y_stride);
-        const float2 times = make_float2(rstd, rstd);
+        __syncthreads();                                         // what is noted is there, and all y before it is written
+        const unsigned n = n_far;
+#pragma unroll 1
+        for (unsigned i = 0; i < n; ++i) {
+            const unsigned row = far_rows[i];
+            const float mean = far_means[i];
+            float x[8], s = 0.0f, q = 0.0f;
+            const auto take = [&](int k) {
+                Raw8 raw;
+                fetch<true>(raw, row_of<T>(p.x, row, p.x_stride), lane, lanes, k, p.width, TYPE);
+                widen8(x, raw, TYPE);
+            };
+            const auto sum = [&](const auto &add) {
+#pragma unroll 1
+                for (int k = 0; k < HELD; ++k) {
+                    take(k);
 #pragma unroll
-        for (int k = 0; k < HELD; ++k) {
-            if (left(k) <= 0) break;
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 v = fma2(mul2(x[k].v[j], times), w[k].v[j], b[k].v[j]);
-                y[2 * j] = v.x;
-                y[2 * j + 1] = v.y;
+                    for (int j = 0; j < 8; ++j)
+                        if (j < left(k)) add(x[j]);
+                }
+            };
+            sum([&](float v) { s += v - mean; });
+            const float rest = __fmul_rn(block_sum(make_float2(s, 0.0f), sums[0]), p.inverse);        // one number in all that follows, not part of an fma
+            sum([&](float v) { q = fmaf(v - mean - rest, v - mean - rest, q); });
+            const float rstd = inverse_root(fmaf(block_sum(make_float2(q, 0.0f), sums[1]), p.inverse, p.eps));
+            if (lane == 0) {
+                if (p.mean) p.mean[row] = mean + rest;
+                if (p.rstd) p.rstd[row] = rstd;
             }
-            put_row<true, FULL>(to, y, lane, lanes, k, p.width, TYPE);
+            void *to = row_of<T>(p.y, row, p.y_stride);
+#pragma unroll 1
+            for (int k = 0; k < HELD; ++k) {
+                if (left(k) <= 0) break;
+                float wk[8], bk[8];
+                take(k);
+                weights<true>(wk, p.w, 1.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+                weights<true>(bk, p.b, 0.0f, lane, lanes, k, p.width, p.wtype, p.wvec != 0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = fmaf((x[j] - mean - rest) * rstd, wk[j], bk[j]);
+                put<true>(to, x, lane, lanes, k, p.width, TYPE);
+            }
         }
+        if (lane == 0) n_far = 0;
     }
     for (; lane == 0 && under_way > 0; --under_way) {            // a wait ran out: the copies under way are waited for, each with the limit once more
         wait_for_copy(bars + stage * 8, phase, kPatience);
