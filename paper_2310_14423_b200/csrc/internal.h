@@ -225,7 +225,7 @@ struct MuonParams {
     const MuonChunk *chunks;
     const MuonBlock *blocks;
     double *partial;          // [chunks]: sums of squares
-    float *factor;            // [matrices]: scale / (norm + eps)
+    float *factor;            // [matrices, 2]: scale / (norm + eps), in two factors
     unsigned *arrived;        // [matrices], zero between launches
     unsigned *late;           // set where a wait ran out
     uint16_t *data;     // all matrices' blocks

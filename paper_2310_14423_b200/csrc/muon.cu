@@ -35,11 +35,16 @@ __device__ __forceinline__ float updated(const MuonParams &p, float m, float g) 
 // What is orthogonalised, from the new momentum.
 __device__ __forceinline__ float direction(const MuonParams &p, float m, float g) { return p.nesterov ? fmaf(p.beta, m - g, g) : m; }
 
-// scale / (norm + eps); nothing to scale where that is 0.
-__device__ __forceinline__ float scale_factor(float scale, double squares, float eps)
+// scale / (norm + eps), whose product with the largest element is at most `scale`; nothing to scale where the norm is 0.  As two factors that
+// are taken one after the other, the first a power of two: the norm of numbers that fp32 holds lies between 2^-149 and 2^146, and for
+// the far ends the quotient, or its full precision, is beyond fp32.
+struct Scaling { float lift, factor; };
+__device__ __forceinline__ Scaling scaling_of(float scale, double squares, float eps)
 {
     const double length = sqrt(squares) + double(eps);
-    return length == 0.0 ? 0.0f : float(isnan(length) ? length : fmin(double(scale) / length, 3.0e38));
+    if (length == 0.0) return {1.0f, 0.0f};
+    const float lift = length < 0x1p-60 ? 0x1p80f : length > 0x1p60 ? 0x1p-64f : 1.0f;
+    return {lift, float(double(scale) / (length * double(lift)))};                          // NaN stays NaN, infinity gives 0
 }
 
 // m <- m + (1 - beta)(g - m) and the sum of squares of u, chunk by chunk; the matrix's last chunk adds them in their order.
@@ -120,7 +125,9 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
     if (threadIdx.x == 0) {
         s = scratch[0];
         for (int w = 1; w < kMomentumThreads / 32; ++w) s += scratch[w];
-        p.factor[c.matrix] = scale_factor(t.scale, s, p.eps);
+        const Scaling z = scaling_of(t.scale, s, p.eps);
+        p.factor[2 * c.matrix] = z.lift;
+        p.factor[2 * c.matrix + 1] = z.factor;
         p.arrived[c.matrix] = 0;
     }
 }
@@ -192,7 +199,7 @@ __device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix
     const int64_t lo = int64_t(t.rb) * t.cb * kBlockElements;
     const int grad_type = t.grad_type;
     const float *momentum = t.momentum;
-    const float factor = p.factor[b.matrix];
+    const float lift = p.factor[2 * b.matrix], factor = p.factor[2 * b.matrix + 1];
     Half o[2];
     Raw8 g[2], m[2];
 #pragma unroll
@@ -208,7 +215,7 @@ __device__ __forceinline__ void pack_block(const MuonParams &p, const MuonMatrix
         widen<WIDE>(x, m[h], QSR_F32);
         Raw8 hi, rest;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = k < o[h].n ? direction(p, x[k], gs[k] * p.grad_scale) * factor : 0.0f;      // whatever the factor
+        for (int k = 0; k < 8; ++k) x[k] = k < o[h].n ? direction(p, x[k], gs[k] * p.grad_scale) * lift * factor : 0.0f;      // whatever the factor
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
             const __half2 f = __floats2half2_rn(x[k], x[k + 1]);
@@ -934,7 +941,7 @@ __device__ __forceinline__ void pack_eighth(const Resident<PRODUCTS> &z, int b, 
     }
 }
 template <bool WIDE, int PRODUCTS>
-__device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix &t, const void *grad, const Resident<PRODUCTS> &z, float factor, const Kept &kept)
+__device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix &t, const void *grad, const Resident<PRODUCTS> &z, Scaling by, const Kept &kept)
 {
     const int blocks = t.rb * t.cb, rb = t.rb, gt = t.grad_type;
     int row, col;
@@ -944,7 +951,7 @@ __device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix
         if (b >= blocks) break;
         float x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = kept.u[b][k] == 0.0f ? 0.0f : kept.u[b][k] * factor;        // padding stays zero, whatever the factor
+        for (int k = 0; k < 8; ++k) x[k] = kept.u[b][k] == 0.0f ? 0.0f : kept.u[b][k] * by.lift * by.factor;        // padding stays zero, whatever the factor
         pack_eighth<WIDE, PRODUCTS>(z, b, row, col, x);
     }
 #pragma unroll 2
@@ -957,7 +964,7 @@ __device__ __forceinline__ void small_pack(const MuonParams &p, const MuonMatrix
         widen<WIDE>(gs, g, gt);
         widen<WIDE>(x, m, QSR_F32);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = k < o.n ? direction(p, x[k], gs[k] * p.grad_scale) * factor : 0.0f;
+        for (int k = 0; k < 8; ++k) x[k] = k < o.n ? direction(p, x[k], gs[k] * p.grad_scale) * by.lift * by.factor : 0.0f;
         pack_eighth<WIDE, PRODUCTS>(z, b, row, col, x);
     }
 }
@@ -993,7 +1000,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
 {
     extern __shared__ char raw[];
     __shared__ double sums[kSmallThreads / 32];
-    __shared__ float factor;
+    __shared__ Scaling factor;
     __shared__ uint64_t done;
     __shared__ uint32_t tensor_memory;
     __shared__ unsigned stop_flag;
@@ -1025,7 +1032,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const __grid_co
     if (threadIdx.x == 0) {
         s = sums[0];
         for (int w = 1; w < kSmallThreads / 32; ++w) s += sums[w];
-        factor = scale_factor(t.scale, s, p.eps);
+        factor = scaling_of(t.scale, s, p.eps);
     }
     __syncthreads();
     if (wide) small_pack<true, PRODUCTS>(p, t, grad, z, factor, kept);

@@ -222,7 +222,7 @@ Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t wo
     l.sync_tensors = take(2 * int64_t(n) * int64_t(sizeof(ListTensor)));
     l.sync_chunks = take(l.n_sync * int64_t(sizeof(ListChunk)));
     l.partial = take(l.n_chunks * int64_t(sizeof(double)));
-    l.factor = take(int64_t(n) * int64_t(sizeof(float)));
+    l.factor = take(2 * int64_t(n) * int64_t(sizeof(float)));
     l.arrived = take(int64_t(n) * int64_t(sizeof(unsigned)));
     l.late = take(int64_t(sizeof(unsigned)));
     l.data = take(data);

@@ -441,3 +441,24 @@ def test_offsets_beyond_32_bits():
         got = -p[part * side:(part + 1) * side].double()
         assert float(torch.linalg.vector_norm(got - want)) <= err + 2.0 ** -8 * float(torch.linalg.vector_norm(want))
     assert torch.equal(m[-side:], y.float())
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape", [(64, 64), (60, 200), (300, 200), (500, 130), (1, 7)])
+def test_the_size_of_a_gradient_does_not_matter(shape, products):
+    """Without eps, a gradient times a power of two has the same update, bit for bit, as long as fp32 holds its elements: from 2^-140 (whole numbers
+    times that; the norm's reciprocal is beyond fp32) to 2^120."""
+    g0 = torch.randint(-8, 9, shape, device=DEV, generator=gen(7)).float()
+    g0.view(-1)[0] = 5.0
+    theta = torch.randn(shape, device=DEV, generator=gen(8))
+    results = []
+    for power in (0, -140, -127, -100, -62, 61, 100, 120):
+        p, m, g = theta.clone(), torch.zeros(shape, device=DEV), torch.ldexp(g0.double(), torch.tensor(power, device=DEV)).float()
+        ws = torch.empty(B.qsr_muon_workspace_bytes([shape], 1, products), dtype=torch.uint8, device=DEV)
+        x = B.MuonList([p], [g], [m], beta=0.0, nesterov=False, eps=0.0, products=products, workspace=ws, stream=stream())
+        x.qsr_muon_step(0.1)
+        x.qsr_muon_check()
+        assert torch.equal(m, g)
+        results.append(p)
+    assert not torch.equal(results[0], theta)
+    assert all(torch.equal(r, results[0]) for r in results)
