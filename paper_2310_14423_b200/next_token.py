@@ -20,6 +20,7 @@ import sys
 from typing import Dict, List
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 from . import workloads as W
@@ -61,23 +62,24 @@ def logits_of(weights: List[torch.Tensor], tokens: torch.Tensor) -> torch.Tensor
 
 
 class Embedding(torch.autograd.Function):
-    """Rows of a table.  The gradient is added to table.grad, which has to be there (zeroed at the beginning of a step): only the
-    rows of tokens that occur are touched."""
+    """Rows of a table."""
 
     @staticmethod
     def forward(ctx, table, tokens):
         out = torch.empty(tokens.numel(), table.shape[1], device=table.device, dtype=table.dtype)
-        B.qsr_embed(table.detach(), tokens, out, stream=torch.cuda.current_stream().cuda_stream)
-        ctx.table, ctx.tokens = table, tokens
+        B.qsr_embed(table, tokens, out, stream=torch.cuda.current_stream().cuda_stream)
+        ctx.save_for_backward(tokens)
+        ctx.shape = table.shape
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_out):
-        table, tokens = ctx.table, ctx.tokens
-        workspace = torch.empty(B.qsr_embed_workspace_bytes(tokens.numel(), *table.shape), dtype=torch.uint8, device=table.device)
-        B.qsr_embed_grad(d_out.contiguous(), tokens, table.grad, accumulate=True, workspace=workspace,
-                         stream=torch.cuda.current_stream().cuda_stream)
-        return None, None
+        tokens, = ctx.saved_tensors
+        d_table = torch.empty(ctx.shape, device=d_out.device, dtype=d_out.dtype)
+        workspace = torch.empty(B.qsr_embed_workspace_bytes(tokens.numel(), *ctx.shape), dtype=torch.uint8, device=d_out.device)
+        B.qsr_embed_grad(d_out.contiguous(), tokens, d_table, workspace=workspace, stream=torch.cuda.current_stream().cuda_stream)
+        return d_table, None
 
 
 class LayerNorm(torch.autograd.Function):
@@ -91,6 +93,7 @@ class LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_y):
         x, weight, mean, rstd = ctx.saved_tensors
         d_x, d_weight, d_bias = torch.empty_like(x), torch.empty_like(weight), torch.empty_like(weight)
