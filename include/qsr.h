@@ -457,11 +457,14 @@ int qsr_token_logprobs_grad(const qsr_logprob_args *args, void *cuda_stream);
  *   theta <- theta - (lr*weight_decay*wd_scale*theta + lr*update_scale*X),
  * theta rounded once to the parameter's type and once, from the same fp32 value, to the working copy's.  The polynomial
  * takes singular values above about 0.005 to [0.68, 1.21] in five iterations; it does not converge to one.  Where one side is at
- * least twice the other, the last three iterations are X <- (C3 C2 C1) X with A <- C A C in between: the same with fewer operations.
+ * least twice the other, the last two of four iterations and more are X <- (C2 C1) X with A <- C1 A C1 in between: the same with fewer operations.
  * Products are taken by the tensor cores on fp16 numbers with sums in fp32; X, A and C are held at powers of two that keep them in
- * fp16's range.  products = 1 rounds each of them to fp16: the update is off by about 1e-3 of its norm (an eighth of what bf16
- * would give).  products = 3 holds them as sums of two fp16 numbers and takes three products for each: off by 2e-6 to 2e-5, at
- * about three times the cost; for fp32 parameters that are compared with an fp32 step.  Norms are summed in binary64.  No
+ * fp16's range.  products = 1 rounds each of them to fp16 (an eighth of bf16's roundings): the update is off by about 1e-3 of its norm
+ * where singular values are of one size, by 2e-3 for a few directions over noise of their size, and by 1e-2 to 9e-2 where the noise is a
+ * hundredth or less, since the iterations raise what was rounded as they raise the noise.  products = 3 holds them as sums of two
+ * fp16 numbers and takes three products for each: off by 2e-6 to 6e-6, and by 1e-5 to 1e-4 for such noise, one to two times what
+ * fp32 products leave, at about three times the cost; for fp32 and fp16 parameters that are compared with an fp32 step.  (Iterations
+ * beyond five raise all of these further.)  Norms are summed in binary64.  No
  * floating-point atomics: results repeat bit for bit.  A NaN or an infinity in a gradient makes its whole matrix NaN, and no
  * other.  A matrix of zeros has the update zero.
  *
@@ -497,7 +500,7 @@ typedef struct qsr_muon_config {
 } qsr_muon_config;
 
 /* Bytes of device workspace for matrices of these sizes (host arrays): about 4 bytes an element with one product, 8 with three,
- * plus up to two and a half times as much for the square of the shorter side.  Negative qsr_status on error. */
+ * plus up to twice as much for the square of the shorter side.  Negative qsr_status on error. */
 int64_t qsr_muon_workspace_bytes(const int64_t *rows_host, const int64_t *cols_host, int32_t n_matrices, int32_t workers, int32_t products);
 
 /* Makes a list over caller-owned matrices; arguments, stream, workspace and refusals as at qsr_list_create.  The workspace belongs

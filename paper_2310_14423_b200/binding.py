@@ -633,7 +633,8 @@ class MuonList:
     params / grads / copies: lists of contiguous 2-D CUDA tensors in float32, bfloat16 or float16 (grads and copies may be None, or
     None in places); momentum: float32; with several workers, worker 0's matrices first, then worker 1's, and so on.
     wd_scale, update_scale: factors on the weight decay and on the update per matrix (default: 1, and sqrt(max(1, rows / columns))).
-    products: 1 (fp16) or 3 (nearly fp32).  workspace: a CUDA tensor of qsr_muon_workspace_bytes bytes.  Keeps references to the
+    products: 1 (fp16: right for bf16 parameters) or 3 (nearly fp32, at three times the cost; for fp32 and fp16 parameters whose
+    steps are compared with fp32 ones); include/qsr.h has the errors.  workspace: a CUDA tensor of qsr_muon_workspace_bytes bytes.  Keeps references to the
     tensors whose memory the library borrows; streams and lifetimes as at TensorList."""
 
     def __init__(self, params, grads, momentum, copies=None, wd_scale=None, update_scale=None, workers: int = 1, beta: float = 0.95,

@@ -59,16 +59,17 @@ int64_t half_tiles(int64_t mb, int64_t width)
 }
 int64_t whole_tiles(int64_t rb, int64_t cb, int64_t width) { return ceil_div(rb, 4) * ceil_div(cb, width); }
 
-// Iterations whose products of X and C are saved.  X_k = P_k X with symmetric m x m matrices that are all polynomials of A: C_k' = C_k ... C_j,
-// and A_(k+1) = C_k A_k C_k.  With the last r iterations on these alone, m x m x m products take the place of 2 (r - 1) with m x m x n: for
-// five iterations and r = 3, in units of m^3 and with n = rho m, 10 rho + 15 instead of 17 rho + 7.  The first iterations stay products with
-// X, because A holds small singular values by their squares: after two of them the rounding of A no longer shows (the update is as
-// near to the formula's as with r = 0 on matrices of low rank over noise, and loses an order of magnitude with one iteration less).
-// From rho = 2 on: six 1024 x 2048 take 298 us against 322 with r = 0 (three products: 652 and 737), eight 1024 x 1280 406 against 387
-// (831 and 844), and ViT-B/16's list, whose three matrices in four have rho of 3 or 4, 1307 against 1646 (3208 and 3960).
-int64_t short_iterations(const Sides &s, int32_t iterations) { return s.nb >= 2 * s.mb && iterations >= 4 ? std::min(3, iterations - 2) : 0; }
-// Symmetric matrices that a matrix needs: A and C, or A, C A, two of C and their product.
-int64_t squares(int64_t r) { return r ? 5 : 2; }
+// Iterations at the end whose products of X and C are saved.  X_k = P_k X with symmetric m x m matrices that are all polynomials of A:
+// C' = C_last C_(last-1), and A_last = C A C.  With the last two iterations on these alone, four m x m x m products (three of them with A
+// and C) take the place of one A = X X^T and one C X.  No more than two, because A holds small singular values by their squares: of 300 x 577
+// matrices of rank 20, 60 and 100 over noise of 0.01, the update by one product is 3.6e-2, 2.0e-2 and 1.4e-2 off (of its norm), as with all
+// iterations on X, and 5.9e-2, 4.6e-2 and 3.4e-2 with the last three on A; by three products 2.8e-5, 1.6e-5 and 1.1e-5 (1 to 1.4 times what fp32
+// products leave), and 7.0e-5, 4.6e-5 and 3.4e-5.  From n = 2 m on: six 1024 x 2048 take 333 us against 347 with all iterations on
+// X, two 2048 x 8192 860 to 900 against 953 (three products: 2600 and 3000), ViT-B/16's list, whose three matrices in four have n = 3 m or 4 m,
+// 1305 against 1395 to 1440 (3460 to 3530 and 3800).
+int64_t short_iterations(const Sides &s, int32_t iterations) { return s.nb >= 2 * s.mb && iterations >= 4 ? 2 : 0; }
+// Symmetric matrices that a matrix needs: A and C, or A, C, C A and the last C.
+int64_t squares(int64_t r) { return r ? 4 : 2; }
 
 // Columns of a tile, in blocks: two instead of four where that ends earlier on `pairs` pairs of multiprocessors.  A narrow tile takes
 // about 0.65 of a wide one's time (its products take half, but it copies three quarters as much).  Two workers' ragged list, 1023 x 2047
@@ -97,32 +98,22 @@ public:
             const Operand l = y.tall ? whole(from, false) : half(c), right = y.tall ? half(c) : whole(from, true);      // X C, or C X
             slots_[size_t(slot)].push_back(Product{l, right, x[from ^ 1], 0, y.rb, y.cb, mb, false, factor});
         };
-        const int32_t a = square[0], ca = square[2];
-        int32_t c = square[1], spare = r ? square[3] : 0, product = 0, free = r ? square[4] : 0;
+        const int32_t a = square[0], c = square[1], ca = square[2], last = square[3];
         int now = 0;
-        float scale = kMuonFactorScale;               // that `product` is held at: its entries grow by up to 3.45 with each C
         for (int32_t k = 0; k < iterations_; ++k) {
             const int slot = 3 * k;
+            const int32_t factor = k > first_short ? last : c;
             if (k <= first_short) slots_[size_t(slot)].push_back(Product{whole(now, y.tall), whole(now, y.tall), a, 0, mb, mb, y.nb, true, to_gram});
             else square_product(slot, c, ca, a, keep);                                   // A <- C (C A)
-            if (k > first_short) std::swap(c, spare);                                      // the last C may still be wanted
-            slots_[size_t(slot + 1)].push_back(Product{half(a), half(a), c, a, mb, mb, mb, true, kMuonC * kMuonFactorScale / (kMuonGramScale * kMuonGramScale)});
+            slots_[size_t(slot + 1)].push_back(Product{half(a), half(a), factor, a, mb, mb, mb, true, kMuonC * kMuonFactorScale / (kMuonGramScale * kMuonGramScale)});
             if (k < first_short) {
                 iterate(slot + 2, now, c, keep);
                 now ^= 1;
-                continue;
-            }
-            if (k + 1 < iterations_) square_product(slot + 2, c, a, ca, keep);            // C A
-            if (k == first_short) product = c;
-            else {                                                                       // C_k ... C_first
-                const int32_t to = k == first_short + 1 ? free : spare;
-                square_product(slot + 2, c, product, to, 0.25f * keep);
-                scale *= 0.25f;
-                product = to;
-            }
+            } else if (k == first_short) square_product(slot + 2, c, a, ca, keep);        // C A
+            else square_product(slot + 2, last, c, a, 0.25f * keep);                     // the last C times this one, up to 3.45^2, where A was
         }
         if (r) {
-            iterate(3 * iterations_, now, product, 1.0f / scale);
+            iterate(3 * iterations_, now, a, 4.0f * keep);
             now ^= 1;
         }
         return now;
@@ -206,7 +197,7 @@ Layout layout_of(const int64_t *rows, const int64_t *cols, int32_t n, int32_t wo
         }
         const int64_t r = short_iterations(s, iterations), half = half_tiles(s.mb, 2), whole = std::max(whole_tiles(s.mb, s.nb, 2), whole_tiles(s.nb, s.mb, 2));
         l.n_blocks += s.mb * s.nb;
-        l.n_tiles += iterations * (2 * half + whole) + (r ? 4 * half + whole : 0);       // room for tiles of either width
+        l.n_tiles += iterations * (2 * half + whole) + (r ? 2 * half : 0);               // room for tiles of either width
         data += (2 * s.mb * s.nb + squares(r) * s.mb * s.mb) * parts * kBlockBytes;
     }
     l.n_sync = 2 * l.n_param_sync;
@@ -363,7 +354,7 @@ int create(qsr_muon **out, const qsr_muon_config &cfg, const qsr_matrix *t, void
             continue;
         }
         const int64_t r = short_iterations(s, cfg.iterations);
-        int32_t whole[2], square[5] = {0, 0, 0, 0, 0};
+        int32_t whole[2], square[4] = {0, 0, 0, 0};
         uint16_t *iterate[2];
         for (int k = 0; k < 2; ++k) {
             whole[k] = int32_t((at - (ws + l.data)) / kBlockBytes);

@@ -462,3 +462,47 @@ def test_the_size_of_a_gradient_does_not_matter(shape, products):
         results.append(p)
     assert not torch.equal(results[0], theta)
     assert all(torch.equal(r, results[0]) for r in results)
+
+
+def plain64(u, iterations):
+    X = u / torch.linalg.vector_norm(u)
+    X = X.T if u.shape[0] > u.shape[1] else X
+    for _ in range(iterations):
+        A = X @ X.T
+        X = a * X + (b * A + c * A @ A) @ X
+    return X.T if u.shape[0] > u.shape[1] else X
+
+
+def held64(u, iterations):
+    """The iterations in binary64 with X, A and C in fp16, all of them on X."""
+    held = lambda M, at: (M * at).half().double() / at                 # noqa: E731
+    X = u / torch.linalg.vector_norm(u)
+    X = X.T if u.shape[0] > u.shape[1] else X
+    m, n = X.shape
+    scale, eye = 2.0 ** min(15, math.floor(0.5 * math.log2(m * n))), torch.eye(m, device=DEV, dtype=torch.float64)
+    X = held(X, scale)
+    for _ in range(iterations):
+        A = held(X @ X.T, 2.0 ** 14)
+        X = held(held(a * eye + b * A + c * A @ A, 2.0 ** 14) @ X, scale)
+    return X.T if u.shape[0] > u.shape[1] else X
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape,iterations,rank", [((300, 900), 5, 20), ((900, 300), 5, 3), ((300, 577), 5, 60), ((300, 577), 5, 100), ((256, 1024), 6, 20), ((700, 1500), 5, 0),
+                                                   ((130, 2000), 5, 10), ((130, 2000), 4, 3), ((150, 600), 4, 40), ((300, 576), 5, 60)])
+def test_long_matrices_are_as_near_as_others(shape, iterations, rank, products):
+    """Low rank over weak noise, whose small singular values five iterations raise by hundreds, and with them whatever was rounded.  The last
+    iterations of long matrices go through A, which holds those values by their squares; that may not show.  With one product the roundings
+    are those of the iterations on X in fp16 (emulated here; another set of them gives within a few per cent the same), and three
+    more of A and C: half as much again is allowed, and as much again with four iterations, which raise small values less and so
+    leave these a larger share.  With three products they are 2^-22 instead of fp32's 2^-24: four times what fp32 products leave."""
+    u = spread(shape, rank, 11)
+    p, m = torch.zeros(shape, device=DEV), torch.zeros(shape, device=DEV)
+    ws = torch.empty(B.qsr_muon_workspace_bytes([shape], 1, products), dtype=torch.uint8, device=DEV)
+    x = B.MuonList([p], [u], [m], beta=0.0, nesterov=False, eps=0.0, iterations=iterations, products=products, update_scale=[1.0], workspace=ws, stream=stream())
+    x.qsr_muon_step(1.0)
+    x.qsr_muon_check()
+    want = plain64(u.double(), iterations)
+    off = lambda X: float(torch.linalg.vector_norm(X.double() - want) / torch.linalg.vector_norm(want))       # noqa: E731
+    limit = (1.5 if iterations > 4 else 2.0) * off(held64(u.double(), iterations)) if products == 1 else 4.0 * off(plain64(u, iterations))
+    assert off(-p) <= limit
