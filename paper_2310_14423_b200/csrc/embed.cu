@@ -401,12 +401,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     __shared__ float shared[8][kJoinThreads];
     // The sorted keys are those of the launch before the one before, which had ended before that one let this one start: what there is
     // to join is found out while the sums are still being taken.  They are read from the second-level cache, where that launch left them.
-    // Blocks without anything to join wait too: a launch none of whose blocks waits may end before the sums are written, and whatever is
-    // ordered behind this launch alone (the next node of a graph, say) would not find them.
+    // The first block waits also where it has nothing to join: a launch none of whose blocks waits may end before the sums are written, and
+    // whatever is ordered behind this launch alone (the next node of a graph, say) would not find them.  The others need not: they would
+    // stand in the sums' way (131072 x 128 bf16 of 1000 tokens 48 us instead of 44).
     const int64_t c = int64_t(blockIdx.x), begin = c * p.chunk, end = begin + p.chunk;
     const uint32_t none = uint32_t(p.vocab), token = end < p.n ? __ldcg(p.keys + end - 1) : none;
     if (token == none || __ldcg(p.keys + end) != token || (begin > 0 && __ldcg(p.keys + begin) == token && __ldcg(p.keys + begin - 1) == token)) {
-        wait_for_launch_before();
+        if (blockIdx.x == 0) wait_for_launch_before();
         return;
     }
     const int lanes = p.join_lanes, ways = kJoinThreads / lanes, lane = int(threadIdx.x) & (lanes - 1), way = int(threadIdx.x) / lanes;
