@@ -258,3 +258,23 @@ def test_sorted_gradient_in_a_graph_before_a_copy(R, V, N, accumulate):
             want[t[some]] += 0.5 * d[some].float()
             graph.replay()
             assert torch.equal(copy, want) and torch.equal(g, want)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_rows_beyond_32_bits(accumulate):
+    """Looked-up rows of more than 2^31 elements; of the gradient, which sorts them, those with a token are the last ones."""
+    R, V, N = (1 << 21) + 1001, 4000, 1024
+    w = torch.randn(V, N, device=DEV, generator=gen(1)).bfloat16()
+    t = torch.full((R,), -1, device=DEV)
+    t[-3000:] = torch.randint(0, V, (3000,), device=DEV, generator=gen(2))
+    y = torch.empty(R, N, device=DEV, dtype=torch.bfloat16)
+    B.qsr_embed(w, t, y, stream=stream())
+    assert torch.equal(y[-3000:], w[t[-3000:]]) and not y[0].any() and not y[R // 2].any() and not y[-3001].any()
+    y[:-3000] = math.nan                                              # of rows without a token nothing is added
+    g = torch.randn(V, N, device=DEV, generator=gen(3))
+    want = (g.double() if accumulate else torch.zeros(V, N, device=DEV, dtype=torch.float64)).index_add_(0, t[-3000:], y[-3000:].double())
+    size = (g.double().abs() if accumulate else torch.zeros_like(want)).index_add_(0, t[-3000:], y[-3000:].double().abs())
+    ws = torch.empty(B.qsr_embed_workspace_bytes(R, V, N), dtype=torch.uint8, device=DEV)
+    B.qsr_embed_grad(y, t, g, accumulate=accumulate, workspace=ws, stream=stream())
+    count = torch.bincount(t[-3000:], minlength=V).double()[:, None]
+    assert not ((g.double() - want).abs() > (count + 10) * U * size).any()

@@ -110,3 +110,33 @@ def test_backward_over_several_rows_each(R, N, how, kind, wkind):
     clean = torch.arange(R, device=DEV) != row
     assert torch.equal(dx2[clean], dx[clean]) and torch.isnan(dx2[row]).all()
     assert torch.isnan(dw2[N - 1]) and torch.equal(dw2[:N - 1], dw[:N - 1]) and torch.equal(db2, db)
+
+
+@pytest.mark.parametrize("R,N,stride", [((1 << 21) + 1001, 760, 1032), (300_001, 8184, 8192), (66_001, 33000, 33001)])
+def test_offsets_beyond_32_bits(R, N, stride):
+    """Matrices of more than 2^31 elements: their last rows are what they are by themselves (the warps, blocks and sums that take them
+    are others, but a row's arithmetic is the same)."""
+    last = 700
+    x, dy, w, b = inputs(last, N, "bf16", "f32", 5)
+    big = lambda: torch.empty(R * stride, device=DEV, dtype=torch.bfloat16).as_strided((R, N), (stride, 1))        # noqa: E731
+    xs, out = big(), big()
+    xs.zero_()
+    xs[-last:] = x
+    mean, rstd = torch.empty(R, device=DEV), torch.empty(R, device=DEV)
+    B.qsr_layer_norm(xs, out, weight=w, bias=b, mean=mean, rstd=rstd, eps=EPS, stream=stream())
+    m64, r64, y64, dm, dr, tol = forward64(x, w, b)
+    close(mean[-last:], m64[:, 0], dm[:, 0] + U * m64[:, 0].abs())
+    close(rstd[-last:], r64[:, 0], dr[:, 0])
+    close(out[-last:], y64, rounded(tol, y64, "bf16"))
+    assert torch.equal(out[0], b.bfloat16()) and torch.equal(out[R // 2], b.bfloat16())
+    dys = xs                                                          # gradients by themselves: x and d_y may be one matrix
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    ws = torch.empty(B.qsr_layer_norm_workspace_bytes(R, N), dtype=torch.uint8, device=DEV)
+    B.qsr_layer_norm_grad(xs, dys, mean, rstd, d_x=out, weight=w, d_weight=dw, d_bias=db, workspace=ws, stream=stream())
+    dx64, dw64, db64, tx, _, _ = backward64(x, x, mean[-last:], rstd[-last:], w)
+    close(out[-last:], dx64, rounded(tx, dx64, "bf16"))
+    hat = (x.double() - mean[-last:].double()[:, None]) * rstd[-last:].double()[:, None]
+    depth = last + 512 + 26                                           # all other rows add zeros
+    close(dw, dw64, rounded((depth + 3) * U * (x.double() * hat).abs().sum(0), dw64, "f32"))
+    close(db, db64, rounded(depth * U * x.double().abs().sum(0), db64, "f32"))
+    assert not out[0].any() and not out[R // 2].any()
