@@ -516,8 +516,9 @@ int qsr_muon_destroy(qsr_muon *muon);
 int qsr_muon_set_grads(qsr_muon *muon, const void *const *grads_host);
 
 /* One step of every matrix.  QSR_ESTATE: no gradients set, or another device than the list's is current.  One launch
- * for all matrices that one multiprocessor holds (up to 128 x 512), and for all others 3 + 3 * iterations, or one more, whatever
- * their number; asynchronous.  It may be captured; lr and grad_scale are then those of the capture. */
+ * for all matrices that one multiprocessor holds (up to 128 x 512 with one product, 128 x 256 or 64 x 512 with three), and for all others
+ * 3 + 3 * iterations, or one more, whatever their number; asynchronous.  It may be captured; lr and grad_scale are then those of the
+ * capture. */
 int qsr_muon_step(qsr_muon *muon, double lr, double grad_scale);
 
 /* End of a round over the list's K workers, as qsr_list_sync: every parameter becomes the mean (sum over k = 0..K-1 in fp32) / K;
@@ -580,7 +581,7 @@ int qsr_layer_norm_grad(const qsr_layer_norm_args *args, void *cuda_stream);
 /*
  * A model's input end: out[r] = scale * table[tokens[r]], and the gradient of the table, d_table[v] = scale * (sum of d_out[r] over
  * the rows r whose token is v).  Products and sums in fp32, one rounding at the end.  The rows of a token are added in an order
- * that depends on the tokens alone (no floating-point atomics), so that results repeat bit for bit.  A token < 0 marks a row
+ * that depends on the tokens and the matrices' sizes alone (no floating-point atomics), so that results repeat bit for bit.  A token < 0 marks a row
  * without one: zeros, no gradient.  A token >= vocab: NaN, no gradient.
  */
 typedef struct qsr_embed_args {

@@ -695,8 +695,8 @@ __global__ void __launch_bounds__(THREADS) backward_ring_kernel(const __grid_con
 }
 
 // Forward over many aligned rows, in the same way: blocks that stay, each thread with the weight and bias of its sixteen columns, so that a
-// row's exchanges are few beside its elements.  Mean and variance take two passes over the registers.  8192 x 4096 bf16: 30 us (4.5 TB/s) instead of
-// 37 with the first kernel above, 8192 x 5120 39 instead of 56, 4096 x 5120 fp32 31 instead of 35 (5.4 TB/s); eight columns a thread, two rows at a
+// row's exchanges are few beside its elements.  Mean and variance take two passes over the registers.  8192 x 4096 bf16: 31 us (4.4 TB/s) instead of
+// 37 with the first kernel above, 8192 x 5120 40 instead of 56, 4096 x 5120 fp32 31 instead of 35 (5.4 TB/s); eight columns a thread, two rows at a
 // time: 37.  Bound by instructions (widening, exchanges, the loop) beside the copies.  (Backward, sixteen columns a thread leave
 // too few warps: 64 us for 4099 x 5003 fp32 instead of 60, 73 for 8192 x 4096 bf16 instead of 56.)
 //
@@ -965,7 +965,7 @@ __global__ void __launch_bounds__(32 * kFinish) finish_kernel(const float *parti
 template <typename T, int HELD, bool VEC, bool FULL>
 int launch_held(const Params &p, int lanes, cudaStream_t st)
 {
-    // Warps that stay where each gets two rows and more: 12544 x 768 in bf16 takes 8.8 us, 14.4 with a warp for every row.
+    // Warps that stay where each gets two rows and more: 12544 x 768 in bf16 takes 9.4 us, 14.4 with a warp for every row.
     if (lanes <= 32 && p.rows >= int64_t(2) * kResident * (256 / lanes)) {
         forward_rows_kernel<T, HELD, VEC, FULL><<<unsigned(kResident), 256, 0, st>>>(p, lanes);
         return int(cudaGetLastError());
@@ -1010,7 +1010,7 @@ int launch_forward(const Params &p, cudaStream_t st)
 {
     if (VEC && p.granules > 32 * kMaxHeld && p.granules <= 2 * kMaxThreads) {
         const int lanes = (p.granules + 63) / 64 * 32, blocks = kBlocks * (kMaxThreads / std::max(128, power_of_two(lanes)));
-        // two rows and more for each block: 1200 x 4096 bf16 6.5 us against 8.7 below, 2400 x 2048 6.4 against 7.4; 600 x 2048 4.0 against 3.8
+        // two rows and more for each block: 1200 x 4096 bf16 6.9 us against 8.7 below, 2400 x 2048 6.7 against 7.4; 600 x 2048 4.0 against 3.8
         if (p.rows >= 2 * int64_t(blocks))
             return p.width % 8 == 0 ? launch_forward_ring<T, true>(p, lanes, st) : launch_forward_ring<T, false>(p, lanes, st);
     }

@@ -766,8 +766,8 @@ product_kernel(const __grid_constant__ MuonParams p, const __grid_constant__ Map
 
 // ---- small matrices --------------------------------------------------------------------------------------
 
-// A whole step of one matrix by one block: its shorter side is at most 128, its longer one at most 512, and X and A fit in shared memory,
-// where they stay through all iterations (C takes the place of A, every product that of its operand, once all sums are in tensor
+// A whole step of one matrix by one block: its shorter side is at most 128, its longer one at most 512 (with three products 256, or 512 for a
+// shorter side of 64), and X and A fit in shared memory, where they stay through all iterations (C takes the place of A, every product that of its operand, once all sums are in tensor
 // memory).  The general way takes a launch for every product, whatever its size: 115 us for four of 128 x 128, 25 us this way, of which
 // fifteen products take 1.3 us each: one after the other, copies in and out of tensor memory included, and far from its rate.
 constexpr int kSmallThreads = 512;

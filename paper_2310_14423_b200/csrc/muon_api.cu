@@ -73,7 +73,7 @@ int64_t squares(int64_t r) { return r ? 4 : 2; }
 
 // Columns of a tile, in blocks: two instead of four where that ends earlier on `pairs` pairs of multiprocessors.  A narrow tile takes
 // about 0.65 of a wide one's time (its products take half, but it copies three quarters as much).  Two workers' ragged list, 1023 x 2047
-// the largest, takes 426 us by this rule, 490 with wide tiles alone and 429 with narrow ones; ViT-B/16's bf16 list 1347, 1353 and 1681.
+// the largest, takes 446 us by this rule, 517 with wide tiles alone and 452 with narrow ones; ViT-B/16's bf16 list 1444, 1444 and 1804.
 int32_t tile_width(int64_t wide, int64_t narrow, int64_t pairs) { return ceil_div(narrow, pairs) * 65 < ceil_div(wide, pairs) * 100 ? 2 : 4; }
 
 // The products of a step.  Three slots an iteration -- A, C, and what takes C -- and one more for matrices whose last iterations are short.
