@@ -506,3 +506,42 @@ def test_long_matrices_are_as_near_as_others(shape, iterations, rank, products):
     off = lambda X: float(torch.linalg.vector_norm(X.double() - want) / torch.linalg.vector_norm(want))       # noqa: E731
     limit = (1.5 if iterations > 4 else 2.0) * off(held64(u.double(), iterations)) if products == 1 else 4.0 * off(plain64(u, iterations))
     assert off(-p) <= limit
+
+
+def cut64(u, iterations):
+    """The iterations in binary64 with X, A and C as sums of two fp16 numbers, and every product too small by what three products may cut off at
+    most: all errors in one direction, whereas those of the kernels fall both ways where sums are rounded."""
+    def held(M, at):
+        hi = (M * at).half().double()
+        return (hi + (M * at - hi).half().double()) / at
+
+    def product(L, R):
+        P = L @ R
+        return P - torch.sign(P) * (12 * 2.0 ** -23 + (L.shape[1] / 64 + 2) * 2.0 ** -24 + 2.0 ** -22) * (L.abs() @ R.abs())
+
+    X = u / torch.linalg.vector_norm(u)
+    X = X.T if u.shape[0] > u.shape[1] else X
+    m, n = X.shape
+    scale, eye = 2.0 ** min(15, math.floor(0.5 * math.log2(m * n))), torch.eye(m, device=DEV, dtype=torch.float64)
+    X = held(X, scale)
+    for _ in range(iterations):
+        A = held(product(X, X.T), 2.0 ** 14)
+        X = held(product(held(a * eye + b * A + c * product(A, A), 2.0 ** 14), X), scale)
+    return X.T if u.shape[0] > u.shape[1] else X
+
+
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("shape,iterations", [((1500, 700), 16), ((128, 128), 16), ((700, 900), 12), ((300, 900), 9)])
+def test_many_iterations(shape, iterations, products):
+    """The polynomial does not converge, so that each iteration raises what was rounded before: compared with the same roundings in binary64 (half
+    as much again, since others than those give within a few per cent the same), or with the most that can be cut off."""
+    u = spread(shape, 0, 13)
+    p, m = torch.zeros(shape, device=DEV), torch.zeros(shape, device=DEV)
+    ws = torch.empty(B.qsr_muon_workspace_bytes([shape], 1, products), dtype=torch.uint8, device=DEV)
+    x = B.MuonList([p], [u], [m], beta=0.0, nesterov=False, eps=0.0, iterations=iterations, products=products, update_scale=[1.0], workspace=ws, stream=stream())
+    x.qsr_muon_step(1.0)
+    x.qsr_muon_check()
+    want = plain64(u.double(), iterations)
+    off = lambda X: float(torch.linalg.vector_norm(X.double() - want) / torch.linalg.vector_norm(want))       # noqa: E731
+    limit = 1.5 * off(held64(u.double(), iterations)) if products == 1 else off(cut64(u.double(), iterations))
+    assert off(-p) <= limit < 0.05
